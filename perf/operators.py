@@ -167,7 +167,7 @@ def _clip_inputs(case, seed):
         buf.normal_(0.0, 0.02 * (1 + i % 5), generator=g)
         grads.append(buf[off:])
         expected += n * (0.02 * (1 + i % 5)) ** 2
-    return {"grads": grads, "max_norm": math.sqrt(expected) * (0.25 if case["clips"] else 16.0)}
+    return {"grads": grads, "max_norm": math.sqrt(expected) * (0.3 if case["clips"] else 16.0)}
 
 
 def _inputs(case, seed):

@@ -179,6 +179,9 @@ def prepare(case, seed):
     s["case"] = case
     if case["op"] == "clip":                                                # the optimizer's copy: one buffer for each type
         s["flat"], s["out"] = _flat(s["grads"])
+        if own:
+            from paper_2508_21613_amd import operators as ops
+            s["list"] = ops.Gradients(s["grads"], s["out"])                 # the buffers stay where they are from step to step
     return s
 
 
@@ -273,9 +276,7 @@ def _plain_clip(s):
 
 
 def _own_clip(s):
-    from paper_2508_21613_amd import operators as ops
-    norm = ops.clip_gradients(s["grads"], s["max_norm"], out=s["out"])
-    return {"norm": norm, "grads": s["flat"]}
+    return {"norm": s["list"].clip(s["max_norm"]), "grads": s["flat"]}
 
 
 def run(state):

@@ -19,7 +19,9 @@ INFEASIBLE = (1 << 63) - 1
 SYMBOLS = ["chm_load_scenario", "chm_plan_space", "chm_score_plans", "chm_score_ranks", "chm_search_best", "chm_search_best_static", "chm_search_best_batch", "chm_kernel_selection", "chm_halves_selection", "chm_halves_work_of", "chm_set_halves_shares",
            "chm_search_range", "chm_search_ranks", "chm_search_cuts", "chm_rank_partitions", "chm_decode_plan", "chm_set_timing", "chm_set_filter_compaction", "chm_set_bounded_search", "chm_get_timing", "chm_family_classes",
            "chm_reroute_shape", "chm_transfer_plan", "chm_replan", "chm_replan_table", "chm_compare_objective", "chm_valu_probe", "chm_free_scenario",
-           "chm_strerror"]
+           "chm_strerror",
+           "chm_ffn_sizes", "chm_ffn_forward", "chm_ffn_backward", "chm_embedding_lookup", "chm_embedding_gradient_scratch", "chm_embedding_gradient",
+           "chm_load_gradients", "chm_gradient_sumsq", "chm_clip_gradients", "chm_free_gradients"]
 
 
 class Desc(C.Structure):
@@ -89,6 +91,25 @@ class Timing(C.Structure):
                 ("evaluated", C.c_uint64 * 3)]
 
 
+class Ffn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("activation", C.c_int32),
+                ("tokens", C.c_int64), ("width", C.c_int64), ("features", C.c_int64),
+                ("x", C.c_void_p), ("w_gate", C.c_void_p), ("w_up", C.c_void_p), ("w_down", C.c_void_p),
+                ("ld_x", C.c_int64), ("ld_gate", C.c_int64), ("ld_up", C.c_int64), ("ld_down", C.c_int64),
+                ("saved", C.c_void_p)]
+
+
+class FfnGradients(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("dx", C.c_void_p),
+                ("dw_gate", C.c_void_p), ("dw_up", C.c_void_p), ("dw_down", C.c_void_p),
+                ("ld_dy", C.c_int64), ("ld_dx", C.c_int64), ("ld_dw_gate", C.c_int64), ("ld_dw_up", C.c_int64), ("ld_dw_down", C.c_int64),
+                ("grad_dtype", C.c_int32), ("accumulate", C.c_int32)]
+
+
+class Gradient(C.Structure):
+    _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
+
+
 class ChmError(RuntimeError):
     def __init__(self, code, msg=""):
         super().__init__("libchm error %d: %s" % (code, msg))
@@ -142,12 +163,24 @@ def lib():
         L.chm_replan_table.argtypes = [C.POINTER(ReplanDesc), C.c_int32, C.POINTER(ReplanPlan), vp]
         L.chm_compare_objective.argtypes = [C.c_int64] * 5
         L.chm_valu_probe.argtypes = [C.c_int32, C.c_uint32, C.POINTER(C.c_double), vp]
+        i32, i64, u64 = C.c_int32, C.c_int64, C.c_uint64
+        L.chm_ffn_sizes.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), C.POINTER(u64), C.POINTER(u64), C.POINTER(u64)]
+        L.chm_ffn_forward.argtypes = [C.POINTER(Ffn), vp, i64, vp, u64, vp]
+        L.chm_ffn_backward.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), vp, u64, vp]
+        L.chm_embedding_lookup.argtypes = [i32, i32, vp, i64, vp, i64, i64, i64, C.c_float, vp, i64, vp]
+        L.chm_embedding_gradient_scratch.argtypes = [i64, i64, C.POINTER(u64)]
+        L.chm_embedding_gradient.argtypes = [i32, i32, i32, vp, i64, vp, i64, i64, i64, C.c_float, vp, i64, i32, vp, u64, vp]
+        L.chm_load_gradients.argtypes = [C.POINTER(Gradient), i32, C.POINTER(vp)]
+        L.chm_gradient_sumsq.argtypes = [vp, vp, vp]
+        L.chm_clip_gradients.argtypes = [vp, C.c_float, vp, vp, vp]
+        L.chm_free_gradients.argtypes = [vp]
+        L.chm_free_gradients.restype = None
         L.chm_free_scenario.argtypes = [vp]
         L.chm_free_scenario.restype = None
         L.chm_strerror.argtypes = [C.c_int]
         L.chm_strerror.restype = C.c_char_p
         for n in SYMBOLS:
-            if n not in ("chm_free_scenario", "chm_strerror"):
+            if n not in ("chm_free_scenario", "chm_free_gradients", "chm_strerror"):
                 getattr(L, n).restype = C.c_int
         _lib = L
     return _lib

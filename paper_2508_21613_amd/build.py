@@ -25,11 +25,15 @@ LIB = os.path.join(HERE, "libchm_san.so" if SANITIZE else "libchm.so")
 HOST_SANITIZE = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined", "-Xarch_host", "-fno-omit-frame-pointer",
                  "-Xarch_host", "-g"]
 SOURCES = ["chm_host.cpp", "chm_pool.cpp", "chm_kernels.hip", "chm_fast.hip", "chm_search_s0.hip", "chm_search_s1.hip", "chm_search_s2.hip", "chm_families_8.hip",
-           "chm_families_12.hip", "chm_families_16.hip", "chm_families_24.hip", "chm_window.hip", "chm_list.hip", "chm_replan.hip", "chm_probe.hip"]
-# no device code meets a NaN: a maximum of floats is one instruction then, not one more for each operand that might be one;
-# packed-FP32 instruction selection is switched off for all device code; so is the vectorizer of straight-line code, which
+           "chm_families_12.hip", "chm_families_16.hip", "chm_families_24.hip", "chm_window.hip", "chm_list.hip", "chm_replan.hip", "chm_probe.hip",
+           "chm_ffn.hip", "chm_ffn_bf16.hip", "chm_ffn_f16.hip", "chm_embedding.hip", "chm_clip.hip"]
+# the operators of a training step: their values may be infinite or not a number, and pass through as such
+FLOAT_SOURCES = ("chm_ffn.hip", "chm_ffn_bf16.hip", "chm_ffn_f16.hip", "chm_embedding.hip", "chm_clip.hip")
+NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
+# no device code of the search meets a NaN (NO_NANS): a maximum of floats is one instruction then, not one more for each operand
+# that might be one; packed-FP32 instruction selection is switched off for all device code; so is the vectorizer of straight-line code, which
 # finds nothing to gain in integer kernels and puts arrays it has half packed into scratch
-FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-slp-vectorize", "-Xarch_device", "-fno-honor-nans",
+FLAGS = ["--offload-arch=gfx950", "-O3", "-std=c++17", "-fPIC", "-fno-slp-vectorize",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-Wall", "-Wno-unused-command-line-argument"]
 
 
@@ -49,7 +53,7 @@ def build(verbose=True, changed_only=False):
         objs.append(obj)
         fresh = os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src), newest_header)
         if not (changed_only and fresh):
-            todo.append(["hipcc"] + FLAGS + (HOST_SANITIZE if SANITIZE else []) + ["-x", "hip", "-c", src, "-o", obj])
+            todo.append(["hipcc"] + FLAGS + ([] if s in FLOAT_SOURCES else NO_NANS) + (HOST_SANITIZE if SANITIZE else []) + ["-x", "hip", "-c", src, "-o", obj])
 
     def run(cmd):
         if verbose:

@@ -1,0 +1,668 @@
+// Embedding lookup with scaling, and its gradient by sorted tokens.
+//
+// Lookup: out[t] = s W[tok t]; a copy of rows, bound by memory (or by one memory latency for a few tokens).
+//
+// Gradient: dW[v] = s sum_{t: tok t = v} dY[t].  The (token, place) pairs are sorted by token, stably, so that every row's sum is
+// taken in the order of places without atomics on floats: the result does not change from call to call.  A token's run may be
+// anything from one place to all of them (text holds its most frequent token in some ten percent of the places), so the sorted
+// list is cut into pieces of equal length: a group of threads sums up one piece, stores runs that lie inside it, and leaves the
+// float32 sums of runs that cross its ends (two at most) for a second launch, which adds them in order.  Rows that no token
+// names are set to zero by further workgroups of the same launch, which look them up in the sorted list: the dense gradient is written
+// once.  Up to 256 places (a few sequences' ends, a probe) nothing is sorted: every workgroup finds the places of its token itself.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "chm_elements.h"
+
+namespace {
+
+using namespace chm_elements;
+
+constexpr int NT = 256;
+constexpr int SMALL = 256;               // places the unsorted kernel takes
+constexpr int ONE_GROUP = 16384;         // places one workgroup sorts in its shared memory (128 KiB of pairs)
+constexpr int BINS = 512, DIGIT = 9;
+constexpr int SORT_GROUPS = 64;
+constexpr int ZERO_ROWS = 32;            // rows that a workgroup sets to zero where no token names them
+
+struct Tokens {
+  const void *p;
+  int32_t bits;
+  uint32_t rows;
+};
+// the token of place i as a key: `rows` for one outside the table, behind all others
+__device__ __forceinline__ uint32_t key_of(const Tokens &t, int64_t i) {
+  if (t.bits == 32) {
+    const uint32_t v = ((const CHM_GLOBAL uint32_t *)t.p)[i];
+    return v < t.rows ? v : t.rows;
+  }
+  const uint64_t v = ((const CHM_GLOBAL uint64_t *)t.p)[i];
+  return v < t.rows ? (uint32_t)v : t.rows;
+}
+
+// ---------------------------------------------------------------------------------------------- rows in pieces of 16 bytes
+// `count` (<= N) values of a row as float32; the rest 0
+template <int DT>
+__device__ __forceinline__ void row_load(const char *p, int count, float *v) {
+  typedef Lane<DT> L;
+  if (count >= L::N) {
+    L::up(load16(p), v);
+  } else {
+#pragma unroll
+    for (int e = 0; e < L::N; ++e) v[e] = e < count ? L::one(p + e * L::SIZE) : 0.f;
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void row_store(char *p, int count, const float *v) {
+  typedef Lane<DT> L;
+  if (count >= N) {
+#pragma unroll
+    for (int i = 0; i < N / L::N; ++i) store16(p + i * 16, L::down(v + i * L::N));
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < count) L::put(p + e * L::SIZE, v[e]);
+  }
+}
+template <int DT, int N>
+__device__ __forceinline__ void row_add(char *p, int count, float *v) {
+  typedef Lane<DT> L;
+  if (count >= N) {
+#pragma unroll
+    for (int i = 0; i < N / L::N; ++i) {
+      float old[L::N];
+      L::up(load16(p + i * 16), old);
+#pragma unroll
+      for (int e = 0; e < L::N; ++e) v[i * L::N + e] += old[e];
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < N; ++e)
+      if (e < count) v[e] += L::one(p + e * L::SIZE);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- lookup
+struct Lookup {
+  Tokens tokens;
+  const char *table;
+  char *out;
+  int64_t n, ld_table, ld_out;           // rows in bytes
+  int32_t width, across;                 // threads along a row
+  float scale;
+};
+
+template <int DT, int ROWS>
+__global__ void __launch_bounds__(NT) k_lookup(Lookup c) {
+  typedef Lane<DT> L;
+  const int x = threadIdx.x % c.across, y = threadIdx.x / c.across, down = NT / c.across;
+  const int col = (blockIdx.y * c.across + x) * L::N, left = c.width - col;
+  if (left <= 0) return;
+  const int64_t first = (int64_t)blockIdx.x * down * ROWS + y;
+  float v[ROWS][8];
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t t = first + (int64_t)r * down;
+    const uint32_t key = t < c.n ? key_of(c.tokens, t) : c.tokens.rows;
+    if (key < c.tokens.rows) {
+      row_load<DT>(c.table + key * c.ld_table + (int64_t)col * L::SIZE, left, v[r]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < L::N; ++e) v[r][e] = 0.f;
+    }
+#pragma unroll
+    for (int e = 0; e < L::N; ++e) v[r][e] = key < c.tokens.rows ? v[r][e] * c.scale : 0.f;
+  }
+#pragma unroll
+  for (int r = 0; r < ROWS; ++r) {
+    const int64_t t = first + (int64_t)r * down;
+    if (t < c.n) row_store<DT, L::N>(c.out + t * c.ld_out + (int64_t)col * L::SIZE, left, v[r]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- sort
+// Stable sort by digits of at most 9 bits.  Lanes of a wavefront that hold the same digit find each other by ballots; a
+// wavefront's items keep their order, wavefronts take consecutive items.
+__device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits) {
+  uint64_t m = ~0ull;
+  for (int b = 0; b < bits; ++b) {
+    const uint64_t set = __ballot((d >> b) & 1);
+    m &= (d >> b) & 1 ? set : ~set;
+  }
+  return m;
+}
+
+// One workgroup, n <= 16,384: the pairs stay in shared memory.
+__global__ void __launch_bounds__(1024) k_sort_one(Tokens tokens, int n, int passes, int digit, uint32_t *keys, uint32_t *places) {
+  __shared__ uint32_t lk[ONE_GROUP], lp[ONE_GROUP];
+  __shared__ __attribute__((aligned(16))) uint16_t counts[BINS * 16];
+  __shared__ uint32_t totals[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int rounds = (n + 1023) / 1024, first = wave * rounds * 64;
+  uint32_t key[16], place[16], rank[16];
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int i = first + r * 64 + lane;
+    key[r] = r < rounds && i < n ? key_of(tokens, i) : ~0u;       // behind everything
+    place[r] = i;
+  }
+  for (int pass = 0; pass < passes; ++pass) {
+    const int shift = pass * digit;
+    const uint32_t mask = (1u << digit) - 1;
+    *(Words *)(counts + threadIdx.x * 8) = Words{0, 0, 0, 0};
+    __syncthreads();
+    volatile uint16_t *mine = counts + wave;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if (r >= rounds) continue;
+      const uint32_t d = (key[r] >> shift) & mask;
+      const uint64_t m = same_digit(d, digit);
+      const uint32_t before = mine[d * 16];
+      rank[r] = before + __popcll(m & ((1ull << lane) - 1));
+      __builtin_amdgcn_wave_barrier();
+      if ((m >> lane) == 1) mine[d * 16] = (uint16_t)(before + __popcll(m));   // the group's last lane
+      __builtin_amdgcn_wave_barrier();
+    }
+    __syncthreads();
+    // exclusive sums over (digit, wavefront), 8 entries a thread
+    uint32_t c[8], sum = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { c[e] = counts[threadIdx.x * 8 + e]; sum += c[e]; }
+    uint32_t incl = sum;
+#pragma unroll
+    for (int d = 1; d < 64; d <<= 1) {
+      const uint32_t o = __shfl_up(incl, d);
+      if (lane >= d) incl += o;
+    }
+    if (lane == 63) totals[wave] = incl;
+    __syncthreads();
+    uint32_t at = incl - sum;
+    for (int w = 0; w < wave; ++w) at += totals[w];
+#pragma unroll
+    for (int e = 0; e < 8; ++e) { counts[threadIdx.x * 8 + e] = (uint16_t)at; at += c[e]; }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if (r >= rounds) continue;
+      const uint32_t to = counts[((key[r] >> shift) & mask) * 16 + wave] + rank[r];
+      lk[to] = key[r];
+      lp[to] = place[r];
+    }
+    __syncthreads();
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      if (r >= rounds) continue;
+      key[r] = lk[first + r * 64 + lane];
+      place[r] = lp[first + r * 64 + lane];
+    }
+    __syncthreads();
+  }
+#pragma unroll
+  for (int r = 0; r < 16; ++r) {
+    const int i = first + r * 64 + lane;
+    if (r < rounds && i < n) { keys[i] = key[r]; places[i] = place[r]; }
+  }
+}
+
+// Many workgroups: per pass, the digits of every workgroup's stretch are counted, then its pairs are moved
+struct SortPass {
+  Tokens tokens;                          // first pass: keys come from here, places are the indices
+  const uint32_t *keys_in, *places_in;    // null in the first pass
+  uint32_t *keys, *places, *counts;       // counts: [workgroup][BINS]
+  int64_t n;
+  int32_t stretch, shift, digit;          // stretch: items of a workgroup, a multiple of 512
+};
+constexpr int SORT_NT = 512;
+
+__device__ __forceinline__ uint32_t pass_key(const SortPass &c, int64_t i) { return c.keys_in ? c.keys_in[i] : key_of(c.tokens, i); }
+
+__global__ void __launch_bounds__(SORT_NT) k_sort_count(SortPass c) {
+  __shared__ uint32_t counts[BINS];
+  counts[threadIdx.x] = 0;
+  __syncthreads();
+  const int64_t first = (int64_t)blockIdx.x * c.stretch, last = first + c.stretch < c.n ? first + c.stretch : c.n;
+  const uint32_t mask = (1u << c.digit) - 1;
+  for (int64_t i = first + threadIdx.x; i < last; i += SORT_NT) atomicAdd(&counts[(pass_key(c, i) >> c.shift) & mask], 1u);
+  __syncthreads();
+  c.counts[(int64_t)blockIdx.x * BINS + threadIdx.x] = counts[threadIdx.x];
+}
+
+__global__ void __launch_bounds__(SORT_NT) k_sort_move(SortPass c) {
+  constexpr int WAVES = SORT_NT / 64;
+  __shared__ uint32_t counts[BINS * WAVES];
+  __shared__ uint32_t totals[WAVES];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint32_t mask = (1u << c.digit) - 1;
+  const int64_t first = (int64_t)blockIdx.x * c.stretch + (int64_t)wave * (c.stretch / WAVES);
+  const int64_t end = first + c.stretch / WAVES, last = end < c.n ? end : c.n;
+  for (int i = threadIdx.x; i < BINS * WAVES; i += SORT_NT) counts[i] = 0;
+  __syncthreads();
+  for (int64_t i = first + lane; i < last; i += 64) atomicAdd(&counts[((pass_key(c, i) >> c.shift) & mask) * WAVES + wave], 1u);
+  // where this workgroup's items of digit threadIdx.x start: all smaller digits, and this one in the workgroups before
+  uint32_t all = 0, before = 0;
+  for (uint32_t g = 0; g < gridDim.x; ++g) {
+    const uint32_t v = c.counts[(int64_t)g * BINS + threadIdx.x];
+    if (g < blockIdx.x) before += v;
+    all += v;
+  }
+  uint32_t incl = all;
+#pragma unroll
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
+  }
+  if (lane == 63) totals[wave] = incl;
+  __syncthreads();
+  uint32_t at = incl - all + before;
+  for (int w = 0; w < wave; ++w) at += totals[w];
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    const uint32_t v = counts[threadIdx.x * WAVES + w];
+    counts[threadIdx.x * WAVES + w] = at;
+    at += v;
+  }
+  __syncthreads();
+  volatile uint32_t *mine = counts + wave;
+  for (int64_t i0 = first; i0 < end; i0 += 64) {
+    const int64_t i = i0 + lane;
+    const bool in = i < last;
+    const uint32_t key = in ? pass_key(c, i) : 0;
+    const uint32_t place = in ? (c.places_in ? c.places_in[i] : (uint32_t)i) : 0;
+    const uint32_t d = (key >> c.shift) & mask;
+    const uint64_t m = same_digit(d, c.digit) & __ballot(in);
+    const uint32_t base = mine[d * WAVES];
+    __builtin_amdgcn_wave_barrier();
+    if (in) {
+      if ((m >> lane) == 1) mine[d * WAVES] = base + __popcll(m);
+      const uint32_t to = base + __popcll(m & ((1ull << lane) - 1));
+      c.keys[to] = key;
+      c.places[to] = place;
+    }
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- sums over runs
+struct Gather {
+  Tokens tokens;
+  const uint32_t *keys, *places;         // sorted
+  const char *dy;
+  char *grad;
+  float *part;                           // [pieces][2][width rounded up to 8]
+  int64_t n, ld_dy, ld_grad;             // rows in bytes
+  int32_t width, across, piece, pieces;
+  int32_t piece_groups;                  // workgroups (along x) that take pieces; the ones behind set rows to zero
+  int32_t accumulate;
+  float scale;
+};
+
+template <int GT, int N>
+__device__ __forceinline__ void finish_row(const Gather &c, uint32_t key, int col, int left, float *v) {
+  char *p = c.grad + key * c.ld_grad + (int64_t)col * Lane<GT>::SIZE;
+#pragma unroll
+  for (int e = 0; e < N; ++e) v[e] *= c.scale;
+  if (c.accumulate) row_add<GT, N>(p, left, v);
+  row_store<GT, N>(p, left, v);
+}
+
+__device__ __forceinline__ int64_t part_row(const Gather &c, int64_t piece, int slot) {
+  return (piece * 2 + slot) * ((c.width + 7) & ~7);
+}
+
+// first place in the sorted list whose key is not below `key`
+__device__ __forceinline__ int64_t lower_bound(const uint32_t *keys, int64_t n, uint32_t key) {
+  int64_t lo = 0, hi = n;
+  while (lo < hi) {
+    const int64_t mid = (lo + hi) >> 1;
+    if (keys[mid] < key) lo = mid + 1; else hi = mid;
+  }
+  return lo;
+}
+
+// rows [first, first + ZERO_ROWS) without a token, of which `named` knows
+template <int GT>
+__device__ __forceinline__ void zero_rows(const Gather &c, int64_t first, const uint8_t *named) {
+  constexpr int N = Lane<GT>::N;
+  const float zero[N] = {};
+  const int groups = (c.width + N - 1) / N;
+  for (int i = threadIdx.x; i < ZERO_ROWS * groups; i += NT) {
+    const int r = i / groups, col = (i - r * groups) * N;
+    if (!named[r]) row_store<GT, N>(c.grad + (first + r) * c.ld_grad + (int64_t)col * Lane<GT>::SIZE, c.width - col, zero);
+  }
+}
+
+template <int DT, int GT>
+__global__ void __launch_bounds__(NT) k_runs(Gather c) {
+  typedef Lane<DT> L;
+  constexpr int N = L::N, AT_ONCE = 8;
+  __shared__ uint32_t lk[2048], lp[2048];        // NT / across pieces of at most 64 places, across >= 8
+  if ((int)blockIdx.x >= c.piece_groups) {
+    if (blockIdx.y) return;
+    __shared__ uint8_t named[ZERO_ROWS];
+    const int64_t first = (int64_t)(blockIdx.x - c.piece_groups) * ZERO_ROWS;
+    if (threadIdx.x < ZERO_ROWS) {
+      const int64_t r = first + threadIdx.x;
+      uint8_t there = 1;
+      if (r < c.tokens.rows) {
+        const int64_t at = lower_bound(c.keys, c.n, (uint32_t)r);
+        there = at < c.n && c.keys[at] == (uint32_t)r;
+      }
+      named[threadIdx.x] = there;
+    }
+    __syncthreads();
+    zero_rows<GT>(c, first, named);
+    return;
+  }
+  const int x = threadIdx.x % c.across, y = threadIdx.x / c.across, down = NT / c.across;
+  const int64_t group_first = (int64_t)blockIdx.x * down * c.piece;
+  for (int i = threadIdx.x; i < down * c.piece; i += NT)
+    if (group_first + i < c.n) { lk[i] = c.keys[group_first + i]; lp[i] = c.places[group_first + i]; }
+  __syncthreads();
+  const int64_t piece = (int64_t)blockIdx.x * down + y, lo = piece * c.piece;
+  const int col = (blockIdx.y * c.across + x) * N, left = c.width - col;
+  if (piece >= c.pieces || left <= 0) return;
+  const int count = c.n - lo < c.piece ? (int)(c.n - lo) : c.piece;
+  const uint32_t *k = lk + y * c.piece, *p = lp + y * c.piece;
+  const uint32_t before = lo > 0 ? c.keys[lo - 1] : ~0u, behind = lo + count < c.n ? c.keys[lo + count] : ~0u;
+  const char *dy = c.dy + (int64_t)col * L::SIZE;
+  float sum[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.f;
+  bool started = k[0] != before;
+  for (int i0 = 0; i0 < count; i0 += AT_ONCE) {
+    float v[AT_ONCE][N];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u < count ? i0 + u : count - 1;
+      if (k[i] < c.tokens.rows) row_load<DT>(dy + p[i] * c.ld_dy, left, v[u]);
+    }
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      const int i = i0 + u;
+      if (i >= count || k[i] >= c.tokens.rows) break;
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] += v[u][e];
+      const uint32_t next = i + 1 < count ? k[i + 1] : behind;
+      if (next == k[i] && i + 1 < count) continue;
+      if (next != k[i] && started) {
+        finish_row<GT, N>(c, k[i], col, left, sum);
+      } else {
+        float *to = c.part + part_row(c, piece, started) + col;
+#pragma unroll
+        for (int e = 0; e < N; e += 4) *(Words *)(to + e) = Lane<CHM_F32>::down(sum + e);
+      }
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] = 0.f;
+      started = true;
+    }
+  }
+}
+
+// runs that cross pieces: the piece in which one starts adds up what the others have left, in order
+template <int GT>
+__global__ void __launch_bounds__(NT) k_join(Gather c) {
+  constexpr int N = 4, AT_ONCE = 8;
+  const int x = threadIdx.x % c.across, y = threadIdx.x / c.across, down = NT / c.across;
+  const int64_t piece = (int64_t)blockIdx.x * down + y;
+  const int col = (blockIdx.y * c.across + x) * N, left = c.width - col;
+  if (piece + 1 >= c.pieces || left <= 0) return;
+  const int64_t lo = piece * c.piece, hi = lo + c.piece;
+  const uint32_t key = c.keys[hi - 1];
+  if (key >= c.tokens.rows || key != c.keys[hi]) return;
+  if (c.keys[lo] == key && lo > 0 && c.keys[lo - 1] == key) return;       // it has come from before
+  const int64_t last = (lower_bound(c.keys + hi, c.n - hi, key + 1) + hi - 1) / c.piece;
+  float sum[N];
+  Lane<CHM_F32>::up(*(const Words *)(c.part + part_row(c, piece, 1) + col), sum);
+  for (int64_t q0 = piece + 1; q0 <= last; q0 += AT_ONCE) {
+    Words w[AT_ONCE];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) w[u] = *(const Words *)(c.part + part_row(c, q0 + u < last ? q0 + u : last, 0) + col);
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (q0 + u > last) break;
+      float v[N];
+      Lane<CHM_F32>::up(w[u], v);
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] += v[e];
+    }
+  }
+  // float32 rows are 16 bytes of 4 columns, 16-bit rows 8 bytes: stored one by one where N columns are no 16 bytes
+  char *to = c.grad + key * c.ld_grad + (int64_t)col * Lane<GT>::SIZE;
+#pragma unroll
+  for (int e = 0; e < N; ++e) {
+    if (e >= left) break;
+    float v = sum[e] * c.scale;
+    if (c.accumulate) v += Lane<GT>::one(to + e * Lane<GT>::SIZE);
+    Lane<GT>::put(to + e * Lane<GT>::SIZE, v);
+  }
+}
+
+// n <= 256: workgroup (t, columns) sums up the places of the token at t if t is its first; the ones behind set rows to zero
+template <int DT, int GT>
+__global__ void __launch_bounds__(NT) k_few(Gather c) {
+  typedef Lane<DT> L;
+  constexpr int N = L::N, AT_ONCE = 8;
+  __shared__ uint32_t keys[SMALL];
+  __shared__ uint16_t list[SMALL + AT_ONCE];
+  const int n = (int)c.n;
+  const uint32_t own = (int)threadIdx.x < n ? key_of(c.tokens, threadIdx.x) : ~0u;
+  keys[threadIdx.x] = own;
+  if ((int)blockIdx.x >= n) {
+    if (blockIdx.y) return;
+    __shared__ uint8_t named[ZERO_ROWS];
+    const int64_t first = (int64_t)(blockIdx.x - n) * ZERO_ROWS;
+    if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x >= c.tokens.rows;
+    __syncthreads();
+    if (own < c.tokens.rows && own >= first && own < first + ZERO_ROWS) named[own - first] = 1;
+    __syncthreads();
+    zero_rows<GT>(c, first, named);
+    return;
+  }
+  __shared__ int counts[NT / 64];
+  __syncthreads();
+  const uint32_t key = keys[blockIdx.x];
+  const bool match = own == key;
+  const uint64_t m = __ballot(match);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane == 0) counts[wave] = __popcll(m);
+  __syncthreads();
+  int at = __popcll(m & ((1ull << lane) - 1)), total = 0;
+  for (int w = 0; w < NT / 64; ++w) {
+    if (w < wave) at += counts[w];
+    total += counts[w];
+  }
+  if (match) list[at] = (uint16_t)threadIdx.x;
+  __syncthreads();
+  if (key >= c.tokens.rows || list[0] != blockIdx.x) return;
+  const int col = (blockIdx.y * NT + threadIdx.x) * N, left = c.width - col;
+  if (left <= 0) return;
+  float sum[N];
+#pragma unroll
+  for (int e = 0; e < N; ++e) sum[e] = 0.f;
+  for (int i0 = 0; i0 < total; i0 += AT_ONCE) {
+    float v[AT_ONCE][N];
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u)
+      if (i0 + u < total) row_load<DT>(c.dy + list[i0 + u] * c.ld_dy + (int64_t)col * L::SIZE, left, v[u]);
+#pragma unroll
+    for (int u = 0; u < AT_ONCE; ++u) {
+      if (i0 + u >= total) break;
+#pragma unroll
+      for (int e = 0; e < N; ++e) sum[e] += v[u][e];
+    }
+  }
+  finish_row<GT, N>(c, key, col, left, sum);
+}
+
+// ---------------------------------------------------------------------------------------------- host side
+int size_of(int dtype) { return dtype == CHM_F32 ? 4 : 2; }
+bool known(int dtype) { return dtype == CHM_F32 || dtype == CHM_BF16 || dtype == CHM_F16; }
+
+// threads along a row of `groups` 16-byte groups: a power of two from 8 to 256
+int across_of(int64_t groups) {
+  int a = 8;
+  while (a < NT && a < groups) a <<= 1;
+  return a;
+}
+
+// places of a piece: about 1,024 pieces and more, 8 to 64 places each
+int piece_of(int64_t n) {
+  int p = 8;
+  while (p < 64 && n / p > 1024) p <<= 1;
+  return p;
+}
+
+struct Scratch { uint64_t keys[2], places[2], counts, part, bytes; };
+
+Scratch scratch_of(int64_t n, int64_t width) {
+  Scratch s{};
+  if (n <= SMALL) return s;
+  uint64_t at = 0;
+  const auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) & ~255ull; return o; };
+  const int sets = n > ONE_GROUP ? 2 : 1;
+  for (int i = 0; i < sets; ++i) { s.keys[i] = take(n * 4); s.places[i] = take(n * 4); }
+  if (sets == 2) s.counts = take((uint64_t)SORT_GROUPS * BINS * 4);
+  const int64_t pieces = (n + piece_of(n) - 1) / piece_of(n);
+  s.part = take((uint64_t)pieces * 2 * ((width + 7) & ~7ll) * 4);
+  s.bytes = at;
+  return s;
+}
+
+template <int DT, int GT>
+bool launch_few(const Gather &c, hipStream_t st) {
+  const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
+  const int cols = (c.width + NT * Lane<DT>::N - 1) / (NT * Lane<DT>::N);
+  if (c.n + zero) hipLaunchKernelGGL((k_few<DT, GT>), dim3((uint32_t)(c.n + zero), cols), dim3(NT), 0, st, c);
+  return hipGetLastError() == hipSuccess;
+}
+
+template <int DT, int GT>
+bool launch_runs(Gather c, hipStream_t st) {
+  int64_t groups = (c.width + Lane<DT>::N - 1) / Lane<DT>::N;
+  c.across = across_of(groups);
+  int down = NT / c.across;
+  c.piece_groups = (c.pieces + down - 1) / down;
+  const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
+  hipLaunchKernelGGL((k_runs<DT, GT>), dim3((uint32_t)(c.piece_groups + zero), (uint32_t)((groups + c.across - 1) / c.across)), dim3(NT), 0, st, c);
+  groups = (c.width + 3) / 4;
+  c.across = across_of(groups);
+  down = NT / c.across;
+  hipLaunchKernelGGL((k_join<GT>), dim3((uint32_t)((c.pieces + down - 1) / down), (uint32_t)((groups + c.across - 1) / c.across)), dim3(NT), 0, st, c);
+  return hipGetLastError() == hipSuccess;
+}
+
+template <int DT>
+bool launch_lookup(Lookup c, hipStream_t st) {
+  const int64_t groups = (c.width + Lane<DT>::N - 1) / Lane<DT>::N;
+  c.across = across_of(groups);
+  const uint32_t cols = (uint32_t)((groups + c.across - 1) / c.across);
+  const int down = NT / c.across;
+  if (c.n >= 4096) hipLaunchKernelGGL((k_lookup<DT, 4>), dim3((uint32_t)((c.n + 4 * down - 1) / (4 * down)), cols), dim3(NT), 0, st, c);
+  else hipLaunchKernelGGL((k_lookup<DT, 1>), dim3((uint32_t)((c.n + down - 1) / down), cols), dim3(NT), 0, st, c);
+  return hipGetLastError() == hipSuccess;
+}
+
+bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
+
+}  // namespace
+
+extern "C" int chm_embedding_lookup(int32_t dtype, int32_t index_bits, const void *tokens, int64_t n, const void *table,
+                                    int64_t ld_table, int64_t rows, int64_t width, float scale, void *out, int64_t ld_out,
+                                    void *hip_stream) {
+  if (!known(dtype) || (index_bits != 32 && index_bits != 64) || n < 0 || n > INT32_MAX || rows < 0 || rows > INT32_MAX || width < 1 ||
+      width > (1 << 24) || ld_table < width || ld_out < width || ld_table > INT32_MAX || ld_out > INT32_MAX)
+    return CHM_ERR_ARG;
+  const int size = size_of(dtype);
+  if (!aligned(tokens, index_bits / 8) || !aligned(table, size) || !aligned(out, size)) return CHM_ERR_ARG;
+  if (n == 0) return CHM_OK;
+  if (!tokens || !out || (rows > 0 && !table)) return CHM_ERR_ARG;
+  Lookup c{};
+  c.tokens = Tokens{tokens, index_bits, (uint32_t)rows};
+  c.table = (const char *)table;
+  c.out = (char *)out;
+  c.n = n;
+  c.ld_table = ld_table * size;
+  c.ld_out = ld_out * size;
+  c.width = (int32_t)width;
+  c.scale = scale;
+  hipStream_t st = (hipStream_t)hip_stream;
+  const bool ok = dtype == CHM_F32 ? launch_lookup<CHM_F32>(c, st) : dtype == CHM_BF16 ? launch_lookup<CHM_BF16>(c, st) : launch_lookup<CHM_F16>(c, st);
+  return ok ? CHM_OK : CHM_ERR_HIP;
+}
+
+extern "C" int chm_embedding_gradient_scratch(int64_t n, int64_t width, uint64_t *bytes) {
+  if (!bytes || n < 0 || n > INT32_MAX || width < 1 || width > (1 << 24)) return CHM_ERR_ARG;
+  *bytes = scratch_of(n, width).bytes;
+  return CHM_OK;
+}
+
+extern "C" int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t index_bits, const void *tokens, int64_t n, const void *dy,
+                                      int64_t ld_dy, int64_t rows, int64_t width, float scale, void *grad, int64_t ld_grad,
+                                      int32_t accumulate, void *scratch, uint64_t scratch_bytes, void *hip_stream) {
+  if (!known(dtype) || (grad_dtype != dtype && grad_dtype != CHM_F32) || (index_bits != 32 && index_bits != 64) || n < 0 || n > INT32_MAX ||
+      rows < 0 || rows > INT32_MAX || width < 1 || width > (1 << 24) || ld_dy < width || ld_grad < width || ld_dy > INT32_MAX ||
+      ld_grad > INT32_MAX)
+    return CHM_ERR_ARG;
+  if (!aligned(tokens, index_bits / 8) || !aligned(dy, size_of(dtype)) || !aligned(grad, size_of(grad_dtype)) || !aligned(scratch, 16))
+    return CHM_ERR_ARG;
+  if (rows == 0) return CHM_OK;
+  if (!grad || (n > 0 && (!tokens || !dy))) return CHM_ERR_ARG;
+  const Scratch s = scratch_of(n, width);
+  if (s.bytes && !scratch) return CHM_ERR_ARG;
+  if (scratch_bytes < s.bytes) return CHM_ERR_LIMIT;
+  hipStream_t st = (hipStream_t)hip_stream;
+  char *mem = (char *)scratch;
+  Gather c{};
+  c.tokens = Tokens{tokens, index_bits, (uint32_t)rows};
+  c.dy = (const char *)dy;
+  c.grad = (char *)grad;
+  c.n = n;
+  c.ld_dy = ld_dy * size_of(dtype);
+  c.ld_grad = ld_grad * size_of(grad_dtype);
+  c.width = (int32_t)width;
+  c.accumulate = accumulate != 0;
+  c.scale = scale;
+  if (n > SMALL) {
+    int bits = 0;
+    while (bits < 32 && (uint64_t)rows >> bits) ++bits;                  // keys 0 .. rows
+    const int passes = (bits + DIGIT - 1) / DIGIT, digit = (bits + passes - 1) / passes;
+    uint32_t *keys = (uint32_t *)(mem + s.keys[0]), *places = (uint32_t *)(mem + s.places[0]);
+    if (n <= ONE_GROUP) {
+      hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(1024), 0, st, c.tokens, (int)n, passes, digit, keys, places);
+    } else {
+      SortPass p{};
+      p.tokens = c.tokens;
+      p.counts = (uint32_t *)(mem + s.counts);
+      p.n = n;
+      int64_t stretch = (n + SORT_GROUPS - 1) / SORT_GROUPS;
+      if (stretch < 4096) stretch = 4096;
+      stretch = (stretch + 511) & ~511ll;
+      p.stretch = (int32_t)stretch;
+      p.digit = digit;
+      const uint32_t groups = (uint32_t)((n + stretch - 1) / stretch);
+      for (int pass = 0; pass < passes; ++pass) {
+        const int to = (passes - 1 - pass) & 1;                          // the last pass ends in the first set
+        p.keys_in = pass ? (uint32_t *)(mem + s.keys[to ^ 1]) : nullptr;
+        p.places_in = pass ? (uint32_t *)(mem + s.places[to ^ 1]) : nullptr;
+        p.keys = (uint32_t *)(mem + s.keys[to]);
+        p.places = (uint32_t *)(mem + s.places[to]);
+        p.shift = pass * digit;
+        hipLaunchKernelGGL(k_sort_count, dim3(groups), dim3(SORT_NT), 0, st, p);
+        hipLaunchKernelGGL(k_sort_move, dim3(groups), dim3(SORT_NT), 0, st, p);
+      }
+    }
+    c.keys = keys;
+    c.places = places;
+    c.part = (float *)(mem + s.part);
+    c.piece = piece_of(n);
+    c.pieces = (int32_t)((n + c.piece - 1) / c.piece);
+  }
+  const bool few = n <= SMALL;
+  bool ok;
+  if (dtype == CHM_F32) ok = few ? launch_few<CHM_F32, CHM_F32>(c, st) : launch_runs<CHM_F32, CHM_F32>(c, st);
+  else if (dtype == CHM_BF16 && grad_dtype == CHM_F32) ok = few ? launch_few<CHM_BF16, CHM_F32>(c, st) : launch_runs<CHM_BF16, CHM_F32>(c, st);
+  else if (dtype == CHM_BF16) ok = few ? launch_few<CHM_BF16, CHM_BF16>(c, st) : launch_runs<CHM_BF16, CHM_BF16>(c, st);
+  else if (grad_dtype == CHM_F32) ok = few ? launch_few<CHM_F16, CHM_F32>(c, st) : launch_runs<CHM_F16, CHM_F32>(c, st);
+  else ok = few ? launch_few<CHM_F16, CHM_F16>(c, st) : launch_runs<CHM_F16, CHM_F16>(c, st);
+  return ok ? CHM_OK : CHM_ERR_HIP;
+}

@@ -1,0 +1,40 @@
+// Layout of one matrix product of the gated feed-forward block and the launch interface between its host part
+// (chm_operators.cpp) and its kernels.  Internal to libchm.
+#ifndef CHM_FFN_H
+#define CHM_FFN_H
+#include <stdint.h>
+
+#include "../../include/chm_operators.h"
+
+// An operand of C[m, n] = sum_k A[m, k] B[n, k]: its base (two bases: two weights side by side, or two runs of k one behind the
+// other), elements from one row of memory to the next, length of a run of k.  Elements of 16 bits, 16-byte aligned rows.
+struct GemmOperand { const void *p[2]; int64_t ld, k; };
+
+struct GemmCall {
+  GemmOperand a, b;
+  int64_t m, n;                 // sizes of the product (n: features of one weight in a two-weight product)
+  int32_t tiles_m, tiles_n;
+  int32_t steps, steps_seg;     // steps of 64 sums over all, steps of the first run of k
+  int32_t splits;               // > 1: the sums are split over blockIdx.y, float32 parts go to `part`
+  int32_t act;
+  // plain store: c[0] for rows below m_first, c[1] (row m - m_first) from there on; rows up to m_real, columns up to n_real
+  void *c[2];
+  int64_t ldc;
+  int64_t m_first, m_real, n_real;
+  int32_t f32_out, accumulate, wide;      // wide: 16-byte stores are possible
+  float *part;                  // [splits][m][ld_part]
+  int64_t ld_part;              // columns rounded up to 8
+  // two-weight product and gradient of the activation: internal buffers of `ldi` elements a row
+  uint16_t *h, *gate, *up;
+  uint16_t *dgate, *dup;
+  int64_t ldi, ldd;             // ldd: row of dgate / dup
+};
+
+enum { GEMM_GATE_UP = 0, GEMM_OUT = 1, GEMM_DH = 2, GEMM_DX = 3, GEMM_DW = 4 };
+enum { TILE_256 = 0, TILE_128 = 1 };
+// Largest row of memory (elements) that the tile kernels take: 256 rows lie within 2^31 bytes.  Longer ones are packed.
+constexpr int64_t GEMM_LD_MAX = 1 << 21;
+// Launches one product; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.
+bool gemm_launch_bf16(int product, int tile, const GemmCall &c, void *stream);
+bool gemm_launch_f16(int product, int tile, const GemmCall &c, void *stream);
+#endif

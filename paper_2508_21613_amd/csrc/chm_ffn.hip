@@ -1,0 +1,452 @@
+// Gated feed-forward block: what its passes consist of, the kernels for few tokens, the packing of unaligned operands, the entry points.
+//
+//   forward    h = act(x Wg^T) * (x Wu^T)      one product with two weights, activation and product in its epilogue
+//              y = h Wd^T
+//   backward   dh = dy Wd, and in its epilogue  h = act(g) u,  du = dh act(g),  dg = dh u act'(g)
+//              dx = [dg du] [Wg; Wu]            one product over 2 F sums
+//              [dWg; dWu] = [dg du]^T x         one product with 2 F rows
+//              dWd = dy^T h
+// All of them are bound by the matrix cores for a micro-batch of tokens (chm_gemm.h) and by reading the weights for a few.
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "chm_elements.h"
+#include "chm_gemm.h"
+
+namespace {
+
+using namespace chm_elements;
+using chm_gemm::f4;
+using chm_gemm::s8;
+
+// ---------------------------------------------------------------------------------------------- few tokens
+// A wavefront takes 16 features (rows of a weight) and a share of the sums, and reads its part of the weight straight into
+// the first operand of the matrix instructions: every byte of a weight is read once, by one wavefront, 64 contiguous bytes a
+// lane quad and step.  The tokens (16 for each instruction, absent ones are zero and not loaded) come from the cache.  The
+// wavefronts of a workgroup share the sums and add them up through shared memory, in order.  Weights may start anywhere.
+constexpr int FEW_MAX = 64;
+
+struct FewCall {
+  const uint16_t *x, *w0, *w1;
+  int64_t ldx, ld0, ld1;
+  uint16_t *out, *gate, *up;
+  int64_t ldo, lds;
+  int32_t tokens, rows, k, act;
+};
+
+// 8 elements at k of a row of `n`, zeros beyond
+__device__ __forceinline__ s8 take8(const uint16_t *row, int k, int n) {
+  if (k + 8 <= n) return __builtin_bit_cast(s8, load16((const char *)(row + k)));
+  s8 v = {};
+#pragma unroll
+  for (int e = 0; e < 8; ++e)
+    if (k + e < n) v[e] = (short)((const CHM_GLOBAL uint16_t *)row)[k + e];
+  return v;
+}
+
+template <class T, int TWO, int TILES>
+__global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
+  extern __shared__ float part[];             // [wavefronts][TWO + 1][TILES][64][4]
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  const int q = lane >> 4, r = lane & 15;
+  const int f0 = blockIdx.x * 16, f = f0 + r < c.rows ? f0 + r : c.rows - 1;
+  const uint16_t *w0 = c.w0 + f * c.ld0, *w1 = TWO ? c.w1 + f * c.ld1 : nullptr;
+  f4 acc[2][TILES];
+#pragma unroll
+  for (int t = 0; t < TILES; ++t) acc[0][t] = acc[1][t] = f4{0.f, 0.f, 0.f, 0.f};
+
+  const auto step = [&](int k, bool whole) {
+    s8 a0[2], a1[2], b[TILES][2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = k + q * 16 + h * 8;
+      if (whole) {
+        a0[h] = __builtin_bit_cast(s8, load16((const char *)(w0 + at)));
+        if (TWO) a1[h] = __builtin_bit_cast(s8, load16((const char *)(w1 + at)));
+      } else {
+        a0[h] = take8(w0, at, c.k);
+        if (TWO) a1[h] = take8(w1, at, c.k);
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const int token = t * 16 + r;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = k + q * 16 + h * 8;
+        s8 v = {};
+        if (token < c.tokens) {
+          const uint16_t *x = c.x + token * c.ldx;
+          v = whole ? __builtin_bit_cast(s8, load16((const char *)(x + at))) : take8(x, at, c.k);
+        }
+        b[t][h] = v;
+      }
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        acc[0][t] = T::mfma(a0[h], b[t][h], acc[0][t]);
+        if (TWO) acc[1][t] = T::mfma(a1[h], b[t][h], acc[1][t]);
+      }
+  };
+  const int whole = c.k / 64;
+  int i = wave;
+  for (; i < whole; i += waves) step(i * 64, true);
+  if (i * 64 < c.k) step(i * 64, false);
+
+#pragma unroll
+  for (int t = 0; t < TILES; ++t)
+#pragma unroll
+    for (int w = 0; w <= TWO; ++w) *(f4 *)(part + ((((wave * (TWO + 1) + w) * TILES) + t) * 64 + lane) * 4) = acc[w][t];
+  __syncthreads();
+  // one value (pair) a thread: feature i % 16, token i / 16
+  for (int o = threadIdx.x; o < 256 * TILES; o += blockDim.x) {
+    const int feature = o & 15, token = o >> 4;
+    if (token >= c.tokens) continue;
+    if (f0 + feature >= c.rows) {             // kept projections have rows of whole words of 8, zeros behind
+      if (TWO && c.gate && f0 + feature < ((c.rows + 7) & ~7)) c.gate[token * c.lds + f0 + feature] = c.up[token * c.lds + f0 + feature] = 0;
+      continue;
+    }
+    const int at = ((token >> 4) * 64 + (feature >> 2) * 16 + (token & 15)) * 4 + (feature & 3);
+    float s0 = 0.f, s1 = 0.f;
+    for (int w = 0; w < waves; ++w) {
+      s0 += part[w * (TWO + 1) * TILES * 256 + at];
+      if (TWO) s1 += part[(w * (TWO + 1) + 1) * TILES * 256 + at];
+    }
+    const int64_t col = f0 + feature;
+    if (TWO) {
+      c.out[token * c.ldo + col] = T::down(chm_gemm::act_of(c.act, s0) * s1);
+      if (c.gate) {
+        c.gate[token * c.lds + col] = T::down(s0);
+        c.up[token * c.lds + col] = T::down(s1);
+      }
+    } else {
+      c.out[token * c.ldo + col] = T::down(s0);
+    }
+  }
+}
+
+// wavefronts of a workgroup: some 16 a compute unit over all, with four steps of 64 sums each at least
+int few_waves(int64_t rows, int64_t k) {
+  const int64_t groups = (rows + 15) / 16, steps = (k + 63) / 64;
+  int w = 1;
+  while (w < 16 && groups * w < 4096 && steps >= w * 8) w <<= 1;
+  return w;
+}
+
+template <class T, int TWO>
+bool launch_few(const FewCall &c, hipStream_t st) {
+  const dim3 grid((c.rows + 15) / 16);
+  const int w = few_waves(c.rows, c.k), tiles = c.tokens <= 16 ? 1 : c.tokens <= 32 ? 2 : 4;
+  const size_t bytes = (size_t)w * (TWO + 1) * tiles * 1024;
+  if (tiles == 1) hipLaunchKernelGGL((k_few_tokens<T, TWO, 1>), grid, dim3(w * 64), bytes, st, c);
+  else if (tiles == 2) hipLaunchKernelGGL((k_few_tokens<T, TWO, 2>), grid, dim3(w * 64), bytes, st, c);
+  else hipLaunchKernelGGL((k_few_tokens<T, TWO, 4>), grid, dim3(w * 64), bytes, st, c);
+  return hipGetLastError() == hipSuccess;
+}
+
+// ---------------------------------------------------------------------------------------------- packing
+// An operand whose rows do not start on 16 bytes or are no whole words of 8 elements is copied into rows that are, with zeros
+// behind: the copy costs its bytes twice, a product reads them some dozens of times.
+__global__ void __launch_bounds__(256) k_pack(const uint16_t *in, int64_t ld, int64_t rows, int cols, uint16_t *out, int64_t ld_out) {
+  const int words = (int)(ld_out / 8);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / words;
+    const int col = (int)(i - row * words) * 8;
+    *(s8 *)(out + row * ld_out + col) = take8(in + row * ld, col, cols);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- sums split over workgroups
+template <class T>
+__global__ void __launch_bounds__(256) k_join_parts(const float *part, int splits, int64_t rows, int64_t ld_part, int cols, uint16_t *out,
+                                                    int64_t ld_out) {
+  const int words = (int)(ld_part / 8);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
+    const int64_t row = i / words;
+    const int col = (int)(i - row * words) * 8;
+    const float *p = part + row * ld_part + col;
+    f4 a = *(const f4 *)p, b = *(const f4 *)(p + 4);
+    for (int s = 1; s < splits; ++s) {
+      p += rows * ld_part;
+      a += *(const f4 *)p;
+      b += *(const f4 *)(p + 4);
+    }
+    const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+    uint16_t *o = out + row * ld_out + col;
+    if (col + 8 <= cols) {
+      store16((char *)o, __builtin_bit_cast(Words, chm_gemm::pack8<T>(v)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (col + e < cols) o[e] = T::down(v[e]);
+    }
+  }
+}
+
+uint32_t copy_groups(int64_t words) {
+  const int64_t g = (words + 255) / 256;
+  return (uint32_t)(g < 1 ? 1 : g < 8192 ? g : 8192);
+}
+
+// ---------------------------------------------------------------------------------------------- passes
+int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
+
+struct Matrix { const void *p; int64_t ld, rows, cols; };
+
+bool needs_pack(const Matrix &m) { return (uintptr_t)m.p % 16 || m.ld % 8 || m.cols % 8 || m.ld > GEMM_LD_MAX; }
+
+// Hands out scratch, in a fixed order; with no base it only counts
+struct Arena {
+  char *base;
+  uint64_t used = 0;
+  void *take(uint64_t bytes) {
+    void *p = base ? base + used : nullptr;
+    used += (bytes + 255) & ~255ull;
+    return p;
+  }
+};
+
+struct Pass {
+  const chm_ffn *f;
+  Arena arena;
+  hipStream_t st;
+  bool run, ok = true;
+
+  Pass(const chm_ffn *f_, char *base, hipStream_t st_, bool run_) : f(f_), arena{base}, st(st_), run(run_) {}
+
+  // the matrix itself, or a packed copy of it
+  Matrix packed(const Matrix &m, bool must = false) {
+    if (!must && !needs_pack(m)) return m;
+    Matrix o{nullptr, up8(m.cols), m.rows, up8(m.cols)};
+    o.p = arena.take((uint64_t)o.rows * o.ld * 2);
+    if (run && m.rows) {
+      hipLaunchKernelGGL(k_pack, dim3(copy_groups(o.rows * (o.ld / 8))), dim3(256), 0, st, (const uint16_t *)m.p, m.ld, m.rows, (int)m.cols,
+                         (uint16_t *)o.p, o.ld);
+      ok = ok && hipGetLastError() == hipSuccess;
+    }
+    return o;
+  }
+  // two weights of one product: rows of equal length in memory
+  void packed_pair(Matrix &a, Matrix &b) {
+    const bool must = a.ld != b.ld && !(needs_pack(a) && needs_pack(b));
+    a = packed(a, must);
+    b = packed(b, must);
+  }
+
+  // Tile by the number of tiles (256 compute units take one of 256 x 256 or two of 128 x 128 at a time), and the sums split where even
+  // the small tiles leave compute units idle (`may_split`: the product has a plain 16-bit output of `n` columns)
+  void launch(int product, GemmCall &c, bool may_split) {
+    const int64_t n_all = product == GEMM_GATE_UP ? 2 * c.n : c.n;
+    const int64_t big = ((c.m + 255) / 256) * ((n_all + 255) / 256), small = ((c.m + 127) / 128) * ((n_all + 127) / 128);
+    const int tile = big >= 192 ? TILE_256 : TILE_128, side = tile == TILE_256 ? 256 : 128;
+    c.tiles_m = (int32_t)((c.m + side - 1) / side);
+    c.tiles_n = (int32_t)((n_all + side - 1) / side);
+    c.splits = 1;
+    if (may_split && tile == TILE_128) {
+      int64_t s = 512 / (small > 0 ? small : 1);
+      if (s > c.steps / 8) s = c.steps / 8;
+      if (s > 8) s = 8;
+      if (s > 1) {
+        c.splits = (int32_t)s;
+        c.ld_part = up8(c.n);
+        c.part = (float *)arena.take((uint64_t)s * c.m * c.ld_part * 4);
+      }
+    }
+    if (!run || c.m == 0) return;
+    c.act = f->activation;
+    ok = ok && (f->dtype == CHM_BF16 ? gemm_launch_bf16 : gemm_launch_f16)(product, tile, c, st);
+    if (c.splits > 1) {
+      const dim3 grid(copy_groups(c.m * (c.ld_part / 8)));
+      if (f->dtype == CHM_BF16)
+        hipLaunchKernelGGL((k_join_parts<chm_gemm::Bf16>), grid, dim3(256), 0, st, c.part, c.splits, c.m, c.ld_part, (int)c.n_real, (uint16_t *)c.c[0], c.ldc);
+      else
+        hipLaunchKernelGGL((k_join_parts<chm_gemm::F16>), grid, dim3(256), 0, st, c.part, c.splits, c.m, c.ld_part, (int)c.n_real, (uint16_t *)c.c[0], c.ldc);
+      ok = ok && hipGetLastError() == hipSuccess;
+    }
+  }
+
+  static void run_of_sums(GemmCall &c, int64_t k, int runs) {
+    c.steps_seg = (int32_t)((k + 63) / 64);
+    c.steps = c.steps_seg * runs;
+  }
+
+  void forward(void *y, int64_t ld_y) {
+    const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
+    uint16_t *gate = (uint16_t *)f->saved, *up = gate ? gate + T * F8 : nullptr;
+    uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
+    if (T <= FEW_MAX) {
+      if (!run || T == 0) return;
+      FewCall c{};
+      c.tokens = (int32_t)T;
+      c.act = f->activation;
+      c.x = (const uint16_t *)f->x; c.ldx = f->ld_x;
+      c.w0 = (const uint16_t *)f->w_gate; c.ld0 = f->ld_gate;
+      c.w1 = (const uint16_t *)f->w_up; c.ld1 = f->ld_up;
+      c.out = h; c.ldo = F8;
+      c.gate = gate; c.up = up; c.lds = F8;
+      c.rows = (int32_t)F; c.k = (int32_t)D;
+      ok = f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 1>(c, st) : launch_few<chm_gemm::F16, 1>(c, st);
+      FewCall d{};
+      d.tokens = (int32_t)T;
+      d.x = h; d.ldx = F8;
+      d.w0 = (const uint16_t *)f->w_down; d.ld0 = f->ld_down;
+      d.out = (uint16_t *)y; d.ldo = ld_y;
+      d.rows = (int32_t)D; d.k = (int32_t)F;
+      ok = ok && (f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 0>(d, st) : launch_few<chm_gemm::F16, 0>(d, st));
+      return;
+    }
+    const Matrix x = packed({f->x, f->ld_x, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
+    Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
+    packed_pair(wg, wu);
+    GemmCall c{};
+    c.a = GemmOperand{{x.p, x.p}, x.ld, x.cols};
+    c.b = GemmOperand{{wg.p, wu.p}, wg.ld, wg.cols};
+    c.m = T; c.n = F;
+    run_of_sums(c, x.cols, 1);
+    c.h = h; c.gate = gate; c.up = up; c.ldi = F8;
+    launch(GEMM_GATE_UP, c, false);
+    GemmCall d{};
+    d.a = GemmOperand{{h, h}, F8, F8};
+    d.b = GemmOperand{{wd.p, wd.p}, wd.ld, wd.cols};
+    d.m = T; d.n = D;
+    run_of_sums(d, F8, 1);
+    out(d, y, ld_y, D);
+    launch(GEMM_OUT, d, true);
+  }
+
+  // one 16-bit output of `cols` columns
+  void out(GemmCall &c, void *p, int64_t ld, int64_t cols) {
+    c.c[0] = c.c[1] = p;
+    c.ldc = ld;
+    c.m_first = c.m_real = c.m;
+    c.n_real = cols;
+    c.wide = (uintptr_t)p % 16 == 0 && ld % 8 == 0;
+  }
+
+  void backward(const chm_ffn_gradients *g) {
+    const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
+    uint16_t *gate = (uint16_t *)f->saved, *up = gate + T * F8;
+    uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2), *d = (uint16_t *)arena.take((uint64_t)T * F8 * 4);
+    const Matrix x = packed({f->x, f->ld_x, T, D}), dy = packed({g->dy, g->ld_dy, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
+    Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
+    packed_pair(wg, wu);
+
+    GemmCall a{};                          // dh, and h, dg, du
+    a.a = GemmOperand{{dy.p, dy.p}, dy.ld, dy.cols};
+    a.b = GemmOperand{{wd.p, wd.p}, wd.ld, D};
+    a.m = T; a.n = F8; a.n_real = F;
+    run_of_sums(a, D, 1);
+    a.h = h; a.gate = gate; a.up = up; a.ldi = F8;
+    a.dgate = d; a.dup = d + F8; a.ldd = 2 * F8;
+    launch(GEMM_DH, a, false);
+
+    const bool wide_grad = ((uintptr_t)g->dw_down % 16 | (uintptr_t)g->dw_gate % 16 | (uintptr_t)g->dw_up % 16) == 0;
+    GemmCall b{};                          // dWd
+    b.a = GemmOperand{{dy.p, dy.p}, dy.ld, T};
+    b.b = GemmOperand{{h, h}, F8, T};
+    b.m = D; b.n = F8;
+    run_of_sums(b, T, 1);
+    out(b, g->dw_down, g->ld_dw_down, F);
+    grad(b, g, wide_grad);
+    launch(GEMM_DW, b, false);
+
+    GemmCall e{};                          // dWg, dWu
+    e.a = GemmOperand{{d, d}, 2 * F8, T};
+    e.b = GemmOperand{{x.p, x.p}, x.ld, T};
+    e.m = 2 * F8; e.n = x.cols;
+    run_of_sums(e, T, 1);
+    out(e, g->dw_gate, g->ld_dw_gate, D);
+    e.c[1] = g->dw_up;
+    e.m_first = F8; e.m_real = F;
+    grad(e, g, wide_grad);
+    launch(GEMM_DW, e, false);
+
+    GemmCall i{};                          // dx
+    i.a = GemmOperand{{d, d + F8}, 2 * F8, F8};
+    i.b = GemmOperand{{wg.p, wu.p}, wg.ld, F};
+    i.m = T; i.n = wg.cols;
+    run_of_sums(i, F8, 2);
+    out(i, g->dx, g->ld_dx, D);
+    launch(GEMM_DX, i, true);
+  }
+
+  void grad(GemmCall &c, const chm_ffn_gradients *g, bool wide) {
+    c.f32_out = g->grad_dtype == CHM_F32;
+    c.accumulate = g->accumulate != 0;
+    c.wide = wide && c.ldc % 8 == 0;
+  }
+};
+
+bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
+
+int check(const chm_ffn *f) {
+  if (!f || (f->dtype != CHM_BF16 && f->dtype != CHM_F16) || f->activation < CHM_ACT_SILU || f->activation > CHM_ACT_GELU_TANH)
+    return CHM_ERR_ARG;
+  if (f->tokens < 0 || f->tokens > INT32_MAX || f->width < 1 || f->width > (1 << 24) || f->features < 1 || f->features > (1 << 24)) return CHM_ERR_ARG;
+  if (f->ld_x < f->width || f->ld_gate < f->width || f->ld_up < f->width || f->ld_down < f->features) return CHM_ERR_ARG;
+  if (f->ld_x > INT32_MAX || f->ld_gate > INT32_MAX || f->ld_up > INT32_MAX || f->ld_down > INT32_MAX) return CHM_ERR_ARG;
+  if (!aligned(f->x, 2) || !aligned(f->w_gate, 2) || !aligned(f->w_up, 2) || !aligned(f->w_down, 2) || !aligned(f->saved, 16)) return CHM_ERR_ARG;
+  return CHM_OK;
+}
+
+int check_gradients(const chm_ffn *f, const chm_ffn_gradients *g) {
+  if (!g || (g->grad_dtype != f->dtype && g->grad_dtype != CHM_F32)) return CHM_ERR_ARG;
+  const int64_t size = g->grad_dtype == CHM_F32 ? 4 : 2;
+  if (g->ld_dy < f->width || g->ld_dx < f->width || g->ld_dw_gate < f->width || g->ld_dw_up != g->ld_dw_gate || g->ld_dw_down < f->features)
+    return CHM_ERR_ARG;
+  if (g->ld_dy > INT32_MAX || g->ld_dx > INT32_MAX || g->ld_dw_gate > INT32_MAX || g->ld_dw_down > INT32_MAX) return CHM_ERR_ARG;
+  if (!aligned(g->dy, 2) || !aligned(g->dx, 2) || !aligned(g->dw_gate, size) || !aligned(g->dw_up, size) || !aligned(g->dw_down, size)) return CHM_ERR_ARG;
+  return CHM_OK;
+}
+
+}  // namespace
+
+extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint64_t *saved, uint64_t *forward_scratch, uint64_t *backward_scratch) {
+  const int rc = check(f);
+  if (rc != CHM_OK) return rc;
+  if (g && check_gradients(f, g) != CHM_OK) return CHM_ERR_ARG;
+  if (saved) *saved = (uint64_t)f->tokens * up8(f->features) * 4;
+  if (forward_scratch) {
+    Pass p(f, nullptr, nullptr, false);
+    p.forward(nullptr, f->width);
+    *forward_scratch = p.arena.used;
+  }
+  if (backward_scratch) {
+    *backward_scratch = 0;
+    if (!g) return CHM_OK;
+    Pass p(f, nullptr, nullptr, false);
+    p.backward(g);
+    *backward_scratch = p.arena.used;
+  }
+  return CHM_OK;
+}
+
+extern "C" int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *scratch, uint64_t scratch_bytes, void *hip_stream) {
+  int rc = check(f);
+  if (rc != CHM_OK) return rc;
+  if (ld_y < f->width || ld_y > INT32_MAX || !aligned(y, 2) || !aligned(scratch, 16)) return CHM_ERR_ARG;
+  if (f->tokens == 0) return CHM_OK;
+  if (!f->x || !f->w_gate || !f->w_up || !f->w_down || !y || !scratch) return CHM_ERR_ARG;
+  Pass need(f, nullptr, nullptr, false);
+  need.forward(y, ld_y);
+  if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
+  p.forward(y, ld_y);
+  return p.ok ? CHM_OK : CHM_ERR_HIP;
+}
+
+extern "C" int chm_ffn_backward(const chm_ffn *f, const chm_ffn_gradients *g, void *scratch, uint64_t scratch_bytes, void *hip_stream) {
+  int rc = check(f);
+  if (rc == CHM_OK) rc = check_gradients(f, g);
+  if (rc != CHM_OK) return rc;
+  if (!aligned(scratch, 16) || !g->dw_gate || !g->dw_up || !g->dw_down) return CHM_ERR_ARG;
+  if (f->tokens > 0 && (!f->x || !f->w_gate || !f->w_up || !f->w_down || !f->saved || !g->dy || !g->dx || !scratch)) return CHM_ERR_ARG;
+  Pass need(f, nullptr, nullptr, false);
+  need.backward(g);
+  if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
+  p.backward(g);
+  return p.ok ? CHM_OK : CHM_ERR_HIP;
+}

@@ -1,0 +1,553 @@
+"""The operators of a training step (feed-forward block, embedding, gradient norm and clipping) on the GPU against their
+formulas in 64 bits.
+
+Tolerances.  A value rounded to a type of unit roundoff u is off by at most u |value| (for float16 at least 2^-25); where such
+values enter a sum their errors are independent, with a standard deviation of that bound / sqrt(3), and the sum is allowed six
+standard deviations of the total, plus its own rounding.  float32 sums of k terms are allowed sqrt(k) roundings of 2^-24 of the
+root of the summed squares, six standard deviations again.  A term that is left out, doubled or misplaced is some
+ten times larger than that at the sizes used here.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.bfloat16: 2.0 ** -9, torch.float16: 2.0 ** -12, torch.float32: 2.0 ** -25}
+U = {k: 2 * v for k, v in U.items()}             # unit roundoff: half a unit in the last place of 1.0
+TINY = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25, torch.float32: 0.0}
+ACC = 2.0 ** -24
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2508_21613_amd import binding, operators
+    binding.lib()
+    return operators
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, rows, cols, dtype, std=1.0, pad=0, shift=0):
+    """rows x cols normal numbers in rows of cols + pad elements, `shift` elements into their buffer"""
+    buf = torch.full((rows * (cols + pad) + shift,), float("nan"), dtype=dtype, device="cuda")
+    t = buf[shift:].view(rows, cols + pad)[:, :cols]
+    t.copy_(torch.randn(rows, cols, generator=g, device="cuda") * std)
+    return t
+
+
+# ------------------------------------------------------------------------------------------------ feed-forward block
+def act_of(act, g):
+    """the activation, its derivative, and a bound of its second derivative"""
+    if act == "silu":
+        s = torch.sigmoid(g)
+        return g * s, s * (1 + g * (1 - s)), 0.5
+    if act == "gelu":
+        p = 0.5 * (1 + torch.erf(g / math.sqrt(2)))
+        return g * p, p + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi), 0.8
+    c = math.sqrt(2 / math.pi)
+    t = torch.tanh(c * (g + 0.044715 * g ** 3))
+    return 0.5 * g * (1 + t), 0.5 * (1 + t) + 0.5 * g * (1 - t * t) * c * (1 + 3 * 0.044715 * g * g), 1.0
+
+
+def rounded(v, dtype):
+    """variance of the error of rounding v"""
+    return (torch.clamp(v.abs() * U[dtype], min=TINY[dtype])) ** 2 / 3
+
+
+def summed(a, b, k):
+    """variance of the float32 roundings of the product a b over k sums"""
+    return (ACC ** 2 * k) * ((a * a) @ (b * b))
+
+
+def formula(x, wg, wu, wd, act, dy=None):
+    """{name: (value, variance of the error)} in 64 bits for inputs of 16 bits"""
+    dtype = x.dtype
+    x, wg, wu, wd = (t.double() for t in (x, wg, wu, wd))
+    T, D = x.shape
+    F = wg.shape[0]
+    g, u = x @ wg.T, x @ wu.T
+    a, da, dda = act_of(act, g)
+    vg, vu = summed(x, wg.T, D), summed(x, wu.T, D)
+    h = a * u
+    vh = rounded(h, dtype) + (da * u) ** 2 * vg + a ** 2 * vu + (8 * ACC * h) ** 2
+    out = {"y": (h @ wd.T, vh @ (wd * wd).T + summed(h, wd.T, F))}
+    if dy is None:
+        return out
+    dy = dy.double()
+    vg, vu = vg + rounded(g, dtype), vu + rounded(u, dtype)                # kept in 16 bits between the passes
+    vh = rounded(h, dtype) + (da * u) ** 2 * vg + a ** 2 * vu + (8 * ACC * h) ** 2
+    dh = dy @ wd
+    vdh = summed(dy, wd, D)
+    du, dg = dh * a, dh * u * da
+    vdu = a ** 2 * vdh + (dh * da) ** 2 * vg + rounded(du, dtype) + (8 * ACC * du) ** 2
+    vdg = (u * da) ** 2 * vdh + (dh * da) ** 2 * vu + (dh * u * dda) ** 2 * vg + rounded(dg, dtype) + (8 * ACC * dh * u) ** 2
+    out["dx"] = (dg @ wg + du @ wu, vdg @ (wg * wg) + vdu @ (wu * wu) + summed(dg, wg, 2 * F) + summed(du, wu, 2 * F))
+    out["dw_gate"] = (dg.T @ x, vdg.T @ (x * x) + summed(dg.T, x, T))
+    out["dw_up"] = (du.T @ x, vdu.T @ (x * x) + summed(du.T, x, T))
+    out["dw_down"] = (dy.T @ h, (dy * dy).T @ vh + summed(dy.T, h, T))
+    return out
+
+
+def check(name, got, want, dtype=None):
+    value, var = want
+    dtype = dtype or got.dtype
+    assert got.shape == value.shape, name
+    assert bool(torch.isfinite(got).all()), name
+    err = (got.double() - value).abs()
+    tol = 6 * var.sqrt() + torch.clamp(value.abs() * U[dtype], min=TINY[dtype]) + 1e-30
+    bad = err > tol * 1.0001
+    assert not bool(bad.any()), (name, int(bad.sum()), float((err / tol).max()), [int(i) for i in bad.nonzero()[0]])
+
+
+def ffn_inputs(seed, T, D, F, dtype, pad=0, shift=0):
+    g = gen(seed)
+    return (normal(g, T, D, dtype, 1.0, pad, shift), normal(g, F, D, dtype, D ** -0.5, pad, shift), normal(g, F, D, dtype, D ** -0.5, pad, shift),
+            normal(g, D, F, dtype, F ** -0.5, pad, shift), normal(g, T, D, dtype, 0.5, pad, shift))
+
+
+NAMES = ("dx", "dw_gate", "dw_up", "dw_down")
+
+
+def ffn_both(ops, inputs, act, **kw):
+    x, wg, wu, wd, dy = inputs
+    y, saved = ops.ffn_forward(x, wg, wu, wd, activation=act, save=True)
+    grads = ops.ffn_backward(dy, x, wg, wu, wd, saved, activation=act, **kw)
+    return dict(zip(("y",) + NAMES, (y,) + grads))
+
+
+FFN_SHAPES = [(1, 1, 1), (1, 64, 128), (2, 7, 5), (3, 130, 9), (15, 64, 72), (16, 72, 200), (17, 65, 130), (31, 8, 8), (32, 256, 24), (33, 128, 64),
+              (63, 200, 96), (64, 513, 1031), (65, 64, 64), (65, 1, 9), (66, 9, 1), (128, 1024, 512), (130, 136, 264), (255, 96, 320), (257, 515, 1001),
+              (300, 72, 520), (513, 2048, 256)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", FFN_SHAPES)
+def test_ffn_forward_and_backward(ops, shape, dtype):
+    act = ("silu", "gelu", "gelu_tanh")[sum(shape) % 3]
+    inputs = ffn_inputs(sum(shape), *shape, dtype)
+    want = formula(*inputs[:4], act, inputs[4])
+    got = ffn_both(ops, inputs, act)
+    for k, v in want.items():
+        check(k, got[k], v)
+    alone = ops.ffn_forward(*inputs[:4], activation=act)                   # without keeping anything: the same bits
+    assert torch.equal(alone, got["y"])
+
+
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("T", [5, 90])
+def test_ffn_activations(ops, act, T):
+    inputs = ffn_inputs(3, T, 64, 96, torch.float16)
+    inputs[0].mul_(4)                                                      # far into both tails of the activation
+    want = formula(*inputs[:4], act, inputs[4])
+    for k, v in ffn_both(ops, inputs, act).items():
+        check(k, v, want[k])
+
+
+@pytest.mark.parametrize("T", [3, 70, 140])
+@pytest.mark.parametrize("pad,shift", [(0, 1), (3, 0), (5, 7), (8, 0), (64, 8)])
+def test_ffn_strides_and_alignment(ops, T, pad, shift):
+    inputs = ffn_inputs(11, T, 72, 104, torch.float16, pad, shift)
+    want = formula(*inputs[:4], "silu", inputs[4])
+    for k, v in ffn_both(ops, inputs, "silu").items():
+        check(k, v, want[k])
+    # weights of different strides, results into strided places that start anywhere
+    x, wg, wu, wd, dy = inputs
+    wu2 = normal(gen(1), 104, 72, torch.float16, 1.0, 16)
+    wu2.copy_(wu)
+    outs = [normal(gen(2), r, c, torch.float16, 1.0, 5, 3) for r, c in ((T, 72), (T, 72), (104, 72), (104, 72), (72, 104))]
+    y, saved = ops.ffn_forward(x, wg, wu2, wd, save=True, out=outs[0])
+    assert y is outs[0]
+    ops.ffn_backward(dy, x, wg, wu2, wd, saved, grads=outs[2:], out=outs[1])
+    for k, v in zip(("y",) + NAMES, outs):
+        check(k, v, want[k])
+        assert bool(torch.isnan(v._base[:3]).all()) and bool(torch.isnan(v._base[3:].view(v.shape[0], -1)[:, v.shape[1]:]).all()), k
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_ffn_large_tiles(ops, dtype):
+    inputs = ffn_inputs(5, 3590, 3592, 3608, dtype)
+    want = formula(*inputs[:4], "silu", inputs[4])
+    for k, v in ffn_both(ops, inputs, "silu").items():
+        check(k, v, want[k])
+
+
+def test_ffn_offsets_beyond_32_bits(ops):
+    T, D, F, dtype = 131080, 64, 16392, torch.float16
+    x, wg, wu, wd, dy = ffn_inputs(7, T, D, F, dtype)
+    got = ffn_both(ops, (x, wg, wu, wd, dy), "silu")
+    sums = None
+    for at in range(0, T, 16384):
+        s = slice(at, min(at + 16384, T))
+        part = formula(x[s], wg, wu, wd, "silu", dy[s])
+        for k in ("y", "dx"):
+            check(k, got[k][s], part[k])
+        part = {k: part[k] for k in NAMES[1:]}
+        sums = part if sums is None else {k: tuple(a + b for a, b in zip(sums[k], part[k])) for k in part}
+    for k in NAMES[1:]:
+        value, var = sums[k]
+        check(k, got[k], (value, var * 10))                                # float32 sums of T terms were allowed for 16,384 only
+
+
+def test_ffn_accumulates(ops):
+    T, D, F, dtype = 100, 136, 72, torch.bfloat16
+    a, b = ffn_inputs(1, T, D, F, dtype), ffn_inputs(2, T, D, F, dtype)
+    b = (b[0],) + a[1:4] + (b[4],)
+    wa, wb = formula(*a[:4], "silu", a[4]), formula(*b[:4], "silu", b[4])
+    for gd in (torch.float32, dtype):
+        shapes = ((F, D), (F, D), (D, F))
+        grads = [torch.full(s, float("nan"), dtype=gd, device="cuda") for s in shapes]
+        ffn_both(ops, a, "silu", grads=grads)                              # written over
+        first = [g.clone() for g in grads]
+        ffn_both(ops, b, "silu", grads=grads, accumulate=True)
+        for k, g, f in zip(NAMES[1:], grads, first):
+            check(k, f, wa[k])
+            check(k, g, (f.double() + wb[k][0], wb[k][1] + (ACC * f.double()) ** 2))
+
+
+@pytest.mark.parametrize("T", [4, 80])
+def test_ffn_bits_repeat_and_streams(ops, T):
+    inputs = ffn_inputs(9, T, 264, 520, torch.bfloat16)
+    want = ffn_both(ops, inputs, "silu")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    y, saved = ops.ffn_forward(*inputs[:4], save=True, stream=side)
+    grads = ops.ffn_backward(inputs[4], *inputs[:4], saved, stream=side.cuda_stream)
+    side.synchronize()
+    for k, v in zip(("y",) + NAMES, (y,) + grads):
+        assert torch.equal(v, want[k]), k
+
+
+def test_ffn_gradients_against_differences(ops):
+    T, D, F, dtype, eps = 70, 40, 48, torch.float16, 1e-5
+    inputs = ffn_inputs(21, T, D, F, dtype)
+    got = ffn_both(ops, inputs, "gelu")
+    want = formula(*inputs[:4], "gelu", inputs[4])
+    wide = [t.double() for t in inputs]
+
+    def loss(i, d):
+        x, wg, wu, wd = [t + d if j == i else t for j, t in enumerate(wide[:4])]
+        return float((((act_of("gelu", x @ wg.T)[0] * (x @ wu.T)) @ wd.T) * wide[4]).sum())
+
+    for i, k in enumerate(NAMES):
+        v = torch.randn(wide[i].shape, generator=gen(i), device="cuda", dtype=torch.float64)
+        slope = (loss(i, eps * v) - loss(i, -eps * v)) / (2 * eps)
+        own = float((got[k].double() * v).sum())
+        sd = math.sqrt(float(((want[k][1] + (U[dtype] * want[k][0]) ** 2) * v * v).sum()))
+        assert abs(slope - own) <= 6 * sd + 1e-5 * abs(slope), (k, slope, own, sd)
+
+
+@pytest.mark.parametrize("T", [2, 67])
+def test_ffn_infinities_and_nans_stay_in_their_rows(ops, T):
+    inputs = ffn_inputs(4, T, 72, 77, torch.bfloat16)
+    clean = ffn_both(ops, inputs, "silu")
+    inputs[0][1, 3] = float("nan")
+    inputs[4][1, 5] = float("inf")
+    got = ffn_both(ops, inputs, "silu")
+    rest = [i for i in range(T) if i != 1]
+    assert bool(torch.isnan(got["y"][1]).all()) and bool(torch.isnan(got["dx"][1]).all())
+    for k in ("y", "dx"):
+        assert torch.equal(got[k][rest], clean[k][rest]), k
+    inputs[0][1, 3] = 0.0                                                  # an infinite gradient alone
+    inputs[3].abs_()
+    inputs[0][1].zero_()                                                   # g = u = 0: dg = dh u act' is not a number, du = dh act(0) too
+    got = ffn_both(ops, inputs, "silu")
+    assert bool(torch.isnan(got["dx"][1]).all()) and bool(torch.isfinite(got["y"]).all())
+
+
+def test_ffn_no_tokens(ops):
+    inputs = ffn_inputs(4, 0, 16, 24, torch.bfloat16)
+    got = ffn_both(ops, inputs, "silu")
+    assert got["y"].shape == (0, 16) and got["dx"].shape == (0, 16)
+    for k in NAMES[1:]:
+        assert bool((got[k] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------ embedding
+def lookup_want(tokens, table, scale):
+    live = (tokens >= 0) & (tokens < table.shape[0])
+    rows = torch.zeros((len(tokens), table.shape[1]), dtype=torch.float64, device="cuda")
+    rows[live] = table[tokens[live].long()].double() * scale
+    return rows
+
+
+def gradient_want(dy, tokens, V, scale):
+    live = (tokens >= 0) & (tokens < V)
+    order = tokens[live].long()
+    v = torch.zeros((V, dy.shape[1]), dtype=torch.float64, device="cuda").index_add_(0, order, dy[live].double() * scale)
+    counts = torch.bincount(order, minlength=V)[:, None].double()
+    sq = torch.zeros_like(v).index_add_(0, order, (dy[live].double() * scale) ** 2)
+    return v, ACC ** 2 * (counts + 2) * sq
+
+
+EMBED = [(1, 1, 1), (1, 5, 64), (7, 3, 9), (255, 40, 31), (256, 100, 515), (257, 100, 515), (300, 7, 64), (1000, 1, 72), (1024, 33, 8), (2049, 5000, 100),
+         (4096, 100, 2049), (5000, 513, 130), (16384, 3000, 72), (16385, 511, 40), (40000, 70000, 24), (70001, 129, 16)]
+
+
+def make_tokens(seed, n, V, index, kind):
+    g = gen(seed)
+    if kind == "same":
+        t = torch.full((n,), V - 1, device="cuda")
+    elif kind == "none":
+        t = torch.full((n,), -1, device="cuda")
+    else:
+        t = (torch.rand(n, generator=g, device="cuda").double() ** 3 * V).long().clamp_(0, V - 1)
+        if kind == "outside":                                              # of another shard, padding, far outside
+            k = torch.rand(n, generator=g, device="cuda")
+            t = torch.where(k < 0.15, -1 - t, torch.where(k < 0.3, t + V, t))
+            t[:: 97] = -(1 << 31) if index == torch.int32 else -(1 << 62)
+            t[5:: 97] = (1 << 31) - 1 if index == torch.int32 else (1 << 32) + V - 1
+    return t.to(index)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32])
+@pytest.mark.parametrize("kind", ["some", "outside"])
+@pytest.mark.parametrize("shape", EMBED)
+def test_embedding(ops, shape, kind, dtype):
+    n, V, D = shape
+    index = (torch.int32, torch.int64)[(n + V) % 2]
+    pad, shift = ((0, 0), (3, 1), (8, 8))[(n + D) % 3]
+    g = gen(n + V)
+    tokens, scale = make_tokens(n, n, V, index, kind), 1.75
+    table, dy = normal(g, V, D, dtype, 1.0, pad, shift), normal(g, n, D, dtype, 1.0, pad, shift)
+    rows = lookup_want(tokens, table, scale)
+    check("rows", ops.embedding_lookup(tokens, table, scale), (rows, torch.zeros_like(rows)))
+    want = gradient_want(dy, tokens, V, scale)
+    got = ops.embedding_gradient(dy, tokens, V, scale)
+    check("dtable", got, want)
+    assert bool((got[want[1].amax(1) == 0] == 0).all())                    # rows that no token names
+    assert torch.equal(got, ops.embedding_gradient(dy, tokens, V, scale))
+    for gd in {dtype, torch.float32}:
+        start = normal(g, V, D, gd, 1.0, pad, shift)
+        out = normal(g, V, D, gd, 1.0, pad, shift)
+        out.copy_(start)
+        ops.embedding_gradient(dy, tokens, scale=scale, out=out, accumulate=True)
+        check("added", out, (want[0] + start.double(), want[1] + (ACC * start.double()) ** 2))
+        named = torch.zeros(V, dtype=torch.bool, device="cuda")
+        named[tokens[(tokens >= 0) & (tokens < V)].long()] = True
+        assert torch.equal(out[~named], start[~named])
+        if pad:
+            assert bool(torch.isnan(out._base[:shift]).all()) and bool(torch.isnan(out._base[shift:].view(V, -1)[:, D:]).all())
+
+
+@pytest.mark.parametrize("kind", ["same", "none"])
+@pytest.mark.parametrize("n", [1, 200, 3000, 20000])
+def test_embedding_one_token_or_none(ops, n, kind):
+    V, D = 37, 100
+    tokens, dy = make_tokens(1, n, V, torch.int64, kind), normal(gen(2), n, D, torch.float32)
+    check("dtable", ops.embedding_gradient(dy, tokens, V), gradient_want(dy, tokens, V, 1.0))
+
+
+def test_embedding_empty(ops):
+    none = torch.empty(0, dtype=torch.int64, device="cuda")
+    table = normal(gen(1), 10, 6, torch.bfloat16)
+    assert ops.embedding_lookup(none, table).shape == (0, 6)
+    out = ops.embedding_gradient(torch.empty((0, 6), dtype=torch.bfloat16, device="cuda"), none, 10)
+    assert out.shape == (10, 6) and bool((out == 0).all())
+    assert bool((ops.embedding_lookup(torch.zeros(3, dtype=torch.int64, device="cuda"), table[:0]) == 0).all())
+
+
+def test_embedding_offsets_beyond_32_bits(ops):
+    V, D = 600000, 4096
+    tokens = torch.tensor([V - 1, 0, V - 1, 530000, -1], device="cuda")
+    table = torch.zeros((V, D), dtype=torch.bfloat16, device="cuda")
+    table[V - 1], table[530000], table[0] = 3, 5, 7
+    got = ops.embedding_lookup(tokens, table)
+    assert [float(v) for v in got[:, D - 1]] == [3, 7, 3, 5, 0] and bool((got == got[:, :1]).all())
+    for n in (5, 300):
+        t = tokens.repeat(n // 5)
+        dy = torch.ones((n, D), dtype=torch.bfloat16, device="cuda")
+        table.fill_(9)
+        ops.embedding_gradient(dy, t, out=table)
+        k = n // 5
+        for row, value in ((V - 1, 2 * k), (0, k), (530000, k), (1, 0), (V - 2, 0), (300000, 0), (530001, 0)):
+            assert bool((table[row] == value).all()), (n, row)
+
+
+def test_embedding_infinities_stay_in_their_rows(ops):
+    for n in (100, 1000):
+        tokens = torch.arange(n, device="cuda") % 50
+        dy = torch.ones((n, 40), dtype=torch.bfloat16, device="cuda")
+        dy[3, 7], dy[4, 8] = float("inf"), float("nan")
+        got = ops.embedding_gradient(dy, tokens, 60)
+        assert float(got[3, 7]) == float("inf") and bool(torch.isnan(got[4, 8]))
+        got[3, 7] = got[4, 8] = n // 50
+        assert bool((got[:50] == n // 50).all()) and bool((got[50:] == 0).all())
+
+
+# ------------------------------------------------------------------------------------------------ norm and clipping
+def clip_want(grads, max_norm, sumsq=None):
+    total = sum(float((g.double() ** 2).sum()) for g in grads) if sumsq is None else sumsq
+    norm = math.sqrt(total)
+    return norm, min(1.0, max_norm / (norm + 1e-6))
+
+
+def check_clip(norm, got, grads, max_norm, sumsq=None):
+    n, c = clip_want(grads, max_norm, sumsq)
+    assert norm.dtype == torch.float32 and norm.dim() == 0
+    assert abs(float(norm) - n) <= 2 * 2.0 ** -24 * n
+    for a, g in zip(got, grads):
+        w = g.double() * c
+        # the factor is off by a few float32 roundings, then one rounding to the gradient's type
+        check("clipped", a, (w, (4 * ACC * w) ** 2))
+
+
+CLIP = [[1], [5, 0, 3], [8191, 8192, 8193], [1 << 20, 1, 77777], [3] * 300, [100003] * 40, [(1 << 22) + 5]]
+
+
+@pytest.mark.parametrize("factor", [0.3, 4.0])
+@pytest.mark.parametrize("sizes", CLIP, ids=lambda s: "%dx%d" % (len(s), s[0]))
+def test_clip(ops, sizes, factor):
+    g = gen(len(sizes))
+    types = (torch.float32, torch.bfloat16, torch.float16)
+    grads = []
+    for i, n in enumerate(sizes):
+        shift = i % 5
+        buf = torch.empty(n + shift + 3, dtype=types[(i + len(sizes)) % 3], device="cuda")
+        buf.copy_(torch.randn(buf.shape, generator=g, device="cuda"))
+        grads.append(buf[shift:shift + n])
+    raw = [t.clone() for t in grads]
+    rims = [t._base.clone() for t in grads]
+    max_norm = factor * clip_want(raw, 1.0)[0]
+    out = [torch.full_like(t, 99.0) for t in grads]
+    with_out = ops.Gradients(grads, out)
+    norm = with_out.clip(max_norm)
+    check_clip(norm, out, raw, max_norm)
+    assert all(torch.equal(a, b) for a, b in zip(grads, raw))
+    here = ops.Gradients(grads)
+    total = here.sumsq()
+    assert total.dtype == torch.float64 and abs(float(total) - clip_want(raw, 1.0)[0] ** 2) <= 1e-12 * float(total) + 1e-300
+    assert torch.equal(here.clip(max_norm), norm)
+    assert all(torch.equal(a, b) for a, b in zip(grads, out))
+    for t, rim in zip(grads, rims):                                        # nothing beside the tensors is written
+        mine = t._base.clone()
+        at = t.storage_offset()
+        mine[at:at + t.numel()] = rim[at:at + t.numel()]
+        assert torch.equal(mine, rim)
+    here.close()
+    with_out.close()
+
+
+def test_clip_with_the_sum_of_other_stages(ops):
+    a, b = [normal(gen(1), 30, 70, torch.float32)], [normal(gen(2), 9, 1000, torch.bfloat16), normal(gen(3), 3, 3, torch.float32)]
+    raw = [t.clone() for t in a + b]
+    sa, sb = ops.Gradients(a), ops.Gradients(b)
+    total = sa.sumsq() + sb.sumsq()
+    norms = [sa.clip(0.5, sumsq=total), sb.clip(0.5, sumsq=total)]
+    for norm in norms:
+        check_clip(norm, a + b, raw, 0.5)
+
+
+def test_clip_in_any_dense_layout(ops):
+    t = torch.randn(40, 50, generator=gen(1), device="cuda").t()
+    raw = t.clone()
+    norm = ops.Gradients([t]).clip(0.1)
+    check_clip(norm, [t], [raw], 0.1)
+
+
+def test_clip_range_of_values(ops):
+    big = torch.full((1000,), 1e30, device="cuda")                         # squares beyond float32, and below it
+    small = torch.full((1000,), 1e-30, device="cuda")
+    for t in (big, small):
+        raw = t.clone()
+        norm = ops.Gradients([t]).clip(float(raw[0]))
+        check_clip(norm, [t], [raw], float(raw[0]))
+    for bad in (float("inf"), float("nan")):
+        t = torch.ones(3000, device="cuda")
+        t[2999] = bad
+        norm = ops.Gradients([t]).clip(1.0)
+        assert not bool(torch.isfinite(norm)) and bool(torch.isnan(t[2999]))
+        if bad == float("inf"):
+            assert float(norm) == bad and bool((t[:2999] == 0).all())      # 1 / infinity
+        else:
+            assert bool(torch.isnan(t).all())
+    t = torch.ones(4, device="cuda")
+    assert float(ops.Gradients([t]).clip(0.0)) == 2.0 and bool((t == 0).all())
+    zero = torch.zeros(4, device="cuda")
+    assert float(ops.Gradients([zero]).clip(1.0)) == 0.0 and bool((zero == 0).all())
+    assert float(ops.Gradients([]).clip(1.0)) == 0.0 and float(ops.Gradients([zero[:0]]).sumsq()) == 0.0
+
+
+def test_clip_lengths_beyond_32_bits(ops):
+    n = (1 << 31) + 5
+    t = torch.ones(n, dtype=torch.bfloat16, device="cuda")
+    t[n - 1] = 2.0
+    norm = ops.Gradients([t]).clip(0.5 * math.sqrt(n + 3.0))
+    assert abs(float(norm) - math.sqrt(n + 3.0)) <= 2.0 ** -23 * float(norm)
+    assert bool((t[:n - 1] == 0.5).all()) and float(t[n - 1]) == 1.0
+
+
+# ------------------------------------------------------------------------------------------------ all of them
+def test_a_captured_step_replays(ops):
+    T, D, F, V, dtype = 300, 128, 264, 500, torch.bfloat16
+    _, wg, wu, wd, dy = ffn_inputs(31, T, D, F, dtype)
+    table = normal(gen(3), V, D, dtype)
+    tokens = make_tokens(4, T, V, torch.int64, "outside")
+    grads = [torch.zeros(s, device="cuda") for s in ((F, D), (F, D), (D, F), (V, D))]
+    clipped = [torch.zeros_like(t) for t in grads]
+    lists = ops.Gradients(grads, clipped)
+
+    def step():
+        x = ops.embedding_lookup(tokens, table, 2.0)
+        y, saved = ops.ffn_forward(x, wg, wu, wd, save=True)
+        dx = ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=grads[:3])[0]
+        ops.embedding_gradient(dx, tokens, scale=2.0, out=grads[3])
+        return y, lists.clip(0.1)
+
+    side = torch.cuda.Stream()
+    with torch.cuda.stream(side):
+        step()
+    side.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        y, norm = step()
+    for seed in range(4):
+        dy.copy_(torch.randn(T, D, generator=gen(seed), device="cuda"))
+        tokens.copy_(make_tokens(seed, T, V, torch.int64, "outside"))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = [t.clone() for t in [y, norm] + grads + clipped]
+        want_y, want_norm = step()
+        torch.cuda.synchronize()
+        for a, b in zip(got, [want_y, want_norm] + grads + clipped):
+            assert torch.equal(a, b)
+
+
+def test_refusals(ops):
+    from paper_2508_21613_amd import binding as B
+    x, wg, wu, wd, dy = ffn_inputs(1, 4, 16, 24, torch.bfloat16)
+    saved = ops.ffn_forward(x, wg, wu, wd, save=True)[1]
+    tokens = torch.zeros(4, dtype=torch.int64, device="cuda")
+    grad = torch.zeros(8, device="cuda")
+    calls = [lambda: ops.ffn_forward(x.float(), wg, wu, wd), lambda: ops.ffn_forward(x, wg.half(), wu, wd), lambda: ops.ffn_forward(x.cpu(), wg, wu, wd),
+             lambda: ops.ffn_forward(x, wg[:, :8], wu, wd), lambda: ops.ffn_forward(x, wg, wu[:20], wd), lambda: ops.ffn_forward(x, wg, wu, wd.t()),
+             lambda: ops.ffn_forward(x[0], wg, wu, wd), lambda: ops.ffn_forward(x, wg, wu, wd, activation="relu"),
+             lambda: ops.ffn_forward(x[:1].expand(4, 16), wg, wu, wd), lambda: ops.ffn_forward(x, wg, wu, wd, out=dy.float()),
+             lambda: ops.ffn_forward(x, wg.t().contiguous().t(), wu, wd), lambda: ops.ffn_forward(x[:, :0], wg[:, :0], wu[:, :0], wd[:0]),
+             lambda: ops.ffn_backward(dy[:3], x, wg, wu, wd, saved), lambda: ops.ffn_backward(dy, x, wg, wu, wd, saved[:100]),
+             lambda: ops.ffn_backward(dy, x, wg, wu, wd, saved, accumulate=True), lambda: ops.ffn_backward(dy, x, wg, wu, wd, None),
+             lambda: ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=[wg.half(), wu.half(), wd.half()]),
+             lambda: ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=[wg.clone(), wu.clone()]),
+             lambda: ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=[torch.zeros((24, 20), dtype=x.dtype, device="cuda")[:, :16], wu.clone(), wd.clone()]),
+             lambda: ops.embedding_lookup(tokens.short(), wg), lambda: ops.embedding_lookup(tokens.cpu(), wg), lambda: ops.embedding_lookup(tokens, wg.double()),
+             lambda: ops.embedding_lookup(tokens, wg, out=torch.zeros((3, 16), dtype=wg.dtype, device="cuda")),
+             lambda: ops.embedding_gradient(dy, tokens[:3], 9), lambda: ops.embedding_gradient(dy, tokens), lambda: ops.embedding_gradient(dy, tokens, -1),
+             lambda: ops.embedding_gradient(dy, tokens, 9, accumulate=True), lambda: ops.embedding_gradient(dy, tokens, out=wg.half()),
+             lambda: ops.embedding_gradient(dy, tokens, 9, out=wg),
+             lambda: ops.Gradients([grad.cpu()]), lambda: ops.Gradients([grad.double()]), lambda: ops.Gradients([grad[::2]]),
+             lambda: ops.Gradients([grad], [grad.half()]), lambda: ops.Gradients([grad], []), lambda: ops.Gradients([grad]).clip(-1.0),
+             lambda: ops.Gradients([grad]).clip(float("nan")), lambda: ops.Gradients([grad]).clip(1.0, sumsq=grad)]
+    for i, call in enumerate(calls):
+        with pytest.raises(B.ChmError) as e:
+            call()
+        assert e.value.code == B.ERR_ARG, i
+    d = ops._ffn(x, wg, wu, wd, "silu")                                    # scratch that is too short
+    ws = torch.empty(64, dtype=torch.uint8, device="cuda")
+    assert B.lib().chm_ffn_forward(d, dy.data_ptr(), 16, ws.data_ptr(), 64, None) == B.ERR_LIMIT

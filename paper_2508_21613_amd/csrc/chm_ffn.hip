@@ -29,8 +29,9 @@ constexpr int FEW_MAX = 64;
 struct FewCall {
   const uint16_t *x, *w0, *w1;
   int64_t ldx, ld0, ld1;
-  uint16_t *out, *gate, *up;
-  int64_t ldo, lds;
+  uint16_t *out;
+  Kept kept;                                  // rows as those of out
+  int64_t ldo;
   int32_t tokens, rows, k, act;
 };
 
@@ -42,6 +43,14 @@ __device__ __forceinline__ s8 take8(const uint16_t *row, int k, int n) {
   for (int e = 0; e < 8; ++e)
     if (k + e < n) v[e] = (short)((const CHM_GLOBAL uint16_t *)row)[k + e];
   return v;
+}
+
+__device__ __forceinline__ void keep_pair(const FewCall &c, int64_t at, float g, float u) {
+  const uint32_t bg = chm_gemm::keep_bits(g), bu = chm_gemm::keep_bits(u);
+  c.kept.gate[at] = (uint16_t)(bg >> 16);
+  c.kept.gate_low[at] = (uint8_t)(bg >> 8);
+  c.kept.up[at] = (uint16_t)(bu >> 16);
+  c.kept.up_low[at] = (uint8_t)(bu >> 8);
 }
 
 template <class T, int TWO, int TILES>
@@ -105,7 +114,7 @@ __global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
     const int feature = o & 15, token = o >> 4;
     if (token >= c.tokens) continue;
     if (f0 + feature >= c.rows) {             // kept projections have rows of whole words of 8, zeros behind
-      if (TWO && c.gate && f0 + feature < ((c.rows + 7) & ~7)) c.gate[token * c.lds + f0 + feature] = c.up[token * c.lds + f0 + feature] = 0;
+      if (TWO && c.kept.gate && f0 + feature < ((c.rows + 7) & ~7)) keep_pair(c, token * c.ldo + f0 + feature, 0.f, 0.f);
       continue;
     }
     const int at = ((token >> 4) * 64 + (feature >> 2) * 16 + (token & 15)) * 4 + (feature & 3);
@@ -117,10 +126,7 @@ __global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
     const int64_t col = f0 + feature;
     if (TWO) {
       c.out[token * c.ldo + col] = T::down(chm_gemm::act_of(c.act, s0) * s1);
-      if (c.gate) {
-        c.gate[token * c.lds + col] = T::down(s0);
-        c.up[token * c.lds + col] = T::down(s1);
-      }
+      if (c.kept.gate) keep_pair(c, token * c.ldo + col, s0, s1);
     } else {
       c.out[token * c.ldo + col] = T::down(s0);
     }
@@ -208,6 +214,14 @@ struct Arena {
   }
 };
 
+// the four planes of chm_ffn::saved: 16-byte rows in each
+Kept kept_of(const chm_ffn *f) {
+  const int64_t n = f->tokens * up8(f->features);
+  char *p = (char *)f->saved;
+  if (!p) return Kept{};
+  return Kept{(uint16_t *)p, (uint16_t *)(p + n * 2), (uint8_t *)(p + n * 4), (uint8_t *)(p + n * 5)};
+}
+
 struct Pass {
   const chm_ffn *f;
   Arena arena;
@@ -274,7 +288,7 @@ struct Pass {
 
   void forward(void *y, int64_t ld_y) {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
-    uint16_t *gate = (uint16_t *)f->saved, *up = gate ? gate + T * F8 : nullptr;
+    const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
     if (T <= FEW_MAX) {
       if (!run || T == 0) return;
@@ -285,7 +299,7 @@ struct Pass {
       c.w0 = (const uint16_t *)f->w_gate; c.ld0 = f->ld_gate;
       c.w1 = (const uint16_t *)f->w_up; c.ld1 = f->ld_up;
       c.out = h; c.ldo = F8;
-      c.gate = gate; c.up = up; c.lds = F8;
+      c.kept = kept;
       c.rows = (int32_t)F; c.k = (int32_t)D;
       ok = f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 1>(c, st) : launch_few<chm_gemm::F16, 1>(c, st);
       FewCall d{};
@@ -305,7 +319,7 @@ struct Pass {
     c.b = GemmOperand{{wg.p, wu.p}, wg.ld, wg.cols};
     c.m = T; c.n = F;
     run_of_sums(c, x.cols, 1);
-    c.h = h; c.gate = gate; c.up = up; c.ldi = F8;
+    c.h = h; c.kept = kept; c.ldi = F8;
     launch(GEMM_GATE_UP, c, false);
     GemmCall d{};
     d.a = GemmOperand{{h, h}, F8, F8};
@@ -327,7 +341,7 @@ struct Pass {
 
   void backward(const chm_ffn_gradients *g) {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
-    uint16_t *gate = (uint16_t *)f->saved, *up = gate + T * F8;
+    const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2), *d = (uint16_t *)arena.take((uint64_t)T * F8 * 4);
     const Matrix x = packed({f->x, f->ld_x, T, D}), dy = packed({g->dy, g->ld_dy, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
     Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
@@ -338,7 +352,7 @@ struct Pass {
     a.b = GemmOperand{{wd.p, wd.p}, wd.ld, D};
     a.m = T; a.n = F8; a.n_real = F;
     run_of_sums(a, D, 1);
-    a.h = h; a.gate = gate; a.up = up; a.ldi = F8;
+    a.h = h; a.kept = kept; a.ldi = F8;
     a.dgate = d; a.dup = d + F8; a.ldd = 2 * F8;
     launch(GEMM_DH, a, false);
 
@@ -407,7 +421,7 @@ extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint6
   const int rc = check(f);
   if (rc != CHM_OK) return rc;
   if (g && check_gradients(f, g) != CHM_OK) return CHM_ERR_ARG;
-  if (saved) *saved = (uint64_t)f->tokens * up8(f->features) * 4;
+  if (saved) *saved = (uint64_t)f->tokens * up8(f->features) * 6;
   if (forward_scratch) {
     Pass p(f, nullptr, nullptr, false);
     p.forward(nullptr, f->width);

@@ -12,8 +12,9 @@
 // that read together touch different banks.  The direct loads write linearly, so the permutation is made on their source addresses.
 //
 // The first operand of a matrix instruction is the n side, the second the m side: a lane then holds four consecutive n of one
-// m.  Which rows of the tile a lane's n stand for is free; they are dealt out such that a lane ends with 16 consecutive n
-// (8 features of the gate and of the up projection each in the two-weight product), which are stored as whole 16-byte words.
+// m.  At the end every wavefront turns its sums round in shared memory, 32 rows of 64 at a time, so that a lane goes on with eight
+// consecutive n and a row's 64 leave (or meet what they are combined with) as one stretch of memory.  In the two-weight product
+// every 16 rows of the gate's weight are followed by the same rows of the up projection's: a wavefront holds both for 32 features.
 //
 // Sums are float32 (the matrix instructions' accumulators) in one fixed order: results do not change from call to call.
 #ifndef CHM_GEMM_H
@@ -75,16 +76,17 @@ __device__ __forceinline__ void act_grad_of(int act, float g, float &a, float &d
 enum { ROWS = 0, COLS = 1 };                       // k contiguous / own index contiguous
 enum { EPI_STORE = 0, EPI_ACT = 1, EPI_ACT_GRAD = 2 };
 enum { BK = 64 };
+enum { TURN_ROW = 272 };                           // bytes of 64 float32 and a gap that spreads the rows over the banks
 
-template <int N_SIDE, int DUAL> __device__ __forceinline__ uint32_t swz_rows(uint32_t row) {
-  if (!N_SIDE) return row & 7u;
-  if (DUAL) return (row & 3u) | (((row >> 3) & 1u) << 2);
-  return (row & 3u) | (((row >> 4) & 1u) << 2);
+// 24 bits of a float32, rounded to nearest, ties to even; not a number stays one
+__device__ __forceinline__ uint32_t keep_bits(float f) {
+  const uint32_t b = __float_as_uint(f), r = b + 0x7fu + ((b >> 8) & 1u);
+  return f != f ? b | 0x00400000u : r;
 }
-template <int N_SIDE> __device__ __forceinline__ uint32_t swz_cols(uint32_t k) {
-  if (!N_SIDE) return ((k & 3u) << 1) | (((k >> 3) & 1u) << 3);
-  return (k & 1u) | (((k >> 1) & 1u) << 3) | (((k >> 3) & 1u) << 2);
-}
+
+
+__device__ __forceinline__ uint32_t swz_rows(uint32_t row) { return row & 7u; }
+__device__ __forceinline__ uint32_t swz_cols(uint32_t k) { return ((k & 3u) << 1) | (((k >> 3) & 1u) << 3); }
 
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const char *p, int64_t bytes) {
   const uint32_t n = bytes <= 0 ? 0u : bytes > 0x7fffffff ? 0x7fffffffu : (uint32_t)bytes;
@@ -92,7 +94,7 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const char *p, int64_t
 }
 
 // One operand's way from memory to shared memory: W of its indices x BK sums a step, by NT threads.
-template <int KIND, int N_SIDE, int DUAL, int W, int NT>
+template <int KIND, int DUAL, int W, int NT>
 struct Feed {
   enum : uint32_t { OUT = 0x7fffffff };
   enum { NI = W * BK * 2 / 16 / NT, BYTES = W * BK * 2 };
@@ -116,11 +118,11 @@ struct Feed {
     for (int i = 0; i < NI; ++i) {
       const uint32_t idx = i * NT + tid;
       if (KIND == ROWS) {
-        const uint32_t row = idx / 8, chunk = (idx & 7u) ^ swz_rows<N_SIDE, DUAL>(row);
+        const uint32_t row = idx / 8, chunk = (idx & 7u) ^ swz_rows(row);
         const uint32_t r = DUAL ? (row >> 5) * 16 + (row & 15u) : row;
         off[i] = r * (uint32_t)ld_bytes + chunk * 16;
       } else {
-        const uint32_t k = idx / (W / 8), chunk = (idx % (W / 8)) ^ swz_cols<N_SIDE>(k);
+        const uint32_t k = idx / (W / 8), chunk = (idx % (W / 8)) ^ swz_cols(k);
         off[i] = (int64_t)chunk * 16 >= width ? OUT : k * (uint32_t)ld_bytes + chunk * 16;
       }
     }
@@ -147,7 +149,7 @@ struct Feed {
       } else {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          const uint32_t row = (i * NT + tid) / 8, chunk = (tid & 7u) ^ swz_rows<N_SIDE, DUAL>(row);
+          const uint32_t row = (i * NT + tid) / 8, chunk = (tid & 7u) ^ swz_rows(row);
           const uint32_t v = (int64_t)chunk * 8 >= k_left ? OUT : off[i];
           __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (i * NT + wave * 64) * 16), 16, v, 0, 0, 0);
         }
@@ -166,29 +168,48 @@ struct Feed {
   }
 };
 
-// 8 sums of one index, from the tile in shared memory: `first` is the wavefront's first index, t its tile of 16
-template <int KIND, int N_SIDE, int DUAL, int W>
-__device__ __forceinline__ s8 fragment(const lds_char *lds, int first, int t, int ks, int lane) {
+// 8 sums of one index of the 16 from `first` on, from the tile in shared memory
+template <int KIND, int W>
+__device__ __forceinline__ s8 fragment(const lds_char *lds, int first, int ks, int lane) {
   const uint32_t q = lane >> 4, c = lane & 15;
   if (KIND == ROWS) {
-    uint32_t row;
-    if (!N_SIDE) row = first + t * 16 + c;
-    else if (DUAL) row = first + (c >> 3) * 32 + (t >> 1) * 16 + ((c >> 2) & 1) * 8 + (t & 1) * 4 + (c & 3);
-    else row = first + (c >> 2) * 16 + t * 4 + (c & 3);
-    const uint32_t chunk = (ks * 4 + q) ^ swz_rows<N_SIDE, DUAL>(row);
+    const uint32_t row = first + c, chunk = (ks * 4 + q) ^ swz_rows(row);
     return *(const __attribute__((address_space(3))) s8 *)(lds + row * (BK * 2) + chunk * 16);
   }
   s4 half[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t k = ks * 32 + q * 8 + h * 4 + (c >> 2);
-    uint32_t chunk, byte;
-    if (!N_SIDE) { chunk = first / 8 + t * 2 + ((c & 3) >> 1); byte = (c & 1) * 8; }
-    else { chunk = first / 8 + (c & 3) * 2 + (t >> 1); byte = (t & 1) * 8; }
-    half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
-        (__attribute__((address_space(3))) s4 *)(lds + k * (W * 2) + (chunk ^ swz_cols<N_SIDE>(k)) * 16 + byte));
+    const uint32_t k = ks * 32 + q * 8 + h * 4 + (c >> 2), chunk = (first / 8 + ((c & 3) >> 1)) ^ swz_cols(k);
+    half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(lds + k * (W * 2) + chunk * 16 + (c & 1) * 8));
   }
   return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
+}
+
+// The fragments of 32 sums of a wavefront's 16 MT x 64 part of the tile
+template <int A_KIND, int B_KIND, int TM, int TN, int MT>
+struct Fragments {
+  enum { READS = (A_KIND == ROWS ? MT : 2 * MT) + (B_KIND == ROWS ? 4 : 8) };
+  s8 a[MT], b[4];
+  __device__ __forceinline__ void read(const lds_char *ta, const lds_char *tb, int wm, int wn, int ks, int lane) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) b[j] = fragment<B_KIND, TN>(tb, wn + j * 16, ks, lane);
+#pragma unroll
+    for (int t = 0; t < MT; ++t) a[t] = fragment<A_KIND, TM>(ta, wm + t * 16, ks, lane);
+  }
+  template <class T> __device__ __forceinline__ void multiply(f4 (&acc)[4][MT]) const {
+#pragma unroll
+    for (int t = 0; t < MT; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) acc[j][t] = T::mfma(b[j], a[t], acc[j][t]);
+  }
+};
+// reads spread between the matrix instructions
+template <int MT, int READS> __device__ __forceinline__ void interleave() {
+#pragma unroll
+  for (int i = 0; i < READS; ++i) {
+    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+    __builtin_amdgcn_sched_group_barrier(0x008, 4 * MT / READS > 0 ? 4 * MT / READS : 1, 0);
+  }
 }
 
 // tile of this workgroup: consecutive tiles of one die (workgroups go round the 8 dies) share operands in its cache, in bands
@@ -210,40 +231,114 @@ template <class T> __device__ __forceinline__ s8 pack8(const float *v) {
   return r;
 }
 
-// stores `count` (<= N) of N consecutive values of one row
-template <class T, int N>
-__device__ __forceinline__ void store_row(const GemmCall &c, void *base, int64_t at, const float *v, int count) {
+// Eight values of row m from column n on: part of a split sum, or a plain output
+template <class T>
+__device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64_t n, const f4 *v) {
+  if (m >= c.m || n >= c.n) return;
+  if (c.splits > 1) {
+    float *p = c.part + ((int64_t)blockIdx.y * c.m + m) * c.ld_part + n;
+    *(f4 *)p = v[0];
+    *(f4 *)(p + 4) = v[1];
+    return;
+  }
+  const int which = m >= c.m_first;
+  const int64_t row = m - (which ? c.m_first : 0), left = c.n_real - n;
+  if (row >= c.m_real || left <= 0) return;
+  const bool whole = c.wide && left >= 8;
   if (c.f32_out) {
-    float *p = (float *)base + at;
-    if (c.wide && count >= N) {
-#pragma unroll
-      for (int i = 0; i < N; i += 4) {
-        f4 w = {v[i], v[i + 1], v[i + 2], v[i + 3]};
-        if (c.accumulate) w += *(const f4 *)(p + i);
-        *(f4 *)(p + i) = w;
-      }
+    float *p = (float *)c.c[which] + row * c.ldc + n;
+    if (whole) {
+      f4 a = v[0], b = v[1];
+      if (c.accumulate) { a += *(const f4 *)p; b += *(const f4 *)(p + 4); }
+      *(f4 *)p = a;
+      *(f4 *)(p + 4) = b;
     } else {
 #pragma unroll
-      for (int i = 0; i < N; ++i)
-        if (i < count) p[i] = v[i] + (c.accumulate ? p[i] : 0.f);
+      for (int e = 0; e < 8; ++e)
+        if (e < left) p[e] = c.accumulate ? v[e >> 2][e & 3] + p[e] : v[e >> 2][e & 3];
     }
     return;
   }
-  uint16_t *p = (uint16_t *)base + at;
-  if (c.wide && count >= N) {
+  uint16_t *p = (uint16_t *)c.c[which] + row * c.ldc + n;
+  float w[8];
 #pragma unroll
-    for (int i = 0; i < N; i += 8) {
-      float w[8];
-      const s8 old = c.accumulate ? *(const s8 *)(p + i) : s8{};
+  for (int e = 0; e < 8; ++e) w[e] = v[e >> 2][e & 3];
+  if (whole) {
+    if (c.accumulate) {
+      const s8 old = *(const s8 *)p;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e] = c.accumulate ? v[i + e] + T::up((uint16_t)old[e]) : v[i + e];
-      *(s8 *)(p + i) = pack8<T>(w);
+      for (int e = 0; e < 8; ++e) w[e] += T::up((uint16_t)old[e]);
     }
+    *(s8 *)p = pack8<T>(w);
   } else {
 #pragma unroll
-    for (int i = 0; i < N; ++i)
-      if (i < count) p[i] = T::down(c.accumulate ? v[i] + T::up(p[i]) : v[i]);
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = T::down(c.accumulate ? w[e] + T::up(p[e]) : w[e]);
   }
+}
+
+// Values kept for the backward pass: rounded to 24 bits (16 of them significant), the upper 16 and the lower 8 apart, 1.5 times the bytes of the
+// tensors' own type.  Rounded to that type they would add an error as large as all others together to every gradient.
+__device__ __forceinline__ void keep8(uint16_t *high, uint8_t *low, int64_t at, const float *v) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  s8 hi;
+  u2 lo = {0, 0};
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t b = keep_bits(v[e]);
+    hi[e] = (short)(b >> 16);
+    lo[e >> 2] |= ((b >> 8) & 0xffu) << (8 * (e & 3));
+  }
+  *(s8 *)(high + at) = hi;
+  *(u2 *)(low + at) = lo;
+}
+__device__ __forceinline__ void kept8(const uint16_t *high, const uint8_t *low, int64_t at, float *v) {
+  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+  const s8 hi = *(const s8 *)(high + at);
+  const u2 lo = *(const u2 *)(low + at);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(((uint32_t)(uint16_t)hi[e] << 16) | (((lo[e >> 2] >> (8 * (e & 3))) & 0xffu) << 8));
+}
+
+// Eight features of both projections (float32 sums): activation and product
+template <class T>
+__device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_t f, const f4 *v) {
+  if (m >= c.m || f >= c.n) return;
+  float g[8], u[8], h[8];
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    g[e] = v[e >> 2][e & 3];
+    u[e] = v[2 + (e >> 2)][e & 3];
+    h[e] = act_of(c.act, g[e]) * u[e];
+    if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;        // rows are whole words of 8, zeros behind the features
+  }
+  *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
+  if (c.kept.gate) {
+    keep8(c.kept.gate, c.kept.gate_low, m * c.ldi + f, g);
+    keep8(c.kept.up, c.kept.up_low, m * c.ldi + f, u);
+  }
+}
+
+// Eight features of dh: the gradients of both projections, and h
+template <class T>
+__device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v) {
+  if (m >= c.m || f >= c.n) return;
+  float g[8], u[8], h[8], dg[8], du[8];
+  kept8(c.kept.gate, c.kept.gate_low, m * c.ldi + f, g);
+  kept8(c.kept.up, c.kept.up_low, m * c.ldi + f, u);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const float dh = v[e >> 2][e & 3];
+    float a, da;
+    act_grad_of(c.act, g[e], a, da);
+    h[e] = a * u[e];
+    du[e] = dh * a;
+    dg[e] = dh * u[e] * da;
+    if (f + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
+  }
+  *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
+  *(s8 *)(c.dgate + m * c.ldd + f) = pack8<T>(dg);
+  *(s8 *)(c.dup + m * c.ldd + f) = pack8<T>(du);
 }
 
 // Both operands of a step, into one of the two buffers
@@ -271,8 +366,8 @@ template <class T, int A_KIND, int B_KIND, int DUAL, int EPI, int WM, int WN, in
 __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(2, 2))) k_gemm(const GemmCall c) {
 #ifdef __HIP_DEVICE_COMPILE__        // the host pass knows no buffer descriptors
   constexpr int NT = 64 * WM * WN, TM = WM * MT * 16, TN = WN * 64;
-  typedef Feed<A_KIND, 0, 0, TM, NT> FeedA;
-  typedef Feed<B_KIND, 1, DUAL, TN, NT> FeedB;
+  typedef Feed<A_KIND, 0, TM, NT> FeedA;
+  typedef Feed<B_KIND, DUAL, TN, NT> FeedB;
   __shared__ __attribute__((aligned(1024))) char shared[2 * (FeedA::BYTES + FeedB::BYTES)];
   lds_char *lds = (lds_char *)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -302,86 +397,63 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
     for (int t = 0; t < MT; ++t) acc[j][t] = f4{0.f, 0.f, 0.f, 0.f};
 
   Fetch<FeedA, FeedB> fetch{c, fa, fb, m0, n0, seg, wave, tid, lds};
-  if (step < last) fetch(step, 0);
+  // Two buffers in shared memory, two sets of fragments in registers: while the matrix instructions of one half of a step run, the
+  // fragments of the next half are read, and the tiles of the step after next are on their way.  One barrier a step: behind
+  // it the next tiles have arrived, and nobody reads the present ones any more.
+  Fragments<A_KIND, B_KIND, TM, TN, MT> half0, half1;
+  const int buffer = FeedA::BYTES + FeedB::BYTES;
+  if (step < last) {
+    fetch(step, 0);
+    __syncthreads();
+    if (step + 1 < last) fetch(step + 1, 1);
+    half0.read(lds, lds + FeedA::BYTES, wm, wn, 0, lane);
+  }
   int buf = 0;
   for (; step < last; ++step, buf ^= 1) {
-    __syncthreads();                        // this step's tiles have arrived, the other buffer is read no more
-    if (step + 1 < last) fetch(step + 1, buf ^ 1);
-    const lds_char *ta = lds + buf * (FeedA::BYTES + FeedB::BYTES), *tb = ta + FeedA::BYTES;
-#pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      s8 b[4];
-#pragma unroll
-      for (int j = 0; j < 4; ++j) b[j] = fragment<B_KIND, 1, DUAL, TN>(tb, wn, j, ks, lane);
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-        const s8 a = fragment<A_KIND, 0, 0, TM>(ta, wm, t, ks, lane);
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j][t] = T::mfma(b[j], a, acc[j][t]);
-      }
-    }
+    const lds_char *now = lds + buf * buffer, *next = lds + (buf ^ 1) * buffer;
+    half1.read(now, now + FeedA::BYTES, wm, wn, 1, lane);
+    half0.template multiply<T>(acc);
+    interleave<MT, Fragments<A_KIND, B_KIND, TM, TN, MT>::READS>();
+    __syncthreads();
+    if (step + 2 < last) fetch(step + 2, buf);
+    half0.read(next, next + FeedA::BYTES, wm, wn, 0, lane);        // behind the last step: stale, and not used
+    half1.template multiply<T>(acc);
+    interleave<MT, Fragments<A_KIND, B_KIND, TM, TN, MT>::READS>();
   }
 
-  const int q = lane >> 4, r = lane & 15;
+  __syncthreads();                          // the tiles are read no more
+  typedef __attribute__((address_space(3))) f4 lds_f4;
+  lds_char *turn = lds + wave * (32 * TURN_ROW);
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    const int64_t m = m0 + wm + t * 16 + r;
-    if (m >= c.m) continue;
-    if (EPI == EPI_ACT) {
-      // 8 features of both projections; the projections are rounded to 16 bits where they are kept for the backward pass,
-      // their product is worked out from the float32 sums
-      const int64_t f = n0 + wn / 2 + q * 8;        // rows of h are whole words of 8: what lies beyond the features is zero
-      if (f >= c.n) continue;
-      float g[8], u[8], h[8];
+  for (int t0 = 0; t0 < MT; t0 += 2) {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        g[e] = acc[e >> 2][t][e & 3];
-        u[e] = acc[2 + (e >> 2)][t][e & 3];
-        h[e] = act_of(c.act, g[e]) * u[e];
-        if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;
-      }
-      *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
-      if (c.gate) {
-        *(s8 *)(c.gate + m * c.ldi + f) = pack8<T>(g);
-        *(s8 *)(c.up + m * c.ldi + f) = pack8<T>(u);
+    for (int t = t0; t < t0 + 2; ++t)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) *(lds_f4 *)(turn + ((t - t0) * 16 + (lane & 15)) * TURN_ROW + (j * 16 + (lane >> 4) * 4) * 4) = acc[j][t];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const int64_t m1 = m0 + wm + t0 * 16;
+    if (DUAL) {
+      // 16 rows of 32 features at a time
+#pragma nounroll
+      for (int r = lane >> 2; r < 32; r += 16) {
+        const int f = (lane & 3) * 8;
+        const lds_char *at = turn + r * TURN_ROW + ((f >> 4) * 32 + (f & 8)) * 4;
+        const f4 v[4] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16), *(const lds_f4 *)(at + 64), *(const lds_f4 *)(at + 80)};
+        finish_pair<T>(c, m1 + r, n0 + wn / 2 + f, v);
       }
     } else {
-      const int64_t n = n0 + wn + q * 16;
-      float v[16];
-#pragma unroll
-      for (int e = 0; e < 16; ++e) v[e] = acc[e >> 2][t][e & 3];
-      if (EPI == EPI_ACT_GRAD) {
-#pragma unroll
-        for (int p = 0; p < 16; p += 8) {
-          if (n + p >= c.n) continue;
-          const s8 gs = *(const s8 *)(c.gate + m * c.ldi + n + p), us = *(const s8 *)(c.up + m * c.ldi + n + p);
-          float h[8], dg[8], du[8];
-#pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const float g = T::up((uint16_t)gs[e]), u = T::up((uint16_t)us[e]);
-            float a, da;
-            act_grad_of(c.act, g, a, da);
-            h[e] = a * u;
-            du[e] = v[p + e] * a;
-            dg[e] = v[p + e] * u * da;
-            if (n + p + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
-          }
-          *(s8 *)(c.h + m * c.ldi + n + p) = pack8<T>(h);
-          *(s8 *)(c.dgate + m * c.ldd + n + p) = pack8<T>(dg);
-          *(s8 *)(c.dup + m * c.ldd + n + p) = pack8<T>(du);
-        }
-      } else if (c.splits > 1) {
-        float *p = c.part + ((int64_t)blockIdx.y * c.m + m) * c.ld_part + n;
-#pragma unroll
-        for (int e = 0; e < 16; e += 4)
-          if (n + e < c.ld_part) *(f4 *)(p + e) = f4{v[e], v[e + 1], v[e + 2], v[e + 3]};
-      } else {
-        const int which = m >= c.m_first;
-        const int64_t row = m - (which ? c.m_first : 0);
-        if (row >= c.m_real || n >= c.n_real) continue;
-        store_row<T, 16>(c, c.c[which], row * c.ldc + n, v, c.n_real - n < 16 ? (int)(c.n_real - n) : 16);
+      // 8 rows of 64 at a time
+#pragma nounroll
+      for (int r = lane >> 3; r < 32; r += 8) {
+        const lds_char *at = turn + r * TURN_ROW + (lane & 7) * 32;
+        const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
+        if (EPI == EPI_ACT_GRAD) finish_gradient<T>(c, m1 + r, n0 + wn + (lane & 7) * 8, v);
+        else finish_plain<T>(c, m1 + r, n0 + wn + (lane & 7) * 8, v);
       }
     }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
   }
 #endif
 }

@@ -88,7 +88,7 @@ def _ffn(x, w_gate, w_up, w_down, activation):
 def ffn_forward(x, w_gate, w_up, w_down, activation="silu", save=False, out=None, stream=None):
     """chm_ffn_forward: y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [tokens, width], w_gate and w_up [features, width],
     w_down [width, features], all bfloat16 or all float16, rows of any stride.  activation: "silu", "gelu", "gelu_tanh".  With
-    save=True returns (y, saved), `saved` being what ffn_backward wants (opaque; 4 bytes per token and feature)."""
+    save=True returns (y, saved), `saved` being what ffn_backward wants (opaque; 6 bytes per token and feature)."""
     d = _ffn(x, w_gate, w_up, w_down, activation)
     if out is not None:
         ld_y = _matrix("out", out, d.tokens, d.width, x.dtype, x.device)

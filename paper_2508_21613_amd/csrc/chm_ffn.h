@@ -17,7 +17,7 @@ struct GemmCall {
   GemmOperand a, b;
   int64_t m, n;                 // sizes of the product (n: features of one weight in a two-weight product)
   int32_t tiles_m, tiles_n;
-  int32_t steps, steps_seg;     // steps of 64 sums over all, steps of the first run of k
+  int32_t runs;                 // 2: a second run of k follows the first, from the operands' second bases
   int32_t splits;               // > 1: the sums are split over blockIdx.y, float32 parts go to `part`
   int32_t act;
   // plain store: c[0] for rows below m_first, c[1] (row m - m_first) from there on; rows up to m_real, columns up to n_real

@@ -45,8 +45,13 @@ __device__ __forceinline__ s8 take8(const uint16_t *row, int k, int n) {
   return v;
 }
 
+__device__ __forceinline__ float act(int kind, float g) {
+  if (kind == CHM_ACT_SILU) return chm_gemm::act_of<CHM_ACT_SILU>(g);
+  return kind == CHM_ACT_GELU ? chm_gemm::act_of<CHM_ACT_GELU>(g) : chm_gemm::act_of<CHM_ACT_GELU_TANH>(g);
+}
+
 __device__ __forceinline__ void keep_pair(const FewCall &c, int64_t at, float g, float u) {
-  const uint32_t bg = chm_gemm::keep_bits(g), bu = chm_gemm::keep_bits(u);
+  const uint32_t bg = __float_as_uint(g), bu = __float_as_uint(u);
   c.kept.gate[at] = (uint16_t)(bg >> 16);
   c.kept.gate_low[at] = (uint8_t)(bg >> 8);
   c.kept.up[at] = (uint16_t)(bu >> 16);
@@ -125,7 +130,7 @@ __global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
     }
     const int64_t col = f0 + feature;
     if (TWO) {
-      c.out[token * c.ldo + col] = T::down(chm_gemm::act_of(c.act, s0) * s1);
+      c.out[token * c.ldo + col] = T::down(act(c.act, s0) * s1);
       if (c.kept.gate) keep_pair(c, token * c.ldo + col, s0, s1);
     } else {
       c.out[token * c.ldo + col] = T::down(s0);
@@ -260,7 +265,8 @@ struct Pass {
     c.splits = 1;
     if (may_split && tile == TILE_128) {
       int64_t s = 512 / (small > 0 ? small : 1);
-      if (s > c.steps / 8) s = c.steps / 8;
+      const int64_t most = (c.a.k > c.b.k ? c.a.k : c.b.k) * c.runs / 512;      // 512 sums a part at least
+      if (s > most) s = most;
       if (s > 8) s = 8;
       if (s > 1) {
         c.splits = (int32_t)s;
@@ -279,11 +285,6 @@ struct Pass {
         hipLaunchKernelGGL((k_join_parts<chm_gemm::F16>), grid, dim3(256), 0, st, c.part, c.splits, c.m, c.ld_part, (int)c.n_real, (uint16_t *)c.c[0], c.ldc);
       ok = ok && hipGetLastError() == hipSuccess;
     }
-  }
-
-  static void run_of_sums(GemmCall &c, int64_t k, int runs) {
-    c.steps_seg = (int32_t)((k + 63) / 64);
-    c.steps = c.steps_seg * runs;
   }
 
   void forward(void *y, int64_t ld_y) {
@@ -318,14 +319,14 @@ struct Pass {
     c.a = GemmOperand{{x.p, x.p}, x.ld, x.cols};
     c.b = GemmOperand{{wg.p, wu.p}, wg.ld, wg.cols};
     c.m = T; c.n = F;
-    run_of_sums(c, x.cols, 1);
+    c.runs = 1;
     c.h = h; c.kept = kept; c.ldi = F8;
     launch(GEMM_GATE_UP, c, false);
     GemmCall d{};
     d.a = GemmOperand{{h, h}, F8, F8};
     d.b = GemmOperand{{wd.p, wd.p}, wd.ld, wd.cols};
     d.m = T; d.n = D;
-    run_of_sums(d, F8, 1);
+    d.runs = 1;
     out(d, y, ld_y, D);
     launch(GEMM_OUT, d, true);
   }
@@ -351,7 +352,7 @@ struct Pass {
     a.a = GemmOperand{{dy.p, dy.p}, dy.ld, dy.cols};
     a.b = GemmOperand{{wd.p, wd.p}, wd.ld, D};
     a.m = T; a.n = F8; a.n_real = F;
-    run_of_sums(a, D, 1);
+    a.runs = 1;
     a.h = h; a.kept = kept; a.ldi = F8;
     a.dgate = d; a.dup = d + F8; a.ldd = 2 * F8;
     launch(GEMM_DH, a, false);
@@ -361,7 +362,7 @@ struct Pass {
     b.a = GemmOperand{{dy.p, dy.p}, dy.ld, T};
     b.b = GemmOperand{{h, h}, F8, T};
     b.m = D; b.n = F8;
-    run_of_sums(b, T, 1);
+    b.runs = 1;
     out(b, g->dw_down, g->ld_dw_down, F);
     grad(b, g, wide_grad);
     launch(GEMM_DW, b, false);
@@ -370,7 +371,7 @@ struct Pass {
     e.a = GemmOperand{{d, d}, 2 * F8, T};
     e.b = GemmOperand{{x.p, x.p}, x.ld, T};
     e.m = 2 * F8; e.n = x.cols;
-    run_of_sums(e, T, 1);
+    e.runs = 1;
     out(e, g->dw_gate, g->ld_dw_gate, D);
     e.c[1] = g->dw_up;
     e.m_first = F8; e.m_real = F;
@@ -381,7 +382,7 @@ struct Pass {
     i.a = GemmOperand{{d, d + F8}, 2 * F8, F8};
     i.b = GemmOperand{{wg.p, wu.p}, wg.ld, F};
     i.m = T; i.n = wg.cols;
-    run_of_sums(i, F8, 2);
+    i.runs = 2;
     out(i, g->dx, g->ld_dx, D);
     launch(GEMM_DX, i, true);
   }

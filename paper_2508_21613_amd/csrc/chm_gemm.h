@@ -12,7 +12,7 @@
 // that read together touch different banks.  The direct loads write linearly, so the permutation is made on their source addresses.
 //
 // The first operand of a matrix instruction is the n side, the second the m side: a lane then holds four consecutive n of one
-// m.  At the end every wavefront turns its sums round in shared memory, 32 rows of 64 at a time, so that a lane goes on with eight
+// m.  At the end every wavefront turns its sums round in shared memory, 64 rows of 64 at a time, so that a lane goes on with eight
 // consecutive n and a row's 64 leave (or meet what they are combined with) as one stretch of memory.  In the two-weight product
 // every 16 rows of the gate's weight are followed by the same rows of the up projection's: a wavefront holds both for 32 features.
 //
@@ -27,6 +27,7 @@
 namespace chm_gemm {
 
 typedef float f4 __attribute__((ext_vector_type(4)));
+typedef int i4 __attribute__((ext_vector_type(4)));
 typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
@@ -48,26 +49,26 @@ struct F16 {
   static __device__ __forceinline__ float up(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
 };
 
-// the activation of g and its derivative, in float32
-__device__ __forceinline__ float act_of(int act, float g) {
-  if (act == CHM_ACT_SILU) return g / (1.f + __expf(-g));
-  if (act == CHM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+// the activation of g and its derivative, in float32; the reciprocal instruction is right to one unit in the last place
+template <int ACT> __device__ __forceinline__ float act_of(float g) {
+  if (ACT == CHM_ACT_SILU) return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
+  if (ACT == CHM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
   // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
   const float z = 0.79788456080286536f * (g + 0.044715f * g * g * g);
-  return g / (1.f + __expf(-2.f * z));
+  return g * __builtin_amdgcn_rcpf(1.f + __expf(-2.f * z));
 }
-__device__ __forceinline__ void act_grad_of(int act, float g, float &a, float &da) {
-  if (act == CHM_ACT_SILU) {
-    const float s = 1.f / (1.f + __expf(-g));
+template <int ACT> __device__ __forceinline__ void act_grad_of(float g, float &a, float &da) {
+  if (ACT == CHM_ACT_SILU) {
+    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
     a = g * s;
     da = s * (1.f + g * (1.f - s));
-  } else if (act == CHM_ACT_GELU) {
+  } else if (ACT == CHM_ACT_GELU) {
     const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
     a = g * p;
     da = p + g * 0.39894228040143268f * __expf(-0.5f * g * g);
   } else {
     const float z = 0.79788456080286536f * (g + 0.044715f * g * g * g);
-    const float s = 1.f / (1.f + __expf(-2.f * z));
+    const float s = __builtin_amdgcn_rcpf(1.f + __expf(-2.f * z));
     a = g * s;
     da = s + 2.f * g * s * (1.f - s) * 0.79788456080286536f * (1.f + 3.f * 0.044715f * g * g);
   }
@@ -75,100 +76,85 @@ __device__ __forceinline__ void act_grad_of(int act, float g, float &a, float &d
 
 enum { ROWS = 0, COLS = 1 };                       // k contiguous / own index contiguous
 enum { EPI_STORE = 0, EPI_ACT = 1, EPI_ACT_GRAD = 2 };
-enum { BK = 64 };
+enum { BK = 64 };                                  // sums of a step
 enum { TURN_ROW = 272 };                           // bytes of 64 float32 and a gap that spreads the rows over the banks
-
-// 24 bits of a float32, rounded to nearest, ties to even; not a number stays one
-__device__ __forceinline__ uint32_t keep_bits(float f) {
-  const uint32_t b = __float_as_uint(f), r = b + 0x7fu + ((b >> 8) & 1u);
-  return f != f ? b | 0x00400000u : r;
-}
-
 
 __device__ __forceinline__ uint32_t swz_rows(uint32_t row) { return row & 7u; }
 __device__ __forceinline__ uint32_t swz_cols(uint32_t k) { return ((k & 3u) << 1) | (((k >> 3) & 1u) << 3); }
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const char *p, int64_t bytes) {
-  const uint32_t n = bytes <= 0 ? 0u : bytes > 0x7fffffff ? 0x7fffffffu : (uint32_t)bytes;
-  return __builtin_amdgcn_make_buffer_rsrc((void *)p, 0, (int)n, 0x00027000);
-}
 
 // One operand's way from memory to shared memory: W of its indices x BK sums a step, by NT threads.
 template <int KIND, int DUAL, int W, int NT>
 struct Feed {
   enum : uint32_t { OUT = 0x7fffffff };
-  enum { NI = W * BK * 2 / 16 / NT, BYTES = W * BK * 2 };
+  enum { CHUNKS = BK / 8, NI = W * BK * 2 / 16 / NT, BYTES = W * BK * 2 };
   const char *base;        // of the tile at the present step
-  int64_t ld_bytes;        // from one row of memory to the next
-  int64_t left;            // ROWS: bytes from base to the end of the tile's last row
-  int64_t k_left;          // sums from the present step's first to the end of the run of k
-  int64_t width;           // bytes of a row from the tile's first index to the operand's edge (COLS), rows of the tile (ROWS)
+  const char *base2;       // of the tile at the second run of k
+  int64_t step_bytes;      // from one step to the next
+  uint32_t ld_bytes;       // from one row of memory to the next
+  uint32_t rows;           // ROWS: rows of the tile less one; COLS: bytes of a row from the tile's first index to the operand's edge
+  int32_t k_left;          // sums from the present step's first to the end of the run of k; below 1: nothing is left
   uint32_t off[NI];
 
-  // at: first index of the tile, size: the operand's indices.  wave: uniform.
-  __device__ __forceinline__ void start(const GemmOperand &o, int64_t at, int64_t size, int tid) {
-    ld_bytes = o.ld * 2;
+  // at: first index of the tile, size: the operand's indices, from sum k0 of the run `seg` on.  wave: uniform.  Two weights side by side:
+  // rows 16 to 31 of every 32 are the second's; the rows of one wavefront's loads belong to one of them.
+  __device__ __forceinline__ void start(const GemmOperand &o, int64_t at, int64_t size, int seg, int64_t k0, int wave, int tid) {
+    ld_bytes = (uint32_t)(o.ld * 2);
+    const char *p = (const char *)(DUAL ? o.p[(wave >> 1) & 1] : o.p[seg]);
+    const int64_t along = KIND == ROWS ? 2 : o.ld * 2, across = KIND == ROWS ? o.ld * 2 : 2;
+    base = p + at * across + k0 * along;
+    base2 = (const char *)o.p[1] + at * across;
+    step_bytes = along * BK;
+    k_left = (int32_t)(o.k - k0);
     if (KIND == ROWS) {
-      const int64_t cap = DUAL ? W / 2 : W, rows = size - at;
-      width = rows < cap ? rows : cap;
+      const int64_t cap = DUAL ? W / 2 : W, n = size - at;
+      rows = (uint32_t)(n < cap ? n : cap) - 1;
     } else {
-      width = (((size + 7) & ~(int64_t)7) - at) * 2;      // whole words of 8: an operand that has no such rows is packed
+      const int64_t w = (((size + 7) & ~(int64_t)7) - at) * 2;      // whole words of 8: an operand that has no such rows is packed
+      rows = (uint32_t)(w < W * 2 ? w : W * 2);
     }
 #pragma unroll
     for (int i = 0; i < NI; ++i) {
       const uint32_t idx = i * NT + tid;
       if (KIND == ROWS) {
-        const uint32_t row = idx / 8, chunk = (idx & 7u) ^ swz_rows(row);
-        const uint32_t r = DUAL ? (row >> 5) * 16 + (row & 15u) : row;
-        off[i] = r * (uint32_t)ld_bytes + chunk * 16;
+        const uint32_t row = idx / CHUNKS, r = DUAL ? (row >> 5) * 16 + (row & 15u) : row;
+        off[i] = r * ld_bytes + chunk_of(i, tid) * 16;
       } else {
         const uint32_t k = idx / (W / 8), chunk = (idx % (W / 8)) ^ swz_cols(k);
-        off[i] = (int64_t)chunk * 16 >= width ? OUT : k * (uint32_t)ld_bytes + chunk * 16;
+        off[i] = chunk * 16 >= rows ? OUT : k * ld_bytes + chunk * 16;
       }
     }
   }
-  // The run of k `seg`, from sum k0 on.  Two weights side by side: rows 16 to 31 of every 32 are the second's; the rows of one
-  // wavefront's loads belong to one of them.
-  __device__ __forceinline__ void seek(const GemmOperand &o, int64_t at, int seg, int64_t k0, int wave) {
-    const char *p = (const char *)(DUAL ? o.p[(wave >> 1) & 1] : o.p[seg]);
-    k_left = o.k - k0;
-    if (KIND == ROWS) {
-      base = p + at * ld_bytes + k0 * 2;
-      left = (width - 1) * ld_bytes + (o.k - k0) * 2;
-    } else {
-      base = p + k0 * ld_bytes + at * 2;
-    }
+  __device__ __forceinline__ static uint32_t chunk_of(int i, int tid) {
+    const uint32_t idx = i * NT + tid;
+    return (idx % CHUNKS) ^ swz_rows(idx / CHUNKS);
   }
-  __device__ __forceinline__ void load(lds_char *lds, int wave, int tid) {
-    if (KIND == ROWS) {
-      const __amdgpu_buffer_rsrc_t r = rsrc_of(base, left);
-      if (k_left >= BK) {
+  // the second run of k begins
+  __device__ __forceinline__ void turn(const GemmOperand &o, bool now) {
+    base = now ? base2 : base;
+    k_left = now ? (int32_t)o.k : k_left;
+  }
+  // a step's loads, one by one
+  i4 rsrc;                 // buffer descriptor: base, bytes, raw 32-bit words
+  uint32_t offset[NI];
+  __device__ __forceinline__ void begin(int tid) {
+    const int32_t left = __builtin_amdgcn_readfirstlane(k_left < 0 ? 0 : k_left < BK ? k_left : BK);
+    // from base to the end of the last element that is there
+    const uint32_t bytes = KIND == ROWS ? rows * ld_bytes + left * 2 : (left - 1) * ld_bytes + rows;
+    const uint64_t at = (uint64_t)base;
+    rsrc = i4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, left > 0 ? (int)bytes : 0, 0x00027000};
 #pragma unroll
-        for (int i = 0; i < NI; ++i)
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
-      } else {
-#pragma unroll
-        for (int i = 0; i < NI; ++i) {
-          const uint32_t row = (i * NT + tid) / 8, chunk = (tid & 7u) ^ swz_rows(row);
-          const uint32_t v = (int64_t)chunk * 8 >= k_left ? OUT : off[i];
-          __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (i * NT + wave * 64) * 16), 16, v, 0, 0, 0);
-        }
-      }
-      base += BK * 2;
-      left -= BK * 2;
-    } else {
-      const int64_t rows = k_left < BK ? k_left : BK;
-      const __amdgpu_buffer_rsrc_t r = rsrc_of(base, (rows - 1) * ld_bytes + width);
-#pragma unroll
-      for (int i = 0; i < NI; ++i)
-        __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)(lds + (i * NT + wave * 64) * 16), 16, off[i], 0, 0, 0);
-      base += BK * ld_bytes;
-    }
+    for (int i = 0; i < NI; ++i) offset[i] = KIND == ROWS && (int32_t)chunk_of(i, tid) * 8 >= left ? (uint32_t)OUT : off[i];
+    base += step_bytes;
     k_left -= BK;
+  }
+  // Written out, because the compiler otherwise waits for all loads under way before every transposing read of shared memory.  It writes no
+  // register; the waits for what it brings are in arrived().
+  __device__ __forceinline__ void one(int i, uint32_t lds, int wave) {
+    asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tbuffer_load_dwordx4 %0, %1, 0 offen lds" ::"v"(offset[i]), "s"(rsrc), "s"(lds + (i * NT + wave * 64) * 16));
   }
 };
 
-// 8 sums of one index of the 16 from `first` on, from the tile in shared memory
+// 8 sums (of the 32 `ks`) of one index of the 16 from `first` on, from the tile in shared memory
 template <int KIND, int W>
 __device__ __forceinline__ s8 fragment(const lds_char *lds, int first, int ks, int lane) {
   const uint32_t q = lane >> 4, c = lane & 15;
@@ -188,29 +174,14 @@ __device__ __forceinline__ s8 fragment(const lds_char *lds, int first, int ks, i
 // The fragments of 32 sums of a wavefront's 16 MT x 64 part of the tile
 template <int A_KIND, int B_KIND, int TM, int TN, int MT>
 struct Fragments {
-  enum { READS = (A_KIND == ROWS ? MT : 2 * MT) + (B_KIND == ROWS ? 4 : 8) };
+  enum { READS = MT + 4 };
   s8 a[MT], b[4];
-  __device__ __forceinline__ void read(const lds_char *ta, const lds_char *tb, int wm, int wn, int ks, int lane) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) b[j] = fragment<B_KIND, TN>(tb, wn + j * 16, ks, lane);
-#pragma unroll
-    for (int t = 0; t < MT; ++t) a[t] = fragment<A_KIND, TM>(ta, wm + t * 16, ks, lane);
-  }
-  template <class T> __device__ __forceinline__ void multiply(f4 (&acc)[4][MT]) const {
-#pragma unroll
-    for (int t = 0; t < MT; ++t)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) acc[j][t] = T::mfma(b[j], a[t], acc[j][t]);
+  // the i-th of READS fragments
+  __device__ __forceinline__ void read(int i, const lds_char *ta, const lds_char *tb, int wm, int wn, int ks, int lane) {
+    if (i < 4) b[i & 3] = fragment<B_KIND, TN>(tb, wn + i * 16, ks, lane);
+    else a[(i - 4) & (MT - 1)] = fragment<A_KIND, TM>(ta, wm + (i - 4) * 16, ks, lane);
   }
 };
-// reads spread between the matrix instructions
-template <int MT, int READS> __device__ __forceinline__ void interleave() {
-#pragma unroll
-  for (int i = 0; i < READS; ++i) {
-    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-    __builtin_amdgcn_sched_group_barrier(0x008, 4 * MT / READS > 0 ? 4 * MT / READS : 1, 0);
-  }
-}
 
 // tile of this workgroup: consecutive tiles of one die (workgroups go round the 8 dies) share operands in its cache, in bands
 // of 8 tiles along m
@@ -277,31 +248,39 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
   }
 }
 
-// Values kept for the backward pass: rounded to 24 bits (16 of them significant), the upper 16 and the lower 8 apart, 1.5 times the bytes of the
-// tensors' own type.  Rounded to that type they would add an error as large as all others together to every gradient.
+// Values kept for the backward pass: the upper 24 bits of float32 (16 of them significant), upper 16 and lower 8 apart, 1.5 times the
+// bytes of the tensors' own type.  Rounded to that type they would add an error as large as all others together to every gradient.
+// Cut off rather than rounded: two byte permutations for four values, and not a number stays one.
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ void keep8(uint16_t *high, uint8_t *low, int64_t at, const float *v) {
-  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-  s8 hi;
-  u2 lo = {0, 0};
+  u4 hi;
+  u2 lo;
 #pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t b = keep_bits(v[e]);
-    hi[e] = (short)(b >> 16);
-    lo[e >> 2] |= ((b >> 8) & 0xffu) << (8 * (e & 3));
+  for (int i = 0; i < 4; ++i) hi[i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302);
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i]), 0x0c0c0501);
+    const uint32_t b = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 3]), __float_as_uint(v[4 * i + 2]), 0x05010c0c);
+    lo[i] = a | b;
   }
-  *(s8 *)(high + at) = hi;
+  *(u4 *)(high + at) = hi;
   *(u2 *)(low + at) = lo;
 }
-__device__ __forceinline__ void kept8(const uint16_t *high, const uint8_t *low, int64_t at, float *v) {
-  typedef uint32_t u2 __attribute__((ext_vector_type(2)));
-  const s8 hi = *(const s8 *)(high + at);
-  const u2 lo = *(const u2 *)(low + at);
+struct Kept8 { u4 hi; u2 lo; };
+__device__ __forceinline__ Kept8 kept8(const uint16_t *high, const uint8_t *low, int64_t at) { return Kept8{*(const u4 *)(high + at), *(const u2 *)(low + at)}; }
+__device__ __forceinline__ void unkeep8(const Kept8 &k, float *v) {
 #pragma unroll
-  for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(((uint32_t)(uint16_t)hi[e] << 16) | (((lo[e >> 2] >> (8 * (e & 3))) & 0xffu) << 8));
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t word = k.hi[e >> 1], bytes = k.lo[e >> 2];
+    // bytes from the top: upper 16 bits of the value, its lower 8, zero
+    const uint32_t sel = (e & 1 ? 0x07060000u : 0x05040000u) | ((uint32_t)(e & 3) << 8) | 0x0cu;
+    v[e] = __uint_as_float(__builtin_amdgcn_perm(word, bytes, sel));
+  }
 }
 
 // Eight features of both projections (float32 sums): activation and product
-template <class T>
+template <class T, int ACT>
 __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_t f, const f4 *v) {
   if (m >= c.m || f >= c.n) return;
   float g[8], u[8], h[8];
@@ -309,58 +288,145 @@ __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_
   for (int e = 0; e < 8; ++e) {
     g[e] = v[e >> 2][e & 3];
     u[e] = v[2 + (e >> 2)][e & 3];
-    h[e] = act_of(c.act, g[e]) * u[e];
-    if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;        // rows are whole words of 8, zeros behind the features
+    h[e] = act_of<ACT>(g[e]) * u[e];
   }
-  *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
+  if (f + 8 > c.n) {                        // rows are whole words of 8, zeros behind the features
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;
+  }
+  const int64_t at = m * c.ldi + f;
+  *(s8 *)(c.h + at) = pack8<T>(h);
   if (c.kept.gate) {
-    keep8(c.kept.gate, c.kept.gate_low, m * c.ldi + f, g);
-    keep8(c.kept.up, c.kept.up_low, m * c.ldi + f, u);
+    keep8(c.kept.gate, c.kept.gate_low, at, g);
+    keep8(c.kept.up, c.kept.up_low, at, u);
   }
 }
 
 // Eight features of dh: the gradients of both projections, and h
-template <class T>
-__device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v) {
+template <class T, int ACT>
+__device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v, const Kept8 &kg, const Kept8 &ku) {
   if (m >= c.m || f >= c.n) return;
   float g[8], u[8], h[8], dg[8], du[8];
-  kept8(c.kept.gate, c.kept.gate_low, m * c.ldi + f, g);
-  kept8(c.kept.up, c.kept.up_low, m * c.ldi + f, u);
+  unkeep8(kg, g);
+  unkeep8(ku, u);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float dh = v[e >> 2][e & 3];
     float a, da;
-    act_grad_of(c.act, g[e], a, da);
+    act_grad_of<ACT>(g[e], a, da);
     h[e] = a * u[e];
     du[e] = dh * a;
     dg[e] = dh * u[e] * da;
-    if (f + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
+  }
+  if (f + 8 > c.n_real) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (f + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
   }
   *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
   *(s8 *)(c.dgate + m * c.ldd + f) = pack8<T>(dg);
   *(s8 *)(c.dup + m * c.ldd + f) = pack8<T>(du);
 }
 
-// Both operands of a step, into one of the two buffers
+typedef __attribute__((address_space(3))) f4 lds_f4;
+
+// A wavefront's ROWS_ rows of 64 sums, turned round in shared memory at `turn`; m1, n1: the first row and column (feature) of them.
+// A loop, not a sequence: code that runs once a tile is read from the cache of instructions' own source, and slowly.
+template <class T, int DUAL, int EPI, int ACT, int ROWS_>
+__device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, int64_t m1, int64_t n1, int lane) {
+  if (DUAL) {                               // 16 rows of 32 features at a time
+    const int f = (lane & 3) * 8;
+#pragma nounroll
+    for (int r = lane >> 2; r < ROWS_; r += 16) {
+      const lds_char *at = turn + r * TURN_ROW + ((f >> 4) * 32 + (f & 8)) * 4;
+      const f4 v[4] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16), *(const lds_f4 *)(at + 64), *(const lds_f4 *)(at + 80)};
+      finish_pair<T, ACT>(c, m1 + r, n1 + f, v);
+    }
+    return;
+  }
+  // 8 rows of 64 at a time
+  const int64_t n = n1 + (lane & 7) * 8;
+  const lds_char *at = turn + (lane >> 3) * TURN_ROW + (lane & 7) * 32;
+  int64_t m = m1 + (lane >> 3);
+  if (EPI == EPI_ACT_GRAD) {                // what is kept of two times 8 rows is on its way
+    const int64_t col = n < c.n ? n : 0, last = c.m - 1;
+    Kept8 kg[2], ku[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int64_t p = (m + i * 8 < last ? m + i * 8 : last) * c.ldi + col;
+      kg[i] = kept8(c.kept.gate, c.kept.gate_low, p);
+      ku[i] = kept8(c.kept.up, c.kept.up_low, p);
+    }
+#pragma nounroll
+    for (int r = 0; r < ROWS_; r += 16) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const Kept8 g = kg[i], u = ku[i];
+        const int64_t p = (m + 16 < last ? m + 16 : last) * c.ldi + col;
+        kg[i] = kept8(c.kept.gate, c.kept.gate_low, p);
+        ku[i] = kept8(c.kept.up, c.kept.up_low, p);
+        const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
+        finish_gradient<T, ACT>(c, m, n, v, g, u);
+        at += 8 * TURN_ROW;
+        m += 8;
+      }
+    }
+    return;
+  }
+#pragma nounroll
+  for (int r = 0; r < ROWS_; r += 8) {
+    const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
+    finish_plain<T>(c, m, n, v);
+    at += 8 * TURN_ROW;
+    m += 8;
+  }
+}
+
+// Both operands of a step, into one of the slots in shared memory; behind the last step zeros arrive: the number of loads under way
+// is the same in every step
 template <class FeedA, class FeedB>
 struct Fetch {
   const GemmCall &c;
-  FeedA &a;
-  FeedB &b;
-  int64_t m0, n0;
-  int seg, wave, tid;
-  lds_char *lds;
-  __device__ __forceinline__ void operator()(int step, int buf) {
-    if (step == c.steps_seg && step > 0 && seg == 0) {
-      seg = 1;
-      a.seek(c.a, m0, 1, 0, wave);
-      b.seek(c.b, n0, 1, 0, wave);
-    }
-    lds_char *to = lds + buf * (FeedA::BYTES + FeedB::BYTES);
-    a.load(to, wave, tid);
-    b.load(to + FeedA::BYTES, wave, tid);
+  FeedA a;
+  FeedB b;
+  int turn_at, wave, tid;
+  uint32_t lds;
+  enum { LOADS = FeedA::NI + FeedB::NI, A_BYTES = FeedA::BYTES, STAGE = FeedA::BYTES + FeedB::BYTES };
+  __device__ __forceinline__ void begin(int step) {
+    a.turn(c.a, step == turn_at);
+    b.turn(c.b, step == turn_at);
+    a.begin(tid);
+    b.begin(tid);
+  }
+  __device__ __forceinline__ void one(int i, int slot) {
+    if (i < FeedA::NI) a.one(i, lds + slot * STAGE, wave);
+    else b.one(i - FeedA::NI, lds + slot * STAGE + A_BYTES, wave);
   }
 };
+
+// waits until at most PENDING loads are under way and all shared memory reads are back, then for the workgroup
+template <int PENDING>
+__device__ __forceinline__ void arrived() {
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(PENDING) : "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// 4 MT matrix instructions on the fragments `now`; between them the fragments `next` are read (from `from`, its sums `ks`) and, with
+// LOAD, the loads of a later step are issued into `slot`
+template <class T, int MT, int LOAD, class F, class G>
+__device__ __forceinline__ void multiply(const F &now, F &next, f4 (&acc)[4][MT], G &fetch, int slot, const lds_char *from, int ks, int wm, int wn, int lane) {
+  constexpr int M = 4 * MT, LOADS = LOAD ? G::LOADS : 0, READS = F::READS;
+#pragma unroll
+  for (int i = 0; i < M; ++i) {
+    if ((i + 1) * LOADS / M > i * LOADS / M) fetch.one(i * LOADS / M, slot);
+    const int r0 = i * READS / M, r1 = (i + 1) * READS / M;
+    if (r1 > r0) next.read(r0, from, from + G::A_BYTES, wm, wn, ks, lane);
+    acc[i & 3][i >> 2] = T::mfma(now.b[i & 3], now.a[i >> 2], acc[i & 3][i >> 2]);
+    __builtin_amdgcn_sched_barrier(0);
+  }
+}
 
 template <class T, int A_KIND, int B_KIND, int DUAL, int EPI, int WM, int WN, int MT>
 __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(2, 2))) k_gemm(const GemmCall c) {
@@ -368,7 +434,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
   constexpr int NT = 64 * WM * WN, TM = WM * MT * 16, TN = WN * 64;
   typedef Feed<A_KIND, 0, TM, NT> FeedA;
   typedef Feed<B_KIND, DUAL, TN, NT> FeedB;
-  __shared__ __attribute__((aligned(1024))) char shared[2 * (FeedA::BYTES + FeedB::BYTES)];
+  typedef Fragments<A_KIND, B_KIND, TM, TN, MT> Frags;
+  constexpr int STAGE = FeedA::BYTES + FeedB::BYTES, LOADS = FeedA::NI + FeedB::NI;
+  __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE > WM * WN * 64 * TURN_ROW ? 2 * STAGE : WM * WN * 64 * TURN_ROW];
   lds_char *lds = (lds_char *)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int tm, tn;
@@ -376,19 +444,18 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
   const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * (DUAL ? TN / 2 : TN);
   const int wm = (wave / WN) * (MT * 16), wn = (wave % WN) * 64;
 
-  int step = 0, last = c.steps;
+  // steps of this workgroup
+  const int steps_seg = (int)((c.a.k > c.b.k ? c.a.k : c.b.k) + BK - 1) / BK, steps = steps_seg * c.runs;
+  int step = 0, last = steps;
   if (c.splits > 1) {
-    step = (int)((int64_t)c.steps * blockIdx.y / c.splits);
-    last = (int)((int64_t)c.steps * (blockIdx.y + 1) / c.splits);
+    step = (int)((int64_t)steps * blockIdx.y / c.splits);
+    last = (int)((int64_t)steps * (blockIdx.y + 1) / c.splits);
   }
-  FeedA fa;
-  FeedB fb;
-  fa.start(c.a, m0, c.m, tid);
-  fb.start(c.b, n0, c.n, tid);
-  int seg = step >= c.steps_seg;
-  const int64_t k0 = (int64_t)(step - seg * c.steps_seg) * BK;
-  fa.seek(c.a, m0, seg, k0, wave);
-  fb.seek(c.b, n0, seg, k0, wave);
+  Fetch<FeedA, FeedB> fetch{c, {}, {}, c.runs > 1 ? steps_seg : -1, wave, tid, (uint32_t)(uintptr_t)lds};
+  const int seg = c.runs > 1 && step >= steps_seg;
+  const int64_t k0 = (int64_t)(step - seg * steps_seg) * BK;
+  fetch.a.start(c.a, m0, c.m, seg, k0, wave, tid);
+  fetch.b.start(c.b, n0, c.n, seg, k0, wave, tid);
 
   f4 acc[4][MT];
 #pragma unroll
@@ -396,62 +463,43 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[j][t] = f4{0.f, 0.f, 0.f, 0.f};
 
-  Fetch<FeedA, FeedB> fetch{c, fa, fb, m0, n0, seg, wave, tid, lds};
-  // Two buffers in shared memory, two sets of fragments in registers: while the matrix instructions of one half of a step run, the
-  // fragments of the next half are read, and the tiles of the step after next are on their way.  One barrier a step: behind
-  // it the next tiles have arrived, and nobody reads the present ones any more.
-  Fragments<A_KIND, B_KIND, TM, TN, MT> half0, half1;
-  const int buffer = FeedA::BYTES + FeedB::BYTES;
+  // Two buffers in shared memory, two sets of fragments in registers.  While the matrix instructions of 32 sums run, the
+  // fragments of the next 32 are read, and in a step's second half the loads of the step after next are issued: all of them
+  // spread between the matrix instructions, which they would hold up if they were issued in a row.  One barrier a step: behind it
+  // the next step's tiles have arrived, and the present ones have been read by everybody.
+  Frags even, odd;
   if (step < last) {
-    fetch(step, 0);
-    __syncthreads();
-    if (step + 1 < last) fetch(step + 1, 1);
-    half0.read(lds, lds + FeedA::BYTES, wm, wn, 0, lane);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      fetch.begin(step + i);
+#pragma unroll
+      for (int l = 0; l < LOADS; ++l) fetch.one(l, i);
+    }
+    arrived<LOADS>();
+#pragma unroll
+    for (int i = 0; i < Frags::READS; ++i) even.read(i, lds, lds + FeedA::BYTES, wm, wn, 0, lane);
   }
-  int buf = 0;
-  for (; step < last; ++step, buf ^= 1) {
-    const lds_char *now = lds + buf * buffer, *next = lds + (buf ^ 1) * buffer;
-    half1.read(now, now + FeedA::BYTES, wm, wn, 1, lane);
-    half0.template multiply<T>(acc);
-    interleave<MT, Fragments<A_KIND, B_KIND, TM, TN, MT>::READS>();
-    __syncthreads();
-    if (step + 2 < last) fetch(step + 2, buf);
-    half0.read(next, next + FeedA::BYTES, wm, wn, 0, lane);        // behind the last step: stale, and not used
-    half1.template multiply<T>(acc);
-    interleave<MT, Fragments<A_KIND, B_KIND, TM, TN, MT>::READS>();
+  for (int slot = 0; step < last; ++step, slot ^= 1) {
+    multiply<T, MT, 0>(even, odd, acc, fetch, slot, lds + slot * STAGE, 1, wm, wn, lane);
+    fetch.begin(step + 2);
+    arrived<0>();
+    multiply<T, MT, 1>(odd, even, acc, fetch, slot, lds + (slot ^ 1) * STAGE, 0, wm, wn, lane);
   }
 
-  __syncthreads();                          // the tiles are read no more
-  typedef __attribute__((address_space(3))) f4 lds_f4;
-  lds_char *turn = lds + wave * (32 * TURN_ROW);
+  arrived<0>();                             // the tiles are read no more, and nothing is under way to them
+  lds_char *turn = lds + wave * (64 * TURN_ROW);
 #pragma unroll
-  for (int t0 = 0; t0 < MT; t0 += 2) {
+  for (int t0 = 0; t0 < MT; t0 += 4) {
 #pragma unroll
-    for (int t = t0; t < t0 + 2; ++t)
+    for (int t = t0; t < t0 + 4; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) *(lds_f4 *)(turn + ((t - t0) * 16 + (lane & 15)) * TURN_ROW + (j * 16 + (lane >> 4) * 4) * 4) = acc[j][t];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const int64_t m1 = m0 + wm + t0 * 16;
-    if (DUAL) {
-      // 16 rows of 32 features at a time
-#pragma nounroll
-      for (int r = lane >> 2; r < 32; r += 16) {
-        const int f = (lane & 3) * 8;
-        const lds_char *at = turn + r * TURN_ROW + ((f >> 4) * 32 + (f & 8)) * 4;
-        const f4 v[4] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16), *(const lds_f4 *)(at + 64), *(const lds_f4 *)(at + 80)};
-        finish_pair<T>(c, m1 + r, n0 + wn / 2 + f, v);
-      }
-    } else {
-      // 8 rows of 64 at a time
-#pragma nounroll
-      for (int r = lane >> 3; r < 32; r += 8) {
-        const lds_char *at = turn + r * TURN_ROW + (lane & 7) * 32;
-        const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
-        if (EPI == EPI_ACT_GRAD) finish_gradient<T>(c, m1 + r, n0 + wn + (lane & 7) * 8, v);
-        else finish_plain<T>(c, m1 + r, n0 + wn + (lane & 7) * 8, v);
-      }
-    }
+    const int64_t m1 = m0 + wm + t0 * 16, n1 = n0 + (DUAL ? wn / 2 : wn);
+    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, 64>(c, turn, m1, n1, lane);
+    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, 64>(c, turn, m1, n1, lane);
+    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, 64>(c, turn, m1, n1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }

@@ -82,7 +82,7 @@ def formula(x, wg, wu, wd, act, dy=None):
     if dy is None:
         return out
     dy = dy.double()
-    vg, vu = vg + (2.0 ** -16 * g) ** 2 / 3, vu + (2.0 ** -16 * u) ** 2 / 3     # kept in 24 bits (16 significant) between the passes
+    vg, vu = vg + (2.0 ** -15 * g) ** 2 / 3, vu + (2.0 ** -15 * u) ** 2 / 3     # 24 bits (16 significant) are kept between the passes
     vh = rounded(h, dtype) + (da * u) ** 2 * vg + a ** 2 * vu + (8 * ACC * h) ** 2
     dh = dy @ wd
     vdh = summed(dy, wd, D)

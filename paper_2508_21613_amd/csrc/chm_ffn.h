@@ -35,7 +35,10 @@ struct GemmCall {
 };
 
 enum { GEMM_GATE_UP = 0, GEMM_OUT = 1, GEMM_DH = 2, GEMM_DX = 3, GEMM_DW = 4 };
-enum { TILE_256 = 0, TILE_128 = 1 };
+// Tiles of 256 x 256, two steps in shared memory; of 128 x 128, two steps (two workgroups a compute unit) or four (one: a step's loads
+// have three steps' time to arrive).  All of 8 wavefronts: with 4 the 128 x 128 ones take 1.1 to 1.4 times as long, since nothing
+// runs while a wavefront issues loads.
+enum { TILE_256 = 0, TILE_128 = 1, TILE_128_DEEP = 2 };
 // Largest row of memory (elements) that the tile kernels take: 256 rows lie within 2^31 bytes.  Longer ones are packed.
 constexpr int64_t GEMM_LD_MAX = 1 << 21;
 // Launches one product; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.

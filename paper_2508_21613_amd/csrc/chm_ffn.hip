@@ -254,18 +254,21 @@ struct Pass {
     b = packed(b, must);
   }
 
-  // Tile by the number of tiles (256 compute units take one of 256 x 256 or two of 128 x 128 at a time), and the sums split where even
-  // the small tiles leave compute units idle (`may_split`: the product has a plain 16-bit output of `n` columns)
+  // The kind of tile with the least time by the number of rounds over the 256 compute units; the units are microseconds of a round at 4,096
+  // sums: 256 x 256 tiles 83, 128 x 128 ones 37 for up to 256 of them (one a compute unit), 66 for every 512 (measured: 2,048 x 4,096 83 and
+  // 66, 1,024 x 4,096 79 and 37, 512 x 22,016 83 and 132, 4,096 x 11,008 240 and 400).  Where the small tiles leave compute units idle
+  // and the output is plain (`may_split`), the sums are split as well, 512 of them a part at least.
   void launch(int product, GemmCall &c, bool may_split) {
     const int64_t n_all = product == GEMM_GATE_UP ? 2 * c.n : c.n;
     const int64_t big = ((c.m + 255) / 256) * ((n_all + 255) / 256), small = ((c.m + 127) / 128) * ((n_all + 127) / 128);
-    const int tile = big >= 192 ? TILE_256 : TILE_128, side = tile == TILE_256 ? 256 : 128;
+    const int64_t time_big = (big + 255) / 256 * 83, time_small = small <= 256 ? 37 : (small + 511) / 512 * 66;
+    const int tile = time_big < time_small ? TILE_256 : small <= 256 ? TILE_128_DEEP : TILE_128, side = tile == TILE_256 ? 256 : 128;
     c.tiles_m = (int32_t)((c.m + side - 1) / side);
     c.tiles_n = (int32_t)((n_all + side - 1) / side);
     c.splits = 1;
-    if (may_split && tile == TILE_128) {
-      int64_t s = 512 / (small > 0 ? small : 1);
-      const int64_t most = (c.a.k > c.b.k ? c.a.k : c.b.k) * c.runs / 512;      // 512 sums a part at least
+    if (may_split && tile == TILE_128_DEEP) {
+      int64_t s = 256 / (small > 0 ? small : 1);
+      const int64_t most = (c.a.k > c.b.k ? c.a.k : c.b.k) * c.runs / 512;
       if (s > most) s = most;
       if (s > 8) s = 8;
       if (s > 1) {

@@ -428,15 +428,16 @@ __device__ __forceinline__ void multiply(const F &now, F &next, f4 (&acc)[4][MT]
   }
 }
 
-template <class T, int A_KIND, int B_KIND, int DUAL, int EPI, int WM, int WN, int MT>
-__global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(2, 2))) k_gemm(const GemmCall c) {
+template <class T, int A_KIND, int B_KIND, int DUAL, int EPI, int WM, int WN, int MT, int SLOTS>
+__global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(MT == 2 && SLOTS == 2 ? 4 : 2))) k_gemm(const GemmCall c) {
 #ifdef __HIP_DEVICE_COMPILE__        // the host pass knows no buffer descriptors
   constexpr int NT = 64 * WM * WN, TM = WM * MT * 16, TN = WN * 64;
   typedef Feed<A_KIND, 0, TM, NT> FeedA;
   typedef Feed<B_KIND, DUAL, TN, NT> FeedB;
   typedef Fragments<A_KIND, B_KIND, TM, TN, MT> Frags;
   constexpr int STAGE = FeedA::BYTES + FeedB::BYTES, LOADS = FeedA::NI + FeedB::NI;
-  __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE > WM * WN * 64 * TURN_ROW ? 2 * STAGE : WM * WN * 64 * TURN_ROW];
+  constexpr int TURN = MT < 4 ? MT * 16 : 64;        // rows turned round at a time
+  __shared__ __attribute__((aligned(1024))) char shared[SLOTS * STAGE > WM * WN * TURN * TURN_ROW ? SLOTS * STAGE : WM * WN * TURN * TURN_ROW];
   lds_char *lds = (lds_char *)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int tm, tn;
@@ -463,43 +464,45 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
 #pragma unroll
     for (int t = 0; t < MT; ++t) acc[j][t] = f4{0.f, 0.f, 0.f, 0.f};
 
-  // Two buffers in shared memory, two sets of fragments in registers.  While the matrix instructions of 32 sums run, the
-  // fragments of the next 32 are read, and in a step's second half the loads of the step after next are issued: all of them
+  // SLOTS buffers in shared memory, two sets of fragments in registers.  While the matrix instructions of 32 sums run, the
+  // fragments of the next 32 are read, and in a step's second half the loads of the step SLOTS ahead are issued: all of them
   // spread between the matrix instructions, which they would hold up if they were issued in a row.  One barrier a step: behind it
   // the next step's tiles have arrived, and the present ones have been read by everybody.
   Frags even, odd;
   if (step < last) {
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < SLOTS; ++i) {
       fetch.begin(step + i);
 #pragma unroll
       for (int l = 0; l < LOADS; ++l) fetch.one(l, i);
     }
-    arrived<LOADS>();
+    arrived<(SLOTS - 1) * LOADS>();
 #pragma unroll
     for (int i = 0; i < Frags::READS; ++i) even.read(i, lds, lds + FeedA::BYTES, wm, wn, 0, lane);
   }
-  for (int slot = 0; step < last; ++step, slot ^= 1) {
+  for (int slot = 0; step < last; ++step) {
     multiply<T, MT, 0>(even, odd, acc, fetch, slot, lds + slot * STAGE, 1, wm, wn, lane);
-    fetch.begin(step + 2);
-    arrived<0>();
-    multiply<T, MT, 1>(odd, even, acc, fetch, slot, lds + (slot ^ 1) * STAGE, 0, wm, wn, lane);
+    fetch.begin(step + SLOTS);
+    arrived<(SLOTS - 2) * LOADS>();
+    const int next = slot + 1 == SLOTS ? 0 : slot + 1;
+    multiply<T, MT, 1>(odd, even, acc, fetch, slot, lds + next * STAGE, 0, wm, wn, lane);
+    slot = next;
   }
 
   arrived<0>();                             // the tiles are read no more, and nothing is under way to them
-  lds_char *turn = lds + wave * (64 * TURN_ROW);
+  lds_char *turn = lds + wave * (TURN * TURN_ROW);
 #pragma unroll
-  for (int t0 = 0; t0 < MT; t0 += 4) {
+  for (int t0 = 0; t0 < MT; t0 += TURN / 16) {
 #pragma unroll
-    for (int t = t0; t < t0 + 4; ++t)
+    for (int t = t0; t < t0 + TURN / 16; ++t)
 #pragma unroll
       for (int j = 0; j < 4; ++j) *(lds_f4 *)(turn + ((t - t0) * 16 + (lane & 15)) * TURN_ROW + (j * 16 + (lane >> 4) * 4) * 4) = acc[j][t];
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int64_t m1 = m0 + wm + t0 * 16, n1 = n0 + (DUAL ? wn / 2 : wn);
-    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, 64>(c, turn, m1, n1, lane);
-    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, 64>(c, turn, m1, n1, lane);
-    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, 64>(c, turn, m1, n1, lane);
+    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, TURN>(c, turn, m1, n1, lane);
+    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, TURN>(c, turn, m1, n1, lane);
+    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, TURN>(c, turn, m1, n1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
@@ -509,8 +512,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
 template <class T, int A_KIND, int B_KIND, int DUAL, int EPI>
 bool launch_product(int tile, const GemmCall &c, hipStream_t st) {
   const dim3 grid((uint32_t)(c.tiles_m * c.tiles_n), (uint32_t)(c.splits > 1 ? c.splits : 1));
-  if (tile == TILE_256) hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 2, 4, 8>), grid, dim3(512), 0, st, c);
-  else hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 2, 2, 4>), grid, dim3(256), 0, st, c);
+  if (tile == TILE_256) hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 2, 4, 8, 2>), grid, dim3(512), 0, st, c);
+  else if (tile == TILE_128_DEEP) hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 4, 2, 2, 4>), grid, dim3(512), 0, st, c);
+  else hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 4, 2, 2, 2>), grid, dim3(512), 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
 

@@ -24,7 +24,13 @@ using chm_gemm::s8;
 // the first operand of the matrix instructions: every byte of a weight is read once, by one wavefront, 64 contiguous bytes a
 // lane quad and step.  The tokens (16 for each instruction, absent ones are zero and not loaded) come from the cache.  The
 // wavefronts of a workgroup share the sums and add them up through shared memory, in order.  Weights may start anywhere.
-constexpr int FEW_MAX = 64;
+// Tokens up to which these kernels run rather than the tiles: 16, 32 with small weights, 64 with smaller ones.  From there on the
+// tokens' fragments, which every wavefront reads for itself, cost more than the tiles' fixed time (us, these kernels and tiles: width 4,096,
+// 11,008 features, 16 tokens 70 and 70, 32 tokens 93 and 70; 2,048 x 5,504: 16 tokens 32 and 33, 32 tokens 39 and 34; 1,024 x 2,752: 32 tokens
+// 21 and 24, 48 tokens 27 and 24; 512 x 1,376: 64 tokens 21 and 22).
+bool few_tokens(int64_t tokens, int64_t width, int64_t features) {
+  return tokens <= 16 || (tokens <= 32 && width * features <= 1 << 22) || (tokens <= 64 && width * features <= 1 << 20);
+}
 
 struct FewCall {
   const uint16_t *x, *w0, *w1;
@@ -58,10 +64,46 @@ __device__ __forceinline__ void keep_pair(const FewCall &c, int64_t at, float g,
   c.kept.up_low[at] = (uint8_t)(bu >> 8);
 }
 
+// wavefronts of a workgroup at most: two steps and more of several tiles take more registers than 16 of them leave
+constexpr int few_waves_most(int tiles) { return tiles == 1 ? 16 : 8; }
+
+// 64 sums: 16 of every lane's feature and of its token of each tile
+template <int TWO, int TILES>
+struct FewStep {
+  s8 a[TWO + 1][2], b[TILES][2];
+  __device__ __forceinline__ void load(const FewCall &c, const uint16_t *w0, const uint16_t *w1, int k, bool whole, int q, int r) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int at = k + h * 32 + q * 8;
+      a[0][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(w0 + at))) : take8(w0, at, c.k);
+      if (TWO) a[TWO][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(w1 + at))) : take8(w1, at, c.k);
+    }
+#pragma unroll
+    for (int t = 0; t < TILES; ++t) {
+      const int token = t * 16 + r < c.tokens ? t * 16 + r : c.tokens - 1;        // an absent one: the last again, its sums are dropped
+      const uint16_t *x = c.x + token * c.ldx;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int at = k + h * 32 + q * 8;
+        b[t][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(x + at))) : take8(x, at, c.k);
+      }
+    }
+  }
+  template <class T> __device__ __forceinline__ void multiply(f4 (&acc)[2][TILES]) const {
+#pragma unroll
+    for (int t = 0; t < TILES; ++t)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int w = 0; w <= TWO; ++w) acc[w][t] = T::mfma(a[w][h], b[t][h], acc[w][t]);
+  }
+};
+
 template <class T, int TWO, int TILES>
-__global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
+__global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCall c) {
   extern __shared__ float part[];             // [wavefronts][TWO + 1][TILES][64][4]
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6;
+  // uniform: a matrix instruction does not heed which lanes are switched off
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int q = lane >> 4, r = lane & 15;
   const int f0 = blockIdx.x * 16, f = f0 + r < c.rows ? f0 + r : c.rows - 1;
   const uint16_t *w0 = c.w0 + f * c.ld0, *w1 = TWO ? c.w1 + f * c.ld1 : nullptr;
@@ -69,45 +111,36 @@ __global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
 #pragma unroll
   for (int t = 0; t < TILES; ++t) acc[0][t] = acc[1][t] = f4{0.f, 0.f, 0.f, 0.f};
 
-  const auto step = [&](int k, bool whole) {
-    s8 a0[2], a1[2], b[TILES][2];
+  // DEPTH steps of 64 sums are under way.  All loads are issued whatever the number of steps (a step too many reads the last one
+  // again), and none depends on a branch: else the waits in front of the matrix instructions would be for all of them.  Workgroups
+  // begin at different sums, so that they do not all ask the same channels of the cache for the tokens.
+  constexpr int DEPTH = TWO && TILES > 2 ? 3 : 4;
+  const int whole = c.k / 64, last = whole - 1;
+  if (wave < whole) {
+    const int turn = (int)((blockIdx.x >> 3) % (uint32_t)whole);
+    const auto at = [&](int i) {
+      i = (i < last ? i : last) + turn;
+      return (i < whole ? i : i - whole) * 64;
+    };
+    FewStep<TWO, TILES> set[DEPTH];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int at = k + q * 16 + h * 8;
-      if (whole) {
-        a0[h] = __builtin_bit_cast(s8, load16((const char *)(w0 + at)));
-        if (TWO) a1[h] = __builtin_bit_cast(s8, load16((const char *)(w1 + at)));
-      } else {
-        a0[h] = take8(w0, at, c.k);
-        if (TWO) a1[h] = take8(w1, at, c.k);
+    for (int d = 0; d < DEPTH; ++d) set[d].load(c, w0, w1, at(wave + d * waves), true, q, r);
+    int i = wave;
+    for (; i + DEPTH * waves < whole; i += DEPTH * waves)
+#pragma unroll
+      for (int d = 0; d < DEPTH; ++d) {
+        set[d].template multiply<T>(acc);
+        set[d].load(c, w0, w1, at(i + (d + DEPTH) * waves), true, q, r);
       }
-    }
 #pragma unroll
-    for (int t = 0; t < TILES; ++t) {
-      const int token = t * 16 + r;
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = k + q * 16 + h * 8;
-        s8 v = {};
-        if (token < c.tokens) {
-          const uint16_t *x = c.x + token * c.ldx;
-          v = whole ? __builtin_bit_cast(s8, load16((const char *)(x + at))) : take8(x, at, c.k);
-        }
-        b[t][h] = v;
-      }
-    }
-#pragma unroll
-    for (int t = 0; t < TILES; ++t)
-#pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        acc[0][t] = T::mfma(a0[h], b[t][h], acc[0][t]);
-        if (TWO) acc[1][t] = T::mfma(a1[h], b[t][h], acc[1][t]);
-      }
-  };
-  const int whole = c.k / 64;
-  int i = wave;
-  for (; i < whole; i += waves) step(i * 64, true);
-  if (i * 64 < c.k) step(i * 64, false);
+    for (int d = 0; d < DEPTH; ++d)
+      if (i + d * waves < whole) set[d].template multiply<T>(acc);
+  }
+  if (c.k % 64 && wave == whole % waves) {
+    FewStep<TWO, TILES> rest;
+    rest.load(c, w0, w1, whole * 64, false, q, r);
+    rest.template multiply<T>(acc);
+  }
 
 #pragma unroll
   for (int t = 0; t < TILES; ++t)
@@ -139,20 +172,21 @@ __global__ void __launch_bounds__(1024) k_few_tokens(FewCall c) {
 }
 
 // wavefronts of a workgroup: some 16 a compute unit over all, with four steps of 64 sums each at least
-int few_waves(int64_t rows, int64_t k) {
+int few_waves(int64_t rows, int64_t k, int tiles) {
   const int64_t groups = (rows + 15) / 16, steps = (k + 63) / 64;
   int w = 1;
-  while (w < 16 && groups * w < 4096 && steps >= w * 8) w <<= 1;
+  while (w < few_waves_most(tiles) && groups * w < 4096 && steps >= w * 8) w <<= 1;
   return w;
 }
 
 template <class T, int TWO>
 bool launch_few(const FewCall &c, hipStream_t st) {
   const dim3 grid((c.rows + 15) / 16);
-  const int w = few_waves(c.rows, c.k), tiles = c.tokens <= 16 ? 1 : c.tokens <= 32 ? 2 : 4;
+  const int tiles = (c.tokens + 15) / 16, w = few_waves(c.rows, c.k, tiles);
   const size_t bytes = (size_t)w * (TWO + 1) * tiles * 1024;
   if (tiles == 1) hipLaunchKernelGGL((k_few_tokens<T, TWO, 1>), grid, dim3(w * 64), bytes, st, c);
   else if (tiles == 2) hipLaunchKernelGGL((k_few_tokens<T, TWO, 2>), grid, dim3(w * 64), bytes, st, c);
+  else if (tiles == 3) hipLaunchKernelGGL((k_few_tokens<T, TWO, 3>), grid, dim3(w * 64), bytes, st, c);
   else hipLaunchKernelGGL((k_few_tokens<T, TWO, 4>), grid, dim3(w * 64), bytes, st, c);
   return hipGetLastError() == hipSuccess;
 }
@@ -294,7 +328,7 @@ struct Pass {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
     const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
-    if (T <= FEW_MAX) {
+    if (few_tokens(T, D, F)) {
       if (!run || T == 0) return;
       FewCall c{};
       c.tokens = (int32_t)T;

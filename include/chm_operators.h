@@ -75,7 +75,7 @@ int chm_embedding_lookup(int32_t dtype, int32_t index_bits, const void *tokens, 
 /* grad[v] = scale * sum of dy[t] over the t with tokens[t] = v, in the order of t (accumulate: grad[v] +=, rows that no token
  * names are not touched).  grad is of the type of dy or CHM_F32.  n below 2^31, rows below 2^31.
  * Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
-int chm_embedding_gradient_scratch(int64_t n, int64_t width, uint64_t *bytes);
+int chm_embedding_gradient_scratch(int64_t n, int64_t rows, int64_t width, uint64_t *bytes);
 int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t index_bits, const void *tokens, int64_t n, const void *dy,
                            int64_t ld_dy, int64_t rows, int64_t width, float scale, void *grad, int64_t ld_grad, int32_t accumulate,
                            void *scratch, uint64_t scratch_bytes, void *hip_stream);

@@ -168,7 +168,7 @@ def lib():
         L.chm_ffn_forward.argtypes = [C.POINTER(Ffn), vp, i64, vp, u64, vp]
         L.chm_ffn_backward.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), vp, u64, vp]
         L.chm_embedding_lookup.argtypes = [i32, i32, vp, i64, vp, i64, i64, i64, C.c_float, vp, i64, vp]
-        L.chm_embedding_gradient_scratch.argtypes = [i64, i64, C.POINTER(u64)]
+        L.chm_embedding_gradient_scratch.argtypes = [i64, i64, i64, C.POINTER(u64)]
         L.chm_embedding_gradient.argtypes = [i32, i32, i32, vp, i64, vp, i64, i64, i64, C.c_float, vp, i64, i32, vp, u64, vp]
         L.chm_load_gradients.argtypes = [C.POINTER(Gradient), i32, C.POINTER(vp)]
         L.chm_gradient_sumsq.argtypes = [vp, vp, vp]

@@ -80,7 +80,7 @@ __device__ __forceinline__ void piece_scale(const char *p, char *o, int bytes, f
       L::up(x[i], v);
 #pragma unroll
       for (int e = 0; e < L::N; ++e) v[e] *= c;
-      store16(o + (i * THREADS + threadIdx.x) * 16, L::down(v));
+      store16_past(o + (i * THREADS + threadIdx.x) * 16, L::down(v));
     }
     return;
   }
@@ -90,7 +90,7 @@ __device__ __forceinline__ void piece_scale(const char *p, char *o, int bytes, f
       L::up(load16(p + at), v);
 #pragma unroll
       for (int e = 0; e < L::N; ++e) v[e] *= c;
-      store16(o + at, L::down(v));
+      store16_past(o + at, L::down(v));
     } else {
       for (int b = at; b < bytes; b += L::SIZE) L::put(o + b, L::one(p + b) * c);
     }

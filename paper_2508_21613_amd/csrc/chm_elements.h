@@ -22,6 +22,8 @@ __device__ __forceinline__ uint32_t f16_down(float f) { return __builtin_bit_cas
 
 __device__ __forceinline__ Words load16(const char *p) { return *(const CHM_GLOBAL WordsAnywhere *)p; }
 __device__ __forceinline__ void store16(char *p, Words x) { *(CHM_GLOBAL WordsAnywhere *)p = x; }
+// past the caches: for results that are larger than they are (lookup of 16,384 rows of 8 KiB: 44 us with store16, 30 with this)
+__device__ __forceinline__ void store16_past(char *p, Words x) { __builtin_nontemporal_store((WordsAnywhere)x, (CHM_GLOBAL WordsAnywhere *)p); }
 
 // The N values of 16 bytes as float32, and back
 template <int DT> struct Lane;

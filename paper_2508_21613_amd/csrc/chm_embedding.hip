@@ -19,8 +19,9 @@ namespace {
 using namespace chm_elements;
 
 constexpr int NT = 256;
+typedef float f4 __attribute__((ext_vector_type(4)));
 constexpr int SMALL = 256;               // places the unsorted kernel takes
-constexpr int ONE_GROUP = 16384;         // places one workgroup sorts in its shared memory (128 KiB of pairs)
+constexpr int RANGES_MAX = 16384, RANGE_ROWS = 512 * 512 - 1;      // places and rows the sort by ranges of keys takes
 constexpr int BINS = 512, DIGIT = 9;
 constexpr int SORT_GROUPS = 64;
 constexpr int ZERO_ROWS = 32;            // rows that a workgroup sets to zero where no token names them
@@ -39,6 +40,23 @@ __device__ __forceinline__ uint32_t key_of(const Tokens &t, int64_t i) {
   const uint64_t v = ((const CHM_GLOBAL uint64_t *)t.p)[i];
   return v < t.rows ? (uint32_t)v : t.rows;
 }
+// the keys of the places first, first + 64, ...; ~0, behind everything, from place n on.  All loads are issued before any is used.
+template <int N>
+__device__ __forceinline__ void keys_of(const Tokens &t, int first, int n, uint32_t *key) {
+  if (t.bits == 32) {
+    uint32_t v[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) v[r] = ((const CHM_GLOBAL uint32_t *)t.p)[first + r * 64 < n ? first + r * 64 : n - 1];
+#pragma unroll
+    for (int r = 0; r < N; ++r) key[r] = first + r * 64 >= n ? ~0u : v[r] < t.rows ? v[r] : t.rows;
+  } else {
+    uint64_t v[N];
+#pragma unroll
+    for (int r = 0; r < N; ++r) v[r] = ((const CHM_GLOBAL uint64_t *)t.p)[first + r * 64 < n ? first + r * 64 : n - 1];
+#pragma unroll
+    for (int r = 0; r < N; ++r) key[r] = first + r * 64 >= n ? ~0u : v[r] < t.rows ? (uint32_t)v[r] : t.rows;
+  }
+}
 
 // ---------------------------------------------------------------------------------------------- rows in pieces of 16 bytes
 // `count` (<= N) values of a row as float32; the rest 0
@@ -52,12 +70,15 @@ __device__ __forceinline__ void row_load(const char *p, int count, float *v) {
     for (int e = 0; e < L::N; ++e) v[e] = e < count ? L::one(p + e * L::SIZE) : 0.f;
   }
 }
-template <int DT, int N>
+template <int DT, int N, int PAST>
 __device__ __forceinline__ void row_store(char *p, int count, const float *v) {
   typedef Lane<DT> L;
   if (count >= N) {
 #pragma unroll
-    for (int i = 0; i < N / L::N; ++i) store16(p + i * 16, L::down(v + i * L::N));
+    for (int i = 0; i < N / L::N; ++i) {
+      if (PAST) store16_past(p + i * 16, L::down(v + i * L::N));
+      else store16(p + i * 16, L::down(v + i * L::N));
+    }
   } else {
 #pragma unroll
     for (int e = 0; e < N; ++e)
@@ -116,7 +137,7 @@ __global__ void __launch_bounds__(NT) k_lookup(Lookup c) {
 #pragma unroll
   for (int r = 0; r < ROWS; ++r) {
     const int64_t t = first + (int64_t)r * down;
-    if (t < c.n) row_store<DT, L::N>(c.out + t * c.ld_out + (int64_t)col * L::SIZE, left, v[r]);
+    if (t < c.n) row_store<DT, L::N, (ROWS > 1)>(c.out + t * c.ld_out + (int64_t)col * L::SIZE, left, v[r]);
   }
 }
 
@@ -132,75 +153,64 @@ __device__ __forceinline__ uint64_t same_digit(uint32_t d, int bits) {
   return m;
 }
 
-// One workgroup, n <= 16,384: the pairs stay in shared memory.
-__global__ void __launch_bounds__(1024) k_sort_one(Tokens tokens, int n, int passes, int digit, uint32_t *keys, uint32_t *places) {
-  __shared__ uint32_t lk[ONE_GROUP], lp[ONE_GROUP];
-  __shared__ __attribute__((aligned(16))) uint16_t counts[BINS * 16];
-  __shared__ uint32_t totals[16];
+// n <= 16,384 and at most 512 x 512 rows: every workgroup takes 512 neighbouring keys.  It looks at all tokens: those below its keys give
+// the place where its own begin, its own are counted by key and wavefront, and then put where they belong, in order.  Nothing is written
+// in between, and one launch sorts; all workgroups read the same 64 or 128 KiB from the cache.
+__global__ void __launch_bounds__(1024) k_sort_ranges(Tokens tokens, int n, uint32_t *keys, uint32_t *places, uint8_t *named) {
+  __shared__ __attribute__((aligned(16))) uint32_t counts[BINS * 16];           // [key][wavefront]
+  __shared__ uint32_t totals[16], belows[16];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int rounds = (n + 1023) / 1024, first = wave * rounds * 64;
-  uint32_t key[16], place[16], rank[16];
+  const uint32_t base = blockIdx.x * BINS;
+  const int rounds = (n + 1023) / 1024, first = wave * rounds * 64 + lane, end = (wave + 1) * rounds * 64;
+  for (int i = threadIdx.x; i < BINS * 16 / 4; i += 1024) ((Words *)counts)[i] = Words{0, 0, 0, 0};
+  uint32_t key[16];
+  keys_of<16>(tokens, first, n < end ? n : end, key);
+  __syncthreads();
+  uint32_t below = 0;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const int i = first + r * 64 + lane;
-    key[r] = r < rounds && i < n ? key_of(tokens, i) : ~0u;       // behind everything
-    place[r] = i;
+    if (r >= rounds) continue;
+    below += __popcll(__ballot(key[r] < base));
+    if (key[r] - base < BINS) atomicAdd(&counts[(key[r] - base) * 16 + wave], 1u);
   }
-  for (int pass = 0; pass < passes; ++pass) {
-    const int shift = pass * digit;
-    const uint32_t mask = (1u << digit) - 1;
-    *(Words *)(counts + threadIdx.x * 8) = Words{0, 0, 0, 0};
-    __syncthreads();
-    volatile uint16_t *mine = counts + wave;
+  if (lane == 0) belows[wave] = below;
+  __syncthreads();
+  // exclusive sums over (key, wavefront), 8 entries a thread, behind all smaller keys
+  uint32_t c[8], sum = 0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (r >= rounds) continue;
-      const uint32_t d = (key[r] >> shift) & mask;
-      const uint64_t m = same_digit(d, digit);
-      const uint32_t before = mine[d * 16];
-      rank[r] = before + __popcll(m & ((1ull << lane) - 1));
-      __builtin_amdgcn_wave_barrier();
-      if ((m >> lane) == 1) mine[d * 16] = (uint16_t)(before + __popcll(m));   // the group's last lane
-      __builtin_amdgcn_wave_barrier();
-    }
-    __syncthreads();
-    // exclusive sums over (digit, wavefront), 8 entries a thread
-    uint32_t c[8], sum = 0;
+  for (int e = 0; e < 8; ++e) { c[e] = counts[threadIdx.x * 8 + e]; sum += c[e]; }
+  const uint32_t both = sum + __shfl_xor(sum, 1);
+  if (!(threadIdx.x & 1) && base + threadIdx.x / 2 < tokens.rows) named[base + threadIdx.x / 2] = both != 0;
+  uint32_t incl = sum;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) { c[e] = counts[threadIdx.x * 8 + e]; sum += c[e]; }
-    uint32_t incl = sum;
-#pragma unroll
-    for (int d = 1; d < 64; d <<= 1) {
-      const uint32_t o = __shfl_up(incl, d);
-      if (lane >= d) incl += o;
-    }
-    if (lane == 63) totals[wave] = incl;
-    __syncthreads();
-    uint32_t at = incl - sum;
-    for (int w = 0; w < wave; ++w) at += totals[w];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) { counts[threadIdx.x * 8 + e] = (uint16_t)at; at += c[e]; }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (r >= rounds) continue;
-      const uint32_t to = counts[((key[r] >> shift) & mask) * 16 + wave] + rank[r];
-      lk[to] = key[r];
-      lp[to] = place[r];
-    }
-    __syncthreads();
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (r >= rounds) continue;
-      key[r] = lk[first + r * 64 + lane];
-      place[r] = lp[first + r * 64 + lane];
-    }
-    __syncthreads();
+  for (int d = 1; d < 64; d <<= 1) {
+    const uint32_t o = __shfl_up(incl, d);
+    if (lane >= d) incl += o;
   }
+  if (lane == 63) totals[wave] = incl;
+  __syncthreads();
+  uint32_t at = incl - sum;
+  for (int w = 0; w < 16; ++w) at += belows[w] + (w < wave ? totals[w] : 0u);
+#pragma unroll
+  for (int e = 0; e < 8; ++e) { counts[threadIdx.x * 8 + e] = at; at += c[e]; }
+  __syncthreads();
+  volatile uint32_t *mine = counts + wave;
 #pragma unroll
   for (int r = 0; r < 16; ++r) {
-    const int i = first + r * 64 + lane;
-    if (r < rounds && i < n) { keys[i] = key[r]; places[i] = place[r]; }
+    if (r >= rounds) continue;
+    const bool in = key[r] - base < BINS;
+    const uint64_t ins = __ballot(in);
+    if (!ins) continue;
+    const uint32_t d = in ? key[r] - base : 0;
+    const uint64_t m = __popcll(ins) == 1 ? ins : same_digit(d, DIGIT) & ins;
+    if (in) {
+      const uint32_t to = mine[d * 16];
+      const uint32_t p = to + __popcll(m & ((1ull << lane) - 1));
+      keys[p] = key[r];
+      places[p] = first + r * 64;
+      if ((m >> lane) == 1) mine[d * 16] = to + __popcll(m);        // the group's last lane; the wavefront's reads are behind it
+    }
+    __builtin_amdgcn_wave_barrier();
   }
 }
 
@@ -209,6 +219,7 @@ struct SortPass {
   Tokens tokens;                          // first pass: keys come from here, places are the indices
   const uint32_t *keys_in, *places_in;    // null in the first pass
   uint32_t *keys, *places, *counts;       // counts: [workgroup][BINS]
+  uint8_t *named;                         // first pass: which rows are named by a token
   int64_t n;
   int32_t stretch, shift, digit;          // stretch: items of a workgroup, a multiple of 512
 };
@@ -222,6 +233,8 @@ __global__ void __launch_bounds__(SORT_NT) k_sort_count(SortPass c) {
   __syncthreads();
   const int64_t first = (int64_t)blockIdx.x * c.stretch, last = first + c.stretch < c.n ? first + c.stretch : c.n;
   const uint32_t mask = (1u << c.digit) - 1;
+  if (!c.keys_in)
+    for (int64_t i = (int64_t)blockIdx.x * SORT_NT + threadIdx.x; i < c.tokens.rows; i += (int64_t)gridDim.x * SORT_NT) c.named[i] = 0;
   for (int64_t i = first + threadIdx.x; i < last; i += SORT_NT) atomicAdd(&counts[(pass_key(c, i) >> c.shift) & mask], 1u);
   __syncthreads();
   c.counts[(int64_t)blockIdx.x * BINS + threadIdx.x] = counts[threadIdx.x];
@@ -240,6 +253,7 @@ __global__ void __launch_bounds__(SORT_NT) k_sort_move(SortPass c) {
   for (int64_t i = first + lane; i < last; i += 64) atomicAdd(&counts[((pass_key(c, i) >> c.shift) & mask) * WAVES + wave], 1u);
   // where this workgroup's items of digit threadIdx.x start: all smaller digits, and this one in the workgroups before
   uint32_t all = 0, before = 0;
+#pragma unroll 16
   for (uint32_t g = 0; g < gridDim.x; ++g) {
     const uint32_t v = c.counts[(int64_t)g * BINS + threadIdx.x];
     if (g < blockIdx.x) before += v;
@@ -277,6 +291,7 @@ __global__ void __launch_bounds__(SORT_NT) k_sort_move(SortPass c) {
       const uint32_t to = base + __popcll(m & ((1ull << lane) - 1));
       c.keys[to] = key;
       c.places[to] = place;
+      if (!c.keys_in && key < c.tokens.rows) c.named[key] = 1;
     }
     __builtin_amdgcn_wave_barrier();
   }
@@ -286,6 +301,7 @@ __global__ void __launch_bounds__(SORT_NT) k_sort_move(SortPass c) {
 struct Gather {
   Tokens tokens;
   const uint32_t *keys, *places;         // sorted
+  const uint8_t *named;                  // [rows]: some token names the row
   const char *dy;
   char *grad;
   float *part;                           // [pieces][2][width rounded up to 8]
@@ -302,21 +318,11 @@ __device__ __forceinline__ void finish_row(const Gather &c, uint32_t key, int co
 #pragma unroll
   for (int e = 0; e < N; ++e) v[e] *= c.scale;
   if (c.accumulate) row_add<GT, N>(p, left, v);
-  row_store<GT, N>(p, left, v);
+  row_store<GT, N, 1>(p, left, v);
 }
 
 __device__ __forceinline__ int64_t part_row(const Gather &c, int64_t piece, int slot) {
   return (piece * 2 + slot) * ((c.width + 7) & ~7);
-}
-
-// first place in the sorted list whose key is not below `key`
-__device__ __forceinline__ int64_t lower_bound(const uint32_t *keys, int64_t n, uint32_t key) {
-  int64_t lo = 0, hi = n;
-  while (lo < hi) {
-    const int64_t mid = (lo + hi) >> 1;
-    if (keys[mid] < key) lo = mid + 1; else hi = mid;
-  }
-  return lo;
 }
 
 // rows [first, first + ZERO_ROWS) without a token, of which `named` knows
@@ -327,7 +333,7 @@ __device__ __forceinline__ void zero_rows(const Gather &c, int64_t first, const 
   const int groups = (c.width + N - 1) / N;
   for (int i = threadIdx.x; i < ZERO_ROWS * groups; i += NT) {
     const int r = i / groups, col = (i - r * groups) * N;
-    if (!named[r]) row_store<GT, N>(c.grad + (first + r) * c.ld_grad + (int64_t)col * Lane<GT>::SIZE, c.width - col, zero);
+    if (!named[r]) row_store<GT, N, 1>(c.grad + (first + r) * c.ld_grad + (int64_t)col * Lane<GT>::SIZE, c.width - col, zero);
   }
 }
 
@@ -340,15 +346,7 @@ __global__ void __launch_bounds__(NT) k_runs(Gather c) {
     if (blockIdx.y) return;
     __shared__ uint8_t named[ZERO_ROWS];
     const int64_t first = (int64_t)(blockIdx.x - c.piece_groups) * ZERO_ROWS;
-    if (threadIdx.x < ZERO_ROWS) {
-      const int64_t r = first + threadIdx.x;
-      uint8_t there = 1;
-      if (r < c.tokens.rows) {
-        const int64_t at = lower_bound(c.keys, c.n, (uint32_t)r);
-        there = at < c.n && c.keys[at] == (uint32_t)r;
-      }
-      named[threadIdx.x] = there;
-    }
+    if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x < c.tokens.rows ? c.named[first + threadIdx.x] : 1;
     __syncthreads();
     zero_rows<GT>(c, first, named);
     return;
@@ -398,42 +396,68 @@ __global__ void __launch_bounds__(NT) k_runs(Gather c) {
   }
 }
 
-// runs that cross pieces: the piece in which one starts adds up what the others have left, in order
+// Runs that cross pieces: the piece in which one starts adds up what the others have left, in order.  A workgroup takes 256 columns of
+// JOIN_PIECES pieces, its four wavefronts a quarter of every run each, so that the most frequent token's run (some ten percent of the places)
+// is no chain of additions as long as its pieces.
+constexpr int JOIN_PIECES = 8;
 template <int GT>
 __global__ void __launch_bounds__(NT) k_join(Gather c) {
   constexpr int N = 4, AT_ONCE = 8;
-  const int x = threadIdx.x % c.across, y = threadIdx.x / c.across, down = NT / c.across;
-  const int64_t piece = (int64_t)blockIdx.x * down + y;
-  const int col = (blockIdx.y * c.across + x) * N, left = c.width - col;
-  if (piece + 1 >= c.pieces || left <= 0) return;
-  const int64_t lo = piece * c.piece, hi = lo + c.piece;
-  const uint32_t key = c.keys[hi - 1];
-  if (key >= c.tokens.rows || key != c.keys[hi]) return;
-  if (c.keys[lo] == key && lo > 0 && c.keys[lo - 1] == key) return;       // it has come from before
-  const int64_t last = (lower_bound(c.keys + hi, c.n - hi, key + 1) + hi - 1) / c.piece;
-  float sum[N];
-  Lane<CHM_F32>::up(*(const Words *)(c.part + part_row(c, piece, 1) + col), sum);
-  for (int64_t q0 = piece + 1; q0 <= last; q0 += AT_ONCE) {
-    Words w[AT_ONCE];
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) w[u] = *(const Words *)(c.part + part_row(c, q0 + u < last ? q0 + u : last, 0) + col);
-#pragma unroll
-    for (int u = 0; u < AT_ONCE; ++u) {
-      if (q0 + u > last) break;
-      float v[N];
-      Lane<CHM_F32>::up(w[u], v);
-#pragma unroll
-      for (int e = 0; e < N; ++e) sum[e] += v[e];
-    }
+  __shared__ f4 sums[NT];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = (blockIdx.y * 64 + lane) * N, left = c.width - col;
+  // pieces of this workgroup in which a run starts that goes on behind them
+  uint32_t key = 0;
+  bool starts = false;
+  const int64_t piece = (int64_t)blockIdx.x * JOIN_PIECES + lane;
+  if (lane < JOIN_PIECES && piece + 1 < c.pieces) {
+    const int64_t lo = piece * c.piece, hi = lo + c.piece;
+    key = c.keys[hi - 1];
+    starts = key < c.tokens.rows && key == c.keys[hi] && !(c.keys[lo] == key && lo > 0 && c.keys[lo - 1] == key);
   }
-  // float32 rows are 16 bytes of 4 columns, 16-bit rows 8 bytes: stored one by one where N columns are no 16 bytes
-  char *to = c.grad + key * c.ld_grad + (int64_t)col * Lane<GT>::SIZE;
+  uint64_t todo = __ballot(starts);
+  while (todo) {
+    const int l = __ffsll((unsigned long long)todo) - 1;
+    todo &= todo - 1;
+    const uint32_t k = __builtin_amdgcn_readlane(key, l);
+    const int64_t p = (int64_t)blockIdx.x * JOIN_PIECES + l;
+    int64_t last = p;                       // the last piece that begins with the key
+    for (bool more = true; more;) {
+      const int64_t q = last + 1 + lane;
+      const uint64_t same = __ballot(q < c.pieces && c.keys[q < c.pieces ? q * c.piece : 0] == k);
+      more = same == ~0ull;
+      last += more ? 64 : __ffsll((unsigned long long)~same) - 1;
+    }
+    // parts: slot 1 of piece p, slot 0 of p + 1 .. last
+    const int count = (int)(last - p) + 1, from = count * wave / 4, to = count * (wave + 1) / 4;
+    f4 sum = {0.f, 0.f, 0.f, 0.f};
+    if (left > 0)
+      for (int i0 = from; i0 < to; i0 += AT_ONCE) {
+        f4 v[AT_ONCE];
 #pragma unroll
-  for (int e = 0; e < N; ++e) {
-    if (e >= left) break;
-    float v = sum[e] * c.scale;
-    if (c.accumulate) v += Lane<GT>::one(to + e * Lane<GT>::SIZE);
-    Lane<GT>::put(to + e * Lane<GT>::SIZE, v);
+        for (int u = 0; u < AT_ONCE; ++u) {
+          const int i = i0 + u < to ? i0 + u : to - 1;
+          v[u] = *(const CHM_GLOBAL f4 *)(c.part + part_row(c, p + i, i == 0) + col);
+        }
+#pragma unroll
+        for (int u = 0; u < AT_ONCE; ++u)
+          if (i0 + u < to) sum += v[u];
+      }
+    sums[threadIdx.x] = sum;
+    __syncthreads();
+    if (wave == 0 && left > 0) {
+      sum = sums[lane] + sums[64 + lane] + sums[128 + lane] + sums[192 + lane];
+      float v[N] = {sum[0], sum[1], sum[2], sum[3]};
+      char *to_row = c.grad + k * c.ld_grad + (int64_t)col * Lane<GT>::SIZE;
+#pragma unroll
+      for (int e = 0; e < N; ++e) {
+        if (e >= left) break;
+        v[e] *= c.scale;
+        if (c.accumulate) v[e] += Lane<GT>::one(to_row + e * Lane<GT>::SIZE);
+        Lane<GT>::put(to_row + e * Lane<GT>::SIZE, v[e]);
+      }
+    }
+    __syncthreads();
   }
 }
 
@@ -505,23 +529,25 @@ int across_of(int64_t groups) {
   return a;
 }
 
-// places of a piece: about 1,024 pieces and more, 8 to 64 places each
+// places of a piece: about 512 pieces and more, 8 to 64 places each
 int piece_of(int64_t n) {
   int p = 8;
-  while (p < 64 && n / p > 1024) p <<= 1;
+  while (p < 64 && n / p > 512) p <<= 1;
   return p;
 }
 
-struct Scratch { uint64_t keys[2], places[2], counts, part, bytes; };
+struct Scratch { uint64_t keys[2], places[2], counts, named, part, bytes; };
 
-Scratch scratch_of(int64_t n, int64_t width) {
+bool by_ranges(int64_t n, int64_t rows) { return n <= RANGES_MAX && rows <= RANGE_ROWS; }
+
+Scratch scratch_of(int64_t n, int64_t rows, int64_t width) {
   Scratch s{};
   if (n <= SMALL) return s;
   uint64_t at = 0;
   const auto take = [&](uint64_t bytes) { const uint64_t o = at; at += (bytes + 255) & ~255ull; return o; };
-  const int sets = n > ONE_GROUP ? 2 : 1;
-  for (int i = 0; i < sets; ++i) { s.keys[i] = take(n * 4); s.places[i] = take(n * 4); }
-  if (sets == 2) s.counts = take((uint64_t)SORT_GROUPS * BINS * 4);
+  for (int i = 0; i < 2; ++i) { s.keys[i] = take(n * 4); s.places[i] = take(n * 4); }
+  s.counts = take((uint64_t)SORT_GROUPS * BINS * 4);
+  s.named = take(rows);
   const int64_t pieces = (n + piece_of(n) - 1) / piece_of(n);
   s.part = take((uint64_t)pieces * 2 * ((width + 7) & ~7ll) * 4);
   s.bytes = at;
@@ -538,16 +564,13 @@ bool launch_few(const Gather &c, hipStream_t st) {
 
 template <int DT, int GT>
 bool launch_runs(Gather c, hipStream_t st) {
-  int64_t groups = (c.width + Lane<DT>::N - 1) / Lane<DT>::N;
+  const int64_t groups = (c.width + Lane<DT>::N - 1) / Lane<DT>::N;
   c.across = across_of(groups);
-  int down = NT / c.across;
+  const int down = NT / c.across;
   c.piece_groups = (c.pieces + down - 1) / down;
   const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
   hipLaunchKernelGGL((k_runs<DT, GT>), dim3((uint32_t)(c.piece_groups + zero), (uint32_t)((groups + c.across - 1) / c.across)), dim3(NT), 0, st, c);
-  groups = (c.width + 3) / 4;
-  c.across = across_of(groups);
-  down = NT / c.across;
-  hipLaunchKernelGGL((k_join<GT>), dim3((uint32_t)((c.pieces + down - 1) / down), (uint32_t)((groups + c.across - 1) / c.across)), dim3(NT), 0, st, c);
+  hipLaunchKernelGGL((k_join<GT>), dim3((uint32_t)((c.pieces + JOIN_PIECES - 1) / JOIN_PIECES), (uint32_t)((c.width + 255) / 256)), dim3(NT), 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -557,7 +580,7 @@ bool launch_lookup(Lookup c, hipStream_t st) {
   c.across = across_of(groups);
   const uint32_t cols = (uint32_t)((groups + c.across - 1) / c.across);
   const int down = NT / c.across;
-  if (c.n >= 4096) hipLaunchKernelGGL((k_lookup<DT, 4>), dim3((uint32_t)((c.n + 4 * down - 1) / (4 * down)), cols), dim3(NT), 0, st, c);
+  if (c.n >= 4096) hipLaunchKernelGGL((k_lookup<DT, 2>), dim3((uint32_t)((c.n + 2 * down - 1) / (2 * down)), cols), dim3(NT), 0, st, c);
   else hipLaunchKernelGGL((k_lookup<DT, 1>), dim3((uint32_t)((c.n + down - 1) / down), cols), dim3(NT), 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
@@ -590,9 +613,9 @@ extern "C" int chm_embedding_lookup(int32_t dtype, int32_t index_bits, const voi
   return ok ? CHM_OK : CHM_ERR_HIP;
 }
 
-extern "C" int chm_embedding_gradient_scratch(int64_t n, int64_t width, uint64_t *bytes) {
-  if (!bytes || n < 0 || n > INT32_MAX || width < 1 || width > (1 << 24)) return CHM_ERR_ARG;
-  *bytes = scratch_of(n, width).bytes;
+extern "C" int chm_embedding_gradient_scratch(int64_t n, int64_t rows, int64_t width, uint64_t *bytes) {
+  if (!bytes || n < 0 || n > INT32_MAX || rows < 0 || rows > INT32_MAX || width < 1 || width > (1 << 24)) return CHM_ERR_ARG;
+  *bytes = scratch_of(n, rows, width).bytes;
   return CHM_OK;
 }
 
@@ -607,7 +630,7 @@ extern "C" int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t
     return CHM_ERR_ARG;
   if (rows == 0) return CHM_OK;
   if (!grad || (n > 0 && (!tokens || !dy))) return CHM_ERR_ARG;
-  const Scratch s = scratch_of(n, width);
+  const Scratch s = scratch_of(n, rows, width);
   if (s.bytes && !scratch) return CHM_ERR_ARG;
   if (scratch_bytes < s.bytes) return CHM_ERR_LIMIT;
   hipStream_t st = (hipStream_t)hip_stream;
@@ -627,15 +650,16 @@ extern "C" int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t
     while (bits < 32 && (uint64_t)rows >> bits) ++bits;                  // keys 0 .. rows
     const int passes = (bits + DIGIT - 1) / DIGIT, digit = (bits + passes - 1) / passes;
     uint32_t *keys = (uint32_t *)(mem + s.keys[0]), *places = (uint32_t *)(mem + s.places[0]);
-    if (n <= ONE_GROUP) {
-      hipLaunchKernelGGL(k_sort_one, dim3(1), dim3(1024), 0, st, c.tokens, (int)n, passes, digit, keys, places);
+    if (by_ranges(n, rows)) {
+      hipLaunchKernelGGL(k_sort_ranges, dim3((uint32_t)(rows / BINS + 1)), dim3(1024), 0, st, c.tokens, (int)n, keys, places, (uint8_t *)(mem + s.named));
     } else {
       SortPass p{};
       p.tokens = c.tokens;
       p.counts = (uint32_t *)(mem + s.counts);
+      p.named = (uint8_t *)(mem + s.named);
       p.n = n;
       int64_t stretch = (n + SORT_GROUPS - 1) / SORT_GROUPS;
-      if (stretch < 4096) stretch = 4096;
+      if (stretch < 1024) stretch = 1024;
       stretch = (stretch + 511) & ~511ll;
       p.stretch = (int32_t)stretch;
       p.digit = digit;
@@ -653,6 +677,7 @@ extern "C" int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t
     }
     c.keys = keys;
     c.places = places;
+    c.named = (const uint8_t *)(mem + s.named);
     c.part = (float *)(mem + s.part);
     c.piece = piece_of(n);
     c.pieces = (int32_t)((n + c.piece - 1) / c.piece);

@@ -14,6 +14,7 @@ import torch
 from . import binding as B
 
 DTYPES = {torch.float32: 0, torch.bfloat16: 1, torch.float16: 2}
+INDEX_BITS = {torch.int32: 32, torch.int64: 64}
 ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2}
 
 
@@ -23,148 +24,163 @@ def _need(ok, what):
 
 
 def _matrix(name, t, rows=None, cols=None, dtype=None, device=None):
-    """checks a row-major matrix (unit stride along rows) and returns the elements from one row to the next"""
-    _need(isinstance(t, torch.Tensor) and t.dim() == 2, name + " must be a matrix")
-    _need(t.is_cuda, name + " must be on the GPU")
-    _need(device is None or t.device == device, name + " must be on the same GPU as the others")
-    _need(dtype is None or t.dtype == dtype, "%s must be %s" % (name, dtype))
-    _need((rows is None or t.shape[0] == rows) and (cols is None or t.shape[1] == cols),
-          "%s must be %s x %s, is %s" % (name, rows, cols, tuple(t.shape)))
-    _need(t.shape[1] <= 1 or t.stride(1) == 1, name + " must have unit stride along its rows")
-    if t.shape[0] <= 1:
-        return max(t.shape[1], 1)
-    _need(t.stride(0) >= t.shape[1], name + "'s rows must not overlap")
-    return max(t.stride(0), 1)
+    """checks a row-major matrix (unit stride along rows) and returns the elements from one row to the next; device: an index"""
+    if not isinstance(t, torch.Tensor):
+        raise B.ChmError(B.ERR_ARG, name + " must be a tensor")
+    shape = t.shape
+    if len(shape) != 2:
+        raise B.ChmError(B.ERR_ARG, name + " must be a matrix")
+    r, c = shape
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise B.ChmError(B.ERR_ARG, name + " must be on the GPU, the same as the others")
+    if dtype is not None and t.dtype != dtype:
+        raise B.ChmError(B.ERR_ARG, "%s must be %s" % (name, dtype))
+    if (rows is not None and r != rows) or (cols is not None and c != cols):
+        raise B.ChmError(B.ERR_ARG, "%s must be %s x %s, is %d x %d" % (name, rows, cols, r, c))
+    ld, step = t.stride()
+    if c > 1 and step != 1:
+        raise B.ChmError(B.ERR_ARG, name + " must have unit stride along its rows")
+    if r <= 1:
+        return c or 1
+    if ld < c:
+        raise B.ChmError(B.ERR_ARG, name + "'s rows must not overlap")
+    return ld or 1
 
 
-class _Stream:
-    """the stream of a call, made current for the allocations within"""
+class _Other:
+    """another stream or device than the current one, made current for the launches and allocations within"""
 
     def __init__(self, stream, device):
-        current = torch.cuda.current_stream(device)
         if isinstance(stream, int):
-            stream = torch.cuda.ExternalStream(stream, device=device)
-        self.other = stream is not None and stream != current
+            stream = torch.cuda.ExternalStream(stream, device=torch.device("cuda", device))
+        self.scopes = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
         self.device = device
-        self.scope = torch.cuda.stream(stream) if self.other else None
-        self.ptr = C.c_void_p((stream if self.other else current).cuda_stream)
 
     def __enter__(self):
-        self.guard = None
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        if self.scope is not None:
-            self.scope.__enter__()
+        for scope in self.scopes:
+            scope.__enter__()
+        return torch._C._cuda_getCurrentRawStream(self.device)
+
+    def __exit__(self, *exc):
+        for scope in reversed(self.scopes):
+            scope.__exit__(*exc)
+
+
+class _Current:
+    """the current stream of the current device: nothing to change"""
+
+    def __init__(self, ptr):
+        self.ptr = ptr
+
+    def __enter__(self):
         return self.ptr
 
     def __exit__(self, *exc):
-        if self.scope is not None:
-            self.scope.__exit__(*exc)
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+        pass
 
 
-def _bytes(n, device):
-    return torch.empty(max(int(n), 16), dtype=torch.uint8, device=device)
+def _scope(stream, device):
+    """scope of a call on the GPU of that index: the stream to launch on, current for what is allocated within"""
+    if stream is None and torch._C._cuda_getDevice() == device:
+        return _Current(torch._C._cuda_getCurrentRawStream(device))
+    return _Other(stream, device)
+
+
+def _bytes(n, like):
+    return like.new_empty(max(n, 16), dtype=torch.uint8)
 
 
 def _ffn(x, w_gate, w_up, w_down, activation):
-    _need(activation in ACTIVATIONS, "activation must be one of %s" % ", ".join(ACTIVATIONS))
+    """the call's description, its sizes, type and GPU"""
+    _need(activation in ACTIVATIONS, "activation must be silu, gelu or gelu_tanh")
     ld_x = _matrix("x", x)
-    _need(x.dtype in (torch.bfloat16, torch.float16), "x must be bfloat16 or float16")
+    dtype, dev = x.dtype, x.get_device()
+    _need(dtype in (torch.bfloat16, torch.float16), "x must be bfloat16 or float16")
     T, D = x.shape
-    d = B.Ffn()
-    d.ld_gate = _matrix("w_gate", w_gate, None, D, x.dtype, x.device)
+    ld_gate = _matrix("w_gate", w_gate, None, D, dtype, dev)
     F = w_gate.shape[0]
-    d.ld_up = _matrix("w_up", w_up, F, D, x.dtype, x.device)
-    d.ld_down = _matrix("w_down", w_down, D, F, x.dtype, x.device)
-    d.ld_x, d.dtype, d.activation = ld_x, DTYPES[x.dtype], ACTIVATIONS[activation]
-    d.tokens, d.width, d.features = T, D, F
-    d.x, d.w_gate, d.w_up, d.w_down = x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr()
-    return d
+    ld_up = _matrix("w_up", w_up, F, D, dtype, dev)
+    ld_down = _matrix("w_down", w_down, D, F, dtype, dev)
+    d = B.Ffn(DTYPES[dtype], ACTIVATIONS[activation], T, D, F, x.data_ptr(), w_gate.data_ptr(), w_up.data_ptr(), w_down.data_ptr(),
+              ld_x, ld_gate, ld_up, ld_down)
+    return d, T, D, F, dtype, dev
 
 
 def ffn_forward(x, w_gate, w_up, w_down, activation="silu", save=False, out=None, stream=None):
     """chm_ffn_forward: y = (act(x w_gate^T) * (x w_up^T)) w_down^T for x [tokens, width], w_gate and w_up [features, width],
     w_down [width, features], all bfloat16 or all float16, rows of any stride.  activation: "silu", "gelu", "gelu_tanh".  With
     save=True returns (y, saved), `saved` being what ffn_backward wants (opaque; 6 bytes per token and feature)."""
-    d = _ffn(x, w_gate, w_up, w_down, activation)
-    if out is not None:
-        ld_y = _matrix("out", out, d.tokens, d.width, x.dtype, x.device)
-    with _Stream(stream, x.device) as st:
+    d, T, D, F, dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
+    ld_y = D if out is None else _matrix("out", out, T, D, dtype, dev)
+    lib = B.lib()
+    with _scope(stream, dev) as st:
         need, scratch = C.c_uint64(), C.c_uint64()
-        B._check(B.lib().chm_ffn_sizes(C.byref(d), None, C.byref(need), C.byref(scratch), None))
-        saved = _bytes(need.value, x.device) if save else None
-        d.saved = saved.data_ptr() if save else None
+        B._check(lib.chm_ffn_sizes(d, None, need, scratch, None))
+        saved = None
+        if save:
+            saved = _bytes(need.value, x)
+            d.saved = saved.data_ptr()
         if out is None:
-            out = torch.empty((d.tokens, d.width), dtype=x.dtype, device=x.device)
-            ld_y = d.width
-        ws = _bytes(scratch.value, x.device)
-        B._check(B.lib().chm_ffn_forward(C.byref(d), out.data_ptr(), ld_y, ws.data_ptr(), ws.numel(), st))
+            out = x.new_empty((T, D))
+        ws = _bytes(scratch.value, x)
+        B._check(lib.chm_ffn_forward(d, out.data_ptr(), ld_y, ws.data_ptr(), scratch, st))
     return (out, saved) if save else out
 
 
 def ffn_backward(dy, x, w_gate, w_up, w_down, saved, activation="silu", grads=None, accumulate=False, out=None, stream=None):
     """chm_ffn_backward: (dx, dw_gate, dw_up, dw_down) for dy, the gradient with respect to ffn_forward's result.  `grads`: the three
     weights' gradients to write, or with accumulate=True to add to; of the weights' type or float32.  `out`: dx to write."""
-    d = _ffn(x, w_gate, w_up, w_down, activation)
-    T, D, F, dev = d.tokens, d.width, d.features, x.device
-    g = B.FfnGradients()
-    g.ld_dy = _matrix("dy", dy, T, D, x.dtype, dev)
-    _need(isinstance(saved, torch.Tensor) and saved.is_cuda and saved.device == dev and saved.dtype == torch.uint8, "saved must be what ffn_forward returned")
-    if out is not None:
-        g.ld_dx = _matrix("out", out, T, D, x.dtype, dev)
+    d, T, D, F, x_dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
+    ld_dy = _matrix("dy", dy, T, D, x_dtype, dev)
+    _need(isinstance(saved, torch.Tensor) and saved.get_device() == dev and saved.dtype == torch.uint8, "saved must be what ffn_forward returned")
+    ld_dx = D if out is None else _matrix("out", out, T, D, x_dtype, dev)
     if grads is None:
         _need(not accumulate, "accumulate needs grads")
-        dtype = x.dtype
+        dtype, lds = x_dtype, (D, D, F)
     else:
         _need(len(grads) == 3 and all(isinstance(t, torch.Tensor) for t in grads), "grads must be three matrices")
         dtype = grads[0].dtype
-        _need(dtype in (x.dtype, torch.float32), "grads must be of the weights' type or float32")
-        g.ld_dw_gate = _matrix("grads[0]", grads[0], F, D, dtype, dev)
-        g.ld_dw_up = _matrix("grads[1]", grads[1], F, D, dtype, dev)
-        g.ld_dw_down = _matrix("grads[2]", grads[2], D, F, dtype, dev)
-    g.grad_dtype, g.accumulate = DTYPES[dtype], int(bool(accumulate))
-    with _Stream(stream, dev) as st:
+        _need(dtype in (x_dtype, torch.float32), "grads must be of the weights' type or float32")
+        lds = (_matrix("grads[0]", grads[0], F, D, dtype, dev), _matrix("grads[1]", grads[1], F, D, dtype, dev),
+               _matrix("grads[2]", grads[2], D, F, dtype, dev))
+    lib = B.lib()
+    with _scope(stream, dev) as st:
         if out is None:
-            out = torch.empty((T, D), dtype=x.dtype, device=dev)
-            g.ld_dx = D
+            out = x.new_empty((T, D))
         if grads is None:
-            grads = [torch.empty((F, D), dtype=dtype, device=dev), torch.empty((F, D), dtype=dtype, device=dev),
-                     torch.empty((D, F), dtype=dtype, device=dev)]
-            g.ld_dw_gate, g.ld_dw_up, g.ld_dw_down = D, D, F
+            grads = (x.new_empty((F, D)), x.new_empty((F, D)), x.new_empty((D, F)))
         d.saved = saved.data_ptr()
-        g.dy, g.dx = dy.data_ptr(), out.data_ptr()
-        g.dw_gate, g.dw_up, g.dw_down = (t.data_ptr() for t in grads)
+        g = B.FfnGradients(dy.data_ptr(), out.data_ptr(), grads[0].data_ptr(), grads[1].data_ptr(), grads[2].data_ptr(),
+                           ld_dy, ld_dx, *lds, DTYPES[dtype], 1 if accumulate else 0)
         need, scratch = C.c_uint64(), C.c_uint64()
-        B._check(B.lib().chm_ffn_sizes(C.byref(d), C.byref(g), C.byref(need), None, C.byref(scratch)))
+        B._check(lib.chm_ffn_sizes(d, g, need, None, scratch))
         _need(saved.numel() >= need.value, "saved is not of a forward call of these sizes")
-        ws = _bytes(scratch.value, dev)
-        B._check(B.lib().chm_ffn_backward(C.byref(d), C.byref(g), ws.data_ptr(), ws.numel(), st))
+        ws = _bytes(scratch.value, x)
+        B._check(lib.chm_ffn_backward(d, g, ws.data_ptr(), scratch, st))
     return (out,) + tuple(grads)
 
 
 def _tokens(tokens, device):
-    _need(isinstance(tokens, torch.Tensor) and tokens.is_cuda and tokens.dtype in (torch.int32, torch.int64), "tokens must be int32 or int64 on the GPU")
-    _need(device is None or tokens.device == device, "tokens must be on the same GPU as the others")
+    """checks the tokens and returns their bits and number"""
+    _need(isinstance(tokens, torch.Tensor) and tokens.is_cuda and tokens.get_device() == device, "tokens must be on the same GPU as the others")
+    _need(tokens.dtype in INDEX_BITS, "tokens must be int32 or int64")
     _need(tokens.is_contiguous(), "tokens must be contiguous")
-    return tokens.element_size() * 8
+    return INDEX_BITS[tokens.dtype], tokens.numel()
 
 
 def embedding_lookup(tokens, table, scale=1.0, out=None, stream=None):
     """chm_embedding_lookup: rows scale * table[token], [tokens.numel(), width]; zeros for a token outside the table (padding,
     or a token of another shard)."""
     ld = _matrix("table", table)
-    _need(table.dtype in DTYPES, "table must be float32, bfloat16 or float16")
-    bits, n, (rows, width) = _tokens(tokens, table.device), tokens.numel(), table.shape
-    if out is not None:
-        ld_out = _matrix("out", out, n, width, table.dtype, table.device)
-    with _Stream(stream, table.device) as st:
+    dtype, dev = table.dtype, table.get_device()
+    _need(dtype in DTYPES, "table must be float32, bfloat16 or float16")
+    bits, n = _tokens(tokens, dev)
+    rows, width = table.shape
+    ld_out = width if out is None else _matrix("out", out, n, width, dtype, dev)
+    with _scope(stream, dev) as st:
         if out is None:
-            out = torch.empty((n, width), dtype=table.dtype, device=table.device)
-            ld_out = width
-        B._check(B.lib().chm_embedding_lookup(DTYPES[table.dtype], bits, tokens.data_ptr(), n, table.data_ptr(), ld, rows, width, scale,
+            out = table.new_empty((n, width))
+        B._check(B.lib().chm_embedding_lookup(DTYPES[dtype], bits, tokens.data_ptr(), n, table.data_ptr(), ld, rows, width, scale,
                                               out.data_ptr(), ld_out, st))
     return out
 
@@ -174,25 +190,27 @@ def embedding_gradient(dy, tokens, rows=None, scale=1.0, out=None, accumulate=Fa
     token v.  `out`: the gradient to write, or with accumulate=True to add to (rows without a token are not touched); of dy's type
     or float32."""
     ld = _matrix("dy", dy)
-    _need(dy.dtype in DTYPES, "dy must be float32, bfloat16 or float16")
-    bits, n, width = _tokens(tokens, dy.device), tokens.numel(), dy.shape[1]
+    dtype, dev = dy.dtype, dy.get_device()
+    _need(dtype in DTYPES, "dy must be float32, bfloat16 or float16")
+    bits, n = _tokens(tokens, dev)
     _need(dy.shape[0] == n, "dy must have a row for each token")
-    _need(rows is not None or out is not None, "rows or out must be given")
-    _need(out is not None or not accumulate, "accumulate needs out")
-    if out is not None:
-        ld_out = _matrix("out", out, rows, width, None, dy.device)
-        rows = out.shape[0]
-        _need(out.dtype in (dy.dtype, torch.float32), "out must be of dy's type or float32")
-    with _Stream(stream, dy.device) as st:
+    width = dy.shape[1]
+    if out is None:
+        _need(rows is not None and rows >= 0 and not accumulate, "rows or, with accumulate, out must be given")
+        grad_dtype, ld_out = dtype, width
+    else:
+        ld_out = _matrix("out", out, rows, width, None, dev)
+        rows, grad_dtype = out.shape[0], out.dtype
+        _need(grad_dtype in (dtype, torch.float32), "out must be of dy's type or float32")
+    lib = B.lib()
+    with _scope(stream, dev) as st:
         if out is None:
-            _need(rows >= 0, "rows must not be negative")
-            out = torch.empty((rows, width), dtype=dy.dtype, device=dy.device)
-            ld_out = width
+            out = dy.new_empty((rows, width))
         scratch = C.c_uint64()
-        B._check(B.lib().chm_embedding_gradient_scratch(n, width, C.byref(scratch)))
-        ws = _bytes(scratch.value, dy.device)
-        B._check(B.lib().chm_embedding_gradient(DTYPES[dy.dtype], DTYPES[out.dtype], bits, tokens.data_ptr(), n, dy.data_ptr(), ld, rows, width,
-                                                scale, out.data_ptr(), ld_out, int(bool(accumulate)), ws.data_ptr(), ws.numel(), st))
+        B._check(lib.chm_embedding_gradient_scratch(n, rows, width, scratch))
+        ws = _bytes(scratch.value, dy)
+        B._check(lib.chm_embedding_gradient(DTYPES[dtype], DTYPES[grad_dtype], bits, tokens.data_ptr(), n, dy.data_ptr(), ld, rows, width,
+                                            scale, out.data_ptr(), ld_out, 1 if accumulate else 0, ws.data_ptr(), scratch, st))
     return out
 
 
@@ -247,7 +265,7 @@ class Gradients:
 
     def sumsq(self, stream=None):
         """chm_gradient_sumsq: the sum of squares, a float64 tensor of one element on the GPU; those of the stages of a pipeline add up"""
-        with _Stream(stream, self.device) as st:
+        with _scope(stream, self.device.index) as st:
             total = torch.empty(1, dtype=torch.float64, device=self.device)
             B._check(B.lib().chm_gradient_sumsq(self._h, total.data_ptr(), st))
         return total
@@ -260,7 +278,7 @@ class Gradients:
         if sumsq is not None:
             _need(isinstance(sumsq, torch.Tensor) and sumsq.device == self.device and sumsq.dtype == torch.float64 and sumsq.numel() == 1,
                   "sumsq must be a float64 tensor of one element")
-        with _Stream(stream, self.device) as st:
+        with _scope(stream, self.device.index) as st:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
             B._check(B.lib().chm_clip_gradients(self._h, max_norm, None if sumsq is None else sumsq.data_ptr(), norm.data_ptr(), st))
         return norm

@@ -548,6 +548,6 @@ def test_refusals(ops):
         with pytest.raises(B.ChmError) as e:
             call()
         assert e.value.code == B.ERR_ARG, i
-    d = ops._ffn(x, wg, wu, wd, "silu")                                    # scratch that is too short
+    d = ops._ffn(x, wg, wu, wd, "silu")[0]                                 # scratch that is too short
     ws = torch.empty(64, dtype=torch.uint8, device="cuda")
     assert B.lib().chm_ffn_forward(d, dy.data_ptr(), 16, ws.data_ptr(), 64, None) == B.ERR_LIMIT

@@ -24,7 +24,7 @@ struct GemmCall {
   void *c[2];
   int64_t ldc;
   int64_t m_first, m_real, n_real;
-  int32_t f32_out, accumulate, wide;      // wide: 16-byte stores are possible
+  int32_t f32_out, accumulate;
   float *part;                  // [splits][m][ld_part]
   int64_t ld_part;              // columns rounded up to 8
   // two-weight product and gradient of the activation: internal buffers of `ldi` elements a row

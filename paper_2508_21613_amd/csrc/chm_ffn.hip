@@ -194,12 +194,28 @@ bool launch_few(const FewCall &c, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------- packing
 // An operand whose rows do not start on 16 bytes or are no whole words of 8 elements is copied into rows that are, with zeros
 // behind: the copy costs its bytes twice, a product reads them some dozens of times.
-__global__ void __launch_bounds__(256) k_pack(const uint16_t *in, int64_t ld, int64_t rows, int cols, uint16_t *out, int64_t ld_out) {
-  const int words = (int)(ld_out / 8);
-  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < rows * words; i += (int64_t)gridDim.x * 256) {
-    const int64_t row = i / words;
-    const int col = (int)(i - row * words) * 8;
-    *(s8 *)(out + row * ld_out + col) = take8(in + row * ld, col, cols);
+struct PackCall {
+  struct { const uint16_t *in; uint16_t *out; int64_t ld, rows; int32_t cols, words, groups; } m[5];
+  int32_t count;
+};
+constexpr int PACK_WORDS = 4 * 256;           // 16-byte words of a workgroup
+
+// all operands of a pass in one launch, one behind the other
+__global__ void __launch_bounds__(256) k_pack(PackCall c) {
+  int g = blockIdx.x, i = 0;
+  while (i + 1 < c.count && g >= c.m[i].groups) g -= c.m[i++].groups;
+  const int words = c.m[i].words, cols = c.m[i].cols;
+  const int64_t all = c.m[i].rows * words, first = (int64_t)g * PACK_WORDS + threadIdx.x;
+  s8 v[4];
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t w = first + u * 256;
+    if (w < all) v[u] = take8(c.m[i].in + w / words * c.m[i].ld, (int)(w % words) * 8, cols);
+  }
+#pragma unroll
+  for (int u = 0; u < 4; ++u) {
+    const int64_t w = first + u * 256;
+    if (w < all) *(s8 *)(c.m[i].out + w * 8) = v[u];
   }
 }
 
@@ -269,17 +285,31 @@ struct Pass {
 
   Pass(const chm_ffn *f_, char *base, hipStream_t st_, bool run_) : f(f_), arena{base}, st(st_), run(run_) {}
 
-  // the matrix itself, or a packed copy of it
+  // the matrix itself, or a packed copy of it: made by the next flush()
+  PackCall pack{};
   Matrix packed(const Matrix &m, bool must = false) {
     if (!must && !needs_pack(m)) return m;
     Matrix o{nullptr, up8(m.cols), m.rows, up8(m.cols)};
     o.p = arena.take((uint64_t)o.rows * o.ld * 2);
-    if (run && m.rows) {
-      hipLaunchKernelGGL(k_pack, dim3(copy_groups(o.rows * (o.ld / 8))), dim3(256), 0, st, (const uint16_t *)m.p, m.ld, m.rows, (int)m.cols,
-                         (uint16_t *)o.p, o.ld);
-      ok = ok && hipGetLastError() == hipSuccess;
+    const int64_t words = o.rows * (o.ld / 8);
+    if (words) {
+      auto &p = pack.m[pack.count++];
+      p.in = (const uint16_t *)m.p;
+      p.out = (uint16_t *)o.p;
+      p.ld = m.ld;
+      p.rows = m.rows;
+      p.cols = (int32_t)m.cols;
+      p.words = (int32_t)(o.ld / 8);
+      p.groups = (int32_t)((words + PACK_WORDS - 1) / PACK_WORDS);
     }
     return o;
+  }
+  void flush() {
+    if (!run || !pack.count) return;
+    uint32_t groups = 0;
+    for (int i = 0; i < pack.count; ++i) groups += pack.m[i].groups;
+    hipLaunchKernelGGL(k_pack, dim3(groups), dim3(256), 0, st, pack);
+    ok = ok && hipGetLastError() == hipSuccess;
   }
   // two weights of one product: rows of equal length in memory
   void packed_pair(Matrix &a, Matrix &b) {
@@ -352,6 +382,7 @@ struct Pass {
     const Matrix x = packed({f->x, f->ld_x, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
     Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
     packed_pair(wg, wu);
+    flush();
     GemmCall c{};
     c.a = GemmOperand{{x.p, x.p}, x.ld, x.cols};
     c.b = GemmOperand{{wg.p, wu.p}, wg.ld, wg.cols};
@@ -374,7 +405,6 @@ struct Pass {
     c.ldc = ld;
     c.m_first = c.m_real = c.m;
     c.n_real = cols;
-    c.wide = (uintptr_t)p % 16 == 0 && ld % 8 == 0;
   }
 
   void backward(const chm_ffn_gradients *g) {
@@ -384,6 +414,7 @@ struct Pass {
     const Matrix x = packed({f->x, f->ld_x, T, D}), dy = packed({g->dy, g->ld_dy, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
     Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
     packed_pair(wg, wu);
+    flush();
 
     GemmCall a{};                          // dh, and h, dg, du
     a.a = GemmOperand{{dy.p, dy.p}, dy.ld, dy.cols};
@@ -394,14 +425,13 @@ struct Pass {
     a.dgate = d; a.dup = d + F8; a.ldd = 2 * F8;
     launch(GEMM_DH, a, false);
 
-    const bool wide_grad = ((uintptr_t)g->dw_down % 16 | (uintptr_t)g->dw_gate % 16 | (uintptr_t)g->dw_up % 16) == 0;
     GemmCall b{};                          // dWd
     b.a = GemmOperand{{dy.p, dy.p}, dy.ld, T};
     b.b = GemmOperand{{h, h}, F8, T};
     b.m = D; b.n = F8;
     b.runs = 1;
     out(b, g->dw_down, g->ld_dw_down, F);
-    grad(b, g, wide_grad);
+    grad(b, g);
     launch(GEMM_DW, b, false);
 
     GemmCall e{};                          // dWg, dWu
@@ -412,7 +442,7 @@ struct Pass {
     out(e, g->dw_gate, g->ld_dw_gate, D);
     e.c[1] = g->dw_up;
     e.m_first = F8; e.m_real = F;
-    grad(e, g, wide_grad);
+    grad(e, g);
     launch(GEMM_DW, e, false);
 
     GemmCall i{};                          // dx
@@ -424,10 +454,9 @@ struct Pass {
     launch(GEMM_DX, i, true);
   }
 
-  void grad(GemmCall &c, const chm_ffn_gradients *g, bool wide) {
+  void grad(GemmCall &c, const chm_ffn_gradients *g) {
     c.f32_out = g->grad_dtype == CHM_F32;
     c.accumulate = g->accumulate != 0;
-    c.wide = wide && c.ldc % 8 == 0;
   }
 };
 

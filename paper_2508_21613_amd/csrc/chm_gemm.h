@@ -215,14 +215,15 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
   const int which = m >= c.m_first;
   const int64_t row = m - (which ? c.m_first : 0), left = c.n_real - n;
   if (row >= c.m_real || left <= 0) return;
-  const bool whole = c.wide && left >= 8;
+  const bool whole = left >= 8;             // outputs start on any element: 16-byte accesses at any address
   if (c.f32_out) {
+    typedef f4 f4_anywhere __attribute__((aligned(4)));
     float *p = (float *)c.c[which] + row * c.ldc + n;
     if (whole) {
       f4 a = v[0], b = v[1];
-      if (c.accumulate) { a += *(const f4 *)p; b += *(const f4 *)(p + 4); }
-      *(f4 *)p = a;
-      *(f4 *)(p + 4) = b;
+      if (c.accumulate) { a += *(const f4_anywhere *)p; b += *(const f4_anywhere *)(p + 4); }
+      *(f4_anywhere *)p = a;
+      *(f4_anywhere *)(p + 4) = b;
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -230,17 +231,18 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
     }
     return;
   }
+  typedef s8 s8_anywhere __attribute__((aligned(2)));
   uint16_t *p = (uint16_t *)c.c[which] + row * c.ldc + n;
   float w[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) w[e] = v[e >> 2][e & 3];
   if (whole) {
     if (c.accumulate) {
-      const s8 old = *(const s8 *)p;
+      const s8 old = *(const s8_anywhere *)p;
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] += T::up((uint16_t)old[e]);
     }
-    *(s8 *)p = pack8<T>(w);
+    *(s8_anywhere *)p = pack8<T>(w);
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)

@@ -1,0 +1,122 @@
+"""What the operators' entry points answer without a GPU: sizes of workspaces and refusals."""
+import ctypes as C
+
+import pytest
+import torch
+
+from paper_2508_21613_amd import binding as B
+from paper_2508_21613_amd import operators as ops
+
+
+def _ffn(T=100, D=64, F=96, **kw):
+    d = B.Ffn(dtype=1, activation=0, tokens=T, width=D, features=F, ld_x=D, ld_gate=D, ld_up=D, ld_down=F)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return d
+
+
+def _grads(T=100, D=64, F=96, **kw):
+    g = B.FfnGradients(ld_dy=D, ld_dx=D, ld_dw_gate=D, ld_dw_up=D, ld_dw_down=F, grad_dtype=1)
+    for k, v in kw.items():
+        setattr(g, k, v)
+    return g
+
+
+def _sizes(d, g=None):
+    out = [C.c_uint64() for _ in range(3)]
+    rc = B.lib().chm_ffn_sizes(d, g, *out)
+    return rc, [int(v.value) for v in out]
+
+
+def test_ffn_sizes():
+    rc, (saved, forward, backward) = _sizes(_ffn(), _grads())
+    assert rc == B.OK and saved == 100 * 96 * 6 and forward >= 100 * 96 * 2 and backward >= 100 * 96 * 6
+    assert _sizes(_ffn())[1][2] == 0
+    assert _sizes(_ffn(F=97, ld_down=97))[1][0] == 100 * 104 * 6                       # rows of whole words of 8
+    even, odd = _sizes(_ffn(), _grads())[1], _sizes(_ffn(ld_gate=65, ld_up=65), _grads())[1]
+    assert odd[1] >= even[1] + 2 * 96 * 64 * 2 and odd[2] >= even[2] + 2 * 96 * 64 * 2  # packed copies of both weights
+    assert _sizes(_ffn(T=0), _grads(T=0))[0] == B.OK
+
+
+@pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
+                                    dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
+                                    dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])
+def test_ffn_refusals(change):
+    assert _sizes(_ffn(**change))[0] == B.ERR_ARG
+    assert B.lib().chm_ffn_forward(_ffn(**change), None, 64, None, 0, None) == B.ERR_ARG
+    assert B.lib().chm_ffn_backward(_ffn(**change), _grads(), None, 0, None) == B.ERR_ARG
+
+
+@pytest.mark.parametrize("change", [dict(grad_dtype=2), dict(grad_dtype=-1), dict(ld_dy=63), dict(ld_dx=63), dict(ld_dw_gate=63), dict(ld_dw_up=65),
+                                    dict(ld_dw_down=95), dict(dy=1), dict(dw_gate=1)])
+def test_ffn_gradient_refusals(change):
+    assert _sizes(_ffn(), _grads(**change))[0] == B.ERR_ARG
+    assert B.lib().chm_ffn_backward(_ffn(), _grads(**change), None, 0, None) == B.ERR_ARG
+
+
+def test_null_pointers():
+    L = B.lib()
+    assert L.chm_ffn_sizes(None, None, None, None, None) == B.ERR_ARG
+    assert L.chm_ffn_forward(None, None, 64, None, 0, None) == B.ERR_ARG
+    assert L.chm_ffn_forward(_ffn(), None, 64, None, 0, None) == B.ERR_ARG
+    assert L.chm_ffn_backward(_ffn(), None, None, 0, None) == B.ERR_ARG
+    assert L.chm_embedding_lookup(1, 64, None, 5, None, 8, 10, 8, 1.0, None, 8, None) == B.ERR_ARG
+    assert L.chm_embedding_gradient(1, 1, 64, None, 5, None, 8, 10, 8, 1.0, None, 8, 0, None, 0, None) == B.ERR_ARG
+    assert L.chm_gradient_sumsq(None, None, None) == B.ERR_ARG
+    assert L.chm_clip_gradients(None, 1.0, None, None, None) == B.ERR_ARG
+    assert L.chm_load_gradients(None, 1, None) == B.ERR_ARG
+    L.chm_free_gradients(None)
+    assert L.chm_ffn_forward(_ffn(T=0), None, 64, None, 0, None) == B.OK               # nothing to do
+
+
+def test_embedding_sizes_and_refusals():
+    L, n = B.lib(), C.c_uint64()
+    assert L.chm_embedding_gradient_scratch(256, 1000, 64, n) == B.OK and n.value == 0
+    assert L.chm_embedding_gradient_scratch(257, 1000, 64, n) == B.OK and n.value >= 257 * 16 + 1000
+    for args in ((-1, 10, 8), (5, -1, 8), (5, 10, 0), (1 << 31, 10, 8), (5, 1 << 31, 8)):
+        assert L.chm_embedding_gradient_scratch(*args, n) == B.ERR_ARG
+    assert L.chm_embedding_gradient_scratch(5, 5, 5, None) == B.ERR_ARG
+
+    def lookup(dtype=1, bits=64, n=0, ld=8, rows=10, width=8, ld_out=8):
+        return L.chm_embedding_lookup(dtype, bits, None, n, None, ld, rows, width, 1.0, None, ld_out, None)
+
+    assert lookup() == B.OK
+    for change in (dict(dtype=3), dict(bits=16), dict(n=-1), dict(ld=7), dict(rows=-1), dict(width=0), dict(ld_out=7)):
+        assert lookup(**change) == B.ERR_ARG, change
+
+
+def test_loading_gradients_refuses_before_the_device():
+    h = C.c_void_p()
+    for bad in (B.Gradient(None, None, 5, 0), B.Gradient(2, None, 5, 0), B.Gradient(4, 2, 5, 0), B.Gradient(4, None, -1, 0), B.Gradient(4, None, 5, 3)):
+        assert B.lib().chm_load_gradients(bad, 1, h) == B.ERR_ARG and not h.value
+    assert B.lib().chm_load_gradients(None, -1, h) == B.ERR_ARG
+
+
+def test_tensors_that_are_not_on_the_gpu_are_refused():
+    x, w, d = torch.zeros(2, 8).bfloat16(), torch.zeros(16, 8).bfloat16(), torch.zeros(8, 16).bfloat16()
+    for call in (lambda: ops.ffn_forward(x, w, w, d), lambda: ops.embedding_lookup(torch.zeros(3, dtype=torch.int64), w),
+                 lambda: ops.embedding_gradient(x, torch.zeros(2, dtype=torch.int64), 4), lambda: ops.ffn_forward(None, w, w, d)):
+        with pytest.raises(B.ChmError) as e:
+            call()
+        assert e.value.code == B.ERR_ARG
+
+
+def test_structures_match_the_header(tmp_path):
+    """sizes and field offsets of the binding's structures against what a C compiler makes of include/chm_operators.h"""
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    structs = {"chm_ffn": B.Ffn, "chm_ffn_gradients": B.FfnGradients, "chm_gradient": B.Gradient}
+    lines = ['#include <stdio.h>', '#include <stddef.h>', '#include "chm_operators.h"', 'int main(void) {']
+    for cname, cls in structs.items():
+        lines.append('  printf("%s %%zu\\n", sizeof(%s));' % (cname, cname))
+        lines += ['  printf("%s.%s %%zu\\n", offsetof(%s, %s));' % (cname, f, cname, f) for f, _ in cls._fields_]
+    src = tmp_path / "layout.c"
+    src.write_text("\n".join(lines + ['  return 0;', '}']))
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "layout"), str(src)], check=True)
+    out = subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout
+    want = dict(line.split() for line in out.splitlines())
+    for cname, cls in structs.items():
+        assert C.sizeof(cls) == int(want[cname]), cname
+        for field, _ in cls._fields_:
+            assert getattr(cls, field).offset == int(want["%s.%s" % (cname, field)]), (cname, field)

@@ -10,8 +10,8 @@
 // other), elements from one row of memory to the next, length of a run of k.  Elements of 16 bits, 16-byte aligned rows.
 struct GemmOperand { const void *p[2]; int64_t ld, k; };
 
-// The projections g and u as the backward pass reads them, rows as those of h: 24 bits each, upper 16 and lower 8 apart
-struct Kept { uint16_t *gate, *up; uint8_t *gate_low, *up_low; };
+// The projections g and u as the backward pass reads them: blocks of 16 rows x 32 features, `blocks` of them side by side (layout: chm_gemm.h)
+struct Kept { char *p; int64_t blocks; };
 
 struct GemmCall {
   GemmOperand a, b;
@@ -29,7 +29,7 @@ struct GemmCall {
   int64_t ld_part;              // columns rounded up to 8
   // two-weight product and gradient of the activation: internal buffers of `ldi` elements a row
   uint16_t *h;
-  Kept kept;                    // gate null: not kept
+  Kept kept;                    // null: not kept
   uint16_t *dgate, *dup;
   int64_t ldi, ldd;             // ldd: row of dgate / dup
 };

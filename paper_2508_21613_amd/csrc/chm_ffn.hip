@@ -36,7 +36,7 @@ struct FewCall {
   const uint16_t *x, *w0, *w1;
   int64_t ldx, ld0, ld1;
   uint16_t *out;
-  Kept kept;                                  // rows as those of out
+  Kept kept;
   int64_t ldo;
   int32_t tokens, rows, k, act;
 };
@@ -56,12 +56,14 @@ __device__ __forceinline__ float act(int kind, float g) {
   return kind == CHM_ACT_GELU ? chm_gemm::act_of<CHM_ACT_GELU>(g) : chm_gemm::act_of<CHM_ACT_GELU_TANH>(g);
 }
 
-__device__ __forceinline__ void keep_pair(const FewCall &c, int64_t at, float g, float u) {
+__device__ __forceinline__ void keep_pair(const FewCall &c, int64_t m, int64_t f, float g, float u) {
   const uint32_t bg = __float_as_uint(g), bu = __float_as_uint(u);
-  c.kept.gate[at] = (uint16_t)(bg >> 16);
-  c.kept.gate_low[at] = (uint8_t)(bg >> 8);
-  c.kept.up[at] = (uint16_t)(bu >> 16);
-  c.kept.up_low[at] = (uint8_t)(bu >> 8);
+  char *p = chm_gemm::kept_at(c.kept, m, f);
+  const int e = (int)f & 7;
+  ((uint16_t *)p)[e] = (uint16_t)(bg >> 16);
+  ((uint16_t *)(p + 1024))[e] = (uint16_t)(bu >> 16);
+  ((uint8_t *)(p + 2048))[e] = (uint8_t)(bg >> 8);
+  ((uint8_t *)(p + 2048))[8 + e] = (uint8_t)(bu >> 8);
 }
 
 // wavefronts of a workgroup at most: two steps and more of several tiles take more registers than 16 of them leave
@@ -152,7 +154,7 @@ __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCa
     const int feature = o & 15, token = o >> 4;
     if (token >= c.tokens) continue;
     if (f0 + feature >= c.rows) {             // kept projections have rows of whole words of 8, zeros behind
-      if (TWO && c.kept.gate && f0 + feature < ((c.rows + 7) & ~7)) keep_pair(c, token * c.ldo + f0 + feature, 0.f, 0.f);
+      if (TWO && c.kept.p && f0 + feature < ((c.rows + 7) & ~7)) keep_pair(c, token, f0 + feature, 0.f, 0.f);
       continue;
     }
     const int at = ((token >> 4) * 64 + (feature >> 2) * 16 + (token & 15)) * 4 + (feature & 3);
@@ -164,7 +166,7 @@ __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCa
     const int64_t col = f0 + feature;
     if (TWO) {
       c.out[token * c.ldo + col] = T::down(act(c.act, s0) * s1);
-      if (c.kept.gate) keep_pair(c, token * c.ldo + col, s0, s1);
+      if (c.kept.p) keep_pair(c, token, col, s0, s1);
     } else {
       c.out[token * c.ldo + col] = T::down(s0);
     }
@@ -269,13 +271,9 @@ struct Arena {
   }
 };
 
-// the four planes of chm_ffn::saved: 16-byte rows in each
-Kept kept_of(const chm_ffn *f) {
-  const int64_t n = f->tokens * up8(f->features);
-  char *p = (char *)f->saved;
-  if (!p) return Kept{};
-  return Kept{(uint16_t *)p, (uint16_t *)(p + n * 2), (uint8_t *)(p + n * 4), (uint8_t *)(p + n * 5)};
-}
+int64_t kept_blocks(const chm_ffn *f) { return (f->features + 31) / 32; }
+uint64_t kept_bytes(const chm_ffn *f) { return (uint64_t)((f->tokens + 15) / 16) * kept_blocks(f) * 3072; }
+Kept kept_of(const chm_ffn *f) { return Kept{(char *)f->saved, kept_blocks(f)}; }
 
 struct Pass {
   const chm_ffn *f;
@@ -488,7 +486,7 @@ extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint6
   const int rc = check(f);
   if (rc != CHM_OK) return rc;
   if (g && check_gradients(f, g) != CHM_OK) return CHM_ERR_ARG;
-  if (saved) *saved = (uint64_t)f->tokens * up8(f->features) * 6;
+  if (saved) *saved = kept_bytes(f);
   if (forward_scratch) {
     Pass p(f, nullptr, nullptr, false);
     p.forward(nullptr, f->width);

@@ -202,8 +202,12 @@ template <class T> __device__ __forceinline__ s8 pack8(const float *v) {
   return r;
 }
 
+// What large products store goes past the caches (PAST), where it would displace the operands: 4,096 tokens, product with two weights 585 us
+// without and 540 with it, gradient of the activation 389 and 379, 8,192^3 805 and 743.
+#define CHM_PUT(p, v) do { if (PAST) __builtin_nontemporal_store(v, p); else *(p) = v; } while (0)
+
 // Eight values of row m from column n on: part of a split sum, or a plain output
-template <class T>
+template <class T, int PAST>
 __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64_t n, const f4 *v) {
   if (m >= c.m || n >= c.n) return;
   if (c.splits > 1) {
@@ -222,8 +226,8 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
     if (whole) {
       f4 a = v[0], b = v[1];
       if (c.accumulate) { a += *(const f4_anywhere *)p; b += *(const f4_anywhere *)(p + 4); }
-      *(f4_anywhere *)p = a;
-      *(f4_anywhere *)(p + 4) = b;
+      CHM_PUT((f4_anywhere *)p, a);
+      CHM_PUT((f4_anywhere *)(p + 4), b);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
@@ -242,7 +246,7 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
 #pragma unroll
       for (int e = 0; e < 8; ++e) w[e] += T::up((uint16_t)old[e]);
     }
-    *(s8_anywhere *)p = pack8<T>(w);
+    CHM_PUT((s8_anywhere *)p, pack8<T>(w));
   } else {
 #pragma unroll
     for (int e = 0; e < 8; ++e)
@@ -250,39 +254,52 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64
   }
 }
 
-// Values kept for the backward pass: the upper 24 bits of float32 (16 of them significant), upper 16 and lower 8 apart, 1.5 times the
-// bytes of the tensors' own type.  Rounded to that type they would add an error as large as all others together to every gradient.
-// Cut off rather than rounded: two byte permutations for four values, and not a number stays one.
+// Values kept for the backward pass: the upper 24 bits of float32 (16 of them significant), 1.5 times the bytes of the tensors' own type.
+// Rounded to that type they would add an error as large as all others together to every gradient.  Cut off rather than rounded: two
+// byte permutations for four values, and not a number stays one.
+//
+// They lie in blocks of 16 rows x 32 features of 3 KiB: upper 16 bits of g, those of u, lower 8 of both, each eight features' 16 bytes behind
+// the other, row by row.  That is how the 64 lanes of a wavefront hold them: every store is one stretch of 1 KiB (in planes of rows
+// they were pieces of 64 and 32 bytes, and cost twice the time that their bytes take).
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u4 __attribute__((ext_vector_type(4)));
-__device__ __forceinline__ void keep8(uint16_t *high, uint8_t *low, int64_t at, const float *v) {
-  u4 hi;
-  u2 lo;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) hi[i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302);
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const uint32_t a = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i]), 0x0c0c0501);
-    const uint32_t b = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 3]), __float_as_uint(v[4 * i + 2]), 0x05010c0c);
-    lo[i] = a | b;
-  }
-  *(u4 *)(high + at) = hi;
-  *(u2 *)(low + at) = lo;
+__device__ __forceinline__ char *kept_at(const Kept &k, int64_t m, int64_t f) {
+  return k.p + ((m >> 4) * k.blocks + (f >> 5)) * 3072 + ((m & 15) * 4 + ((f >> 3) & 3)) * 16;
 }
-struct Kept8 { u4 hi; u2 lo; };
-__device__ __forceinline__ Kept8 kept8(const uint16_t *high, const uint8_t *low, int64_t at) { return Kept8{*(const u4 *)(high + at), *(const u2 *)(low + at)}; }
-__device__ __forceinline__ void unkeep8(const Kept8 &k, float *v) {
+template <int PAST>
+__device__ __forceinline__ void keep8(const Kept &k, int64_t m, int64_t f, const float *g, const float *u) {
+  u4 hi[2], lo;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    const float *v = w ? u : g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[w][i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      lo[w * 2 + i] = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i]), 0x0c0c0501) |
+                      __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 3]), __float_as_uint(v[4 * i + 2]), 0x05010c0c);
+  }
+  char *p = kept_at(k, m, f);
+  CHM_PUT((u4 *)p, hi[0]);
+  CHM_PUT((u4 *)(p + 1024), hi[1]);
+  CHM_PUT((u4 *)(p + 2048), lo);
+}
+struct Kept8 { u4 g, u, lo; };
+__device__ __forceinline__ Kept8 kept8(const Kept &k, int64_t m, int64_t f) {
+  const char *p = kept_at(k, m, f);
+  return Kept8{*(const u4 *)p, *(const u4 *)(p + 1024), *(const u4 *)(p + 2048)};
+}
+__device__ __forceinline__ void unkeep8(u4 hi, u2 lo, float *v) {
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t word = k.hi[e >> 1], bytes = k.lo[e >> 2];
     // bytes from the top: upper 16 bits of the value, its lower 8, zero
     const uint32_t sel = (e & 1 ? 0x07060000u : 0x05040000u) | ((uint32_t)(e & 3) << 8) | 0x0cu;
-    v[e] = __uint_as_float(__builtin_amdgcn_perm(word, bytes, sel));
+    v[e] = __uint_as_float(__builtin_amdgcn_perm(hi[e >> 1], lo[e >> 2], sel));
   }
 }
 
 // Eight features of both projections (float32 sums): activation and product
-template <class T, int ACT>
+template <class T, int ACT, int PAST>
 __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_t f, const f4 *v) {
   if (m >= c.m || f >= c.n) return;
   float g[8], u[8], h[8];
@@ -298,20 +315,17 @@ __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_
       if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;
   }
   const int64_t at = m * c.ldi + f;
-  *(s8 *)(c.h + at) = pack8<T>(h);
-  if (c.kept.gate) {
-    keep8(c.kept.gate, c.kept.gate_low, at, g);
-    keep8(c.kept.up, c.kept.up_low, at, u);
-  }
+  CHM_PUT((s8 *)(c.h + at), pack8<T>(h));
+  if (c.kept.p) keep8<PAST>(c.kept, m, f, g, u);
 }
 
 // Eight features of dh: the gradients of both projections, and h
-template <class T, int ACT>
-__device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v, const Kept8 &kg, const Kept8 &ku) {
+template <class T, int ACT, int PAST>
+__device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v, const Kept8 &k) {
   if (m >= c.m || f >= c.n) return;
   float g[8], u[8], h[8], dg[8], du[8];
-  unkeep8(kg, g);
-  unkeep8(ku, u);
+  unkeep8(k.g, u2{k.lo[0], k.lo[1]}, g);
+  unkeep8(k.u, u2{k.lo[2], k.lo[3]}, u);
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     const float dh = v[e >> 2][e & 3];
@@ -326,16 +340,16 @@ __device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, in
     for (int e = 0; e < 8; ++e)
       if (f + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
   }
-  *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
-  *(s8 *)(c.dgate + m * c.ldd + f) = pack8<T>(dg);
-  *(s8 *)(c.dup + m * c.ldd + f) = pack8<T>(du);
+  CHM_PUT((s8 *)(c.h + m * c.ldi + f), pack8<T>(h));
+  CHM_PUT((s8 *)(c.dgate + m * c.ldd + f), pack8<T>(dg));
+  CHM_PUT((s8 *)(c.dup + m * c.ldd + f), pack8<T>(du));
 }
 
 typedef __attribute__((address_space(3))) f4 lds_f4;
 
 // A wavefront's ROWS_ rows of 64 sums, turned round in shared memory at `turn`; m1, n1: the first row and column (feature) of them.
 // A loop, not a sequence: code that runs once a tile is read from the cache of instructions' own source, and slowly.
-template <class T, int DUAL, int EPI, int ACT, int ROWS_>
+template <class T, int DUAL, int EPI, int ACT, int ROWS_, int PAST>
 __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, int64_t m1, int64_t n1, int lane) {
   if (DUAL) {                               // 16 rows of 32 features at a time
     const int f = (lane & 3) * 8;
@@ -343,7 +357,7 @@ __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, 
     for (int r = lane >> 2; r < ROWS_; r += 16) {
       const lds_char *at = turn + r * TURN_ROW + ((f >> 4) * 32 + (f & 8)) * 4;
       const f4 v[4] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16), *(const lds_f4 *)(at + 64), *(const lds_f4 *)(at + 80)};
-      finish_pair<T, ACT>(c, m1 + r, n1 + f, v);
+      finish_pair<T, ACT, PAST>(c, m1 + r, n1 + f, v);
     }
     return;
   }
@@ -353,23 +367,17 @@ __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, 
   int64_t m = m1 + (lane >> 3);
   if (EPI == EPI_ACT_GRAD) {                // what is kept of two times 8 rows is on its way
     const int64_t col = n < c.n ? n : 0, last = c.m - 1;
-    Kept8 kg[2], ku[2];
+    Kept8 kept[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const int64_t p = (m + i * 8 < last ? m + i * 8 : last) * c.ldi + col;
-      kg[i] = kept8(c.kept.gate, c.kept.gate_low, p);
-      ku[i] = kept8(c.kept.up, c.kept.up_low, p);
-    }
+    for (int i = 0; i < 2; ++i) kept[i] = kept8(c.kept, m + i * 8 < last ? m + i * 8 : last, col);
 #pragma nounroll
     for (int r = 0; r < ROWS_; r += 16) {
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const Kept8 g = kg[i], u = ku[i];
-        const int64_t p = (m + 16 < last ? m + 16 : last) * c.ldi + col;
-        kg[i] = kept8(c.kept.gate, c.kept.gate_low, p);
-        ku[i] = kept8(c.kept.up, c.kept.up_low, p);
+        const Kept8 k = kept[i];
+        kept[i] = kept8(c.kept, m + 16 < last ? m + 16 : last, col);
         const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
-        finish_gradient<T, ACT>(c, m, n, v, g, u);
+        finish_gradient<T, ACT, PAST>(c, m, n, v, k);
         at += 8 * TURN_ROW;
         m += 8;
       }
@@ -379,7 +387,7 @@ __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, 
 #pragma nounroll
   for (int r = 0; r < ROWS_; r += 8) {
     const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
-    finish_plain<T>(c, m, n, v);
+    finish_plain<T, PAST>(c, m, n, v);
     at += 8 * TURN_ROW;
     m += 8;
   }
@@ -502,9 +510,9 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int64_t m1 = m0 + wm + t0 * 16, n1 = n0 + (DUAL ? wn / 2 : wn);
-    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, TURN>(c, turn, m1, n1, lane);
-    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, TURN>(c, turn, m1, n1, lane);
-    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, TURN>(c, turn, m1, n1, lane);
+    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, TURN, MT == 8>(c, turn, m1, n1, lane);
+    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, TURN, MT == 8>(c, turn, m1, n1, lane);
+    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, TURN, MT == 8>(c, turn, m1, n1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }

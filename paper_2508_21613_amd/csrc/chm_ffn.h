@@ -18,7 +18,7 @@ struct GemmCall {
   int64_t m, n;                 // sizes of the product (n: features of one weight in a two-weight product)
   int32_t tiles_m, tiles_n;
   int32_t runs;                 // 2: a second run of k follows the first, from the operands' second bases
-  int32_t splits;               // > 1: the sums are split over blockIdx.y, float32 parts go to `part`
+  int32_t splits;               // > 1: the sums are split over workgroups, float32 parts go to `part`
   int32_t act;
   // plain store: c[0] for rows below m_first, c[1] (row m - m_first) from there on; rows up to m_real, columns up to n_real
   void *c[2];
@@ -34,14 +34,22 @@ struct GemmCall {
   int64_t ldi, ldd;             // ldd: row of dgate / dup
 };
 
-enum { GEMM_GATE_UP = 0, GEMM_OUT = 1, GEMM_DH = 2, GEMM_DX = 3, GEMM_DW = 4 };
+// Products that one launch works out.  GEMM_BACK: dx (the longest sums, first), then both weight gradients, which depend on nothing but what
+// GEMM_DH has left: together they fill the compute units that each alone leaves idle at its end.
+enum { GEMM_GATE_UP = 0, GEMM_OUT = 1, GEMM_DH = 2, GEMM_BACK = 3 };
+struct GemmGroup {
+  GemmCall call[3];
+  int32_t count;
+  int32_t first[4];             // first workgroup of each call (a multiple of 8), and one behind the last
+};
+
 // Tiles of 256 x 256, two steps in shared memory; of 128 x 128, two steps (two workgroups a compute unit) or four (one: a step's loads
 // have three steps' time to arrive).  All of 8 wavefronts: with 4 the 128 x 128 ones take 1.1 to 1.4 times as long, since nothing
 // runs while a wavefront issues loads.
 enum { TILE_256 = 0, TILE_128 = 1, TILE_128_DEEP = 2 };
 // Largest row of memory (elements) that the tile kernels take: 256 rows lie within 2^31 bytes.  Longer ones are packed.
 constexpr int64_t GEMM_LD_MAX = 1 << 21;
-// Launches one product; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.
-bool gemm_launch_bf16(int product, int tile, const GemmCall &c, void *stream);
-bool gemm_launch_f16(int product, int tile, const GemmCall &c, void *stream);
+// Launches them; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.
+bool gemm_launch_bf16(int products, int tile, const GemmGroup &g, void *stream);
+bool gemm_launch_f16(int products, int tile, const GemmGroup &g, void *stream);
 #endif

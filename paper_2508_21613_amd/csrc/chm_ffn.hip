@@ -316,32 +316,60 @@ struct Pass {
     b = packed(b, must);
   }
 
-  // The kind of tile with the least time by the number of rounds over the 256 compute units; the units are microseconds of a round at 4,096
-  // sums: 256 x 256 tiles 83, 128 x 128 ones 37 for up to 256 of them (one a compute unit), 66 for every 512 (measured: 2,048 x 4,096 83 and
-  // 66, 1,024 x 4,096 79 and 37, 512 x 22,016 83 and 132, 4,096 x 11,008 240 and 400).  Where the small tiles leave compute units idle
-  // and the output is plain (`may_split`), the sums are split as well, 512 of them a part at least.
-  void launch(int product, GemmCall &c, bool may_split) {
-    const int64_t n_all = product == GEMM_GATE_UP ? 2 * c.n : c.n;
-    const int64_t big = ((c.m + 255) / 256) * ((n_all + 255) / 256), small = ((c.m + 127) / 128) * ((n_all + 127) / 128);
-    const int64_t time_big = (big + 255) / 256 * 83, time_small = small <= 256 ? 37 : (small + 511) / 512 * 66;
-    const int tile = time_big < time_small ? TILE_256 : small <= 256 ? TILE_128_DEEP : TILE_128, side = tile == TILE_256 ? 256 : 128;
-    c.tiles_m = (int32_t)((c.m + side - 1) / side);
-    c.tiles_n = (int32_t)((n_all + side - 1) / side);
-    c.splits = 1;
-    if (may_split && tile == TILE_128_DEEP) {
-      int64_t s = 256 / (small > 0 ? small : 1);
-      const int64_t most = (c.a.k > c.b.k ? c.a.k : c.b.k) * c.runs / 512;
-      if (s > most) s = most;
-      if (s > 8) s = 8;
-      if (s > 1) {
-        c.splits = (int32_t)s;
-        c.ld_part = up8(c.n);
-        c.part = (float *)arena.take((uint64_t)s * c.m * c.ld_part * 4);
-      }
+  // A launch's products on the kind of tile that takes the least time.  A step over one tile a compute unit takes 1.3 us with tiles of 256 x 256
+  // and 0.58 us with 128 x 128, 1.03 us for two of those at once (measured over 64 steps: 2,048 x 4,096 83 and 66 us, 1,024 x 4,096 79 and 37,
+  // 512 x 22,016 83 and 132, 4,096 x 11,008 240 and 400); no launch takes less than its longest tile.  Where small tiles are too few for the
+  // compute units, the sums of a first product with a plain 16-bit output are split as well, 512 of them a part at least.
+  void launch(int products, GemmGroup &g) {
+    double work_big = 0, work_small = 0, longest = 0;
+    int64_t small = 0;
+    for (int i = 0; i < g.count; ++i) {
+      const GemmCall &c = g.call[i];
+      const int64_t n = products == GEMM_GATE_UP ? 2 * c.n : c.n, k = sums(c), t = ((c.m + 127) / 128) * ((n + 127) / 128);
+      work_big += (double)(((c.m + 255) / 256) * ((n + 255) / 256)) * k;
+      work_small += (double)t * k;
+      small += t;
+      if (k > longest) longest = (double)k;
     }
-    if (!run || c.m == 0) return;
-    c.act = f->activation;
-    ok = ok && (f->dtype == CHM_BF16 ? gemm_launch_bf16 : gemm_launch_f16)(product, tile, c, st);
+    // the first product's sums may be split: as far as that gives every compute unit a tile
+    const bool may_split = products == GEMM_OUT || products == GEMM_BACK;
+    int64_t splits = 1;
+    double longest_small = longest;
+    if (may_split) {
+      GemmCall &c = g.call[0];
+      const int64_t k = sums(c), t = ((c.m + 127) / 128) * ((c.n + 127) / 128);
+      splits = (256 - (small - t < 0 ? 0 : small - t)) / (t > 0 ? t : 1);
+      // and so that no part is much longer than the launch's other tiles, taken together, keep the compute units busy
+      const int64_t even = (int64_t)((double)k * 512 / (work_small > 1 ? work_small : 1));
+      if (splits < even) splits = even;
+      if (splits > k / 512) splits = k / 512;
+      if (splits > 8) splits = 8;
+      if (splits < 1) splits = 1;
+      longest_small = (double)k / splits;
+      for (int i = 1; i < g.count; ++i) longest_small = sums(g.call[i]) > longest_small ? (double)sums(g.call[i]) : longest_small;
+      small += t * (splits - 1);
+    }
+    const auto most = [](double a, double b) { return a > b ? a : b; };
+    const double time_big = most(work_big / 256, longest) * 1.3;
+    const double time_small = small <= 256 ? longest_small * 0.58 : most(work_small / 512, longest_small) * 1.03;
+    const int tile = time_big < time_small ? TILE_256 : small <= 256 ? TILE_128_DEEP : TILE_128, side = tile == TILE_256 ? 256 : 128;
+    g.first[0] = 0;
+    for (int i = 0; i < g.count; ++i) {
+      GemmCall &c = g.call[i];
+      const int64_t n = products == GEMM_GATE_UP ? 2 * c.n : c.n;
+      c.tiles_m = (int32_t)((c.m + side - 1) / side);
+      c.tiles_n = (int32_t)((n + side - 1) / side);
+      c.splits = i == 0 && tile != TILE_256 ? (int32_t)splits : 1;
+      c.act = f->activation;
+      if (c.splits > 1) {
+        c.ld_part = up8(c.n);
+        c.part = (float *)arena.take((uint64_t)c.splits * c.m * c.ld_part * 4);
+      }
+      g.first[i + 1] = g.first[i] + ((c.tiles_m * c.tiles_n + 7) & ~7) * c.splits;
+    }
+    if (!run || g.first[g.count] == 0) return;
+    ok = ok && (f->dtype == CHM_BF16 ? gemm_launch_bf16 : gemm_launch_f16)(products, tile, g, st);
+    const GemmCall &c = g.call[0];
     if (c.splits > 1) {
       const dim3 grid(copy_groups(c.m * (c.ld_part / 8)));
       if (f->dtype == CHM_BF16)
@@ -351,6 +379,7 @@ struct Pass {
       ok = ok && hipGetLastError() == hipSuccess;
     }
   }
+  static int64_t sums(const GemmCall &c) { return (c.a.k > c.b.k ? c.a.k : c.b.k) * c.runs; }
 
   void forward(void *y, int64_t ld_y) {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
@@ -381,20 +410,21 @@ struct Pass {
     Matrix wg{f->w_gate, f->ld_gate, F, D}, wu{f->w_up, f->ld_up, F, D};
     packed_pair(wg, wu);
     flush();
-    GemmCall c{};
+    GemmGroup first{}, second{};
+    first.count = second.count = 1;
+    GemmCall &c = first.call[0], &d = second.call[0];
     c.a = GemmOperand{{x.p, x.p}, x.ld, x.cols};
     c.b = GemmOperand{{wg.p, wu.p}, wg.ld, wg.cols};
     c.m = T; c.n = F;
     c.runs = 1;
     c.h = h; c.kept = kept; c.ldi = F8;
-    launch(GEMM_GATE_UP, c, false);
-    GemmCall d{};
+    launch(GEMM_GATE_UP, first);
     d.a = GemmOperand{{h, h}, F8, F8};
     d.b = GemmOperand{{wd.p, wd.p}, wd.ld, wd.cols};
     d.m = T; d.n = D;
     d.runs = 1;
     out(d, y, ld_y, D);
-    launch(GEMM_OUT, d, true);
+    launch(GEMM_OUT, second);
   }
 
   // one 16-bit output of `cols` columns
@@ -414,25 +444,34 @@ struct Pass {
     packed_pair(wg, wu);
     flush();
 
-    GemmCall a{};                          // dh, and h, dg, du
+    GemmGroup first{}, second{};
+    first.count = 1;
+    second.count = 3;
+    GemmCall &a = first.call[0];           // dh, and h, dg, du
     a.a = GemmOperand{{dy.p, dy.p}, dy.ld, dy.cols};
     a.b = GemmOperand{{wd.p, wd.p}, wd.ld, D};
     a.m = T; a.n = F8; a.n_real = F;
     a.runs = 1;
     a.h = h; a.kept = kept; a.ldi = F8;
     a.dgate = d; a.dup = d + F8; a.ldd = 2 * F8;
-    launch(GEMM_DH, a, false);
+    launch(GEMM_DH, first);
 
-    GemmCall b{};                          // dWd
+    GemmCall &i = second.call[0];          // dx
+    i.a = GemmOperand{{d, d + F8}, 2 * F8, F8};
+    i.b = GemmOperand{{wg.p, wu.p}, wg.ld, F};
+    i.m = T; i.n = wg.cols;
+    i.runs = 2;
+    out(i, g->dx, g->ld_dx, D);
+
+    GemmCall &b = second.call[1];          // dWd
     b.a = GemmOperand{{dy.p, dy.p}, dy.ld, T};
     b.b = GemmOperand{{h, h}, F8, T};
     b.m = D; b.n = F8;
     b.runs = 1;
     out(b, g->dw_down, g->ld_dw_down, F);
     grad(b, g);
-    launch(GEMM_DW, b, false);
 
-    GemmCall e{};                          // dWg, dWu
+    GemmCall &e = second.call[2];          // dWg, dWu
     e.a = GemmOperand{{d, d}, 2 * F8, T};
     e.b = GemmOperand{{x.p, x.p}, x.ld, T};
     e.m = 2 * F8; e.n = x.cols;
@@ -441,15 +480,7 @@ struct Pass {
     e.c[1] = g->dw_up;
     e.m_first = F8; e.m_real = F;
     grad(e, g);
-    launch(GEMM_DW, e, false);
-
-    GemmCall i{};                          // dx
-    i.a = GemmOperand{{d, d + F8}, 2 * F8, F8};
-    i.b = GemmOperand{{wg.p, wu.p}, wg.ld, F};
-    i.m = T; i.n = wg.cols;
-    i.runs = 2;
-    out(i, g->dx, g->ld_dx, D);
-    launch(GEMM_DX, i, true);
+    launch(GEMM_BACK, second);
   }
 
   void grad(GemmCall &c, const chm_ffn_gradients *g) {

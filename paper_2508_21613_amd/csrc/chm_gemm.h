@@ -183,16 +183,20 @@ struct Fragments {
   }
 };
 
-// tile of this workgroup: consecutive tiles of one die (workgroups go round the 8 dies) share operands in its cache, in bands
-// of 8 tiles along m
-__device__ __forceinline__ void tile_of(const GemmCall &c, int &tm, int &tn) {
-  const int n = c.tiles_m * c.tiles_n, die = blockIdx.x & 7, i = blockIdx.x >> 3;
-  const int per = n >> 3, rem = n & 7;
+// Tile and part of the sums of workgroup `block` of a call; false: there is none (a call's workgroups are made a multiple of 8).  Consecutive
+// tiles of one die (workgroups go round the 8 dies) share operands in its cache, in bands of 8 tiles along m.
+__device__ __forceinline__ bool tile_of(const GemmCall &c, int block, int &tm, int &tn, int &split) {
+  const int n = c.tiles_m * c.tiles_n, padded = (n + 7) & ~7;
+  split = block / padded;
+  block -= split * padded;
+  const int die = block & 7, i = block >> 3, per = n >> 3, rem = n & 7;
+  if (i >= per + (die < rem)) return false;
   const int t = die * per + (die < rem ? die : rem) + i;
   const int band = 8 * c.tiles_n, b = t / band, r = t - b * band;
   const int rows = c.tiles_m - b * 8 < 8 ? c.tiles_m - b * 8 : 8;
   tm = b * 8 + r % rows;
   tn = r / rows;
+  return true;
 }
 
 template <class T> __device__ __forceinline__ s8 pack8(const float *v) {
@@ -202,16 +206,17 @@ template <class T> __device__ __forceinline__ s8 pack8(const float *v) {
   return r;
 }
 
-// What large products store goes past the caches (PAST), where it would displace the operands: 4,096 tokens, product with two weights 585 us
-// without and 540 with it, gradient of the activation 389 and 379, 8,192^3 805 and 743.
+// What large products store for the caller or for much later goes past the caches (PAST), where it would displace the operands: a step of 4,096
+// tokens, 4,096 x 11,008, takes 2,754 us with and 2,818 without.  What the next launch reads (h, the gradients of the projections) is better left
+// there.
 #define CHM_PUT(p, v) do { if (PAST) __builtin_nontemporal_store(v, p); else *(p) = v; } while (0)
 
 // Eight values of row m from column n on: part of a split sum, or a plain output
 template <class T, int PAST>
-__device__ __forceinline__ void finish_plain(const GemmCall &c, int64_t m, int64_t n, const f4 *v) {
+__device__ __forceinline__ void finish_plain(const GemmCall &c, int split, int64_t m, int64_t n, const f4 *v) {
   if (m >= c.m || n >= c.n) return;
   if (c.splits > 1) {
-    float *p = c.part + ((int64_t)blockIdx.y * c.m + m) * c.ld_part + n;
+    float *p = c.part + ((int64_t)split * c.m + m) * c.ld_part + n;
     *(f4 *)p = v[0];
     *(f4 *)(p + 4) = v[1];
     return;
@@ -320,7 +325,7 @@ __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_
 }
 
 // Eight features of dh: the gradients of both projections, and h
-template <class T, int ACT, int PAST>
+template <class T, int ACT>
 __device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, int64_t f, const f4 *v, const Kept8 &k) {
   if (m >= c.m || f >= c.n) return;
   float g[8], u[8], h[8], dg[8], du[8];
@@ -350,7 +355,7 @@ typedef __attribute__((address_space(3))) f4 lds_f4;
 // A wavefront's ROWS_ rows of 64 sums, turned round in shared memory at `turn`; m1, n1: the first row and column (feature) of them.
 // A loop, not a sequence: code that runs once a tile is read from the cache of instructions' own source, and slowly.
 template <class T, int DUAL, int EPI, int ACT, int ROWS_, int PAST>
-__device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, int64_t m1, int64_t n1, int lane) {
+__device__ __forceinline__ void finish(const GemmCall &c, int split, const lds_char *turn, int64_t m1, int64_t n1, int lane) {
   if (DUAL) {                               // 16 rows of 32 features at a time
     const int f = (lane & 3) * 8;
 #pragma nounroll
@@ -377,7 +382,7 @@ __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, 
         const Kept8 k = kept[i];
         kept[i] = kept8(c.kept, m + 16 < last ? m + 16 : last, col);
         const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
-        finish_gradient<T, ACT, PAST>(c, m, n, v, k);
+        finish_gradient<T, ACT>(c, m, n, v, k);
         at += 8 * TURN_ROW;
         m += 8;
       }
@@ -387,7 +392,7 @@ __device__ __forceinline__ void finish(const GemmCall &c, const lds_char *turn, 
 #pragma nounroll
   for (int r = 0; r < ROWS_; r += 8) {
     const f4 v[2] = {*(const lds_f4 *)at, *(const lds_f4 *)(at + 16)};
-    finish_plain<T, PAST>(c, m, n, v);
+    finish_plain<T, PAST>(c, split, m, n, v);
     at += 8 * TURN_ROW;
     m += 8;
   }
@@ -438,20 +443,24 @@ __device__ __forceinline__ void multiply(const F &now, F &next, f4 (&acc)[4][MT]
   }
 }
 
+// bytes of shared memory of a configuration: the steps under way, or the sums that are turned round at the end
+template <int WM, int WN, int MT, int SLOTS> constexpr int shared_bytes() {
+  constexpr int stage = (WM * MT * 16 + WN * 64) * BK * 2, turn = WM * WN * (MT < 4 ? MT * 16 : 64) * TURN_ROW;
+  return SLOTS * stage > turn ? SLOTS * stage : turn;
+}
+
+// One tile of one product
 template <class T, int A_KIND, int B_KIND, int DUAL, int EPI, int WM, int WN, int MT, int SLOTS>
-__global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(MT == 2 && SLOTS == 2 ? 4 : 2))) k_gemm(const GemmCall c) {
-#ifdef __HIP_DEVICE_COMPILE__        // the host pass knows no buffer descriptors
+__device__ __forceinline__ void tile_product(const GemmCall &c, int block, lds_char *lds) {
   constexpr int NT = 64 * WM * WN, TM = WM * MT * 16, TN = WN * 64;
   typedef Feed<A_KIND, 0, TM, NT> FeedA;
   typedef Feed<B_KIND, DUAL, TN, NT> FeedB;
   typedef Fragments<A_KIND, B_KIND, TM, TN, MT> Frags;
   constexpr int STAGE = FeedA::BYTES + FeedB::BYTES, LOADS = FeedA::NI + FeedB::NI;
   constexpr int TURN = MT < 4 ? MT * 16 : 64;        // rows turned round at a time
-  __shared__ __attribute__((aligned(1024))) char shared[SLOTS * STAGE > WM * WN * TURN * TURN_ROW ? SLOTS * STAGE : WM * WN * TURN * TURN_ROW];
-  lds_char *lds = (lds_char *)shared;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int tm, tn;
-  tile_of(c, tm, tn);
+  int tm, tn, split;
+  if (!tile_of(c, block, tm, tn, split)) return;
   const int64_t m0 = (int64_t)tm * TM, n0 = (int64_t)tn * (DUAL ? TN / 2 : TN);
   const int wm = (wave / WN) * (MT * 16), wn = (wave % WN) * 64;
 
@@ -459,8 +468,8 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
   const int steps_seg = (int)((c.a.k > c.b.k ? c.a.k : c.b.k) + BK - 1) / BK, steps = steps_seg * c.runs;
   int step = 0, last = steps;
   if (c.splits > 1) {
-    step = (int)((int64_t)steps * blockIdx.y / c.splits);
-    last = (int)((int64_t)steps * (blockIdx.y + 1) / c.splits);
+    step = (int)((int64_t)steps * split / c.splits);
+    last = (int)((int64_t)steps * (split + 1) / c.splits);
   }
   Fetch<FeedA, FeedB> fetch{c, {}, {}, c.runs > 1 ? steps_seg : -1, wave, tid, (uint32_t)(uintptr_t)lds};
   const int seg = c.runs > 1 && step >= steps_seg;
@@ -510,33 +519,48 @@ __global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_p
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
     const int64_t m1 = m0 + wm + t0 * 16, n1 = n0 + (DUAL ? wn / 2 : wn);
-    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, TURN, MT == 8>(c, turn, m1, n1, lane);
-    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, TURN, MT == 8>(c, turn, m1, n1, lane);
-    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, TURN, MT == 8>(c, turn, m1, n1, lane);
+    if (EPI == EPI_STORE || c.act == CHM_ACT_SILU) finish<T, DUAL, EPI, CHM_ACT_SILU, TURN, MT == 8>(c, split, turn, m1, n1, lane);
+    else if (c.act == CHM_ACT_GELU) finish<T, DUAL, EPI, CHM_ACT_GELU, TURN, MT == 8>(c, split, turn, m1, n1, lane);
+    else finish<T, DUAL, EPI, CHM_ACT_GELU_TANH, TURN, MT == 8>(c, split, turn, m1, n1, lane);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
+  }
+}
+
+template <class T, int PRODUCTS, int WM, int WN, int MT, int SLOTS>
+__global__ void __launch_bounds__(64 * WM * WN, 1) __attribute__((amdgpu_waves_per_eu(MT == 2 && SLOTS == 2 ? 4 : 2))) k_gemm(const GemmGroup g) {
+#ifdef __HIP_DEVICE_COMPILE__        // the host pass knows no instructions of the matrix cores
+  __shared__ __attribute__((aligned(1024))) char shared[shared_bytes<WM, WN, MT, SLOTS>()];
+  lds_char *lds = (lds_char *)shared;
+  const int block = blockIdx.x;
+  if (PRODUCTS == GEMM_GATE_UP) tile_product<T, ROWS, ROWS, 1, EPI_ACT, WM, WN, MT, SLOTS>(g.call[0], block, lds);
+  else if (PRODUCTS == GEMM_OUT) tile_product<T, ROWS, ROWS, 0, EPI_STORE, WM, WN, MT, SLOTS>(g.call[0], block, lds);
+  else if (PRODUCTS == GEMM_DH) tile_product<T, ROWS, COLS, 0, EPI_ACT_GRAD, WM, WN, MT, SLOTS>(g.call[0], block, lds);
+  else if (block < g.first[1]) tile_product<T, ROWS, COLS, 0, EPI_STORE, WM, WN, MT, SLOTS>(g.call[0], block, lds);
+  else {
+    const int i = block < g.first[2] ? 1 : 2;
+    tile_product<T, COLS, COLS, 0, EPI_STORE, WM, WN, MT, SLOTS>(g.call[i], block - g.first[i], lds);
   }
 #endif
 }
 
-template <class T, int A_KIND, int B_KIND, int DUAL, int EPI>
-bool launch_product(int tile, const GemmCall &c, hipStream_t st) {
-  const dim3 grid((uint32_t)(c.tiles_m * c.tiles_n), (uint32_t)(c.splits > 1 ? c.splits : 1));
-  if (tile == TILE_256) hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 2, 4, 8, 2>), grid, dim3(512), 0, st, c);
-  else if (tile == TILE_128_DEEP) hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 4, 2, 2, 4>), grid, dim3(512), 0, st, c);
-  else hipLaunchKernelGGL((k_gemm<T, A_KIND, B_KIND, DUAL, EPI, 4, 2, 2, 2>), grid, dim3(512), 0, st, c);
+template <class T, int PRODUCTS>
+bool launch_products(int tile, const GemmGroup &g, hipStream_t st) {
+  const dim3 grid((uint32_t)g.first[g.count]);
+  if (tile == TILE_256) hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 2, 4, 8, 2>), grid, dim3(512), 0, st, g);
+  else if (tile == TILE_128_DEEP) hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 4, 2, 2, 4>), grid, dim3(512), 0, st, g);
+  else hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 4, 2, 2, 2>), grid, dim3(512), 0, st, g);
   return hipGetLastError() == hipSuccess;
 }
 
 template <class T>
-bool launch(int product, int tile, const GemmCall &c, void *stream) {
+bool launch(int products, int tile, const GemmGroup &g, void *stream) {
   hipStream_t st = (hipStream_t)stream;
-  switch (product) {
-    case GEMM_GATE_UP: return launch_product<T, ROWS, ROWS, 1, EPI_ACT>(tile, c, st);
-    case GEMM_OUT: return launch_product<T, ROWS, ROWS, 0, EPI_STORE>(tile, c, st);
-    case GEMM_DH: return launch_product<T, ROWS, COLS, 0, EPI_ACT_GRAD>(tile, c, st);
-    case GEMM_DX: return launch_product<T, ROWS, COLS, 0, EPI_STORE>(tile, c, st);
-    default: return launch_product<T, COLS, COLS, 0, EPI_STORE>(tile, c, st);
+  switch (products) {
+    case GEMM_GATE_UP: return launch_products<T, GEMM_GATE_UP>(tile, g, st);
+    case GEMM_OUT: return launch_products<T, GEMM_OUT>(tile, g, st);
+    case GEMM_DH: return launch_products<T, GEMM_DH>(tile, g, st);
+    default: return launch_products<T, GEMM_BACK>(tile, g, st);
   }
 }
 

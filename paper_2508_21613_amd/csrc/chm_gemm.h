@@ -292,7 +292,7 @@ __device__ __forceinline__ void keep8(const Kept &k, int64_t m, int64_t f, const
 struct Kept8 { u4 g, u, lo; };
 __device__ __forceinline__ Kept8 kept8(const Kept &k, int64_t m, int64_t f) {
   const char *p = kept_at(k, m, f);
-  return Kept8{*(const u4 *)p, *(const u4 *)(p + 1024), *(const u4 *)(p + 2048)};
+  return Kept8{__builtin_nontemporal_load((const u4 *)p), __builtin_nontemporal_load((const u4 *)(p + 1024)), __builtin_nontemporal_load((const u4 *)(p + 2048))};
 }
 __device__ __forceinline__ void unkeep8(u4 hi, u2 lo, float *v) {
 #pragma unroll
@@ -320,7 +320,7 @@ __device__ __forceinline__ void finish_pair(const GemmCall &c, int64_t m, int64_
       if (f + e >= c.n) g[e] = u[e] = h[e] = 0.f;
   }
   const int64_t at = m * c.ldi + f;
-  CHM_PUT((s8 *)(c.h + at), pack8<T>(h));
+  *(s8 *)(c.h + at) = pack8<T>(h);
   if (c.kept.p) keep8<PAST>(c.kept, m, f, g, u);
 }
 
@@ -345,9 +345,9 @@ __device__ __forceinline__ void finish_gradient(const GemmCall &c, int64_t m, in
     for (int e = 0; e < 8; ++e)
       if (f + e >= c.n_real) h[e] = du[e] = dg[e] = 0.f;
   }
-  CHM_PUT((s8 *)(c.h + m * c.ldi + f), pack8<T>(h));
-  CHM_PUT((s8 *)(c.dgate + m * c.ldd + f), pack8<T>(dg));
-  CHM_PUT((s8 *)(c.dup + m * c.ldd + f), pack8<T>(du));
+  *(s8 *)(c.h + m * c.ldi + f) = pack8<T>(h);
+  *(s8 *)(c.dgate + m * c.ldd + f) = pack8<T>(dg);
+  *(s8 *)(c.dup + m * c.ldd + f) = pack8<T>(du);
 }
 
 typedef __attribute__((address_space(3))) f4 lds_f4;

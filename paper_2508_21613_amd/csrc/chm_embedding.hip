@@ -202,7 +202,17 @@ __global__ void __launch_bounds__(1024) k_sort_ranges(Tokens tokens, int n, uint
     const uint64_t ins = __ballot(in);
     if (!ins) continue;
     const uint32_t d = in ? key[r] - base : 0;
-    const uint64_t m = __popcll(ins) == 1 ? ins : same_digit(d, DIGIT) & ins;
+    uint64_t m = 0;
+    if (__popcll(ins) > 8) {
+      m = same_digit(d, DIGIT) & ins;
+    } else {                                // few lanes: key by key
+      for (uint64_t left = ins; left;) {
+        const uint32_t one = __builtin_amdgcn_readlane(d, __ffsll((unsigned long long)left) - 1);
+        const uint64_t same = __ballot(in && d == one);
+        if (d == one) m = same;
+        left &= ~same;
+      }
+    }
     if (in) {
       const uint32_t to = mine[d * 16];
       const uint32_t p = to + __popcll(m & ((1ull << lane) - 1));
@@ -306,7 +316,7 @@ struct Gather {
   char *grad;
   float *part;                           // [pieces][2][width rounded up to 8]
   int64_t n, ld_dy, ld_grad;             // rows in bytes
-  int32_t width, across, piece, pieces;
+  int32_t width, across, zero_across, piece, pieces;
   int32_t piece_groups;                  // workgroups (along x) that take pieces; the ones behind set rows to zero
   int32_t accumulate;
   float scale;
@@ -330,10 +340,12 @@ template <int GT>
 __device__ __forceinline__ void zero_rows(const Gather &c, int64_t first, const uint8_t *named) {
   constexpr int N = Lane<GT>::N;
   const float zero[N] = {};
-  const int groups = (c.width + N - 1) / N;
-  for (int i = threadIdx.x; i < ZERO_ROWS * groups; i += NT) {
-    const int r = i / groups, col = (i - r * groups) * N;
-    if (!named[r]) row_store<GT, N, 1>(c.grad + (first + r) * c.ld_grad + (int64_t)col * Lane<GT>::SIZE, c.width - col, zero);
+  // a power of two of threads along a row, as many rows at a time as that leaves
+  const int x = threadIdx.x & (c.zero_across - 1), down = NT / c.zero_across;
+  for (int r = threadIdx.x / c.zero_across; r < ZERO_ROWS; r += down) {
+    if (named[r]) continue;
+    char *row = c.grad + (first + r) * c.ld_grad;
+    for (int col = x * N; col < c.width; col += c.zero_across * N) row_store<GT, N, 1>(row + (int64_t)col * Lane<GT>::SIZE, c.width - col, zero);
   }
 }
 
@@ -399,7 +411,7 @@ __global__ void __launch_bounds__(NT) k_runs(Gather c) {
 // Runs that cross pieces: the piece in which one starts adds up what the others have left, in order.  A workgroup takes 256 columns of
 // JOIN_PIECES pieces, its four wavefronts a quarter of every run each, so that the most frequent token's run (some ten percent of the places)
 // is no chain of additions as long as its pieces.
-constexpr int JOIN_PIECES = 8;
+constexpr int JOIN_PIECES = 2;
 template <int GT>
 __global__ void __launch_bounds__(NT) k_join(Gather c) {
   constexpr int N = 4, AT_ONCE = 8;
@@ -529,6 +541,13 @@ int across_of(int64_t groups) {
   return a;
 }
 
+// at most that many threads
+int zero_across_of(int64_t groups) {
+  int a = 8;
+  while (a < NT && a * 2 <= groups) a <<= 1;
+  return a;
+}
+
 // places of a piece: about 512 pieces and more, 8 to 64 places each
 int piece_of(int64_t n) {
   int p = 8;
@@ -555,7 +574,8 @@ Scratch scratch_of(int64_t n, int64_t rows, int64_t width) {
 }
 
 template <int DT, int GT>
-bool launch_few(const Gather &c, hipStream_t st) {
+bool launch_few(Gather c, hipStream_t st) {
+  c.zero_across = zero_across_of(c.width / Lane<GT>::N);
   const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
   const int cols = (c.width + NT * Lane<DT>::N - 1) / (NT * Lane<DT>::N);
   if (c.n + zero) hipLaunchKernelGGL((k_few<DT, GT>), dim3((uint32_t)(c.n + zero), cols), dim3(NT), 0, st, c);
@@ -566,6 +586,7 @@ template <int DT, int GT>
 bool launch_runs(Gather c, hipStream_t st) {
   const int64_t groups = (c.width + Lane<DT>::N - 1) / Lane<DT>::N;
   c.across = across_of(groups);
+  c.zero_across = zero_across_of(c.width / Lane<GT>::N);
   const int down = NT / c.across;
   c.piece_groups = (c.pieces + down - 1) / down;
   const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;

@@ -3,7 +3,7 @@
 The gated feed-forward block forward and backward, the embedding's lookup and gradient, the global gradient norm with clipping.
 As everywhere in this package torch provides device memory and streams; every value is computed by the library's HIP kernels, and
 without a usable GPU the calls fail.  A call works on the current stream, or on `stream`; scratch and results that the caller does
-not hand in are allocated on that stream.  Inputs used there must be ready there, as with any torch call.  Wrong arguments raise
+not hand in are allocated on that stream.  Inputs must be ready there, as with any torch call.  Wrong arguments raise
 binding.ChmError with the library's code.
 """
 import ctypes as C
@@ -48,17 +48,22 @@ def _matrix(name, t, rows=None, cols=None, dtype=None, device=None):
 
 
 class _Other:
-    """another stream or device than the current one, made current for the launches and allocations within"""
+    """another stream or device than the current one, made current for the launches and allocations within; the caller's tensors are
+    not given to anybody else before the work there has been done"""
 
-    def __init__(self, stream, device):
+    def __init__(self, stream, device, tensors):
         if isinstance(stream, int):
             stream = torch.cuda.ExternalStream(stream, device=torch.device("cuda", device))
         self.scopes = [torch.cuda.device(device)] + ([torch.cuda.stream(stream)] if stream is not None else [])
-        self.device = device
+        self.device, self.tensors = device, tensors
 
     def __enter__(self):
         for scope in self.scopes:
             scope.__enter__()
+        stream = torch.cuda.current_stream()
+        for t in self.tensors:
+            if t is not None:
+                t.record_stream(stream)
         return torch._C._cuda_getCurrentRawStream(self.device)
 
     def __exit__(self, *exc):
@@ -79,11 +84,11 @@ class _Current:
         pass
 
 
-def _scope(stream, device):
-    """scope of a call on the GPU of that index: the stream to launch on, current for what is allocated within"""
+def _scope(stream, device, *tensors):
+    """scope of a call on the GPU of that index with these tensors: the stream to launch on, current for what is allocated within"""
     if stream is None and torch._C._cuda_getDevice() == device:
         return _Current(torch._C._cuda_getCurrentRawStream(device))
-    return _Other(stream, device)
+    return _Other(stream, device, tensors)
 
 
 def _bytes(n, like):
@@ -113,7 +118,7 @@ def ffn_forward(x, w_gate, w_up, w_down, activation="silu", save=False, out=None
     d, T, D, F, dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
     ld_y = D if out is None else _matrix("out", out, T, D, dtype, dev)
     lib = B.lib()
-    with _scope(stream, dev) as st:
+    with _scope(stream, dev, x, w_gate, w_up, w_down, out) as st:
         need, scratch = C.c_uint64(), C.c_uint64()
         B._check(lib.chm_ffn_sizes(d, None, need, scratch, None))
         saved = None
@@ -144,7 +149,7 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, activation="silu", grads=No
         lds = (_matrix("grads[0]", grads[0], F, D, dtype, dev), _matrix("grads[1]", grads[1], F, D, dtype, dev),
                _matrix("grads[2]", grads[2], D, F, dtype, dev))
     lib = B.lib()
-    with _scope(stream, dev) as st:
+    with _scope(stream, dev, dy, x, w_gate, w_up, w_down, saved, out, *(grads or ())) as st:
         if out is None:
             out = x.new_empty((T, D))
         if grads is None:
@@ -177,7 +182,7 @@ def embedding_lookup(tokens, table, scale=1.0, out=None, stream=None):
     bits, n = _tokens(tokens, dev)
     rows, width = table.shape
     ld_out = width if out is None else _matrix("out", out, n, width, dtype, dev)
-    with _scope(stream, dev) as st:
+    with _scope(stream, dev, tokens, table, out) as st:
         if out is None:
             out = table.new_empty((n, width))
         B._check(B.lib().chm_embedding_lookup(DTYPES[dtype], bits, tokens.data_ptr(), n, table.data_ptr(), ld, rows, width, scale,
@@ -203,7 +208,7 @@ def embedding_gradient(dy, tokens, rows=None, scale=1.0, out=None, accumulate=Fa
         rows, grad_dtype = out.shape[0], out.dtype
         _need(grad_dtype in (dtype, torch.float32), "out must be of dy's type or float32")
     lib = B.lib()
-    with _scope(stream, dev) as st:
+    with _scope(stream, dev, dy, tokens, out) as st:
         if out is None:
             out = dy.new_empty((rows, width))
         scratch = C.c_uint64()
@@ -278,7 +283,7 @@ class Gradients:
         if sumsq is not None:
             _need(isinstance(sumsq, torch.Tensor) and sumsq.device == self.device and sumsq.dtype == torch.float64 and sumsq.numel() == 1,
                   "sumsq must be a float64 tensor of one element")
-        with _scope(stream, self.device.index) as st:
+        with _scope(stream, self.device.index, sumsq) as st:
             norm = torch.empty((), dtype=torch.float32, device=self.device)
             B._check(B.lib().chm_clip_gradients(self._h, max_norm, None if sumsq is None else sumsq.data_ptr(), norm.data_ptr(), st))
         return norm

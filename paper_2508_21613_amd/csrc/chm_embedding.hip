@@ -8,7 +8,7 @@
 // list is cut into pieces of equal length: a group of threads sums up one piece, stores runs that lie inside it, and leaves the
 // float32 sums of runs that cross its ends (two at most) for a second launch, which adds them in order.  Rows that no token
 // names are set to zero by further workgroups of the same launch, which look them up in the sorted list: the dense gradient is written
-// once.  Up to 256 places (a few sequences' ends, a probe) nothing is sorted: every workgroup finds the places of its token itself.
+// once.  Up to 512 places (a few sequences' ends, a probe) nothing is sorted: every workgroup finds the places of its token itself.
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
@@ -20,7 +20,7 @@ using namespace chm_elements;
 
 constexpr int NT = 256;
 typedef float f4 __attribute__((ext_vector_type(4)));
-constexpr int SMALL = 256;               // places the unsorted kernel takes
+constexpr int SMALL = 512;               // places the unsorted kernel takes
 constexpr int RANGES_MAX = 16384, RANGE_ROWS = 512 * 512 - 1;      // places and rows the sort by ranges of keys takes
 constexpr int BINS = 512, DIGIT = 9;
 constexpr int SORT_GROUPS = 64;
@@ -473,41 +473,47 @@ __global__ void __launch_bounds__(NT) k_join(Gather c) {
   }
 }
 
-// n <= 256: workgroup (t, columns) sums up the places of the token at t if t is its first; the ones behind set rows to zero
+// n <= SMALL: workgroup (t, columns) sums up the places of the token at t if t is its first; the ones behind set rows to zero
 template <int DT, int GT>
 __global__ void __launch_bounds__(NT) k_few(Gather c) {
   typedef Lane<DT> L;
-  constexpr int N = L::N, AT_ONCE = 8;
-  __shared__ uint32_t keys[SMALL];
-  __shared__ uint16_t list[SMALL + AT_ONCE];
+  constexpr int N = L::N, AT_ONCE = 8, EACH = SMALL / NT, WAVES = NT / 64;
   const int n = (int)c.n;
-  const uint32_t own = (int)threadIdx.x < n ? key_of(c.tokens, threadIdx.x) : ~0u;
-  keys[threadIdx.x] = own;
+  uint32_t own[EACH];                       // tokens threadIdx.x, threadIdx.x + NT, ...
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) own[i] = (int)threadIdx.x + i * NT < n ? key_of(c.tokens, threadIdx.x + i * NT) : ~0u;
   if ((int)blockIdx.x >= n) {
     if (blockIdx.y) return;
     __shared__ uint8_t named[ZERO_ROWS];
     const int64_t first = (int64_t)(blockIdx.x - n) * ZERO_ROWS;
     if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x >= c.tokens.rows;
     __syncthreads();
-    if (own < c.tokens.rows && own >= first && own < first + ZERO_ROWS) named[own - first] = 1;
+#pragma unroll
+    for (int i = 0; i < EACH; ++i)
+      if (own[i] < c.tokens.rows && own[i] >= first && own[i] < first + ZERO_ROWS) named[own[i] - first] = 1;
     __syncthreads();
     zero_rows<GT>(c, first, named);
     return;
   }
-  __shared__ int counts[NT / 64];
-  __syncthreads();
-  const uint32_t key = keys[blockIdx.x];
-  const bool match = own == key;
-  const uint64_t m = __ballot(match);
+  __shared__ uint16_t list[SMALL];
+  __shared__ int counts[EACH * WAVES];
+  const uint32_t key = key_of(c.tokens, blockIdx.x);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (lane == 0) counts[wave] = __popcll(m);
-  __syncthreads();
-  int at = __popcll(m & ((1ull << lane) - 1)), total = 0;
-  for (int w = 0; w < NT / 64; ++w) {
-    if (w < wave) at += counts[w];
-    total += counts[w];
+  uint64_t m[EACH];
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    m[i] = __ballot(own[i] == key);
+    if (lane == 0) counts[i * WAVES + wave] = __popcll(m[i]);
   }
-  if (match) list[at] = (uint16_t)threadIdx.x;
+  __syncthreads();
+  int total = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    int at = __popcll(m[i] & ((1ull << lane) - 1));
+    for (int w = 0; w < i * WAVES + wave; ++w) at += counts[w];
+    if (own[i] == key) list[at] = (uint16_t)(threadIdx.x + i * NT);
+  }
+  for (int w = 0; w < EACH * WAVES; ++w) total += counts[w];
   __syncthreads();
   if (key >= c.tokens.rows || list[0] != blockIdx.x) return;
   const int col = (blockIdx.y * NT + threadIdx.x) * N, left = c.width - col;

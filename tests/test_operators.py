@@ -287,7 +287,7 @@ def gradient_want(dy, tokens, V, scale):
     return v, ACC ** 2 * (counts + 2) * sq
 
 
-EMBED = [(1, 1, 1), (1, 5, 64), (7, 3, 9), (255, 40, 31), (256, 100, 515), (257, 100, 515), (300, 7, 64), (1000, 1, 72), (1024, 33, 8), (2049, 5000, 100),
+EMBED = [(1, 1, 1), (1, 5, 64), (7, 3, 9), (255, 40, 31), (256, 100, 515), (257, 100, 515), (300, 7, 64), (511, 60, 9), (512, 300, 70), (513, 300, 70), (1000, 1, 72), (1024, 33, 8), (2049, 5000, 100),
          (4096, 100, 2049), (5000, 513, 130), (16384, 3000, 72), (16385, 511, 40), (40000, 70000, 24), (70001, 129, 16)]
 
 
@@ -338,7 +338,7 @@ def test_embedding(ops, shape, kind, dtype):
 
 
 @pytest.mark.parametrize("kind", ["same", "none"])
-@pytest.mark.parametrize("n", [1, 200, 3000, 20000])
+@pytest.mark.parametrize("n", [1, 200, 500, 3000, 20000])
 def test_embedding_one_token_or_none(ops, n, kind):
     V, D = 37, 100
     tokens, dy = make_tokens(1, n, V, torch.int64, kind), normal(gen(2), n, D, torch.float32)

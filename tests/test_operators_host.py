@@ -71,8 +71,8 @@ def test_null_pointers():
 
 def test_embedding_sizes_and_refusals():
     L, n = B.lib(), C.c_uint64()
-    assert L.chm_embedding_gradient_scratch(256, 1000, 64, n) == B.OK and n.value == 0
-    assert L.chm_embedding_gradient_scratch(257, 1000, 64, n) == B.OK and n.value >= 257 * 16 + 1000
+    assert L.chm_embedding_gradient_scratch(512, 1000, 64, n) == B.OK and n.value == 0
+    assert L.chm_embedding_gradient_scratch(513, 1000, 64, n) == B.OK and n.value >= 513 * 16 + 1000
     for args in ((-1, 10, 8), (5, -1, 8), (5, 10, 0), (1 << 31, 10, 8), (5, 1 << 31, 8)):
         assert L.chm_embedding_gradient_scratch(*args, n) == B.ERR_ARG
     assert L.chm_embedding_gradient_scratch(5, 5, 5, None) == B.ERR_ARG

@@ -129,21 +129,28 @@ struct Feed {
     return (idx % CHUNKS) ^ swz_rows(idx / CHUNKS);
   }
   // the second run of k begins
-  __device__ __forceinline__ void turn(const GemmOperand &o, bool now) {
-    base = now ? base2 : base;
-    k_left = now ? (int32_t)o.k : k_left;
+  __device__ __forceinline__ void turn(const GemmOperand &o) {
+    base = base2;
+    k_left = (int32_t)o.k;
   }
   // a step's loads, one by one
-  i4 rsrc;                 // buffer descriptor: base, bytes, raw 32-bit words
+  i4 rsrc;                 // buffer descriptor: base, bytes from there to the end of the last element that is there, raw 32-bit words
   uint32_t offset[NI];
   __device__ __forceinline__ void begin(int tid) {
-    const int32_t left = __builtin_amdgcn_readfirstlane(k_left < 0 ? 0 : k_left < BK ? k_left : BK);
-    // from base to the end of the last element that is there
-    const uint32_t bytes = KIND == ROWS ? rows * ld_bytes + left * 2 : (left - 1) * ld_bytes + rows;
     const uint64_t at = (uint64_t)base;
-    rsrc = i4{(int)(uint32_t)at, (int)(uint32_t)(at >> 32) & 0xffff, left > 0 ? (int)bytes : 0, 0x00027000};
+    rsrc[0] = (int)(uint32_t)at;
+    rsrc[1] = (int)(uint32_t)(at >> 32) & 0xffff;
+    rsrc[3] = 0x00027000;
+    if (k_left >= BK) {
+      rsrc[2] = (int)(KIND == ROWS ? rows * ld_bytes + BK * 2 : (BK - 1) * ld_bytes + rows);
 #pragma unroll
-    for (int i = 0; i < NI; ++i) offset[i] = KIND == ROWS && (int32_t)chunk_of(i, tid) * 8 >= left ? (uint32_t)OUT : off[i];
+      for (int i = 0; i < NI; ++i) offset[i] = off[i];
+    } else {
+      const int32_t left = __builtin_amdgcn_readfirstlane(k_left < 0 ? 0 : k_left);
+      rsrc[2] = left > 0 ? (int)(KIND == ROWS ? rows * ld_bytes + left * 2 : (left - 1) * ld_bytes + rows) : 0;
+#pragma unroll
+      for (int i = 0; i < NI; ++i) offset[i] = KIND == ROWS && (int32_t)chunk_of(i, tid) * 8 >= left ? (uint32_t)OUT : off[i];
+    }
     base += step_bytes;
     k_left -= BK;
   }
@@ -409,8 +416,10 @@ struct Fetch {
   uint32_t lds;
   enum { LOADS = FeedA::NI + FeedB::NI, A_BYTES = FeedA::BYTES, STAGE = FeedA::BYTES + FeedB::BYTES };
   __device__ __forceinline__ void begin(int step) {
-    a.turn(c.a, step == turn_at);
-    b.turn(c.b, step == turn_at);
+    if (step == turn_at) {
+      a.turn(c.a);
+      b.turn(c.b);
+    }
     a.begin(tid);
     b.begin(tid);
   }
@@ -436,8 +445,7 @@ __device__ __forceinline__ void multiply(const F &now, F &next, f4 (&acc)[4][MT]
 #pragma unroll
   for (int i = 0; i < M; ++i) {
     if ((i + 1) * LOADS / M > i * LOADS / M) fetch.one(i * LOADS / M, slot);
-    const int r0 = i * READS / M, r1 = (i + 1) * READS / M;
-    if (r1 > r0) next.read(r0, from, from + G::A_BYTES, wm, wn, ks, lane);
+    if ((i + 1) * READS / M > i * READS / M) next.read(i * READS / M, from, from + G::A_BYTES, wm, wn, ks, lane);
     acc[i & 3][i >> 2] = T::mfma(now.b[i & 3], now.a[i >> 2], acc[i & 3][i >> 2]);
     __builtin_amdgcn_sched_barrier(0);
   }

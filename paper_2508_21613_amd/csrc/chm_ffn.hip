@@ -316,50 +316,58 @@ struct Pass {
     b = packed(b, must);
   }
 
-  // A launch's products on the kind of tile that takes the least time.  A step over one tile a compute unit takes 1.3 us with tiles of 256 x 256
-  // and 0.58 us with 128 x 128, 1.03 us for two of those at once (measured over 64 steps: 2,048 x 4,096 83 and 66 us, 1,024 x 4,096 79 and 37,
-  // 512 x 22,016 83 and 132, 4,096 x 11,008 240 and 400); no launch takes less than its longest tile.  Where small tiles are too few for the
-  // compute units, the sums of a first product with a plain 16-bit output are split as well, 512 of them a part at least.
+  // How a launch's products are laid out: kind of tile, parts of the first one's sums, and the time that takes.
+  struct Layout { int tile = TILE_256, splits = 1; double us = 1e30; };
+
+  // A tile takes a time for every step of 64 sums and one for its start and end, and 256 of them are worked on at a time, or 512 (two a compute
+  // unit): 256 x 256 1.3 us a step and 10, 128 x 128 1.03 and 4.6, or alone on its compute unit, with more steps under way, 0.58 and 4.
+  // Measured against that (us): 1,024 x 22,016 x 4,096 186 and 211 expected, 176 and 197 taken; 512 x 22,016 93 and 113, 86 and 99; 256 x
+  // 22,016 93 and 71, 81 and 61; 1,024 x 4,096 x 4,096 93, 42 and 41 (alone), 76, 44 and 40; 4,096 x 11,008 x 512 61 and 72, 67 and 72.
+  // Sums are split (a first product with a plain 16-bit output only) 512 a part at least; the parts are written and read once more.
+  // Whole steps against every choice of tile and split for dx and the weight gradients, with dx in a launch of its own and without: at 256 to
+  // 2,048 tokens and widths of 1,000 to 4,096 this one is within 2% of the best (8% at 256 x 4,096 x 11,008), which is never the one apart.
+  Layout layout(int products, const GemmCall *call, int count, bool may_split) const {
+    static const double STEP[3] = {1.3, 1.03, 0.58}, ENDS[3] = {10, 4.6, 4};
+    Layout best;
+    for (int tile = TILE_256; tile <= TILE_128_DEEP; ++tile) {
+      const int bits = tile == TILE_256 ? 8 : 7, at_once = tile == TILE_128 ? 512 : 256;
+      const int64_t most = (1 << bits) - 1;
+      for (int s = 1; s <= 8; ++s) {
+        if (s > 1 && (!may_split || sums(call[0]) < 512 * (int64_t)s)) break;
+        double work = 0, longest = 0, us;
+        int64_t tiles = 0;
+        for (int i = 0; i < count; ++i) {
+          const int parts = i == 0 ? s : 1;
+          const int64_t n = products == GEMM_GATE_UP ? 2 * call[i].n : call[i].n;
+          const int64_t t = ((call[i].m + most) >> bits) * ((n + most) >> bits) * parts;
+          const double unit = (double)((sums(call[i]) + 63) / 64 + parts - 1) / parts * STEP[tile] + ENDS[tile];
+          work += t * unit;
+          tiles += t;
+          if (t && unit > longest) longest = unit;
+        }
+        if (count == 1) {                  // equal tiles: whole rounds, one of single tiles where two fit goes faster
+          const int64_t rest = tiles % at_once;
+          us = tiles / at_once * longest + (rest == 0 ? 0 : tile == TILE_128 && rest <= 256 ? 0.7 * longest : longest);
+        } else {
+          us = work / at_once > longest ? work / at_once : longest;
+        }
+        if (s > 1) us += 3 + (double)s * call[0].m * up8(call[0].n) * 8 / 4.5e6;
+        if (us < best.us) best = Layout{tile, s, us};
+      }
+    }
+    return best;
+  }
+
   void launch(int products, GemmGroup &g) {
-    double work_big = 0, work_small = 0, longest = 0;
-    int64_t small = 0;
-    for (int i = 0; i < g.count; ++i) {
-      const GemmCall &c = g.call[i];
-      const int64_t n = products == GEMM_GATE_UP ? 2 * c.n : c.n, k = sums(c), t = ((c.m + 127) / 128) * ((n + 127) / 128);
-      work_big += (double)(((c.m + 255) / 256) * ((n + 255) / 256)) * k;
-      work_small += (double)t * k;
-      small += t;
-      if (k > longest) longest = (double)k;
-    }
-    // the first product's sums may be split: as far as that gives every compute unit a tile
-    const bool may_split = products == GEMM_OUT || products == GEMM_BACK;
-    int64_t splits = 1;
-    double longest_small = longest;
-    if (may_split) {
-      GemmCall &c = g.call[0];
-      const int64_t k = sums(c), t = ((c.m + 127) / 128) * ((c.n + 127) / 128);
-      splits = (256 - (small - t < 0 ? 0 : small - t)) / (t > 0 ? t : 1);
-      // and so that no part is much longer than the launch's other tiles, taken together, keep the compute units busy
-      const int64_t even = (int64_t)((double)k * 512 / (work_small > 1 ? work_small : 1));
-      if (splits < even) splits = even;
-      if (splits > k / 512) splits = k / 512;
-      if (splits > 8) splits = 8;
-      if (splits < 1) splits = 1;
-      longest_small = (double)k / splits;
-      for (int i = 1; i < g.count; ++i) longest_small = sums(g.call[i]) > longest_small ? (double)sums(g.call[i]) : longest_small;
-      small += t * (splits - 1);
-    }
-    const auto most = [](double a, double b) { return a > b ? a : b; };
-    const double time_big = most(work_big / 256, longest) * 1.3;
-    const double time_small = small <= 256 ? longest_small * 0.58 : most(work_small / 512, longest_small) * 1.03;
-    const int tile = time_big < time_small ? TILE_256 : small <= 256 ? TILE_128_DEEP : TILE_128, side = tile == TILE_256 ? 256 : 128;
+    const Layout l = layout(products, g.call, g.count, products == GEMM_OUT || products == GEMM_BACK);
+    const int side = l.tile == TILE_256 ? 256 : 128;
     g.first[0] = 0;
     for (int i = 0; i < g.count; ++i) {
       GemmCall &c = g.call[i];
       const int64_t n = products == GEMM_GATE_UP ? 2 * c.n : c.n;
       c.tiles_m = (int32_t)((c.m + side - 1) / side);
       c.tiles_n = (int32_t)((n + side - 1) / side);
-      c.splits = i == 0 && tile != TILE_256 ? (int32_t)splits : 1;
+      c.splits = i == 0 ? l.splits : 1;
       c.act = f->activation;
       if (c.splits > 1) {
         c.ld_part = up8(c.n);
@@ -368,7 +376,7 @@ struct Pass {
       g.first[i + 1] = g.first[i] + ((c.tiles_m * c.tiles_n + 7) & ~7) * c.splits;
     }
     if (!run || g.first[g.count] == 0) return;
-    ok = ok && (f->dtype == CHM_BF16 ? gemm_launch_bf16 : gemm_launch_f16)(products, tile, g, st);
+    ok = ok && (f->dtype == CHM_BF16 ? gemm_launch_bf16 : gemm_launch_f16)(products, l.tile, g, st);
     const GemmCall &c = g.call[0];
     if (c.splits > 1) {
       const dim3 grid(copy_groups(c.m * (c.ld_part / 8)));

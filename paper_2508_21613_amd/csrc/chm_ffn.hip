@@ -20,7 +20,7 @@ using chm_gemm::f4;
 using chm_gemm::s8;
 
 // ---------------------------------------------------------------------------------------------- few tokens
-// A wavefront takes 16 features (rows of a weight) and a share of the sums, and reads its part of the weight straight into
+// A wavefront takes 16 features (rows of a weight; fewer with few tokens) and a share of the sums, and reads its part of the weight straight into
 // the first operand of the matrix instructions: every byte of a weight is read once, by one wavefront, 64 contiguous bytes a
 // lane quad and step.  The tokens (16 for each instruction, absent ones are zero and not loaded) come from the cache.  The
 // wavefronts of a workgroup share the sums and add them up through shared memory, in order.  Weights may start anywhere.
@@ -31,6 +31,8 @@ using chm_gemm::s8;
 bool few_tokens(int64_t tokens, int64_t width, int64_t features) {
   return tokens <= 16 || (tokens <= 32 && width * features <= 1 << 22) || (tokens <= 64 && width * features <= 1 << 20);
 }
+
+int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
 
 struct FewCall {
   const uint16_t *x, *w0, *w1;
@@ -69,26 +71,26 @@ __device__ __forceinline__ void keep_pair(const FewCall &c, int64_t m, int64_t f
 // wavefronts of a workgroup at most: two steps and more of several tiles take more registers than 16 of them leave
 constexpr int few_waves_most(int tiles) { return tiles == 1 ? 16 : 8; }
 
-// 64 sums: 16 of every lane's feature and of its token of each tile
-template <int TWO, int TILES>
+// 64 sums of each slice: 16 of every lane's feature and of its token of each tile.  Eight that would end behind the row are its last eight
+// instead; what of these belongs to an earlier lane or step is set to zero before the product, which heeds no order of the sums.
+template <int TWO, int TILES, int SLICES, int ENDS>
 struct FewStep {
   s8 a[TWO + 1][2], b[TILES][2];
-  __device__ __forceinline__ void load(const FewCall &c, const uint16_t *w0, const uint16_t *w1, int k, bool whole, int q, int r) {
+  template <bool SHORT> __device__ __forceinline__ void load(const FewCall &c, const uint16_t *w0, const uint16_t *w1, int k, int q, int r) {
+    int at[2];
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
-      const int at = k + h * 32 + q * 8;
-      a[0][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(w0 + at))) : take8(w0, at, c.k);
-      if (TWO) a[TWO][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(w1 + at))) : take8(w1, at, c.k);
+      at[h] = first(k, h, q, r);
+      if (ENDS && !SHORT) at[h] = at[h] < c.k - 8 ? at[h] : c.k - 8;
+      a[0][h] = take<SHORT>(w0, at[h], c.k);
+      if (TWO) a[TWO][h] = take<SHORT>(w1, at[h], c.k);
     }
 #pragma unroll
     for (int t = 0; t < TILES; ++t) {
-      const int token = t * 16 + r < c.tokens ? t * 16 + r : c.tokens - 1;        // an absent one: the last again, its sums are dropped
-      const uint16_t *x = c.x + token * c.ldx;
+      const int token = t * 16 + r % (16 / SLICES), there = token < c.tokens ? token : c.tokens - 1;     // an absent one: the last again, its sums are dropped
+      const uint16_t *x = c.x + there * c.ldx;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        const int at = k + h * 32 + q * 8;
-        b[t][h] = whole ? __builtin_bit_cast(s8, load16((const char *)(x + at))) : take8(x, at, c.k);
-      }
+      for (int h = 0; h < 2; ++h) b[t][h] = take<SHORT>(x, at[h], c.k);
     }
   }
   template <class T> __device__ __forceinline__ void multiply(f4 (&acc)[2][TILES]) const {
@@ -99,49 +101,75 @@ struct FewStep {
 #pragma unroll
         for (int w = 0; w <= TWO; ++w) acc[w][t] = T::mfma(a[w][h], b[t][h], acc[w][t]);
   }
+  // the step that starts at sum k
+  template <class T> __device__ __forceinline__ void multiply(f4 (&acc)[2][TILES], const FewCall &c, int k, int q, int r) {
+    if (ENDS && k + 64 * SLICES > c.k) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const int drop = first(k, h, q, r) - (c.k - 8);
+        uint4 keep;
+        keep.x = (drop > 0 ? 0 : 0xffffu) | (drop > 1 ? 0 : 0xffff0000u);
+        keep.y = (drop > 2 ? 0 : 0xffffu) | (drop > 3 ? 0 : 0xffff0000u);
+        keep.z = (drop > 4 ? 0 : 0xffffu) | (drop > 5 ? 0 : 0xffff0000u);
+        keep.w = (drop > 6 ? 0 : 0xffffu) | (drop > 7 ? 0 : 0xffff0000u);
+        const s8 mask = __builtin_bit_cast(s8, keep);
+#pragma unroll
+        for (int w = 0; w <= TWO; ++w) a[w][h] &= mask;
+#pragma unroll
+        for (int t = 0; t < TILES; ++t) b[t][h] &= mask;
+      }
+    }
+    multiply<T>(acc);
+  }
+  static __device__ __forceinline__ int first(int k, int h, int q, int r) { return k + r / (16 / SLICES) * 64 + h * 32 + q * 8; }
+  template <bool SHORT> static __device__ __forceinline__ s8 take(const uint16_t *row, int at, int n) {
+    return SHORT ? take8(row, at, n) : __builtin_bit_cast(s8, load16((const char *)(row + at)));
+  }
 };
 
-template <class T, int TWO, int TILES>
+template <class T, int TWO, int TILES, int SLICES, int ENDS>
 __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCall c) {
   extern __shared__ float part[];             // [wavefronts][TWO + 1][TILES][64][4]
   // uniform: a matrix instruction does not heed which lanes are switched off
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = blockDim.x >> 6;
   const int q = lane >> 4, r = lane & 15;
-  const int f0 = blockIdx.x * 16, f = f0 + r < c.rows ? f0 + r : c.rows - 1;
+  constexpr int EACH = 16 / SLICES;           // features, and tokens of a tile
+  const int f0 = blockIdx.x * EACH, f = f0 + r % EACH < c.rows ? f0 + r % EACH : c.rows - 1;
   const uint16_t *w0 = c.w0 + f * c.ld0, *w1 = TWO ? c.w1 + f * c.ld1 : nullptr;
   f4 acc[2][TILES];
 #pragma unroll
   for (int t = 0; t < TILES; ++t) acc[0][t] = acc[1][t] = f4{0.f, 0.f, 0.f, 0.f};
 
-  // DEPTH steps of 64 sums are under way.  All loads are issued whatever the number of steps (a step too many reads the last one
+  // DEPTH steps of 64 sums a slice are under way.  All loads are issued whatever the number of steps (a step too many reads the last one
   // again), and none depends on a branch: else the waits in front of the matrix instructions would be for all of them.  Workgroups
   // begin at different sums, so that they do not all ask the same channels of the cache for the tokens.
   constexpr int DEPTH = TWO && TILES > 2 ? 3 : 4;
-  const int whole = c.k / 64, last = whole - 1;
-  if (wave < whole) {
-    const int turn = (int)((blockIdx.x >> 3) % (uint32_t)whole);
+  const int steps = (c.k + 64 * SLICES - 1) / (64 * SLICES);
+  if (ENDS && c.k < 8) {
+    if (wave == 0) {
+      FewStep<TWO, TILES, SLICES, ENDS> only;
+      only.template load<true>(c, w0, w1, 0, q, r);
+      only.template multiply<T>(acc);
+    }
+  } else if (wave < steps) {
+    const int turn = (int)((blockIdx.x >> 3) % (uint32_t)steps);
     const auto at = [&](int i) {
-      i = (i < last ? i : last) + turn;
-      return (i < whole ? i : i - whole) * 64;
+      i = (i < steps ? i : steps - 1) + turn;
+      return (i < steps ? i : i - steps) * 64 * SLICES;
     };
-    FewStep<TWO, TILES> set[DEPTH];
+    FewStep<TWO, TILES, SLICES, ENDS> set[DEPTH];
 #pragma unroll
-    for (int d = 0; d < DEPTH; ++d) set[d].load(c, w0, w1, at(wave + d * waves), true, q, r);
+    for (int d = 0; d < DEPTH; ++d) set[d].template load<false>(c, w0, w1, at(wave + d * waves), q, r);
     int i = wave;
-    for (; i + DEPTH * waves < whole; i += DEPTH * waves)
+    for (; i + DEPTH * waves < steps; i += DEPTH * waves)
 #pragma unroll
       for (int d = 0; d < DEPTH; ++d) {
-        set[d].template multiply<T>(acc);
-        set[d].load(c, w0, w1, at(i + (d + DEPTH) * waves), true, q, r);
+        set[d].template multiply<T>(acc, c, at(i + d * waves), q, r);
+        set[d].template load<false>(c, w0, w1, at(i + (d + DEPTH) * waves), q, r);
       }
 #pragma unroll
     for (int d = 0; d < DEPTH; ++d)
-      if (i + d * waves < whole) set[d].template multiply<T>(acc);
-  }
-  if (c.k % 64 && wave == whole % waves) {
-    FewStep<TWO, TILES> rest;
-    rest.load(c, w0, w1, whole * 64, false, q, r);
-    rest.template multiply<T>(acc);
+      if (i + d * waves < steps) set[d].template multiply<T>(acc, c, at(i + d * waves), q, r);
   }
 
 #pragma unroll
@@ -149,9 +177,9 @@ __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCa
 #pragma unroll
     for (int w = 0; w <= TWO; ++w) *(f4 *)(part + ((((wave * (TWO + 1) + w) * TILES) + t) * 64 + lane) * 4) = acc[w][t];
   __syncthreads();
-  // one value (pair) a thread: feature i % 16, token i / 16
-  for (int o = threadIdx.x; o < 256 * TILES; o += blockDim.x) {
-    const int feature = o & 15, token = o >> 4;
+  // one value (pair) a thread: feature o % EACH, token o / EACH
+  for (int o = threadIdx.x; o < EACH * EACH * TILES; o += blockDim.x) {
+    const int feature = o % EACH, token = o / EACH;
     if (token >= c.tokens) continue;
     if (f0 + feature >= c.rows) {             // kept projections have rows of whole words of 8, zeros behind
       if (TWO && c.kept.p && f0 + feature < ((c.rows + 7) & ~7)) keep_pair(c, token, f0 + feature, 0.f, 0.f);
@@ -159,10 +187,13 @@ __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCa
     }
     const int at = ((token >> 4) * 64 + (feature >> 2) * 16 + (token & 15)) * 4 + (feature & 3);
     float s0 = 0.f, s1 = 0.f;
-    for (int w = 0; w < waves; ++w) {
-      s0 += part[w * (TWO + 1) * TILES * 256 + at];
-      if (TWO) s1 += part[(w * (TWO + 1) + 1) * TILES * 256 + at];
-    }
+    for (int w = 0; w < waves; ++w)
+#pragma unroll
+      for (int s = 0; s < SLICES; ++s) {      // EACH features and tokens on: EACH lanes for the tokens, EACH / 4 times 16 for the features
+        const float *p = part + w * (TWO + 1) * TILES * 256 + at + s * (EACH + EACH / 4 * 16) * 4;
+        s0 += p[0];
+        if (TWO) s1 += p[TILES * 256];
+      }
     const int64_t col = f0 + feature;
     if (TWO) {
       c.out[token * c.ldo + col] = T::down(act(c.act, s0) * s1);
@@ -174,22 +205,48 @@ __global__ void __launch_bounds__(64 * few_waves_most(TILES)) k_few_tokens(FewCa
 }
 
 // wavefronts of a workgroup: some 16 a compute unit over all, with four steps of 64 sums each at least
-int few_waves(int64_t rows, int64_t k, int tiles) {
-  const int64_t groups = (rows + 15) / 16, steps = (k + 63) / 64;
+int few_waves(int64_t groups, int64_t steps, int tiles) {
   int w = 1;
   while (w < few_waves_most(tiles) && groups * w < 4096 && steps >= w * 8) w <<= 1;
   return w;
 }
 
+// Up to 8 tokens the 16 rows of the operands may be 8 or 4 features (and as many tokens) of 2 or 4 slices of the sums; of the products of all
+// pairs of slices, those of a slice with itself are added up.  That gives 2 or 4 times the workgroups and longer runs of a weight's row, but each
+// of them loads 2 or 4 times as many tokens.  The least of: how unevenly the workgroups fall on 256 compute units, times what short runs
+// cost (more where rows do not start on whole lines of 128 bytes), times what the tokens cost.
+// Measured (us; one slice, two, four in both launches): 1 token, 2,048 x 5,504 24.3, 19.0, 19.4; 1,024 x 2,752 12.4, 10.4, 9.6; 1,000 x 2,731
+// 18.8, 13.4, 10.3; 3,000 x 8,000 38.8, 33.6, 32.2; 4,096 x 11,008 55.8, 55.5, 54.4; 8,192 x 22,016 212, 202, 189.  4 tokens, the same widths:
+// 25.7, 19.4, 21.8; 13.4, 11.3, 10.5; 19.5, 14.2, 10.8; 41.5, 37.8, 40.3; 57.0, 59.8, 65.7; 217, 217, 233.  8 tokens, two last widths: 60.5, 67.8; 227, 248.
+int few_slices(int two, const FewCall &c) {
+  const bool lines = (c.ld0 % 64 == 0) && (c.ld1 % 64 == 0);
+  int best = 1;
+  double least = 1e30;
+  for (int s = 1; s <= 4 && s * c.tokens <= 16; s <<= 1) {
+    const double groups = (double)((c.rows * (int64_t)s + 15) / 16), loaded = c.tokens * s;
+    const double cost = ceil(groups / 256) / groups * (1 + (lines ? 0.1 : 0.5) / s) * (1 + (two ? 0.001 : 0.002) * loaded * loaded);
+    if (cost < least) least = cost, best = s;
+  }
+  return best;
+}
+
+template <class T, int TWO, int TILES, int SLICES>
+void launch_few(const FewCall &c, hipStream_t st) {
+  const int64_t each = 16 / SLICES, groups = (up8(c.rows) + each - 1) / each;          // kept projections have zeros up to a whole word
+  const int w = few_waves(groups, (c.k + 64 * SLICES - 1) / (64 * SLICES), TILES);
+  const size_t bytes = (size_t)w * (TWO + 1) * TILES * 1024;
+  if (c.k % (64 * SLICES)) hipLaunchKernelGGL((k_few_tokens<T, TWO, TILES, SLICES, 1>), dim3((uint32_t)groups), dim3(w * 64), bytes, st, c);
+  else hipLaunchKernelGGL((k_few_tokens<T, TWO, TILES, SLICES, 0>), dim3((uint32_t)groups), dim3(w * 64), bytes, st, c);
+}
 template <class T, int TWO>
 bool launch_few(const FewCall &c, hipStream_t st) {
-  const dim3 grid((c.rows + 15) / 16);
-  const int tiles = (c.tokens + 15) / 16, w = few_waves(c.rows, c.k, tiles);
-  const size_t bytes = (size_t)w * (TWO + 1) * tiles * 1024;
-  if (tiles == 1) hipLaunchKernelGGL((k_few_tokens<T, TWO, 1>), grid, dim3(w * 64), bytes, st, c);
-  else if (tiles == 2) hipLaunchKernelGGL((k_few_tokens<T, TWO, 2>), grid, dim3(w * 64), bytes, st, c);
-  else if (tiles == 3) hipLaunchKernelGGL((k_few_tokens<T, TWO, 3>), grid, dim3(w * 64), bytes, st, c);
-  else hipLaunchKernelGGL((k_few_tokens<T, TWO, 4>), grid, dim3(w * 64), bytes, st, c);
+  const int tiles = (c.tokens + 15) / 16, slices = few_slices(TWO, c);
+  if (slices == 4) launch_few<T, TWO, 1, 4>(c, st);
+  else if (slices == 2) launch_few<T, TWO, 1, 2>(c, st);
+  else if (tiles == 1) launch_few<T, TWO, 1, 1>(c, st);
+  else if (tiles == 2) launch_few<T, TWO, 2, 1>(c, st);
+  else if (tiles == 3) launch_few<T, TWO, 3, 1>(c, st);
+  else launch_few<T, TWO, 4, 1>(c, st);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -254,7 +311,6 @@ uint32_t copy_groups(int64_t words) {
 }
 
 // ---------------------------------------------------------------------------------------------- passes
-int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
 
 struct Matrix { const void *p; int64_t ld, rows, cols; };
 

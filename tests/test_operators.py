@@ -141,6 +141,27 @@ def test_ffn_forward_and_backward(ops, shape, dtype):
     assert torch.equal(alone, got["y"])
 
 
+# up to 8 tokens the sums go in 1, 2 or 4 slices: ends of rows inside each, several steps a wavefront, fewer sums than one load takes
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", [(1, 8, 8), (1, 7, 9), (1, 1000, 2731), (2, 3001, 800), (3, 8200, 40), (4, 515, 4099), (4, 4096, 72), (5, 1027, 515), (6, 40, 8200),
+                                   (7, 2051, 260), (8, 256, 128), (8, 1100, 2049), (9, 515, 1027)])
+def test_ffn_slices_of_the_sums(ops, shape, dtype):
+    inputs = ffn_inputs(sum(shape), *shape, dtype)
+    want = formula(*inputs[:4], "silu", inputs[4])
+    got = ffn_both(ops, inputs, "silu")
+    for k, v in want.items():
+        check(k, got[k], v)
+    assert torch.equal(ops.ffn_forward(*inputs[:4]), got["y"])
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+def test_ffn_split_sums_on_large_tiles(ops, dtype):
+    inputs = ffn_inputs(7, 520, 2051, 5500, dtype)
+    want = formula(*inputs[:4], "gelu", inputs[4])
+    for k, v in ffn_both(ops, inputs, "gelu").items():
+        check(k, v, want[k])
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("T", [5, 90])
 def test_ffn_activations(ops, act, T):

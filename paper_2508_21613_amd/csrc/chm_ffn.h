@@ -45,8 +45,9 @@ struct GemmGroup {
 
 // Tiles of 256 x 256, two steps in shared memory; of 128 x 128, two steps (two workgroups a compute unit) or four (one: a step's loads
 // have three steps' time to arrive).  All of 8 wavefronts: with 4 the 128 x 128 ones take 1.1 to 1.4 times as long, since nothing
-// runs while a wavefront issues loads.
-enum { TILE_256 = 0, TILE_128 = 1, TILE_128_DEEP = 2 };
+// runs while a wavefront issues loads.  And of 64 x 64 by 4 wavefronts, four steps, two workgroups a compute unit, where the others are too few:
+// 37 tokens, 2,048 x 5,504, forward 27 us (128 x 128: 34), 64 tokens of a whole step at 512 x 1,376 38 us (42).
+enum { TILE_256 = 0, TILE_128 = 1, TILE_128_DEEP = 2, TILE_64 = 3 };
 // Largest row of memory (elements) that the tile kernels take: 256 rows lie within 2^31 bytes.  Longer ones are packed.
 constexpr int64_t GEMM_LD_MAX = 1 << 21;
 // Launches them; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.

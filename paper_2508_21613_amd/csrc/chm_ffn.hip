@@ -24,12 +24,14 @@ using chm_gemm::s8;
 // the first operand of the matrix instructions: every byte of a weight is read once, by one wavefront, 64 contiguous bytes a
 // lane quad and step.  The tokens (16 for each instruction, absent ones are zero and not loaded) come from the cache.  The
 // wavefronts of a workgroup share the sums and add them up through shared memory, in order.  Weights may start anywhere.
-// Tokens up to which these kernels run rather than the tiles: 16, 32 with small weights, 64 with smaller ones.  From there on the
-// tokens' fragments, which every wavefront reads for itself, cost more than the tiles' fixed time (us, these kernels and tiles: width 4,096,
-// 11,008 features, 16 tokens 70 and 70, 32 tokens 93 and 70; 2,048 x 5,504: 16 tokens 32 and 33, 32 tokens 39 and 34; 1,024 x 2,752: 32 tokens
-// 21 and 24, 48 tokens 27 and 24; 512 x 1,376: 64 tokens 21 and 22).
-bool few_tokens(int64_t tokens, int64_t width, int64_t features) {
-  return tokens <= 16 || (tokens <= 32 && width * features <= 1 << 22) || (tokens <= 64 && width * features <= 1 << 20);
+// Tokens up to which these kernels run rather than the tiles: 8, 24 with small weights, 48 with smaller ones.  From there on the tokens'
+// fragments, which every wavefront reads for itself, cost more than the tiles' fixed time (us, these kernels and tiles: 512 x 1,376, 48 tokens
+// 15 and 15, 64 tokens 18 and 15; 1,024 x 2,752, 24 tokens 19 and 19, 32 tokens 21 and 19; 2,048 x 5,504, 8 tokens 23 and 28, 10 tokens 28 and
+// 28, 16 tokens 31 and 26; 4,096 x 11,008, 8 tokens 62 and 67, 16 tokens 66 and 66, 20 tokens 79 and 68; 8,192 x 22,016, 5 tokens 213 and 224, 8 tokens
+// 233 and 224).  32 with large weights that the tiles would have to pack first (4,001 x 11,001, 32 tokens 168 and 184, 40 tokens 212 and 186).
+bool few_tokens(int64_t tokens, int64_t width, int64_t features, bool packs) {
+  const int64_t weight = width * features;
+  return tokens <= (weight <= 1 << 20 ? 48 : weight <= 1 << 23 ? 24 : packs && weight > 1 << 25 ? 32 : 8);
 }
 
 int64_t up8(int64_t n) { return (n + 7) & ~7ll; }
@@ -245,8 +247,7 @@ bool launch_few(const FewCall &c, hipStream_t st) {
   else if (slices == 2) launch_few<T, TWO, 1, 2>(c, st);
   else if (tiles == 1) launch_few<T, TWO, 1, 1>(c, st);
   else if (tiles == 2) launch_few<T, TWO, 2, 1>(c, st);
-  else if (tiles == 3) launch_few<T, TWO, 3, 1>(c, st);
-  else launch_few<T, TWO, 4, 1>(c, st);
+  else launch_few<T, TWO, 3, 1>(c, st);
   return hipGetLastError() == hipSuccess;
 }
 
@@ -376,17 +377,20 @@ struct Pass {
   struct Layout { int tile = TILE_256, splits = 1; double us = 1e30; };
 
   // A tile takes a time for every step of 64 sums and one for its start and end, and 256 of them are worked on at a time, or 512 (two a compute
-  // unit): 256 x 256 1.3 us a step and 10, 128 x 128 1.03 and 4.6, or alone on its compute unit, with more steps under way, 0.58 and 4.
+  // unit): 256 x 256 1.3 us a step and 10, 128 x 128 1.03 and 4.6, or alone on its compute unit, with more steps under way, 0.58 and 4,
+  // 64 x 64 0.6 and 4 (4 and 1 more for dh, whose tiles read and write most at their end).
   // Measured against that (us): 1,024 x 22,016 x 4,096 186 and 211 expected, 176 and 197 taken; 512 x 22,016 93 and 113, 86 and 99; 256 x
   // 22,016 93 and 71, 81 and 61; 1,024 x 4,096 x 4,096 93, 42 and 41 (alone), 76, 44 and 40; 4,096 x 11,008 x 512 61 and 72, 67 and 72.
   // Sums are split (a first product with a plain 16-bit output only) 512 a part at least; the parts are written and read once more.
   // Whole steps against every choice of tile and split for dx and the weight gradients, with dx in a launch of its own and without: at 256 to
   // 2,048 tokens and widths of 1,000 to 4,096 this one is within 2% of the best (8% at 256 x 4,096 x 11,008), which is never the one apart.
   Layout layout(int products, const GemmCall *call, int count, bool may_split) const {
-    static const double STEP[3] = {1.3, 1.03, 0.58}, ENDS[3] = {10, 4.6, 4};
+    static const double STEP[4] = {1.3, 1.03, 0.58, 0.6}, ENDS[4] = {10, 4.6, 4, 4};
     Layout best;
-    for (int tile = TILE_256; tile <= TILE_128_DEEP; ++tile) {
-      const int bits = tile == TILE_256 ? 8 : 7, at_once = tile == TILE_128 ? 512 : 256;
+    for (int tile = TILE_256; tile <= TILE_64; ++tile) {
+      if (tile == TILE_64 && products == GEMM_BACK) break;
+      const int bits = side_bits(tile), at_once = tile == TILE_128 || tile == TILE_64 ? 512 : 256;
+      const double ends = ENDS[tile] + (products != GEMM_DH || tile == TILE_256 ? 0 : tile == TILE_64 ? 1 : 4);
       const int64_t most = (1 << bits) - 1;
       for (int s = 1; s <= 8; ++s) {
         if (s > 1 && (!may_split || sums(call[0]) < 512 * (int64_t)s)) break;
@@ -396,12 +400,14 @@ struct Pass {
           const int parts = i == 0 ? s : 1;
           const int64_t n = products == GEMM_GATE_UP ? 2 * call[i].n : call[i].n;
           const int64_t t = ((call[i].m + most) >> bits) * ((n + most) >> bits) * parts;
-          const double unit = (double)((sums(call[i]) + 63) / 64 + parts - 1) / parts * STEP[tile] + ENDS[tile];
+          const double unit = (double)((sums(call[i]) + 63) / 64 + parts - 1) / parts * STEP[tile] + ends;
           work += t * unit;
           tiles += t;
           if (t && unit > longest) longest = unit;
         }
-        if (count == 1) {                  // equal tiles: whole rounds, one of single tiles where two fit goes faster
+        if (tile == TILE_64) {             // the third of a compute unit begins where the first ends
+          us = tiles <= 256 ? 0.8 * longest : tiles <= 512 ? longest : tiles * longest / 512;
+        } else if (count == 1) {           // equal tiles: whole rounds, one of single tiles where two fit goes faster
           const int64_t rest = tiles % at_once;
           us = tiles / at_once * longest + (rest == 0 ? 0 : tile == TILE_128 && rest <= 256 ? 0.7 * longest : longest);
         } else {
@@ -414,9 +420,11 @@ struct Pass {
     return best;
   }
 
+  static int side_bits(int tile) { return tile == TILE_256 ? 8 : tile == TILE_64 ? 6 : 7; }
+
   void launch(int products, GemmGroup &g) {
     const Layout l = layout(products, g.call, g.count, products == GEMM_OUT || products == GEMM_BACK);
-    const int side = l.tile == TILE_256 ? 256 : 128;
+    const int side = 1 << side_bits(l.tile);
     g.first[0] = 0;
     for (int i = 0; i < g.count; ++i) {
       GemmCall &c = g.call[i];
@@ -449,7 +457,8 @@ struct Pass {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
     const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
-    if (few_tokens(T, D, F)) {
+    const bool packs = needs_pack({f->w_gate, f->ld_gate, F, D}) || needs_pack({f->w_up, f->ld_up, F, D}) || needs_pack({f->w_down, f->ld_down, D, F});
+    if (few_tokens(T, D, F, packs)) {
       if (!run || T == 0) return;
       FewCall c{};
       c.tokens = (int32_t)T;

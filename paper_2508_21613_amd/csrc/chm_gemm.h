@@ -80,7 +80,10 @@ enum { BK = 64 };                                  // sums of a step
 enum { TURN_ROW = 272 };                           // bytes of 64 float32 and a gap that spreads the rows over the banks
 
 __device__ __forceinline__ uint32_t swz_rows(uint32_t row) { return row & 7u; }
-__device__ __forceinline__ uint32_t swz_cols(uint32_t k) { return ((k & 3u) << 1) | (((k >> 3) & 1u) << 3); }
+// W: the indices of a row; rows of 64 take half the banks, two of them all
+template <int W> __device__ __forceinline__ uint32_t swz_cols(uint32_t k) {
+  return W == 64 ? (k & 2u) | (((k >> 3) & 1u) << 2) : ((k & 3u) << 1) | (((k >> 3) & 1u) << 3);
+}
 
 // One operand's way from memory to shared memory: W of its indices x BK sums a step, by NT threads.
 template <int KIND, int DUAL, int W, int NT>
@@ -119,7 +122,7 @@ struct Feed {
         const uint32_t row = idx / CHUNKS, r = DUAL ? (row >> 5) * 16 + (row & 15u) : row;
         off[i] = r * ld_bytes + chunk_of(i, tid) * 16;
       } else {
-        const uint32_t k = idx / (W / 8), chunk = (idx % (W / 8)) ^ swz_cols(k);
+        const uint32_t k = idx / (W / 8), chunk = (idx % (W / 8)) ^ swz_cols<W>(k);
         off[i] = chunk * 16 >= rows ? OUT : k * ld_bytes + chunk * 16;
       }
     }
@@ -172,7 +175,7 @@ __device__ __forceinline__ s8 fragment(const lds_char *lds, int first, int ks, i
   s4 half[2];
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
-    const uint32_t k = ks * 32 + q * 8 + h * 4 + (c >> 2), chunk = (first / 8 + ((c & 3) >> 1)) ^ swz_cols(k);
+    const uint32_t k = ks * 32 + q * 8 + h * 4 + (c >> 2), chunk = (first / 8 + ((c & 3) >> 1)) ^ swz_cols<W>(k);
     half[h] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(lds + k * (W * 2) + chunk * 16 + (c & 1) * 8));
   }
   return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
@@ -444,8 +447,10 @@ __device__ __forceinline__ void multiply(const F &now, F &next, f4 (&acc)[4][MT]
   constexpr int M = 4 * MT, LOADS = LOAD ? G::LOADS : 0, READS = F::READS;
 #pragma unroll
   for (int i = 0; i < M; ++i) {
-    if ((i + 1) * LOADS / M > i * LOADS / M) fetch.one(i * LOADS / M, slot);
-    if ((i + 1) * READS / M > i * READS / M) next.read(i * READS / M, from, from + G::A_BYTES, wm, wn, ks, lane);
+#pragma unroll
+    for (int l = i * LOADS / M; l < (i + 1) * LOADS / M; ++l) fetch.one(l, slot);
+#pragma unroll
+    for (int r = i * READS / M; r < (i + 1) * READS / M; ++r) next.read(r, from, from + G::A_BYTES, wm, wn, ks, lane);
     acc[i & 3][i >> 2] = T::mfma(now.b[i & 3], now.a[i >> 2], acc[i & 3][i >> 2]);
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -557,6 +562,7 @@ bool launch_products(int tile, const GemmGroup &g, hipStream_t st) {
   const dim3 grid((uint32_t)g.first[g.count]);
   if (tile == TILE_256) hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 2, 4, 8, 2>), grid, dim3(512), 0, st, g);
   else if (tile == TILE_128_DEEP) hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 4, 2, 2, 4>), grid, dim3(512), 0, st, g);
+  else if (tile == TILE_64 && PRODUCTS != GEMM_BACK) hipLaunchKernelGGL((k_gemm<T, PRODUCTS == GEMM_BACK ? GEMM_OUT : PRODUCTS, 4, 1, 1, 4>), grid, dim3(256), 0, st, g);
   else hipLaunchKernelGGL((k_gemm<T, PRODUCTS, 4, 2, 2, 2>), grid, dim3(512), 0, st, g);
   return hipGetLastError() == hipSuccess;
 }

@@ -154,6 +154,17 @@ def test_ffn_slices_of_the_sums(ops, shape, dtype):
     assert torch.equal(ops.ffn_forward(*inputs[:4]), got["y"])
 
 
+# tiles of 64 x 64: one to many a product, edges inside, split sums, weights that are packed
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("shape", [(25, 1100, 8000), (37, 2048, 5504), (49, 72, 1000), (60, 1001, 2731), (64, 3000, 3200), (100, 520, 1100), (129, 264, 2000), (49, 8, 16)])
+def test_ffn_small_tiles(ops, shape, dtype):
+    act = ("silu", "gelu", "gelu_tanh")[sum(shape) % 3]
+    inputs = ffn_inputs(sum(shape), *shape, dtype)
+    want = formula(*inputs[:4], act, inputs[4])
+    for k, v in ffn_both(ops, inputs, act).items():
+        check(k, v, want[k])
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_ffn_split_sums_on_large_tiles(ops, dtype):
     inputs = ffn_inputs(7, 520, 2051, 5500, dtype)

@@ -366,9 +366,9 @@ struct Pass {
     hipLaunchKernelGGL(k_pack, dim3(groups), dim3(256), 0, st, pack);
     ok = ok && hipGetLastError() == hipSuccess;
   }
-  // two weights of one product: rows of equal length in memory
+  // two weights of one product: rows of equal length in memory, so both are packed where one has to be
   void packed_pair(Matrix &a, Matrix &b) {
-    const bool must = a.ld != b.ld && !(needs_pack(a) && needs_pack(b));
+    const bool must = a.ld != b.ld || needs_pack(a) || needs_pack(b);
     a = packed(a, must);
     b = packed(b, must);
   }

@@ -203,6 +203,21 @@ def test_ffn_strides_and_alignment(ops, T, pad, shift):
         assert bool(torch.isnan(v._base[:3]).all()) and bool(torch.isnan(v._base[3:].view(v.shape[0], -1)[:, v.shape[1]:]).all()), k
 
 
+# rows of equal stride, but only one weight of the pair starts off 16 bytes: both have to come to the same place
+@pytest.mark.parametrize("T", [5, 70, 140])
+@pytest.mark.parametrize("shifts", [(3, 0), (0, 3), (8, 5)])
+def test_ffn_one_unaligned_weight(ops, T, shifts):
+    x, wg, wu, wd, dy = ffn_inputs(12, T, 72, 104, torch.bfloat16)
+    wide = []
+    for i, (w, shift) in enumerate(zip((wg, wu), shifts)):
+        wide.append(normal(gen(i), 104, 72, torch.bfloat16, 1.0, 16, shift))
+        wide[-1].copy_(w)
+    inputs = (x, wide[0], wide[1], wd, dy)
+    want = formula(*inputs[:4], "silu", inputs[4])
+    for k, v in ffn_both(ops, inputs, "silu").items():
+        check(k, v, want[k])
+
+
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
 def test_ffn_large_tiles(ops, dtype):
     inputs = ffn_inputs(5, 3590, 3592, 3608, dtype)

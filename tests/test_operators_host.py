@@ -38,6 +38,15 @@ def test_ffn_sizes():
     assert _sizes(_ffn(T=0), _grads(T=0))[0] == B.OK
 
 
+def test_ffn_packs_both_weights_of_a_product_or_none():
+    """the tiles take both at one row length: a weight that starts off 16 bytes takes the other one with it"""
+    plain = _sizes(_ffn(ld_gate=72, ld_up=72), _grads())[1]
+    copy = 96 * 64 * 2
+    for one in (dict(w_gate=8), dict(w_up=8), dict(w_gate=8, w_up=2), dict(ld_up=80)):
+        both = _sizes(_ffn(**dict(dict(ld_gate=72, ld_up=72), **one)), _grads())[1]
+        assert both[1] == plain[1] + 2 * copy and both[2] == plain[2] + 2 * copy, one
+
+
 @pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
                                     dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
                                     dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])

@@ -340,10 +340,10 @@ struct Pass {
 
   Pass(const chm_ffn *f_, char *base, hipStream_t st_, bool run_) : f(f_), arena{base}, st(st_), run(run_) {}
 
-  // the matrix itself, or a packed copy of it: made by the next flush()
+  // the matrix itself, or a packed copy of it: made by the next flush().  Without tokens no operand is read, and none need be there.
   PackCall pack{};
   Matrix packed(const Matrix &m, bool must = false) {
-    if (!must && !needs_pack(m)) return m;
+    if (f->tokens == 0 || (!must && !needs_pack(m))) return m;
     Matrix o{nullptr, up8(m.cols), m.rows, up8(m.cols)};
     o.p = arena.take((uint64_t)o.rows * o.ld * 2);
     const int64_t words = o.rows * (o.ld / 8);
@@ -625,6 +625,7 @@ extern "C" int chm_ffn_backward(const chm_ffn *f, const chm_ffn_gradients *g, vo
   if (rc == CHM_OK) rc = check_gradients(f, g);
   if (rc != CHM_OK) return rc;
   if (!aligned(scratch, 16) || !g->dw_gate || !g->dw_up || !g->dw_down) return CHM_ERR_ARG;
+  if (f->tokens == 0 && g->accumulate) return CHM_OK;
   if (f->tokens > 0 && (!f->x || !f->w_gate || !f->w_up || !f->w_down || !f->saved || !g->dy || !g->dx || !scratch)) return CHM_ERR_ARG;
   Pass need(f, nullptr, nullptr, false);
   need.backward(g);

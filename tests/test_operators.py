@@ -317,6 +317,27 @@ def test_ffn_no_tokens(ops):
         assert bool((got[k] == 0).all())
 
 
+# odd widths, strides that differ: what a packing would read and copy
+def test_ffn_no_tokens_at_odd_widths(ops):
+    from paper_2508_21613_amd import binding as B
+    D, F = 65, 97
+    x, wg, wu, wd, dy = ffn_inputs(4, 0, D, F, torch.bfloat16)
+    wu = normal(gen(1), F, D, torch.bfloat16, 1.0, 2)
+    y, saved = ops.ffn_forward(x, wg, wu, wd, save=True)
+    assert y.shape == (0, D)
+    grads = [torch.full(s, 7.0, device="cuda") for s in ((F, D), (F, D), (D, F))]
+    ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=grads, accumulate=True)
+    assert all(bool((t == 7).all()) for t in grads)
+    assert ops.ffn_backward(dy, x, wg, wu, wd, saved, grads=grads)[0].shape == (0, D)
+    assert all(bool((t == 0).all()) for t in grads)
+    # inputs, results for tokens and scratch may be missing altogether
+    grads = [torch.full(s, 7.0, device="cuda") for s in ((F, D), (F, D), (D, F))]
+    d = B.Ffn(1, 0, 0, D, F, None, None, None, None, D, D, D + 2, F)
+    g = B.FfnGradients(None, None, *(t.data_ptr() for t in grads), D, D, D, D, F, 0, 0)
+    assert B.lib().chm_ffn_backward(d, g, None, 0, torch.cuda.current_stream().cuda_stream) == B.OK
+    assert all(bool((t == 0).all()) for t in grads)
+
+
 # ------------------------------------------------------------------------------------------------ embedding
 def lookup_want(tokens, table, scale):
     live = (tokens >= 0) & (tokens < table.shape[0])

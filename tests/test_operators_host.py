@@ -47,6 +47,16 @@ def test_ffn_packs_both_weights_of_a_product_or_none():
         assert both[1] == plain[1] + 2 * copy and both[2] == plain[2] + 2 * copy, one
 
 
+def test_ffn_without_tokens_packs_nothing():
+    """no operand need be there then: a packing would read the weights, wherever their pointers lead"""
+    d = _ffn(T=0, D=65, F=97, ld_x=65, ld_gate=65, ld_up=67, ld_down=97)
+    g = _grads(T=0, ld_dy=65, ld_dx=65, ld_dw_gate=65, ld_dw_up=65, ld_dw_down=97)
+    assert _sizes(d, g) == (B.OK, [0, 0, 0])
+    g.dw_gate = g.dw_up = g.dw_down = 64                                                # never touched: nothing is added
+    g.accumulate = 1
+    assert B.lib().chm_ffn_backward(d, g, None, 0, None) == B.OK
+
+
 @pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
                                     dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
                                     dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])

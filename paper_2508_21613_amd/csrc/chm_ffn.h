@@ -48,8 +48,10 @@ struct GemmGroup {
 // runs while a wavefront issues loads.  And of 64 x 64 by 4 wavefronts, four steps, two workgroups a compute unit, where the others are too few:
 // 37 tokens, 2,048 x 5,504, forward 27 us (128 x 128: 34), 64 tokens of a whole step at 512 x 1,376 38 us (42).
 enum { TILE_256 = 0, TILE_128 = 1, TILE_128_DEEP = 2, TILE_64 = 3 };
-// Largest row of memory (elements) that the tile kernels take: 256 rows lie within 2^31 bytes.  Longer ones are packed.
-constexpr int64_t GEMM_LD_MAX = 1 << 21;
+// Largest row of memory (elements) that the tile kernels take: 255 rows and a step of the next lie below Feed::OUT, so that no offset of a
+// tile wraps or falls on the mark of what is outside.  Longer rows of memory are packed; a packed or internal row is as long as its columns, and
+// passes with more of these are refused: width beyond GEMM_LD_MAX, or features beyond half of it (a row of dg and du).
+constexpr int64_t GEMM_LD_MAX = 1 << 22;
 // Launches them; false when HIP fails.  dtype: CHM_BF16 or CHM_F16.
 bool gemm_launch_bf16(int products, int tile, const GemmGroup &g, void *stream);
 bool gemm_launch_f16(int products, int tile, const GemmGroup &g, void *stream);

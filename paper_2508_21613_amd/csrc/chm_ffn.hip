@@ -317,6 +317,13 @@ struct Matrix { const void *p; int64_t ld, rows, cols; };
 
 bool needs_pack(const Matrix &m) { return (uintptr_t)m.p % 16 || m.ld % 8 || m.cols % 8 || m.ld > GEMM_LD_MAX; }
 
+// whether the forward pass runs on the kernels for few tokens
+bool takes_few(const chm_ffn *f) {
+  const int64_t D = f->width, F = f->features;
+  const bool packs = needs_pack({f->w_gate, f->ld_gate, F, D}) || needs_pack({f->w_up, f->ld_up, F, D}) || needs_pack({f->w_down, f->ld_down, D, F});
+  return few_tokens(f->tokens, D, F, packs);
+}
+
 // Hands out scratch, in a fixed order; with no base it only counts
 struct Arena {
   char *base;
@@ -457,8 +464,7 @@ struct Pass {
     const int64_t T = f->tokens, D = f->width, F = f->features, F8 = up8(F);
     const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
-    const bool packs = needs_pack({f->w_gate, f->ld_gate, F, D}) || needs_pack({f->w_up, f->ld_up, F, D}) || needs_pack({f->w_down, f->ld_down, D, F});
-    if (few_tokens(T, D, F, packs)) {
+    if (takes_few(f)) {
       if (!run || T == 0) return;
       FewCall c{};
       c.tokens = (int32_t)T;
@@ -574,6 +580,12 @@ int check(const chm_ffn *f) {
   return CHM_OK;
 }
 
+// The tiles take rows up to GEMM_LD_MAX elements, dg and du lie side by side in one; the kernels for few tokens count in 64 bits.
+bool in_reach(const chm_ffn *f, bool backward) {
+  if (f->tokens == 0 || (f->width <= GEMM_LD_MAX && f->features <= GEMM_LD_MAX / 2)) return true;
+  return !backward && takes_few(f);
+}
+
 int check_gradients(const chm_ffn *f, const chm_ffn_gradients *g) {
   if (!g || (g->grad_dtype != f->dtype && g->grad_dtype != CHM_F32)) return CHM_ERR_ARG;
   const int64_t size = g->grad_dtype == CHM_F32 ? 4 : 2;
@@ -590,6 +602,7 @@ extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint6
   const int rc = check(f);
   if (rc != CHM_OK) return rc;
   if (g && check_gradients(f, g) != CHM_OK) return CHM_ERR_ARG;
+  if ((forward_scratch && !in_reach(f, false)) || (g && !in_reach(f, true))) return CHM_ERR_ARG;
   if (saved) *saved = kept_bytes(f);
   if (forward_scratch) {
     Pass p(f, nullptr, nullptr, false);
@@ -609,7 +622,7 @@ extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint6
 extern "C" int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *scratch, uint64_t scratch_bytes, void *hip_stream) {
   int rc = check(f);
   if (rc != CHM_OK) return rc;
-  if (ld_y < f->width || ld_y > INT32_MAX || !aligned(y, 2) || !aligned(scratch, 16)) return CHM_ERR_ARG;
+  if (ld_y < f->width || ld_y > INT32_MAX || !aligned(y, 2) || !aligned(scratch, 16) || !in_reach(f, false)) return CHM_ERR_ARG;
   if (f->tokens == 0) return CHM_OK;
   if (!f->x || !f->w_gate || !f->w_up || !f->w_down || !y || !scratch) return CHM_ERR_ARG;
   Pass need(f, nullptr, nullptr, false);
@@ -624,7 +637,7 @@ extern "C" int chm_ffn_backward(const chm_ffn *f, const chm_ffn_gradients *g, vo
   int rc = check(f);
   if (rc == CHM_OK) rc = check_gradients(f, g);
   if (rc != CHM_OK) return rc;
-  if (!aligned(scratch, 16) || !g->dw_gate || !g->dw_up || !g->dw_down) return CHM_ERR_ARG;
+  if (!aligned(scratch, 16) || !g->dw_gate || !g->dw_up || !g->dw_down || !in_reach(f, true)) return CHM_ERR_ARG;
   if (f->tokens == 0 && g->accumulate) return CHM_OK;
   if (f->tokens > 0 && (!f->x || !f->w_gate || !f->w_up || !f->w_down || !f->saved || !g->dy || !g->dx || !scratch)) return CHM_ERR_ARG;
   Pass need(f, nullptr, nullptr, false);

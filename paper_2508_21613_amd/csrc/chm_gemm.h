@@ -90,6 +90,7 @@ template <int KIND, int DUAL, int W, int NT>
 struct Feed {
   enum : uint32_t { OUT = 0x7fffffff };
   enum { CHUNKS = BK / 8, NI = W * BK * 2 / 16 / NT, BYTES = W * BK * 2 };
+  static_assert((W - 1) * GEMM_LD_MAX * 2 + BK * 2 <= OUT && (BK - 1) * GEMM_LD_MAX * 2 + W * 2 <= OUT, "offsets within a tile");
   const char *base;        // of the tile at the present step
   const char *base2;       // of the tile at the second run of k
   int64_t step_bytes;      // from one step to the next

@@ -243,6 +243,15 @@ def test_ffn_offsets_beyond_32_bits(ops):
         check(k, got[k], (value, var * 10))                                # float32 sums of T terms were allowed for 16,384 only
 
 
+# the longest rows that the tiles take: 2^22 elements, of x and the weights, or of dg and du side by side
+@pytest.mark.parametrize("shape", [(130, 1 << 22, 64), (130, 64, 1 << 21)])
+def test_ffn_longest_rows(ops, shape):
+    inputs = ffn_inputs(6, *shape, torch.bfloat16)
+    want = formula(*inputs[:4], "silu", inputs[4])
+    for k, v in ffn_both(ops, inputs, "silu").items():
+        check(k, v, want[k])
+
+
 def test_ffn_accumulates(ops):
     T, D, F, dtype = 100, 136, 72, torch.bfloat16
     a, b = ffn_inputs(1, T, D, F, dtype), ffn_inputs(2, T, D, F, dtype)

@@ -57,6 +57,24 @@ def test_ffn_without_tokens_packs_nothing():
     assert B.lib().chm_ffn_backward(d, g, None, 0, None) == B.OK
 
 
+def test_ffn_rows_that_the_tiles_cannot_reach_are_refused():
+    """offsets within a tile are of 32 bits: up to 2^22 elements a row, of which dg and du take two of `features`"""
+    def sizes(T, D, F):
+        d, g = _ffn(T, D, F), _grads(T, D, F)
+        some = [C.c_uint64() for _ in range(2)]
+        return B.lib().chm_ffn_sizes(d, None, *some, None), B.lib().chm_ffn_sizes(d, g, some[0], None, some[1])
+
+    W, H = 1 << 22, 1 << 21
+    assert sizes(128, W, 64) == sizes(128, 64, H) == sizes(8, W, H) == (B.OK, B.OK)
+    assert sizes(128, W + 8, 64) == sizes(128, 64, H + 8) == sizes(256, 64, 8454664) == (B.ERR_ARG, B.ERR_ARG)
+    assert sizes(8, 1 << 24, 1 << 24) == sizes(1, W + 8, 8) == (B.OK, B.ERR_ARG)        # few tokens count in 64 bits
+    assert sizes(0, 1 << 24, 1 << 24) == (B.OK, B.OK)
+    for D, F in ((W + 8, 64), (64, H + 8)):
+        assert B.lib().chm_ffn_forward(_ffn(128, D, F), None, D, None, 0, None) == B.ERR_ARG
+        one = _grads(128, D, F, dw_gate=64, dw_up=64, dw_down=64)
+        assert B.lib().chm_ffn_backward(_ffn(128, D, F), one, None, 0, None) == B.ERR_ARG
+
+
 @pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
                                     dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
                                     dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])

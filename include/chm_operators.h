@@ -34,8 +34,8 @@ enum { CHM_ACT_SILU = 0, CHM_ACT_GELU = 1, CHM_ACT_GELU_TANH = 2 };          /* 
 typedef struct {
   int32_t dtype;                              /* CHM_BF16 or CHM_F16: type of all tensors */
   int32_t activation;                         /* CHM_ACT_* */
-  int64_t tokens, width, features;            /* tokens >= 0, the others >= 1; tokens below 2^31, width up to 2^22, features up to
-                                                 2^21; both up to 2^24 in forward calls of up to 8 tokens */
+  int64_t tokens, width, features;            /* tokens >= 0, the others >= 1; tokens below 2^31 - 2^13, width up to 2^22, features
+                                                 up to 2^21; both up to 2^24 in forward calls of up to 8 tokens */
   const void *x, *w_gate, *w_up, *w_down;
   int64_t ld_x, ld_gate, ld_up, ld_down;
   void *saved;                                /* g and u as the backward pass wants them (opaque, 16-byte aligned): written by the

@@ -344,6 +344,7 @@ struct Pass {
   Arena arena;
   hipStream_t st;
   bool run, ok = true;
+  bool fits = true;                        // every launch's threads can be counted in 32 bits, as a grid's are; else the calls refuse
 
   Pass(const chm_ffn *f_, char *base, hipStream_t st_, bool run_) : f(f_), arena{base}, st(st_), run(run_) {}
 
@@ -402,16 +403,18 @@ struct Pass {
       for (int s = 1; s <= 8; ++s) {
         if (s > 1 && (!may_split || sums(call[0]) < 512 * (int64_t)s)) break;
         double work = 0, longest = 0, us;
-        int64_t tiles = 0;
+        int64_t tiles = 0, groups = 0;
         for (int i = 0; i < count; ++i) {
           const int parts = i == 0 ? s : 1;
           const int64_t n = products == GEMM_GATE_UP ? 2 * call[i].n : call[i].n;
           const int64_t t = ((call[i].m + most) >> bits) * ((n + most) >> bits) * parts;
+          groups += ((t / parts + 7) & ~7ll) * parts;
           const double unit = (double)((sums(call[i]) + 63) / 64 + parts - 1) / parts * STEP[tile] + ends;
           work += t * unit;
           tiles += t;
           if (t && unit > longest) longest = unit;
         }
+        if (groups * (tile == TILE_64 ? 256 : 512) > UINT32_MAX) continue;
         if (tile == TILE_64) {             // the third of a compute unit begins where the first ends
           us = tiles <= 256 ? 0.8 * longest : tiles <= 512 ? longest : tiles * longest / 512;
         } else if (count == 1) {           // equal tiles: whole rounds, one of single tiles where two fit goes faster
@@ -431,6 +434,8 @@ struct Pass {
 
   void launch(int products, GemmGroup &g) {
     const Layout l = layout(products, g.call, g.count, products == GEMM_OUT || products == GEMM_BACK);
+    fits = fits && l.us < 1e30;
+    if (!fits) return;
     const int side = 1 << side_bits(l.tile);
     g.first[0] = 0;
     for (int i = 0; i < g.count; ++i) {
@@ -627,6 +632,7 @@ extern "C" int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *sc
   if (!f->x || !f->w_gate || !f->w_up || !f->w_down || !y || !scratch) return CHM_ERR_ARG;
   Pass need(f, nullptr, nullptr, false);
   need.forward(y, ld_y);
+  if (!need.fits) return CHM_ERR_ARG;
   if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
   Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
   p.forward(y, ld_y);
@@ -642,6 +648,7 @@ extern "C" int chm_ffn_backward(const chm_ffn *f, const chm_ffn_gradients *g, vo
   if (f->tokens > 0 && (!f->x || !f->w_gate || !f->w_up || !f->w_down || !f->saved || !g->dy || !g->dx || !scratch)) return CHM_ERR_ARG;
   Pass need(f, nullptr, nullptr, false);
   need.backward(g);
+  if (!need.fits) return CHM_ERR_ARG;
   if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
   Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
   p.backward(g);

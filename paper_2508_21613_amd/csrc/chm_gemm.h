@@ -479,7 +479,7 @@ __device__ __forceinline__ void tile_product(const GemmCall &c, int block, lds_c
   const int wm = (wave / WN) * (MT * 16), wn = (wave % WN) * 64;
 
   // steps of this workgroup
-  const int steps_seg = (int)((c.a.k > c.b.k ? c.a.k : c.b.k) + BK - 1) / BK, steps = steps_seg * c.runs;
+  const int steps_seg = (int)(((c.a.k > c.b.k ? c.a.k : c.b.k) + BK - 1) / BK), steps = steps_seg * c.runs;
   int step = 0, last = steps;
   if (c.splits > 1) {
     step = (int)((int64_t)steps * split / c.splits);

@@ -252,6 +252,17 @@ def test_ffn_longest_rows(ops, shape):
         check(k, v, want[k])
 
 
+# more tokens than tiles of 128 x 128 can be counted for in one launch
+def test_ffn_more_tokens_than_small_tiles_reach(ops):
+    T, D, F, dtype = (1 << 30) + 77, 8, 8, torch.bfloat16
+    _, wg, wu, wd, _ = ffn_inputs(8, 1, D, F, dtype)
+    x = torch.empty((T, D), dtype=dtype, device="cuda").normal_(0.0, 1.0, generator=gen(8))
+    y = ops.ffn_forward(x, wg, wu, wd)
+    for at in (0, (1 << 29) - 500, (1 << 30) - 500, T - 1000):
+        s = slice(at, at + 1000)
+        check("y", y[s], formula(x[s], wg, wu, wd, "silu")["y"])
+
+
 def test_ffn_accumulates(ops):
     T, D, F, dtype = 100, 136, 72, torch.bfloat16
     a, b = ffn_inputs(1, T, D, F, dtype), ffn_inputs(2, T, D, F, dtype)

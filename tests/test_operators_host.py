@@ -75,6 +75,15 @@ def test_ffn_rows_that_the_tiles_cannot_reach_are_refused():
         assert B.lib().chm_ffn_backward(_ffn(128, D, F), one, None, 0, None) == B.ERR_ARG
 
 
+def test_ffn_launches_fit_a_grid():
+    """a launch has fewer than 2^32 threads: the largest tiles reach up to 2^31 - 2^13 tokens, and what none reaches is refused"""
+    L, any_ = B.lib(), dict(x=64, w_gate=64, w_up=64, w_down=64)
+    for T, F, rc in (((1 << 31) - 1, 8, B.ERR_ARG), ((1 << 31) - 8193, 8, B.ERR_LIMIT), (1 << 30, 8, B.ERR_LIMIT), (1 << 30, 4096, B.ERR_ARG)):
+        assert L.chm_ffn_forward(_ffn(T, 8, F, **any_), 64, 8, 64, 1, None) == rc, T     # ERR_LIMIT: taken, but the scratch is too short
+        g = _grads(T, 8, F, dy=64, dx=64, dw_gate=64, dw_up=64, dw_down=64)
+        assert L.chm_ffn_backward(_ffn(T, 8, F, saved=64, **any_), g, 64, 1, None) == rc, T
+
+
 @pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
                                     dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
                                     dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])

@@ -24,7 +24,9 @@ constexpr int SMALL = 512;               // places the unsorted kernel takes
 constexpr int RANGES_MAX = 16384, RANGE_ROWS = 512 * 512 - 1;      // places and rows the sort by ranges of keys takes
 constexpr int BINS = 512, DIGIT = 9;
 constexpr int SORT_GROUPS = 64;
-constexpr int ZERO_ROWS = 32;            // rows that a workgroup sets to zero where no token names them
+constexpr int ZERO_ROWS = 32;            // rows that a workgroup sets to zero at a time where no token names them
+// A grid has fewer than 2^32 threads: workgroups that set rows to zero go on to further ones beyond 2^25 rows, a lookup is a launch for every 2^24 places
+constexpr int64_t ZERO_GROUPS_MAX = 1 << 20, LOOKUP_PLACES = 1 << 24;
 
 struct Tokens {
   const void *p;
@@ -357,10 +359,13 @@ __global__ void __launch_bounds__(NT) k_runs(Gather c) {
   if ((int)blockIdx.x >= c.piece_groups) {
     if (blockIdx.y) return;
     __shared__ uint8_t named[ZERO_ROWS];
-    const int64_t first = (int64_t)(blockIdx.x - c.piece_groups) * ZERO_ROWS;
-    if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x < c.tokens.rows ? c.named[first + threadIdx.x] : 1;
-    __syncthreads();
-    zero_rows<GT>(c, first, named);
+    const int64_t step = (int64_t)(gridDim.x - c.piece_groups) * ZERO_ROWS;
+    for (int64_t first = (int64_t)(blockIdx.x - c.piece_groups) * ZERO_ROWS; first < c.tokens.rows; first += step) {
+      if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x < c.tokens.rows ? c.named[first + threadIdx.x] : 1;
+      __syncthreads();
+      zero_rows<GT>(c, first, named);
+      __syncthreads();
+    }
     return;
   }
   const int x = threadIdx.x % c.across, y = threadIdx.x / c.across, down = NT / c.across;
@@ -485,14 +490,17 @@ __global__ void __launch_bounds__(NT) k_few(Gather c) {
   if ((int)blockIdx.x >= n) {
     if (blockIdx.y) return;
     __shared__ uint8_t named[ZERO_ROWS];
-    const int64_t first = (int64_t)(blockIdx.x - n) * ZERO_ROWS;
-    if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x >= c.tokens.rows;
-    __syncthreads();
+    const int64_t step = (int64_t)(gridDim.x - n) * ZERO_ROWS;
+    for (int64_t first = (int64_t)(blockIdx.x - n) * ZERO_ROWS; first < c.tokens.rows; first += step) {
+      if (threadIdx.x < ZERO_ROWS) named[threadIdx.x] = first + threadIdx.x >= c.tokens.rows;
+      __syncthreads();
 #pragma unroll
-    for (int i = 0; i < EACH; ++i)
-      if (own[i] < c.tokens.rows && own[i] >= first && own[i] < first + ZERO_ROWS) named[own[i] - first] = 1;
-    __syncthreads();
-    zero_rows<GT>(c, first, named);
+      for (int i = 0; i < EACH; ++i)
+        if (own[i] < c.tokens.rows && own[i] >= first && own[i] < first + ZERO_ROWS) named[own[i] - first] = 1;
+      __syncthreads();
+      zero_rows<GT>(c, first, named);
+      __syncthreads();
+    }
     return;
   }
   __shared__ uint16_t list[SMALL];
@@ -579,10 +587,16 @@ Scratch scratch_of(int64_t n, int64_t rows, int64_t width) {
   return s;
 }
 
+// workgroups that set the rows without a token to zero
+int64_t zero_groups(const Gather &c) {
+  const int64_t g = ((int64_t)c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
+  return c.accumulate ? 0 : g < ZERO_GROUPS_MAX ? g : ZERO_GROUPS_MAX;
+}
+
 template <int DT, int GT>
 bool launch_few(Gather c, hipStream_t st) {
   c.zero_across = zero_across_of(c.width / Lane<GT>::N);
-  const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
+  const int64_t zero = zero_groups(c);
   const int cols = (c.width + NT * Lane<DT>::N - 1) / (NT * Lane<DT>::N);
   if (c.n + zero) hipLaunchKernelGGL((k_few<DT, GT>), dim3((uint32_t)(c.n + zero), cols), dim3(NT), 0, st, c);
   return hipGetLastError() == hipSuccess;
@@ -595,7 +609,7 @@ bool launch_runs(Gather c, hipStream_t st) {
   c.zero_across = zero_across_of(c.width / Lane<GT>::N);
   const int down = NT / c.across;
   c.piece_groups = (c.pieces + down - 1) / down;
-  const int64_t zero = c.accumulate ? 0 : (c.tokens.rows + ZERO_ROWS - 1) / ZERO_ROWS;
+  const int64_t zero = zero_groups(c);
   hipLaunchKernelGGL((k_runs<DT, GT>), dim3((uint32_t)(c.piece_groups + zero), (uint32_t)((groups + c.across - 1) / c.across)), dim3(NT), 0, st, c);
   hipLaunchKernelGGL((k_join<GT>), dim3((uint32_t)((c.pieces + JOIN_PIECES - 1) / JOIN_PIECES), (uint32_t)((c.width + 255) / 256)), dim3(NT), 0, st, c);
   return hipGetLastError() == hipSuccess;
@@ -607,8 +621,13 @@ bool launch_lookup(Lookup c, hipStream_t st) {
   c.across = across_of(groups);
   const uint32_t cols = (uint32_t)((groups + c.across - 1) / c.across);
   const int down = NT / c.across;
-  if (c.n >= 4096) hipLaunchKernelGGL((k_lookup<DT, 2>), dim3((uint32_t)((c.n + 2 * down - 1) / (2 * down)), cols), dim3(NT), 0, st, c);
-  else hipLaunchKernelGGL((k_lookup<DT, 1>), dim3((uint32_t)((c.n + down - 1) / down), cols), dim3(NT), 0, st, c);
+  for (int64_t left = c.n; left > 0; left -= LOOKUP_PLACES) {
+    c.n = left < LOOKUP_PLACES ? left : LOOKUP_PLACES;
+    if (c.n >= 4096) hipLaunchKernelGGL((k_lookup<DT, 2>), dim3((uint32_t)((c.n + 2 * down - 1) / (2 * down)), cols), dim3(NT), 0, st, c);
+    else hipLaunchKernelGGL((k_lookup<DT, 1>), dim3((uint32_t)((c.n + down - 1) / down), cols), dim3(NT), 0, st, c);
+    c.tokens.p = (const char *)c.tokens.p + LOOKUP_PLACES * (c.tokens.bits / 8);
+    c.out += LOOKUP_PLACES * c.ld_out;
+  }
   return hipGetLastError() == hipSuccess;
 }
 

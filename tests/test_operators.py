@@ -459,6 +459,31 @@ def test_embedding_offsets_beyond_32_bits(ops):
             assert bool((table[row] == value).all()), (n, row)
 
 
+# rows and places that one launch of a workgroup each cannot count: 2^32 threads
+@pytest.mark.parametrize("n", [300, 1000])
+def test_embedding_gradient_of_more_rows_than_a_grid_holds(ops, n):
+    V = (1 << 29) + 45
+    tokens = torch.tensor([V - 1, 0, 1 << 25, (1 << 25) - 1, V - 1, 400000001, -1, V], device="cuda").repeat((n + 7) // 8)[:n]
+    dy = torch.ones((n, 1), dtype=torch.bfloat16, device="cuda")
+    out = torch.full((V, 1), 9.0, dtype=torch.bfloat16, device="cuda")
+    ops.embedding_gradient(dy, tokens, out=out)
+    for row in (V - 1, 0, 1 << 25, (1 << 25) - 1, 400000001):
+        assert float(out[row]) == float((tokens == row).sum()), row
+        out[row] = 0
+    assert bool((out == 0).all())
+
+
+def test_embedding_lookup_of_more_places_than_a_grid_holds(ops):
+    n, V = (1 << 30) + 4099, 251
+    tokens = torch.arange(n, dtype=torch.int32, device="cuda") % (V + 1)                # the last one is outside the table
+    table = torch.arange(1, V + 1, device="cuda").bfloat16()[:, None]
+    got = ops.embedding_lookup(tokens, table)
+    want = torch.cat([table[:, 0], torch.zeros(1, dtype=table.dtype, device="cuda")])
+    for at in range(0, n, 1 << 28):
+        s = slice(at, min(at + (1 << 28), n))
+        assert torch.equal(got[s, 0], want[tokens[s].long()]), at
+
+
 def test_embedding_infinities_stay_in_their_rows(ops):
     for n in (100, 1000):
         tokens = torch.arange(n, device="cuda") % 50

@@ -49,10 +49,11 @@ struct F16 {
   static __device__ __forceinline__ float up(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
 };
 
-// the activation of g and its derivative, in float32; the reciprocal instruction is right to one unit in the last place
+// the activation of g and its derivative, in float32; the reciprocal instruction is right to one unit in the last place.
+// Phi(g) = erfc(-g / sqrt 2) / 2: 1 + erf(g / sqrt 2) would cancel to the left of 0 (a tenth of the value at g = -5, all of it from -5.5 on).
 template <int ACT> __device__ __forceinline__ float act_of(float g) {
   if (ACT == CHM_ACT_SILU) return g * __builtin_amdgcn_rcpf(1.f + __expf(-g));
-  if (ACT == CHM_ACT_GELU) return 0.5f * g * (1.f + erff(g * 0.70710678118654752f));
+  if (ACT == CHM_ACT_GELU) return 0.5f * g * erfcf(g * -0.70710678118654752f);
   // 0.5 (1 + tanh z) = 1 / (1 + exp(-2 z))
   const float z = 0.79788456080286536f * (g + 0.044715f * g * g * g);
   return g * __builtin_amdgcn_rcpf(1.f + __expf(-2.f * z));
@@ -63,7 +64,7 @@ template <int ACT> __device__ __forceinline__ void act_grad_of(float g, float &a
     a = g * s;
     da = s * (1.f + g * (1.f - s));
   } else if (ACT == CHM_ACT_GELU) {
-    const float p = 0.5f * (1.f + erff(g * 0.70710678118654752f));
+    const float p = 0.5f * erfcf(g * -0.70710678118654752f);
     a = g * p;
     da = p + g * 0.39894228040143268f * __expf(-0.5f * g * g);
   } else {

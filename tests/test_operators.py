@@ -183,6 +183,38 @@ def test_ffn_activations(ops, act, T):
         check(k, v, want[k])
 
 
+# The activation's left tail by itself: one token whose projections are g in [-6, -3] and u = 1,024, a down projection that hands h on, so that
+# every result is one value of the formula, rounded once to its type.  float32 gets that value to 2^-16: the exponents (up to 25) and the
+# argument's square (up to 18) are off by some 2^-23 of themselves.
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("T", [1, 70])
+def test_ffn_left_tail_of_the_activations(ops, act, T, dtype):
+    F = 192
+    g = torch.linspace(-6, -3, F, device="cuda").to(dtype)
+    x, wg, wu, dy = (torch.zeros(s, dtype=dtype, device="cuda") for s in ((T, F), (F, F), (F, F), (T, F)))
+    x[0, 0], wg[:, 0], wu[:, 0], dy[0] = 1, g, 1024, 1024
+    wd = torch.eye(F, device="cuda").to(dtype)
+    y, saved = ops.ffn_forward(x, wg, wu, wd, activation=act, save=True)
+    grads = [torch.empty((F, F), device="cuda") for _ in range(3)]
+    ops.ffn_backward(dy, x, wg, wu, wd, saved, activation=act, grads=grads)
+    g = g.double()
+    if act == "gelu":
+        a = g * torch.special.ndtr(g)
+        da = torch.special.ndtr(g) + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    else:
+        z, dz = (g, 1.0) if act == "silu" else (math.sqrt(8 / math.pi) * (g + 0.044715 * g ** 3), math.sqrt(8 / math.pi) * (1 + 3 * 0.044715 * g * g))
+        s = torch.sigmoid(z)
+        a, da = g * s, s + g * s * torch.sigmoid(-z) * dz
+    for name, got, want in (("h", y[0], 1024 * a), ("h again", grads[2][0] / 1024, 1024 * a), ("du", grads[1][:, 0], 1024 * a),
+                            ("dg", grads[0][:, 0], 1024 * 1024 * da)):
+        beyond = want.abs() > torch.finfo(dtype).max                       # infinite in the type, as the formula's value is
+        assert torch.equal(got[beyond].double(), want[beyond].sign() * math.inf), name
+        err = (got.double() - want).abs()[~beyond]
+        tol = (torch.clamp(want.abs() * U[dtype], min=TINY[dtype]) + 2.0 ** -16 * want.abs())[~beyond]
+        assert bool((err <= tol).all()), (name, float((err / tol).max()))
+
+
 @pytest.mark.parametrize("T", [3, 70, 140])
 @pytest.mark.parametrize("pad,shift", [(0, 1), (3, 0), (5, 7), (8, 0), (64, 8)])
 def test_ffn_strides_and_alignment(ops, T, pad, shift):

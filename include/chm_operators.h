@@ -8,7 +8,8 @@
  *
  * Conventions, beside those of chm.h
  *   - Tensors are DEVICE memory of the caller, aligned to their element size, rows of `ld` elements (>= the row's length).
- *     Inputs and outputs must not overlap, except where a call says so.
+ *     Outputs must not lie over inputs, scratch or each other, except where a call says so (CHM_ERR_ARG); columns of the same rows of
+ *     memory may be different tensors.
  *   - Calls are asynchronous on hip_stream, allocate nothing, and may be captured into a graph.  Scratch is device memory of
  *     the caller, 16-byte aligned, at least as long as the matching *_sizes / *_scratch call says; it is free again when the call's
  *     work on the stream has finished.
@@ -42,7 +43,7 @@ typedef struct {
                                                  forward call, read by the backward call; NULL in a forward call: not kept */
 } chm_ffn;
 
-/* The block forward.  Up to a few dozen tokens it is bound by reading the weights and runs on kernels for that.
+/* The block forward.  Up to a few dozen tokens it is bound by reading the weights and runs on kernels for that.  y may lie over x.
  * Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
 int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *scratch, uint64_t scratch_bytes, void *hip_stream);
 
@@ -97,7 +98,8 @@ int chm_load_gradients(const chm_gradient *list, int32_t count, chm_gradients **
 /* *d_sumsq (device) = sum of squares over the handle's tensors: what the stages of a pipeline add up. */
 int chm_gradient_sumsq(chm_gradients *g, double *d_sumsq, void *hip_stream);
 /* *d_norm (device) = the norm; the tensors are clipped.  d_sumsq (device, nullable): the sum of squares over all stages;
- * NULL: that of the handle's own tensors.  In place, tensors that need no clipping are not written.  max_norm >= 0. */
+ * NULL: that of the handle's own tensors.  In place, tensors that need no clipping are not written.  max_norm >= 0.
+ * A tensor that is listed twice, or a result over another tensor, is CHM_ERR_ARG here (the sum of squares counts it twice). */
 int chm_clip_gradients(chm_gradients *g, float max_norm, const double *d_sumsq, float *d_norm, void *hip_stream);
 /* Waits for the device's work on the handle. */
 void chm_free_gradients(chm_gradients *g);

@@ -11,6 +11,7 @@
 #include <stdint.h>
 #include <string.h>
 
+#include <algorithm>
 #include <new>
 #include <vector>
 
@@ -177,10 +178,29 @@ __global__ void __launch_bounds__(NT) k_scale(List l, const double *sums, int n,
   run_scale<NT>(l, l.groups - 1 - blockIdx.x, factor_of(norm, max_norm));
 }
 
+// Whether every result shares memory with no tensor but its own, and with that one wholly or not at all
+bool apart(const std::vector<Tensor> &tensors) {
+  struct Span { uintptr_t from, to; bool out; };
+  std::vector<Span> spans;
+  for (const Tensor &t : tensors) {
+    const uintptr_t in = (uintptr_t)t.in, out = (uintptr_t)t.out, bytes = (uintptr_t)(t.n * t.bytes);
+    spans.push_back(Span{out, out + bytes, true});
+    if (in != out) spans.push_back(Span{in, in + bytes, false});
+  }
+  std::sort(spans.begin(), spans.end(), [](const Span &a, const Span &b) { return a.from < b.from; });
+  uintptr_t end[2] = {0, 0};             // of the inputs and of the results so far
+  for (const Span &s : spans) {
+    if (s.from < end[1] || (s.out && s.from < end[0])) return false;
+    if (s.to > end[s.out]) end[s.out] = s.to;
+  }
+  return true;
+}
+
 }  // namespace
 
 struct chm_gradients {
   int device = 0;
+  bool apart = true;                     // no result lies over another tensor: else clipping would read what it has written
   List list{};
   char *memory = nullptr;                // tensors, starts, sums
   double *sums = nullptr;
@@ -218,6 +238,7 @@ extern "C" int chm_load_gradients(const chm_gradient *in, int32_t count, chm_gra
       while (t + 1 < tensors.size() && first[t + 1] <= at) ++t;
       starts[b] = Start{(int32_t)t, tensors.empty() ? 0 : (int32_t)(at - first[t])};
     }
+    g->apart = apart(tensors);
     const size_t bt = tensors.size() * sizeof(Tensor), bs = starts.size() * sizeof(Start), bd = GROUPS_MAX * sizeof(double);
     std::vector<char> host(bt + bs);
     if (bt) memcpy(host.data(), tensors.data(), bt);
@@ -251,7 +272,7 @@ extern "C" int chm_gradient_sumsq(chm_gradients *g, double *d_sumsq, void *hip_s
 }
 
 extern "C" int chm_clip_gradients(chm_gradients *g, float max_norm, const double *d_sumsq, float *d_norm, void *hip_stream) {
-  if (!g || !d_norm || !(max_norm >= 0)) return CHM_ERR_ARG;
+  if (!g || !d_norm || !(max_norm >= 0) || !g->apart) return CHM_ERR_ARG;
   hipStream_t st = (hipStream_t)hip_stream;
   if (!d_sumsq) hipLaunchKernelGGL(k_sumsq, dim3(g->list.groups), dim3(NT), 0, st, g->list, g->sums);
   hipLaunchKernelGGL(k_scale, dim3(g->list.groups), dim3(NT), 0, st, g->list, d_sumsq ? d_sumsq : g->sums, d_sumsq ? 1 : g->list.groups,

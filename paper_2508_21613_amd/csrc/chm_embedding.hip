@@ -13,6 +13,7 @@
 #include <stdint.h>
 
 #include "chm_elements.h"
+#include "chm_overlap.h"
 
 namespace {
 
@@ -633,6 +634,10 @@ bool launch_lookup(Lookup c, hipStream_t st) {
 
 bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
 
+using chm_overlap::Rows;
+using chm_overlap::stretch;
+Rows rows_of(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size) { return Rows{p, rows, cols * size, ld * size}; }
+
 }  // namespace
 
 extern "C" int chm_embedding_lookup(int32_t dtype, int32_t index_bits, const void *tokens, int64_t n, const void *table,
@@ -645,6 +650,8 @@ extern "C" int chm_embedding_lookup(int32_t dtype, int32_t index_bits, const voi
   if (!aligned(tokens, index_bits / 8) || !aligned(table, size) || !aligned(out, size)) return CHM_ERR_ARG;
   if (n == 0) return CHM_OK;
   if (!tokens || !out || (rows > 0 && !table)) return CHM_ERR_ARG;
+  const Rows result[] = {rows_of(out, n, width, ld_out, size)}, inputs[] = {rows_of(table, rows, width, ld_table, size), stretch(tokens, n * (index_bits / 8))};
+  if (chm_overlap::clash(result, inputs)) return CHM_ERR_ARG;
   Lookup c{};
   c.tokens = Tokens{tokens, index_bits, (uint32_t)rows};
   c.table = (const char *)table;
@@ -679,6 +686,9 @@ extern "C" int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t
   const Scratch s = scratch_of(n, rows, width);
   if (s.bytes && !scratch) return CHM_ERR_ARG;
   if (scratch_bytes < s.bytes) return CHM_ERR_LIMIT;
+  const Rows results[] = {rows_of(grad, rows, width, ld_grad, size_of(grad_dtype)), stretch(scratch, (int64_t)s.bytes)},
+             inputs[] = {rows_of(dy, n, width, ld_dy, size_of(dtype)), stretch(tokens, n * (index_bits / 8))};
+  if (chm_overlap::clash(results, inputs)) return CHM_ERR_ARG;
   hipStream_t st = (hipStream_t)hip_stream;
   char *mem = (char *)scratch;
   Gather c{};

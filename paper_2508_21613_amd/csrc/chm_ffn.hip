@@ -12,6 +12,7 @@
 
 #include "chm_elements.h"
 #include "chm_gemm.h"
+#include "chm_overlap.h"
 
 namespace {
 
@@ -585,6 +586,31 @@ int check(const chm_ffn *f) {
   return CHM_OK;
 }
 
+using chm_overlap::Rows;
+using chm_overlap::stretch;
+Rows rows_of(const void *p, int64_t rows, int64_t cols, int64_t ld, int64_t size) { return Rows{p, rows, cols * size, ld * size}; }
+
+// y is stored when x has been read for the last time: it may lie over x, but over nothing else
+bool clash_forward(const chm_ffn *f, void *y, int64_t ld_y, void *scratch, uint64_t scratch_bytes) {
+  const int64_t T = f->tokens, D = f->width, F = f->features;
+  const Rows x = rows_of(f->x, T, D, f->ld_x, 2), wg = rows_of(f->w_gate, F, D, f->ld_gate, 2), wu = rows_of(f->w_up, F, D, f->ld_up, 2),
+             wd = rows_of(f->w_down, D, F, f->ld_down, 2);
+  const Rows last[] = {rows_of(y, T, D, ld_y, 2)}, weights[] = {wg, wu, wd};
+  const Rows before[] = {stretch(f->saved, f->saved ? (int64_t)kept_bytes(f) : 0), stretch(scratch, (int64_t)scratch_bytes)},
+             all[] = {wg, wu, wd, x, last[0]};
+  return chm_overlap::clash(last, weights) || chm_overlap::clash(before, all);
+}
+
+bool clash_backward(const chm_ffn *f, const chm_ffn_gradients *g, void *scratch, uint64_t scratch_bytes) {
+  const int64_t T = f->tokens, D = f->width, F = f->features, size = g->grad_dtype == CHM_F32 ? 4 : 2;
+  const int64_t there = T > 0;               // without tokens no input is read
+  const Rows results[] = {rows_of(g->dx, T, D, g->ld_dx, 2), rows_of(g->dw_gate, F, D, g->ld_dw_gate, size), rows_of(g->dw_up, F, D, g->ld_dw_up, size),
+                          rows_of(g->dw_down, D, F, g->ld_dw_down, size), stretch(scratch, (int64_t)scratch_bytes)};
+  const Rows inputs[] = {rows_of(f->x, T, D, f->ld_x, 2), rows_of(g->dy, T, D, g->ld_dy, 2), rows_of(f->w_gate, F * there, D, f->ld_gate, 2),
+                         rows_of(f->w_up, F * there, D, f->ld_up, 2), rows_of(f->w_down, D * there, F, f->ld_down, 2), stretch(f->saved, (int64_t)kept_bytes(f))};
+  return chm_overlap::clash(results, inputs);
+}
+
 // The tiles take rows up to GEMM_LD_MAX elements, dg and du lie side by side in one; the kernels for few tokens count in 64 bits.
 bool in_reach(const chm_ffn *f, bool backward) {
   if (f->tokens == 0 || (f->width <= GEMM_LD_MAX && f->features <= GEMM_LD_MAX / 2)) return true;
@@ -634,6 +660,7 @@ extern "C" int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *sc
   need.forward(y, ld_y);
   if (!need.fits) return CHM_ERR_ARG;
   if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  if (clash_forward(f, y, ld_y, scratch, need.arena.used)) return CHM_ERR_ARG;
   Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
   p.forward(y, ld_y);
   return p.ok ? CHM_OK : CHM_ERR_HIP;
@@ -650,6 +677,7 @@ extern "C" int chm_ffn_backward(const chm_ffn *f, const chm_ffn_gradients *g, vo
   need.backward(g);
   if (!need.fits) return CHM_ERR_ARG;
   if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  if (clash_backward(f, g, scratch, need.arena.used)) return CHM_ERR_ARG;
   Pass p(f, (char *)scratch, (hipStream_t)hip_stream, true);
   p.backward(g);
   return p.ok ? CHM_OK : CHM_ERR_HIP;

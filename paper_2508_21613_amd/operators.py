@@ -3,8 +3,8 @@
 The gated feed-forward block forward and backward, the embedding's lookup and gradient, the global gradient norm with clipping.
 As everywhere in this package torch provides device memory and streams; every value is computed by the library's HIP kernels, and
 without a usable GPU the calls fail.  A call works on the current stream, or on `stream`; scratch and results that the caller does
-not hand in are allocated on that stream.  Inputs must be ready there, as with any torch call.  Wrong arguments raise
-binding.ChmError with the library's code.
+not hand in are allocated on that stream.  Inputs must be ready there, as with any torch call.  Results must not lie over inputs or each
+other (ffn_forward's may lie over x).  Wrong arguments raise binding.ChmError with the library's code.
 """
 import ctypes as C
 import math

@@ -84,6 +84,87 @@ def test_ffn_launches_fit_a_grid():
         assert L.chm_ffn_backward(_ffn(T, 8, F, saved=64, **any_), g, 64, 1, None) == rc, T
 
 
+@pytest.mark.skipif(torch.cuda.is_available(), reason="pointers that nobody may follow")
+def test_results_over_other_tensors_are_refused():
+    """without a GPU a call that goes on to its launches says ERR_HIP"""
+    L, T, D, F, M = B.lib(), 100, 64, 96, 1 << 20
+    at = {k: (i + 1) * M for i, k in enumerate(("x", "w_gate", "w_up", "w_down", "saved", "dy", "dx", "dw_gate", "dw_up", "dw_down"))}
+    ffn, grad = ("x", "w_gate", "w_up", "w_down", "saved"), ("dy", "dx", "dw_gate", "dw_up", "dw_down")
+
+    def forward(y=20 * M, ld_y=D, scratch=30 * M, **kw):
+        return L.chm_ffn_forward(_ffn(T, D, F, **{k: dict(at, **kw)[k] for k in ffn}), y, ld_y, scratch, M, None)
+
+    def backward(scratch=30 * M, ld=None, **kw):
+        g = _grads(T, D, F, **{k: dict(at, **kw)[k] for k in grad})
+        if ld:
+            g.ld_dw_gate = g.ld_dw_up = ld
+        return L.chm_ffn_backward(_ffn(T, D, F, **{k: dict(at, **kw)[k] for k in ffn}), g, scratch, M, None)
+
+    assert forward() == forward(y=at["x"]) == forward(y=at["x"] + 2) == B.ERR_HIP         # y may lie over x
+    for k in ("w_gate", "w_up", "w_down", "saved"):
+        assert forward(y=at[k]) == forward(scratch=at[k]) == B.ERR_ARG, k
+    assert forward(saved=at["x"]) == forward(scratch=at["x"]) == forward(y=30 * M) == forward(y=30 * M - 2 * T * D + 2) == B.ERR_ARG
+    assert forward(y=30 * M - 2 * T * D) == B.ERR_HIP
+    assert backward() == B.ERR_HIP
+    for k in grad[1:]:
+        for other in ffn + grad:
+            if other != k:
+                assert backward(**{k: at[other]}) == B.ERR_ARG, (k, other)
+    assert backward(dx=at["dy"] + 2 * (T * D - 1)) == B.ERR_ARG and backward(dx=at["dy"] + 2 * T * D) == B.ERR_HIP
+    # columns of one buffer
+    assert backward(dw_up=at["dw_gate"] + 2 * D, ld=2 * D) == B.ERR_HIP and backward(dw_up=at["dw_gate"] + 2 * D - 2, ld=2 * D) == B.ERR_ARG
+    assert backward(dw_up=at["dw_gate"] + 2 * D, ld=2 * D - 1) == B.ERR_ARG
+
+    n, V = 600, 50
+
+    def embedding_gradient(grad=M, dy=2 * M, tokens=3 * M, scratch=4 * M):
+        return L.chm_embedding_gradient(1, 1, 64, tokens, n, dy, D, V, D, 1.0, grad, D, 0, scratch, M, None)
+
+    assert embedding_gradient() == embedding_gradient(grad=2 * M - 2 * V * D) == B.ERR_HIP
+    for bad in (dict(grad=2 * M), dict(grad=2 * M - 2), dict(grad=3 * M), dict(scratch=2 * M), dict(scratch=3 * M), dict(scratch=M)):
+        assert embedding_gradient(**bad) == B.ERR_ARG, bad
+    for out in (M, M + 2 * V * D - 2, 3 * M, 3 * M + 8 * n - 2):
+        assert L.chm_embedding_lookup(1, 64, 3 * M, n, M, D, V, D, 1.0, out, D, None) == B.ERR_ARG
+    assert L.chm_embedding_lookup(1, 64, 3 * M, n, M, D, V, D, 1.0, M + 2 * V * D, D, None) == B.ERR_HIP
+
+
+def test_rows_that_share_memory(tmp_path):
+    """csrc/chm_overlap.h against marking every byte"""
+    import os
+    import subprocess
+    csrc = os.path.join(os.path.dirname(os.path.abspath(B.__file__)), "csrc")
+    src = tmp_path / "overlap.cpp"
+    src.write_text(r'''
+#include "chm_overlap.h"
+#include <stdio.h>
+#include <string.h>
+#include <random>
+using chm_overlap::Rows;
+int main() {
+  std::mt19937 rng(1);
+  static char memory[400], mark[400];
+  long shared = 0;
+  const auto pick = [&](int n) { return (int64_t)(rng() % n); };
+  const auto rows = [&]() { Rows r{memory + pick(90), pick(7), pick(9), 0}; r.pitch = r.bytes + (pick(3) ? pick(12) : 0); if (!r.pitch) r.pitch = 1; return r; };
+  for (int t = 0; t < 1000000; ++t) {
+    const Rows a = rows();
+    Rows b = rows();
+    if (pick(2) && a.pitch >= b.bytes) b.pitch = a.pitch;
+    bool want = false;
+    memset(mark, 0, sizeof mark);
+    for (int64_t i = 0; i < a.rows; ++i) memset(mark + ((const char *)a.p - memory) + i * a.pitch, 1, a.bytes);
+    for (int64_t i = 0; i < b.rows; ++i)
+      for (int64_t k = 0; k < b.bytes; ++k) want |= mark[((const char *)b.p - memory) + i * b.pitch + k] != 0;
+    if (chm_overlap::share(a, b) != want || chm_overlap::share(b, a) != want) { printf("case %d\n", t); return 1; }
+    shared += want;
+  }
+  return shared > 100000 ? 0 : 2;
+}
+''')
+    subprocess.run(["g++", "-O2", "-std=c++17", "-I", csrc, "-o", str(tmp_path / "overlap"), str(src)], check=True)
+    subprocess.run([str(tmp_path / "overlap")], check=True)
+
+
 @pytest.mark.parametrize("change", [dict(dtype=0), dict(dtype=3), dict(activation=3), dict(activation=-1), dict(tokens=-1), dict(width=0),
                                     dict(features=0), dict(width=1 << 25), dict(ld_x=63), dict(ld_gate=63), dict(ld_up=63), dict(ld_down=95),
                                     dict(x=1), dict(w_down=3), dict(saved=8), dict(ld_x=1 << 32)])

@@ -137,7 +137,8 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, activation="silu", grads=No
     weights' gradients to write, or with accumulate=True to add to; of the weights' type or float32.  `out`: dx to write."""
     d, T, D, F, x_dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
     ld_dy = _matrix("dy", dy, T, D, x_dtype, dev)
-    _need(isinstance(saved, torch.Tensor) and saved.get_device() == dev and saved.dtype == torch.uint8, "saved must be what ffn_forward returned")
+    _need(isinstance(saved, torch.Tensor) and saved.get_device() == dev and saved.dtype == torch.uint8 and saved.is_contiguous(),
+          "saved must be what ffn_forward returned")
     ld_dx = D if out is None else _matrix("out", out, T, D, x_dtype, dev)
     if grads is None:
         _need(not accumulate, "accumulate needs grads")

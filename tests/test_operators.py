@@ -609,6 +609,17 @@ def test_clip_refuses_results_over_other_tensors(ops):
         assert e.value.code == B.ERR_ARG and torch.equal(buf, raw)
 
 
+def test_saved_has_to_be_one_stretch_of_memory(ops):
+    from paper_2508_21613_amd import binding as B
+    x, wg, wu, wd, dy = ffn_inputs(15, 20, 64, 64, torch.bfloat16)
+    y, saved = ops.ffn_forward(x, wg, wu, wd, save=True)
+    for other in (saved.repeat_interleave(2)[::2], saved[:1].expand(saved.shape)):     # as many elements, elsewhere in memory or nowhere
+        with pytest.raises(B.ChmError) as e:
+            ops.ffn_backward(dy, x, wg, wu, wd, other)
+        assert e.value.code == B.ERR_ARG
+    assert torch.equal(ops.ffn_backward(dy, x, wg, wu, wd, saved.clone())[0], ops.ffn_backward(dy, x, wg, wu, wd, saved)[0])
+
+
 def test_results_over_inputs(ops):
     from paper_2508_21613_amd import binding as B
     for T in (5, 100):

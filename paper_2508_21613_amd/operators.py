@@ -240,10 +240,11 @@ class Gradients:
         grads = list(grads)
         out = None if out is None else list(out)
         _need(out is None or len(out) == len(grads), "out must have a tensor for each gradient")
+        _need(all(isinstance(t, torch.Tensor) for t in grads), "gradients must be tensors")
         self.device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
         items = (B.Gradient * max(len(grads), 1))()
         for i, t in enumerate(grads):
-            _need(isinstance(t, torch.Tensor) and t.is_cuda and t.device == self.device, "gradients must be on one GPU")
+            _need(t.is_cuda and t.device == self.device, "gradients must be on one GPU")
             _need(t.dtype in DTYPES, "gradients must be float32, bfloat16 or float16")
             _need(_dense(t), "gradients must be dense")
             items[i].grad, items[i].n, items[i].dtype = t.data_ptr(), t.numel(), DTYPES[t.dtype]

@@ -228,6 +228,14 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
         assert e.value.code == B.ERR_ARG
 
 
+def test_gradients_that_are_no_tensors_are_refused():
+    """a parameter's missing gradient among them"""
+    for bad in ([None], [3.0], [None, torch.zeros(3)], [torch.zeros(3), None]):
+        with pytest.raises(B.ChmError) as e:
+            ops.Gradients(bad)
+        assert e.value.code == B.ERR_ARG, bad
+
+
 def test_structures_match_the_header(tmp_path):
     """sizes and field offsets of the binding's structures against what a C compiler makes of include/chm_operators.h"""
     import os

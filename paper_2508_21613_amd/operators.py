@@ -5,6 +5,9 @@ As everywhere in this package torch provides device memory and streams; every va
 without a usable GPU the calls fail.  A call works on the current stream, or on `stream`; scratch and results that the caller does
 not hand in are allocated on that stream.  Inputs must be ready there, as with any torch call.  Results must not lie over inputs or each
 other (ffn_forward's may lie over x).  Wrong arguments raise binding.ChmError with the library's code.
+
+Results are no part of autograd's graph; the gradients are calls of their own.  While torch records gradients, inputs that require one are
+taken only where the caller asks for what the gradient's call wants (ffn_forward with save=True): anything else would lose it without a word.
 """
 import ctypes as C
 import math
@@ -91,6 +94,12 @@ def _scope(stream, device, *tensors):
     return _Other(stream, device, tensors)
 
 
+def _unrecorded(*tensors):
+    if any([t.requires_grad for t in tensors]) and torch.is_grad_enabled():
+        raise B.ChmError(B.ERR_ARG, "the result would carry no gradient to inputs that require one: call under torch.no_grad() and take the "
+                                    "gradients from ffn_backward and embedding_gradient")
+
+
 def _bytes(n, like):
     return like.new_empty(max(n, 16), dtype=torch.uint8)
 
@@ -117,6 +126,8 @@ def ffn_forward(x, w_gate, w_up, w_down, activation="silu", save=False, out=None
     save=True returns (y, saved), `saved` being what ffn_backward wants (opaque; 6 bytes per token and feature)."""
     d, T, D, F, dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
     ld_y = D if out is None else _matrix("out", out, T, D, dtype, dev)
+    if not save:
+        _unrecorded(x, w_gate, w_up, w_down)
     lib = B.lib()
     with _scope(stream, dev, x, w_gate, w_up, w_down, out) as st:
         need, scratch = C.c_uint64(), C.c_uint64()
@@ -183,6 +194,7 @@ def embedding_lookup(tokens, table, scale=1.0, out=None, stream=None):
     bits, n = _tokens(tokens, dev)
     rows, width = table.shape
     ld_out = width if out is None else _matrix("out", out, n, width, dtype, dev)
+    _unrecorded(table)
     with _scope(stream, dev, tokens, table, out) as st:
         if out is None:
             out = table.new_empty((n, width))

@@ -620,6 +620,26 @@ def test_saved_has_to_be_one_stretch_of_memory(ops):
     assert torch.equal(ops.ffn_backward(dy, x, wg, wu, wd, saved.clone())[0], ops.ffn_backward(dy, x, wg, wu, wd, saved)[0])
 
 
+def test_gradients_are_not_lost_without_a_word(ops):
+    from paper_2508_21613_amd import binding as B
+    inputs = ffn_inputs(16, 20, 64, 64, torch.bfloat16)
+    x, wg, wu, wd, dy = inputs
+    tokens = torch.arange(20, device="cuda")
+    want, row = ops.ffn_forward(x, wg, wu, wd), ops.embedding_lookup(tokens, wg)
+    for t in inputs[:4]:
+        t.requires_grad_()
+        calls = [lambda: ops.ffn_forward(x, wg, wu, wd)] + ([lambda: ops.embedding_lookup(tokens, wg)] if t is wg else [])
+        for call in calls:
+            with pytest.raises(B.ChmError) as e:
+                call()
+            assert e.value.code == B.ERR_ARG and "no_grad" in str(e.value)
+        with torch.no_grad():
+            assert torch.equal(ops.ffn_forward(x, wg, wu, wd), want) and torch.equal(ops.embedding_lookup(tokens, wg), row)
+        y, saved = ops.ffn_forward(x, wg, wu, wd, save=True)               # a caller that takes the gradients by the calls for them
+        assert torch.equal(y, want) and not y.requires_grad and not ops.ffn_backward(dy, x, wg, wu, wd, saved)[0].requires_grad
+        t.requires_grad_(False)
+
+
 def test_results_over_inputs(ops):
     from paper_2508_21613_amd import binding as B
     for T in (5, 100):

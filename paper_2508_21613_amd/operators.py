@@ -246,7 +246,9 @@ class Gradients:
     """chm_load_gradients ... chm_free_gradients: the gradients of a stage, whose buffers stay where they are from step to step.
 
     `grads`: dense tensors (float32, bfloat16, float16, mixed) on one GPU.  `out`: tensors of the same types, shapes and strides that
-    receive the clipped gradients; without it they are clipped in place.  The tensors are kept alive."""
+    receive the clipped gradients; without it they are clipped in place.  The tensors are kept alive.  Calls share the handle's workspace:
+    one on another stream than the last waits for that one on the GPU (a stream that was handed in lives until then).  A captured call is
+    ordered by whoever replays it."""
 
     def __init__(self, grads, out=None):
         grads = list(grads)
@@ -268,6 +270,7 @@ class Gradients:
                 items[i].out = o.data_ptr()
         self._h = C.c_void_p()
         self._tensors = (grads, out)
+        self._last = None                                                  # the stream of the last call
         with torch.cuda.device(self.device):
             B._check(B.lib().chm_load_gradients(items, len(grads), C.byref(self._h)))
 
@@ -282,9 +285,18 @@ class Gradients:
         except Exception:
             pass
 
+    def _ordered(self, st):
+        """the current stream (st) goes on behind the handle's last call"""
+        if (self._last is None or self._last.cuda_stream != st) and not torch.cuda.is_current_stream_capturing():
+            here = torch.cuda.current_stream()
+            if self._last is not None:
+                here.wait_stream(self._last)
+            self._last = here
+
     def sumsq(self, stream=None):
         """chm_gradient_sumsq: the sum of squares, a float64 tensor of one element on the GPU; those of the stages of a pipeline add up"""
         with _scope(stream, self.device.index) as st:
+            self._ordered(st)
             total = torch.empty(1, dtype=torch.float64, device=self.device)
             B._check(B.lib().chm_gradient_sumsq(self._h, total.data_ptr(), st))
         return total
@@ -298,6 +310,7 @@ class Gradients:
             _need(isinstance(sumsq, torch.Tensor) and sumsq.device == self.device and sumsq.dtype == torch.float64 and sumsq.numel() == 1,
                   "sumsq must be a float64 tensor of one element")
         with _scope(stream, self.device.index, sumsq) as st:
+            self._ordered(st)
             norm = torch.empty((), dtype=torch.float32, device=self.device)
             B._check(B.lib().chm_clip_gradients(self._h, max_norm, None if sumsq is None else sumsq.data_ptr(), norm.data_ptr(), st))
         return norm

@@ -662,6 +662,28 @@ def test_results_over_inputs(ops):
         assert e.value.code == B.ERR_ARG
 
 
+def test_clip_on_one_stream_after_another(ops):
+    """calls share a workspace: one on another stream begins when the one before has ended"""
+    t = normal(gen(1), 1000, 1000, torch.float32)
+    filler = torch.empty(1 << 28, device="cuda")
+    g = ops.Gradients([t], [torch.empty_like(t)])
+    want = float(g.clip(1.0))
+    a, b = torch.cuda.Stream(), torch.cuda.Stream()
+    torch.cuda.synchronize()
+    for first, second, call in ((a, b, g.sumsq), (b, a, lambda stream: g.clip(1.0, stream=stream)), (a, b, lambda stream: g.clip(1.0, stream=stream.cuda_stream))):
+        with torch.cuda.stream(first):
+            for _ in range(30):
+                filler.zero_()                                             # some 5 ms in all
+        one = call(stream=first) if call == g.sumsq else call(first)
+        ended = torch.cuda.Event()
+        ended.record(first)
+        two = g.clip(1.0, stream=second)
+        second.synchronize()
+        assert ended.query()
+        assert float(two) == want and (float(one) == want or call == g.sumsq)
+        torch.cuda.synchronize()
+
+
 def test_clip_in_any_dense_layout(ops):
     t = torch.randn(40, 50, generator=gen(1), device="cuda").t()
     raw = t.clone()

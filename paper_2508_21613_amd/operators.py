@@ -246,7 +246,7 @@ class Gradients:
     """chm_load_gradients ... chm_free_gradients: the gradients of a stage, whose buffers stay where they are from step to step.
 
     `grads`: dense tensors (float32, bfloat16, float16, mixed) on one GPU.  `out`: tensors of the same types, shapes and strides that
-    receive the clipped gradients; without it they are clipped in place.  The tensors are kept alive.  Calls share the handle's workspace:
+    receive the clipped gradients; without it they are clipped in place.  The tensors' memory is kept.  Calls share the handle's workspace:
     one on another stream than the last waits for that one on the GPU (a stream that was handed in lives until then).  A captured call is
     ordered by whoever replays it."""
 
@@ -269,7 +269,7 @@ class Gradients:
                       "out must match the gradients")
                 items[i].out = o.data_ptr()
         self._h = C.c_void_p()
-        self._tensors = (grads, out)
+        self._tensors = [t.detach() for t in grads + (out or [])]          # aliases: a tensor may be given other memory
         self._last = None                                                  # the stream of the last call
         with torch.cuda.device(self.device):
             B._check(B.lib().chm_load_gradients(items, len(grads), C.byref(self._h)))

@@ -684,6 +684,16 @@ def test_clip_on_one_stream_after_another(ops):
         torch.cuda.synchronize()
 
 
+def test_gradients_keep_their_memory(ops):
+    """a tensor that is given other memory leaves the listed one with the list"""
+    t, o = torch.ones(1 << 20, device="cuda"), torch.zeros(1 << 20, device="cuda")
+    g, places = ops.Gradients([t], [o]), {t.data_ptr(), o.data_ptr()}
+    t.data, o.data = torch.zeros(3, device="cuda"), torch.zeros(3, device="cuda")
+    others = [torch.zeros(1 << 20, device="cuda") for _ in range(4)]
+    assert not places & {k.data_ptr() for k in others}
+    assert float(g.clip(1.0)) == 1024.0 and all(bool((k == 0).all()) for k in others)
+
+
 def test_clip_in_any_dense_layout(ops):
     t = torch.randn(40, 50, generator=gen(1), device="cuda").t()
     raw = t.clone()

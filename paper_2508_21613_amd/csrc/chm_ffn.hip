@@ -62,7 +62,7 @@ __device__ __forceinline__ float act(int kind, float g) {
 }
 
 __device__ __forceinline__ void keep_pair(const FewCall &c, int64_t m, int64_t f, float g, float u) {
-  const uint32_t bg = __float_as_uint(g), bu = __float_as_uint(u);
+  const uint32_t bg = chm_gemm::upper24(g), bu = chm_gemm::upper24(u);
   char *p = chm_gemm::kept_at(c.kept, m, f);
   const int e = (int)f & 7;
   ((uint16_t *)p)[e] = (uint16_t)(bg >> 16);

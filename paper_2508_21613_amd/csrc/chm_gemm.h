@@ -272,8 +272,9 @@ __device__ __forceinline__ void finish_plain(const GemmCall &c, int split, int64
 }
 
 // Values kept for the backward pass: the upper 24 bits of float32 (16 of them significant), 1.5 times the bytes of the tensors' own type.
-// Rounded to that type they would add an error as large as all others together to every gradient.  Cut off rather than rounded: two
-// byte permutations for four values, and not a number stays one.
+// Rounded to that type they would add an error as large as all others together to every gradient.  Rounded to the nearest, half away from
+// zero: cut off they are too small by 2^-17 to 2^-16 on average, which a float32 gradient over 65,536 tokens shows (1.3e-5 to 2.7e-5 of itself,
+// ten times its other errors).  Infinities stay, and so does what is not a number: sums of products of 16-bit values have zeros in its lower bits.
 //
 // They lie in blocks of 16 rows x 32 features of 3 KiB: upper 16 bits of g, those of u, lower 8 of both, each eight features' 16 bytes behind
 // the other, row by row.  That is how the 64 lanes of a wavefront hold them: every store is one stretch of 1 KiB (in planes of rows
@@ -283,18 +284,20 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 __device__ __forceinline__ char *kept_at(const Kept &k, int64_t m, int64_t f) {
   return k.p + ((m >> 4) * k.blocks + (f >> 5)) * 3072 + ((m & 15) * 4 + ((f >> 3) & 3)) * 16;
 }
+__device__ __forceinline__ uint32_t upper24(float v) { return __float_as_uint(v) + 0x80u; }      // in the upper 24 bits; the others are left over
 template <int PAST>
 __device__ __forceinline__ void keep8(const Kept &k, int64_t m, int64_t f, const float *g, const float *u) {
   u4 hi[2], lo;
 #pragma unroll
   for (int w = 0; w < 2; ++w) {
-    const float *v = w ? u : g;
+    uint32_t v[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) hi[w][i] = __builtin_amdgcn_perm(__float_as_uint(v[2 * i + 1]), __float_as_uint(v[2 * i]), 0x07060302);
+    for (int e = 0; e < 8; ++e) v[e] = upper24(w ? u[e] : g[e]);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) hi[w][i] = __builtin_amdgcn_perm(v[2 * i + 1], v[2 * i], 0x07060302);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
-      lo[w * 2 + i] = __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 1]), __float_as_uint(v[4 * i]), 0x0c0c0501) |
-                      __builtin_amdgcn_perm(__float_as_uint(v[4 * i + 3]), __float_as_uint(v[4 * i + 2]), 0x05010c0c);
+      lo[w * 2 + i] = __builtin_amdgcn_perm(v[4 * i + 1], v[4 * i], 0x0c0c0501) | __builtin_amdgcn_perm(v[4 * i + 3], v[4 * i + 2], 0x05010c0c);
   }
   char *p = kept_at(k, m, f);
   CHM_PUT((u4 *)p, hi[0]);

@@ -311,6 +311,22 @@ def test_ffn_accumulates(ops):
             check(k, g, (f.double() + wb[k][0], wb[k][1] + (ACC * f.double()) ** 2))
 
 
+# What is kept between the passes must not lean to one side.  All values are positive, so that a lean adds up and the roundings do not: of 65,536 x 64
+# roundings of h, du or dg to 11 bits a mean of 2^-12 / sqrt(3) / 2^11 is left, six times that 4e-7; the float32 sums (2,048 additions each, 4,096 of
+# them) leave less, and the activation's instructions are right to 2^-22.  2^-19 is allowed; values cut to 16 bits lean by 1.1e-5 and more.
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_ffn_float32_gradients_of_many_tokens_lean_to_no_side(ops, act):
+    T, D, F, dtype = 65536, 64, 64, torch.float16
+    x, wg, wu, wd, dy = (torch.rand(s, generator=gen(30 + i), device="cuda") for i, s in enumerate(((T, D), (F, D), (F, D), (D, F), (T, D))))
+    x, wg, wu, wd, dy = [t.to(dtype) for t in (x + 0.25, wg * 4 / D, wu * 4 / D, wd / D, dy + 0.25)]
+    grads = [torch.empty(s, device="cuda") for s in ((F, D), (F, D), (D, F))]
+    ffn_both(ops, (x, wg, wu, wd, dy), act, grads=grads)
+    want = formula(x, wg, wu, wd, act, dy)
+    for k, got in zip(NAMES[1:], grads):
+        value = want[k][0]
+        assert abs(float((got.double() - value).sum() / value.sum())) <= 2.0 ** -19, k
+
+
 @pytest.mark.parametrize("T", [4, 80])
 def test_ffn_bits_repeat_and_streams(ops, T):
     inputs = ffn_inputs(9, T, 264, 520, torch.bfloat16)

@@ -87,14 +87,40 @@ class Stage:
         return self.clipper.clip(max_norm, sumsq=sumsq), to_inputs
 
 
+class _Queued:
+    """Times of calls on the GPU alone: fills of a large buffer keep it busy until the calls between two marks have all been made, more of them
+    as long as it came to the first mark before that.  The calls find their operands out of the caches, as in a step."""
+
+    def __init__(self, device):
+        self.buffer = torch.empty(1 << 26, device=device)                  # some 40 us a fill
+        self.fills, self.most = 4, 4096
+
+    def __call__(self, *calls):
+        """ms of each call, made in turn"""
+        while True:
+            marks = [torch.cuda.Event(enable_timing=True) for _ in range(len(calls) + 1)]
+            for _ in range(self.fills):
+                self.buffer.zero_()
+            marks[0].record()
+            for call, mark in zip(calls, marks[1:]):
+                call()
+                mark.record()
+            early = marks[0].query()
+            marks[-1].synchronize()
+            if not early or self.fills >= self.most:
+                return [a.elapsed_time(b) for a, b in zip(marks, marks[1:])]
+            self.fills *= 2
+
+
 def measure(stage, tokens, repeats=10, optimizer_bytes=12, seed=1):
     """Tables of the stage's layers (the embedding first, if it has one) for micro-batches of `tokens` tokens: forward and backward time
-    in us (medians, at least 1), MiB of weights, float32 gradients and `optimizer_bytes` per weight, MiB kept per micro-batch in flight."""
+    in us (medians on the GPU, at least 1), MiB of weights, float32 gradients and `optimizer_bytes` per weight, MiB kept per micro-batch in flight."""
     dev = stage.blocks[0][0].device if stage.blocks else stage.table.device
     g = torch.Generator(device=dev)
     g.manual_seed(seed)
     some = stage.blocks[0][0] if stage.blocks else stage.table
     fwd, bwd, mem, act = [], [], [], []
+    timed = _Queued(dev)
     for i in stage.layers:
         if i < 0:
             x = torch.randint(stage.table.shape[0], (tokens,), generator=g, device=dev)
@@ -103,20 +129,16 @@ def measure(stage, tokens, repeats=10, optimizer_bytes=12, seed=1):
             x = torch.empty((tokens, stage.width), dtype=some.dtype, device=dev).normal_(0.0, 1.0, generator=g)
             weights = stage.blocks[i]
         dy = torch.empty((tokens, stage.width), dtype=some.dtype, device=dev).normal_(0.0, 0.05, generator=g)
-        times = [[], []]
-        for r in range(repeats + 2):
-            marks = [torch.cuda.Event(enable_timing=True) for _ in range(3)]
-            marks[0].record()
-            _, kept = stage.forward_layer(i, x)
-            marks[1].record()
-            stage.backward_layer(i, dy, kept, first=False)
-            marks[2].record()
-            marks[2].synchronize()
-            if r >= 2:                                                     # the first ones load the kernels
-                times[0].append(marks[0].elapsed_time(marks[1]))
-                times[1].append(marks[1].elapsed_time(marks[2]))
-        fwd.append(max(1, round(statistics.median(times[0]) * 1e3)))
-        bwd.append(max(1, round(statistics.median(times[1]) * 1e3)))
+        kept = None
+
+        def forward():
+            nonlocal kept
+            kept = stage.forward_layer(i, x)[1]
+
+        times = [timed(forward, lambda: stage.backward_layer(i, dy, kept, first=False)) for _ in range(repeats + 2)]
+        times = [statistics.median(t) for t in zip(*times[2:])]            # the first ones load the kernels
+        fwd.append(max(1, round(times[0] * 1e3)))
+        bwd.append(max(1, round(times[1] * 1e3)))
         n = sum(w.numel() for w in weights)
         mem.append(-(-n * (some.element_size() + 4 + optimizer_bytes) // MIB))
         held = [kept] if torch.is_tensor(kept) else kept

@@ -74,6 +74,23 @@ def test_scenario_of_measured_tables(stage_module):
     assert (rc, best) == O.Scenario(sc).search(7)
 
 
+def test_times_are_those_of_the_gpu(stage_module, monkeypatch):
+    """a host that takes milliseconds to make a layer's calls adds nothing to its times"""
+    import time
+    stage = stage_module.Stage(1, 128, 256, 500)
+
+    def late(call):
+        def f(*args, **kw):
+            time.sleep(0.003)
+            return call(*args, **kw)
+        return f
+
+    monkeypatch.setattr(stage, "forward_layer", late(stage.forward_layer))
+    monkeypatch.setattr(stage, "backward_layer", late(stage.backward_layer))
+    tables = stage_module.measure(stage, 20, repeats=3)
+    assert max(tables["fwd_us"] + tables["bwd_us"]) < 1000, tables
+
+
 def test_command(stage_module, capsys):
     assert stage_module.main(["--layers", "8", "--width", "128", "--features", "256", "--vocabulary", "500", "--tokens", "50", "--pp", "4"]) == 0
     assert "best plan after the loss of [3]" in capsys.readouterr().out

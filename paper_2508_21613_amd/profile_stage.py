@@ -65,7 +65,7 @@ class Stage:
         at most `ahead` + 1 of them in flight as in 1F1B with `ahead` stages behind this one.  gradient_of(k, y): the gradient
         with respect to the result of micro-batch k.  Returns the gradient norm (`sumsq`: of all stages) and, for a stage without an
         embedding, the gradients with respect to the inputs."""
-        flying, to_inputs = collections.deque(), []
+        flying, to_inputs, k = collections.deque(), [], None
 
         def backward():
             k, y, kept = flying.popleft()
@@ -84,6 +84,9 @@ class Stage:
                 backward()
         while flying:
             backward()
+        if k is None:                                                      # the last step's gradients are not this one's
+            for t in [t for block in self.grads for t in block] + ([] if self.table is None else [self.table_grad]):
+                t.zero_()
         return self.clipper.clip(max_norm, sumsq=sumsq), to_inputs
 
 

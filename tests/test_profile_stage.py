@@ -55,6 +55,14 @@ def test_step_against_autograd(stage_module, tokens, ahead):
         assert torch.allclose(a, b * (total / 2 / float(norm)), rtol=1e-3, atol=0)
 
 
+def test_a_step_of_no_micro_batches_has_no_gradients(stage_module):
+    stage = stage_module.Stage(1, 64, 72, 30)
+    tokens = torch.arange(20, device="cuda")
+    assert float(stage.step([tokens], lambda k, y: y, max_norm=1.0)[0]) > 0
+    norm, dx = stage.step([], lambda k, y: y, max_norm=1.0)
+    assert float(norm) == 0 and dx == [] and not any(bool(t.any()) for b in stage.grads for t in b) and not bool(stage.table_grad.any())
+
+
 def test_stage_without_embedding_returns_the_gradients_of_its_inputs(stage_module):
     stage = stage_module.Stage(1, 64, 72, dtype=torch.float16)
     x = [torch.randn(20, 64, device="cuda").half() for _ in range(2)]

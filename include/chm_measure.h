@@ -11,6 +11,7 @@
 #ifndef CHM_MEASURE_H
 #define CHM_MEASURE_H
 #include "chm.h"
+#include "chm_operators.h"
 
 #ifdef __cplusplus
 extern "C" {
@@ -48,6 +49,18 @@ typedef struct {
                                   * and 2^23 vectors each), which chm_search_best_static refuses; no search sweeps it */
 } chm_selection;
 int chm_kernel_selection(const chm_scenario_desc *desc, chm_selection *out);
+
+/* Which kernels the feed-forward block's passes over these tensors run on (chm_operators.h).  Host only; the decision the calls take; results
+ * do not depend on it but for the order of float32 sums.  Errors: CHM_ERR_ARG. */
+typedef struct {
+  int32_t few;                   /* forward on the kernels for few tokens: blocks of 16 tokens of one; 0: on tiles */
+  int32_t few_slices[2];         /* slices of the sums (1, 2, 4) of the two projections and of the down projection */
+  int32_t few_ends[2];           /* 1: rows that end within a step */
+  int32_t tile[4];               /* tiles of both projections, the down projection, dh, and dx with the weights' gradients: 0 256 x 256, 1 128 x 128 by
+                                    two steps, 2 by four, 3 64 x 64; -1: not run */
+  int32_t splits[4];             /* parts of the (first) product's sums */
+} chm_ffn_kernels;
+int chm_ffn_selection(const chm_ffn *f, const chm_ffn_gradients *g, chm_ffn_kernels *out);
 
 /* Whether chm_search_best takes a strategy's family by halves (a partition = a lower half that a lane keeps and an
  * upper half that its wavefront walks over; families of 2^21 partitions and more at nominal speed): *upper_cuts = cuts of an upper half, 0 = it

@@ -21,7 +21,7 @@ SYMBOLS = ["chm_load_scenario", "chm_plan_space", "chm_score_plans", "chm_score_
            "chm_reroute_shape", "chm_transfer_plan", "chm_replan", "chm_replan_table", "chm_compare_objective", "chm_valu_probe", "chm_free_scenario",
            "chm_strerror",
            "chm_ffn_sizes", "chm_ffn_forward", "chm_ffn_backward", "chm_embedding_lookup", "chm_embedding_gradient_scratch", "chm_embedding_gradient",
-           "chm_load_gradients", "chm_gradient_sumsq", "chm_clip_gradients", "chm_free_gradients"]
+           "chm_load_gradients", "chm_gradient_sumsq", "chm_clip_gradients", "chm_free_gradients", "chm_ffn_selection"]
 
 
 class Desc(C.Structure):
@@ -106,6 +106,10 @@ class FfnGradients(C.Structure):
                 ("grad_dtype", C.c_int32), ("accumulate", C.c_int32)]
 
 
+class FfnKernels(C.Structure):
+    _fields_ = [("few", C.c_int32), ("few_slices", C.c_int32 * 2), ("few_ends", C.c_int32 * 2), ("tile", C.c_int32 * 4), ("splits", C.c_int32 * 4)]
+
+
 class Gradient(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
@@ -165,6 +169,7 @@ def lib():
         L.chm_valu_probe.argtypes = [C.c_int32, C.c_uint32, C.POINTER(C.c_double), vp]
         i32, i64, u64 = C.c_int32, C.c_int64, C.c_uint64
         L.chm_ffn_sizes.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), C.POINTER(u64), C.POINTER(u64), C.POINTER(u64)]
+        L.chm_ffn_selection.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), C.POINTER(FfnKernels)]
         L.chm_ffn_forward.argtypes = [C.POINTER(Ffn), vp, i64, vp, u64, vp]
         L.chm_ffn_backward.argtypes = [C.POINTER(Ffn), C.POINTER(FfnGradients), vp, u64, vp]
         L.chm_embedding_lookup.argtypes = [i32, i32, vp, i64, vp, i64, i64, i64, C.c_float, vp, i64, vp]

@@ -10,6 +10,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "../../include/chm_measure.h"
 #include "chm_elements.h"
 #include "chm_gemm.h"
 #include "chm_overlap.h"
@@ -241,9 +242,10 @@ void launch_few(const FewCall &c, hipStream_t st) {
   if (c.k % (64 * SLICES)) hipLaunchKernelGGL((k_few_tokens<T, TWO, TILES, SLICES, 1>), dim3((uint32_t)groups), dim3(w * 64), bytes, st, c);
   else hipLaunchKernelGGL((k_few_tokens<T, TWO, TILES, SLICES, 0>), dim3((uint32_t)groups), dim3(w * 64), bytes, st, c);
 }
+int few_blocks(const FewCall &c) { return (c.tokens + 15) / 16; }
 template <class T, int TWO>
 bool launch_few(const FewCall &c, hipStream_t st) {
-  const int tiles = (c.tokens + 15) / 16, slices = few_slices(TWO, c);
+  const int tiles = few_blocks(c), slices = few_slices(TWO, c);
   if (slices == 4) launch_few<T, TWO, 1, 4>(c, st);
   else if (slices == 2) launch_few<T, TWO, 1, 2>(c, st);
   else if (tiles == 1) launch_few<T, TWO, 1, 1>(c, st);
@@ -347,6 +349,8 @@ struct Pass {
   bool run, ok = true;
   bool fits = true;                        // every launch's threads can be counted in 32 bits, as a grid's are; else the calls refuse
 
+  chm_ffn_kernels chosen{0, {0, 0}, {0, 0}, {-1, -1, -1, -1}, {0, 0, 0, 0}};
+
   Pass(const chm_ffn *f_, char *base, hipStream_t st_, bool run_) : f(f_), arena{base}, st(st_), run(run_) {}
 
   // the matrix itself, or a packed copy of it: made by the next flush().  Without tokens no operand is read, and none need be there.
@@ -437,6 +441,8 @@ struct Pass {
     const Layout l = layout(products, g.call, g.count, products == GEMM_OUT || products == GEMM_BACK);
     fits = fits && l.us < 1e30;
     if (!fits) return;
+    chosen.tile[products] = l.tile;
+    chosen.splits[products] = l.splits;
     const int side = 1 << side_bits(l.tile);
     g.first[0] = 0;
     for (int i = 0; i < g.count; ++i) {
@@ -471,7 +477,7 @@ struct Pass {
     const Kept kept = kept_of(f);
     uint16_t *h = (uint16_t *)arena.take((uint64_t)T * F8 * 2);
     if (takes_few(f)) {
-      if (!run || T == 0) return;
+      if (T == 0) return;
       FewCall c{};
       c.tokens = (int32_t)T;
       c.act = f->activation;
@@ -481,14 +487,16 @@ struct Pass {
       c.out = h; c.ldo = F8;
       c.kept = kept;
       c.rows = (int32_t)F; c.k = (int32_t)D;
-      ok = f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 1>(c, st) : launch_few<chm_gemm::F16, 1>(c, st);
+      few(0, c);
+      if (run) ok = f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 1>(c, st) : launch_few<chm_gemm::F16, 1>(c, st);
       FewCall d{};
       d.tokens = (int32_t)T;
       d.x = h; d.ldx = F8;
       d.w0 = (const uint16_t *)f->w_down; d.ld0 = f->ld_down;
       d.out = (uint16_t *)y; d.ldo = ld_y;
       d.rows = (int32_t)D; d.k = (int32_t)F;
-      ok = ok && (f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 0>(d, st) : launch_few<chm_gemm::F16, 0>(d, st));
+      few(1, d);
+      if (run) ok = ok && (f->dtype == CHM_BF16 ? launch_few<chm_gemm::Bf16, 0>(d, st) : launch_few<chm_gemm::F16, 0>(d, st));
       return;
     }
     const Matrix x = packed({f->x, f->ld_x, T, D}), wd = packed({f->w_down, f->ld_down, D, F});
@@ -510,6 +518,12 @@ struct Pass {
     d.runs = 1;
     out(d, y, ld_y, D);
     launch(GEMM_OUT, second);
+  }
+
+  void few(int which, const FewCall &c) {
+    chosen.few = few_blocks(c);
+    chosen.few_slices[which] = few_slices(!which, c);
+    chosen.few_ends[which] = c.k % (64 * chosen.few_slices[which]) != 0;
   }
 
   // one 16-bit output of `cols` columns
@@ -647,6 +661,16 @@ extern "C" int chm_ffn_sizes(const chm_ffn *f, const chm_ffn_gradients *g, uint6
     p.backward(g);
     *backward_scratch = p.arena.used;
   }
+  return CHM_OK;
+}
+
+extern "C" int chm_ffn_selection(const chm_ffn *f, const chm_ffn_gradients *g, chm_ffn_kernels *out) {
+  if (!out || check(f) != CHM_OK || (g && check_gradients(f, g) != CHM_OK) || !in_reach(f, false) || (g && !in_reach(f, true))) return CHM_ERR_ARG;
+  Pass p(f, nullptr, nullptr, false);
+  p.forward(nullptr, f->width);
+  if (g) p.backward(g);
+  if (!p.fits) return CHM_ERR_ARG;
+  *out = p.chosen;
   return CHM_OK;
 }
 

@@ -173,6 +173,22 @@ def test_ffn_split_sums_on_large_tiles(ops, dtype):
         check(k, v, want[k])
 
 
+# every kernel of the block, each with every activation: all kinds of tile for every product, whole and split sums, all slices, blocks of
+# tokens and ends of the kernels for few tokens (tests/test_operators_host.py asks the library that none is missing)
+FFN_KERNELS = [(1, 10, 8), (401, 8, 5888), (2268, 129, 6656), (263, 8384, 75), (309, 4483, 1664), (2711, 3328, 789), (5, 10, 8), (9, 8, 12), (22, 8, 8), (33, 9, 10),
+               (14, 64, 64), (1, 256, 256), (34, 64, 64), (5, 128, 256), (17, 64, 256), (49, 8, 12), (10, 7512, 8192), (129, 8576, 8798)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("shape", FFN_KERNELS)
+def test_ffn_every_kernel(ops, shape, act, dtype):
+    inputs = ffn_inputs(sum(shape), *shape, dtype)
+    want = formula(*inputs[:4], act, inputs[4])
+    for k, v in ffn_both(ops, inputs, act).items():
+        check(k, v, want[k])
+
+
 @pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
 @pytest.mark.parametrize("T", [5, 90])
 def test_ffn_activations(ops, act, T):

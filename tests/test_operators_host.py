@@ -236,6 +236,39 @@ def test_gradients_that_are_no_tensors_are_refused():
         assert e.value.code == B.ERR_ARG, bad
 
 
+def test_shapes_of_the_gpu_tests_reach_every_kernel_of_the_block():
+    from tests.test_operators import FFN_KERNELS
+    reached = set()
+    for T, D, F in FFN_KERNELS:
+        k = B.FfnKernels()
+        assert B.lib().chm_ffn_selection(_ffn(T, D, F, ld_x=D, ld_gate=D, ld_up=D, ld_down=F), _grads(T, D, F), k) == B.OK
+        reached |= {("tile", p, k.tile[p], k.splits[p] > 1) for p in range(4) if k.tile[p] >= 0}
+        reached |= {("few", p, k.few, k.few_slices[p], k.few_ends[p]) for p in range(2) if k.few}
+    products = {0: (4, False), 1: (4, True), 2: (4, False), 3: (3, True)}              # kinds of tile, whether sums may be split
+    want = {("tile", p, t, s) for p, (tiles, split) in products.items() for t in range(tiles) for s in {False, split}}
+    want |= {("few", p, blocks, slices, ends) for p in (0, 1) for blocks, slices in ((1, 1), (1, 2), (1, 4), (2, 1), (3, 1)) for ends in (0, 1)}
+    assert reached == want
+
+
+def test_ffn_selection_refuses_what_the_calls_refuse():
+    L, k = B.lib(), B.FfnKernels()
+    assert L.chm_ffn_selection(_ffn(), None, k) == B.OK and list(k.tile[2:]) == [-1, -1]
+    assert L.chm_ffn_selection(None, None, k) == L.chm_ffn_selection(_ffn(), None, None) == L.chm_ffn_selection(_ffn(dtype=0), None, k) == B.ERR_ARG
+    assert L.chm_ffn_selection(_ffn(), _grads(grad_dtype=2), k) == L.chm_ffn_selection(_ffn((1 << 31) - 1, 8, 8), None, k) == B.ERR_ARG
+
+
+def test_structure_of_the_selection_matches_the_header(tmp_path):
+    import os
+    import subprocess
+    root = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+    src = tmp_path / "layout.c"
+    src.write_text('#include <stdio.h>\n#include <stddef.h>\n#include "chm_measure.h"\nint main(void) { printf("%zu", sizeof(chm_ffn_kernels));' +
+                   "".join('printf(" %%zu", offsetof(chm_ffn_kernels, %s));' % f for f, _ in B.FfnKernels._fields_) + " return 0; }")
+    subprocess.run(["gcc", "-std=c99", "-I", os.path.join(root, "include"), "-o", str(tmp_path / "layout"), str(src)], check=True)
+    out = [int(v) for v in subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout.split()]
+    assert out == [C.sizeof(B.FfnKernels)] + [getattr(B.FfnKernels, f).offset for f, _ in B.FfnKernels._fields_]
+
+
 def test_structures_match_the_header(tmp_path):
     """sizes and field offsets of the binding's structures against what a C compiler makes of include/chm_operators.h"""
     import os

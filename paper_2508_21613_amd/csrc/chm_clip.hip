@@ -136,10 +136,10 @@ __device__ __forceinline__ double run_sum(const List &l, int group, double *shar
   return group_sum<THREADS>(s, shared);
 }
 
-// min(1, max_norm / (norm + 1e-6)); not a number where the norm is none
-__device__ __forceinline__ float factor_of(float norm, float max_norm) {
-  const float c = max_norm / (norm + 1e-6f);
-  return c > 1.f ? 1.f : c;
+// min(1, max_norm / (norm + 1e-6)), rounded once; not a number where the norm is none.  A norm beyond float32 of finite values still has one.
+__device__ __forceinline__ float factor_of(double norm, float max_norm) {
+  const double c = max_norm / (norm + 1e-6);
+  return c > 1. ? 1.f : (float)c;
 }
 
 template <int THREADS>
@@ -172,8 +172,8 @@ __global__ void __launch_bounds__(NT) k_total(const double *sums, int n, double 
 
 __global__ void __launch_bounds__(NT) k_scale(List l, const double *sums, int n, float max_norm, float *norm_out) {
   __shared__ double shared[NT / 64];
-  const float norm = (float)sqrt(all_sums(sums, n, shared));
-  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = norm;
+  const double norm = sqrt(all_sums(sums, n, shared));
+  if (blockIdx.x == 0 && threadIdx.x == 0) *norm_out = (float)norm;
   // the pieces read last by the first pass come first: the cache still holds them
   run_scale<NT>(l, l.groups - 1 - blockIdx.x, factor_of(norm, max_norm));
 }

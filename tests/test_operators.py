@@ -756,6 +756,16 @@ def test_clip_range_of_values(ops):
     assert float(ops.Gradients([]).clip(1.0)) == 0.0 and float(ops.Gradients([zero[:0]]).sumsq()) == 0.0
 
 
+def test_clip_by_a_norm_beyond_float32(ops):
+    """the gradients are finite: so is the factor, whatever the returned norm's type holds"""
+    t = torch.full((1000,), 3e38, device="cuda")
+    raw = t.clone()
+    norm = ops.Gradients([t]).clip(1000.0)
+    want = clip_want([raw], 1000.0)[1] * raw.double()
+    assert float(norm) == math.inf
+    check("clipped", t, (want, (4 * ACC * want) ** 2))
+
+
 def test_clip_lengths_beyond_32_bits(ops):
     n = (1 << 31) + 5
     t = torch.ones(n, dtype=torch.bfloat16, device="cuda")

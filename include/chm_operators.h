@@ -1,10 +1,10 @@
 /*
- * libchm - the operators of a pipeline stage's training step.
+ * libchm - operators of a pipeline stage's training step.
  *
- * A scenario (chm.h) is made of the forward and backward times and the memory of every layer on every node; these are the
- * operators such times are those of, for one stage on one MI355X (gfx950): the gated feed-forward block forward and backward,
- * the embedding's lookup and gradient, and the global gradient norm with the clipping that ends a step.  All of them run in
- * hand-written HIP kernels; there is no other path.
+ * A scenario (chm.h) is made of the forward and backward times and the memory of every layer on every node.  These are some of the
+ * operators that such a step consists of, for one stage on one MI355X (gfx950): the gated feed-forward block forward and backward,
+ * the embedding's lookup and gradient, and the global gradient norm with the clipping that ends a step (no attention, norms, output
+ * head or optimizer).  All of them run in hand-written HIP kernels; there is no other path.
  *
  * Conventions, beside those of chm.h
  *   - Tensors are DEVICE memory of the caller, aligned to their element size, rows of `ld` elements (>= the row's length).
@@ -43,14 +43,16 @@ typedef struct {
                                                  forward call, read by the backward call; NULL in a forward call: not kept */
 } chm_ffn;
 
-/* The block forward.  Up to a few dozen tokens it is bound by reading the weights and runs on kernels for that.  y may lie over x.
+/* The block forward.  With few tokens (up to 8; 24 or 48 with small weights, 32 with large ones that do not start on 16 bytes) it is
+ * bound by reading the weights and runs on kernels for that.  y may lie over x.
  * Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
 int chm_ffn_forward(const chm_ffn *f, void *y, int64_t ld_y, void *scratch, uint64_t scratch_bytes, void *hip_stream);
 
 /* Gradients of a scalar of which dy is the gradient with respect to y:
  *   dh = dy w_down;  du = dh * act(g);  dg = dh * u * act'(g)
  *   dx = dg w_gate + du w_up;  dw_gate = dg^T x;  dw_up = du^T x;  dw_down = dy^T h
- * dh, h, dg and du are worked out in float32 and rounded to the tensors' type once, where they enter a product. */
+ * dh, h, dg and du are worked out in float32, from g and u of 16 significant bits, and h, dg and du are rounded to the tensors' type once,
+ * where they enter a product: against the formulas in 64 bits results are off by 1.4 times what one rounding to that type makes. */
 typedef struct {
   const void *dy;                             /* [tokens, width], the tensors' type */
   void *dx;                                   /* [tokens, width], the tensors' type */

@@ -1,5 +1,5 @@
 // Layout of one matrix product of the gated feed-forward block and the launch interface between its host part
-// (chm_operators.cpp) and its kernels.  Internal to libchm.
+// (chm_ffn.hip) and its tile kernels (chm_gemm.h).  Internal to libchm.
 #ifndef CHM_FFN_H
 #define CHM_FFN_H
 #include <stdint.h>

@@ -1,4 +1,4 @@
-"""The operators of a pipeline stage's training step, over torch tensors: the calls of include/chm_operators.h.
+"""Operators of a pipeline stage's training step, over torch tensors: the calls of include/chm_operators.h.
 
 The gated feed-forward block forward and backward, the embedding's lookup and gradient, the global gradient norm with clipping.
 As everywhere in this package torch provides device memory and streams; every value is computed by the library's HIP kernels, and
@@ -243,7 +243,8 @@ def _dense(t):
 
 
 class Gradients:
-    """chm_load_gradients ... chm_free_gradients: the gradients of a stage, whose buffers stay where they are from step to step.
+    """chm_load_gradients ... chm_free_gradients: the gradients of a stage, whose buffers stay where they are from step to step (where they
+    are made anew, as by zero_grad(set_to_none=True), the list is too, which waits for the device).
 
     `grads`: dense tensors (float32, bfloat16, float16, mixed) on one GPU.  `out`: tensors of the same types, shapes and strides that
     receive the clipped gradients; without it they are clipped in place.  The tensors' memory is kept.  Calls share the handle's workspace:

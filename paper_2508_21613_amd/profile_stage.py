@@ -1,13 +1,14 @@
-"""A pipeline stage's training step on this package's operators, and the tables of a scenario measured from it.
+"""A training step of embedding and feed-forward blocks on this package's operators, and a scenario's tables measured from it.
 
     python -m paper_2508_21613_amd.profile_stage --layers 32 --width 4096 --features 11008 --vocabulary 32000 --tokens 4096 \\
         --pp 4 --dp 2 --micro-batches 8 --failed 3
 
 A scenario wants the forward and backward time and the memory of every layer, which the paper's profiler collects at run time (System
-Design, workflow step 1).  `Stage` runs what such times are those of: the embedding of the first stage and gated feed-forward blocks,
-forward and backward over the micro-batches of a step in 1F1B order, gradients added up in float32 and clipped at the end.
-`measure` times every layer on the GPU with events, `scenario` makes a scenario of the tables, and the command searches it for the best
-plan after the given failures.
+Design, workflow step 1): a job's tables come from the job.  `Stage` runs the part of such a step that this package has operators for: the
+embedding of the first stage and gated feed-forward blocks (no attention, norms, output head or optimizer), forward and backward over the
+micro-batches of a step in 1F1B order, gradients added up in float32 and clipped at the end.  `measure` times every layer on the GPU with
+events (the clipping is the step's, and in no table), `scenario` makes a scenario of the tables, and the command searches it for the best plan
+after the given failures.
 """
 import argparse
 import collections

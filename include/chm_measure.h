@@ -62,6 +62,17 @@ typedef struct {
 } chm_ffn_kernels;
 int chm_ffn_selection(const chm_ffn *f, const chm_ffn_gradients *g, chm_ffn_kernels *out);
 
+/* Which kernels attention's passes over these tensors run on.  Host only; the decision the calls take; results do not depend on it but for the
+ * order of float32 sums.  Errors: CHM_ERR_ARG. */
+typedef struct {
+  int32_t few;                   /* 1: forward on the kernel for few rows */
+  int32_t dim;                   /* elements of a row that the kernels are made for: 64 or 128 */
+  int32_t packed;                /* inputs copied first: 1 q, 2 k, 4 v, 8 dy */
+  int32_t forward_rows, dq_rows, dkdv_keys;       /* of a workgroup; 0: not run */
+  int32_t forward_splits, dkdv_splits;            /* parts of the sums */
+} chm_attention_kernels;
+int chm_attention_selection(const chm_attention *a, const chm_attention_gradients *g, chm_attention_kernels *out);
+
 /* Whether chm_search_best takes a strategy's family by halves (a partition = a lower half that a lane keeps and an
  * upper half that its wavefront walks over; families of 2^21 partitions and more at nominal speed): *upper_cuts = cuts of an upper half, 0 = it
  * goes through the kernels that take partitions one by one; *wave_steps = steps of 64 lanes, one upper half each, where a lane keeps one

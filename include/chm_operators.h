@@ -3,8 +3,8 @@
  *
  * A scenario (chm.h) is made of the forward and backward times and the memory of every layer on every node.  These are some of the
  * operators that such a step consists of, for one stage on one MI355X (gfx950): the gated feed-forward block forward and backward,
- * the embedding's lookup and gradient, and the global gradient norm with the clipping that ends a step (no attention, norms, output
- * head or optimizer).  All of them run in hand-written HIP kernels; there is no other path.
+ * the embedding's lookup and gradient, rotary positions, attention forward and backward, and the global gradient norm with the clipping
+ * that ends a step (no projections, norms, output head or optimizer).  All of them run in hand-written HIP kernels; there is no other path.
  *
  * Conventions, beside those of chm.h
  *   - Tensors are DEVICE memory of the caller, aligned to their element size, rows of `ld` elements (>= the row's length).
@@ -83,6 +83,76 @@ int chm_embedding_gradient_scratch(int64_t n, int64_t rows, int64_t width, uint6
 int chm_embedding_gradient(int32_t dtype, int32_t grad_dtype, int32_t index_bits, const void *tokens, int64_t n, const void *dy,
                            int64_t ld_dy, int64_t rows, int64_t width, float scale, void *grad, int64_t ld_grad, int32_t accumulate,
                            void *scratch, uint64_t scratch_bytes, void *hip_stream);
+
+/* ---- Rotary positions ----------------------------------------------------------------------------------
+ * Pair i of every head (i < pairs) is turned by the angle positions[axis[i]][t] * frequencies[i] (radians) of its token t:
+ *   a' = a cos - b sin,  b' = a sin + b cos;  backwards: by the negative angle, which is the gradient of the forward call.
+ * The pair is the elements i and i + pairs (CHM_PAIRS_HALVES) or 2 i and 2 i + 1 (CHM_PAIRS_NEIGHBOURS); elements from 2 pairs on are
+ * copied.  One axis for text, more for images (height, width) and video (time, height, width).  Angles are worked out in float64 and
+ * reduced to a turn, the sine and cosine in float32: positions may lie far out. */
+enum { CHM_PAIRS_HALVES = 0, CHM_PAIRS_NEIGHBOURS = 1 };
+typedef struct {
+  int32_t dtype;                              /* of x and out: CHM_F32, CHM_BF16 or CHM_F16 */
+  int32_t index_bits;                         /* of the positions: 32 or 64 (signed) */
+  int32_t pairing;                            /* CHM_PAIRS_* */
+  int32_t axes;                               /* >= 1 */
+  int64_t tokens, heads;                      /* >= 0, below 2^31 */
+  int32_t head_dim, pairs;                    /* 1 <= pairs <= 128, 2 pairs <= head_dim <= 2^20 */
+  const void *x;                              /* [tokens, heads, head_dim], strides in elements; x may be out (the same strides) */
+  void *out;
+  int64_t x_token, x_head, out_token, out_head;
+  const void *positions;                      /* [axes, tokens], any strides */
+  int64_t positions_axis, positions_token;
+  const double *frequencies;                  /* HOST, [pairs], finite; read by the call */
+  const int32_t *axis;                        /* HOST, [pairs], each in [0, axes); NULL: all 0 */
+} chm_rotary;
+/* Errors: CHM_ERR_ARG, CHM_ERR_HIP. */
+int chm_rotary_turn(const chm_rotary *r, int32_t backwards, void *hip_stream);
+
+/* ---- Attention -----------------------------------------------------------------------------------------
+ * q [batch, tokens, heads, dim], k and v [batch, keys, kv_heads, dim]; query head h reads key head h / (heads / kv_heads).
+ *   x = scale q.k;  z = x, or cap tanh(x / cap) where cap > 0;  s = z - slopes[h] |i + keys - tokens - j|
+ *   y_i = sum over the visible j of exp(s_ij) v_j / sum over the visible j of exp(s_ij)
+ * Query i stands at position i + keys - tokens (new tokens behind those whose keys are there).  Visible are the keys j
+ *   - of its own document (documents: a number a token; outside [0, 2^31 - 1) it stands for none, such a token sees nothing and is seen by nobody),
+ *   - causal: up to its own position, and wherever prefix[j] is set (a prompt that all of its document sees).
+ * A query that sees nothing has a result of zeros and no gradient.  Queries, keys and values of tokens of no document may hold anything; a
+ * value that is not finite at a key which some queries see may reach the results of others of the same sequence.
+ * Gradients, of a scalar of which dy is the gradient with respect to y:
+ *   ds = p (dy.v - dy.y);  dq = scale sum_j ds z' k;  dk = scale sum_i ds z' q;  dv = sum_i p dy    (sums over the group's heads)
+ * p and ds are worked out in float32 and rounded to the tensors' type once, where they enter a product. */
+typedef struct {
+  int32_t dtype;                              /* CHM_BF16 or CHM_F16: type of all tensors */
+  int32_t causal;
+  int64_t batch, tokens, keys, heads, kv_heads;   /* heads a multiple of kv_heads; tokens and keys up to 2^30, tokens * heads / kv_heads below 2^31 - 2^13 */
+  int64_t dim;                                /* 1 to 128 */
+  const void *q, *k, *v;
+  int64_t q_stride[3], k_stride[3], v_stride[3];  /* elements from one sequence, token, head to the next; >= 0 */
+  float scale, cap;                           /* scale finite and > 0; cap finite and >= 0, 0: none */
+  const float *slopes;                        /* [heads], nullable */
+  int32_t index_bits;                         /* of the documents: 32 or 64 (signed) */
+  const void *q_documents, *k_documents;      /* [batch, tokens], [batch, keys], rows of ld; both or neither */
+  int64_t ld_q_documents, ld_k_documents;
+  const uint8_t *prefix;                      /* [batch, keys], rows of ld_prefix, 0 or not; nullable; causal only */
+  int64_t ld_prefix;
+  void *saved;                                /* what the backward pass wants (opaque, 16-byte aligned): written by the forward call, read by the
+                                                 backward call; NULL in a forward call: not kept */
+} chm_attention;
+
+typedef struct {
+  const void *dy, *y;                         /* [batch, tokens, heads, dim]; y: the forward call's result */
+  void *dq, *dk, *dv;                         /* shaped like q, k, v */
+  int64_t dy_stride[3], y_stride[3], dq_stride[3], dk_stride[3], dv_stride[3];
+} chm_attention_gradients;
+
+/* Bytes of `saved` and of the scratch of both calls (an input whose rows do not start on 16 bytes is packed into scratch).  g: nullable,
+ * then *backward_scratch is 0.  Host only.  Errors: CHM_ERR_ARG. */
+int chm_attention_sizes(const chm_attention *a, const chm_attention_gradients *g, uint64_t *saved, uint64_t *forward_scratch, uint64_t *backward_scratch);
+
+/* With up to 32 tokens times heads of a group it is bound by reading the keys and values, and runs on a kernel for that; few rows over many keys are
+ * split over the keys and joined.  Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
+int chm_attention_forward(const chm_attention *a, void *y, const int64_t y_stride[3], void *scratch, uint64_t scratch_bytes, void *hip_stream);
+int chm_attention_backward(const chm_attention *a, const chm_attention_gradients *g, void *scratch, uint64_t scratch_bytes, void *hip_stream);
 
 /* ---- Global gradient norm and clipping -----------------------------------------------------------------
  * norm = sqrt(sum over all tensors of g^2);  out = g * min(1, max_norm / (norm + 1e-6)).

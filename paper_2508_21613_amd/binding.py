@@ -21,7 +21,8 @@ SYMBOLS = ["chm_load_scenario", "chm_plan_space", "chm_score_plans", "chm_score_
            "chm_reroute_shape", "chm_transfer_plan", "chm_replan", "chm_replan_table", "chm_compare_objective", "chm_valu_probe", "chm_free_scenario",
            "chm_strerror",
            "chm_ffn_sizes", "chm_ffn_forward", "chm_ffn_backward", "chm_embedding_lookup", "chm_embedding_gradient_scratch", "chm_embedding_gradient",
-           "chm_load_gradients", "chm_gradient_sumsq", "chm_clip_gradients", "chm_free_gradients", "chm_ffn_selection"]
+           "chm_load_gradients", "chm_gradient_sumsq", "chm_clip_gradients", "chm_free_gradients", "chm_ffn_selection",
+           "chm_rotary_turn", "chm_attention_sizes", "chm_attention_forward", "chm_attention_backward", "chm_attention_selection"]
 
 
 class Desc(C.Structure):
@@ -114,6 +115,38 @@ class Gradient(C.Structure):
     _fields_ = [("grad", C.c_void_p), ("out", C.c_void_p), ("n", C.c_int64), ("dtype", C.c_int32)]
 
 
+class RotaryTurn(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("index_bits", C.c_int32), ("pairing", C.c_int32), ("axes", C.c_int32),
+                ("tokens", C.c_int64), ("heads", C.c_int64), ("head_dim", C.c_int32), ("pairs", C.c_int32),
+                ("x", C.c_void_p), ("out", C.c_void_p),
+                ("x_token", C.c_int64), ("x_head", C.c_int64), ("out_token", C.c_int64), ("out_head", C.c_int64),
+                ("positions", C.c_void_p), ("positions_axis", C.c_int64), ("positions_token", C.c_int64),
+                ("frequencies", C.c_void_p), ("axis", C.c_void_p)]
+
+
+Strides = C.c_int64 * 3
+
+
+class Attention(C.Structure):
+    _fields_ = [("dtype", C.c_int32), ("causal", C.c_int32),
+                ("batch", C.c_int64), ("tokens", C.c_int64), ("keys", C.c_int64), ("heads", C.c_int64), ("kv_heads", C.c_int64), ("dim", C.c_int64),
+                ("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p),
+                ("q_stride", Strides), ("k_stride", Strides), ("v_stride", Strides),
+                ("scale", C.c_float), ("cap", C.c_float), ("slopes", C.c_void_p),
+                ("index_bits", C.c_int32), ("q_documents", C.c_void_p), ("k_documents", C.c_void_p),
+                ("ld_q_documents", C.c_int64), ("ld_k_documents", C.c_int64),
+                ("prefix", C.c_void_p), ("ld_prefix", C.c_int64), ("saved", C.c_void_p)]
+
+
+class AttentionGradients(C.Structure):
+    _fields_ = [("dy", C.c_void_p), ("y", C.c_void_p), ("dq", C.c_void_p), ("dk", C.c_void_p), ("dv", C.c_void_p),
+                ("dy_stride", Strides), ("y_stride", Strides), ("dq_stride", Strides), ("dk_stride", Strides), ("dv_stride", Strides)]
+
+
+class AttentionKernels(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("few", "dim", "packed", "forward_rows", "dq_rows", "dkdv_keys", "forward_splits", "dkdv_splits")]
+
+
 class ChmError(RuntimeError):
     def __init__(self, code, msg=""):
         super().__init__("libchm error %d: %s" % (code, msg))
@@ -180,6 +213,11 @@ def lib():
         L.chm_clip_gradients.argtypes = [vp, C.c_float, vp, vp, vp]
         L.chm_free_gradients.argtypes = [vp]
         L.chm_free_gradients.restype = None
+        L.chm_rotary_turn.argtypes = [C.POINTER(RotaryTurn), i32, vp]
+        L.chm_attention_sizes.argtypes = [C.POINTER(Attention), C.POINTER(AttentionGradients), C.POINTER(u64), C.POINTER(u64), C.POINTER(u64)]
+        L.chm_attention_forward.argtypes = [C.POINTER(Attention), vp, Strides, vp, u64, vp]
+        L.chm_attention_backward.argtypes = [C.POINTER(Attention), C.POINTER(AttentionGradients), vp, u64, vp]
+        L.chm_attention_selection.argtypes = [C.POINTER(Attention), C.POINTER(AttentionGradients), C.POINTER(AttentionKernels)]
         L.chm_free_scenario.argtypes = [vp]
         L.chm_free_scenario.restype = None
         L.chm_strerror.argtypes = [C.c_int]

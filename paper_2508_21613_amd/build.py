@@ -26,9 +26,11 @@ HOST_SANITIZE = ["-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize
                  "-Xarch_host", "-g"]
 SOURCES = ["chm_host.cpp", "chm_pool.cpp", "chm_kernels.hip", "chm_fast.hip", "chm_search_s0.hip", "chm_search_s1.hip", "chm_search_s2.hip", "chm_families_8.hip",
            "chm_families_12.hip", "chm_families_16.hip", "chm_families_24.hip", "chm_window.hip", "chm_list.hip", "chm_replan.hip", "chm_probe.hip",
-           "chm_ffn.hip", "chm_ffn_bf16.hip", "chm_ffn_f16.hip", "chm_embedding.hip", "chm_clip.hip"]
+           "chm_ffn.hip", "chm_ffn_bf16.hip", "chm_ffn_f16.hip", "chm_embedding.hip", "chm_clip.hip", "chm_rotary.hip", "chm_attention.hip",
+           "chm_attention_forward_bf16.hip", "chm_attention_forward_f16.hip", "chm_attention_dq_bf16.hip", "chm_attention_dq_f16.hip",
+           "chm_attention_dkdv_bf16.hip", "chm_attention_dkdv_f16.hip"]
 # the operators of a training step: their values may be infinite or not a number, and pass through as such
-FLOAT_SOURCES = ("chm_ffn.hip", "chm_ffn_bf16.hip", "chm_ffn_f16.hip", "chm_embedding.hip", "chm_clip.hip")
+FLOAT_SOURCES = tuple(s for s in SOURCES if s.startswith(("chm_ffn", "chm_embedding", "chm_clip", "chm_rotary", "chm_attention")))
 NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
 # no device code of the search meets a NaN (NO_NANS): a maximum of floats is one instruction then, not one more for each operand
 # that might be one; packed-FP32 instruction selection is switched off for all device code; so is the vectorizer of straight-line code, which

@@ -1,0 +1,58 @@
+// Attention: what its host part (chm_attention.hip) hands to its kernels (chm_attention_kernels.h).  Internal to libchm.
+//
+// The query heads that share a key head (a group of G) are rows of one matrix: row r of (sequence, key head) is token r / G, head r % G of the
+// group.  A lane knows its row's token and slope, so nothing else changes, keys and values are read once a group, and a single token's heads fill the
+// rows of a matrix instruction.
+#ifndef CHM_ATTENTION_H
+#define CHM_ATTENTION_H
+#include <stdint.h>
+
+#include "../../include/chm_operators.h"
+
+// Elements of 16 bits; strides in elements.  Inputs: every row of `dim` starts on 16 bytes and dim is a multiple of 8 (others are packed first).
+struct AttnInput { const uint16_t *p; int64_t batch, token, head; };
+struct AttnOutput { uint16_t *p; int64_t batch, token, head; };
+
+// r / d for r below 2^31: the upper half of r m, shifted; d = 1: m = 0
+struct AttnDivide { uint32_t m; int32_t shift; };
+
+// What 64 tokens' documents are: the least and the largest number (first > last: none), and flags.  A document and "in the prefix" of a token
+// are one word: number * 2 + prefix; all ones: of none.
+struct AttnTile { int32_t first, last, flags, unused; };
+enum { ATTN_SOME_NONE = 1, ATTN_SOME_PREFIX = 2, ATTN_ALL_PREFIX = 4 };
+constexpr uint32_t ATTN_NONE = 0xffffffffu;
+constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles are laid out for whole ones
+
+struct AttnCall {
+  AttnInput q, k, v, dy;
+  AttnOutput y, dq, dk, dv;
+  int32_t batch, tokens, keys, kv_heads, group, dim, width;      // dim: elements of the inputs' rows; width: of the outputs' (dim less what packing added)
+  int32_t rows, rows_pad;                  // tokens * group, rounded up to whole tiles
+  int32_t offset;                          // keys - tokens: position of the first query
+  int32_t causal, tiles;                   // tiles of 64 keys
+  AttnDivide by_group;
+  float scale;                             // of the gradients dq and dk
+  float to2;                               // score in powers of two: scale * log2(e)
+  float tanh2, cap2;                       // 2 scale / cap * log2(e); cap * log2(e)
+  const float *slopes;                     // [kv_heads * group], or null
+  const uint32_t *q_words, *k_words;       // [batch][whole tiles], or null: no documents and no prefix
+  const AttnTile *q_tiles, *k_tiles;       // [batch][tiles]
+  int32_t q_tile_count;
+  float *lse, *delta;                      // [batch * kv_heads][rows_pad]: log2 of the sum of powers of two (+inf: the row sees nothing); dy . y
+  // sums split over workgroups: float32 parts, joined in order
+  int32_t splits;
+  float *part, *part2;                     // forward: [splits][batch * kv_heads][rows][width4] and (maximum, sum); backward: dk and dv [splits][batch * kv_heads][keys][width4]
+  int32_t width4;                          // width rounded up to 4
+  // layout of the launch
+  int32_t row_tiles, key_tiles, heads_abreast;
+};
+
+// Kernels of a pass.  tile: 0 or 1, 32 or 64 rows (keys) a wavefront.  false: HIP failed.
+struct AttnLaunch { int32_t dim, tile; uint32_t groups; void *stream; };
+bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);
+bool attn_forward_f16(const AttnCall &c, const AttnLaunch &l, bool few);
+bool attn_dq_bf16(const AttnCall &c, const AttnLaunch &l);
+bool attn_dq_f16(const AttnCall &c, const AttnLaunch &l);
+bool attn_dkdv_bf16(const AttnCall &c, const AttnLaunch &l);
+bool attn_dkdv_f16(const AttnCall &c, const AttnLaunch &l);
+#endif

@@ -1,0 +1,573 @@
+// Attention: what its passes consist of, the small kernels around the tiles (documents, packing, delta, joined sums), the entry points.
+//
+//   forward    [pack] [documents] tiles [join]
+//   backward   [pack] [documents] delta = dy.y, dq, dk and dv [join]
+// dq and dk with dv are kernels of their own, each of which works out the scores again: seven products in place of five, but no sums that several
+// workgroups add to, so that the same inputs give the same bits.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include <stdint.h>
+
+#include "../../include/chm_measure.h"
+#include "chm_attention.h"
+#include "chm_elements.h"
+#include "chm_strided.h"
+
+namespace {
+
+using namespace chm_elements;
+typedef float f4 __attribute__((ext_vector_type(4)));
+
+// ---------------------------------------------------------------------------------------------- documents
+struct DocumentsCall {
+  const char *documents;                  // or null: all of one
+  const uint8_t *prefix;                  // or null
+  int64_t ld_documents, ld_prefix;
+  uint32_t *words;
+  AttnTile *tiles;
+  int32_t n, index_bits, tiles_each;
+};
+// a wavefront for each tile of 64 tokens
+__global__ void __launch_bounds__(64) k_documents(DocumentsCall a, DocumentsCall b, int first) {
+  const bool second = (int)blockIdx.x >= first;
+  const DocumentsCall &c = second ? b : a;
+  const int block = blockIdx.x - (second ? first : 0), seq = block / c.tiles_each, tile = block - seq * c.tiles_each, t = tile * ATTN_TILE + threadIdx.x;
+  int64_t doc = -1;
+  bool pre = false;
+  if (t < c.n) {
+    const int64_t at = seq * c.ld_documents + t;
+    doc = !c.documents ? 0 : c.index_bits == 32 ? ((const int32_t *)c.documents)[at] : ((const int64_t *)c.documents)[at];
+    pre = c.prefix && c.prefix[seq * c.ld_prefix + t] != 0;
+  }
+  const bool some = doc >= 0 && doc < INT32_MAX;
+  const int64_t at = (int64_t)block * ATTN_TILE + threadIdx.x;
+  c.words[at] = some ? (uint32_t)doc * 2 + (pre ? 1 : 0) : ATTN_NONE;
+  int lo = some ? (int)doc : INT32_MAX, hi = some ? (int)doc : -1;
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    const int l = __shfl_xor(lo, d), h = __shfl_xor(hi, d);
+    lo = l < lo ? l : lo;
+    hi = h > hi ? h : hi;
+  }
+  const uint64_t none = __ballot(!some), yes = __ballot(some && pre);
+  if (threadIdx.x == 0)
+    c.tiles[block] = AttnTile{lo, hi, (none ? ATTN_SOME_NONE : 0) | (yes ? ATTN_SOME_PREFIX : 0) | (yes == ~0ull ? ATTN_ALL_PREFIX : 0), 0};
+}
+
+// ---------------------------------------------------------------------------------------------- packing
+struct PackCall {
+  struct { AttnInput in; uint16_t *out; int32_t tokens, heads; int64_t words; uint32_t groups; } m[4];
+  int32_t count, dim, dim8;
+};
+// rows of dim elements one behind the other, rounded up to whole words of 8, zeros behind
+__global__ void __launch_bounds__(256) k_pack(PackCall c) {
+  uint32_t g = blockIdx.x;
+  int i = 0;
+  while (i + 1 < c.count && g >= c.m[i].groups) g -= c.m[i++].groups;
+  const auto &m = c.m[i];
+  const int words = c.dim8 / 8;
+  const int64_t w = (int64_t)g * 256 + threadIdx.x;
+  if (w >= m.words) return;
+  int64_t row = w / words;
+  const int d = (int)(w - row * words) * 8;
+  const int64_t token = row / m.heads;
+  const int head = (int)(row - token * m.heads);
+  const int64_t seq = token / m.tokens;
+  const uint16_t *p = m.in.p + seq * m.in.batch + (token - seq * m.tokens) * m.in.token + head * m.in.head + d;
+  Words v{0, 0, 0, 0};
+  if (d + 8 <= c.dim) {
+    v = load16((const char *)p);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (d + e < c.dim) v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+  }
+  *(Words *)(m.out + w * 8) = v;
+}
+
+// ---------------------------------------------------------------------------------------------- delta
+// dy.y of every row, by 16 lanes a row
+struct DeltaCall {
+  AttnInput dy, y;
+  float *delta;
+  int32_t dim, tokens, heads, group, kv_heads, rows_pad;
+  int64_t all;
+};
+template <int DT>
+__global__ void __launch_bounds__(256) k_delta(DeltaCall c) {
+  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  const int d = (threadIdx.x & 15) * 8;
+  const int64_t token = row / c.heads, seq = token / c.tokens;
+  const int head = (int)(row - token * c.heads), t = (int)(token - seq * c.tokens);
+  float sum = 0.f;
+  if (row < c.all && d < c.dim) {
+    const char *a = (const char *)(c.dy.p + seq * c.dy.batch + t * c.dy.token + head * c.dy.head + d);
+    const char *b = (const char *)(c.y.p + seq * c.y.batch + t * c.y.token + head * c.y.head + d);
+    if (d + 8 <= c.dim) {
+      float v[8], w[8];
+      Lane<DT>::up(load16(a), v);
+      Lane<DT>::up(load16(b), w);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(v[e], w[e], sum);
+    } else {
+      for (int e = 0; d + e < c.dim; ++e) sum = fmaf(Lane<DT>::one(a + e * 2), Lane<DT>::one(b + e * 2), sum);
+    }
+  }
+#pragma unroll
+  for (int x = 8; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+  if (row < c.all && d == 0) {
+    const int h = head / c.group;
+    c.delta[(seq * c.kv_heads + h) * c.rows_pad + (int64_t)t * c.group + head - h * c.group] = sum;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------- joins
+template <int DT>
+__device__ __forceinline__ void put4(uint16_t *p, int d, int width, f4 v) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e)
+    if (d + e < width) Lane<DT>::put((char *)(p + d + e), v[e]);
+}
+
+// the parts of a row's softmax over the splits of its keys
+template <int DT>
+__global__ void __launch_bounds__(256) k_join_forward(const AttnCall c, int64_t all) {
+  const int words = c.width4 / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int64_t at = i / words, rows = (int64_t)c.batch * c.kv_heads * c.rows;
+  const int d = (int)(i - at * words) * 4;
+  float top = c.part2[at * 2];
+  for (int s = 1; s < c.splits; ++s) top = fmaxf(top, c.part2[(s * rows + at) * 2]);
+  float sum = 0.f;
+  f4 v{0.f, 0.f, 0.f, 0.f};
+  for (int s = 0; s < c.splits; ++s) {
+    const float f = __builtin_amdgcn_exp2f(c.part2[(s * rows + at) * 2] - top);
+    sum += c.part2[(s * rows + at) * 2 + 1] * f;
+    v += *(const f4 *)(c.part + (s * rows + at) * c.width4 + d) * f;
+  }
+  const int64_t hb = at / c.rows, b = hb / c.kv_heads;
+  const int h = (int)(hb - b * c.kv_heads), r = (int)(at - hb * c.rows), token = r / c.group, head = h * c.group + r - token * c.group;
+  if (c.lse && d == 0) c.lse[hb * c.rows_pad + r] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
+  put4<DT>(c.y.p + b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v * (sum == 0.f ? 0.f : 1.f / sum));
+}
+
+// dk and dv from the parts over the splits of the rows
+template <int DT>
+__global__ void __launch_bounds__(256) k_join_backward(const AttnCall c, int64_t all) {
+  const int words = c.width4 / 4;
+  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (i >= all) return;
+  const int64_t at = i / words, step = (int64_t)c.batch * c.kv_heads * c.keys * c.width4;
+  const int d = (int)(i - at * words) * 4;
+  f4 k{0.f, 0.f, 0.f, 0.f}, v = k;
+  for (int s = 0; s < c.splits; ++s) {
+    k += *(const f4 *)(c.part + s * step + at * c.width4 + d);
+    v += *(const f4 *)(c.part2 + s * step + at * c.width4 + d);
+  }
+  const int64_t hb = at / c.keys, b = hb / c.kv_heads, j = at - hb * c.keys;
+  const int h = (int)(hb - b * c.kv_heads);
+  put4<DT>(c.dk.p + b * c.dk.batch + j * c.dk.token + h * c.dk.head, d, c.width, k);
+  put4<DT>(c.dv.p + b * c.dv.batch + j * c.dv.token + h * c.dv.head, d, c.width, v);
+}
+
+// ---------------------------------------------------------------------------------------------- passes
+int64_t up(int64_t n, int64_t d) { return (n + d - 1) / d; }
+
+AttnDivide divide_by(int64_t d) {
+  if (d <= 1) return AttnDivide{0, 0};
+  int l = 0;
+  while ((1ll << l) < d) ++l;
+  return AttnDivide{(uint32_t)((1ull << (31 + l)) / (uint64_t)d + 1), l - 1};
+}
+
+// Hands out scratch, in a fixed order; with no base it only counts
+struct Arena {
+  char *base;
+  uint64_t used = 0;
+  void *take(uint64_t bytes) {
+    void *p = base ? base + used : nullptr;
+    used += (bytes + 255) & ~255ull;
+    return p;
+  }
+};
+
+constexpr int FEW_ROWS = 32;
+constexpr int64_t LENGTH_MAX = 1ll << 30, ROWS_MAX = INT32_MAX - (1 << 13);
+
+int64_t group_of(const chm_attention *a) { return a->heads / a->kv_heads; }
+int64_t rows_pad(const chm_attention *a) { return up(a->tokens * group_of(a), ATTN_TILE) * ATTN_TILE; }
+uint64_t saved_bytes(const chm_attention *a) { return (uint64_t)(a->batch * a->kv_heads * rows_pad(a)) * 4; }
+
+// the strides of dimensions of one element say nothing
+AttnInput input(const void *p, const int64_t s[3], int64_t b, int64_t t, int64_t h) {
+  return AttnInput{(const uint16_t *)p, b > 1 ? s[0] : 0, t > 1 ? s[1] : 0, h > 1 ? s[2] : 0};
+}
+AttnOutput output(void *p, const int64_t s[3], int64_t b, int64_t t, int64_t h) {
+  return AttnOutput{(uint16_t *)p, b > 1 ? s[0] : 0, t > 1 ? s[1] : 0, h > 1 ? s[2] : 0};
+}
+
+struct Pass {
+  const chm_attention *a;
+  Arena arena;
+  hipStream_t st;
+  bool run, ok = true;
+  bool fits = true;                        // every launch's threads can be counted in 32 bits
+  AttnCall c{};
+  chm_attention_kernels chosen{0, 0, 0, 0, 0, 0, 1, 1};
+
+  Pass(const chm_attention *a_, char *base, hipStream_t st_, bool run_) : a(a_), arena{base}, st(st_), run(run_) {
+    const int64_t G = group_of(a), d8 = up(a->dim, 8) * 8;
+    c.batch = (int32_t)a->batch;
+    c.tokens = (int32_t)a->tokens;
+    c.keys = (int32_t)a->keys;
+    c.kv_heads = (int32_t)a->kv_heads;
+    c.group = (int32_t)G;
+    c.dim = (int32_t)d8;
+    c.width = (int32_t)a->dim;
+    c.width4 = (int32_t)up(a->dim, 4) * 4;
+    c.rows = (int32_t)(a->tokens * G);
+    c.rows_pad = (int32_t)rows_pad(a);
+    c.offset = (int32_t)(a->keys - a->tokens);
+    c.causal = a->causal != 0;
+    c.tiles = (int32_t)up(a->keys, ATTN_TILE);
+    c.q_tile_count = (int32_t)up(a->tokens, ATTN_TILE);
+    c.by_group = divide_by(G);
+    const double log2e = 1.4426950408889634;
+    c.scale = a->scale;
+    c.to2 = (float)(a->scale * log2e);
+    if (a->cap > 0) {
+      c.tanh2 = (float)(2 * log2e * a->scale / a->cap);
+      c.cap2 = (float)(a->cap * log2e);
+    }
+    c.slopes = a->slopes;
+    c.lse = (float *)a->saved;
+    c.q = input(a->q, a->q_stride, a->batch, a->tokens, a->heads);
+    c.k = input(a->k, a->k_stride, a->batch, a->keys, a->kv_heads);
+    c.v = input(a->v, a->v_stride, a->batch, a->keys, a->kv_heads);
+    chosen.dim = d8 <= 64 ? 64 : 128;
+    c.heads_abreast = heads() % 8 == 0 ? 8 : (int32_t)heads();
+  }
+  int64_t heads() const { return a->batch * a->kv_heads; }
+  int64_t rows() const { return a->tokens * group_of(a); }
+  bool bf16() const { return a->dtype == CHM_BF16; }
+
+  uint32_t threads(int64_t groups, int64_t each) {
+    fits = fits && groups * each <= UINT32_MAX;
+    return (uint32_t)groups;
+  }
+
+  // Inputs as the tiles take them: 16-byte rows, and 64 of them within offsets of 31 bits
+  PackCall pack{};
+  void packed(AttnInput &in, int64_t tokens, int64_t heads, int64_t group, int bit) {
+    const int64_t across = group == 1 ? 63 : 63 / group + 1;
+    const bool reach = 2 * (across * in.token + (group - 1) * in.head + 128) < (1ll << 31) - 256;
+    if ((uintptr_t)in.p % 16 == 0 && a->dim % 8 == 0 && in.batch % 8 == 0 && in.token % 8 == 0 && in.head % 8 == 0 && reach) return;
+    chosen.packed |= bit;
+    const int64_t d8 = c.dim, words = a->batch * tokens * heads * (d8 / 8);
+    auto &m = pack.m[pack.count++];
+    m.in = in;
+    m.out = (uint16_t *)arena.take((uint64_t)words * 16);
+    m.tokens = (int32_t)tokens;
+    m.heads = (int32_t)heads;
+    m.words = words;
+    m.groups = (uint32_t)up(words, 256);
+    fits = fits && up(words, 256) < (1ll << 30);
+    in = AttnInput{m.out, tokens * heads * d8, heads * d8, d8};
+  }
+  void inputs(const chm_attention_gradients *g) {
+    packed(c.q, a->tokens, a->heads, group_of(a), 1);
+    packed(c.k, a->keys, a->kv_heads, 1, 2);
+    packed(c.v, a->keys, a->kv_heads, 1, 4);
+    if (g) packed(c.dy, a->tokens, a->heads, group_of(a), 8);
+    pack.dim = (int32_t)a->dim;
+    pack.dim8 = c.dim;
+    if (pack.count) {
+      int64_t groups = 0;
+      for (int i = 0; i < pack.count; ++i) groups += pack.m[i].groups;
+      const uint32_t n = threads(groups, 256);
+      if (run && fits && n) {
+        hipLaunchKernelGGL(k_pack, dim3(n), dim3(256), 0, st, pack);
+        ok = ok && hipGetLastError() == hipSuccess;
+      }
+    }
+    if (!a->k_documents && !a->prefix) return;
+    DocumentsCall kd{(const char *)a->k_documents, a->prefix, a->ld_k_documents, a->ld_prefix, nullptr, nullptr, c.keys, a->index_bits, c.tiles};
+    DocumentsCall qd{(const char *)a->q_documents, nullptr, a->ld_q_documents, 0, nullptr, nullptr, c.tokens, a->index_bits, c.q_tile_count};
+    const auto room = [&](DocumentsCall &d) {
+      d.words = (uint32_t *)arena.take((uint64_t)a->batch * d.tiles_each * ATTN_TILE * 4);
+      d.tiles = (AttnTile *)arena.take((uint64_t)a->batch * d.tiles_each * sizeof(AttnTile));
+    };
+    room(kd);
+    // the queries' tokens are the keys': their words are (the prefix is asked of keys alone)
+    const bool same = a->tokens == a->keys && a->q_documents == a->k_documents && (a->batch == 1 || a->ld_q_documents == a->ld_k_documents);
+    if (same) qd.words = kd.words, qd.tiles = kd.tiles;
+    else room(qd);
+    c.k_words = kd.words; c.k_tiles = kd.tiles;
+    c.q_words = qd.words; c.q_tiles = qd.tiles;
+    if (!run) {                            // only whether there are any is asked
+      c.k_words = c.q_words = (const uint32_t *)1;
+    }
+    const int64_t first = a->batch * kd.tiles_each, all = first + (same ? 0 : a->batch * qd.tiles_each);
+    const uint32_t n = threads(all, 64);
+    if (run && fits && n) {
+      hipLaunchKernelGGL(k_documents, dim3(n), dim3(64), 0, st, kd, qd, (int)first);
+      ok = ok && hipGetLastError() == hipSuccess;
+    }
+  }
+
+  // Parts of the keys of the kernel for few rows: as many workgroups as run at once (1 a compute unit, 2 with rows of 64), in whole rounds
+  static int few_splits(int64_t heads, int64_t tiles, int dim) {
+    const int64_t slots = dim == 64 ? 512 : 256;
+    int best = 1;
+    double least = 1e30;
+    for (int64_t s = 1; s <= 64 && (s == 1 || s * 4 <= tiles); ++s) {
+      const double cost = (double)up(heads * s, slots) / s + 0.002 * s;
+      if (cost < least) least = cost, best = (int)s;
+    }
+    return best;
+  }
+  // Parts of the sums of a tile kernel with `groups` workgroups, each of which goes through `steps` of 64: as many as fill `slots`, of 8 steps and more
+  static int tile_splits(int64_t groups, int64_t steps, int64_t slots) {
+    int64_t s = slots / (groups < 1 ? 1 : groups);
+    if (s > steps / 8) s = steps / 8;
+    return (int)(s < 1 ? 1 : s < 16 ? s : 16);
+  }
+
+  void forward(void *y, const int64_t y_stride[3]) {
+    c.y = output(y, y_stride, a->batch, a->tokens, a->heads);
+    if (a->batch == 0 || a->tokens == 0) return;
+    inputs(nullptr);
+    chosen.few = rows() <= FEW_ROWS;
+    AttnLaunch l{chosen.dim, 0, 0, st};
+    if (chosen.few) {
+      chosen.forward_rows = FEW_ROWS;
+      c.splits = few_splits(heads(), c.tiles, chosen.dim);
+      l.groups = threads(heads() * c.splits, 256);
+    } else {
+      chosen.forward_rows = 128;
+      c.row_tiles = (int32_t)up(rows(), chosen.forward_rows);
+      c.splits = tile_splits(heads() * c.row_tiles, c.tiles, 512);
+      l.groups = threads(heads() * c.row_tiles * c.splits, 256);
+    }
+    chosen.forward_splits = c.splits;
+    const int64_t all = heads() * rows();
+    if (c.splits > 1) {
+      c.part = (float *)arena.take((uint64_t)(c.splits * all * c.width4) * 4);
+      c.part2 = (float *)arena.take((uint64_t)(c.splits * all * 2) * 4);
+    }
+    const uint32_t joins = threads(up(all * (c.width4 / 4), 256), 256);
+    if (!run || !fits) return;
+    ok = ok && (bf16() ? attn_forward_bf16 : attn_forward_f16)(c, l, chosen.few);
+    if (c.splits > 1) {
+      if (bf16()) hipLaunchKernelGGL(k_join_forward<CHM_BF16>, dim3(joins), dim3(256), 0, st, c, all * (c.width4 / 4));
+      else hipLaunchKernelGGL(k_join_forward<CHM_F16>, dim3(joins), dim3(256), 0, st, c, all * (c.width4 / 4));
+      ok = ok && hipGetLastError() == hipSuccess;
+    }
+  }
+
+  void backward(const chm_attention_gradients *g) {
+    if (a->batch == 0) return;
+    const int64_t B = a->batch, T = a->tokens, K = a->keys;
+    c.dy = input(g->dy, g->dy_stride, B, T, a->heads);
+    const AttnInput dy = c.dy, y = input(g->y, g->y_stride, B, T, a->heads);
+    c.dq = output(g->dq, g->dq_stride, B, T, a->heads);
+    c.dk = output(g->dk, g->dk_stride, B, K, a->kv_heads);
+    c.dv = output(g->dv, g->dv_stride, B, K, a->kv_heads);
+    inputs(g);
+    c.delta = (float *)arena.take(saved_bytes(a));
+    const int64_t all = B * T * a->heads;
+    const uint32_t deltas = threads(up(all, 16), 256);
+    if (run && fits && deltas) {
+      DeltaCall d{dy, y, c.delta, (int32_t)a->dim, c.tokens, (int32_t)a->heads, c.group, c.kv_heads, c.rows_pad, all};
+      if (bf16()) hipLaunchKernelGGL(k_delta<CHM_BF16>, dim3(deltas), dim3(256), 0, st, d);
+      else hipLaunchKernelGGL(k_delta<CHM_F16>, dim3(deltas), dim3(256), 0, st, d);
+      ok = ok && hipGetLastError() == hipSuccess;
+    }
+    if (T > 0) {
+      chosen.dq_rows = 128;
+      c.row_tiles = (int32_t)up(rows(), chosen.dq_rows);
+      c.splits = 1;
+      const AttnLaunch l{chosen.dim, 0, threads(heads() * c.row_tiles, 256), st};
+      if (run && fits) ok = ok && (bf16() ? attn_dq_bf16 : attn_dq_f16)(c, l);
+    }
+    if (K > 0) {
+      chosen.dkdv_keys = 128;
+      c.key_tiles = (int32_t)up(K, chosen.dkdv_keys);
+      c.splits = tile_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), 512);
+      chosen.dkdv_splits = c.splits;
+      const int64_t words = heads() * K * (c.width4 / 4);
+      if (c.splits > 1) {
+        c.part = (float *)arena.take((uint64_t)(c.splits * words) * 16);
+        c.part2 = (float *)arena.take((uint64_t)(c.splits * words) * 16);
+      }
+      const AttnLaunch l{chosen.dim, 0, threads(heads() * c.key_tiles * c.splits, 256), st};
+      const uint32_t joins = threads(up(words, 256), 256);
+      if (!run || !fits) return;
+      ok = ok && (bf16() ? attn_dkdv_bf16 : attn_dkdv_f16)(c, l);
+      if (c.splits > 1) {
+        if (bf16()) hipLaunchKernelGGL(k_join_backward<CHM_BF16>, dim3(joins), dim3(256), 0, st, c, words);
+        else hipLaunchKernelGGL(k_join_backward<CHM_F16>, dim3(joins), dim3(256), 0, st, c, words);
+        ok = ok && hipGetLastError() == hipSuccess;
+      }
+    }
+  }
+};
+
+bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
+// strides that are no negative ones and whose ends can be counted in bytes
+bool fine(const int64_t s[3], int64_t b, int64_t t, int64_t h) {
+  const int64_t n[3] = {b, t, h};
+  for (int i = 0; i < 3; ++i)
+    if (s[i] < 0 || (n[i] > 1 && s[i] > (1ll << 60) / n[i])) return false;
+  return true;
+}
+
+int check(const chm_attention *a) {
+  if (!a || (a->dtype != CHM_BF16 && a->dtype != CHM_F16)) return CHM_ERR_ARG;
+  if (a->batch < 0 || a->batch > INT32_MAX || a->tokens < 0 || a->tokens > LENGTH_MAX || a->keys < 0 || a->keys > LENGTH_MAX) return CHM_ERR_ARG;
+  if (a->kv_heads < 1 || a->kv_heads > (1 << 20) || a->heads < a->kv_heads || a->heads > (1 << 20) || a->heads % a->kv_heads || a->dim < 1 || a->dim > 128) return CHM_ERR_ARG;
+  if (a->tokens * group_of(a) > ROWS_MAX || a->batch * a->kv_heads > INT32_MAX) return CHM_ERR_ARG;
+  if (a->batch * a->kv_heads > 0 && rows_pad(a) > (1ll << 50) / (a->batch * a->kv_heads)) return CHM_ERR_ARG;
+  if (!(a->scale > 0) || !isfinite(a->scale) || !(a->cap >= 0) || !isfinite(a->cap)) return CHM_ERR_ARG;
+  if (!fine(a->q_stride, a->batch, a->tokens, a->heads) || !fine(a->k_stride, a->batch, a->keys, a->kv_heads) ||
+      !fine(a->v_stride, a->batch, a->keys, a->kv_heads)) return CHM_ERR_ARG;
+  if (!aligned(a->q, 2) || !aligned(a->k, 2) || !aligned(a->v, 2) || !aligned(a->saved, 16) || !aligned(a->slopes, 4)) return CHM_ERR_ARG;
+  if (!a->q_documents != !a->k_documents || (a->prefix && !a->causal)) return CHM_ERR_ARG;
+  if (a->k_documents) {
+    if (a->index_bits != 32 && a->index_bits != 64) return CHM_ERR_ARG;
+    if (!aligned(a->q_documents, a->index_bits / 8) || !aligned(a->k_documents, a->index_bits / 8)) return CHM_ERR_ARG;
+    if (a->batch > 1 && (a->ld_q_documents < 0 || a->ld_k_documents < 0)) return CHM_ERR_ARG;
+  }
+  if (a->prefix && a->batch > 1 && a->ld_prefix < 0) return CHM_ERR_ARG;
+  return CHM_OK;
+}
+
+int check_gradients(const chm_attention *a, const chm_attention_gradients *g) {
+  if (!g || !fine(g->dy_stride, a->batch, a->tokens, a->heads) || !fine(g->y_stride, a->batch, a->tokens, a->heads) ||
+      !fine(g->dq_stride, a->batch, a->tokens, a->heads) || !fine(g->dk_stride, a->batch, a->keys, a->kv_heads) ||
+      !fine(g->dv_stride, a->batch, a->keys, a->kv_heads)) return CHM_ERR_ARG;
+  if (!aligned(g->dy, 2) || !aligned(g->y, 2) || !aligned(g->dq, 2) || !aligned(g->dk, 2) || !aligned(g->dv, 2)) return CHM_ERR_ARG;
+  return CHM_OK;
+}
+
+using chm_strided::Dim;
+using chm_strided::Tensor;
+Tensor tensor(const chm_attention *a, const void *p, const int64_t s[3], int64_t tokens, int64_t heads) {
+  return Tensor(p, a->dim, 2, {Dim{a->batch, s[0]}, Dim{tokens, s[1]}, Dim{heads, s[2]}});
+}
+Tensor bytes(const void *p, uint64_t n) { return Tensor(p, (int64_t)n, 1, {Dim{1, 0}, Dim{1, 0}, Dim{1, 0}}); }
+Tensor rows(const void *p, int64_t n, int64_t width, int64_t ld, int size) { return Tensor(p, width, size, {Dim{n, ld}, Dim{1, 0}, Dim{1, 0}}); }
+
+// whether one of the results lies over another one, over itself, or over an input
+template <int R, int I>
+bool clash(const Tensor (&results)[R], const Tensor (&inputs)[I]) {
+  for (int r = 0; r < R; ++r) {
+    if (!results[r].apart()) return true;
+    for (int i = 0; i < I; ++i)
+      if (chm_strided::share(results[r], inputs[i])) return true;
+    for (int o = 0; o < r; ++o)
+      if (chm_strided::share(results[r], results[o])) return true;
+  }
+  return false;
+}
+
+bool clash_forward(const chm_attention *a, void *y, const int64_t s[3], void *scratch, uint64_t scratch_bytes) {
+  const Tensor results[] = {tensor(a, y, s, a->tokens, a->heads), bytes(a->saved, a->saved ? saved_bytes(a) : 0), bytes(scratch, scratch_bytes)};
+  const Tensor inputs[] = {tensor(a, a->q, a->q_stride, a->tokens, a->heads), tensor(a, a->k, a->k_stride, a->keys, a->kv_heads),
+                           tensor(a, a->v, a->v_stride, a->keys, a->kv_heads), bytes(a->slopes, a->slopes ? a->heads * 4 : 0),
+                           rows(a->q_documents, a->batch, a->tokens, a->ld_q_documents, a->index_bits / 8),
+                           rows(a->k_documents, a->batch, a->keys, a->ld_k_documents, a->index_bits / 8), rows(a->prefix, a->batch, a->keys, a->ld_prefix, 1)};
+  return clash(results, inputs);
+}
+
+bool clash_backward(const chm_attention *a, const chm_attention_gradients *g, void *scratch, uint64_t scratch_bytes) {
+  const Tensor results[] = {tensor(a, g->dq, g->dq_stride, a->tokens, a->heads), tensor(a, g->dk, g->dk_stride, a->keys, a->kv_heads),
+                            tensor(a, g->dv, g->dv_stride, a->keys, a->kv_heads), bytes(scratch, scratch_bytes)};
+  const Tensor inputs[] = {tensor(a, a->q, a->q_stride, a->tokens, a->heads), tensor(a, a->k, a->k_stride, a->keys, a->kv_heads),
+                           tensor(a, a->v, a->v_stride, a->keys, a->kv_heads), tensor(a, g->dy, g->dy_stride, a->tokens, a->heads),
+                           tensor(a, g->y, g->y_stride, a->tokens, a->heads), bytes(a->saved, saved_bytes(a)), bytes(a->slopes, a->slopes ? a->heads * 4 : 0),
+                           rows(a->q_documents, a->batch, a->tokens, a->ld_q_documents, a->index_bits / 8),
+                           rows(a->k_documents, a->batch, a->keys, a->ld_k_documents, a->index_bits / 8), rows(a->prefix, a->batch, a->keys, a->ld_prefix, 1)};
+  return clash(results, inputs);
+}
+
+const int64_t ANY[3] = {0, 0, 0};
+
+}  // namespace
+
+extern "C" int chm_attention_sizes(const chm_attention *a, const chm_attention_gradients *g, uint64_t *saved, uint64_t *forward_scratch, uint64_t *backward_scratch) {
+  const int rc = check(a);
+  if (rc != CHM_OK) return rc;
+  if (g && check_gradients(a, g) != CHM_OK) return CHM_ERR_ARG;
+  if (saved) *saved = saved_bytes(a);
+  if (forward_scratch) {
+    Pass p(a, nullptr, nullptr, false);
+    p.forward(nullptr, ANY);
+    if (!p.fits) return CHM_ERR_ARG;
+    *forward_scratch = p.arena.used;
+  }
+  if (backward_scratch) {
+    *backward_scratch = 0;
+    if (!g) return CHM_OK;
+    Pass p(a, nullptr, nullptr, false);
+    p.backward(g);
+    if (!p.fits) return CHM_ERR_ARG;
+    *backward_scratch = p.arena.used;
+  }
+  return CHM_OK;
+}
+
+extern "C" int chm_attention_selection(const chm_attention *a, const chm_attention_gradients *g, chm_attention_kernels *out) {
+  if (!out || check(a) != CHM_OK || (g && check_gradients(a, g) != CHM_OK)) return CHM_ERR_ARG;
+  Pass p(a, nullptr, nullptr, false);
+  p.forward(nullptr, ANY);
+  if (!p.fits) return CHM_ERR_ARG;
+  *out = p.chosen;
+  if (g) {
+    Pass b(a, nullptr, nullptr, false);
+    b.backward(g);
+    if (!b.fits) return CHM_ERR_ARG;
+    out->packed = b.chosen.packed;
+    out->dq_rows = b.chosen.dq_rows;
+    out->dkdv_keys = b.chosen.dkdv_keys;
+    out->dkdv_splits = b.chosen.dkdv_splits;
+  }
+  return CHM_OK;
+}
+
+extern "C" int chm_attention_forward(const chm_attention *a, void *y, const int64_t y_stride[3], void *scratch, uint64_t scratch_bytes, void *hip_stream) {
+  const int rc = check(a);
+  if (rc != CHM_OK) return rc;
+  if (!y_stride || !fine(y_stride, a->batch, a->tokens, a->heads) || !aligned(y, 2) || !aligned(scratch, 16)) return CHM_ERR_ARG;
+  if (a->batch == 0 || a->tokens == 0) return CHM_OK;
+  if (!a->q || !y || (a->keys > 0 && (!a->k || !a->v))) return CHM_ERR_ARG;
+  Pass need(a, nullptr, nullptr, false);
+  need.forward(y, y_stride);
+  if (!need.fits) return CHM_ERR_ARG;
+  if (need.arena.used && !scratch) return CHM_ERR_ARG;
+  if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  if (clash_forward(a, y, y_stride, scratch, need.arena.used)) return CHM_ERR_ARG;
+  Pass p(a, (char *)scratch, (hipStream_t)hip_stream, true);
+  p.forward(y, y_stride);
+  return p.ok ? CHM_OK : CHM_ERR_HIP;
+}
+
+extern "C" int chm_attention_backward(const chm_attention *a, const chm_attention_gradients *g, void *scratch, uint64_t scratch_bytes, void *hip_stream) {
+  int rc = check(a);
+  if (rc == CHM_OK) rc = check_gradients(a, g);
+  if (rc != CHM_OK) return rc;
+  if (!aligned(scratch, 16)) return CHM_ERR_ARG;
+  if (a->batch == 0 || (a->tokens == 0 && a->keys == 0)) return CHM_OK;
+  if (a->tokens > 0 && (!a->q || !g->dy || !g->y || !g->dq || !a->saved)) return CHM_ERR_ARG;
+  if (a->keys > 0 && (!a->k || !a->v || !g->dk || !g->dv)) return CHM_ERR_ARG;
+  Pass need(a, nullptr, nullptr, false);
+  need.backward(g);
+  if (!need.fits) return CHM_ERR_ARG;
+  if (need.arena.used && !scratch) return CHM_ERR_ARG;
+  if (scratch_bytes < need.arena.used) return CHM_ERR_LIMIT;
+  if (clash_backward(a, g, scratch, need.arena.used)) return CHM_ERR_ARG;
+  Pass p(a, (char *)scratch, (hipStream_t)hip_stream, true);
+  p.backward(g);
+  return p.ok ? CHM_OK : CHM_ERR_HIP;
+}

@@ -1,13 +1,14 @@
 """Operators of a pipeline stage's training step, over torch tensors: the calls of include/chm_operators.h.
 
-The gated feed-forward block forward and backward, the embedding's lookup and gradient, the global gradient norm with clipping.
+The gated feed-forward block forward and backward, the embedding's lookup and gradient, rotary positions, attention forward and backward, the
+global gradient norm with clipping.
 As everywhere in this package torch provides device memory and streams; every value is computed by the library's HIP kernels, and
 without a usable GPU the calls fail.  A call works on the current stream, or on `stream`; scratch and results that the caller does
 not hand in are allocated on that stream.  Inputs must be ready there, as with any torch call.  Results must not lie over inputs or each
 other (ffn_forward's may lie over x).  Wrong arguments raise binding.ChmError with the library's code.
 
 Results are no part of autograd's graph; the gradients are calls of their own.  While torch records gradients, inputs that require one are
-taken only where the caller asks for what the gradient's call wants (ffn_forward with save=True): anything else would lose it without a word.
+taken only where the caller asks for what the gradient's call wants (ffn_forward and attention_forward with save=True): anything else would lose it without a word.
 """
 import ctypes as C
 import math
@@ -97,7 +98,7 @@ def _scope(stream, device, *tensors):
 def _unrecorded(*tensors):
     if any([t.requires_grad for t in tensors]) and torch.is_grad_enabled():
         raise B.ChmError(B.ERR_ARG, "the result would carry no gradient to inputs that require one: call under torch.no_grad() and take the "
-                                    "gradients from ffn_backward and embedding_gradient")
+                                    "gradients from ffn_backward, embedding_gradient, Rotary.gradient and attention_backward")
 
 
 def _bytes(n, like):
@@ -229,6 +230,192 @@ def embedding_gradient(dy, tokens, rows=None, scale=1.0, out=None, accumulate=Fa
         ws = _bytes(scratch.value, dy)
         B._check(lib.chm_embedding_gradient(DTYPES[dtype], DTYPES[grad_dtype], bits, tokens.data_ptr(), n, dy.data_ptr(), ld, rows, width,
                                             scale, out.data_ptr(), ld_out, 1 if accumulate else 0, ws.data_ptr(), scratch, st))
+    return out
+
+
+PAIRINGS = {"halves": 0, "neighbours": 1}
+
+
+def _strided(name, t, shape, dtype, device):
+    """checks a tensor of that many dimensions (sizes of None: any) whose last one has unit stride"""
+    if not isinstance(t, torch.Tensor):
+        raise B.ChmError(B.ERR_ARG, name + " must be a tensor")
+    if t.dim() != len(shape) or any([want is not None and n != want for n, want in zip(t.shape, shape)]):
+        raise B.ChmError(B.ERR_ARG, "%s must be %s, is %s" % (name, " x ".join(["any" if n is None else str(n) for n in shape]), list(t.shape)))
+    if not t.is_cuda or (device is not None and t.get_device() != device):
+        raise B.ChmError(B.ERR_ARG, name + " must be on the GPU, the same as the others")
+    if dtype is not None and t.dtype != dtype:
+        raise B.ChmError(B.ERR_ARG, "%s must be %s" % (name, dtype))
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise B.ChmError(B.ERR_ARG, name + " must have unit stride along its last dimension")
+    return t
+
+
+class Rotary:
+    """Rotary positions of one or several axes: the description of chm_rotary_turn, made once for a model.
+
+    `sections`: how many pairs each axis turns, one axis behind the other ([64] for text; [16, 24, 24] for time, height and width), or `axes`:
+    the axis of every pair, in any order.  Neither: all pairs by one axis.  `frequencies`: radians a position of every pair; without them
+    base ** (-i / pairs) for pair i.  `pairing`: "halves" (elements i and i + pairs of a head) or "neighbours" (2 i and 2 i + 1).  Elements behind
+    the pairs are copied."""
+
+    def __init__(self, head_dim, sections=None, axes=None, frequencies=None, base=10000.0, pairing="halves"):
+        _need(isinstance(head_dim, int) and 2 <= head_dim <= 1 << 20, "head_dim must be a whole number from 2 to 2^20")
+        _need(pairing in PAIRINGS, "pairing must be halves or neighbours")
+        _need(sections is None or axes is None, "sections or axes, not both")
+        if sections is not None:
+            sections = list(sections)
+            _need(sections and all(isinstance(n, int) and n >= 0 for n in sections), "sections must be whole numbers")
+            axes = [a for a, n in enumerate(sections) for _ in range(n)]
+        elif axes is None:
+            axes = [0] * (len(list(frequencies)) if frequencies is not None else head_dim // 2)
+        axes = list(axes)
+        _need(all(isinstance(a, int) and 0 <= a < 256 for a in axes), "axes must be whole numbers from 0 to 255")
+        pairs = len(axes)
+        _need(1 <= pairs <= 128 and 2 * pairs <= head_dim, "there must be 1 to 128 pairs, twice as many elements of a head at least")
+        if frequencies is None:
+            base = float(base)
+            _need(base > 0 and math.isfinite(base), "base must be positive")
+            frequencies = [base ** (-i / pairs) for i in range(pairs)]
+        frequencies = [float(f) for f in frequencies]
+        _need(len(frequencies) == pairs and all(math.isfinite(f) for f in frequencies), "frequencies must be a finite number for each pair")
+        self.head_dim, self.pairs, self.axes = head_dim, pairs, len(sections) if sections is not None else max(axes) + 1
+        self._frequencies, self._axis = (C.c_double * pairs)(*frequencies), (C.c_int32 * pairs)(*axes)
+        self._pairing = PAIRINGS[pairing]
+
+    def _turn(self, name, x, positions, backwards, out, stream):
+        _strided(name, x, (None, None, self.head_dim), None, None)
+        dtype, dev = x.dtype, x.get_device()
+        _need(dtype in DTYPES, name + " must be float32, bfloat16 or float16")
+        n, heads = x.shape[0], x.shape[1]
+        _need(isinstance(positions, torch.Tensor) and positions.is_cuda and positions.get_device() == dev, "positions must be on the same GPU as the others")
+        _need(positions.dtype in INDEX_BITS, "positions must be int32 or int64")
+        if positions.dim() == 1 and self.axes == 1:
+            positions = positions[None]
+        _need(tuple(positions.shape) == (self.axes, n), "positions must be %d x %d (axes x tokens)" % (self.axes, n))
+        if out is not None:
+            _strided("out", out, (n, heads, self.head_dim), dtype, dev)
+        _unrecorded(x)
+        with _scope(stream, dev, x, positions, out) as st:
+            if out is None:
+                out = x.new_empty((n, heads, self.head_dim))
+            d = B.RotaryTurn(DTYPES[dtype], INDEX_BITS[positions.dtype], self._pairing, self.axes, n, heads, self.head_dim, self.pairs, x.data_ptr(),
+                             out.data_ptr(), x.stride(0), x.stride(1), out.stride(0), out.stride(1), positions.data_ptr(), positions.stride(0),
+                             positions.stride(1), C.addressof(self._frequencies), C.addressof(self._axis))
+            B._check(B.lib().chm_rotary_turn(d, backwards, st))
+        return out
+
+    def rotate(self, x, positions, out=None, stream=None):
+        """x [tokens, heads, head_dim] (queries, keys, or both side by side; any strides) turned by positions [axes, tokens] (or [tokens] for one
+        axis), whole numbers of either sign.  `out` may be x."""
+        return self._turn("x", x, positions, 0, out, stream)
+
+    def gradient(self, dy, positions, out=None, stream=None):
+        """the gradient of x for dy, that of rotate's result.  `out` may be dy."""
+        return self._turn("dy", dy, positions, 1, out, stream)
+
+
+def _strides(t):
+    return t.stride()[:3]
+
+
+def _attention(q, k, v, scale, cap, slopes, causal, documents, prefix):
+    """the call's description, its GPU, and the tensors it points to"""
+    _strided("q", q, (None, None, None, None), None, None)
+    dtype, dev = q.dtype, q.get_device()
+    _need(dtype in (torch.bfloat16, torch.float16), "q must be bfloat16 or float16")
+    batch, tokens, heads, dim = q.shape
+    _strided("k", k, (batch, None, None, dim), dtype, dev)
+    keys, kv_heads = k.shape[1], k.shape[2]
+    _strided("v", v, (batch, keys, kv_heads, dim), dtype, dev)
+    _need(kv_heads > 0 and heads > 0 and heads % kv_heads == 0, "the heads of q must be a multiple of those of k and v")
+    _need(1 <= dim <= 128, "heads must have 1 to 128 elements")
+    scale = dim ** -0.5 if scale is None else float(scale)
+    cap = float(cap)
+    _need(scale > 0 and math.isfinite(scale), "scale must be positive")
+    _need(cap >= 0 and math.isfinite(cap), "cap must not be negative")
+    d = B.Attention(DTYPES[dtype], 1 if causal else 0, batch, tokens, keys, heads, kv_heads, dim, q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                    _strides(q), _strides(k), _strides(v), scale, cap)
+    held = [q, k, v]
+    if slopes is not None:
+        _need(isinstance(slopes, torch.Tensor) and slopes.is_cuda and slopes.get_device() == dev and slopes.dtype == torch.float32 and
+              tuple(slopes.shape) == (heads,) and slopes.is_contiguous(), "slopes must be a float32 for each head, on the same GPU")
+        _need(not slopes.requires_grad, "slopes are constants: they get no gradient")
+        d.slopes = slopes.data_ptr()
+        held.append(slopes)
+    if documents is not None:
+        pair = tuple(documents) if isinstance(documents, (tuple, list)) else (documents, documents)
+        _need(len(pair) == 2, "documents must be one tensor, or one for the queries and one for the keys")
+        for name, t, n in (("q", pair[0], tokens), ("k", pair[1], keys)):
+            _strided(name + "'s documents", t, (batch, n), None, dev)
+            _need(t.dtype in INDEX_BITS and t.dtype == pair[0].dtype, "documents must be int32 or int64")
+        d.index_bits = INDEX_BITS[pair[0].dtype]
+        d.q_documents, d.k_documents = pair[0].data_ptr(), pair[1].data_ptr()
+        d.ld_q_documents, d.ld_k_documents = pair[0].stride(0), pair[1].stride(0)
+        # a tensor of no elements has no address, and a query needs its document
+        _need(tokens == 0 or batch == 0 or keys > 0, "documents need keys")
+        held += pair
+    if prefix is not None:
+        _need(causal, "a prefix is what a causal mask leaves visible: it needs causal")
+        _strided("prefix", prefix, (batch, keys), None, dev)
+        _need(prefix.dtype in (torch.bool, torch.uint8), "prefix must be bool or uint8")
+        d.prefix, d.ld_prefix = prefix.data_ptr(), prefix.stride(0)
+        held.append(prefix)
+    return d, dev, held
+
+
+def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None, save=False, out=None, stream=None):
+    """chm_attention_forward: y [batch, tokens, heads, dim] for q of that shape and k, v [batch, keys, kv_heads, dim], all bfloat16 or all float16, any
+    strides; query head h reads key head h // (heads // kv_heads).  Scores are scale q.k (scale: dim ** -0.5), capped to
+    cap tanh(. / cap) where cap > 0, less slopes[head] times the distance (slopes: float32 [heads]).
+
+    Query i stands at position i + keys - tokens.  It sees the keys of its document (documents: whole numbers [batch, tokens], or a pair of them for
+    queries and keys; outside [0, 2^31 - 1) they stand for none) and, if causal, those up to its own position and those that prefix
+    (bool [batch, keys]) names.  One that sees nothing gets zeros.  With save=True returns (y, saved), `saved` being what attention_backward wants."""
+    d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
+    if out is not None:
+        _strided("out", out, tuple(q.shape), q.dtype, dev)
+    if not save:
+        _unrecorded(q, k, v)
+    lib = B.lib()
+    with _scope(stream, dev, out, *held) as st:
+        need, scratch = C.c_uint64(), C.c_uint64()
+        B._check(lib.chm_attention_sizes(d, None, need, scratch, None))
+        saved = None
+        if save:
+            saved = _bytes(need.value, q)
+            d.saved = saved.data_ptr()
+        if out is None:
+            out = q.new_empty(q.shape)
+        ws = _bytes(scratch.value, q)
+        B._check(lib.chm_attention_forward(d, out.data_ptr(), B.Strides(*_strides(out)), ws.data_ptr(), ws.numel(), st))
+    return (out, saved) if save else out
+
+
+def attention_backward(dy, q, k, v, y, saved, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None, out=None, stream=None):
+    """chm_attention_backward: (dq, dk, dv) for dy, the gradient with respect to y, from attention_forward's y and saved; the other arguments as there.
+    `out`: the three tensors to write (of any strides: the parts of one projection's gradient)."""
+    d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
+    _strided("dy", dy, tuple(q.shape), q.dtype, dev)
+    _strided("y", y, tuple(q.shape), q.dtype, dev)
+    _need(isinstance(saved, torch.Tensor) and saved.get_device() == dev and saved.dtype == torch.uint8 and saved.is_contiguous(),
+          "saved must be what attention_forward returned")
+    if out is not None:
+        out = tuple(out)
+        _need(len(out) == 3, "out must be three tensors")
+        for name, t, like in zip(("out[0]", "out[1]", "out[2]"), out, (q, k, v)):
+            _strided(name, t, tuple(like.shape), q.dtype, dev)
+    lib = B.lib()
+    with _scope(stream, dev, dy, y, saved, *held, *(out or ())) as st:
+        if out is None:
+            out = (q.new_empty(q.shape), k.new_empty(k.shape), v.new_empty(v.shape))
+        d.saved = saved.data_ptr()
+        g = B.AttentionGradients(dy.data_ptr(), y.data_ptr(), *[t.data_ptr() for t in out], _strides(dy), _strides(y), *[_strides(t) for t in out])
+        need, scratch = C.c_uint64(), C.c_uint64()
+        B._check(lib.chm_attention_sizes(d, g, need, None, scratch))
+        _need(saved.numel() >= need.value, "saved is not of a forward call of these sizes")
+        ws = _bytes(scratch.value, q)
+        B._check(lib.chm_attention_backward(d, g, ws.data_ptr(), ws.numel(), st))
     return out
 
 

@@ -1,0 +1,465 @@
+"""Attention on the GPU against its formulas in 64 bits.
+
+Tolerances.  Weights p and their gradients ds enter products rounded to the tensors' type of unit roundoff u: each is off by at most u of itself
+(in float16 at least 2^-25), independently, with a standard deviation of that bound / sqrt(3).  dy.y is taken with y as it was stored, rounded
+once: that error is common to a row of ds.  Scores are float32 sums of dim products, and the exponential's argument is rounded a few times: 2^-24 of
+its terms.  The sum of these variances is worked out for every element of the results; an error of six standard deviations and the rounding of the
+result itself is allowed.  A pair that is seen or left out wrongly, or a sum that misses a tile, is tens of times that.
+"""
+import math
+
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+
+U = {torch.bfloat16: 2.0 ** -8, torch.float16: 2.0 ** -11}
+TINY = {torch.bfloat16: 0.0, torch.float16: 2.0 ** -25}
+ACC = 2.0 ** -24
+BOTH = [torch.bfloat16, torch.float16]
+NAMES = ("dq", "dk", "dv")
+
+
+@pytest.fixture(scope="module")
+def ops():
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2508_21613_amd import binding, operators
+    binding.lib()
+    return operators
+
+
+def gen(seed):
+    g = torch.Generator(device="cuda")
+    g.manual_seed(seed)
+    return g
+
+
+def normal(g, shape, dtype, std=1.0, pad=0, shift=0):
+    """[batch, tokens, heads, dim] of normal numbers; tokens `pad` elements further apart than they are long, the first `shift` into its buffer"""
+    B, T, H, d = shape
+    buf = torch.full((B * T * (H * d + pad) + shift,), float("nan"), dtype=dtype, device="cuda")
+    t = buf[shift:].view(B, T, H * d + pad)[:, :, :H * d].unflatten(2, (H, d))
+    t.copy_(torch.randn(shape, generator=g, device="cuda") * std)
+    return t
+
+
+def inputs(seed, B, T, K, H, Hk, d, dtype, pad=0, shift=0):
+    g = gen(seed)
+    return [normal(g, s, dtype, std, pad, shift) for s, std in (((B, T, H, d), 1.5), ((B, K, Hk, d), 1.5), ((B, K, Hk, d), 1.0), ((B, T, H, d), 0.3))]
+
+
+def visible(B, T, K, causal=True, documents=None, prefix=None):
+    i, j = torch.arange(T, device="cuda")[:, None] + K - T, torch.arange(K, device="cuda")[None]
+    see = torch.ones((B, T, K), dtype=torch.bool, device="cuda")
+    if causal:
+        see &= j <= i
+        if prefix is not None:
+            see |= prefix.bool()[:, None, :]
+    if documents is not None:
+        dq, dk = documents if isinstance(documents, tuple) else (documents, documents)
+        see &= (dq[:, :, None] == dk[:, None, :]) & (dk >= 0)[:, None, :] & (dk < 2 ** 31 - 1)[:, None, :]
+    return see
+
+
+def clean(t, documents, which):
+    """zeros in the places of no document: what lies there is no input"""
+    t = t.double()
+    if documents is None:
+        return t
+    ids = documents[which] if isinstance(documents, tuple) else documents
+    return torch.where(((ids >= 0) & (ids < 2 ** 31 - 1))[:, :, None, None], t, 0.0)
+
+
+def formula(q, k, v, dy=None, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None):
+    """{name: (value, variance of the error)} in 64 bits, one key head after the other"""
+    dtype, (B, T, H, d), (K, Hk) = q.dtype, q.shape, k.shape[1:3]
+    u, tiny, G = U[dtype], TINY[dtype], H // Hk
+    scale = d ** -0.5 if scale is None else scale
+    see = visible(B, T, K, causal, documents, prefix)
+    far = (torch.arange(T, device="cuda")[:, None] + K - T - torch.arange(K, device="cuda")[None]).abs().double()
+    q, k, v = clean(q, documents, 0), clean(k, documents, 1), clean(v, documents, 1)
+    dy = None if dy is None else clean(dy, documents, 0)
+    out = {n: (torch.zeros(s, dtype=torch.float64, device="cuda"), torch.zeros(s, dtype=torch.float64, device="cuda"))
+           for n, s in (("y", q.shape), ("dq", q.shape), ("dk", k.shape), ("dv", v.shape))}
+
+    def put(name, b, at, value, var):
+        out[name][0][b, :, at] += value
+        out[name][1][b, :, at] += var
+
+    for b in range(B):
+        for h in range(H):
+            qq, kk, vv = q[b, :, h], k[b, :, h // G], v[b, :, h // G]
+            x = scale * qq @ kk.T
+            e = scale * ACC * math.sqrt(d) * ((qq * qq) @ (kk * kk).T).sqrt() + 2 * ACC * x.abs()
+            dz = torch.ones_like(x)
+            z, more = x, torch.zeros_like(x)
+            if cap:
+                t = torch.tanh(x / cap)
+                z, dz = cap * t, 1 - t * t
+                more = 8 * ACC + 2 * e / cap                     # of dz
+                e = e * dz + 4 * ACC * cap
+            s = z - (float(slopes[h]) * far if slopes is not None else 0.0)
+            s = s.masked_fill(~see[b], -math.inf)
+            some = see[b].any(1, keepdim=True)
+            lse = torch.where(some, torch.logsumexp(s, 1, keepdim=True), 0.0)
+            p = torch.exp(s - lse)
+            e = e + ACC * (4 * torch.where(see[b], s, 0.0).abs() + 4 * lse.abs() + 8)
+            vp = ((u * p) ** 2 + torch.where(see[b], tiny, 0.0) ** 2) / 3
+            y = p @ vv
+            pe = (p * e) ** 2
+            vy = vp @ (vv * vv) + 2 * (pe @ (vv * vv) + y * y * pe.sum(1, keepdim=True)) + ACC ** 2 * K * ((p * p) @ (vv * vv)) + (8 * ACC * y) ** 2
+            put("y", b, h, y, vy)
+            if dy is None:
+                continue
+            gy = dy[b, :, h]
+            dp = gy @ vv.T
+            vdp = ACC ** 2 * d * ((gy * gy) @ (vv * vv).T)
+            delta = (gy * y).sum(1, keepdim=True)
+            vdelta = ((gy * gy) * (vy + (u * y).clamp(min=tiny) ** 2 / 3)).sum(1, keepdim=True) + ACC ** 2 * d * ((gy * y) ** 2).sum(1, keepdim=True)
+            ds = p * (dp - delta) * dz
+            vds = (p * dz) ** 2 * vdp + (ds * e) ** 2 + (p * (dp - delta) * more) ** 2 + (8 * ACC * p * dp * dz) ** 2 + (
+                (u * ds) ** 2 + torch.where(see[b], tiny, 0.0) ** 2) / 3
+            pz = p * dz
+            dq, dk, dv = scale * ds @ kk, scale * ds.T @ qq, p.T @ gy
+            put("dq", b, h, dq, scale ** 2 * (vds @ (kk * kk) + vdelta * (pz @ kk) ** 2 + ACC ** 2 * K * ((ds * ds) @ (kk * kk))) + (8 * ACC * dq) ** 2)
+            put("dk", b, h // G, dk, scale ** 2 * ((vds + pz * pz * vdelta).T @ (qq * qq) + ACC ** 2 * T * G * ((ds * ds).T @ (qq * qq))) + (8 * ACC * dk) ** 2)
+            put("dv", b, h // G, dv, (vp + pe).T @ (gy * gy) + ACC ** 2 * T * G * ((p * p).T @ (gy * gy)) + (8 * ACC * dv) ** 2)
+    return out if dy is not None else {"y": out["y"]}
+
+
+def check(name, got, want):
+    value, var = want
+    assert got.shape == value.shape, name
+    assert bool(torch.isfinite(got).all()), name
+    err = (got.double() - value).abs()
+    tol = 6 * var.sqrt() + torch.clamp(value.abs() * U[got.dtype], min=TINY[got.dtype]) * 1.0001 + 1e-30
+    bad = err > tol
+    assert not bool(bad.any()), (name, int(bad.sum()), float((err / tol).max()), [int(i) for i in bad.nonzero()[0]])
+
+
+def both(ops, q, k, v, dy, **kw):
+    y, saved = ops.attention_forward(q, k, v, save=True, **kw)
+    return dict(zip(("y",) + NAMES, (y,) + ops.attention_backward(dy, q, k, v, y, saved, **kw)))
+
+
+def compare(ops, x, **kw):
+    want = formula(*x, **kw)
+    got = both(ops, *x, **kw)
+    for name in want:
+        check(name, got[name], want[name])
+    alone = ops.attention_forward(*x[:3], **kw)                 # without keeping anything: the same bits
+    assert torch.equal(alone, got["y"])
+    return got, want
+
+
+def slopes_of(H):
+    return torch.exp2(-8.0 * torch.arange(1, H + 1, device="cuda") / H).float()
+
+
+def documents_of(seed, B, n, count, padding=0):
+    """documents one behind the other, of random lengths; `padding` places at the end belong to none"""
+    g = torch.Generator()
+    g.manual_seed(seed)
+    ids = torch.full((B, n), -1, dtype=torch.int64)
+    for b in range(B):
+        live = n - padding
+        cuts = sorted(torch.randint(0, live + 1, (count - 1,), generator=g).tolist())
+        for i, (lo, hi) in enumerate(zip([0] + cuts, cuts + [live])):
+            ids[b, lo:hi] = 3 * i
+    return ids.cuda()
+
+
+TERMS = [dict(), dict(cap=15.0), dict(slopes=True), dict(cap=5.0, slopes=True, scale=0.3)]
+
+
+def terms(which, H):
+    t = dict(TERMS[which])
+    if t.get("slopes"):
+        t["slopes"] = slopes_of(H)
+    return t
+
+
+# sizes around the tiles' (32 rows of an instruction, 64 keys of a tile, 128 rows of a workgroup), groups of every kind, odd head sizes
+SHAPES = [(1, 1, 1, 1, 1, 1), (1, 1, 1, 1, 1, 64), (2, 3, 3, 2, 1, 8), (1, 31, 31, 1, 1, 64), (1, 32, 32, 2, 2, 128), (1, 33, 33, 1, 1, 16), (3, 17, 17, 4, 4, 64),
+          (1, 63, 63, 3, 1, 72), (1, 64, 64, 7, 1, 40), (2, 65, 65, 6, 3, 96), (1, 127, 127, 2, 1, 128), (1, 128, 128, 8, 2, 64), (1, 129, 129, 5, 5, 33),
+          (1, 200, 200, 12, 4, 80), (2, 255, 255, 2, 1, 127), (1, 257, 257, 9, 3, 128), (1, 515, 515, 4, 2, 65), (1, 700, 700, 4, 1, 128), (1, 1100, 1100, 2, 2, 64)]
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("shape", SHAPES)
+def test_causal(ops, shape, dtype):
+    compare(ops, inputs(sum(shape), *shape, dtype), **terms(sum(shape) % 4, shape[3]))
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("which", range(4))
+@pytest.mark.parametrize("d", [64, 128])
+def test_every_kernel(ops, which, d, dtype):
+    """the kernels for many rows and for few, with every combination of a score's terms"""
+    for B, T, K, H, Hk in ((2, 150, 150, 4, 2), (2, 3, 200, 8, 2)):
+        for causal in (True, False):
+            compare(ops, inputs(which + T, B, T, K, H, Hk, d, dtype), causal=causal, **terms(which, H))
+
+
+# new tokens behind those whose keys are there, and more queries than keys: the first ones see nothing
+@pytest.mark.parametrize("T,K", [(1, 64), (5, 70), (40, 100), (130, 1000), (100, 40), (200, 1), (65, 64)])
+@pytest.mark.parametrize("which", range(4))
+def test_queries_and_keys_of_different_lengths(ops, T, K, which):
+    x = inputs(T + K, 2, T, K, 4, 2, 64, torch.bfloat16)
+    got, _ = compare(ops, x, **terms(which, 4))
+    if T > K:
+        assert not bool(got["y"][:, :T - K].any()) and not bool(got["dq"][:, :T - K].any())
+    compare(ops, x, causal=False, **terms(which, 4))
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("B,K,H,Hk,d", [(1, 1, 8, 1, 128), (1, 31, 32, 1, 64), (2, 32, 4, 4, 128), (1, 33, 6, 2, 72), (3, 95, 8, 8, 64), (1, 1000, 40, 8, 128),
+                                        (2, 4099, 8, 2, 128), (5, 513, 33, 3, 64), (1, 20000, 16, 2, 128), (1, 9000, 48, 1, 100), (70, 300, 16, 16, 64)])
+def test_one_new_token(ops, B, K, H, Hk, d, dtype):
+    for which in (0, 3):
+        for causal in (True, False):
+            kw = dict(causal=causal, **terms(which, H))
+            q, k, v, _ = inputs(K + which, B, 1, K, H, Hk, d, dtype)
+            check("y", ops.attention_forward(q, k, v, **kw), formula(q, k, v, **kw)["y"])
+
+
+@pytest.mark.parametrize("T,K,H,Hk,d", [(256, 5000, 8, 2, 128), (100, 9000, 2, 1, 64), (40, 3001, 1, 1, 96)])
+def test_few_rows_over_many_keys_are_split(ops, T, K, H, Hk, d):
+    q, k, v, dy = inputs(K, 1, T, K, H, Hk, d, torch.bfloat16)
+    compare(ops, (q, k, v, dy), slopes=slopes_of(H))
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("B,T,count,padding", [(1, 17, 3, 0), (2, 150, 4, 20), (1, 515, 7, 100), (2, 640, 2, 0), (1, 700, 40, 5)])
+@pytest.mark.parametrize("which", [0, 3])
+def test_documents(ops, B, T, count, padding, which, dtype):
+    ids = documents_of(T, B, T, count, padding)
+    for causal in (True, False):
+        x = inputs(T, B, T, T, 6, 2, 72, dtype)
+        got, _ = compare(ops, x, causal=causal, documents=ids, **terms(which, 6))
+        none = ids < 0
+        assert not any(bool(got[n][none].any()) for n in got)
+    got32 = both(ops, *x, documents=ids.int(), causal=False, **terms(which, 6))
+    assert all(torch.equal(got[n], got32[n]) for n in got)
+
+
+def test_documents_in_any_order(ops):
+    """numbers that alternate, repeat far apart, are as large as they may be, or mean none"""
+    T = 300
+    ids = torch.stack([torch.arange(T) % 3, torch.arange(T) // 7 % 5, torch.tensor([2 ** 31 - 2, 2 ** 31 - 3, -1, 2 ** 31 - 1, 2 ** 40, -2 ** 40])[torch.arange(T) % 6]]).cuda()
+    x = inputs(5, 3, T, T, 2, 1, 64, torch.float16)
+    got, _ = compare(ops, x, documents=ids)
+    assert not bool(got["y"][2, torch.arange(T, device="cuda") % 6 > 1].any())
+    compare(ops, x, documents=ids, causal=False, cap=3.0)
+
+
+@pytest.mark.parametrize("T,K,H,Hk", [(1, 700, 8, 2), (5, 300, 4, 2), (200, 700, 2, 1), (130, 64, 2, 2)])
+def test_documents_of_queries_and_keys(ops, T, K, H, Hk):
+    B = 4
+    kid = documents_of(K, B, K, 3, 30)
+    kid[2] = -1                                                 # a sequence without any key
+    kid[3, K // 2:] = -1                                        # and one whose second half is not there
+    qid = torch.zeros((B, T), dtype=torch.int64, device="cuda")
+    qid[1, T // 2:] = 3
+    if T > 3:
+        qid[0, 2] = -1                                          # and a query of none
+    for causal in (True, False):
+        x = inputs(T, B, T, K, H, Hk, 64, torch.bfloat16)
+        got, _ = compare(ops, x, documents=(qid, kid), causal=causal)
+        assert not bool(got["y"][2].any()) and not bool(got["dk"][2].any())
+
+
+@pytest.mark.parametrize("T,count,padding", [(40, 1, 0), (150, 2, 10), (515, 3, 60)])
+@pytest.mark.parametrize("which", [0, 3])
+def test_prefix(ops, T, count, padding, which):
+    ids = documents_of(T, 2, T, count, padding)
+    prefix = torch.zeros((2, T), dtype=torch.bool, device="cuda")
+    for b in range(2):
+        for doc in ids[b].unique():
+            places = (ids[b] == doc).nonzero().flatten()
+            prefix[b, places[:len(places) * (2 + b) // 5]] = True
+    x = inputs(T, 2, T, T, 4, 2, 64, torch.float16)
+    compare(ops, x, documents=ids, prefix=prefix, **terms(which, 4))
+    compare(ops, x, prefix=prefix, **terms(which, 4))           # of one document
+    g = torch.Generator()
+    g.manual_seed(T)
+    anywhere = (torch.rand((2, T), generator=g) < 0.1).cuda()   # and not only at its start
+    compare(ops, x, documents=ids, prefix=anywhere.to(torch.uint8) * 7, **terms(which, 4))
+    compare(ops, x, prefix=torch.ones_like(prefix), **terms(which, 4))
+
+
+@pytest.mark.parametrize("T", [20, 300])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_places_of_no_document_may_hold_anything(ops, T, value):
+    for causal in (True, False):
+        ids = documents_of(T, 2, T, 2, T // 3)
+        ids[1, 3:9] = -1
+        x = inputs(T, 2, T, T, 4, 2, 128, torch.bfloat16)
+        for t in x:
+            t[ids < 0] = value
+        y, saved = ops.attention_forward(*x[:3], documents=ids, causal=causal, save=True)
+        got = dict(zip(NAMES, ops.attention_backward(x[3], *x[:3], y, saved, documents=ids, causal=causal)), y=y)
+        want = formula(*x, documents=ids, causal=causal)
+        for name in want:
+            check(name, got[name], want[name])
+            assert not bool(got[name][ids < 0].any())
+
+
+@pytest.mark.parametrize("pad,shift", [(0, 1), (3, 0), (5, 7), (8, 0), (64, 8)])
+@pytest.mark.parametrize("T", [6, 140])
+def test_strides_and_alignment(ops, T, pad, shift):
+    x = inputs(3, 2, T, T, 4, 2, 72, torch.float16, pad, shift)
+    want = formula(*x)
+    outs = [normal(gen(i), t.shape, torch.float16, 1.0, 5, 3) for i, t in enumerate((x[0], x[0], x[1], x[2]))]
+    y, saved = ops.attention_forward(*x[:3], save=True, out=outs[0])
+    assert y is outs[0]
+    ops.attention_backward(x[3], *x[:3], y, saved, out=outs[1:])
+    for name, t in zip(("y",) + NAMES, outs):
+        check(name, t, want[name])
+        assert bool(torch.isnan(t._base[:3]).all()) and bool(torch.isnan(t._base[3:].view(2, T, -1)[:, :, t.shape[2] * 72:]).all()), name
+
+
+def test_one_projection_and_heads_first(ops):
+    """queries, keys and values side by side, their gradients too; tensors laid out by heads; keys that all sequences share"""
+    B, T, H, Hk, d = 2, 150, 4, 2, 64
+    g = gen(9)
+    both_ = torch.randn((B, T, H + 2 * Hk, d), generator=g, device="cuda").bfloat16()
+    q, k, v = both_[:, :, :H], both_[:, :, H:H + Hk], both_[:, :, H + Hk:]
+    dy = torch.randn((B, T, H, d), generator=g, device="cuda").bfloat16()
+    want = formula(q, k, v, dy)
+    y, saved = ops.attention_forward(q, k, v, save=True)
+    grads = torch.full_like(both_, float("nan"))
+    ops.attention_backward(dy, q, k, v, y, saved, out=(grads[:, :, :H], grads[:, :, H:H + Hk], grads[:, :, H + Hk:]))
+    for name, t in zip(("y",) + NAMES, (y, grads[:, :, :H], grads[:, :, H:H + Hk], grads[:, :, H + Hk:])):
+        check(name, t, want[name])
+    by_head = [t.transpose(1, 2).contiguous().transpose(1, 2) for t in (q, k, v, dy)]
+    got = both(ops, *by_head)
+    assert all(torch.equal(got[n], t) for n, t in zip(("y",) + NAMES, (y, grads[:, :, :H], grads[:, :, H:H + Hk], grads[:, :, H + Hk:])))
+    shared = [q, k[:1].expand(B, -1, -1, -1), v[:1].expand(B, -1, -1, -1), dy]
+    want = formula(*shared)
+    for name, t in both(ops, *shared).items():
+        check(name, t, want[name])
+
+
+def test_lengths_of_zero(ops):
+    for B, T, K in ((0, 5, 5), (2, 0, 0), (2, 0, 70), (2, 70, 0), (2, 3, 0)):
+        x = inputs(1, B, T, K, 4, 2, 64, torch.bfloat16)
+        got = both(ops, *x, causal=False)
+        for name, like in zip(("y",) + NAMES, (x[0], x[0], x[1], x[2])):
+            assert got[name].shape == like.shape and not bool(got[name].any())
+
+
+def test_scores_far_apart(ops):
+    """maxima that grow from tile to tile by more than the exponential reaches, and scores beyond it either way"""
+    B, T, H, d = 1, 400, 2, 64
+    q, k, v, dy = inputs(2, B, T, T, H, H, d, torch.bfloat16)
+    q[..., 0], k[..., 0] = 30.0, (torch.arange(T, device="cuda") * 0.5 - 100).bfloat16()[None, :, None]
+    for sign in (1, -1):
+        k[..., 0] *= sign
+        for kw in (dict(), dict(cap=50.0)):
+            compare(ops, (q, k, v, dy), **kw)
+
+
+def test_infinities_and_nans_follow_the_formulas(ops):
+    q, k, v, _ = inputs(4, 1, 70, 70, 1, 1, 64, torch.bfloat16)
+    q[0, 40] = float("nan")
+    y = ops.attention_forward(q, k, v)
+    rows = torch.isnan(y[0, :, 0]).any(1)
+    assert rows.nonzero().flatten().tolist() == [40] and bool(torch.isnan(y[0, 40]).all())
+    q[0, 40] = 1.0
+    k[0, 69] = float("inf")                                     # capped: a score of the cap, or less it
+    q[0, 69] = 1.0
+    y = ops.attention_forward(q, k, v, cap=8.0)
+    assert bool(torch.isfinite(y).all())
+
+
+def test_same_inputs_same_bits(ops):
+    x = inputs(8, 1, 900, 900, 8, 2, 128, torch.bfloat16)
+    ids = documents_of(1, 1, 900, 3, 9)
+    first = both(ops, *x, documents=ids)
+    for _ in range(3):
+        again = both(ops, *x, documents=ids)
+        assert all(torch.equal(first[n], again[n]) for n in first)
+
+
+@pytest.mark.parametrize("which", [0, 3])
+def test_gradients_against_differences(ops, which):
+    """dy.y changes along a direction as the gradients say: central differences of the formula in 64 bits (off by step^2) against the kernels'
+    gradients, whose errors' variances add up along the direction"""
+    x = inputs(21, 1, 90, 90, 4, 2, 40, torch.float16)
+    kw = terms(which, 4)
+    got, want = both(ops, *x, **kw), formula(*x, **kw)
+
+    def loss(t):
+        return float((formula(*t, **kw)["y"][0] * x[3].double()).sum())
+
+    # the 16-bit inputs are the middle; the formula takes them as 64-bit ones
+    formula_dtype = torch.float64
+    U[formula_dtype], TINY[formula_dtype] = 0.0, 0.0
+    try:
+        for i, name in enumerate(NAMES):
+            step, g = 1e-4, gen(i)
+            along = torch.randn(x[i].shape, generator=g, device="cuda", dtype=torch.float64)
+            ends = []
+            for sign in (1, -1):
+                t = [a.double() for a in x[:3]]
+                t[i] = t[i] + sign * step * along
+                ends.append(loss(t))
+            slope = (ends[0] - ends[1]) / (2 * step)
+            here = float((got[name].double() * along).sum())
+            sigma = float(((want[name][1] + (U[torch.float16] * want[name][0]) ** 2 / 3) * along ** 2).sum().sqrt())
+            assert abs(here - slope) <= 6 * sigma + 1e-5 * abs(slope) + 1e-6, (name, here, slope, sigma)
+    finally:
+        del U[formula_dtype], TINY[formula_dtype]
+
+
+def test_captured_and_replayed(ops):
+    """a step in a graph, replayed with other inputs in the same places, eager work between the replays"""
+    shape = (1, 300, 300, 4, 2, 64)
+    ids = documents_of(3, 1, 300, 3, 20)
+    place, others = inputs(1, *shape, torch.bfloat16), [inputs(s, *shape, torch.bfloat16) for s in (2, 3, 4)]
+    tok = inputs(5, 2, 1, 5000, 8, 2, 128, torch.bfloat16)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        both(ops, *place, documents=ids)
+        ops.attention_forward(*tok[:3])
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = both(ops, *place, documents=ids)
+        one = ops.attention_forward(*tok[:3])
+    for x in others + others:
+        for a, b in zip(place, x):
+            a.copy_(b)
+        tok[0].mul_(-1)
+        graph.replay()
+        want, want_one = both(ops, *x, documents=ids), ops.attention_forward(*tok[:3])
+        torch.cuda.synchronize()
+        assert all(torch.equal(got[n], want[n]) for n in want) and torch.equal(one, want_one)
+
+
+def test_on_another_stream(ops):
+    x = inputs(6, 1, 500, 500, 4, 2, 64, torch.bfloat16)
+    want = both(ops, *x)
+    torch.cuda.synchronize()
+    stream = torch.cuda.Stream()
+    y, saved = ops.attention_forward(*x[:3], save=True, stream=stream)
+    got = (y,) + ops.attention_backward(x[3], *x[:3], y, saved, stream=stream.cuda_stream)
+    stream.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want.values()))
+
+
+def test_offsets_beyond_32_bits(ops):
+    """a cache of more than 2^31 elements, and tokens further apart than offsets of 31 bits reach within a tile"""
+    K, Hk, d = 300000, 64, 128
+    g = gen(1)
+    k, v = (torch.empty((1, K, Hk, d), dtype=torch.bfloat16, device="cuda").normal_(0, 1, generator=g) for _ in range(2))
+    q = normal(g, (1, 1, Hk, d), torch.bfloat16)
+    y = ops.attention_forward(q, k, v)
+    for h in (0, 31, 63):
+        check("y", y[:, :, h:h + 1], formula(q[:, :, h:h + 1], k[:, :, h:h + 1], v[:, :, h:h + 1])["y"])
+    wide = k.view(-1)[:(K // 8) * Hk * d * 8].view(1, 8, -1)[:, :, :Hk * d].unflatten(2, (Hk, d))          # 8 tokens 300 million elements apart
+    y = ops.attention_forward(wide, wide, wide)
+    check("y", y[:, :, :4], formula(wide[:, :, :4], wide[:, :, :4], wide[:, :, :4])["y"])

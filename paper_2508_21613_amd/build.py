@@ -32,6 +32,8 @@ SOURCES = ["chm_host.cpp", "chm_pool.cpp", "chm_kernels.hip", "chm_fast.hip", "c
 # the operators of a training step: their values may be infinite or not a number, and pass through as such
 FLOAT_SOURCES = tuple(s for s in SOURCES if s.startswith(("chm_ffn", "chm_embedding", "chm_clip", "chm_rotary", "chm_attention")))
 NO_NANS = ["-Xarch_device", "-fno-honor-nans"]
+# accumulators of the matrix instructions that a loop carries stay in one block of registers: taken apart, attention's 64 of them are moved twice a step
+WHOLE_PHIS = ["-mllvm", "-amdgpu-codegenprepare-break-large-phis=false"]
 # no device code of the search meets a NaN (NO_NANS): a maximum of floats is one instruction then, not one more for each operand
 # that might be one; packed-FP32 instruction selection is switched off for all device code; so is the vectorizer of straight-line code, which
 # finds nothing to gain in integer kernels and puts arrays it has half packed into scratch
@@ -55,7 +57,7 @@ def build(verbose=True, changed_only=False):
         objs.append(obj)
         fresh = os.path.exists(obj) and os.path.getmtime(obj) >= max(os.path.getmtime(src), newest_header)
         if not (changed_only and fresh):
-            todo.append(["hipcc"] + FLAGS + ([] if s in FLOAT_SOURCES else NO_NANS) + (HOST_SANITIZE if SANITIZE else []) + ["-x", "hip", "-c", src, "-o", obj])
+            todo.append(["hipcc"] + FLAGS + ([] if s in FLOAT_SOURCES else NO_NANS) + (WHOLE_PHIS if s.startswith("chm_attention_") else []) + (HOST_SANITIZE if SANITIZE else []) + ["-x", "hip", "-c", src, "-o", obj])
 
     def run(cmd):
         if verbose:

@@ -17,11 +17,22 @@ struct AttnOutput { uint16_t *p; int64_t batch, token, head; };
 struct AttnDivide { uint32_t m; int32_t shift; };
 
 // What 64 tokens' documents are: the least and the largest number (first > last: none), and flags.  A document and "in the prefix" of a token
-// are one word: number * 2 + prefix; all ones: of none.
+// are one word: number * 2 + prefix (the largest is 0xfffffffd).
 struct AttnTile { int32_t first, last, flags, unused; };
 enum { ATTN_SOME_NONE = 1, ATTN_SOME_PREFIX = 2, ATTN_ALL_PREFIX = 4 };
-constexpr uint32_t ATTN_NONE = 0xffffffffu;
+constexpr uint32_t ATTN_NONE = 0xfffffffeu;
 constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles are laid out for whole ones
+
+// What the backward pass knows of 32 rows, one value after the other, rounded up to whole blocks (rows behind the last see nothing)
+struct AttnRows {
+  float lse[32];                           // log2 of the sum of powers of two; +inf: the row sees nothing
+  float delta[32];                         // dy . y
+  int32_t last[32];                        // last key that a causal mask leaves (no mask: all)
+  uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
+  float slope2[32];
+  int32_t pos[32];
+};
+constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // with or without the lowest bit it equals no key's word, ATTN_NONE neither
 
 struct AttnCall {
   AttnInput q, k, v, dy;
@@ -38,7 +49,10 @@ struct AttnCall {
   const uint32_t *q_words, *k_words;       // [batch][whole tiles], or null: no documents and no prefix
   const AttnTile *q_tiles, *k_tiles;       // [batch][tiles]
   int32_t q_tile_count;
-  float *lse, *delta;                      // [batch * kv_heads][rows_pad]: log2 of the sum of powers of two (+inf: the row sees nothing); dy . y
+  int32_t prefix;                          // some words may have the prefix's bit
+  float *lse;                              // [batch * kv_heads][rows_pad]: kept by the forward pass
+  uint16_t *low;                           // [batch, tokens, heads, width]: what rounding took from y
+  AttnRows *row_data;                      // [batch * kv_heads][rows_pad / 32]
   // sums split over workgroups: float32 parts, joined in order
   int32_t splits;
   float *part, *part2;                     // forward: [splits][batch * kv_heads][rows][width4] and (maximum, sum); backward: dk and dv [splits][batch * kv_heads][keys][width4]

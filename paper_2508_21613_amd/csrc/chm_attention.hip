@@ -1,7 +1,7 @@
-// Attention: what its passes consist of, the small kernels around the tiles (documents, packing, delta, joined sums), the entry points.
+// Attention: what its passes consist of, the small kernels around the tiles (documents, packing, rows, joined sums), the entry points.
 //
 //   forward    [pack] [documents] tiles [join]
-//   backward   [pack] [documents] delta = dy.y, dq, dk and dv [join]
+//   backward   [pack] [documents] rows (delta = dy.y), dq, dk and dv [join]
 // dq and dk with dv are kernels of their own, each of which works out the scores again: seven products in place of five, but no sums that several
 // workgroups add to, so that the same inputs give the same bits.
 #include <hip/hip_runtime.h>
@@ -85,40 +85,52 @@ __global__ void __launch_bounds__(256) k_pack(PackCall c) {
   *(Words *)(m.out + w * 8) = v;
 }
 
-// ---------------------------------------------------------------------------------------------- delta
-// dy.y of every row, by 16 lanes a row
-struct DeltaCall {
-  AttnInput dy, y;
-  float *delta;
-  int32_t dim, tokens, heads, group, kv_heads, rows_pad;
-  int64_t all;
-};
+// ---------------------------------------------------------------------------------------------- rows
+// What the backward pass wants to know of every row: delta = dy.y, by 16 lanes a row, and what tells which keys it sees.  y is taken with what its
+// rounding took from it: where few keys share a row, dy.v and delta are near each other, and 2^-9 of y would be 1.5 times the error that the
+// gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3 without, 2.4e-3 with).
+struct RowsCall { AttnInput dy, y; };
 template <int DT>
-__global__ void __launch_bounds__(256) k_delta(DeltaCall c) {
-  const int64_t row = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+__global__ void __launch_bounds__(256) k_rows(const AttnCall c, const RowsCall in, int64_t all) {
+  const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+  if (i >= all) return;                    // all 16 lanes of a row
   const int d = (threadIdx.x & 15) * 8;
-  const int64_t token = row / c.heads, seq = token / c.tokens;
-  const int head = (int)(row - token * c.heads), t = (int)(token - seq * c.tokens);
+  const int64_t hb = i / c.rows_pad, seq = hb / c.kv_heads;
+  const int r = (int)(i - hb * c.rows_pad), h = (int)(hb - seq * c.kv_heads);
+  const int t = r / c.group, head = h * c.group + r - t * c.group;
+  const bool there = r < c.rows;
   float sum = 0.f;
-  if (row < c.all && d < c.dim) {
-    const char *a = (const char *)(c.dy.p + seq * c.dy.batch + t * c.dy.token + head * c.dy.head + d);
-    const char *b = (const char *)(c.y.p + seq * c.y.batch + t * c.y.token + head * c.y.head + d);
-    if (d + 8 <= c.dim) {
-      float v[8], w[8];
+  if (there && d < c.width) {
+    const char *a = (const char *)(in.dy.p + seq * in.dy.batch + t * in.dy.token + head * in.dy.head + d);
+    const char *b = (const char *)(in.y.p + seq * in.y.batch + t * in.y.token + head * in.y.head + d);
+    const char *l = (const char *)(c.low + ((seq * c.tokens + t) * (c.kv_heads * c.group) + head) * c.width + d);
+    if (d + 8 <= c.width) {
+      float v[8], w[8], x[8];
       Lane<DT>::up(load16(a), v);
       Lane<DT>::up(load16(b), w);
+      Lane<DT>::up(load16(l), x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(v[e], w[e], sum);
+      for (int e = 0; e < 8; ++e) sum = fmaf(v[e], w[e] + x[e], sum);
     } else {
-      for (int e = 0; d + e < c.dim; ++e) sum = fmaf(Lane<DT>::one(a + e * 2), Lane<DT>::one(b + e * 2), sum);
+      for (int e = 0; d + e < c.width; ++e) sum = fmaf(Lane<DT>::one(a + e * 2), Lane<DT>::one(b + e * 2) + Lane<DT>::one(l + e * 2), sum);
     }
   }
 #pragma unroll
   for (int x = 8; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-  if (row < c.all && d == 0) {
-    const int h = head / c.group;
-    c.delta[(seq * c.kv_heads + h) * c.rows_pad + (int64_t)t * c.group + head - h * c.group] = sum;
+  if (d != 0) return;
+  AttnRows &block = c.row_data[i / 32];
+  const int at = r % 32, pos = t + c.offset;
+  block.delta[at] = sum;
+  block.lse[at] = there ? c.lse[i] : INFINITY;
+  block.last[at] = !there ? INT32_MIN : c.causal ? pos : INT32_MAX;
+  uint32_t word = there ? 0 : ATTN_NOBODY;
+  if (there && c.q_words) {
+    word = c.q_words[seq * c.q_tile_count * ATTN_TILE + t];
+    word = word == ATTN_NONE ? ATTN_NOBODY : word & ~1u;
   }
+  block.word[at] = word;
+  block.slope2[at] = there && c.slopes ? c.slopes[head] * 1.44269504088896341f : 0.f;
+  block.pos[at] = pos;
 }
 
 // ---------------------------------------------------------------------------------------------- joins
@@ -149,7 +161,13 @@ __global__ void __launch_bounds__(256) k_join_forward(const AttnCall c, int64_t 
   const int64_t hb = at / c.rows, b = hb / c.kv_heads;
   const int h = (int)(hb - b * c.kv_heads), r = (int)(at - hb * c.rows), token = r / c.group, head = h * c.group + r - token * c.group;
   if (c.lse && d == 0) c.lse[hb * c.rows_pad + r] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
-  put4<DT>(c.y.p + b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v * (sum == 0.f ? 0.f : 1.f / sum));
+  v *= sum == 0.f ? 0.f : 1.f / sum;
+  put4<DT>(c.y.p + b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v);
+  if (!c.low) return;
+  f4 low;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) low[e] = v[e] - (DT == CHM_BF16 ? bf16_up(bf16_down(v[e])) : f16_up(f16_down(v[e])));
+  put4<DT>(c.low + ((b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width, d, c.width, low);
 }
 
 // dk and dv from the parts over the splits of the rows
@@ -197,7 +215,9 @@ constexpr int64_t LENGTH_MAX = 1ll << 30, ROWS_MAX = INT32_MAX - (1 << 13);
 
 int64_t group_of(const chm_attention *a) { return a->heads / a->kv_heads; }
 int64_t rows_pad(const chm_attention *a) { return up(a->tokens * group_of(a), ATTN_TILE) * ATTN_TILE; }
-uint64_t saved_bytes(const chm_attention *a) { return (uint64_t)(a->batch * a->kv_heads * rows_pad(a)) * 4; }
+// lse of every row; what rounding took from y
+uint64_t lse_bytes(const chm_attention *a) { return (uint64_t)(a->batch * a->kv_heads * rows_pad(a)) * 4; }
+uint64_t saved_bytes(const chm_attention *a) { return lse_bytes(a) + (((uint64_t)(a->batch * a->tokens * a->heads) * a->dim * 2 + 15) & ~15ull); }
 
 // the strides of dimensions of one element say nothing
 AttnInput input(const void *p, const int64_t s[3], int64_t b, int64_t t, int64_t h) {
@@ -242,6 +262,8 @@ struct Pass {
     }
     c.slopes = a->slopes;
     c.lse = (float *)a->saved;
+    c.low = a->saved ? (uint16_t *)((char *)a->saved + lse_bytes(a)) : nullptr;
+    c.prefix = a->prefix != nullptr;
     c.q = input(a->q, a->q_stride, a->batch, a->tokens, a->heads);
     c.k = input(a->k, a->k_stride, a->batch, a->keys, a->kv_heads);
     c.v = input(a->v, a->v_stride, a->batch, a->keys, a->kv_heads);
@@ -375,13 +397,13 @@ struct Pass {
     c.dk = output(g->dk, g->dk_stride, B, K, a->kv_heads);
     c.dv = output(g->dv, g->dv_stride, B, K, a->kv_heads);
     inputs(g);
-    c.delta = (float *)arena.take(saved_bytes(a));
-    const int64_t all = B * T * a->heads;
-    const uint32_t deltas = threads(up(all, 16), 256);
-    if (run && fits && deltas) {
-      DeltaCall d{dy, y, c.delta, (int32_t)a->dim, c.tokens, (int32_t)a->heads, c.group, c.kv_heads, c.rows_pad, all};
-      if (bf16()) hipLaunchKernelGGL(k_delta<CHM_BF16>, dim3(deltas), dim3(256), 0, st, d);
-      else hipLaunchKernelGGL(k_delta<CHM_F16>, dim3(deltas), dim3(256), 0, st, d);
+    const int64_t all = heads() * c.rows_pad;
+    c.row_data = (AttnRows *)arena.take((uint64_t)(all / 32) * sizeof(AttnRows));
+    const uint32_t row_groups = threads(up(all, 16), 256);
+    if (run && fits && row_groups) {
+      const RowsCall in{dy, y};
+      if (bf16()) hipLaunchKernelGGL(k_rows<CHM_BF16>, dim3(row_groups), dim3(256), 0, st, c, in, all);
+      else hipLaunchKernelGGL(k_rows<CHM_F16>, dim3(row_groups), dim3(256), 0, st, c, in, all);
       ok = ok && hipGetLastError() == hipSuccess;
     }
     if (T > 0) {
@@ -394,7 +416,7 @@ struct Pass {
     if (K > 0) {
       chosen.dkdv_keys = 128;
       c.key_tiles = (int32_t)up(K, chosen.dkdv_keys);
-      c.splits = tile_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), 512);
+      c.splits = tile_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), a->causal ? 1024 : 512);
       chosen.dkdv_splits = c.splits;
       const int64_t words = heads() * K * (c.width4 / 4);
       if (c.splits > 1) {

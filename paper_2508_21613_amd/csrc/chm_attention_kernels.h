@@ -40,12 +40,14 @@ struct Bf16 {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint16_t down(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
+  static __device__ __forceinline__ float up(uint16_t u) { return __builtin_bit_cast(float, (uint32_t)u << 16); }
 };
 struct F16 {
   static __device__ __forceinline__ f16 mfma(s8 a, s8 b, f16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
   static __device__ __forceinline__ uint16_t down(float f) { return __builtin_bit_cast(uint16_t, (_Float16)f); }
+  static __device__ __forceinline__ float up(uint16_t u) { return (float)__builtin_bit_cast(_Float16, u); }
 };
 
 constexpr float LOWEST = -1.5e38f;          // reference of a row that has met nothing: finite, so that no difference of infinities arises
@@ -219,12 +221,13 @@ struct KeyWalk {
   const AttnTile *tiles;
   int group_from, group_to, wave_from, wave_to;           // positions of the queries
   Range group_docs, wave_docs;
-  int at, end;                              // tiles of the present ballot: at .. at + 63; end: behind the last
+  int first, step;                          // every step-th tile from the first on: so the parts of split sums see equally much of any mask
+  int at, end;                              // those of the present ballot: at .. at + 63; end: behind the last tile
   uint64_t visit, mine, mask, none;
   int tile;                                 // the present one; -1: no more
   bool run, masked, some_none;
 
-  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int group_rows, int wave_row, int wave_rows, int first, int end_) {
+  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int group_rows, int wave_row, int wave_rows, int first_, int step_, int end_) {
     tiles = c.k_words ? c.k_tiles + (int64_t)b * c.tiles : nullptr;
     const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
     const int gf = token(group_row), gt = token(group_row + group_rows - 1), wf = token(wave_row), wt = token(wave_row + wave_rows - 1);
@@ -235,19 +238,22 @@ struct KeyWalk {
       group_docs = range_of(q, gf, gt);
       wave_docs = range_of(q, wf, wt);
     }
-    at = first - 64;
+    first = first_;
+    step = step_;
+    at = -64;
     end = end_;
     visit = 0;
   }
   __device__ __forceinline__ void next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if (at >= end) { tile = -1; return; }
-      const int t = at + lane;
-      const bool there = t < end;
+      if ((int64_t)at * step + first >= end) { tile = -1; return; }
+      const int64_t tt = (int64_t)(at + lane) * step + first;
+      const bool there = tt < end;
+      const int t = there ? (int)tt : 0;
       Range k{0, 0, 0};
       if (tiles && there) { const AttnTile x = tiles[t]; k = Range{x.first, x.last, x.flags}; }
-      const int k0 = there ? t * ATTN_TILE : 0, k1 = k0 + ATTN_TILE - 1;
+      const int k0 = t * ATTN_TILE, k1 = k0 + ATTN_TILE - 1;
       bool some, all, wave_some, wave_all;
       sees(c, group_from, group_to, group_docs, k0, k1, k, some, all);
       sees(c, wave_from, wave_to, wave_docs, k0, k1, k, wave_some, wave_all);
@@ -258,34 +264,37 @@ struct KeyWalk {
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    tile = at + i;
+    tile = (at + i) * step + first;
     run = (mine >> i) & 1;
     masked = (mask >> i) & 1;
     some_none = (none >> i) & 1;
   }
 };
 
-// Of the keys k0 + row_of(r): those that the query at `pos` of document `doc` sees, a bit each
-__device__ __forceinline__ uint32_t seen_by_query(const AttnCall &c, const uint32_t *words, int k0, int pos, uint32_t doc) {
-  uint32_t ok = 0;
+// Of the keys k0 + row_of(r): tells set(r, .) whether the query at `pos` of the document `word` sees it
+template <class F>
+__device__ __forceinline__ void seen_keys(const AttnCall &c, const uint32_t *words, int k0, int pos, uint32_t word, F set) {
+  const int rel = words ? (c.causal ? pos - k0 : 64) : (c.causal && pos < c.keys - 1 ? pos : c.keys - 1) - k0;
   if (!words) {
-    const int rel = (c.causal && pos < c.keys - 1 ? pos : c.keys - 1) - k0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) ok |= (row_of(r) <= rel ? 1u : 0u) << r;
-    return ok;
+    for (int r = 0; r < 16; ++r) set(r, row_of(r) <= rel);
+    return;
   }
-  const int rel = c.causal ? pos - k0 : 64;
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
     const u4 w = *(const u4 *)(words + k0 + g * 8);
+    if (c.prefix) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) ok |= ((w[e] >> 1) == doc && (g * 8 + e <= rel || (w[e] & 1u)) ? 1u : 0u) << (g * 4 + e);
+      for (int e = 0; e < 4; ++e) set(g * 4 + e, (w[e] == (word | 1u)) | ((w[e] == word) & (g * 8 + e <= rel)));
+    } else {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) set(g * 4 + e, (w[e] == word) & (g * 8 + e <= rel));
+    }
   }
-  return ok;
 }
 
-// document of a token as the comparisons want it: one that equals no key's where it has none
-__device__ __forceinline__ uint32_t document_of(uint32_t word) { return word == ATTN_NONE ? 0x80000000u : word >> 1; }
+// a query's document as the comparisons want it: one that equals no key's where it has none
+__device__ __forceinline__ uint32_t query_word(uint32_t word) { return word == ATTN_NONE ? ATTN_NOBODY : word & ~1u; }
 
 // ---------------------------------------------------------------------------------------------- scores
 // The score in powers of two from the product q.k.  CAP: the tanh is 1 - 2 / (1 + exp(2 x)), off by 2^-23 of the cap, not of itself, which is what
@@ -302,7 +311,7 @@ template <class T, int D, int NQ>
 struct QueryRows {
   s8 q[NQ][D / 16];
   int pos[NQ];
-  uint32_t doc[NQ];
+  uint32_t word[NQ];
   float slope2[NQ];
   int row[NQ], token[NQ], head[NQ];
   // rows first + 32 n + lane % 32; those behind the last take its place (they are not stored)
@@ -314,7 +323,7 @@ struct QueryRows {
       token[n] = divide(c.by_group, r);
       head[n] = h * c.group + r - token[n] * c.group;
       pos[n] = token[n] + c.offset;
-      doc[n] = c.q_words ? document_of(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token[n]]) : 0;
+      word[n] = c.q_words ? query_word(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token[n]]) : 0;
       slope2[n] = c.slopes ? c.slopes[head[n]] * 1.44269504088896341f : 0.f;
       operand(c, c.q, b, n, lane, q[n]);
     }
@@ -345,6 +354,12 @@ __device__ __forceinline__ void store4(uint16_t *p, int d, int width, float a, f
     for (int i = 0; i < 4; ++i)
       if (d + i < width) p[d + i] = T::down(v[i]);
   }
+}
+
+// what rounding took from them
+template <class T>
+__device__ __forceinline__ void store4_low(uint16_t *p, int d, int width, float a, float b, float e, float f) {
+  store4<T>(p, d, width, a - T::up(T::down(a)), b - T::up(T::down(b)), e - T::up(T::down(e)), f - T::up(T::down(f)));
 }
 
 // One softmax over blocks of keys: running reference (powers of two) and sum.  The reference follows the maximum only when that has grown by more than
@@ -392,11 +407,7 @@ struct Softmax {
             s[b][n][r] = v;
           }
         }
-        if (masked) {
-          const uint32_t ok = seen_by_query(c, words, k0 + b * 32 + h4, rows.pos[n], rows.doc[n]);
-#pragma unroll
-          for (int r = 0; r < 16; ++r) s[b][n][r] = (ok >> r) & 1u ? s[b][n][r] : -INFINITY;
-        }
+        if (masked) seen_keys(c, words, k0 + b * 32 + h4, rows.pos[n], rows.word[n], [&](int r, bool see) { s[b][n][r] = see ? s[b][n][r] : -INFINITY; });
       }
     const float unit = RAW ? c.to2 : 1.f;
     float most[NQ];
@@ -484,7 +495,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
   vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, (int)((int64_t)c.tiles * p.split / c.splits), (int)((int64_t)c.tiles * (p.split + 1) / c.splits));
+  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, p.split, c.splits, c.tiles);
   Softmax<T, D, NQ, CAP, SLOPE, KB> soft;
   soft.start();
 
@@ -540,6 +551,13 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
 #pragma unroll
       for (int g = 0; g < 4; ++g)
         store4<T>(out, d * 32 + g * 8 + h4, c.width, soft.o[d][n][g * 4] * f, soft.o[d][n][g * 4 + 1] * f, soft.o[d][n][g * 4 + 2] * f, soft.o[d][n][g * 4 + 3] * f);
+    if (!c.low) continue;
+    out = c.low + (((int64_t)p.b * c.tokens + rows.token[n]) * (c.kv_heads * c.group) + rows.head[n]) * c.width;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        store4_low<T>(out, d * 32 + g * 8 + h4, c.width, soft.o[d][n][g * 4] * f, soft.o[d][n][g * 4 + 1] * f, soft.o[d][n][g * 4 + 2] * f, soft.o[d][n][g * 4 + 3] * f);
   }
 #endif
 }
@@ -565,9 +583,8 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   kf.start(c.k, p.b, p.h, c.keys, c.dim, lane);
   vf.start(c.v, p.b, p.h, c.keys, c.dim, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
-  const int64_t shares = (int64_t)c.splits * WAVES, share = (int64_t)p.split * WAVES + wave;
   KeyWalk walk;
-  walk.start(c, p.b, 0, 32, 0, 32, (int)(c.tiles * share / shares), (int)(c.tiles * (share + 1) / shares));
+  walk.start(c, p.b, 0, 32, 0, 32, p.split * WAVES + wave, c.splits * WAVES, c.tiles);
   Softmax<T, D, 1, CAP, SLOPE, 1> soft;
   soft.start();
 
@@ -645,31 +662,20 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
     const float f = sum == 0.f ? 0.f : 1.f / sum;
     if (c.lse && d == 0) c.lse[(int64_t)p.hb * c.rows_pad + r] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
     store4<T>(c.y.p + p.b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+    if (c.low)
+      store4_low<T>(c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width, d, c.width, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
   }
 #endif
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// p and ds of one lane's 16 scores of a block, from the products q.k and dy.v
-template <int CAP, int SLOPE>
-__device__ __forceinline__ void gradient16(const AttnCall &c, f16 &s, f16 &dp, float slope2, float rel, const float *lse, const float *delta, int stride) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    float share, v = capped<CAP>(c, s[r], share);
-    if (SLOPE) v = biased(v, slope2, rel, r);
-    const float p = exp2_(v - lse[r * stride]);
-    float ds = p * (dp[r] - delta[r * stride]);
-    if (CAP) ds *= 4.f * (share - share * share);
-    s[r] = p;
-    dp[r] = ds;
-  }
-}
-__device__ __forceinline__ void mask16(f16 &p, f16 &ds, uint32_t ok) {
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    p[r] = (ok >> r) & 1u ? p[r] : 0.f;
-    ds[r] = (ok >> r) & 1u ? ds[r] : 0.f;
-  }
+// p and ds of a score from the products q.k and dy.v; bias: of the distance, in powers of two
+template <int CAP>
+__device__ __forceinline__ void gradient(const AttnCall &c, float &s, float &dp, float bias, float lse, float delta) {
+  float share, v = capped<CAP>(c, s, share);
+  s = exp2_(v - bias - lse);
+  dp = s * (dp - delta);
+  if (CAP) dp *= 4.f * (share - share * share);
 }
 
 template <class T, int D, int NQ, int CAP, int SLOPE>
@@ -690,16 +696,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
 #pragma unroll
   for (int n = 0; n < NQ; ++n) {
     rows.operand(c, c.dy, p.b, n, lane, dy[n]);
-    const int64_t at = (int64_t)p.hb * c.rows_pad + (rows.row[n] < c.rows ? rows.row[n] : c.rows - 1);
-    lse[n] = c.lse[at];
-    delta[n] = c.delta[at];
+    const int r = rows.row[n] < c.rows ? rows.row[n] : c.rows - 1;
+    const AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + r / 32];
+    lse[n] = block.lse[r % 32];
+    delta[n] = block.delta[r % 32];
   }
   Feed kf, vf;
   kf.start(c.k, p.b, p.h, c.keys, c.dim, tid);
   vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, 0, c.tiles);
+  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, 0, 1, c.tiles);
   f16 dq[D / 32][NQ];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d)
@@ -747,8 +754,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       s8 ds[NQ][2];
 #pragma unroll
       for (int n = 0; n < NQ; ++n) {
-        gradient16<CAP, SLOPE>(c, s[n], dp[n], rows.slope2[n], SLOPE ? (float)(rows.pos[n] - k0) : 0.f, &lse[n], &delta[n], 0);
-        if (masked) mask16(s[n], dp[n], seen_by_query(c, words, k0, rows.pos[n], rows.doc[n]));
+        const float rel = SLOPE ? (float)(rows.pos[n] - k0) : 0.f;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          float x = s[n][r], y = dp[n][r];
+          gradient<CAP>(c, x, y, SLOPE ? rows.slope2[n] * fabsf(rel - (float)row_of(r)) : 0.f, lse[n], delta[n]);
+          dp[n][r] = y;
+        }
+        if (masked) seen_keys(c, words, k0, rows.pos[n], rows.word[n], [&](int r, bool see) { dp[n][r] = see ? dp[n][r] : 0.f; });
         ds[n][0] = pack8<T>(dp[n], 0);
         ds[n][1] = pack8<T>(dp[n], 8);
       }
@@ -776,16 +789,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
 #endif
 }
 
-// Tiles of 64 rows that see some of a wavefront's keys, as KeyWalk
+// Blocks of 32 rows that see some of a workgroup's keys, as KeyWalk
 struct RowWalk {
   int group_from, group_to, wave_from, wave_to;           // keys
   Range group_docs, wave_docs;
   const AttnTile *tiles;                    // of the queries' tokens
-  int at, end;
+  int first, step, at, end;
   uint64_t visit, mine, mask, none;
   int tile;
   bool run, masked, some_none;
-  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_key, int group_keys, int wave_key, int wave_keys, int first, int end_) {
+  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_key, int group_keys, int wave_key, int wave_keys, int first_, int step_, int end_) {
     group_from = group_key;
     group_to = group_key + group_keys - 1 < c.keys ? group_key + group_keys - 1 : c.keys - 1;
     wave_from = wave_key < c.keys ? wave_key : c.keys - 1;
@@ -797,7 +810,9 @@ struct RowWalk {
       group_docs = keys_of(k, group_from, group_to);
       wave_docs = keys_of(k, wave_from, wave_to);
     }
-    at = first - 64;
+    first = first_;
+    step = step_;
+    at = -64;
     end = end_;
     visit = 0;
   }
@@ -814,10 +829,10 @@ struct RowWalk {
   __device__ __forceinline__ void next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if (at >= end) { tile = -1; return; }
-      const int t = at + lane;
-      const bool there = t < end;
-      const int r0 = there ? t * ATTN_TILE : 0, r1 = r0 + ATTN_TILE - 1 < c.rows ? r0 + ATTN_TILE - 1 : c.rows - 1;
+      if ((int64_t)at * step + first >= end) { tile = -1; return; }
+      const int64_t tt = (int64_t)(at + lane) * step + first;
+      const bool there = tt < end;
+      const int r0 = there ? (int)tt * 32 : 0, r1 = r0 + 31 < c.rows ? r0 + 31 : c.rows - 1;
       const int t0 = divide(c.by_group, r0), t1 = divide(c.by_group, r1);
       Range q{0, 0, 0};
       if (tiles) q = range_of(tiles, t0, t1);
@@ -827,91 +842,75 @@ struct RowWalk {
       sees(c, from, to, q, wave_from, wave_to, wave_docs, wave_some, wave_all);
       visit = __ballot(there && some);
       mine = __ballot(there && wave_some);
-      mask = __ballot(there && !(wave_all && r0 + ATTN_TILE <= c.rows));
+      mask = __ballot(there && !(wave_all && r0 + 32 <= c.rows));
       none = __ballot(there && tiles && (q.flags & ATTN_SOME_NONE));
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    tile = at + i;
+    tile = (at + i) * step + first;
     run = (mine >> i) & 1;
     masked = (mask >> i) & 1;
     some_none = (none >> i) & 1;
   }
 };
 
-// Of the rows r0 + row_of(r): those that see the key, a bit each
-__device__ __forceinline__ uint32_t seen_by_rows(const AttnCall &c, const uint32_t *q_words, int r0, int key, uint32_t word) {
-  uint32_t ok = 0;
-#pragma unroll
-  for (int r = 0; r < 16; ++r) {
-    const int row = r0 + row_of(r), token = divide(c.by_group, row < c.rows ? row : c.rows - 1);
-    bool see = row < c.rows && key < c.keys;
-    const bool before = !c.causal || key <= token + c.offset;
-    if (q_words) see = see && document_of(q_words[token]) == word >> 1 && (before || (word & 1u));
-    else see = see && before;
-    ok |= (see ? 1u : 0u) << r;
-  }
-  return ok;
-}
-
-template <class T, int D, int NK, int CAP, int SLOPE>
-__global__ void __launch_bounds__(256) k_dkdv(const AttnCall c) {
+// A wavefront has 32 keys: their operands, and 2 x 32 x D sums, which with the scores fill half of a lane's registers (two wavefronts a SIMD) if the
+// values stay in shared memory: they are read from there a block, as the queries and dy are.
+template <class T, int D, int CAP, int SLOPE>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k_dkdv(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4, NT = 64 * WAVES;
-  typedef RowFeed<D, ATTN_TILE, NT> Feed;
-  constexpr int STAGE = 2 * Feed::BYTES + 1024;            // queries, dy, lse and delta of 64 rows
-  __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE];
-  lds_char *lds = (lds_char *)shared;
+  constexpr int WAVES = 4, NT = 64 * WAVES, KEYS = WAVES * 32;
+  typedef RowFeed<D, 32, NT> Feed;
+  typedef KeyFeed<D, KEYS, NT> Values;
+  typedef __attribute__((address_space(3))) const AttnRows lds_rows;
+  constexpr int STAGE = 2 * Feed::BYTES + 1024;            // queries, dy and what is known of 32 rows
+  static_assert(sizeof(AttnRows) <= 1024, "a wavefront brings it in one load");
+  __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE + Values::BYTES];
+  lds_char *lds = (lds_char *)shared, *values = lds + 2 * STAGE;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.key_tiles, false);
-  const int key0 = p.tile * (WAVES * NK * 32), wave_key = key0 + wave * NK * 32;
+  const int key0 = p.tile * KEYS, wave_key = key0 + wave * 32;
   const int h4 = (lane >> 5) * 4;
-  // this lane's keys and values
-  s8 k[NK][D / 16], v[NK][D / 16];
-  int key[NK];
-  uint32_t word[NK];
-#pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    key[n] = wave_key + n * 32 + (lane & 31);
-    const int j = key[n] < c.keys ? key[n] : c.keys - 1;
-    word[n] = c.k_words ? c.k_words[(int64_t)p.b * c.tiles * ATTN_TILE + j] : 0;
-    const uint16_t *kp = c.k.p + p.b * c.k.batch + j * c.k.token + p.h * c.k.head, *vp = c.v.p + p.b * c.v.batch + j * c.v.token + p.h * c.v.head;
+  // this lane's key
+  const int key = wave_key + (lane & 31), there = key < c.keys ? key : c.keys - 1;
+  const uint32_t word = c.k_words ? c.k_words[(int64_t)p.b * c.tiles * ATTN_TILE + there] : 0;
+  s8 k[D / 16];
+  {
+    const uint16_t *kp = c.k.p + p.b * c.k.batch + there * c.k.token + p.h * c.k.head;
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       const int d = i * 16 + (lane >> 5) * 8;
-      k[n][i] = d < c.dim ? *(const s8 *)(kp + d) : s8{};
-      v[n][i] = d < c.dim ? *(const s8 *)(vp + d) : s8{};
+      k[i] = d < c.dim ? *(const s8 *)(kp + d) : s8{};
     }
+    Values vf;
+    vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
+    vf.load(key0, lds0 + 2 * STAGE, wave);
   }
   Feed qf, df;
   qf.start(c.q, p.b, p.h * c.group);
   df.start(c.dy, p.b, p.h * c.group);
   const uint32_t *q_words = c.q_words ? c.q_words + (int64_t)p.b * c.q_tile_count * ATTN_TILE : nullptr;
-  const float *lse_at = c.lse + (int64_t)p.hb * c.rows_pad, *delta_at = c.delta + (int64_t)p.hb * c.rows_pad;
+  const AttnRows *row_data = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
 
-  // this part of the rows that may see the keys: without a prefix, those from the first key's position on
-  const int all_tiles = (c.rows + ATTN_TILE - 1) / ATTN_TILE;
-  int64_t first = 0;
-  if (c.causal && !c.k_words) {
-    const int64_t token = key0 - c.offset;
-    if (token > 0) first = token * c.group / ATTN_TILE;
-    if (first > all_tiles) first = all_tiles;
+  // without a prefix a causal mask leaves the rows from the first key's position on
+  const int blocks = (c.rows + 31) / 32;
+  int first = 0;
+  if (c.causal && !c.prefix && key0 > c.offset) {
+    const int64_t f = (int64_t)(key0 - c.offset) * c.group / 32;
+    first = f < blocks ? (int)f : blocks;
   }
   RowWalk walk;
-  walk.start(c, p.b, key0, WAVES * NK * 32, wave_key, NK * 32, (int)(first + (all_tiles - first) * p.split / c.splits), (int)(first + (all_tiles - first) * (p.split + 1) / c.splits));
-  f16 dk[D / 32][NK], dv[D / 32][NK];
+  walk.start(c, p.b, key0, KEYS, wave_key, 32, first + p.split, c.splits, blocks);
+  f16 dk[D / 32], dv[D / 32];
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int n = 0; n < NK; ++n) dk[d][n] = dv[d][n] = f16{};
+  for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f16{};
 
   const auto load = [&](int tile, int slot) {
     const uint32_t at = lds0 + slot * STAGE;
-    qf.load(c, tile * ATTN_TILE, at, wave, tid);
-    df.load(c, tile * ATTN_TILE, at + Feed::BYTES, wave, tid);
-    if (wave == 0) load_lds4(descriptor(lse_at + tile * ATTN_TILE, ATTN_TILE * 4), lane * 4, at + 2 * Feed::BYTES);
-    if (wave == 1) load_lds4(descriptor(delta_at + tile * ATTN_TILE, ATTN_TILE * 4), lane * 4, at + 2 * Feed::BYTES + 512);
+    qf.load(c, tile * 32, at, wave, tid);
+    df.load(c, tile * 32, at + Feed::BYTES, wave, tid);
+    if (wave == 0) load_lds16(descriptor(row_data + tile, sizeof(AttnRows)), lane * 16, at + 2 * Feed::BYTES);
   };
   int slot = 0;
   walk.next(c, lane);
@@ -923,8 +922,8 @@ __global__ void __launch_bounds__(256) k_dkdv(const AttnCall c) {
     arrived();
     lds_char *here = lds + slot * STAGE;
     if (some_none) {
-      for (int idx = tid; idx < ATTN_TILE * Shape<D>::CHUNKS; idx += NT) {
-        const int r = tile * ATTN_TILE + idx / Shape<D>::CHUNKS;
+      for (int idx = tid; idx < 32 * Shape<D>::CHUNKS; idx += NT) {
+        const int r = tile * 32 + idx / Shape<D>::CHUNKS;
         if (r < c.rows && q_words[divide(c.by_group, r)] == ATTN_NONE) {
           *(__attribute__((address_space(3))) u4 *)(here + idx * 16) = u4{0, 0, 0, 0};
           *(__attribute__((address_space(3))) u4 *)(here + Feed::BYTES + idx * 16) = u4{0, 0, 0, 0};
@@ -935,92 +934,78 @@ __global__ void __launch_bounds__(256) k_dkdv(const AttnCall c) {
     slot ^= 1;
     if (walk.tile >= 0) load(walk.tile, slot);
     if (!run) continue;
+    const lds_char *queries = here, *dys = here + Feed::BYTES;
+    lds_rows *known = (lds_rows *)(here + 2 * Feed::BYTES);
+    f16 s = {}, dp = {};
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int r0 = tile * ATTN_TILE + b * 32;
-      f16 s[NK], dp[NK];
+    for (int i = 0; i < D / 16; ++i) s = T::mfma(row_fragment<D>(queries, 0, i, lane), k[i], s);
 #pragma unroll
-      for (int n = 0; n < NK; ++n) s[n] = dp[n] = f16{};
+    for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, 0, i, lane), row_fragment<D>(values, wave * 32, i, lane), dp);
 #pragma unroll
-      for (int i = 0; i < D / 16; ++i) {
-        const s8 q = row_fragment<D>(here, b * 32, i, lane), y = row_fragment<D>(here + Feed::BYTES, b * 32, i, lane);
+    for (int g = 0; g < 4; ++g) {
+      const int r0 = g * 8 + h4;
+      const f4 lse = *(__attribute__((address_space(3))) const f4 *)&known->lse[r0], delta = *(__attribute__((address_space(3))) const f4 *)&known->delta[r0];
+      f4 bias = f4{0.f, 0.f, 0.f, 0.f};
+      if (SLOPE) {
+        const f4 slope2 = *(__attribute__((address_space(3))) const f4 *)&known->slope2[r0];
+        const i4 pos = *(__attribute__((address_space(3))) const i4 *)&known->pos[r0];
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-          s[n] = T::mfma(q, k[n][i], s[n]);
-          dp[n] = T::mfma(y, v[n][i], dp[n]);
-        }
+        for (int e = 0; e < 4; ++e) bias[e] = slope2[e] * fabsf((float)(pos[e] - key));
       }
-      float lse[16], delta[16];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        float x = s[g * 4 + e], y = dp[g * 4 + e];
+        gradient<CAP>(c, x, y, bias[e], lse[e], delta[e]);
+        s[g * 4 + e] = x;
+        dp[g * 4 + e] = y;
+      }
+    }
+    if (masked) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        const f4 l = *(const __attribute__((address_space(3))) f4 *)(here + 2 * Feed::BYTES + (b * 32 + g * 8 + h4) * 4);
-        const f4 e = *(const __attribute__((address_space(3))) f4 *)(here + 2 * Feed::BYTES + 512 + (b * 32 + g * 8 + h4) * 4);
+        const i4 last = *(__attribute__((address_space(3))) const i4 *)&known->last[g * 8 + h4];
+        const u4 words = *(__attribute__((address_space(3))) const u4 *)&known->word[g * 8 + h4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { lse[g * 4 + i] = l[i]; delta[g * 4 + i] = e[i]; }
-      }
-      s8 pp[NK][2], ds[NK][2];
-#pragma unroll
-      for (int n = 0; n < NK; ++n) {
-        if (SLOPE) {                        // a row's own slope and distance
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            const int row = r0 + h4 + row_of(r), rr = row < c.rows ? row : c.rows - 1, t = divide(c.by_group, rr);
-            const float bias = c.slopes[p.h * c.group + rr - t * c.group] * 1.44269504088896341f * fabsf((float)(t + c.offset - key[n]));
-            float share, x = capped<CAP>(c, s[n][r], share) - bias;
-            const float w = exp2_(x - lse[r]);
-            float g = w * (dp[n][r] - delta[r]);
-            if (CAP) g *= 4.f * (share - share * share);
-            s[n][r] = w;
-            dp[n][r] = g;
-          }
-        } else {
-          gradient16<CAP, 0>(c, s[n], dp[n], 0.f, 0.f, lse, delta, 1);
-        }
-        if (masked) mask16(s[n], dp[n], seen_by_rows(c, q_words, r0 + h4, key[n], word[n]));
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-          pp[n][i] = pack8<T>(s[n], i * 8);
-          ds[n][i] = pack8<T>(dp[n], i * 8);
+        for (int e = 0; e < 4; ++e) {
+          const bool before = key <= last[e], see = q_words ? (word == (words[e] | 1u)) | ((word == words[e]) & before) : before;
+          s[g * 4 + e] = see ? s[g * 4 + e] : 0.f;
+          dp[g * 4 + e] = see ? dp[g * 4 + e] : 0.f;
         }
       }
+    }
 #pragma unroll
-      for (int i = 0; i < 2; ++i)
+    for (int i = 0; i < 2; ++i) {
+      const s8 w = pack8<T>(s, i * 8), ds = pack8<T>(dp, i * 8);
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const s8 y = column_fragment<D>(here + Feed::BYTES, b * 32 + i * 16, d, lane), q = column_fragment<D>(here, b * 32 + i * 16, d, lane);
-#pragma unroll
-          for (int n = 0; n < NK; ++n) {
-            dv[d][n] = T::mfma(y, pp[n][i], dv[d][n]);
-            dk[d][n] = T::mfma(q, ds[n][i], dk[d][n]);
-          }
-        }
+      for (int d = 0; d < D / 32; ++d) {
+        dv[d] = T::mfma(column_fragment<D>(dys, i * 16, d, lane), w, dv[d]);
+        dk[d] = T::mfma(column_fragment<D>(queries, i * 16, d, lane), ds, dk[d]);
+      }
     }
   }
-#pragma unroll
-  for (int n = 0; n < NK; ++n) {
-    if (key[n] >= c.keys) continue;
-    if (c.splits > 1) {
-      const int64_t at = (((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + key[n]) * c.width4;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const int e = d * 32 + g * 8 + h4;
-          if (e >= c.width4) continue;
-          *(f4 *)(c.part + at + e) = f4{dk[d][n][g * 4], dk[d][n][g * 4 + 1], dk[d][n][g * 4 + 2], dk[d][n][g * 4 + 3]} * c.scale;
-          *(f4 *)(c.part2 + at + e) = f4{dv[d][n][g * 4], dv[d][n][g * 4 + 1], dv[d][n][g * 4 + 2], dv[d][n][g * 4 + 3]};
-        }
-      continue;
-    }
-    uint16_t *ko = c.dk.p + p.b * c.dk.batch + key[n] * c.dk.token + p.h * c.dk.head, *vo = c.dv.p + p.b * c.dv.batch + key[n] * c.dv.token + p.h * c.dv.head;
+  if (walk.tile < 0) waited<0>();           // the values, where no block was visited
+  if (key >= c.keys) return;
+  if (c.splits > 1) {
+    const int64_t at = (((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + key) * c.width4;
 #pragma unroll
     for (int d = 0; d < D / 32; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
-        store4<T>(ko, d * 32 + g * 8 + h4, c.width, dk[d][n][g * 4] * c.scale, dk[d][n][g * 4 + 1] * c.scale, dk[d][n][g * 4 + 2] * c.scale, dk[d][n][g * 4 + 3] * c.scale);
-        store4<T>(vo, d * 32 + g * 8 + h4, c.width, dv[d][n][g * 4], dv[d][n][g * 4 + 1], dv[d][n][g * 4 + 2], dv[d][n][g * 4 + 3]);
+        const int e = d * 32 + g * 8 + h4;
+        if (e >= c.width4) continue;
+        *(f4 *)(c.part + at + e) = f4{dk[d][g * 4], dk[d][g * 4 + 1], dk[d][g * 4 + 2], dk[d][g * 4 + 3]} * c.scale;
+        *(f4 *)(c.part2 + at + e) = f4{dv[d][g * 4], dv[d][g * 4 + 1], dv[d][g * 4 + 2], dv[d][g * 4 + 3]};
       }
+    return;
   }
+  uint16_t *ko = c.dk.p + p.b * c.dk.batch + key * c.dk.token + p.h * c.dk.head, *vo = c.dv.p + p.b * c.dv.batch + key * c.dv.token + p.h * c.dv.head;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      store4<T>(ko, d * 32 + g * 8 + h4, c.width, dk[d][g * 4] * c.scale, dk[d][g * 4 + 1] * c.scale, dk[d][g * 4 + 2] * c.scale, dk[d][g * 4 + 3] * c.scale);
+      store4<T>(vo, d * 32 + g * 8 + h4, c.width, dv[d][g * 4], dv[d][g * 4 + 1], dv[d][g * 4 + 2], dv[d][g * 4 + 3]);
+    }
 #endif
 }
 
@@ -1033,7 +1018,7 @@ bool launch(const AttnCall &c, const AttnLaunch &l) {
   if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, N, CAP, SLOPE>), grid, block, 0, st, c);
   else if constexpr (WHAT == FEW) hipLaunchKernelGGL((k_forward_few<T, D, CAP, SLOPE>), grid, block, 0, st, c);
   else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, N, CAP, SLOPE>), grid, block, 0, st, c);
-  else hipLaunchKernelGGL((k_dkdv<T, D, N, CAP, SLOPE>), grid, block, 0, st, c);
+  else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE>), grid, block, 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
 template <class T, int WHAT, int D, int N>

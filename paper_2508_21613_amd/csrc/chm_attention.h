@@ -23,7 +23,7 @@ enum { ATTN_SOME_NONE = 1, ATTN_SOME_PREFIX = 2, ATTN_ALL_PREFIX = 4 };
 constexpr uint32_t ATTN_NONE = 0xfffffffeu;
 constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles are laid out for whole ones
 
-// What the backward pass knows of 32 rows, one value after the other, rounded up to whole blocks (rows behind the last see nothing)
+// What the kernel of dq leaves to that of dk and dv about 32 rows, one value after the other (rows behind the last see nothing)
 struct AttnRows {
   float lse[32];                           // log2 of the sum of powers of two; +inf: the row sees nothing
   float delta[32];                         // dy . y
@@ -36,12 +36,14 @@ constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // with or without the lowest
 
 struct AttnCall {
   AttnInput q, k, v, dy;
+  AttnInput y_in;                          // the forward pass's result, at any alignment
   AttnOutput y, dq, dk, dv;
   int32_t batch, tokens, keys, kv_heads, group, dim, width;      // dim: elements of the inputs' rows; width: of the outputs' (dim less what packing added)
   int32_t rows, rows_pad;                  // tokens * group, rounded up to whole tiles
   int32_t offset;                          // keys - tokens: position of the first query
   int32_t causal, tiles;                   // tiles of 64 keys
   AttnDivide by_group;
+  int32_t even_group;                      // 32 is a multiple of the group
   float scale;                             // of the gradients dq and dk
   float to2;                               // score in powers of two: scale * log2(e)
   float tanh2, cap2;                       // 2 scale / cap * log2(e); cap * log2(e)
@@ -61,8 +63,8 @@ struct AttnCall {
   int32_t row_tiles, key_tiles, heads_abreast;
 };
 
-// Kernels of a pass.  tile: 0 or 1, 32 or 64 rows (keys) a wavefront.  false: HIP failed.
-struct AttnLaunch { int32_t dim, tile; uint32_t groups; void *stream; };
+// Kernels of a pass; dim: 64 or 128.  false: HIP failed.
+struct AttnLaunch { int32_t dim; uint32_t groups; void *stream; };
 bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_forward_f16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_dq_bf16(const AttnCall &c, const AttnLaunch &l);

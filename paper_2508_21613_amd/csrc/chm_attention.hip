@@ -1,7 +1,7 @@
-// Attention: what its passes consist of, the small kernels around the tiles (documents, packing, rows, joined sums), the entry points.
+// Attention: what its passes consist of, the small kernels around the tiles (documents, packing, joined sums), the entry points.
 //
 //   forward    [pack] [documents] tiles [join]
-//   backward   [pack] [documents] rows (delta = dy.y), dq, dk and dv [join]
+//   backward   [pack] [documents] dq (and delta = dy.y), dk and dv [join]
 // dq and dk with dv are kernels of their own, each of which works out the scores again: seven products in place of five, but no sums that several
 // workgroups add to, so that the same inputs give the same bits.
 #include <hip/hip_runtime.h>
@@ -83,54 +83,6 @@ __global__ void __launch_bounds__(256) k_pack(PackCall c) {
       if (d + e < c.dim) v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
   }
   *(Words *)(m.out + w * 8) = v;
-}
-
-// ---------------------------------------------------------------------------------------------- rows
-// What the backward pass wants to know of every row: delta = dy.y, by 16 lanes a row, and what tells which keys it sees.  y is taken with what its
-// rounding took from it: where few keys share a row, dy.v and delta are near each other, and 2^-9 of y would be 1.5 times the error that the
-// gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3 without, 2.4e-3 with).
-struct RowsCall { AttnInput dy, y; };
-template <int DT>
-__global__ void __launch_bounds__(256) k_rows(const AttnCall c, const RowsCall in, int64_t all) {
-  const int64_t i = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
-  if (i >= all) return;                    // all 16 lanes of a row
-  const int d = (threadIdx.x & 15) * 8;
-  const int64_t hb = i / c.rows_pad, seq = hb / c.kv_heads;
-  const int r = (int)(i - hb * c.rows_pad), h = (int)(hb - seq * c.kv_heads);
-  const int t = r / c.group, head = h * c.group + r - t * c.group;
-  const bool there = r < c.rows;
-  float sum = 0.f;
-  if (there && d < c.width) {
-    const char *a = (const char *)(in.dy.p + seq * in.dy.batch + t * in.dy.token + head * in.dy.head + d);
-    const char *b = (const char *)(in.y.p + seq * in.y.batch + t * in.y.token + head * in.y.head + d);
-    const char *l = (const char *)(c.low + ((seq * c.tokens + t) * (c.kv_heads * c.group) + head) * c.width + d);
-    if (d + 8 <= c.width) {
-      float v[8], w[8], x[8];
-      Lane<DT>::up(load16(a), v);
-      Lane<DT>::up(load16(b), w);
-      Lane<DT>::up(load16(l), x);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(v[e], w[e] + x[e], sum);
-    } else {
-      for (int e = 0; d + e < c.width; ++e) sum = fmaf(Lane<DT>::one(a + e * 2), Lane<DT>::one(b + e * 2) + Lane<DT>::one(l + e * 2), sum);
-    }
-  }
-#pragma unroll
-  for (int x = 8; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-  if (d != 0) return;
-  AttnRows &block = c.row_data[i / 32];
-  const int at = r % 32, pos = t + c.offset;
-  block.delta[at] = sum;
-  block.lse[at] = there ? c.lse[i] : INFINITY;
-  block.last[at] = !there ? INT32_MIN : c.causal ? pos : INT32_MAX;
-  uint32_t word = there ? 0 : ATTN_NOBODY;
-  if (there && c.q_words) {
-    word = c.q_words[seq * c.q_tile_count * ATTN_TILE + t];
-    word = word == ATTN_NONE ? ATTN_NOBODY : word & ~1u;
-  }
-  block.word[at] = word;
-  block.slope2[at] = there && c.slopes ? c.slopes[head] * 1.44269504088896341f : 0.f;
-  block.pos[at] = pos;
 }
 
 // ---------------------------------------------------------------------------------------------- joins
@@ -253,6 +205,7 @@ struct Pass {
     c.tiles = (int32_t)up(a->keys, ATTN_TILE);
     c.q_tile_count = (int32_t)up(a->tokens, ATTN_TILE);
     c.by_group = divide_by(G);
+    c.even_group = 32 % G == 0;
     const double log2e = 1.4426950408889634;
     c.scale = a->scale;
     c.to2 = (float)(a->scale * log2e);
@@ -361,7 +314,7 @@ struct Pass {
     if (a->batch == 0 || a->tokens == 0) return;
     inputs(nullptr);
     chosen.few = rows() <= FEW_ROWS;
-    AttnLaunch l{chosen.dim, 0, 0, st};
+    AttnLaunch l{chosen.dim, 0, st};
     if (chosen.few) {
       chosen.forward_rows = FEW_ROWS;
       c.splits = few_splits(heads(), c.tiles, chosen.dim);
@@ -392,25 +345,17 @@ struct Pass {
     if (a->batch == 0) return;
     const int64_t B = a->batch, T = a->tokens, K = a->keys;
     c.dy = input(g->dy, g->dy_stride, B, T, a->heads);
-    const AttnInput dy = c.dy, y = input(g->y, g->y_stride, B, T, a->heads);
+    c.y_in = input(g->y, g->y_stride, B, T, a->heads);
     c.dq = output(g->dq, g->dq_stride, B, T, a->heads);
     c.dk = output(g->dk, g->dk_stride, B, K, a->kv_heads);
     c.dv = output(g->dv, g->dv_stride, B, K, a->kv_heads);
     inputs(g);
-    const int64_t all = heads() * c.rows_pad;
-    c.row_data = (AttnRows *)arena.take((uint64_t)(all / 32) * sizeof(AttnRows));
-    const uint32_t row_groups = threads(up(all, 16), 256);
-    if (run && fits && row_groups) {
-      const RowsCall in{dy, y};
-      if (bf16()) hipLaunchKernelGGL(k_rows<CHM_BF16>, dim3(row_groups), dim3(256), 0, st, c, in, all);
-      else hipLaunchKernelGGL(k_rows<CHM_F16>, dim3(row_groups), dim3(256), 0, st, c, in, all);
-      ok = ok && hipGetLastError() == hipSuccess;
-    }
+    c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
     if (T > 0) {
       chosen.dq_rows = 128;
       c.row_tiles = (int32_t)up(rows(), chosen.dq_rows);
       c.splits = 1;
-      const AttnLaunch l{chosen.dim, 0, threads(heads() * c.row_tiles, 256), st};
+      const AttnLaunch l{chosen.dim, threads(heads() * c.row_tiles, 256), st};
       if (run && fits) ok = ok && (bf16() ? attn_dq_bf16 : attn_dq_f16)(c, l);
     }
     if (K > 0) {
@@ -423,7 +368,7 @@ struct Pass {
         c.part = (float *)arena.take((uint64_t)(c.splits * words) * 16);
         c.part2 = (float *)arena.take((uint64_t)(c.splits * words) * 16);
       }
-      const AttnLaunch l{chosen.dim, 0, threads(heads() * c.key_tiles * c.splits, 256), st};
+      const AttnLaunch l{chosen.dim, threads(heads() * c.key_tiles * c.splits, 256), st};
       const uint32_t joins = threads(up(words, 256), 256);
       if (!run || !fits) return;
       ok = ok && (bf16() ? attn_dkdv_bf16 : attn_dkdv_f16)(c, l);

@@ -76,13 +76,17 @@ template <class T> __device__ __forceinline__ s8 pack8(const f16 &v, int from) {
 __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r >> 2); }
 
 // ---------------------------------------------------------------------------------------------- shared memory
-// Rows of D elements (64, or up to 128 in rows of 128).  Rows read: 16 lanes, 16 rows, one chunk each.  Transposing reads: 16 lanes, 4 rows,
-// 2 chunks of each; the two halves of the wavefront 4 rows apart.  With 8 chunks a row, two rows fill the banks.
+// Rows of D elements (64, or up to 128 in rows of 128), as direct loads leave them: 1 KiB of whole rows by each.  The banks give 256 bytes a cycle: 16 lanes of
+// a read of rows, one chunk of 16 rows each, or 32 lanes of a transposing read, 4 chunks of 4 rows.  The chunks of a row are exchanged in fours by
+// the row's last two bits, and 16 bytes between the loads do the rest: so most of a read's address is a constant.  With 8 chunks a row, where two rows
+// fill the banks, they are exchanged by three bits of the row.
 template <int D> struct Shape {
-  enum { PITCH = D == 64 ? 128 : 256, CHUNKS = PITCH / 16, STEPS = D / 16, BLOCKS = D / 32 };
+  enum { PITCH = D == 64 ? 128 : 256, CHUNKS = PITCH / 16, GROUP = 1024 / PITCH, GROUP_BYTES = 1024 + (D == 64 ? 0 : 16) };
   static __device__ __forceinline__ uint32_t swizzle(uint32_t row) {
-    return PITCH == 128 ? (row & 6u) | ((row >> 3) & 1u) : ((row & 7u) << 1) | ((row >> 3) & 1u);
+    return PITCH == 128 ? ((row & 2u) << 1) | ((row >> 2) & 3u) : (row & 3u) << 2;
   }
+  static __device__ __forceinline__ constexpr uint32_t row_at(uint32_t row) { return row / GROUP * GROUP_BYTES + row % GROUP * PITCH; }
+  static constexpr int bytes(int rows) { return rows / GROUP * GROUP_BYTES; }
 };
 
 __device__ __forceinline__ i4 descriptor(const void *p, uint32_t bytes) {
@@ -110,87 +114,100 @@ __device__ __forceinline__ void arrived() {
   asm volatile("" ::: "memory");
 }
 
-// ROWS rows of keys or values to shared memory by NT threads; rows from `size` on and chunks from dim on arrive as zeros
-template <int D, int ROWS, int NT>
+// ROWS rows of keys or values to shared memory by WAVES wavefronts; rows from `size` on and chunks from dim on arrive as zeros.
+template <int D, int ROWS, int WAVES>
 struct KeyFeed {
   typedef Shape<D> S;
-  enum { BYTES = ROWS * S::PITCH, LOADS = BYTES / 16 / NT };
+  enum { BYTES = S::bytes(ROWS), LOADS = ROWS / S::GROUP / WAVES };
   const char *base;
   int64_t token;                           // bytes from one to the next
   int32_t size, dim;
   uint32_t off[LOADS];
-  __device__ __forceinline__ void start(const AttnInput &in, int b, int h, int size_, int dim_, int tid) {
+  __device__ __forceinline__ void start(const AttnInput &in, int b, int h, int size_, int dim_, int wave, int lane) {
     base = (const char *)(in.p + b * in.batch + h * in.head);
     token = in.token * 2;
     size = size_;
     dim = dim_;
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) {
-      const uint32_t idx = i * NT + tid, row = idx / S::CHUNKS, chunk = (idx % S::CHUNKS) ^ S::swizzle(row);
+      const uint32_t idx = (i * WAVES + wave) * 64 + lane, row = idx / S::CHUNKS, chunk = (idx % S::CHUNKS) ^ S::swizzle(row);
       off[i] = (int)chunk * 8 >= dim ? OUT : row * (uint32_t)token + chunk * 16;
     }
   }
-  // first: the first row (uniform)
+  // the rows from `first` on (uniform)
   __device__ __forceinline__ void load(int first, uint32_t lds, int wave) const {
     const int left = size - first < ROWS ? size - first : ROWS;
     const i4 rsrc = descriptor(base + first * token, left > 0 ? (uint32_t)((left - 1) * (int32_t)token + dim * 2) : 0);
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) load_lds16(rsrc, off[i], lds + (i * NT + wave * 64) * 16);
+    for (int i = 0; i < LOADS; ++i) load_lds16(rsrc, off[i], lds + (i * WAVES + wave) * S::GROUP_BYTES);
   }
 };
 
-// ROWS rows of queries or dy
-template <int D, int ROWS, int NT>
+// ROWS rows of queries or dy.  Where the group divides 32 every block of rows starts with a token, and a lane's offsets stay what they are; worked out
+// anew for every block they cost a sixth of the time of dk and dv.
+template <int D, int ROWS, int WAVES>
 struct RowFeed {
   typedef Shape<D> S;
-  enum { BYTES = ROWS * S::PITCH, LOADS = BYTES / 16 / NT };
+  enum { BYTES = S::bytes(ROWS), LOADS = ROWS / S::GROUP / WAVES };
   const char *base;
   int64_t token;
-  uint32_t head;
-  __device__ __forceinline__ void start(const AttnInput &in, int b, int first_head) {
+  uint32_t head, off[LOADS];
+  __device__ __forceinline__ void start(const AttnCall &c, const AttnInput &in, int b, int first_head, int wave, int lane) {
     base = (const char *)(in.p + b * in.batch + first_head * in.head);
     token = in.token * 2;
     head = (uint32_t)in.head * 2;
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) off[i] = offset(c, i, 0, 0, wave, lane);
   }
-  __device__ __forceinline__ void load(const AttnCall &c, int first, uint32_t lds, int wave, int tid) const {
+  __device__ __forceinline__ uint32_t offset(const AttnCall &c, int i, int first, int t0, int wave, int lane) const {
+    const uint32_t idx = (i * WAVES + wave) * 64 + lane, row = idx / S::CHUNKS, chunk = (idx % S::CHUNKS) ^ S::swizzle(row);
+    const int r = first + (int)row, t = divide(c.by_group, r), g = r - t * c.group;
+    return r >= c.rows || (int)chunk * 8 >= c.dim ? OUT : (uint32_t)(t - t0) * (uint32_t)token + (uint32_t)g * head + chunk * 16;
+  }
+  // the rows from `first` on (uniform)
+  __device__ __forceinline__ void load(const AttnCall &c, int first, uint32_t lds, int wave, int lane) const {
     const int t0 = divide(c.by_group, first);
     const i4 rsrc = descriptor(base + t0 * token, OUT - 64);
+    if (c.even_group && first + ROWS <= c.rows) {
 #pragma unroll
-    for (int i = 0; i < LOADS; ++i) {
-      const uint32_t idx = i * NT + tid, row = idx / S::CHUNKS, chunk = (idx % S::CHUNKS) ^ S::swizzle(row);
-      const int r = first + (int)row, t = divide(c.by_group, r), g = r - t * c.group;
-      const uint32_t off = (uint32_t)(t - t0) * (uint32_t)token + (uint32_t)g * head + chunk * 16;
-      load_lds16(rsrc, r >= c.rows || (int)chunk * 8 >= c.dim ? OUT : off, lds + (i * NT + wave * 64) * 16);
+      for (int i = 0; i < LOADS; ++i) load_lds16(rsrc, off[i], lds + (i * WAVES + wave) * S::GROUP_BYTES);
+    } else {
+#pragma unroll
+      for (int i = 0; i < LOADS; ++i) load_lds16(rsrc, offset(c, i, first, t0, wave, lane), lds + (i * WAVES + wave) * S::GROUP_BYTES);
     }
   }
 };
 
-// 8 elements (16 k + 8 h ..) of row `first` + lane % 32: operand of a product over a row's elements
+// 8 elements (16 k + 8 h ..) of row `first` + lane % 32: operand of a product over a row's elements.  first: a multiple of 32
 template <int D>
 __device__ __forceinline__ s8 row_fragment(const lds_char *lds, int first, int k, int lane) {
-  const uint32_t row = first + (lane & 31), chunk = (k * 2 + (lane >> 5)) ^ Shape<D>::swizzle(row);
-  return *(const __attribute__((address_space(3))) s8 *)(lds + row * Shape<D>::PITCH + chunk * 16);
+  typedef Shape<D> S;
+  const uint32_t row = lane & 31, chunk = (k * 2 + (lane >> 5)) ^ S::swizzle(row);
+  return *(const __attribute__((address_space(3))) s8 *)(lds + S::row_at(first) + S::row_at(row) + chunk * 16);
 }
-// element 32 d + lane % 32 of the rows `first` + 4 h .. + 3 and 8 more on: operand of a product over rows
+// element 32 d + lane % 32 of the rows `first` + 4 h .. + 3 and 8 more on: operand of a product over rows.  first: a multiple of 16
 template <int D>
 __device__ __forceinline__ s8 column_fragment(const lds_char *lds, int first, int d, int lane) {
-  const uint32_t c = lane & 15;
+  typedef Shape<D> S;
+  const uint32_t c = lane & 15, row = (lane >> 5) * 4 + (c >> 2);
   s4 half[2];
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    const uint32_t row = first + (lane >> 5) * 4 + (c >> 2) + i * 8;
-    const uint32_t chunk = (d * 4 + ((lane >> 4) & 1) * 2 + ((c & 3) >> 1)) ^ Shape<D>::swizzle(row);
-    half[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(lds + row * Shape<D>::PITCH + chunk * 16 + (c & 1) * 8));
+    const uint32_t chunk = (d * 4 + ((lane >> 4) & 1) * 2 + ((c & 3) >> 1)) ^ S::swizzle(row + i * 8);      // first changes none of the bits
+    half[i] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((__attribute__((address_space(3))) s4 *)(lds + S::row_at(first + i * 8) + S::row_at(row) + chunk * 16 + (c & 1) * 8));
   }
   return __builtin_shufflevector(half[0], half[1], 0, 1, 2, 3, 4, 5, 6, 7);
 }
 
 // rows of tokens that belong to no document may hold anything: zeros take their place where a product sums over them
+template <int D>
+__device__ __forceinline__ void clear_row(lds_char *lds, int row, int chunk) {
+  *(__attribute__((address_space(3))) u4 *)(lds + Shape<D>::row_at(row) + chunk * 16) = u4{0, 0, 0, 0};
+}
 template <int D, int ROWS, int NT>
 __device__ __forceinline__ void clear_none(lds_char *lds, const uint32_t *words, int tid) {
-  typedef Shape<D> S;
-  for (int idx = tid; idx < ROWS * S::CHUNKS; idx += NT)
-    if (words[idx / S::CHUNKS] == ATTN_NONE) *(__attribute__((address_space(3))) u4 *)(lds + idx * 16) = u4{0, 0, 0, 0};
+  for (int idx = tid; idx < ROWS * Shape<D>::CHUNKS; idx += NT)
+    if (words[idx / Shape<D>::CHUNKS] == ATTN_NONE) clear_row<D>(lds, idx / Shape<D>::CHUNKS, idx % Shape<D>::CHUNKS);
 }
 
 // ---------------------------------------------------------------------------------------------- what is seen
@@ -216,7 +233,10 @@ __device__ __forceinline__ void sees(const AttnCall &c, int from, int to, const 
   }
 }
 
-// Tiles of 64 keys that some rows see, in order: one that the workgroup visits, whether this wavefront does, whether it has to mask
+// A tile that the workgroup visits (-1: no more), whether this wavefront does, whether it has to mask, whether there are places of no document
+struct Visit { int tile; bool run, masked, some_none; };
+
+// Tiles of 64 keys that some rows see, in order
 struct KeyWalk {
   const AttnTile *tiles;
   int group_from, group_to, wave_from, wave_to;           // positions of the queries
@@ -224,8 +244,6 @@ struct KeyWalk {
   int first, step;                          // every step-th tile from the first on: so the parts of split sums see equally much of any mask
   int at, end;                              // those of the present ballot: at .. at + 63; end: behind the last tile
   uint64_t visit, mine, mask, none;
-  int tile;                                 // the present one; -1: no more
-  bool run, masked, some_none;
 
   __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int group_rows, int wave_row, int wave_rows, int first_, int step_, int end_) {
     tiles = c.k_words ? c.k_tiles + (int64_t)b * c.tiles : nullptr;
@@ -244,10 +262,10 @@ struct KeyWalk {
     end = end_;
     visit = 0;
   }
-  __device__ __forceinline__ void next(const AttnCall &c, int lane) {
+  __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if ((int64_t)at * step + first >= end) { tile = -1; return; }
+      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false};
       const int64_t tt = (int64_t)(at + lane) * step + first;
       const bool there = tt < end;
       const int t = there ? (int)tt : 0;
@@ -264,10 +282,7 @@ struct KeyWalk {
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    tile = (at + i) * step + first;
-    run = (mine >> i) & 1;
-    masked = (mask >> i) & 1;
-    some_none = (none >> i) & 1;
+    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((mask >> i) & 1), (bool)((none >> i) & 1)};
   }
 };
 
@@ -307,30 +322,27 @@ __device__ __forceinline__ float capped(const AttnCall &c, float product, float 
 }
 __device__ __forceinline__ float biased(float s, float slope2, float rel, int r) { return fmaf(-slope2, fabsf(rel - (float)row_of(r)), s); }
 
-template <class T, int D, int NQ>
-struct QueryRows {
-  s8 q[NQ][D / 16];
-  int pos[NQ];
-  uint32_t word[NQ];
-  float slope2[NQ];
-  int row[NQ], token[NQ], head[NQ];
-  // rows first + 32 n + lane % 32; those behind the last take its place (they are not stored)
+// A lane's row of the 32 of its wavefront
+template <class T, int D>
+struct QueryRow {
+  s8 q[D / 16];
+  int row, token, head, pos;
+  uint32_t word;
+  float slope2;
+  // row first + lane % 32; those behind the last take its place (they are not stored)
   __device__ __forceinline__ void start(const AttnCall &c, int b, int h, int first, int lane) {
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      row[n] = first + n * 32 + (lane & 31);
-      const int r = row[n] < c.rows ? row[n] : c.rows - 1;
-      token[n] = divide(c.by_group, r);
-      head[n] = h * c.group + r - token[n] * c.group;
-      pos[n] = token[n] + c.offset;
-      word[n] = c.q_words ? query_word(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token[n]]) : 0;
-      slope2[n] = c.slopes ? c.slopes[head[n]] * 1.44269504088896341f : 0.f;
-      operand(c, c.q, b, n, lane, q[n]);
-    }
+    row = first + (lane & 31);
+    const int r = row < c.rows ? row : c.rows - 1;
+    token = divide(c.by_group, r);
+    head = h * c.group + r - token * c.group;
+    pos = token + c.offset;
+    word = c.q_words ? query_word(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token]) : 0;
+    slope2 = c.slopes ? c.slopes[head] * 1.44269504088896341f : 0.f;
+    operand(c, c.q, b, lane, q);
   }
-  // this lane's elements of its row n of another tensor of the queries' shape
-  __device__ __forceinline__ void operand(const AttnCall &c, const AttnInput &in, int b, int n, int lane, s8 *out) const {
-    const uint16_t *p = in.p + b * in.batch + token[n] * in.token + head[n] * in.head;
+  // this lane's elements of its row of another tensor of the queries' shape
+  __device__ __forceinline__ void operand(const AttnCall &c, const AttnInput &in, int b, int lane, s8 (&out)[D / 16]) const {
+    const uint16_t *p = in.p + b * in.batch + token * in.token + head * in.head;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const int d = k * 16 + (lane >> 5) * 8;
@@ -339,123 +351,132 @@ struct QueryRows {
   }
 };
 
-// four consecutive elements d.. of a row of the results
+// A running softmax over blocks of 32 keys: reference (powers of two) and sum.  The reference follows the maximum only when that has grown by more than
+// 2^8: until then weights are up to 256, which 16-bit floats hold as exactly as smaller ones, and nothing has to be rescaled.
+//
+// Until the exponential a score stays what it costs least to get: the product; with a cap 1 / (1 + exp(2 x)) (capped()), which falls as the score grows;
+// with a bias the score itself.  weight = exp2(value * unit() + base() - reference).
+template <class T, int D, int CAP, int SLOPE>
+struct Softmax {
+  enum { LEAST = CAP && !SLOPE };           // values fall as scores grow
+  f16 o[D / 32];
+  float top, sum;
+  __device__ __forceinline__ void start() {
+    top = LOWEST;
+    sum = 0.f;
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d) o[d] = f16{};
+  }
+  static __device__ __forceinline__ float unit(const AttnCall &c) { return SLOPE ? 1.f : CAP ? -2.f * c.cap2 : c.to2; }
+  static __device__ __forceinline__ float base(const AttnCall &c) { return LEAST ? c.cap2 : 0.f; }
+  static __device__ __forceinline__ float more(float a, float b) { return LEAST ? fminf(a, b) : fmaxf(a, b); }
+
+  static __device__ __forceinline__ f16 products(const QueryRow<T, D> &row, const lds_char *keys, int first, int lane) {
+    f16 s = {};
+#pragma unroll
+    for (int k = 0; k < D / 16; ++k) s = T::mfma(row_fragment<D>(keys, first, k, lane), row.q[k], s);
+    return s;
+  }
+  // values from the products with the keys k0 + row_of(r); hidden ones are those of no weight
+  static __device__ __forceinline__ void values_of(const AttnCall &c, const QueryRow<T, D> &row, const uint32_t *words, int k0, bool masked, f16 &s) {
+    if (CAP || SLOPE) {
+      const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        if (LEAST) {
+          s[r] = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * c.tanh2));
+        } else {
+          float share;
+          s[r] = biased(capped<CAP>(c, s[r], share), row.slope2, rel, r);
+        }
+      }
+    }
+    if (masked) seen_keys(c, words, k0, row.pos, row.word, [&](int r, bool see) { s[r] = see ? s[r] : LEAST ? INFINITY : -INFINITY; });
+  }
+  static __device__ __forceinline__ float most_of(const f16 &s) {
+    float m = s[0];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) m = more(m, s[r]);
+    return m;
+  }
+  // brings the reference to where the weights of values up to `most` are at most 2^8
+  __device__ __forceinline__ void follow(const AttnCall &c, float most) {
+    const float to = both_max(fmaf(most, unit(c), base(c)));
+    if (__any(to > top + 8.f)) {
+      const float up = fmaxf(top, to), f = exp2_(top - up);
+      top = up;
+      sum *= f;
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] *= f;
+    }
+  }
+  // the weights of 32 keys, and the sums of their values (the rows from `first` on)
+  __device__ __forceinline__ void add(const AttnCall &c, f16 &s, const lds_char *values, int first, int lane) {
+    const float less = base(c) - top;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      s[r] = exp2_(SLOPE ? s[r] + less : fmaf(s[r], unit(c), less));
+      sum += s[r];
+    }
+    const s8 p[2] = {pack8<T>(s, 0), pack8<T>(s, 8)};
+#pragma unroll
+    for (int k = 0; k < 2; ++k)
+#pragma unroll
+      for (int d = 0; d < D / 32; ++d) o[d] = T::mfma(column_fragment<D>(values, first + k * 16, d, lane), p[k], o[d]);
+  }
+};
+
+// A wavefront's 32 x D results (rows in lanes) turned round in shared memory, half of 64 elements at a time, so that they leave as rows: 8 elements a lane
+enum { TURN_PITCH = 68, TURN_BYTES = 32 * TURN_PITCH * 4 };
+template <int D, class F>
+__device__ __forceinline__ void by_rows(lds_char *own, const f16 (&v)[D / 32], int lane, F f) {
+  const int h4 = (lane >> 5) * 4;
+#pragma unroll
+  for (int half = 0; half < D / 64; ++half) {
+#pragma unroll
+    for (int d = 0; d < 2; ++d)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        *(__attribute__((address_space(3))) f4 *)(own + ((lane & 31) * TURN_PITCH + d * 32 + g * 8 + h4) * 4) =
+            f4{v[half * 2 + d][g * 4], v[half * 2 + d][g * 4 + 1], v[half * 2 + d][g * 4 + 2], v[half * 2 + d][g * 4 + 3]};
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int row = i * 8 + (lane >> 3), d = (lane & 7) * 8;
+      const __attribute__((address_space(3))) f4 *p = (const __attribute__((address_space(3))) f4 *)(own + (row * TURN_PITCH + d) * 4);
+      f(row, half * 64 + d, p[0], p[1]);
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+// 8 elements of a row of the results
 template <class T>
-__device__ __forceinline__ void store4(uint16_t *p, int d, int width, float a, float b, float e, float f) {
-  const float v[4] = {a, b, e, f};
-  if (d + 4 <= width) {
-    typedef uint32_t u2_anywhere __attribute__((ext_vector_type(2), aligned(2)));
-    u2_anywhere w;
-    w[0] = (uint32_t)T::down(a) | ((uint32_t)T::down(b) << 16);
-    w[1] = (uint32_t)T::down(e) | ((uint32_t)T::down(f) << 16);
-    *(u2_anywhere *)(p + d) = w;
+__device__ __forceinline__ void store8(uint16_t *p, int d, int width, f4 a, f4 b) {
+  const float v[8] = {a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  if (d + 8 <= width) {
+    typedef uint32_t u4_anywhere __attribute__((ext_vector_type(4), aligned(2)));
+    u4_anywhere w;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = (uint32_t)T::down(v[2 * i]) | ((uint32_t)T::down(v[2 * i + 1]) << 16);
+    *(u4_anywhere *)(p + d) = w;
   } else {
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
       if (d + i < width) p[d + i] = T::down(v[i]);
   }
 }
-
 // what rounding took from them
 template <class T>
-__device__ __forceinline__ void store4_low(uint16_t *p, int d, int width, float a, float b, float e, float f) {
-  store4<T>(p, d, width, a - T::up(T::down(a)), b - T::up(T::down(b)), e - T::up(T::down(e)), f - T::up(T::down(f)));
+__device__ __forceinline__ void store8_low(uint16_t *p, int d, int width, f4 a, f4 b) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    a[i] -= T::up(T::down(a[i]));
+    b[i] -= T::up(T::down(b[i]));
+  }
+  store8<T>(p, d, width, a, b);
 }
-
-// One softmax over blocks of keys: running reference (powers of two) and sum.  The reference follows the maximum only when that has grown by more than
-// 2^8: until then weights are up to 256, which 16-bit floats hold as exactly as smaller ones, and nothing has to be rescaled.
-template <class T, int D, int NQ, int CAP, int SLOPE, int KB>
-struct Softmax {
-  f16 o[D / 32][NQ];
-  float top[NQ], sum[NQ];
-  __device__ __forceinline__ void start() {
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      top[n] = LOWEST;
-      sum[n] = 0.f;
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d) o[d][n] = f16{};
-    }
-  }
-  // KB blocks of 32 keys from key k0 on
-  __device__ __forceinline__ void step(const AttnCall &c, const QueryRows<T, D, NQ> &rows, const uint32_t *words, const lds_char *keys, const lds_char *values, int k0,
-                                       bool masked, int lane) {
-    f16 s[KB][NQ];
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) s[b][n] = f16{};
-#pragma unroll
-      for (int k = 0; k < D / 16; ++k) {
-        const s8 a = row_fragment<D>(keys, b * 32, k, lane);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) s[b][n] = T::mfma(a, rows.q[n][k], s[b][n]);
-      }
-    }
-    const int h4 = (lane >> 5) * 4;
-    constexpr bool RAW = !CAP && !SLOPE;    // then scores stay products until the exponential, which scales them
-#pragma unroll
-    for (int b = 0; b < KB; ++b)
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const float rel = SLOPE ? (float)(rows.pos[n] - (k0 + b * 32 + h4)) : 0.f;
-        if (!RAW) {
-#pragma unroll
-          for (int r = 0; r < 16; ++r) {
-            float share, v = capped<CAP>(c, s[b][n][r], share);
-            if (SLOPE) v = biased(v, rows.slope2[n], rel, r);
-            s[b][n][r] = v;
-          }
-        }
-        if (masked) seen_keys(c, words, k0 + b * 32 + h4, rows.pos[n], rows.word[n], [&](int r, bool see) { s[b][n][r] = see ? s[b][n][r] : -INFINITY; });
-      }
-    const float unit = RAW ? c.to2 : 1.f;
-    float most[NQ];
-    bool grown = false;
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) {
-      float m = s[0][n][0];
-#pragma unroll
-      for (int b = 0; b < KB; ++b)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) m = fmaxf(m, s[b][n][r]);
-      most[n] = both_max(m) * unit;
-      grown = grown || most[n] > top[n] + 8.f;
-    }
-    if (__any(grown)) {
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const float to = fmaxf(top[n], most[n]), f = exp2_(top[n] - to);
-        top[n] = to;
-        sum[n] *= f;
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) o[d][n] *= f;
-      }
-    }
-#pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      s8 p[NQ][2];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          s[b][n][r] = exp2_(RAW ? fmaf(s[b][n][r], c.to2, -top[n]) : s[b][n][r] - top[n]);
-          sum[n] += s[b][n][r];
-        }
-        p[n][0] = pack8<T>(s[b][n], 0);
-        p[n][1] = pack8<T>(s[b][n], 8);
-      }
-#pragma unroll
-      for (int k = 0; k < 2; ++k)
-#pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const s8 a = column_fragment<D>(values, b * 32 + k * 16, d, lane);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) o[d][n] = T::mfma(a, p[n][k], o[d][n]);
-        }
-    }
-  }
-};
 
 // ---------------------------------------------------------------------------------------------- forward
 // which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
@@ -477,88 +498,88 @@ __device__ __forceinline__ Place place_of(const AttnCall &c, int tiles, bool las
   return p;
 }
 
-template <class T, int D, int NQ, int CAP, int SLOPE>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k_forward(const AttnCall c) {
+// 128 rows, 32 a wavefront; two wavefronts a SIMD (three with rows of 64), of different workgroups, so that one's products run beside another's
+// exponentials.
+template <class T, int D, int CAP, int SLOPE>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_forward(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int KB = 2, WAVES = 4, NT = 64 * WAVES;
-  typedef KeyFeed<D, ATTN_TILE, NT> Feed;
-  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES];
+  constexpr int WAVES = 4, NT = 64 * WAVES;
+  typedef KeyFeed<D, ATTN_TILE, WAVES> Feed;
+  typedef Softmax<T, D, CAP, SLOPE> Soft;
+  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES > WAVES * TURN_BYTES ? 4 * Feed::BYTES : WAVES * TURN_BYTES];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.row_tiles, true);
-  const int row0 = p.tile * (WAVES * NQ * 32), wave_row = row0 + wave * NQ * 32;
-  QueryRows<T, D, NQ> rows;
-  rows.start(c, p.b, p.h, wave_row, lane);
+  const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
+  QueryRow<T, D> row;
+  row.start(c, p.b, p.h, wave_row, lane);
   Feed kf, vf;
-  kf.start(c.k, p.b, p.h, c.keys, c.dim, tid);
-  vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
+  kf.start(c.k, p.b, p.h, c.keys, c.dim, wave, lane);
+  vf.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, p.split, c.splits, c.tiles);
-  Softmax<T, D, NQ, CAP, SLOPE, KB> soft;
+  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, p.split, c.splits, c.tiles);
+  Soft soft;
   soft.start();
 
   int slot = 0;
-  walk.next(c, lane);
-  if (walk.tile >= 0) {
-    kf.load(walk.tile * ATTN_TILE, lds0, wave);
-    vf.load(walk.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) {
+    kf.load(next.tile * ATTN_TILE, lds0, wave);
+    vf.load(next.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
   }
-  while (walk.tile >= 0) {
-    const int tile = walk.tile;
-    const bool run = walk.run, masked = walk.masked, some_none = walk.some_none;
-    walk.next(c, lane);
+  while (next.tile >= 0) {
+    const Visit now = next;
+    next = walk.next(c, lane);
     arrived();                              // this tile is there, and the other slot has been read by everybody
-    lds_char *here = lds + slot * 2 * Feed::BYTES;
-    if (some_none) {
-      clear_none<D, ATTN_TILE, NT>(here + Feed::BYTES, words + tile * ATTN_TILE, tid);
+    lds_char *keys = lds + slot * 2 * Feed::BYTES, *values = keys + Feed::BYTES;
+    if (now.some_none) {
+      clear_none<D, ATTN_TILE, NT>(values, words + now.tile * ATTN_TILE, tid);
       arrived();
     }
     slot ^= 1;
-    if (walk.tile >= 0) {
-      kf.load(walk.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
-      vf.load(walk.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
+    if (next.tile >= 0) {
+      kf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
+      vf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
     }
-    if (run) soft.step(c, rows, words, here, here + Feed::BYTES, tile * ATTN_TILE, masked, lane);
+    if (!now.run) continue;
+    const int k0 = now.tile * ATTN_TILE + h4;
+    f16 s = Soft::products(row, keys, 0, lane), t = Soft::products(row, keys, 32, lane);
+    Soft::values_of(c, row, words, k0, now.masked, s);
+    Soft::values_of(c, row, words, k0 + 32, now.masked, t);
+    soft.follow(c, Soft::more(Soft::most_of(s), Soft::most_of(t)));
+    soft.add(c, s, values, 0, lane);
+    soft.add(c, t, values, 32, lane);
   }
 
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    const float sum = both_sum(soft.sum[n]);
-    if (rows.row[n] >= c.rows) continue;
-    const int h4 = (lane >> 5) * 4;
-    if (c.splits > 1) {
-      const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.rows + rows.row[n];
-      float *out = c.part + at * c.width4;
-      if (lane < 32) {
-        c.part2[at * 2] = soft.top[n];
-        c.part2[at * 2 + 1] = sum;
-      }
-#pragma unroll
-      for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          if (d * 32 + g * 8 + h4 < c.width4)
-            *(f4 *)(out + d * 32 + g * 8 + h4) = f4{soft.o[d][n][g * 4], soft.o[d][n][g * 4 + 1], soft.o[d][n][g * 4 + 2], soft.o[d][n][g * 4 + 3]};
-      continue;
+  lds_char *own = lds + wave * TURN_BYTES;
+  arrived();
+  const float sum = both_sum(soft.sum);
+  if (c.splits > 1) {
+    const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.rows + wave_row;
+    if (lane < 32 && row.row < c.rows) {
+      c.part2[(at + lane) * 2] = soft.top;
+      c.part2[(at + lane) * 2 + 1] = sum;
     }
-    const float f = sum == 0.f ? 0.f : 1.f / sum;
-    if (c.lse && lane < 32) c.lse[(int64_t)p.hb * c.rows_pad + rows.row[n]] = sum == 0.f ? INFINITY : soft.top[n] + __builtin_amdgcn_logf(sum);
-    uint16_t *out = c.y.p + p.b * c.y.batch + rows.token[n] * c.y.token + rows.head[n] * c.y.head;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        store4<T>(out, d * 32 + g * 8 + h4, c.width, soft.o[d][n][g * 4] * f, soft.o[d][n][g * 4 + 1] * f, soft.o[d][n][g * 4 + 2] * f, soft.o[d][n][g * 4 + 3] * f);
-    if (!c.low) continue;
-    out = c.low + (((int64_t)p.b * c.tokens + rows.token[n]) * (c.kv_heads * c.group) + rows.head[n]) * c.width;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        store4_low<T>(out, d * 32 + g * 8 + h4, c.width, soft.o[d][n][g * 4] * f, soft.o[d][n][g * 4 + 1] * f, soft.o[d][n][g * 4 + 2] * f, soft.o[d][n][g * 4 + 3] * f);
+    by_rows<D>(own, soft.o, lane, [&](int i, int d, f4 a, f4 b) {
+      if (wave_row + i >= c.rows) return;
+      float *out = c.part + (at + i) * c.width4 + d;
+      if (d < c.width4) *(f4 *)out = a;
+      if (d + 4 < c.width4) *(f4 *)(out + 4) = b;
+    });
+    return;
   }
+  const float f = sum == 0.f ? 0.f : 1.f / sum;
+  if (c.lse && lane < 32 && row.row < c.rows) c.lse[(int64_t)p.hb * c.rows_pad + row.row] = sum == 0.f ? INFINITY : soft.top + __builtin_amdgcn_logf(sum);
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) soft.o[d] *= f;
+  by_rows<D>(own, soft.o, lane, [&](int i, int d, f4 a, f4 b) {
+    const int r = wave_row + i, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
+    if (r >= c.rows) return;
+    store8<T>(c.y.p + p.b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, a, b);
+    if (c.low) store8_low<T>(c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width, d, c.width, a, b);
+  });
 #endif
 }
 
@@ -568,7 +589,7 @@ template <class T, int D, int CAP, int SLOPE>
 __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WAVES = 4;
-  typedef KeyFeed<D, 32, 64> Feed;
+  typedef KeyFeed<D, 32, 1> Feed;
   constexpr int OWN = 4 * Feed::BYTES;      // two steps of keys and values; behind the loop 32 rows of D sums
   __shared__ __attribute__((aligned(1024))) char shared[WAVES * OWN];
   __shared__ float tops[WAVES][32], sums[WAVES][32];
@@ -577,55 +598,59 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   lds_char *own = lds + wave * OWN;
   const uint32_t own0 = (uint32_t)(uintptr_t)own;
   const Place p = place_of(c, 1, false);
-  QueryRows<T, D, 1> rows;
-  rows.start(c, p.b, p.h, 0, lane);
+  QueryRow<T, D> row;
+  row.start(c, p.b, p.h, 0, lane);
   Feed kf, vf;
-  kf.start(c.k, p.b, p.h, c.keys, c.dim, lane);
-  vf.start(c.v, p.b, p.h, c.keys, c.dim, lane);
+  kf.start(c.k, p.b, p.h, c.keys, c.dim, 0, lane);
+  vf.start(c.v, p.b, p.h, c.keys, c.dim, 0, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk walk;
   walk.start(c, p.b, 0, 32, 0, 32, p.split * WAVES + wave, c.splits * WAVES, c.tiles);
-  Softmax<T, D, 1, CAP, SLOPE, 1> soft;
+  typedef Softmax<T, D, CAP, SLOPE> Soft;
+  Soft soft;
   soft.start();
 
   int slot = 0, half = 0;
-  walk.next(c, lane);
-  if (walk.tile >= 0) {
-    kf.load(walk.tile * ATTN_TILE, own0, 0);
-    vf.load(walk.tile * ATTN_TILE, own0 + Feed::BYTES, 0);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) {
+    kf.load(next.tile * ATTN_TILE, own0, 0);
+    vf.load(next.tile * ATTN_TILE, own0 + Feed::BYTES, 0);
   }
-  while (walk.tile >= 0) {
-    const int tile = walk.tile, k0 = tile * ATTN_TILE + half * 32;
-    const bool masked = walk.masked, some_none = walk.some_none;
+  while (next.tile >= 0) {
+    const Visit now = next;
+    const int k0 = now.tile * ATTN_TILE + half * 32;
     half ^= 1;
     if (half == 0 || k0 + 32 >= c.keys) {
       half = 0;
-      walk.next(c, lane);
+      next = walk.next(c, lane);
     }
     lds_char *here = own + slot * 2 * Feed::BYTES;
     slot ^= 1;
-    if (walk.tile >= 0) {
-      const int k = walk.tile * ATTN_TILE + half * 32;
+    if (next.tile >= 0) {
+      const int k = next.tile * ATTN_TILE + half * 32;
       kf.load(k, own0 + slot * 2 * Feed::BYTES, 0);
       vf.load(k, own0 + slot * 2 * Feed::BYTES + Feed::BYTES, 0);
       waited<2 * Feed::LOADS>();
     } else {
       waited<0>();
     }
-    if (some_none) {
+    if (now.some_none) {
       clear_none<D, 32, 64>(here + Feed::BYTES, words + k0, lane);
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+      waited<0>();
     }
-    soft.step(c, rows, words, here, here + Feed::BYTES, k0, masked, lane);
+    f16 s = Soft::products(row, here, 0, lane);
+    Soft::values_of(c, row, words, k0 + (lane >> 5) * 4, now.masked, s);
+    soft.follow(c, Soft::most_of(s));
+    soft.add(c, s, here + Feed::BYTES, 0, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: the next loads go there
   }
 
   constexpr int PITCH = D + 4;              // floats: 32 rows of it in a wavefront's own memory
   static_assert(32 * PITCH * 4 <= OWN, "the sums of a wavefront");
-  const float total = both_sum(soft.sum[0]);
+  const float total = both_sum(soft.sum);
   const int h4 = (lane >> 5) * 4;
   if (lane < 32) {
-    tops[wave][lane] = soft.top[0];
+    tops[wave][lane] = soft.top;
     sums[wave][lane] = total;
   }
 #pragma unroll
@@ -633,21 +658,23 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
 #pragma unroll
     for (int g = 0; g < 4; ++g)
       *(__attribute__((address_space(3))) f4 *)(own + ((lane & 31) * PITCH + d * 32 + g * 8 + h4) * 4) =
-          f4{soft.o[d][0][g * 4], soft.o[d][0][g * 4 + 1], soft.o[d][0][g * 4 + 2], soft.o[d][0][g * 4 + 3]};
+          f4{soft.o[d][g * 4], soft.o[d][g * 4 + 1], soft.o[d][g * 4 + 2], soft.o[d][g * 4 + 3]};
   __syncthreads();
   const int live = c.rows < 32 ? c.rows : 32;
-  for (int i = tid; i < live * (D / 4); i += 256) {
-    const int r = i / (D / 4), d = i % (D / 4) * 4;
+  for (int i = tid; i < live * (D / 8); i += 256) {
+    const int r = i / (D / 8), d = i % (D / 8) * 8;
     float top = tops[0][r];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) top = fmaxf(top, tops[w][r]);
     float sum = 0.f;
-    f4 v = f4{0.f, 0.f, 0.f, 0.f};
+    f4 v = f4{0.f, 0.f, 0.f, 0.f}, u = v;
 #pragma unroll
     for (int w = 0; w < WAVES; ++w) {
       const float f = exp2_(tops[w][r] - top);
+      const __attribute__((address_space(3))) f4 *part = (const __attribute__((address_space(3))) f4 *)(lds + w * OWN + (r * PITCH + d) * 4);
       sum += sums[w][r] * f;
-      v += *(const __attribute__((address_space(3))) f4 *)(lds + w * OWN + (r * PITCH + d) * 4) * f;
+      v += part[0] * f;
+      u += part[1] * f;
     }
     if (c.splits > 1) {
       const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.rows + r;
@@ -656,136 +683,139 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
         c.part2[at * 2 + 1] = sum;
       }
       if (d < c.width4) *(f4 *)(c.part + at * c.width4 + d) = v;
+      if (d + 4 < c.width4) *(f4 *)(c.part + at * c.width4 + d + 4) = u;
       continue;
     }
     const int token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
     const float f = sum == 0.f ? 0.f : 1.f / sum;
     if (c.lse && d == 0) c.lse[(int64_t)p.hb * c.rows_pad + r] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
-    store4<T>(c.y.p + p.b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
-    if (c.low)
-      store4_low<T>(c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width, d, c.width, v[0] * f, v[1] * f, v[2] * f, v[3] * f);
+    store8<T>(c.y.p + p.b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, v * f, u * f);
+    if (c.low) store8_low<T>(c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width, d, c.width, v * f, u * f);
   }
 #endif
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// p and ds of a score from the products q.k and dy.v; bias: of the distance, in powers of two
+// p and dz p, dz being the tanh's derivative, of a score from its product; less: what is taken from it, in powers of two
 template <int CAP>
-__device__ __forceinline__ void gradient(const AttnCall &c, float &s, float &dp, float bias, float lse, float delta) {
-  float share, v = capped<CAP>(c, s, share);
-  s = exp2_(v - bias - lse);
-  dp = s * (dp - delta);
-  if (CAP) dp *= 4.f * (share - share * share);
+__device__ __forceinline__ void weight_of(const AttnCall &c, float product, float less, float &p, float &w) {
+  float share;
+  p = w = exp2_(capped<CAP>(c, product, share) - less);
+  if (CAP) w *= 4.f * (share - share * share);
 }
 
-template <class T, int D, int NQ, int CAP, int SLOPE>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k_dq(const AttnCall c) {
+// delta = dy.y of a lane's row.  y is taken with what its rounding took from it: where few keys share a row, dy.v and delta are near each other, and
+// 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3 without, 2.4e-3 with).
+template <class T, int D>
+__device__ __forceinline__ float delta_of(const AttnCall &c, const Place &p, int token, int head, const s8 (&dy)[D / 16], int lane) {
+  typedef s8 s8_anywhere __attribute__((aligned(2)));
+  const uint16_t *y = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
+  const uint16_t *low = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
+  float sum = 0.f;
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) {
+    const int d = k * 16 + (lane >> 5) * 8;
+    if (d + 8 <= c.width) {
+      const s8 a = *(const s8_anywhere *)(y + d), b = *(const s8_anywhere *)(low + d);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[k][e]), T::up((uint16_t)a[e]) + T::up((uint16_t)b[e]), sum);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (d + e < c.width) sum = fmaf(T::up((uint16_t)dy[k][e]), T::up(y[d + e]) + T::up(low[d + e]), sum);
+    }
+  }
+  return both_sum(sum);
+}
+
+template <class T, int D, int CAP, int SLOPE>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_dq(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int KB = 2, WAVES = 4, NT = 64 * WAVES;
-  typedef KeyFeed<D, ATTN_TILE, NT> Feed;
-  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES];
+  constexpr int WAVES = 4, NT = 64 * WAVES;
+  typedef KeyFeed<D, ATTN_TILE, WAVES> Feed;
+  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES > WAVES * TURN_BYTES ? 4 * Feed::BYTES : WAVES * TURN_BYTES];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.row_tiles, true);
-  const int row0 = p.tile * (WAVES * NQ * 32), wave_row = row0 + wave * NQ * 32;
-  QueryRows<T, D, NQ> rows;
-  rows.start(c, p.b, p.h, wave_row, lane);
-  s8 dy[NQ][D / 16];
-  float lse[NQ], delta[NQ];
-#pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    rows.operand(c, c.dy, p.b, n, lane, dy[n]);
-    const int r = rows.row[n] < c.rows ? rows.row[n] : c.rows - 1;
-    const AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + r / 32];
-    lse[n] = block.lse[r % 32];
-    delta[n] = block.delta[r % 32];
+  const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
+  QueryRow<T, D> row;
+  row.start(c, p.b, p.h, wave_row, lane);
+  s8 dy[D / 16];
+  row.operand(c, c.dy, p.b, lane, dy);
+  const bool there = row.row < c.rows;
+  const float lse = c.lse[(int64_t)p.hb * c.rows_pad + (there ? row.row : c.rows - 1)], delta = delta_of<T, D>(c, p, row.token, row.head, dy, lane);
+  if (lane < 32 && row.row < c.rows_pad) {
+    AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
+    block.lse[lane] = there ? lse : INFINITY;
+    block.delta[lane] = delta;
+    block.last[lane] = !there ? INT32_MIN : c.causal ? row.pos : INT32_MAX;
+    block.word[lane] = there ? row.word : ATTN_NOBODY;
+    block.slope2[lane] = row.slope2;
+    block.pos[lane] = row.pos;
   }
   Feed kf, vf;
-  kf.start(c.k, p.b, p.h, c.keys, c.dim, tid);
-  vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
+  kf.start(c.k, p.b, p.h, c.keys, c.dim, wave, lane);
+  vf.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * NQ * 32, wave_row, NQ * 32, 0, 1, c.tiles);
-  f16 dq[D / 32][NQ];
+  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, 0, 1, c.tiles);
+  f16 dq[D / 32];
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int n = 0; n < NQ; ++n) dq[d][n] = f16{};
+  for (int d = 0; d < D / 32; ++d) dq[d] = f16{};
 
   int slot = 0;
-  const int h4 = (lane >> 5) * 4;
-  walk.next(c, lane);
-  if (walk.tile >= 0) {
-    kf.load(walk.tile * ATTN_TILE, lds0, wave);
-    vf.load(walk.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) {
+    kf.load(next.tile * ATTN_TILE, lds0, wave);
+    vf.load(next.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
   }
-  while (walk.tile >= 0) {
-    const int tile = walk.tile;
-    const bool run = walk.run, masked = walk.masked, some_none = walk.some_none;
-    walk.next(c, lane);
+  while (next.tile >= 0) {
+    const Visit now = next;
+    next = walk.next(c, lane);
     arrived();
-    lds_char *here = lds + slot * 2 * Feed::BYTES;
-    if (some_none) {
-      clear_none<D, ATTN_TILE, NT>(here, words + tile * ATTN_TILE, tid);
+    lds_char *keys = lds + slot * 2 * Feed::BYTES, *values = keys + Feed::BYTES;
+    if (now.some_none) {
+      clear_none<D, ATTN_TILE, NT>(keys, words + now.tile * ATTN_TILE, tid);
       arrived();
     }
     slot ^= 1;
-    if (walk.tile >= 0) {
-      kf.load(walk.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
-      vf.load(walk.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
+    if (next.tile >= 0) {
+      kf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
+      vf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
     }
-    if (!run) continue;
+    if (!now.run) continue;
 #pragma unroll
-    for (int b = 0; b < KB; ++b) {
-      const int k0 = tile * ATTN_TILE + b * 32 + h4;
-      f16 s[NQ], dp[NQ];
-#pragma unroll
-      for (int n = 0; n < NQ; ++n) s[n] = dp[n] = f16{};
+    for (int b = 0; b < 2; ++b) {
+      const int k0 = now.tile * ATTN_TILE + b * 32 + h4;
+      f16 s = {}, dp = {};
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
-        const s8 a = row_fragment<D>(here, b * 32, k, lane), v = row_fragment<D>(here + Feed::BYTES, b * 32, k, lane);
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) {
-          s[n] = T::mfma(a, rows.q[n][k], s[n]);
-          dp[n] = T::mfma(v, dy[n][k], dp[n]);
-        }
+        s = T::mfma(row_fragment<D>(keys, b * 32, k, lane), row.q[k], s);
+        dp = T::mfma(row_fragment<D>(values, b * 32, k, lane), dy[k], dp);
       }
-      s8 ds[NQ][2];
+      const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
 #pragma unroll
-      for (int n = 0; n < NQ; ++n) {
-        const float rel = SLOPE ? (float)(rows.pos[n] - k0) : 0.f;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          float x = s[n][r], y = dp[n][r];
-          gradient<CAP>(c, x, y, SLOPE ? rows.slope2[n] * fabsf(rel - (float)row_of(r)) : 0.f, lse[n], delta[n]);
-          dp[n][r] = y;
-        }
-        if (masked) seen_keys(c, words, k0, rows.pos[n], rows.word[n], [&](int r, bool see) { dp[n][r] = see ? dp[n][r] : 0.f; });
-        ds[n][0] = pack8<T>(dp[n], 0);
-        ds[n][1] = pack8<T>(dp[n], 8);
+      for (int r = 0; r < 16; ++r) {
+        float w, all;
+        weight_of<CAP>(c, s[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), lse) : lse, all, w);
+        dp[r] = w * (dp[r] - delta);
       }
+      if (now.masked) seen_keys(c, words, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
+      const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
       for (int k = 0; k < 2; ++k)
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) {
-          const s8 a = column_fragment<D>(here, b * 32 + k * 16, d, lane);
-#pragma unroll
-          for (int n = 0; n < NQ; ++n) dq[d][n] = T::mfma(a, ds[n][k], dq[d][n]);
-        }
+        for (int d = 0; d < D / 32; ++d) dq[d] = T::mfma(column_fragment<D>(keys, b * 32 + k * 16, d, lane), ds[k], dq[d]);
     }
   }
+  arrived();
 #pragma unroll
-  for (int n = 0; n < NQ; ++n) {
-    if (rows.row[n] >= c.rows) continue;
-    uint16_t *out = c.dq.p + p.b * c.dq.batch + rows.token[n] * c.dq.token + rows.head[n] * c.dq.head;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-        store4<T>(out, d * 32 + g * 8 + h4, c.width, dq[d][n][g * 4] * c.scale, dq[d][n][g * 4 + 1] * c.scale, dq[d][n][g * 4 + 2] * c.scale,
-                  dq[d][n][g * 4 + 3] * c.scale);
-  }
+  for (int d = 0; d < D / 32; ++d) dq[d] *= c.scale;
+  by_rows<D>(lds + wave * TURN_BYTES, dq, lane, [&](int i, int d, f4 a, f4 b) {
+    const int r = wave_row + i, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
+    if (r < c.rows) store8<T>(c.dq.p + p.b * c.dq.batch + token * c.dq.token + head * c.dq.head, d, c.width, a, b);
+  });
 #endif
 }
 
@@ -796,8 +826,6 @@ struct RowWalk {
   const AttnTile *tiles;                    // of the queries' tokens
   int first, step, at, end;
   uint64_t visit, mine, mask, none;
-  int tile;
-  bool run, masked, some_none;
   __device__ __forceinline__ void start(const AttnCall &c, int b, int group_key, int group_keys, int wave_key, int wave_keys, int first_, int step_, int end_) {
     group_from = group_key;
     group_to = group_key + group_keys - 1 < c.keys ? group_key + group_keys - 1 : c.keys - 1;
@@ -826,10 +854,10 @@ struct RowWalk {
     }
     return r;
   }
-  __device__ __forceinline__ void next(const AttnCall &c, int lane) {
+  __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if ((int64_t)at * step + first >= end) { tile = -1; return; }
+      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false};
       const int64_t tt = (int64_t)(at + lane) * step + first;
       const bool there = tt < end;
       const int r0 = there ? (int)tt * 32 : 0, r1 = r0 + 31 < c.rows ? r0 + 31 : c.rows - 1;
@@ -847,26 +875,24 @@ struct RowWalk {
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    tile = (at + i) * step + first;
-    run = (mine >> i) & 1;
-    masked = (mask >> i) & 1;
-    some_none = (none >> i) & 1;
+    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((mask >> i) & 1), (bool)((none >> i) & 1)};
   }
 };
 
 // A wavefront has 32 keys: their operands, and 2 x 32 x D sums, which with the scores fill half of a lane's registers (two wavefronts a SIMD) if the
-// values stay in shared memory: they are read from there a block, as the queries and dy are.
+// values stay in shared memory: they are read from there a block of 32 rows, as the queries and dy are.
 template <class T, int D, int CAP, int SLOPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k_dkdv(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WAVES = 4, NT = 64 * WAVES, KEYS = WAVES * 32;
-  typedef RowFeed<D, 32, NT> Feed;
-  typedef KeyFeed<D, KEYS, NT> Values;
+  typedef RowFeed<D, 32, WAVES> Feed;
+  typedef KeyFeed<D, KEYS, WAVES> Values;
   typedef __attribute__((address_space(3))) const AttnRows lds_rows;
-  constexpr int STAGE = 2 * Feed::BYTES + 1024;            // queries, dy and what is known of 32 rows
+  typedef __attribute__((address_space(3))) const f4 lds_f4;
+  enum { ROWS = 2 * Feed::BYTES, STAGE = ROWS + (int)sizeof(AttnRows), VALUES = 2 * STAGE, BYTES = VALUES + Values::BYTES };
   static_assert(sizeof(AttnRows) <= 1024, "a wavefront brings it in one load");
-  __shared__ __attribute__((aligned(1024))) char shared[2 * STAGE + Values::BYTES];
-  lds_char *lds = (lds_char *)shared, *values = lds + 2 * STAGE;
+  __shared__ __attribute__((aligned(1024))) char shared[BYTES > WAVES * TURN_BYTES ? BYTES : WAVES * TURN_BYTES];
+  lds_char *lds = (lds_char *)shared, *values = lds + VALUES;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.key_tiles, false);
@@ -884,12 +910,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       k[i] = d < c.dim ? *(const s8 *)(kp + d) : s8{};
     }
     Values vf;
-    vf.start(c.v, p.b, p.h, c.keys, c.dim, tid);
-    vf.load(key0, lds0 + 2 * STAGE, wave);
+    vf.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
+    vf.load(key0, lds0 + VALUES, wave);
   }
   Feed qf, df;
-  qf.start(c.q, p.b, p.h * c.group);
-  df.start(c.dy, p.b, p.h * c.group);
+  qf.start(c, c.q, p.b, p.h * c.group, wave, lane);
+  df.start(c, c.dy, p.b, p.h * c.group, wave, lane);
   const uint32_t *q_words = c.q_words ? c.q_words + (int64_t)p.b * c.q_tile_count * ATTN_TILE : nullptr;
   const AttnRows *row_data = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
 
@@ -908,34 +934,32 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
 
   const auto load = [&](int tile, int slot) {
     const uint32_t at = lds0 + slot * STAGE;
-    qf.load(c, tile * 32, at, wave, tid);
-    df.load(c, tile * 32, at + Feed::BYTES, wave, tid);
-    if (wave == 0) load_lds16(descriptor(row_data + tile, sizeof(AttnRows)), lane * 16, at + 2 * Feed::BYTES);
+    qf.load(c, tile * 32, at, wave, lane);
+    df.load(c, tile * 32, at + Feed::BYTES, wave, lane);
+    if (wave == 0 && lane < (int)sizeof(AttnRows) / 16) load_lds16(descriptor(row_data + tile, sizeof(AttnRows)), lane * 16, at + ROWS);
   };
   int slot = 0;
-  walk.next(c, lane);
-  if (walk.tile >= 0) load(walk.tile, 0);
-  while (walk.tile >= 0) {
-    const int tile = walk.tile;
-    const bool run = walk.run, masked = walk.masked, some_none = walk.some_none;
-    walk.next(c, lane);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) load(next.tile, 0);
+  while (next.tile >= 0) {
+    const Visit now = next;
+    next = walk.next(c, lane);
     arrived();
-    lds_char *here = lds + slot * STAGE;
-    if (some_none) {
+    lds_char *queries = lds + slot * STAGE, *dys = queries + Feed::BYTES;
+    lds_rows *known = (lds_rows *)(queries + ROWS);
+    if (now.some_none) {
       for (int idx = tid; idx < 32 * Shape<D>::CHUNKS; idx += NT) {
-        const int r = tile * 32 + idx / Shape<D>::CHUNKS;
+        const int i = idx / Shape<D>::CHUNKS, r = now.tile * 32 + i;
         if (r < c.rows && q_words[divide(c.by_group, r)] == ATTN_NONE) {
-          *(__attribute__((address_space(3))) u4 *)(here + idx * 16) = u4{0, 0, 0, 0};
-          *(__attribute__((address_space(3))) u4 *)(here + Feed::BYTES + idx * 16) = u4{0, 0, 0, 0};
+          clear_row<D>(queries, i, idx % Shape<D>::CHUNKS);
+          clear_row<D>(dys, i, idx % Shape<D>::CHUNKS);
         }
       }
       arrived();
     }
     slot ^= 1;
-    if (walk.tile >= 0) load(walk.tile, slot);
-    if (!run) continue;
-    const lds_char *queries = here, *dys = here + Feed::BYTES;
-    lds_rows *known = (lds_rows *)(here + 2 * Feed::BYTES);
+    if (next.tile >= 0) load(next.tile, slot);
+    if (!now.run) continue;
     f16 s = {}, dp = {};
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) s = T::mfma(row_fragment<D>(queries, 0, i, lane), k[i], s);
@@ -943,24 +967,23 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
     for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, 0, i, lane), row_fragment<D>(values, wave * 32, i, lane), dp);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      const int r0 = g * 8 + h4;
-      const f4 lse = *(__attribute__((address_space(3))) const f4 *)&known->lse[r0], delta = *(__attribute__((address_space(3))) const f4 *)&known->delta[r0];
-      f4 bias = f4{0.f, 0.f, 0.f, 0.f};
+      f4 less = *(lds_f4 *)&known->lse[g * 8 + h4];
+      const f4 delta = *(lds_f4 *)&known->delta[g * 8 + h4];
       if (SLOPE) {
-        const f4 slope2 = *(__attribute__((address_space(3))) const f4 *)&known->slope2[r0];
-        const i4 pos = *(__attribute__((address_space(3))) const i4 *)&known->pos[r0];
+        const f4 slope2 = *(lds_f4 *)&known->slope2[g * 8 + h4];
+        const i4 pos = *(__attribute__((address_space(3))) const i4 *)&known->pos[g * 8 + h4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) bias[e] = slope2[e] * fabsf((float)(pos[e] - key));
+        for (int e = 0; e < 4; ++e) less[e] = fmaf(slope2[e], fabsf((float)(pos[e] - key)), less[e]);
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float x = s[g * 4 + e], y = dp[g * 4 + e];
-        gradient<CAP>(c, x, y, bias[e], lse[e], delta[e]);
-        s[g * 4 + e] = x;
-        dp[g * 4 + e] = y;
+        float one, two;
+        weight_of<CAP>(c, s[g * 4 + e], less[e], one, two);
+        s[g * 4 + e] = one;
+        dp[g * 4 + e] = two * (dp[g * 4 + e] - delta[e]);
       }
     }
-    if (masked) {
+    if (now.masked) {
 #pragma unroll
       for (int g = 0; g < 4; ++g) {
         const i4 last = *(__attribute__((address_space(3))) const i4 *)&known->last[g * 8 + h4];
@@ -975,61 +998,60 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
-      const s8 w = pack8<T>(s, i * 8), ds = pack8<T>(dp, i * 8);
+      const s8 pp = pack8<T>(s, i * 8), ds = pack8<T>(dp, i * 8);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
-        dv[d] = T::mfma(column_fragment<D>(dys, i * 16, d, lane), w, dv[d]);
+        dv[d] = T::mfma(column_fragment<D>(dys, i * 16, d, lane), pp, dv[d]);
         dk[d] = T::mfma(column_fragment<D>(queries, i * 16, d, lane), ds, dk[d]);
       }
     }
   }
-  if (walk.tile < 0) waited<0>();           // the values, where no block was visited
-  if (key >= c.keys) return;
+  arrived();                                // the values, where no block was visited; and nobody reads shared memory any more
+  lds_char *own = lds + wave * TURN_BYTES;
+#pragma unroll
+  for (int d = 0; d < D / 32; ++d) dk[d] *= c.scale;
   if (c.splits > 1) {
-    const int64_t at = (((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + key) * c.width4;
-#pragma unroll
-    for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const int e = d * 32 + g * 8 + h4;
-        if (e >= c.width4) continue;
-        *(f4 *)(c.part + at + e) = f4{dk[d][g * 4], dk[d][g * 4 + 1], dk[d][g * 4 + 2], dk[d][g * 4 + 3]} * c.scale;
-        *(f4 *)(c.part2 + at + e) = f4{dv[d][g * 4], dv[d][g * 4 + 1], dv[d][g * 4 + 2], dv[d][g * 4 + 3]};
-      }
+    const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + wave_key;
+    const auto put = [&](float *part, int row, int d, f4 a, f4 b) {
+      if (wave_key + row >= c.keys) return;
+      float *out = part + (at + row) * c.width4 + d;
+      if (d < c.width4) *(f4 *)out = a;
+      if (d + 4 < c.width4) *(f4 *)(out + 4) = b;
+    };
+    by_rows<D>(own, dk, lane, [&](int row, int d, f4 a, f4 b) { put(c.part, row, d, a, b); });
+    by_rows<D>(own, dv, lane, [&](int row, int d, f4 a, f4 b) { put(c.part2, row, d, a, b); });
     return;
   }
-  uint16_t *ko = c.dk.p + p.b * c.dk.batch + key * c.dk.token + p.h * c.dk.head, *vo = c.dv.p + p.b * c.dv.batch + key * c.dv.token + p.h * c.dv.head;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d)
-#pragma unroll
-    for (int g = 0; g < 4; ++g) {
-      store4<T>(ko, d * 32 + g * 8 + h4, c.width, dk[d][g * 4] * c.scale, dk[d][g * 4 + 1] * c.scale, dk[d][g * 4 + 2] * c.scale, dk[d][g * 4 + 3] * c.scale);
-      store4<T>(vo, d * 32 + g * 8 + h4, c.width, dv[d][g * 4], dv[d][g * 4 + 1], dv[d][g * 4 + 2], dv[d][g * 4 + 3]);
-    }
+  const auto put = [&](const AttnOutput &o, int row, int d, f4 a, f4 b) {
+    const int j = wave_key + row;
+    if (j < c.keys) store8<T>(o.p + p.b * o.batch + j * o.token + p.h * o.head, d, c.width, a, b);
+  };
+  by_rows<D>(own, dk, lane, [&](int row, int d, f4 a, f4 b) { put(c.dk, row, d, a, b); });
+  by_rows<D>(own, dv, lane, [&](int row, int d, f4 a, f4 b) { put(c.dv, row, d, a, b); });
 #endif
 }
 
 // ---------------------------------------------------------------------------------------------- launches
 enum { FORWARD, FEW, DQ, DKDV };
-template <class T, int WHAT, int D, int N, int CAP, int SLOPE>
+template <class T, int WHAT, int D, int CAP, int SLOPE>
 bool launch(const AttnCall &c, const AttnLaunch &l) {
   hipStream_t st = (hipStream_t)l.stream;
   const dim3 grid(l.groups), block(256);
-  if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, N, CAP, SLOPE>), grid, block, 0, st, c);
+  if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, CAP, SLOPE>), grid, block, 0, st, c);
   else if constexpr (WHAT == FEW) hipLaunchKernelGGL((k_forward_few<T, D, CAP, SLOPE>), grid, block, 0, st, c);
-  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, N, CAP, SLOPE>), grid, block, 0, st, c);
+  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, CAP, SLOPE>), grid, block, 0, st, c);
   else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE>), grid, block, 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
-template <class T, int WHAT, int D, int N>
+template <class T, int WHAT, int D>
 bool launch_terms(const AttnCall &c, const AttnLaunch &l) {
   const bool cap = c.cap2 != 0.f, slope = c.slopes != nullptr;
-  if (cap) return slope ? launch<T, WHAT, D, N, 1, 1>(c, l) : launch<T, WHAT, D, N, 1, 0>(c, l);
-  return slope ? launch<T, WHAT, D, N, 0, 1>(c, l) : launch<T, WHAT, D, N, 0, 0>(c, l);
+  if (cap) return slope ? launch<T, WHAT, D, 1, 1>(c, l) : launch<T, WHAT, D, 1, 0>(c, l);
+  return slope ? launch<T, WHAT, D, 0, 1>(c, l) : launch<T, WHAT, D, 0, 0>(c, l);
 }
 template <class T, int WHAT>
 bool launch_shape(const AttnCall &c, const AttnLaunch &l) {
-  return l.dim == 64 ? launch_terms<T, WHAT, 64, 1>(c, l) : launch_terms<T, WHAT, 128, 1>(c, l);
+  return l.dim == 64 ? launch_terms<T, WHAT, 64>(c, l) : launch_terms<T, WHAT, 128>(c, l);
 }
 
 }  // namespace chm_attention_kernels

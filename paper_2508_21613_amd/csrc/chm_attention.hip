@@ -302,11 +302,19 @@ struct Pass {
     }
     return best;
   }
-  // Parts of the sums of a tile kernel with `groups` workgroups, each of which goes through `steps` of 64: as many as fill `slots`, of 8 steps and more
-  static int tile_splits(int64_t groups, int64_t steps, int64_t slots) {
+  // Parts of the sums of a tile kernel with `groups` workgroups, each of which goes through `steps` of 64: as many as fill `slots`, of `least` steps and more
+  static int tile_splits(int64_t groups, int64_t steps, int64_t slots, int64_t least) {
     int64_t s = slots / (groups < 1 ? 1 : groups);
-    if (s > steps / 8) s = steps / 8;
+    if (s > steps / least) s = steps / least;
     return (int)(s < 1 ? 1 : s < 16 ? s : 16);
+  }
+  // of dk and dv: one workgroup a compute unit whatever the parts cost, beyond that where they cost little beside the products (they are written and read in
+  // float32: 2,048 rows a part are 1 / 4 of the products' time).  Two a compute unit run at once; with a causal mask twice as many, since the first
+  // keys see the most rows (us with 1, 2 and 4 parts: 4,096 packed tokens, 32 heads, 8 of keys, 128: -, 249, 194; 8,192 tokens 1,500 (2); 1,024 tokens of 64 x 16 heads,
+  // float16, 64: 71, 85).
+  static int dkdv_splits(int64_t groups, int64_t steps, bool causal) {
+    const int a = tile_splits(groups, steps, 256, 4), b = tile_splits(groups, steps, causal ? 1024 : 512, 32);
+    return a > b ? a : b;
   }
 
   void forward(void *y, const int64_t y_stride[3]) {
@@ -322,7 +330,7 @@ struct Pass {
     } else {
       chosen.forward_rows = 128;
       c.row_tiles = (int32_t)up(rows(), chosen.forward_rows);
-      c.splits = tile_splits(heads() * c.row_tiles, c.tiles, 512);
+      c.splits = tile_splits(heads() * c.row_tiles, c.tiles, 512, 8);
       l.groups = threads(heads() * c.row_tiles * c.splits, 256);
     }
     chosen.forward_splits = c.splits;
@@ -361,7 +369,7 @@ struct Pass {
     if (K > 0) {
       chosen.dkdv_keys = 128;
       c.key_tiles = (int32_t)up(K, chosen.dkdv_keys);
-      c.splits = tile_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), a->causal ? 1024 : 512);
+      c.splits = dkdv_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), a->causal != 0);
       chosen.dkdv_splits = c.splits;
       const int64_t words = heads() * K * (c.width4 / 4);
       if (c.splits > 1) {

@@ -34,6 +34,7 @@ typedef short s8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf8 __attribute__((ext_vector_type(8)));
 typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
+typedef __attribute__((address_space(3))) const uint32_t lds_word;
 
 struct Bf16 {
   static __device__ __forceinline__ f16 mfma(s8 a, s8 b, f16 c) {
@@ -74,6 +75,25 @@ template <class T> __device__ __forceinline__ s8 pack8(const f16 &v, int from) {
 }
 // row of a 32 x 32 result in register r, less 4 h
 __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r >> 2); }
+
+// which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
+// which see the most
+struct Place { int b, h, hb, tile, split; };
+__device__ __forceinline__ Place place_of(const AttnCall &c, int tiles, bool last_first) {
+  const int per = c.heads_abreast * tiles * c.splits;
+  int i = blockIdx.x;
+  const int band = i / per;
+  i -= band * per;
+  Place p;
+  p.hb = band * c.heads_abreast + i % c.heads_abreast;
+  i /= c.heads_abreast;
+  p.split = i % c.splits;
+  p.tile = i / c.splits;
+  if (last_first) p.tile = tiles - 1 - p.tile;
+  p.b = p.hb / c.kv_heads;
+  p.h = p.hb - p.b * c.kv_heads;
+  return p;
+}
 
 // ---------------------------------------------------------------------------------------------- shared memory
 // Rows of D elements (64, or up to 128 in rows of 128), as direct loads leave them: 1 KiB of whole rows by each.  The banks give 256 bytes a cycle: 16 lanes of
@@ -210,6 +230,31 @@ __device__ __forceinline__ void clear_none(lds_char *lds, const uint32_t *words,
     if (words[idx / Shape<D>::CHUNKS] == ATTN_NONE) clear_row<D>(lds, idx / Shape<D>::CHUNKS, idx % Shape<D>::CHUNKS);
 }
 
+// A tile of 64 keys, their values and words, in one of two slots
+template <int D, int WAVES>
+struct TileFeed {
+  typedef KeyFeed<D, ATTN_TILE, WAVES> Feed;
+  enum { VALUES = Feed::BYTES, WORDS = 2 * Feed::BYTES, SLOT = WORDS + ATTN_TILE * 4, BYTES = 2 * SLOT };
+  Feed keys, values;
+  const uint32_t *words;                   // null: none
+  __device__ __forceinline__ void start(const AttnCall &c, const Place &p, int wave, int lane) {
+    keys.start(c.k, p.b, p.h, c.keys, c.dim, wave, lane);
+    values.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
+    words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
+  }
+  __device__ __forceinline__ void load(int tile, uint32_t lds, int wave, int lane) const {
+    keys.load(tile * ATTN_TILE, lds, wave);
+    values.load(tile * ATTN_TILE, lds + VALUES, wave);
+    if (words && wave == 0) load_lds4(descriptor(words + (int64_t)tile * ATTN_TILE, ATTN_TILE * 4), lane * 4, lds + WORDS);
+  }
+  // zeros in the rows at `rows` of keys of no document
+  __device__ __forceinline__ static void clear(lds_char *slot, lds_char *rows, int tid) {
+    lds_word *w = (lds_word *)(slot + WORDS);
+    for (int idx = tid; idx < ATTN_TILE * Shape<D>::CHUNKS; idx += 64 * WAVES)
+      if (w[idx / Shape<D>::CHUNKS] == ATTN_NONE) clear_row<D>(rows, idx / Shape<D>::CHUNKS, idx % Shape<D>::CHUNKS);
+  }
+};
+
 // ---------------------------------------------------------------------------------------------- what is seen
 struct Range { int first, last, flags; };   // documents of some tokens, as those of a tile
 
@@ -286,18 +331,20 @@ struct KeyWalk {
   }
 };
 
-// Of the keys k0 + row_of(r): tells set(r, .) whether the query at `pos` of the document `word` sees it
-template <class F>
-__device__ __forceinline__ void seen_keys(const AttnCall &c, const uint32_t *words, int k0, int pos, uint32_t word, F set) {
-  const int rel = words ? (c.causal ? pos - k0 : 64) : (c.causal && pos < c.keys - 1 ? pos : c.keys - 1) - k0;
-  if (!words) {
+// Of the keys k0 + row_of(r), whose words are at `words`: tells set(r, .) whether the query at `pos` of the document `word` sees it
+template <class Words, class F>
+__device__ __forceinline__ void seen_keys(const AttnCall &c, Words words, int k0, int pos, uint32_t word, F set) {
+  const int rel = c.k_words ? (c.causal ? pos - k0 : 64) : (c.causal && pos < c.keys - 1 ? pos : c.keys - 1) - k0;
+  if (!c.k_words) {
 #pragma unroll
     for (int r = 0; r < 16; ++r) set(r, row_of(r) <= rel);
     return;
   }
 #pragma unroll
   for (int g = 0; g < 4; ++g) {
-    const u4 w = *(const u4 *)(words + k0 + g * 8);
+    u4 w;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) w[e] = words[g * 8 + e];
     if (c.prefix) {
 #pragma unroll
       for (int e = 0; e < 4; ++e) set(g * 4 + e, (w[e] == (word | 1u)) | ((w[e] == word) & (g * 8 + e <= rel)));
@@ -378,7 +425,8 @@ struct Softmax {
     return s;
   }
   // values from the products with the keys k0 + row_of(r); hidden ones are those of no weight
-  static __device__ __forceinline__ void values_of(const AttnCall &c, const QueryRow<T, D> &row, const uint32_t *words, int k0, bool masked, f16 &s) {
+  template <class Words>
+  static __device__ __forceinline__ void values_of(const AttnCall &c, const QueryRow<T, D> &row, Words words, int k0, bool masked, f16 &s) {
     if (CAP || SLOPE) {
       const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
 #pragma unroll
@@ -479,75 +527,49 @@ __device__ __forceinline__ void store8_low(uint16_t *p, int d, int width, f4 a, 
 }
 
 // ---------------------------------------------------------------------------------------------- forward
-// which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
-// which see the most
-struct Place { int b, h, hb, tile, split; };
-__device__ __forceinline__ Place place_of(const AttnCall &c, int tiles, bool last_first) {
-  const int per = c.heads_abreast * tiles * c.splits;
-  int i = blockIdx.x;
-  const int band = i / per;
-  i -= band * per;
-  Place p;
-  p.hb = band * c.heads_abreast + i % c.heads_abreast;
-  i /= c.heads_abreast;
-  p.split = i % c.splits;
-  p.tile = i / c.splits;
-  if (last_first) p.tile = tiles - 1 - p.tile;
-  p.b = p.hb / c.kv_heads;
-  p.h = p.hb - p.b * c.kv_heads;
-  return p;
-}
-
 // 128 rows, 32 a wavefront; two wavefronts a SIMD (three with rows of 64), of different workgroups, so that one's products run beside another's
 // exponentials.
 template <class T, int D, int CAP, int SLOPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_forward(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4, NT = 64 * WAVES;
-  typedef KeyFeed<D, ATTN_TILE, WAVES> Feed;
+  constexpr int WAVES = 4;
+  typedef TileFeed<D, WAVES> Feed;
   typedef Softmax<T, D, CAP, SLOPE> Soft;
-  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES > WAVES * TURN_BYTES ? 4 * Feed::BYTES : WAVES * TURN_BYTES];
+  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > WAVES * TURN_BYTES ? Feed::BYTES : WAVES * TURN_BYTES];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.row_tiles, true);
   const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
-  QueryRow<T, D> row;
-  row.start(c, p.b, p.h, wave_row, lane);
-  Feed kf, vf;
-  kf.start(c.k, p.b, p.h, c.keys, c.dim, wave, lane);
-  vf.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
-  const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
+  Feed feed;
+  feed.start(c, p, wave, lane);
   KeyWalk walk;
   walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, p.split, c.splits, c.tiles);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
+  QueryRow<T, D> row;
+  row.start(c, p.b, p.h, wave_row, lane);
   Soft soft;
   soft.start();
 
   int slot = 0;
-  Visit next = walk.next(c, lane);
-  if (next.tile >= 0) {
-    kf.load(next.tile * ATTN_TILE, lds0, wave);
-    vf.load(next.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
-  }
   while (next.tile >= 0) {
     const Visit now = next;
     next = walk.next(c, lane);
     arrived();                              // this tile is there, and the other slot has been read by everybody
-    lds_char *keys = lds + slot * 2 * Feed::BYTES, *values = keys + Feed::BYTES;
+    lds_char *here = lds + slot * Feed::SLOT, *values = here + Feed::VALUES;
     if (now.some_none) {
-      clear_none<D, ATTN_TILE, NT>(values, words + now.tile * ATTN_TILE, tid);
+      Feed::clear(here, values, tid);
       arrived();
     }
     slot ^= 1;
-    if (next.tile >= 0) {
-      kf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
-      vf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
-    }
+    if (next.tile >= 0) feed.load(next.tile, lds0 + slot * Feed::SLOT, wave, lane);
     if (!now.run) continue;
     const int k0 = now.tile * ATTN_TILE + h4;
-    f16 s = Soft::products(row, keys, 0, lane), t = Soft::products(row, keys, 32, lane);
+    lds_word *words = (lds_word *)(here + Feed::WORDS) + h4;
+    f16 s = Soft::products(row, here, 0, lane), t = Soft::products(row, here, 32, lane);
     Soft::values_of(c, row, words, k0, now.masked, s);
-    Soft::values_of(c, row, words, k0 + 32, now.masked, t);
+    Soft::values_of(c, row, words + 32, k0 + 32, now.masked, t);
     soft.follow(c, Soft::more(Soft::most_of(s), Soft::most_of(t)));
     soft.add(c, s, values, 0, lane);
     soft.add(c, t, values, 32, lane);
@@ -639,7 +661,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
       waited<0>();
     }
     f16 s = Soft::products(row, here, 0, lane);
-    Soft::values_of(c, row, words, k0 + (lane >> 5) * 4, now.masked, s);
+    Soft::values_of(c, row, words + (now.masked ? k0 + (lane >> 5) * 4 : 0), k0 + (lane >> 5) * 4, now.masked, s);
     soft.follow(c, Soft::most_of(s));
     soft.add(c, s, here + Feed::BYTES, 0, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: the next loads go there
@@ -731,14 +753,20 @@ __device__ __forceinline__ float delta_of(const AttnCall &c, const Place &p, int
 template <class T, int D, int CAP, int SLOPE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_dq(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4, NT = 64 * WAVES;
-  typedef KeyFeed<D, ATTN_TILE, WAVES> Feed;
-  __shared__ __attribute__((aligned(1024))) char shared[4 * Feed::BYTES > WAVES * TURN_BYTES ? 4 * Feed::BYTES : WAVES * TURN_BYTES];
+  constexpr int WAVES = 4;
+  typedef TileFeed<D, WAVES> Feed;
+  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > WAVES * TURN_BYTES ? Feed::BYTES : WAVES * TURN_BYTES];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const Place p = place_of(c, c.row_tiles, true);
   const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
+  Feed feed;
+  feed.start(c, p, wave, lane);
+  KeyWalk walk;
+  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, 0, 1, c.tiles);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
   s8 dy[D / 16];
@@ -754,36 +782,23 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     block.slope2[lane] = row.slope2;
     block.pos[lane] = row.pos;
   }
-  Feed kf, vf;
-  kf.start(c.k, p.b, p.h, c.keys, c.dim, wave, lane);
-  vf.start(c.v, p.b, p.h, c.keys, c.dim, wave, lane);
-  const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
-  KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, 0, 1, c.tiles);
   f16 dq[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dq[d] = f16{};
 
   int slot = 0;
-  Visit next = walk.next(c, lane);
-  if (next.tile >= 0) {
-    kf.load(next.tile * ATTN_TILE, lds0, wave);
-    vf.load(next.tile * ATTN_TILE, lds0 + Feed::BYTES, wave);
-  }
   while (next.tile >= 0) {
     const Visit now = next;
     next = walk.next(c, lane);
     arrived();
-    lds_char *keys = lds + slot * 2 * Feed::BYTES, *values = keys + Feed::BYTES;
+    lds_char *keys = lds + slot * Feed::SLOT, *values = keys + Feed::VALUES;
+    lds_word *words = (lds_word *)(keys + Feed::WORDS) + h4;
     if (now.some_none) {
-      clear_none<D, ATTN_TILE, NT>(keys, words + now.tile * ATTN_TILE, tid);
+      Feed::clear(keys, keys, tid);
       arrived();
     }
     slot ^= 1;
-    if (next.tile >= 0) {
-      kf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES, wave);
-      vf.load(next.tile * ATTN_TILE, lds0 + slot * 2 * Feed::BYTES + Feed::BYTES, wave);
-    }
+    if (next.tile >= 0) feed.load(next.tile, lds0 + slot * Feed::SLOT, wave, lane);
     if (!now.run) continue;
 #pragma unroll
     for (int b = 0; b < 2; ++b) {
@@ -801,7 +816,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
         weight_of<CAP>(c, s[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), lse) : lse, all, w);
         dp[r] = w * (dp[r] - delta);
       }
-      if (now.masked) seen_keys(c, words, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
+      if (now.masked) seen_keys(c, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
       for (int k = 0; k < 2; ++k)

@@ -49,7 +49,7 @@ __global__ void __launch_bounds__(64) k_documents(DocumentsCall a, DocumentsCall
     lo = l < lo ? l : lo;
     hi = h > hi ? h : hi;
   }
-  const uint64_t none = __ballot(!some), yes = __ballot(some && pre);
+  const uint64_t none = __ballot(!some && t < c.n), yes = __ballot(some && pre);      // places behind the last token are masked by their number
   if (threadIdx.x == 0)
     c.tiles[block] = AttnTile{lo, hi, (none ? ATTN_SOME_NONE : 0) | (yes ? ATTN_SOME_PREFIX : 0) | (yes == ~0ull ? ATTN_ALL_PREFIX : 0), 0};
 }

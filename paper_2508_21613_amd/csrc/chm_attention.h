@@ -25,8 +25,8 @@ constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles ar
 
 // What the kernel of dq leaves to that of dk and dv about 32 rows, one value after the other (rows behind the last see nothing)
 struct AttnRows {
-  float lse[32];                           // log2 of the sum of powers of two; +inf: the row sees nothing
-  float delta[32];                         // dy . y
+  float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap; +inf: the row sees nothing
+  float delta[32];                         // dy . y; with a cap four times that
   int32_t last[32];                        // last key that a causal mask leaves (no mask: all)
   uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
   float slope2[32];

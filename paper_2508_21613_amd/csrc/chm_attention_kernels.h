@@ -172,10 +172,12 @@ struct RowFeed {
   const char *base;
   int64_t token;
   uint32_t head, off[LOADS];
-  __device__ __forceinline__ void start(const AttnCall &c, const AttnInput &in, int b, int first_head, int wave, int lane) {
+  __device__ __forceinline__ void start(const AttnInput &in, int b, int first_head) {
     base = (const char *)(in.p + b * in.batch + first_head * in.head);
     token = in.token * 2;
     head = (uint32_t)in.head * 2;
+  }
+  __device__ __forceinline__ void keep(const AttnCall &c, int wave, int lane) {
 #pragma unroll
     for (int i = 0; i < LOADS; ++i) off[i] = offset(c, i, 0, 0, wave, lane);
   }
@@ -184,7 +186,14 @@ struct RowFeed {
     const int r = first + (int)row, t = divide(c.by_group, r), g = r - t * c.group;
     return r >= c.rows || (int)chunk * 8 >= c.dim ? OUT : (uint32_t)(t - t0) * (uint32_t)token + (uint32_t)g * head + chunk * 16;
   }
-  // the rows from `first` on (uniform)
+  // the rows from `first` on (uniform), which may lie behind the last
+  __device__ __forceinline__ void once(const AttnCall &c, int first, uint32_t lds, int lane) const {
+    const int t0 = divide(c.by_group, first < c.rows ? first : c.rows - 1);
+    const i4 rsrc = descriptor(base + t0 * token, OUT - 64);
+#pragma unroll
+    for (int i = 0; i < LOADS; ++i) load_lds16(rsrc, offset(c, i, first, t0, 0, lane), lds + i * S::GROUP_BYTES);
+  }
+  // the rows from `first` on, again and again
   __device__ __forceinline__ void load(const AttnCall &c, int first, uint32_t lds, int wave, int lane) const {
     const int t0 = divide(c.by_group, first);
     const i4 rsrc = descriptor(base + t0 * token, OUT - 64);
@@ -369,14 +378,13 @@ __device__ __forceinline__ float capped(const AttnCall &c, float product, float 
 }
 __device__ __forceinline__ float biased(float s, float slope2, float rel, int r) { return fmaf(-slope2, fabsf(rel - (float)row_of(r)), s); }
 
-// A lane's row of the 32 of its wavefront
+// A lane's row of the 32 of its wavefront: row first + lane % 32; those behind the last see what it sees (they are not stored)
 template <class T, int D>
 struct QueryRow {
   s8 q[D / 16];
   int row, token, head, pos;
   uint32_t word;
   float slope2;
-  // row first + lane % 32; those behind the last take its place (they are not stored)
   __device__ __forceinline__ void start(const AttnCall &c, int b, int h, int first, int lane) {
     row = first + (lane & 31);
     const int r = row < c.rows ? row : c.rows - 1;
@@ -385,18 +393,24 @@ struct QueryRow {
     pos = token + c.offset;
     word = c.q_words ? query_word(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token]) : 0;
     slope2 = c.slopes ? c.slopes[head] * 1.44269504088896341f : 0.f;
-    operand(c, c.q, b, lane, q);
   }
-  // this lane's elements of its row of another tensor of the queries' shape
-  __device__ __forceinline__ void operand(const AttnCall &c, const AttnInput &in, int b, int lane, s8 (&out)[D / 16]) const {
-    const uint16_t *p = in.p + b * in.batch + token * in.token + head * in.head;
+  // operands straight from memory, 16 bytes a row and load: for few rows
+  __device__ __forceinline__ void operands(const AttnCall &c, int b, int lane) {
+    const uint16_t *p = c.q.p + b * c.q.batch + token * c.q.token + head * c.q.head;
 #pragma unroll
     for (int k = 0; k < D / 16; ++k) {
       const int d = k * 16 + (lane >> 5) * 8;
-      out[k] = d < c.dim ? *(const s8 *)(p + d) : s8{};
+      q[k] = d < c.dim ? *(const s8 *)(p + d) : s8{};
     }
   }
 };
+// A wavefront's 32 rows of queries or dy to its own memory: whole rows a load
+template <int D>
+__device__ __forceinline__ void bring_rows(const AttnCall &c, const AttnInput &in, const Place &p, int first, uint32_t lds, int lane) {
+  RowFeed<D, 32, 1> feed;
+  feed.start(in, p.b, p.h * c.group);
+  feed.once(c, first, lds, lane);
+}
 
 // A running softmax over blocks of 32 keys: reference (powers of two) and sum.  The reference follows the maximum only when that has grown by more than
 // 2^8: until then weights are up to 256, which 16-bit floats hold as exactly as smaller ones, and nothing has to be rescaled.
@@ -547,10 +561,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, p.split, c.splits, c.tiles);
   Visit next = walk.next(c, lane);
   if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
+  // the queries come by the second slot, a wavefront's to its own part
+  const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
+  static_assert(WAVES * Shape<D>::bytes(32) <= Feed::SLOT, "a slot holds the rows");
+  bring_rows<D>(c, c.q, p, wave_row, lds0 + mine, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
   Soft soft;
   soft.start();
+  waited<0>();
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) row.q[k] = row_fragment<D>(lds + mine, 0, k, lane);
 
   int slot = 0;
   while (next.tile >= 0) {
@@ -622,6 +643,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   const Place p = place_of(c, 1, false);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, 0, lane);
+  row.operands(c, p.b, lane);
   Feed kf, vf;
   kf.start(c.k, p.b, p.h, c.keys, c.dim, 0, lane);
   vf.start(c.v, p.b, p.h, c.keys, c.dim, 0, lane);
@@ -718,36 +740,49 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// p and dz p, dz being the tanh's derivative, of a score from its product; less: what is taken from it, in powers of two
+// p and ds of a score from the products q.k and dy.v.  less: lse (with a bias, and it) in powers of two, less cap2 with a cap; delta: dy.y, four times it with a
+// cap, where ds = p share (1 - share) (4 dy.v - 4 delta)
 template <int CAP>
-__device__ __forceinline__ void weight_of(const AttnCall &c, float product, float less, float &p, float &w) {
-  float share;
-  p = w = exp2_(capped<CAP>(c, product, share) - less);
-  if (CAP) w *= 4.f * (share - share * share);
+__device__ __forceinline__ void gradient(const AttnCall &c, float product, float dp, float less, float delta, float &p, float &ds) {
+  if (CAP) {
+    const float share = __builtin_amdgcn_rcpf(1.f + exp2_(product * c.tanh2));
+    p = exp2_(fmaf(share, -2.f * c.cap2, -less));
+    ds = p * fmaf(-share, share, share) * fmaf(dp, 4.f, -delta);
+  } else {
+    p = exp2_(fmaf(product, c.to2, -less));
+    ds = p * (dp - delta);
+  }
 }
 
-// delta = dy.y of a lane's row.  y is taken with what its rounding took from it: where few keys share a row, dy.v and delta are near each other, and
-// 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3 without, 2.4e-3 with).
+// delta = dy.y of a wavefront's 32 rows, whose dy lie at `dys`, to `out`.  y is taken with what its rounding took from it: where few keys share a row, dy.v and
+// delta are near each other, and 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3
+// without, 2.4e-3 with).  A row by as many lanes as it has chunks.
 template <class T, int D>
-__device__ __forceinline__ float delta_of(const AttnCall &c, const Place &p, int token, int head, const s8 (&dy)[D / 16], int lane) {
+__device__ __forceinline__ void deltas_of(const AttnCall &c, const Place &p, int first, const lds_char *dys, float *out, int lane) {
+  typedef Shape<D> S;
   typedef s8 s8_anywhere __attribute__((aligned(2)));
-  const uint16_t *y = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
-  const uint16_t *low = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
-  float sum = 0.f;
+  constexpr int EACH = S::CHUNKS, ROWS = 64 / EACH;
 #pragma unroll
-  for (int k = 0; k < D / 16; ++k) {
-    const int d = k * 16 + (lane >> 5) * 8;
+  for (int i = 0; i < 32 / ROWS; ++i) {
+    const int row = i * ROWS + lane / EACH, chunk = lane % EACH, d = chunk * 8;
+    const int r = first + row < c.rows ? first + row : c.rows - 1, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
+    const uint16_t *y = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
+    const uint16_t *low = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
+    const s8 dy = *(const __attribute__((address_space(3))) s8 *)(dys + S::row_at(row) + ((uint32_t)chunk ^ S::swizzle(row)) * 16);
+    float sum = 0.f;
     if (d + 8 <= c.width) {
       const s8 a = *(const s8_anywhere *)(y + d), b = *(const s8_anywhere *)(low + d);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[k][e]), T::up((uint16_t)a[e]) + T::up((uint16_t)b[e]), sum);
+      for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[e]), T::up((uint16_t)a[e]) + T::up((uint16_t)b[e]), sum);
     } else {
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (d + e < c.width) sum = fmaf(T::up((uint16_t)dy[k][e]), T::up(y[d + e]) + T::up(low[d + e]), sum);
+        if (d + e < c.width) sum = fmaf(T::up((uint16_t)dy[e]), T::up(y[d + e]) + T::up(low[d + e]), sum);
     }
+#pragma unroll
+    for (int x = EACH / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+    if (chunk == 0) out[row] = sum;
   }
-  return both_sum(sum);
 }
 
 template <class T, int D, int CAP, int SLOPE>
@@ -755,6 +790,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WAVES = 4;
   typedef TileFeed<D, WAVES> Feed;
+  __shared__ float deltas[WAVES][32];
   __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > WAVES * TURN_BYTES ? Feed::BYTES : WAVES * TURN_BYTES];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -767,15 +803,26 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, 0, 1, c.tiles);
   Visit next = walk.next(c, lane);
   if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
+  // dy comes by the second slot, a wavefront's rows to its own part
+  const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
+  static_assert(WAVES * Shape<D>::bytes(32) <= Feed::SLOT, "a slot holds the rows");
+  bring_rows<D>(c, c.dy, p, wave_row, lds0 + mine, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
-  s8 dy[D / 16];
-  row.operand(c, c.dy, p.b, lane, dy);
+  row.operands(c, p.b, lane);
   const bool there = row.row < c.rows;
-  const float lse = c.lse[(int64_t)p.hb * c.rows_pad + (there ? row.row : c.rows - 1)], delta = delta_of<T, D>(c, p, row.token, row.head, dy, lane);
+  const float lse = c.lse[(int64_t)p.hb * c.rows_pad + (there ? row.row : c.rows - 1)];
+  waited<0>();
+  s8 dy[D / 16];
+#pragma unroll
+  for (int k = 0; k < D / 16; ++k) dy[k] = row_fragment<D>(lds + mine, 0, k, lane);
+  deltas_of<T, D>(c, p, wave_row, lds + mine, deltas[wave], lane);
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  const float less = CAP ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[wave][lane & 31] : deltas[wave][lane & 31];
   if (lane < 32 && row.row < c.rows_pad) {
     AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
-    block.lse[lane] = there ? lse : INFINITY;
+    block.less[lane] = there ? less : INFINITY;
     block.delta[lane] = delta;
     block.last[lane] = !there ? INT32_MIN : c.causal ? row.pos : INT32_MAX;
     block.word[lane] = there ? row.word : ATTN_NOBODY;
@@ -812,9 +859,9 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
 #pragma unroll
       for (int r = 0; r < 16; ++r) {
-        float w, all;
-        weight_of<CAP>(c, s[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), lse) : lse, all, w);
-        dp[r] = w * (dp[r] - delta);
+        float weight, ds;
+        gradient<CAP>(c, s[r], dp[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), less) : less, delta, weight, ds);
+        dp[r] = ds;
       }
       if (now.masked) seen_keys(c, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
@@ -929,8 +976,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
     vf.load(key0, lds0 + VALUES, wave);
   }
   Feed qf, df;
-  qf.start(c, c.q, p.b, p.h * c.group, wave, lane);
-  df.start(c, c.dy, p.b, p.h * c.group, wave, lane);
+  qf.start(c.q, p.b, p.h * c.group);
+  df.start(c.dy, p.b, p.h * c.group);
+  qf.keep(c, wave, lane);
+  df.keep(c, wave, lane);
   const uint32_t *q_words = c.q_words ? c.q_words + (int64_t)p.b * c.q_tile_count * ATTN_TILE : nullptr;
   const AttnRows *row_data = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
 
@@ -982,7 +1031,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
     for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, 0, i, lane), row_fragment<D>(values, wave * 32, i, lane), dp);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
-      f4 less = *(lds_f4 *)&known->lse[g * 8 + h4];
+      f4 less = *(lds_f4 *)&known->less[g * 8 + h4];
       const f4 delta = *(lds_f4 *)&known->delta[g * 8 + h4];
       if (SLOPE) {
         const f4 slope2 = *(lds_f4 *)&known->slope2[g * 8 + h4];
@@ -992,10 +1041,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       }
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        float one, two;
-        weight_of<CAP>(c, s[g * 4 + e], less[e], one, two);
-        s[g * 4 + e] = one;
-        dp[g * 4 + e] = two * (dp[g * 4 + e] - delta[e]);
+        float weight, ds;
+        gradient<CAP>(c, s[g * 4 + e], dp[g * 4 + e], less[e], delta[e], weight, ds);
+        s[g * 4 + e] = weight;
+        dp[g * 4 + e] = ds;
       }
     }
     if (now.masked) {

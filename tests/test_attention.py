@@ -342,6 +342,67 @@ def test_one_projection_and_heads_first(ops):
         check(name, t, want[name])
 
 
+def test_a_result_among_the_rows_of_the_inputs(ops):
+    """queries, keys, values and the result as columns of the same rows of memory"""
+    B, T, H, d = 2, 90, 3, 40
+    buf = torch.randn((B, T, 4 * H * d + 5), generator=gen(2), device="cuda").half()
+    q, k, v, y = (buf[:, :, i * H * d:(i + 1) * H * d].unflatten(2, (H, d)) for i in range(4))
+    rest = buf[:, :, 4 * H * d:].clone()
+    want = formula(q, k, v)["y"]
+    assert ops.attention_forward(q, k, v, out=y) is y
+    check("y", y, want)
+    assert torch.equal(buf[:, :, 4 * H * d:], rest)
+    # a part of the tokens of a longer buffer, the others left as they were
+    long = torch.full((B, 3 * T, H, d), 7.0, dtype=torch.float16, device="cuda")
+    ops.attention_forward(q, k, v, out=long[:, T:2 * T])
+    assert torch.equal(long[:, T:2 * T], y) and bool((long[:, :T] == 7).all()) and bool((long[:, 2 * T:] == 7).all())
+
+
+def test_refusals(ops):
+    from paper_2508_21613_amd.binding import ChmError
+    q, k, v, dy = inputs(1, 2, 10, 12, 4, 2, 64, torch.bfloat16)
+    ids = torch.zeros((2, 10), dtype=torch.int32, device="cuda")
+    kid = torch.zeros((2, 12), dtype=torch.int32, device="cuda")
+    slopes = slopes_of(4)
+    bad = [((q.cpu(), k, v), {}), ((q, k.cpu(), v), {}), ((q, k, v.half()), {}), ((q.float(), k.float(), v.float()), {}), ((q[0], k, v), {}), ((q, k[:1], v), {}),
+           ((q, k, v[:, :5]), {}), ((q[:, :, :3], k, v), {}), ((q[..., :32], k, v), {}), ((q.transpose(2, 3), k, v), {}), ((q, k[:, :, :0], v[:, :, :0]), {}),
+           ((q, k, v), dict(scale=0)), ((q, k, v), dict(scale=-1)), ((q, k, v), dict(scale=float("nan"))), ((q, k, v), dict(cap=-1)), ((q, k, v), dict(cap=float("inf"))),
+           ((q, k, v), dict(slopes=slopes[:3])), ((q, k, v), dict(slopes=slopes.double())), ((q, k, v), dict(slopes=slopes.cpu())), ((q, k, v), dict(slopes=[1.0] * 4)),
+           ((q, k, v), dict(documents=ids)), ((q, k, v), dict(documents=(ids, ids))), ((q, k, v), dict(documents=(ids, kid.long()))), ((q, k, v), dict(documents=(ids.float(), kid.float()))),
+           ((q, k, v), dict(documents=(ids, kid, kid))), ((q, k, v), dict(documents=(ids, None))), ((q, k, v), dict(prefix=kid)), ((q, k, v), dict(prefix=kid.bool(), causal=False)),
+           ((q, k, v), dict(prefix=kid.bool()[:, :5])), ((q, k, v), dict(out=q)), ((q, k, v), dict(out=q[:1])), ((q, k, v), dict(out=q.half())), ((q, k, v), dict(out=k)),
+           ((q, k, v), dict(out=torch.empty_like(q[:1]).expand(2, -1, -1, -1)))]
+    for args, kw in bad:
+        with pytest.raises(ChmError):
+            ops.attention_forward(*args, **kw)
+    big = torch.zeros((1, 3, 1, 136), dtype=torch.bfloat16, device="cuda")
+    with pytest.raises(ChmError):
+        ops.attention_forward(big, big, big)
+    y, saved = ops.attention_forward(q, k, v, save=True)
+    for args in ((dy[:, :5], q, k, v, y, saved), (dy.half(), q, k, v, y, saved), (dy, q, k, v, y[:1], saved), (dy, q, k, v, y, saved[:100]), (dy, q, k, v, y, None),
+                 (dy, q, k, v, y, saved.view(torch.int8))):
+        with pytest.raises(ChmError):
+            ops.attention_backward(*args)
+    for out in ((q, k, v), (torch.empty_like(q), torch.empty_like(k)), (torch.empty_like(q), torch.empty_like(k), v), (torch.empty_like(k), torch.empty_like(k), torch.empty_like(v))):
+        with pytest.raises(ChmError):
+            ops.attention_backward(dy, q, k, v, y, saved, out=out)
+
+
+def test_inputs_that_require_a_gradient(ops):
+    """the results are no part of autograd's graph: refused where the gradient would be lost, taken where the caller goes on by hand"""
+    from paper_2508_21613_amd.binding import ChmError
+    q, k, v, dy = inputs(1, 1, 20, 20, 2, 2, 64, torch.bfloat16)
+    k.requires_grad_(True)
+    with pytest.raises(ChmError):
+        ops.attention_forward(q, k, v)
+    y, saved = ops.attention_forward(q, k, v, save=True)
+    assert not y.requires_grad and len(ops.attention_backward(dy, q, k, v, y, saved)) == 3
+    with torch.no_grad():
+        assert torch.equal(ops.attention_forward(q, k, v), y)
+    with pytest.raises(ChmError):
+        ops.attention_forward(q, k, v, save=True, slopes=slopes_of(2).requires_grad_(True))
+
+
 def test_lengths_of_zero(ops):
     for B, T, K in ((0, 5, 5), (2, 0, 0), (2, 0, 70), (2, 70, 0), (2, 3, 0)):
         x = inputs(1, B, T, K, 4, 2, 64, torch.bfloat16)

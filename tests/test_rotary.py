@@ -159,6 +159,22 @@ def test_many_tokens(ops):
     assert ops.Rotary(d).rotate(x[:0], pos[:0]).shape == (0, H, d) and rope.rotate(x[:5, :0], pos[:5]).shape == (5, 0, d)
 
 
+def test_refusals(ops):
+    from paper_2508_21613_amd.binding import ChmError
+    rope = ops.Rotary(64, [8, 24])
+    x, pos = heads(1, 20, 4, 64, torch.bfloat16), torch.zeros((2, 20), dtype=torch.int64, device="cuda")
+    for args, kw in (((x.cpu(), pos), {}), ((x, pos.cpu()), {}), ((x[..., :32], pos), {}), ((x[0], pos), {}), ((x, pos[0]), {}), ((x, pos[:, :7]), {}), ((x, pos.float()), {}),
+                     ((x.double(), pos), {}), ((x.transpose(1, 2), pos), {}), ((x, pos), dict(out=x[:, :2])), ((x, pos), dict(out=x.half())), ((None, pos), {}), ((x, None), {}),
+                     ((x[:, 1:], pos), dict(out=x[:, :3])), ((x, pos), dict(out=x[:1].expand(20, -1, -1)))):
+        with pytest.raises(ChmError):
+            rope.rotate(*args, **kw)
+    x = x.clone().requires_grad_(True)
+    with pytest.raises(ChmError):
+        rope.rotate(x, pos)
+    with torch.no_grad():
+        assert rope.rotate(x, pos).shape == x.shape
+
+
 def test_captured_and_on_another_stream(ops):
     rope = ops.Rotary(64, [8, 24])
     x, pos = heads(1, 200, 8, 64, torch.bfloat16), torch.randint(0, 99, (2, 200), device="cuda")

@@ -5,10 +5,10 @@
 
 A scenario wants the forward and backward time and the memory of every layer, which the paper's profiler collects at run time (System
 Design, workflow step 1): a job's tables come from the job.  `Stage` runs the part of such a step that this package has operators for: the
-embedding of the first stage and gated feed-forward blocks (no attention, norms, output head or optimizer), forward and backward over the
-micro-batches of a step in 1F1B order, gradients added up in float32 and clipped at the end.  `measure` times every layer on the GPU with
-events (the clipping is the step's, and in no table), `scenario` makes a scenario of the tables, and the command searches it for the best plan
-after the given failures.
+embedding of the first stage and gated feed-forward blocks (no projections of attention, norms, output head or optimizer), forward and backward over the
+micro-batches of a step in 1F1B order, gradients added up in float32 and clipped at the end.  `Attention` is what lies between an attention's
+projections.  `measure` times every layer on the GPU with events (the clipping is the step's, and in no table), `measure_attention` an attention,
+`scenario` makes a scenario of the tables, and the command searches it for the best plan after the given failures.
 """
 import argparse
 import collections
@@ -91,6 +91,38 @@ class Stage:
         return self.clipper.clip(max_norm, sumsq=sumsq), to_inputs
 
 
+class Attention:
+    """What lies between an attention's projections: rotary positions of queries and keys, and attention, causal within each document.  Options as those of
+    operators.Rotary (sections, base) and operators.attention_forward (cap, slopes)."""
+
+    def __init__(self, heads, kv_heads, head_dim, sections=None, base=10000.0, cap=0.0, slopes=None):
+        self.heads, self.kv_heads, self.head_dim = heads, kv_heads, head_dim
+        self.rotary = operators.Rotary(head_dim, sections, base=base)
+        self.options = dict(cap=cap, slopes=slopes)
+
+    def _parts(self, x):
+        return [t[None] for t in torch.split(x, [self.heads, self.kv_heads, self.kv_heads][:2 if x.shape[1] < self.heads + 2 * self.kv_heads else 3], dim=1)]
+
+    def forward(self, qkv, positions, documents=None, prefix=None):
+        """qkv [tokens, heads + 2 kv_heads, head_dim], one projection's result; positions as Rotary's; documents and prefix [tokens] as
+        attention_forward's.  Returns [tokens, heads, head_dim] and what the backward pass needs."""
+        turned = self.rotary.rotate(qkv[:, :self.heads + self.kv_heads], positions)
+        q, k = self._parts(turned)
+        v = qkv[None, :, self.heads + self.kv_heads:]
+        masks = dict(documents=None if documents is None else documents[None], prefix=None if prefix is None else prefix[None])
+        y, saved = operators.attention_forward(q, k, v, save=True, **masks, **self.options)
+        return y[0], (turned, qkv, positions, masks, y, saved)
+
+    def backward(self, dy, kept):
+        """the gradient of qkv"""
+        turned, qkv, positions, masks, y, saved = kept
+        grads = torch.empty_like(qkv, memory_format=torch.contiguous_format)
+        operators.attention_backward(dy[None], *self._parts(turned), qkv[None, :, self.heads + self.kv_heads:], y, saved, out=self._parts(grads), **masks, **self.options)
+        both = grads[:, :self.heads + self.kv_heads]
+        self.rotary.gradient(both, positions, out=both)
+        return grads
+
+
 class _Queued:
     """Times of calls on the GPU alone: fills of a large buffer keep it busy until the calls between two marks have all been made, more of them
     as long as it came to the first mark before that.  The calls find their operands out of the caches, as in a step."""
@@ -150,11 +182,36 @@ def measure(stage, tokens, repeats=10, optimizer_bytes=12, seed=1):
     return {"fwd_us": fwd, "bwd_us": bwd, "mem_mib": mem, "act_mib": act}
 
 
-def scenario(tables, layers, pp, dp, micro_batches, failed, comm_us, mem_cap_mib, **kw):
+def measure_attention(attention, tokens, dtype=torch.bfloat16, positions=None, documents=None, prefix=None, repeats=10, seed=1, device="cuda"):
+    """What an attention adds to a block of micro-batches of `tokens` tokens: forward and backward time in us and MiB kept per micro-batch in flight.
+    positions: those of a text by default."""
+    g = torch.Generator(device=device)
+    g.manual_seed(seed)
+    heads = attention.heads + 2 * attention.kv_heads
+    qkv = torch.empty((tokens, heads, attention.head_dim), dtype=dtype, device=device).normal_(0.0, 1.0, generator=g)
+    dy = torch.empty((tokens, attention.heads, attention.head_dim), dtype=dtype, device=device).normal_(0.0, 0.05, generator=g)
+    if positions is None:
+        positions = torch.arange(tokens, device=device).expand(attention.rotary.axes, -1)
+    kept = None
+
+    def forward():
+        nonlocal kept
+        kept = attention.forward(qkv, positions, documents, prefix)[1]
+
+    timed = _Queued(torch.device(device))
+    times = [timed(forward, lambda: attention.backward(dy, kept)) for _ in range(repeats + 2)]
+    fwd, bwd = [max(1, round(statistics.median(t) * 1e3)) for t in zip(*times[2:])]
+    held = sum(t.numel() * t.element_size() for t in kept if torch.is_tensor(t))
+    return {"fwd_us": fwd, "bwd_us": bwd, "act_mib": -(-held // MIB)}
+
+
+def scenario(tables, layers, pp, dp, micro_batches, failed, comm_us, mem_cap_mib, attention=None, **kw):
     """The scenario of a model of `layers` equal blocks behind an embedding: `tables` (measure) of a stage with an embedding and one
-    block.  The embedding's times, weights and kept tokens are added to the first block's: it runs on the same node."""
+    block, `attention` (measure_attention) what an attention adds to every block.  The embedding's times, weights and kept tokens are added to the
+    first block's: it runs on the same node."""
     def spread(name):
         first, block = tables[name]
+        block += (attention or {}).get(name, 0)
         a = np.full(layers, block, dtype=np.int32)
         a[0] += first
         return a
@@ -169,7 +226,8 @@ def main(argv=None):
                               ("features", 11008, "features of a block"), ("vocabulary", 32000, "rows of the embedding"),
                               ("tokens", 4096, "tokens of a micro-batch"), ("pp", 4, "stages"), ("dp", 2, "pipelines"),
                               ("micro-batches", 8, "micro-batches of a pipeline"), ("comm-us", 150, "time of a stage boundary"),
-                              ("mem-cap-mib", 288 * 1024 * 9 // 10, "memory of a node")):
+                              ("mem-cap-mib", 288 * 1024 * 9 // 10, "memory of a node"), ("heads", 0, "heads of the blocks' attention, 0: none"),
+                              ("kv-heads", 0, "heads of its keys and values, 0: as many"), ("documents", 1, "documents of a micro-batch")):
         p.add_argument("--" + name, type=int, default=value, help="%s (%d)" % (text, value))
     p.add_argument("--failed", type=int, nargs="+", default=[3], help="nodes that have failed, pipeline x stages + stage (3)")
     a = p.parse_args(argv)
@@ -180,7 +238,14 @@ def main(argv=None):
     print("one step of an embedding and a block: gradient norm %.4g" % float(norm))
     for name, values in tables.items():
         print("%-8s embedding %6d   block %6d" % (name, *values))
-    g = binding.Scenario(scenario(tables, a.layers, a.pp, a.dp, a.micro_batches, a.failed, a.comm_us, a.mem_cap_mib))
+    extra = None
+    if a.heads:
+        if a.width % a.heads:
+            p.error("--width must be a multiple of --heads")
+        ids = torch.arange(a.tokens, device="cuda") * a.documents // a.tokens
+        extra = measure_attention(Attention(a.heads, a.kv_heads or a.heads, a.width // a.heads), a.tokens, documents=ids if a.documents > 1 else None)
+        print("attention's part between its projections: " + "  ".join("%s %d" % item for item in extra.items()))
+    g = binding.Scenario(scenario(tables, a.layers, a.pp, a.dp, a.micro_batches, a.failed, a.comm_us, a.mem_cap_mib, attention=extra))
     rc, best = g.search_best()
     if rc != binding.OK:
         print("no plan:", binding.strerror(rc))

@@ -31,6 +31,7 @@ struct AttnRows {
   uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
   float slope2[32];
   int32_t pos[32];
+  AttnTile documents;                      // of all of them
 };
 constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // with or without the lowest bit it equals no key's word, ATTN_NONE neither
 
@@ -59,12 +60,13 @@ struct AttnCall {
   int32_t splits;
   float *part, *part2;                     // forward: [splits][batch * kv_heads][rows][width4] and (maximum, sum); backward: dk and dv [splits][batch * kv_heads][keys][width4]
   int32_t width4;                          // width rounded up to 4
-  // layout of the launch
-  int32_t row_tiles, key_tiles, heads_abreast;
+  // layout of the launch: the workgroups' tiles of rows or keys
+  int32_t tiles_here, heads_abreast;
+  AttnDivide by_abreast, by_splits, by_tiles, by_kv_heads;
 };
 
-// Kernels of a pass; dim: 64 or 128.  false: HIP failed.
-struct AttnLaunch { int32_t dim; uint32_t groups; void *stream; };
+// Kernels of a pass; dim: 64 or 128; parts: wavefronts that share a sum, 1 or 2.  false: HIP failed.
+struct AttnLaunch { int32_t dim, parts; uint32_t groups; void *stream; };
 bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_forward_f16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_dq_bf16(const AttnCall &c, const AttnLaunch &l);

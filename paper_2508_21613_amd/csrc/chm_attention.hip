@@ -222,6 +222,8 @@ struct Pass {
     c.v = input(a->v, a->v_stride, a->batch, a->keys, a->kv_heads);
     chosen.dim = d8 <= 64 ? 64 : 128;
     c.heads_abreast = heads() % 8 == 0 ? 8 : (int32_t)heads();
+    c.by_abreast = divide_by(c.heads_abreast);
+    c.by_kv_heads = divide_by(a->kv_heads);
   }
   int64_t heads() const { return a->batch * a->kv_heads; }
   int64_t rows() const { return a->tokens * group_of(a); }
@@ -230,6 +232,15 @@ struct Pass {
   uint32_t threads(int64_t groups, int64_t each) {
     fits = fits && groups * each <= UINT32_MAX;
     return (uint32_t)groups;
+  }
+
+  // a launch of `tiles` tiles of every head in `splits` parts
+  AttnLaunch layout(int64_t tiles, int splits, int parts) {
+    c.tiles_here = (int32_t)tiles;
+    c.splits = splits;
+    c.by_tiles = divide_by(tiles);
+    c.by_splits = divide_by(splits);
+    return AttnLaunch{chosen.dim, parts, threads(heads() * tiles * splits, 256), st};
   }
 
   // Inputs as the tiles take them: 16-byte rows, and 64 of them within offsets of 31 bits
@@ -308,30 +319,34 @@ struct Pass {
     if (s > steps / least) s = steps / least;
     return (int)(s < 1 ? 1 : s < 16 ? s : 16);
   }
-  // of dk and dv: one workgroup a compute unit whatever the parts cost, beyond that where they cost little beside the products (they are written and read in
-  // float32: 2,048 rows a part are 1 / 4 of the products' time).  Two a compute unit run at once; with a causal mask twice as many, since the first
-  // keys see the most rows (us with 1, 2 and 4 parts: 4,096 packed tokens, 32 heads, 8 of keys, 128: -, 249, 194; 8,192 tokens 1,500 (2); 1,024 tokens of 64 x 16 heads,
-  // float16, 64: 71, 85).
-  static int dkdv_splits(int64_t groups, int64_t steps, bool causal) {
-    const int a = tile_splits(groups, steps, 256, 4), b = tile_splits(groups, steps, causal ? 1024 : 512, 32);
+  // Of dk and dv: as many as run at once, two a compute unit; with a causal mask, where the first keys see the most rows, twice as many if each keeps work
+  // enough to be worth its sums' way through memory in float32.  us with the join, 32 heads, 8 of keys, 128, causal, by parts: 512 tokens 38 (4), 33 (8);
+  // 1,024 tokens 74 (4), 55 (8), 60 (12); 2,048 tokens 146 (4), 127 (8), 155 (12), without a mask 169 (4), 198 (8); 4,096 tokens 530 (2), 353 (4), 440 (8); 8,192
+  // tokens 2,087 (1), 1,297 (2), 1,308 (4).  Rows of 64 have twice the workgroups and half the steps: 16 heads, 512 tokens 15 (1), 18 (2).
+  static int dkdv_splits(int64_t groups, int64_t steps, bool causal, int dim) {
+    const int a = tile_splits(groups, steps, 512, dim == 64 ? 8 : 4), b = causal ? tile_splits(groups, steps, 1024, 16) : 1;
     return a > b ? a : b;
   }
+
+  // Rows of a workgroup.  64 of them take half as long as 128 and cost more: taken where the whole launch is no more than the workgroups that run at
+  // once, with a causal mask, where they differ, twice that.
+  bool few_groups() const { return heads() * up(rows(), 128) <= (a->causal ? 512 : 256); }
+  int forward_tile() const { return chosen.dim == 64 || (few_groups() && c.tiles < 64) ? 64 : 128; }
+  int dq_tile() const { return chosen.dim == 64 ? (heads() * up(rows(), 128) <= 1024 ? 64 : 128) : few_groups() ? 64 : 128; }
 
   void forward(void *y, const int64_t y_stride[3]) {
     c.y = output(y, y_stride, a->batch, a->tokens, a->heads);
     if (a->batch == 0 || a->tokens == 0) return;
     inputs(nullptr);
     chosen.few = rows() <= FEW_ROWS;
-    AttnLaunch l{chosen.dim, 0, st};
+    AttnLaunch l;
     if (chosen.few) {
       chosen.forward_rows = FEW_ROWS;
-      c.splits = few_splits(heads(), c.tiles, chosen.dim);
-      l.groups = threads(heads() * c.splits, 256);
+      l = layout(1, few_splits(heads(), c.tiles, chosen.dim), 1);
     } else {
-      chosen.forward_rows = 128;
-      c.row_tiles = (int32_t)up(rows(), chosen.forward_rows);
-      c.splits = tile_splits(heads() * c.row_tiles, c.tiles, 512, 8);
-      l.groups = threads(heads() * c.row_tiles * c.splits, 256);
+      chosen.forward_rows = forward_tile();
+      const int64_t tiles = up(rows(), chosen.forward_rows);
+      l = layout(tiles, tile_splits(heads() * tiles, c.tiles, chosen.dim == 64 ? 768 : 512, 8), 128 / chosen.forward_rows);
     }
     chosen.forward_splits = c.splits;
     const int64_t all = heads() * rows();
@@ -360,23 +375,20 @@ struct Pass {
     inputs(g);
     c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
     if (T > 0) {
-      chosen.dq_rows = 128;
-      c.row_tiles = (int32_t)up(rows(), chosen.dq_rows);
-      c.splits = 1;
-      const AttnLaunch l{chosen.dim, threads(heads() * c.row_tiles, 256), st};
+      chosen.dq_rows = dq_tile();
+      const AttnLaunch l = layout(up(rows(), chosen.dq_rows), 1, 128 / chosen.dq_rows);
       if (run && fits) ok = ok && (bf16() ? attn_dq_bf16 : attn_dq_f16)(c, l);
     }
     if (K > 0) {
-      chosen.dkdv_keys = 128;
-      c.key_tiles = (int32_t)up(K, chosen.dkdv_keys);
-      c.splits = dkdv_splits(heads() * c.key_tiles, up(rows(), ATTN_TILE), a->causal != 0);
+      chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
+      const int64_t tiles = up(K, chosen.dkdv_keys);
+      const AttnLaunch l = layout(tiles, dkdv_splits(heads() * tiles, up(rows(), ATTN_TILE), a->causal != 0, chosen.dim), 128 / chosen.dkdv_keys);
       chosen.dkdv_splits = c.splits;
       const int64_t words = heads() * K * (c.width4 / 4);
       if (c.splits > 1) {
         c.part = (float *)arena.take((uint64_t)(c.splits * words) * 16);
         c.part2 = (float *)arena.take((uint64_t)(c.splits * words) * 16);
       }
-      const AttnLaunch l{chosen.dim, threads(heads() * c.key_tiles * c.splits, 256), st};
       const uint32_t joins = threads(up(words, 256), 256);
       if (!run || !fits) return;
       ok = ok && (bf16() ? attn_dkdv_bf16 : attn_dkdv_f16)(c, l);

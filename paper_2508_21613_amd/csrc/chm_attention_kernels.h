@@ -55,6 +55,12 @@ constexpr float LOWEST = -1.5e38f;          // reference of a row that has met n
 constexpr uint32_t OUT = 0x7fffffff;        // offset behind every buffer: reads as zero
 
 __device__ __forceinline__ int divide(const AttnDivide &d, int n) { return d.m ? (int)(__umulhi((uint32_t)n, d.m) >> d.shift) : n; }
+// the lane's number, worked out where it is used and nowhere before: for loops that have no register left
+__device__ __forceinline__ int own_lane() {
+  int lane;
+  asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=&v"(lane));
+  return lane;
+}
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
 
 // the sum or maximum over both halves of the wavefront
@@ -79,18 +85,14 @@ __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r
 // which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
 // which see the most
 struct Place { int b, h, hb, tile, split; };
-__device__ __forceinline__ Place place_of(const AttnCall &c, int tiles, bool last_first) {
-  const int per = c.heads_abreast * tiles * c.splits;
-  int i = blockIdx.x;
-  const int band = i / per;
-  i -= band * per;
+__device__ __forceinline__ Place place_of(const AttnCall &c, bool last_first) {
   Place p;
-  p.hb = band * c.heads_abreast + i % c.heads_abreast;
-  i /= c.heads_abreast;
-  p.split = i % c.splits;
-  p.tile = i / c.splits;
-  if (last_first) p.tile = tiles - 1 - p.tile;
-  p.b = p.hb / c.kv_heads;
+  const int i = blockIdx.x, j = divide(c.by_abreast, i), k = divide(c.by_splits, j), band = divide(c.by_tiles, k);
+  p.split = j - k * c.splits;
+  p.tile = k - band * c.tiles_here;
+  if (last_first) p.tile = c.tiles_here - 1 - p.tile;
+  p.hb = band * c.heads_abreast + i - j * c.heads_abreast;
+  p.b = divide(c.by_kv_heads, p.hb);
   p.h = p.hb - p.b * c.kv_heads;
   return p;
 }
@@ -270,45 +272,75 @@ struct Range { int first, last, flags; };   // documents of some tokens, as thos
 __device__ __forceinline__ Range join(Range a, const AttnTile &t) {
   return Range{t.first < a.first ? t.first : a.first, t.last > a.last ? t.last : a.last, a.flags | (t.flags & ATTN_SOME_NONE)};
 }
-// documents of the tokens [from, to] of a sequence, whole tiles of 64 of them
+// documents of the tokens [from, to] of a sequence, whole tiles of 64 of them, of which there are at most N: all are asked for at once
+template <int N>
 __device__ __forceinline__ Range range_of(const AttnTile *tiles, int from, int to) {
+  AttnTile x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = tiles[from / ATTN_TILE + i < to / ATTN_TILE ? from / ATTN_TILE + i : to / ATTN_TILE];
   Range r{INT32_MAX, -1, 0};
-  for (int t = from / ATTN_TILE; t <= to / ATTN_TILE; ++t) r = join(r, tiles[t]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) r = join(r, x[i]);
   return r;
 }
 
-// whether queries at positions [from, to] of the documents `q` see some (all) of the keys [k0, k1]
-__device__ __forceinline__ void sees(const AttnCall &c, int from, int to, const Range &q, int k0, int k1, const Range &k, bool &some, bool &all) {
-  some = !c.causal || k0 <= to;
-  all = !c.causal || k1 <= from;
-  if (c.k_words) {
-    some = (some || (k.flags & ATTN_SOME_PREFIX)) && k.first <= q.last && q.first <= k.last;
-    all = (all || (k.flags & ATTN_ALL_PREFIX)) && !((k.flags | q.flags) & ATTN_SOME_NONE) && k.first == k.last && q.first == q.last && k.first == q.first;
+// documents of the words of a wavefront's lanes, the same for all of it
+__device__ __forceinline__ Range range_of(uint32_t word) {
+  const uint32_t one = __builtin_amdgcn_readfirstlane(word);
+  if (__all(word == one)) return one == ATTN_NONE ? Range{INT32_MAX, -1, ATTN_SOME_NONE} : Range{(int)(one >> 1), (int)(one >> 1), one & 1 ? ATTN_SOME_PREFIX | ATTN_ALL_PREFIX : 0};
+  const bool none = word == ATTN_NONE;
+  int lo = none ? INT32_MAX : (int)(word >> 1), hi = none ? -1 : (int)(word >> 1);
+#pragma unroll
+  for (int d = 32; d >= 1; d >>= 1) {
+    const int l = __shfl_xor(lo, d), h = __shfl_xor(hi, d);
+    lo = l < lo ? l : lo;
+    hi = h > hi ? h : hi;
   }
+  const uint64_t pre = __ballot(!none && (word & 1));
+  return Range{__builtin_amdgcn_readfirstlane(lo), __builtin_amdgcn_readfirstlane(hi),
+               (__any(none) ? ATTN_SOME_NONE : 0) | (pre ? ATTN_SOME_PREFIX : 0) | (pre == ~0ull ? ATTN_ALL_PREFIX : 0)};
 }
 
-// A tile that the workgroup visits (-1: no more), whether this wavefront does, whether it has to mask, whether there are places of no document
-struct Visit { int tile; bool run, masked, some_none; };
+// What queries at positions [from, to] of the documents `q` see of the keys [k0, k1]: some; all as far as documents go; all as far as their order goes
+struct Sight { bool some, documents, order; };
+__device__ __forceinline__ Sight sees(const AttnCall &c, int from, int to, const Range &q, int k0, int k1, const Range &k) {
+  Sight s{!c.causal || k0 <= to, true, !c.causal || k1 <= from};
+  if (c.k_words) {
+    s.some = (s.some || (k.flags & ATTN_SOME_PREFIX)) && k.first <= q.last && q.first <= k.last;
+    s.documents = !((k.flags | q.flags) & ATTN_SOME_NONE) && k.first == k.last && q.first == q.last && k.first == q.first;
+    s.order = s.order || (k.flags & ATTN_ALL_PREFIX);
+  }
+  return s;
+}
 
-// Tiles of 64 keys that some rows see, in order
+// A tile that the workgroup visits (-1: no more), whether this wavefront does, what it has to mask, whether there are places of no document.  Most
+// tiles of packed documents lie within one, so that only their order is asked for, or the documents where one ends: half of a mask's cost.
+struct Visit {
+  int tile;
+  bool run, documents, order, some_none;
+  __device__ __forceinline__ bool masked() const { return documents | order; }
+};
+
+// Tiles of 64 keys that some of ROWS rows see, in order; a wavefront has 32 of them
+template <int ROWS>
 struct KeyWalk {
   const AttnTile *tiles;
   int group_from, group_to, wave_from, wave_to;           // positions of the queries
-  Range group_docs, wave_docs;
+  Range group_docs, wave_docs;             // the wavefront's are its own rows' (a tile of the queries may hold two documents)
   int first, step;                          // every step-th tile from the first on: so the parts of split sums see equally much of any mask
   int at, end;                              // those of the present ballot: at .. at + 63; end: behind the last tile
-  uint64_t visit, mine, mask, none;
+  uint64_t visit, mine, documents, order, none;
 
-  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int group_rows, int wave_row, int wave_rows, int first_, int step_, int end_) {
+  // word: of the lane's row
+  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int wave_row, uint32_t word, int first_, int step_, int end_) {
     tiles = c.k_words ? c.k_tiles + (int64_t)b * c.tiles : nullptr;
     const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
-    const int gf = token(group_row), gt = token(group_row + group_rows - 1), wf = token(wave_row), wt = token(wave_row + wave_rows - 1);
+    const int gf = token(group_row), gt = token(group_row + ROWS - 1), wf = token(wave_row), wt = token(wave_row + 31);
     group_from = gf + c.offset; group_to = gt + c.offset;
     wave_from = wf + c.offset; wave_to = wt + c.offset;
     if (tiles) {
-      const AttnTile *q = c.q_tiles + (int64_t)b * c.q_tile_count;
-      group_docs = range_of(q, gf, gt);
-      wave_docs = range_of(q, wf, wt);
+      group_docs = range_of<ROWS / 64 + 1>(c.q_tiles + (int64_t)b * c.q_tile_count, gf, gt);
+      wave_docs = range_of(word);
     }
     first = first_;
     step = step_;
@@ -319,53 +351,52 @@ struct KeyWalk {
   __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false};
+      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false, false};
       const int64_t tt = (int64_t)(at + lane) * step + first;
       const bool there = tt < end;
       const int t = there ? (int)tt : 0;
       Range k{0, 0, 0};
       if (tiles && there) { const AttnTile x = tiles[t]; k = Range{x.first, x.last, x.flags}; }
       const int k0 = t * ATTN_TILE, k1 = k0 + ATTN_TILE - 1;
-      bool some, all, wave_some, wave_all;
-      sees(c, group_from, group_to, group_docs, k0, k1, k, some, all);
-      sees(c, wave_from, wave_to, wave_docs, k0, k1, k, wave_some, wave_all);
-      visit = __ballot(there && some);
-      mine = __ballot(there && wave_some);
-      mask = __ballot(there && !(wave_all && k1 < c.keys));
+      const Sight group = sees(c, group_from, group_to, group_docs, k0, k1, k), wave = sees(c, wave_from, wave_to, wave_docs, k0, k1, k);
+      visit = __ballot(there && group.some);
+      mine = __ballot(there && wave.some);
+      documents = __ballot(there && tiles && !(wave.documents && k1 < c.keys));         // places behind the last key are of no document
+      order = __ballot(there && !(wave.order && (tiles || k1 < c.keys)));
       none = __ballot(there && tiles && (k.flags & ATTN_SOME_NONE));
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((mask >> i) & 1), (bool)((none >> i) & 1)};
+    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((documents >> i) & 1), (bool)((order >> i) & 1), (bool)((none >> i) & 1)};
   }
 };
 
-// Of the keys k0 + row_of(r), whose words are at `words`: tells set(r, .) whether the query at `pos` of the document `word` sees it
+// Of the keys k0 + row_of(r), whose words are at `words`: tells set(r, .) whether the query at `pos` of the document `word` sees it:
+// as far as documents go and as far as their order goes, what `now` asks for (the wavefront's other tiles need neither)
 template <class Words, class F>
-__device__ __forceinline__ void seen_keys(const AttnCall &c, Words words, int k0, int pos, uint32_t word, F set) {
-  const int rel = c.k_words ? (c.causal ? pos - k0 : 64) : (c.causal && pos < c.keys - 1 ? pos : c.keys - 1) - k0;
-  if (!c.k_words) {
+__device__ __forceinline__ void seen_keys(const AttnCall &c, const Visit &now, Words words, int k0, int pos, uint32_t word, F set) {
+  const int rel = (c.causal && (c.k_words || pos < c.keys - 1) ? pos : c.keys - 1) - k0;
+  if (now.documents) {
 #pragma unroll
-    for (int r = 0; r < 16; ++r) set(r, row_of(r) <= rel);
-    return;
+    for (int g = 0; g < 4; ++g)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) set(g * 4 + e, (words[g * 8 + e] & ~1u) == word);
   }
-#pragma unroll
-  for (int g = 0; g < 4; ++g) {
-    u4 w;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) w[e] = words[g * 8 + e];
+  if (now.order) {
     if (c.prefix) {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) set(g * 4 + e, (w[e] == (word | 1u)) | ((w[e] == word) & (g * 8 + e <= rel)));
+      for (int g = 0; g < 4; ++g)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) set(g * 4 + e, (g * 8 + e <= rel) | (words[g * 8 + e] & 1u));
     } else {
 #pragma unroll
-      for (int e = 0; e < 4; ++e) set(g * 4 + e, (w[e] == word) & (g * 8 + e <= rel));
+      for (int r = 0; r < 16; ++r) set(r, row_of(r) <= rel);
     }
   }
 }
 
 // a query's document as the comparisons want it: one that equals no key's where it has none
-__device__ __forceinline__ uint32_t query_word(uint32_t word) { return word == ATTN_NONE ? ATTN_NOBODY : word & ~1u; }
+__device__ __forceinline__ uint32_t query_word(uint32_t word) { return word == ATTN_NONE ? ATTN_NOBODY : word; }
 
 // ---------------------------------------------------------------------------------------------- scores
 // The score in powers of two from the product q.k.  CAP: the tanh is 1 - 2 / (1 + exp(2 x)), off by 2^-23 of the cap, not of itself, which is what
@@ -383,7 +414,7 @@ template <class T, int D>
 struct QueryRow {
   s8 q[D / 16];
   int row, token, head, pos;
-  uint32_t word;
+  uint32_t word, raw;                       // as the comparisons want it, and as it is
   float slope2;
   __device__ __forceinline__ void start(const AttnCall &c, int b, int h, int first, int lane) {
     row = first + (lane & 31);
@@ -391,7 +422,8 @@ struct QueryRow {
     token = divide(c.by_group, r);
     head = h * c.group + r - token * c.group;
     pos = token + c.offset;
-    word = c.q_words ? query_word(c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token]) : 0;
+    raw = c.q_words ? c.q_words[(int64_t)b * c.q_tile_count * ATTN_TILE + token] & ~1u : 0;
+    word = query_word(raw);
     slope2 = c.slopes ? c.slopes[head] * 1.44269504088896341f : 0.f;
   }
   // operands straight from memory, 16 bytes a row and load: for few rows
@@ -438,22 +470,24 @@ struct Softmax {
     for (int k = 0; k < D / 16; ++k) s = T::mfma(row_fragment<D>(keys, first, k, lane), row.q[k], s);
     return s;
   }
-  // values from the products with the keys k0 + row_of(r); hidden ones are those of no weight
-  template <class Words>
-  static __device__ __forceinline__ void values_of(const AttnCall &c, const QueryRow<T, D> &row, Words words, int k0, bool masked, f16 &s) {
-    if (CAP || SLOPE) {
-      const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
+  // values from the products with the keys k0 + row_of(r)
+  static __device__ __forceinline__ void values_of(const AttnCall &c, const QueryRow<T, D> &row, int k0, f16 &s) {
+    if (!CAP && !SLOPE) return;
+    const float rel = SLOPE ? (float)(row.pos - k0) : 0.f;
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (LEAST) {
-          s[r] = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * c.tanh2));
-        } else {
-          float share;
-          s[r] = biased(capped<CAP>(c, s[r], share), row.slope2, rel, r);
-        }
+    for (int r = 0; r < 16; ++r) {
+      if (LEAST) {
+        s[r] = __builtin_amdgcn_rcpf(1.f + exp2_(s[r] * c.tanh2));
+      } else {
+        float share;
+        s[r] = biased(capped<CAP>(c, s[r], share), row.slope2, rel, r);
       }
     }
-    if (masked) seen_keys(c, words, k0, row.pos, row.word, [&](int r, bool see) { s[r] = see ? s[r] : LEAST ? INFINITY : -INFINITY; });
+  }
+  // those of hidden keys become the value of no weight
+  template <class Words>
+  static __device__ __forceinline__ void hide(const AttnCall &c, const QueryRow<T, D> &row, const Visit &now, Words words, int k0, f16 &s) {
+    seen_keys(c, now, words, k0, row.pos, row.word, [&](int r, bool see) { s[r] = see ? s[r] : LEAST ? INFINITY : -INFINITY; });
   }
   static __device__ __forceinline__ float most_of(const f16 &s) {
     float m = s[0];
@@ -488,30 +522,57 @@ struct Softmax {
   }
 };
 
-// A wavefront's 32 x D results (rows in lanes) turned round in shared memory, half of 64 elements at a time, so that they leave as rows: 8 elements a lane
-enum { TURN_PITCH = 68, TURN_BYTES = 32 * TURN_PITCH * 4 };
-template <int D, class F>
-__device__ __forceinline__ void by_rows(lds_char *own, const f16 (&v)[D / 32], int lane, F f) {
+// A wavefront's results, 32 rows (in lanes) of N blocks of 32 columns (the first: d0), turned round in shared memory, two blocks at a time, so that they
+// leave as rows: 8 elements a lane
+constexpr int turn_bytes(int blocks) { return 32 * (blocks >= 2 ? 68 : 36) * 4; }
+template <int N, class F>
+__device__ __forceinline__ void by_rows(lds_char *own, const f16 (&v)[N], int d0, int lane, F f) {
+  constexpr int B = N >= 2 ? 2 : 1, PITCH = B * 32 + 4, EACH = B * 4;       // EACH: lanes a row
   const int h4 = (lane >> 5) * 4;
 #pragma unroll
-  for (int half = 0; half < D / 64; ++half) {
+  for (int at = 0; at < N; at += B) {
 #pragma unroll
-    for (int d = 0; d < 2; ++d)
+    for (int d = 0; d < B; ++d)
 #pragma unroll
       for (int g = 0; g < 4; ++g)
-        *(__attribute__((address_space(3))) f4 *)(own + ((lane & 31) * TURN_PITCH + d * 32 + g * 8 + h4) * 4) =
-            f4{v[half * 2 + d][g * 4], v[half * 2 + d][g * 4 + 1], v[half * 2 + d][g * 4 + 2], v[half * 2 + d][g * 4 + 3]};
+        *(__attribute__((address_space(3))) f4 *)(own + ((lane & 31) * PITCH + d * 32 + g * 8 + h4) * 4) =
+            f4{v[at + d][g * 4], v[at + d][g * 4 + 1], v[at + d][g * 4 + 2], v[at + d][g * 4 + 3]};
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int row = i * 8 + (lane >> 3), d = (lane & 7) * 8;
-      const __attribute__((address_space(3))) f4 *p = (const __attribute__((address_space(3))) f4 *)(own + (row * TURN_PITCH + d) * 4);
-      f(row, half * 64 + d, p[0], p[1]);
+    for (int i = 0; i < EACH / 2; ++i) {
+      const int row = i * (64 / EACH) + lane / EACH, d = lane % EACH * 8;
+      const __attribute__((address_space(3))) f4 *p = (const __attribute__((address_space(3))) f4 *)(own + (row * PITCH + d) * 4);
+      f(row, d0 + at * 32 + d, p[0], p[1]);
     }
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+// Two wavefronts have parts of the same sums of N * 2 blocks.  Each keeps half of them (the second wavefront the second half) and gives the other half
+// to the other by shared memory: `give` before a barrier, `take` behind it
+template <int N>
+__device__ __forceinline__ void give(lds_char *at, const f16 (&v)[2 * N], f16 (&mine)[N], bool second, int lane) {
+#pragma unroll
+  for (int d = 0; d < N; ++d) {
+    const f16 other = second ? v[d] : v[N + d];
+    mine[d] = second ? v[N + d] : v[d];
+#pragma unroll
+    for (int g = 0; g < 4; ++g)
+      *(__attribute__((address_space(3))) f4 *)(at + ((d * 4 + g) * 64 + lane) * 16) = f4{other[g * 4], other[g * 4 + 1], other[g * 4 + 2], other[g * 4 + 3]};
+  }
+}
+template <int N>
+__device__ __forceinline__ void take(const lds_char *at, f16 (&mine)[N], float f, float f_other, int lane) {
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+      const f4 v = *(const __attribute__((address_space(3))) f4 *)(at + ((d * 4 + g) * 64 + lane) * 16);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) mine[d][g * 4 + e] = fmaf(mine[d][g * 4 + e], f, v[e] * f_other);
+    }
 }
 // 8 elements of a row of the results
 template <class T>
@@ -541,32 +602,35 @@ __device__ __forceinline__ void store8_low(uint16_t *p, int d, int width, f4 a, 
 }
 
 // ---------------------------------------------------------------------------------------------- forward
-// 128 rows, 32 a wavefront; two wavefronts a SIMD (three with rows of 64), of different workgroups, so that one's products run beside another's
-// exponentials.
-template <class T, int D, int CAP, int SLOPE>
+// 32 rows a wavefront; two wavefronts a SIMD (three with rows of 64), of different workgroups, so that one's products run beside another's
+// exponentials.  PARTS = 1: a workgroup has 128 rows.  2: it has 64, each wavefront half of the keys of a tile; the sums meet at the end.  Every tile is read
+// for half as many rows then, but a workgroup takes half as long, and the longest one is what a small call waits for.
+template <class T, int D, int CAP, int SLOPE, int PARTS>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_forward(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4;
+  constexpr int WAVES = 4, BLOCKS = WAVES / PARTS, N = D / 32 / PARTS;      // blocks of rows; blocks of columns that a wavefront stores
   typedef TileFeed<D, WAVES> Feed;
   typedef Softmax<T, D, CAP, SLOPE> Soft;
-  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > WAVES * TURN_BYTES ? Feed::BYTES : WAVES * TURN_BYTES];
+  constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 4096 : 0;
+  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > TURN + MEET ? Feed::BYTES : TURN + MEET];
+  __shared__ float tops[WAVES][32], sums[WAVES][32];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place p = place_of(c, c.row_tiles, true);
-  const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
-  Feed feed;
-  feed.start(c, p, wave, lane);
-  KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, p.split, c.splits, c.tiles);
-  Visit next = walk.next(c, lane);
-  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS;
+  const Place p = place_of(c, true);
+  const int row0 = p.tile * (BLOCKS * 32), wave_row = row0 + wave % BLOCKS * 32, h4 = (lane >> 5) * 4;
   // the queries come by the second slot, a wavefront's to its own part
   const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
   static_assert(WAVES * Shape<D>::bytes(32) <= Feed::SLOT, "a slot holds the rows");
   bring_rows<D>(c, c.q, p, wave_row, lds0 + mine, lane);
+  Feed feed;
+  feed.start(c, p, wave, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
+  KeyWalk<BLOCKS * 32> walk;
+  walk.start(c, p.b, row0, wave_row, row.raw, p.split, c.splits, c.tiles);
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
   Soft soft;
   soft.start();
   waited<0>();
@@ -586,26 +650,57 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     slot ^= 1;
     if (next.tile >= 0) feed.load(next.tile, lds0 + slot * Feed::SLOT, wave, lane);
     if (!now.run) continue;
-    const int k0 = now.tile * ATTN_TILE + h4;
-    lds_word *words = (lds_word *)(here + Feed::WORDS) + h4;
-    f16 s = Soft::products(row, here, 0, lane), t = Soft::products(row, here, 32, lane);
-    Soft::values_of(c, row, words, k0, now.masked, s);
-    Soft::values_of(c, row, words + 32, k0 + 32, now.masked, t);
-    soft.follow(c, Soft::more(Soft::most_of(s), Soft::most_of(t)));
-    soft.add(c, s, values, 0, lane);
-    soft.add(c, t, values, 32, lane);
+    const int first = PARTS == 2 ? part * 32 : 0, k0 = now.tile * ATTN_TILE + first + h4;
+    lds_word *words = (lds_word *)(here + Feed::WORDS) + first + h4;
+    f16 s = Soft::products(row, here, first, lane);
+    if (PARTS == 2) {
+      Soft::values_of(c, row, k0, s);
+      if (now.masked()) Soft::hide(c, row, now, words, k0, s);
+      soft.follow(c, Soft::most_of(s));
+      soft.add(c, s, values, first, lane);
+    } else {
+      f16 t = Soft::products(row, here, 32, lane);
+      Soft::values_of(c, row, k0, s);
+      Soft::values_of(c, row, k0 + 32, t);
+      if (now.masked()) {
+        Soft::hide(c, row, now, words, k0, s);
+        Soft::hide(c, row, now, words + 32, k0 + 32, t);
+      }
+      soft.follow(c, Soft::more(Soft::most_of(s), Soft::most_of(t)));
+      soft.add(c, s, values, 0, lane);
+      soft.add(c, t, values, 32, lane);
+    }
   }
 
-  lds_char *own = lds + wave * TURN_BYTES;
   arrived();
-  const float sum = both_sum(soft.sum);
+  float sum = both_sum(soft.sum), top = soft.top;
+  f16 o[N];
+  if constexpr (PARTS == 2) {
+    const int other = wave ^ BLOCKS;
+    if (lane < 32) {
+      tops[wave][lane] = top;
+      sums[wave][lane] = sum;
+    }
+    give<N>(lds + TURN + wave * (N * 4096), soft.o, o, part == 1, lane);
+    __syncthreads();
+    const float far = tops[other][lane & 31];
+    top = fmaxf(top, far);
+    const float f = exp2_(soft.top - top), g = exp2_(far - top);
+    sum = fmaf(sum, f, sums[other][lane & 31] * g);
+    take<N>(lds + TURN + other * (N * 4096), o, f, g, lane);
+  } else {
+#pragma unroll
+    for (int d = 0; d < N; ++d) o[d] = soft.o[d];
+  }
+  lds_char *own = lds + wave * turn_bytes(N);
+  const int d0 = part * (N * 32);
   if (c.splits > 1) {
     const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.rows + wave_row;
-    if (lane < 32 && row.row < c.rows) {
-      c.part2[(at + lane) * 2] = soft.top;
+    if (part == 0 && lane < 32 && row.row < c.rows) {
+      c.part2[(at + lane) * 2] = top;
       c.part2[(at + lane) * 2 + 1] = sum;
     }
-    by_rows<D>(own, soft.o, lane, [&](int i, int d, f4 a, f4 b) {
+    by_rows(own, o, d0, lane, [&](int i, int d, f4 a, f4 b) {
       if (wave_row + i >= c.rows) return;
       float *out = c.part + (at + i) * c.width4 + d;
       if (d < c.width4) *(f4 *)out = a;
@@ -614,10 +709,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     return;
   }
   const float f = sum == 0.f ? 0.f : 1.f / sum;
-  if (c.lse && lane < 32 && row.row < c.rows) c.lse[(int64_t)p.hb * c.rows_pad + row.row] = sum == 0.f ? INFINITY : soft.top + __builtin_amdgcn_logf(sum);
+  if (c.lse && part == 0 && lane < 32 && row.row < c.rows) c.lse[(int64_t)p.hb * c.rows_pad + row.row] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d) soft.o[d] *= f;
-  by_rows<D>(own, soft.o, lane, [&](int i, int d, f4 a, f4 b) {
+  for (int d = 0; d < N; ++d) o[d] *= f;
+  by_rows(own, o, d0, lane, [&](int i, int d, f4 a, f4 b) {
     const int r = wave_row + i, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
     if (r >= c.rows) return;
     store8<T>(c.y.p + p.b * c.y.batch + token * c.y.token + head * c.y.head, d, c.width, a, b);
@@ -640,7 +735,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   lds_char *own = lds + wave * OWN;
   const uint32_t own0 = (uint32_t)(uintptr_t)own;
-  const Place p = place_of(c, 1, false);
+  const Place p = place_of(c, false);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, 0, lane);
   row.operands(c, p.b, lane);
@@ -648,8 +743,8 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   kf.start(c.k, p.b, p.h, c.keys, c.dim, 0, lane);
   vf.start(c.v, p.b, p.h, c.keys, c.dim, 0, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
-  KeyWalk walk;
-  walk.start(c, p.b, 0, 32, 0, 32, p.split * WAVES + wave, c.splits * WAVES, c.tiles);
+  KeyWalk<32> walk;
+  walk.start(c, p.b, 0, 0, row.raw, p.split * WAVES + wave, c.splits * WAVES, c.tiles);
   typedef Softmax<T, D, CAP, SLOPE> Soft;
   Soft soft;
   soft.start();
@@ -683,7 +778,8 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
       waited<0>();
     }
     f16 s = Soft::products(row, here, 0, lane);
-    Soft::values_of(c, row, words + (now.masked ? k0 + (lane >> 5) * 4 : 0), k0 + (lane >> 5) * 4, now.masked, s);
+    Soft::values_of(c, row, k0 + (lane >> 5) * 4, s);
+    if (now.masked()) Soft::hide(c, row, now, words + (words ? k0 + (lane >> 5) * 4 : 0), k0 + (lane >> 5) * 4, s);
     soft.follow(c, Soft::most_of(s));
     soft.add(c, s, here + Feed::BYTES, 0, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: the next loads go there
@@ -757,70 +853,88 @@ __device__ __forceinline__ void gradient(const AttnCall &c, float product, float
 // delta = dy.y of a wavefront's 32 rows, whose dy lie at `dys`, to `out`.  y is taken with what its rounding took from it: where few keys share a row, dy.v and
 // delta are near each other, and 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3
 // without, 2.4e-3 with).  A row by as many lanes as it has chunks.
-template <class T, int D>
-__device__ __forceinline__ void deltas_of(const AttnCall &c, const Place &p, int first, const lds_char *dys, float *out, int lane) {
+template <class T, int D, int ROWS>
+__device__ __forceinline__ void deltas_of(const AttnCall &c, const Place &p, int first, const lds_char *dys, int first_there, float *out, int lane) {
   typedef Shape<D> S;
   typedef s8 s8_anywhere __attribute__((aligned(2)));
-  constexpr int EACH = S::CHUNKS, ROWS = 64 / EACH;
+  constexpr int EACH = S::CHUNKS, AT_ONCE = 64 / EACH, N = ROWS / AT_ONCE;
+  const int chunk = lane % EACH, d = chunk * 8;
+  s8 y[N], low[N];                          // all are asked for before the first is used
 #pragma unroll
-  for (int i = 0; i < 32 / ROWS; ++i) {
-    const int row = i * ROWS + lane / EACH, chunk = lane % EACH, d = chunk * 8;
-    const int r = first + row < c.rows ? first + row : c.rows - 1, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
-    const uint16_t *y = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
-    const uint16_t *low = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
-    const s8 dy = *(const __attribute__((address_space(3))) s8 *)(dys + S::row_at(row) + ((uint32_t)chunk ^ S::swizzle(row)) * 16);
-    float sum = 0.f;
-    if (d + 8 <= c.width) {
-      const s8 a = *(const s8_anywhere *)(y + d), b = *(const s8_anywhere *)(low + d);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[e]), T::up((uint16_t)a[e]) + T::up((uint16_t)b[e]), sum);
+  for (int i = 0; i < N; ++i) {
+    const int row = first + i * AT_ONCE + lane / EACH, r = row < c.rows ? row : c.rows - 1, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
+    const uint16_t *a = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
+    const uint16_t *b = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
+    if (c.width % 8 == 0) {                 // chunks behind the last: left out of the sum
+      const int at = d < c.width ? d : 0;
+      y[i] = *(const s8_anywhere *)(a + at);
+      low[i] = *(const s8_anywhere *)(b + at);
     } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e)
-        if (d + e < c.width) sum = fmaf(T::up((uint16_t)dy[e]), T::up(y[d + e]) + T::up(low[d + e]), sum);
+      for (int e = 0; e < 8; ++e) {
+        const bool in = d + e < c.width;
+        y[i][e] = in ? (short)a[d + e] : (short)0;
+        low[i][e] = in ? (short)b[d + e] : (short)0;
+      }
     }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int row = first_there + i * AT_ONCE + lane / EACH;
+    const s8 dy = *(const __attribute__((address_space(3))) s8 *)(dys + S::row_at(row) + ((uint32_t)chunk ^ S::swizzle(row)) * 16);
+    float sum = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[e]), T::up((uint16_t)y[i][e]) + T::up((uint16_t)low[i][e]), sum);
+    if (d >= c.width) sum = 0.f;
 #pragma unroll
     for (int x = EACH / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-    if (chunk == 0) out[row] = sum;
+    if (chunk == 0) out[i * AT_ONCE + lane / EACH] = sum;
   }
 }
 
-template <class T, int D, int CAP, int SLOPE>
+// PARTS as in k_forward
+template <class T, int D, int CAP, int SLOPE, int PARTS>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_dq(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4;
+  constexpr int WAVES = 4, BLOCKS = WAVES / PARTS, N = D / 32 / PARTS;
   typedef TileFeed<D, WAVES> Feed;
-  __shared__ float deltas[WAVES][32];
-  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > WAVES * TURN_BYTES ? Feed::BYTES : WAVES * TURN_BYTES];
+  constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 4096 : 0;
+  __shared__ float deltas[BLOCKS][32];
+  __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > TURN + MEET ? Feed::BYTES : TURN + MEET];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place p = place_of(c, c.row_tiles, true);
-  const int row0 = p.tile * (WAVES * 32), wave_row = row0 + wave * 32, h4 = (lane >> 5) * 4;
-  Feed feed;
-  feed.start(c, p, wave, lane);
-  KeyWalk walk;
-  walk.start(c, p.b, row0, WAVES * 32, wave_row, 32, 0, 1, c.tiles);
-  Visit next = walk.next(c, lane);
-  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
+  const Place p = place_of(c, true);
+  const int row0 = p.tile * (BLOCKS * 32), wave_row = row0 + block * 32, h4 = (lane >> 5) * 4;
   // dy comes by the second slot, a wavefront's rows to its own part
   const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
   static_assert(WAVES * Shape<D>::bytes(32) <= Feed::SLOT, "a slot holds the rows");
   bring_rows<D>(c, c.dy, p, wave_row, lds0 + mine, lane);
+  Feed feed;
+  feed.start(c, p, wave, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
+  KeyWalk<BLOCKS * 32> walk;
+  walk.start(c, p.b, row0, wave_row, row.raw, 0, 1, c.tiles);
   row.operands(c, p.b, lane);
   const bool there = row.row < c.rows;
   const float lse = c.lse[(int64_t)p.hb * c.rows_pad + (there ? row.row : c.rows - 1)];
+  Visit next = walk.next(c, lane);
+  if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
   waited<0>();
   s8 dy[D / 16];
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) dy[k] = row_fragment<D>(lds + mine, 0, k, lane);
-  deltas_of<T, D>(c, p, wave_row, lds + mine, deltas[wave], lane);
-  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  const float less = CAP ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[wave][lane & 31] : deltas[wave][lane & 31];
-  if (lane < 32 && row.row < c.rows_pad) {
+  constexpr int SHARE = 32 / PARTS;         // rows whose delta a wavefront works out
+  deltas_of<T, D, SHARE>(c, p, wave_row + part * SHARE, lds + mine, part * SHARE, &deltas[block][part * SHARE], lane);
+  if (PARTS == 2) {
+    __syncthreads();
+  } else {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+  const float less = CAP ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[block][lane & 31] : deltas[block][lane & 31];
+  if (part == 0 && lane < 32 && row.row < c.rows_pad) {
     AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
     block.less[lane] = there ? less : INFINITY;
     block.delta[lane] = delta;
@@ -828,6 +942,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     block.word[lane] = there ? row.word : ATTN_NOBODY;
     block.slope2[lane] = row.slope2;
     block.pos[lane] = row.pos;
+    if (c.k_words && lane == 0) block.documents = AttnTile{walk.wave_docs.first, walk.wave_docs.last, walk.wave_docs.flags, 0};
   }
   f16 dq[D / 32];
 #pragma unroll
@@ -848,8 +963,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     if (next.tile >= 0) feed.load(next.tile, lds0 + slot * Feed::SLOT, wave, lane);
     if (!now.run) continue;
 #pragma unroll
-    for (int b = 0; b < 2; ++b) {
-      const int k0 = now.tile * ATTN_TILE + b * 32 + h4;
+    for (int half = 0; half < 2 / PARTS; ++half) {
+      const int b = PARTS == 2 ? part : half, k0 = now.tile * ATTN_TILE + b * 32 + h4;
       f16 s = {}, dp = {};
 #pragma unroll
       for (int k = 0; k < D / 16; ++k) {
@@ -863,7 +978,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
         gradient<CAP>(c, s[r], dp[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), less) : less, delta, weight, ds);
         dp[r] = ds;
       }
-      if (now.masked) seen_keys(c, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
+      if (now.masked()) seen_keys(c, now, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
       for (int k = 0; k < 2; ++k)
@@ -872,33 +987,42 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     }
   }
   arrived();
+  f16 sum[N];
+  if constexpr (PARTS == 2) {
+    give<N>(lds + TURN + wave * (N * 4096), dq, sum, part == 1, lane);
+    __syncthreads();
+    take<N>(lds + TURN + (wave ^ BLOCKS) * (N * 4096), sum, c.scale, c.scale, lane);
+  } else {
 #pragma unroll
-  for (int d = 0; d < D / 32; ++d) dq[d] *= c.scale;
-  by_rows<D>(lds + wave * TURN_BYTES, dq, lane, [&](int i, int d, f4 a, f4 b) {
+    for (int d = 0; d < N; ++d) sum[d] = dq[d] * c.scale;
+  }
+  by_rows(lds + wave * turn_bytes(N), sum, part * (N * 32), lane, [&](int i, int d, f4 a, f4 b) {
     const int r = wave_row + i, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
     if (r < c.rows) store8<T>(c.dq.p + p.b * c.dq.batch + token * c.dq.token + head * c.dq.head, d, c.width, a, b);
   });
 #endif
 }
 
-// Blocks of 32 rows that see some of a workgroup's keys, as KeyWalk
+// Blocks of ROWS rows (32 of a wavefront's own: those from `own` on) that see some of a workgroup's KEYS keys, as KeyWalk
+template <int KEYS, int ROWS>
 struct RowWalk {
   int group_from, group_to, wave_from, wave_to;           // keys
   Range group_docs, wave_docs;
-  const AttnTile *tiles;                    // of the queries' tokens
-  int first, step, at, end;
-  uint64_t visit, mine, mask, none;
-  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_key, int group_keys, int wave_key, int wave_keys, int first_, int step_, int end_) {
+  const AttnRows *rows;                     // what the rows' documents are, or null
+  int own, first, step, at, end;
+  uint64_t visit, mine, documents, order, none;
+  // word: of the lane's key
+  __device__ __forceinline__ void start(const AttnCall &c, const Place &p, int group_key, int wave_key, uint32_t word, int own_, int first_, int step_, int end_) {
+    own = own_;
     group_from = group_key;
-    group_to = group_key + group_keys - 1 < c.keys ? group_key + group_keys - 1 : c.keys - 1;
+    group_to = group_key + KEYS - 1 < c.keys ? group_key + KEYS - 1 : c.keys - 1;
     wave_from = wave_key < c.keys ? wave_key : c.keys - 1;
-    wave_to = wave_key + wave_keys - 1 < c.keys ? wave_key + wave_keys - 1 : c.keys - 1;
-    tiles = nullptr;
+    wave_to = wave_key + 31 < c.keys ? wave_key + 31 : c.keys - 1;
+    rows = nullptr;
     if (c.k_words) {
-      tiles = c.q_tiles + (int64_t)b * c.q_tile_count;
-      const AttnTile *k = c.k_tiles + (int64_t)b * c.tiles;
-      group_docs = keys_of(k, group_from, group_to);
-      wave_docs = keys_of(k, wave_from, wave_to);
+      rows = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
+      group_docs = keys_of<KEYS / 64>(c.k_tiles + (int64_t)p.b * c.tiles, group_from, group_to);
+      wave_docs = range_of(word);
     }
     first = first_;
     step = step_;
@@ -906,66 +1030,86 @@ struct RowWalk {
     end = end_;
     visit = 0;
   }
+  template <int N>
   static __device__ __forceinline__ Range keys_of(const AttnTile *tiles, int from, int to) {
+    AttnTile x[N];
+#pragma unroll
+    for (int i = 0; i < N; ++i) x[i] = tiles[from / ATTN_TILE + i < to / ATTN_TILE ? from / ATTN_TILE + i : to / ATTN_TILE];
     Range r{INT32_MAX, -1, ATTN_ALL_PREFIX};
-    for (int t = from / ATTN_TILE; t <= to / ATTN_TILE; ++t) {
-      const AttnTile x = tiles[t];
-      const int all = r.flags & x.flags & ATTN_ALL_PREFIX;
-      r = join(r, x);
-      r.flags = (r.flags & ~ATTN_ALL_PREFIX) | all | (x.flags & ATTN_SOME_PREFIX);
+#pragma unroll
+    for (int i = 0; i < N; ++i) {
+      const int all = r.flags & x[i].flags & ATTN_ALL_PREFIX;
+      r = join(r, x[i]);
+      r.flags = (r.flags & ~ATTN_ALL_PREFIX) | all | (x[i].flags & ATTN_SOME_PREFIX);
     }
     return r;
   }
   __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
       at += 64;
-      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false};
+      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false, false};
       const int64_t tt = (int64_t)(at + lane) * step + first;
       const bool there = tt < end;
-      const int r0 = there ? (int)tt * 32 : 0, r1 = r0 + 31 < c.rows ? r0 + 31 : c.rows - 1;
-      const int t0 = divide(c.by_group, r0), t1 = divide(c.by_group, r1);
-      Range q{0, 0, 0};
-      if (tiles) q = range_of(tiles, t0, t1);
-      const int from = t0 + c.offset, to = t1 + c.offset;
-      bool some, all, wave_some, wave_all;
-      sees(c, from, to, q, group_from, group_to, group_docs, some, all);
-      sees(c, from, to, q, wave_from, wave_to, wave_docs, wave_some, wave_all);
-      visit = __ballot(there && some);
-      mine = __ballot(there && wave_some);
-      mask = __ballot(there && !(wave_all && r0 + 32 <= c.rows));
-      none = __ballot(there && tiles && (q.flags & ATTN_SOME_NONE));
+      const int r0 = there ? (int)tt * ROWS : 0;
+      const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
+      const int t0 = token(r0), t1 = token(r0 + ROWS - 1);
+      Range q{0, 0, 0}, mine_q{0, 0, 0};
+      if (rows) {
+        const int at_rows = r0 / 32;
+        AttnTile x[ROWS / 32];
+#pragma unroll
+        for (int j = 0; j < ROWS / 32; ++j) x[j] = rows[at_rows + j].documents;
+        q = join(Range{INT32_MAX, -1, 0}, x[0]);
+        if (ROWS == 64) {
+          mine_q = join(Range{INT32_MAX, -1, 0}, own ? x[ROWS / 32 - 1] : x[0]);
+          q = join(q, x[ROWS / 32 - 1]);
+        } else {
+          mine_q = q;
+        }
+      }
+      const Sight group = sees(c, t0 + c.offset, t1 + c.offset, q, group_from, group_to, group_docs);
+      const Sight wave = sees(c, (ROWS == 32 ? t0 : token(r0 + own)) + c.offset, (ROWS == 32 ? t1 : token(r0 + own + 31)) + c.offset, mine_q, wave_from, wave_to, wave_docs);
+      visit = __ballot(there && group.some);
+      mine = __ballot(there && wave.some && r0 + own < c.rows);
+      documents = __ballot(there && rows && !wave.documents);
+      order = __ballot(there && !(wave.order && r0 + own + 32 <= c.rows));
+      none = __ballot(there && rows && (q.flags & ATTN_SOME_NONE));
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
-    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((mask >> i) & 1), (bool)((none >> i) & 1)};
+    return Visit{(at + i) * step + first, (bool)((mine >> i) & 1), (bool)((documents >> i) & 1), (bool)((order >> i) & 1), (bool)((none >> i) & 1)};
   }
 };
 
 // A wavefront has 32 keys: their operands, and 2 x 32 x D sums, which with the scores fill half of a lane's registers (two wavefronts a SIMD) if the
 // values stay in shared memory: they are read from there a block of 32 rows, as the queries and dy are.
-template <class T, int D, int CAP, int SLOPE>
-__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k_dkdv(const AttnCall c) {
+//
+// PARTS = 2: a workgroup has 64 keys and goes through 64 rows at a time, each wavefront through half of them.  Rows of 128 elements have no room for that.
+template <class T, int D, int CAP, int SLOPE, int PARTS>
+__global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 && PARTS == 2 ? 3 : 2))) k_dkdv(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
-  constexpr int WAVES = 4, NT = 64 * WAVES, KEYS = WAVES * 32;
-  typedef RowFeed<D, 32, WAVES> Feed;
+  constexpr int WAVES = 4, NT = 64 * WAVES, BLOCKS = WAVES / PARTS, KEYS = BLOCKS * 32, STEP = PARTS * 32, N = D / 32 / PARTS;
+  typedef RowFeed<D, STEP, WAVES> Feed;
   typedef KeyFeed<D, KEYS, WAVES> Values;
   typedef __attribute__((address_space(3))) const AttnRows lds_rows;
   typedef __attribute__((address_space(3))) const f4 lds_f4;
-  enum { ROWS = 2 * Feed::BYTES, STAGE = ROWS + (int)sizeof(AttnRows), VALUES = 2 * STAGE, BYTES = VALUES + Values::BYTES };
+  enum { ROWS = 2 * Feed::BYTES, STAGE = ROWS + PARTS * (int)sizeof(AttnRows), VALUES = 2 * STAGE, BYTES = VALUES + Values::BYTES };
   static_assert(sizeof(AttnRows) <= 1024, "a wavefront brings it in one load");
-  __shared__ __attribute__((aligned(1024))) char shared[BYTES > WAVES * TURN_BYTES ? BYTES : WAVES * TURN_BYTES];
+  constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 8192 : 0;
+  __shared__ __attribute__((aligned(1024))) char shared[(int)BYTES > TURN + MEET ? (int)BYTES : TURN + MEET];
+  __shared__ uint32_t words[WAVES][32];
   lds_char *lds = (lds_char *)shared, *values = lds + VALUES;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
-  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const Place p = place_of(c, c.key_tiles, false);
-  const int key0 = p.tile * KEYS, wave_key = key0 + wave * 32;
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
+  const Place p = place_of(c, false);
+  const int key0 = p.tile * KEYS, wave_key = key0 + block * 32;
   const int h4 = (lane >> 5) * 4;
-  // this lane's key
-  const int key = wave_key + (lane & 31), there = key < c.keys ? key : c.keys - 1;
-  const uint32_t word = c.k_words ? c.k_words[(int64_t)p.b * c.tiles * ATTN_TILE + there] : 0;
   s8 k[D / 16];
+  uint32_t word = 0;
   {
+    const int there = wave_key + (lane & 31) < c.keys ? wave_key + (lane & 31) : c.keys - 1;
     const uint16_t *kp = c.k.p + p.b * c.k.batch + there * c.k.token + p.h * c.k.head;
+    if (c.k_words) word = c.k_words[(int64_t)p.b * c.tiles * ATTN_TILE + there];
 #pragma unroll
     for (int i = 0; i < D / 16; ++i) {
       const int d = i * 16 + (lane >> 5) * 8;
@@ -984,23 +1128,25 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
   const AttnRows *row_data = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
 
   // without a prefix a causal mask leaves the rows from the first key's position on
-  const int blocks = (c.rows + 31) / 32;
+  const int blocks = (c.rows + STEP - 1) / STEP;
   int first = 0;
   if (c.causal && !c.prefix && key0 > c.offset) {
-    const int64_t f = (int64_t)(key0 - c.offset) * c.group / 32;
+    const int64_t f = (int64_t)(key0 - c.offset) * c.group / STEP;
     first = f < blocks ? (int)f : blocks;
   }
-  RowWalk walk;
-  walk.start(c, p.b, key0, KEYS, wave_key, 32, first + p.split, c.splits, blocks);
+  RowWalk<KEYS, STEP> walk;
+  walk.start(c, p, key0, wave_key, word, part * 32, first + p.split, c.splits, blocks);
+  if (lane < 32) words[wave][lane] = word;  // for this wavefront alone
   f16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f16{};
 
   const auto load = [&](int tile, int slot) {
     const uint32_t at = lds0 + slot * STAGE;
-    qf.load(c, tile * 32, at, wave, lane);
-    df.load(c, tile * 32, at + Feed::BYTES, wave, lane);
-    if (wave == 0 && lane < (int)sizeof(AttnRows) / 16) load_lds16(descriptor(row_data + tile, sizeof(AttnRows)), lane * 16, at + ROWS);
+    qf.load(c, tile * STEP, at, wave, lane);
+    df.load(c, tile * STEP, at + Feed::BYTES, wave, lane);
+    if (wave < PARTS && lane < (int)sizeof(AttnRows) / 16)
+      load_lds16(descriptor(row_data + tile * PARTS + wave, sizeof(AttnRows)), lane * 16, at + ROWS + wave * (int)sizeof(AttnRows));
   };
   int slot = 0;
   Visit next = walk.next(c, lane);
@@ -1010,10 +1156,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
     next = walk.next(c, lane);
     arrived();
     lds_char *queries = lds + slot * STAGE, *dys = queries + Feed::BYTES;
-    lds_rows *known = (lds_rows *)(queries + ROWS);
+    lds_rows *known = (lds_rows *)(queries + ROWS) + part;
     if (now.some_none) {
-      for (int idx = tid; idx < 32 * Shape<D>::CHUNKS; idx += NT) {
-        const int i = idx / Shape<D>::CHUNKS, r = now.tile * 32 + i;
+      for (int idx = tid; idx < STEP * Shape<D>::CHUNKS; idx += NT) {
+        const int i = idx / Shape<D>::CHUNKS, r = now.tile * STEP + i;
         if (r < c.rows && q_words[divide(c.by_group, r)] == ATTN_NONE) {
           clear_row<D>(queries, i, idx % Shape<D>::CHUNKS);
           clear_row<D>(dys, i, idx % Shape<D>::CHUNKS);
@@ -1022,13 +1168,17 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       arrived();
     }
     slot ^= 1;
-    if (next.tile >= 0) load(next.tile, slot);
-    if (!now.run) continue;
+    if (!now.run) {
+      if (next.tile >= 0) load(next.tile, slot);
+      continue;
+    }
     f16 s = {}, dp = {};
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) s = T::mfma(row_fragment<D>(queries, 0, i, lane), k[i], s);
+    for (int i = 0; i < D / 16; ++i) s = T::mfma(row_fragment<D>(queries, part * 32, i, lane), k[i], s);
 #pragma unroll
-    for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, 0, i, lane), row_fragment<D>(values, wave * 32, i, lane), dp);
+    for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, part * 32, i, lane), row_fragment<D>(values, block * 32, i, lane), dp);
+    __builtin_amdgcn_sched_barrier(0);      // reads of shared memory that are moved up from below would take the registers of k
+    if (next.tile >= 0) load(next.tile, slot);
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       f4 less = *(lds_f4 *)&known->less[g * 8 + h4];
@@ -1036,6 +1186,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       if (SLOPE) {
         const f4 slope2 = *(lds_f4 *)&known->slope2[g * 8 + h4];
         const i4 pos = *(__attribute__((address_space(3))) const i4 *)&known->pos[g * 8 + h4];
+        const int key = wave_key + own_lane() % 32;
 #pragma unroll
         for (int e = 0; e < 4; ++e) less[e] = fmaf(slope2[e], fabsf((float)(pos[e] - key)), less[e]);
       }
@@ -1047,16 +1198,28 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
         dp[g * 4 + e] = ds;
       }
     }
-    if (now.masked) {
+    if (now.masked()) {
+      const int i = own_lane() % 32;
+      const uint32_t mine = words[wave][i], word = mine & ~1u;
+      const int key = mine & 1 ? INT32_MIN + 1 : wave_key + i;      // in the prefix: before every row
+      const auto hide = [&](int r, bool see) {
+        s[r] = see ? s[r] : 0.f;
+        dp[r] = see ? dp[r] : 0.f;
+      };
+      if (now.documents) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g) {
-        const i4 last = *(__attribute__((address_space(3))) const i4 *)&known->last[g * 8 + h4];
-        const u4 words = *(__attribute__((address_space(3))) const u4 *)&known->word[g * 8 + h4];
+        for (int g = 0; g < 4; ++g) {
+          const u4 row = *(__attribute__((address_space(3))) const u4 *)&known->word[g * 8 + h4];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const bool before = key <= last[e], see = q_words ? (word == (words[e] | 1u)) | ((word == words[e]) & before) : before;
-          s[g * 4 + e] = see ? s[g * 4 + e] : 0.f;
-          dp[g * 4 + e] = see ? dp[g * 4 + e] : 0.f;
+          for (int e = 0; e < 4; ++e) hide(g * 4 + e, word == row[e]);
+        }
+      }
+      if (now.order) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+          const i4 last = *(__attribute__((address_space(3))) const i4 *)&known->last[g * 8 + h4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) hide(g * 4 + e, key <= last[e]);
         }
       }
     }
@@ -1065,53 +1228,76 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) k
       const s8 pp = pack8<T>(s, i * 8), ds = pack8<T>(dp, i * 8);
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
-        dv[d] = T::mfma(column_fragment<D>(dys, i * 16, d, lane), pp, dv[d]);
-        dk[d] = T::mfma(column_fragment<D>(queries, i * 16, d, lane), ds, dk[d]);
+        dv[d] = T::mfma(column_fragment<D>(dys, part * 32 + i * 16, d, lane), pp, dv[d]);
+        dk[d] = T::mfma(column_fragment<D>(queries, part * 32 + i * 16, d, lane), ds, dk[d]);
       }
     }
   }
   arrived();                                // the values, where no block was visited; and nobody reads shared memory any more
-  lds_char *own = lds + wave * TURN_BYTES;
-#pragma unroll
-  for (int d = 0; d < D / 32; ++d) dk[d] *= c.scale;
-  if (c.splits > 1) {
-    const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + wave_key;
-    const auto put = [&](float *part, int row, int d, f4 a, f4 b) {
-      if (wave_key + row >= c.keys) return;
-      float *out = part + (at + row) * c.width4 + d;
-      if (d < c.width4) *(f4 *)out = a;
-      if (d + 4 < c.width4) *(f4 *)(out + 4) = b;
+  lds_char *own = lds + wave * turn_bytes(N);
+  const int d0 = part * (N * 32);
+  const auto store = [&](const f16 (&k)[N], const f16 (&v)[N]) {
+    if (c.splits > 1) {
+      const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + wave_key;
+      const auto put = [&](float *out, int row, int d, f4 a, f4 b) {
+        if (wave_key + row >= c.keys) return;
+        out += (at + row) * c.width4 + d;
+        if (d < c.width4) *(f4 *)out = a;
+        if (d + 4 < c.width4) *(f4 *)(out + 4) = b;
+      };
+      by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.part, row, d, a, b); });
+      by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.part2, row, d, a, b); });
+      return;
+    }
+    const auto put = [&](const AttnOutput &o, int row, int d, f4 a, f4 b) {
+      const int j = wave_key + row;
+      if (j < c.keys) store8<T>(o.p + p.b * o.batch + j * o.token + p.h * o.head, d, c.width, a, b);
     };
-    by_rows<D>(own, dk, lane, [&](int row, int d, f4 a, f4 b) { put(c.part, row, d, a, b); });
-    by_rows<D>(own, dv, lane, [&](int row, int d, f4 a, f4 b) { put(c.part2, row, d, a, b); });
-    return;
-  }
-  const auto put = [&](const AttnOutput &o, int row, int d, f4 a, f4 b) {
-    const int j = wave_key + row;
-    if (j < c.keys) store8<T>(o.p + p.b * o.batch + j * o.token + p.h * o.head, d, c.width, a, b);
+    by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.dk, row, d, a, b); });
+    by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.dv, row, d, a, b); });
   };
-  by_rows<D>(own, dk, lane, [&](int row, int d, f4 a, f4 b) { put(c.dk, row, d, a, b); });
-  by_rows<D>(own, dv, lane, [&](int row, int d, f4 a, f4 b) { put(c.dv, row, d, a, b); });
+  if constexpr (PARTS == 2) {
+    f16 sk[N], sv[N];
+    lds_char *meet = lds + TURN;
+    give<N>(meet + wave * (N * 8192), dk, sk, part == 1, lane);
+    give<N>(meet + wave * (N * 8192) + N * 4096, dv, sv, part == 1, lane);
+    __syncthreads();
+    take<N>(meet + (wave ^ BLOCKS) * (N * 8192), sk, c.scale, c.scale, lane);
+    take<N>(meet + (wave ^ BLOCKS) * (N * 8192) + N * 4096, sv, 1.f, 1.f, lane);
+    store(sk, sv);
+  } else {
+#pragma unroll
+    for (int d = 0; d < N; ++d) dk[d] *= c.scale;
+    store(dk, dv);
+  }
 #endif
 }
 
 // ---------------------------------------------------------------------------------------------- launches
 enum { FORWARD, FEW, DQ, DKDV };
-template <class T, int WHAT, int D, int CAP, int SLOPE>
+template <class T, int WHAT, int D, int CAP, int SLOPE, int PARTS>
 bool launch(const AttnCall &c, const AttnLaunch &l) {
   hipStream_t st = (hipStream_t)l.stream;
   const dim3 grid(l.groups), block(256);
-  if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, CAP, SLOPE>), grid, block, 0, st, c);
+  if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
   else if constexpr (WHAT == FEW) hipLaunchKernelGGL((k_forward_few<T, D, CAP, SLOPE>), grid, block, 0, st, c);
-  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, CAP, SLOPE>), grid, block, 0, st, c);
-  else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE>), grid, block, 0, st, c);
+  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
+  else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
   return hipGetLastError() == hipSuccess;
+}
+template <class T, int WHAT, int D, int CAP, int SLOPE>
+bool launch_parts(const AttnCall &c, const AttnLaunch &l) {
+  constexpr bool two = D == 64 ? WHAT != FEW : WHAT == FORWARD || WHAT == DQ, one = D == 128 || WHAT == DQ || WHAT == FEW;      // those that are chosen anywhere
+  if constexpr (two)
+    if (!one || l.parts == 2) return launch<T, WHAT, D, CAP, SLOPE, 2>(c, l);
+  if constexpr (one) return launch<T, WHAT, D, CAP, SLOPE, 1>(c, l);
+  return false;
 }
 template <class T, int WHAT, int D>
 bool launch_terms(const AttnCall &c, const AttnLaunch &l) {
   const bool cap = c.cap2 != 0.f, slope = c.slopes != nullptr;
-  if (cap) return slope ? launch<T, WHAT, D, 1, 1>(c, l) : launch<T, WHAT, D, 1, 0>(c, l);
-  return slope ? launch<T, WHAT, D, 0, 1>(c, l) : launch<T, WHAT, D, 0, 0>(c, l);
+  if (cap) return slope ? launch_parts<T, WHAT, D, 1, 1>(c, l) : launch_parts<T, WHAT, D, 1, 0>(c, l);
+  return slope ? launch_parts<T, WHAT, D, 0, 1>(c, l) : launch_parts<T, WHAT, D, 0, 0>(c, l);
 }
 template <class T, int WHAT>
 bool launch_shape(const AttnCall &c, const AttnLaunch &l) {

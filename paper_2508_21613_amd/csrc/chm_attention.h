@@ -63,8 +63,12 @@ struct AttnCall {
   // layout of the launch: the workgroups' tiles of rows or keys
   int32_t tiles_here, heads_abreast;
   AttnDivide by_abreast, by_splits, by_tiles, by_kv_heads;
+  // tiles of `order_keys` keys of each sequence, those that most queries see first, or null; worked out by the first workgroups of dq's launch
+  int32_t *order;
+  int32_t order_groups, order_tiles, order_keys;
 };
 
+enum { ATTN_ORDER_TILES = 1024, ATTN_ORDER_QUERIES = 1024 };      // tiles of keys and of queries that an order is worked out for
 // Kernels of a pass; dim: 64 or 128; parts: wavefronts that share a sum, 1 or 2.  false: HIP failed.
 struct AttnLaunch { int32_t dim, parts; uint32_t groups; void *stream; };
 bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);

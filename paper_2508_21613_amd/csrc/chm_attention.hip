@@ -1,7 +1,7 @@
 // Attention: what its passes consist of, the small kernels around the tiles (documents, packing, joined sums), the entry points.
 //
-//   forward    [pack] [documents] tiles [join]
-//   backward   [pack] [documents] dq (and delta = dy.y), dk and dv [join]
+//   forward    [documents, packing] tiles [join]
+//   backward   [documents, packing] dq (and delta = dy.y), dk and dv [join]
 // dq and dk with dv are kernels of their own, each of which works out the scores again: seven products in place of five, but no sums that several
 // workgroups add to, so that the same inputs give the same bits.
 #include <hip/hip_runtime.h>
@@ -27,11 +27,12 @@ struct DocumentsCall {
   AttnTile *tiles;
   int32_t n, index_bits, tiles_each;
 };
-// a wavefront for each tile of 64 tokens
-__global__ void __launch_bounds__(64) k_documents(DocumentsCall a, DocumentsCall b, int first) {
-  const bool second = (int)blockIdx.x >= first;
+// a wavefront for each tile of 64 tokens: those of the keys, behind them those of the queries
+__device__ void documents_of(const DocumentsCall &a, const DocumentsCall &b, int64_t first, int64_t all, int64_t at_tile, int lane) {
+  if (at_tile >= all) return;
+  const bool second = at_tile >= first;
   const DocumentsCall &c = second ? b : a;
-  const int block = blockIdx.x - (second ? first : 0), seq = block / c.tiles_each, tile = block - seq * c.tiles_each, t = tile * ATTN_TILE + threadIdx.x;
+  const int block = (int)(at_tile - (second ? first : 0)), seq = block / c.tiles_each, tile = block - seq * c.tiles_each, t = tile * ATTN_TILE + lane;
   int64_t doc = -1;
   bool pre = false;
   if (t < c.n) {
@@ -40,7 +41,7 @@ __global__ void __launch_bounds__(64) k_documents(DocumentsCall a, DocumentsCall
     pre = c.prefix && c.prefix[seq * c.ld_prefix + t] != 0;
   }
   const bool some = doc >= 0 && doc < INT32_MAX;
-  const int64_t at = (int64_t)block * ATTN_TILE + threadIdx.x;
+  const int64_t at = (int64_t)block * ATTN_TILE + lane;
   c.words[at] = some ? (uint32_t)doc * 2 + (pre ? 1 : 0) : ATTN_NONE;
   int lo = some ? (int)doc : INT32_MAX, hi = some ? (int)doc : -1;
 #pragma unroll
@@ -50,7 +51,7 @@ __global__ void __launch_bounds__(64) k_documents(DocumentsCall a, DocumentsCall
     hi = h > hi ? h : hi;
   }
   const uint64_t none = __ballot(!some && t < c.n), yes = __ballot(some && pre);      // places behind the last token are masked by their number
-  if (threadIdx.x == 0)
+  if (lane == 0)
     c.tiles[block] = AttnTile{lo, hi, (none ? ATTN_SOME_NONE : 0) | (yes ? ATTN_SOME_PREFIX : 0) | (yes == ~0ull ? ATTN_ALL_PREFIX : 0), 0};
 }
 
@@ -60,8 +61,7 @@ struct PackCall {
   int32_t count, dim, dim8;
 };
 // rows of dim elements one behind the other, rounded up to whole words of 8, zeros behind
-__global__ void __launch_bounds__(256) k_pack(PackCall c) {
-  uint32_t g = blockIdx.x;
+__device__ void pack(const PackCall &c, uint32_t g) {
   int i = 0;
   while (i + 1 < c.count && g >= c.m[i].groups) g -= c.m[i++].groups;
   const auto &m = c.m[i];
@@ -83,6 +83,12 @@ __global__ void __launch_bounds__(256) k_pack(PackCall c) {
       if (d + e < c.dim) v[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
   }
   *(Words *)(m.out + w * 8) = v;
+}
+
+// Both in one launch: neither waits for the other, and each is a few us (515 tokens, 6 heads of 72: 3 and 5)
+__global__ void __launch_bounds__(256) k_prepare(DocumentsCall a, DocumentsCall b, int64_t first, int64_t all, uint32_t document_groups, PackCall c) {
+  if (blockIdx.x < document_groups) documents_of(a, b, first, all, (int64_t)blockIdx.x * 4 + threadIdx.x / 64, threadIdx.x % 64);
+  else pack(c, blockIdx.x - document_groups);
 }
 
 // ---------------------------------------------------------------------------------------------- joins
@@ -268,36 +274,30 @@ struct Pass {
     if (g) packed(c.dy, a->tokens, a->heads, group_of(a), 8);
     pack.dim = (int32_t)a->dim;
     pack.dim8 = c.dim;
-    if (pack.count) {
-      int64_t groups = 0;
-      for (int i = 0; i < pack.count; ++i) groups += pack.m[i].groups;
-      const uint32_t n = threads(groups, 256);
-      if (run && fits && n) {
-        hipLaunchKernelGGL(k_pack, dim3(n), dim3(256), 0, st, pack);
-        ok = ok && hipGetLastError() == hipSuccess;
-      }
-    }
-    if (!a->k_documents && !a->prefix) return;
+    int64_t packs = 0, first = 0, all = 0;
+    for (int i = 0; i < pack.count; ++i) packs += pack.m[i].groups;
     DocumentsCall kd{(const char *)a->k_documents, a->prefix, a->ld_k_documents, a->ld_prefix, nullptr, nullptr, c.keys, a->index_bits, c.tiles};
     DocumentsCall qd{(const char *)a->q_documents, nullptr, a->ld_q_documents, 0, nullptr, nullptr, c.tokens, a->index_bits, c.q_tile_count};
-    const auto room = [&](DocumentsCall &d) {
-      d.words = (uint32_t *)arena.take((uint64_t)a->batch * d.tiles_each * ATTN_TILE * 4);
-      d.tiles = (AttnTile *)arena.take((uint64_t)a->batch * d.tiles_each * sizeof(AttnTile));
-    };
-    room(kd);
-    // the queries' tokens are the keys': their words are (the prefix is asked of keys alone)
-    const bool same = a->tokens == a->keys && a->q_documents == a->k_documents && (a->batch == 1 || a->ld_q_documents == a->ld_k_documents);
-    if (same) qd.words = kd.words, qd.tiles = kd.tiles;
-    else room(qd);
-    c.k_words = kd.words; c.k_tiles = kd.tiles;
-    c.q_words = qd.words; c.q_tiles = qd.tiles;
-    if (!run) {                            // only whether there are any is asked
-      c.k_words = c.q_words = (const uint32_t *)1;
+    if (a->k_documents || a->prefix) {
+      const auto room = [&](DocumentsCall &d) {
+        d.words = (uint32_t *)arena.take((uint64_t)a->batch * d.tiles_each * ATTN_TILE * 4);
+        d.tiles = (AttnTile *)arena.take((uint64_t)a->batch * d.tiles_each * sizeof(AttnTile));
+      };
+      room(kd);
+      // the queries' tokens are the keys': their words are (the prefix is asked of keys alone)
+      const bool same = a->tokens == a->keys && a->q_documents == a->k_documents && (a->batch == 1 || a->ld_q_documents == a->ld_k_documents);
+      if (same) qd.words = kd.words, qd.tiles = kd.tiles;
+      else room(qd);
+      c.k_words = kd.words; c.k_tiles = kd.tiles;
+      c.q_words = qd.words; c.q_tiles = qd.tiles;
+      if (!run) c.k_words = c.q_words = (const uint32_t *)1;      // only whether there are any is asked
+      first = a->batch * kd.tiles_each;
+      all = first + (same ? 0 : a->batch * qd.tiles_each);
     }
-    const int64_t first = a->batch * kd.tiles_each, all = first + (same ? 0 : a->batch * qd.tiles_each);
-    const uint32_t n = threads(all, 64);
+    const int64_t documents = up(all, 4);
+    const uint32_t n = threads(documents + packs, 256);
     if (run && fits && n) {
-      hipLaunchKernelGGL(k_documents, dim3(n), dim3(64), 0, st, kd, qd, (int)first);
+      hipLaunchKernelGGL(k_prepare, dim3(n), dim3(256), 0, st, kd, qd, first, all, (uint32_t)documents, pack);
       ok = ok && hipGetLastError() == hipSuccess;
     }
   }
@@ -364,6 +364,8 @@ struct Pass {
     }
   }
 
+  int dkdv_parts() const { return dkdv_splits(heads() * up(a->keys, chosen.dkdv_keys), up(rows(), ATTN_TILE), a->causal != 0, chosen.dim); }
+
   void backward(const chm_attention_gradients *g) {
     if (a->batch == 0) return;
     const int64_t B = a->batch, T = a->tokens, K = a->keys;
@@ -374,15 +376,24 @@ struct Pass {
     c.dv = output(g->dv, g->dv_stride, B, K, a->kv_heads);
     inputs(g);
     c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
+    chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
     if (T > 0) {
       chosen.dq_rows = dq_tile();
-      const AttnLaunch l = layout(up(rows(), chosen.dq_rows), 1, 128 / chosen.dq_rows);
+      AttnLaunch l = layout(up(rows(), chosen.dq_rows), 1, 128 / chosen.dq_rows);
+      // Where documents make key tiles differ and not all of them run at once, the longest go first.  Their order is worked out beside dq.
+      const int64_t tiles = up(K, chosen.dkdv_keys);
+      if (a->k_documents && heads() * tiles * dkdv_parts() > 512 && tiles <= ATTN_ORDER_TILES && c.q_tile_count <= ATTN_ORDER_QUERIES) {
+        c.order = (int32_t *)arena.take((uint64_t)(a->batch * tiles) * 4);
+        c.order_groups = a->batch;
+        c.order_tiles = (int32_t)tiles;
+        c.order_keys = chosen.dkdv_keys;
+        l.groups = threads((int64_t)l.groups + a->batch, 256);
+      }
       if (run && fits) ok = ok && (bf16() ? attn_dq_bf16 : attn_dq_f16)(c, l);
     }
     if (K > 0) {
-      chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
       const int64_t tiles = up(K, chosen.dkdv_keys);
-      const AttnLaunch l = layout(tiles, dkdv_splits(heads() * tiles, up(rows(), ATTN_TILE), a->causal != 0, chosen.dim), 128 / chosen.dkdv_keys);
+      const AttnLaunch l = layout(tiles, dkdv_parts(), 128 / chosen.dkdv_keys);
       chosen.dkdv_splits = c.splits;
       const int64_t words = heads() * K * (c.width4 / 4);
       if (c.splits > 1) {

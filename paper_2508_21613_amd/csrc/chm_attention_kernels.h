@@ -85,9 +85,9 @@ __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r
 // which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
 // which see the most
 struct Place { int b, h, hb, tile, split; };
-__device__ __forceinline__ Place place_of(const AttnCall &c, bool last_first) {
+__device__ __forceinline__ Place place_of(const AttnCall &c, int i, bool last_first) {
   Place p;
-  const int i = blockIdx.x, j = divide(c.by_abreast, i), k = divide(c.by_splits, j), band = divide(c.by_tiles, k);
+  const int j = divide(c.by_abreast, i), k = divide(c.by_splits, j), band = divide(c.by_tiles, k);
   p.split = j - k * c.splits;
   p.tile = k - band * c.tiles_here;
   if (last_first) p.tile = c.tiles_here - 1 - p.tile;
@@ -617,7 +617,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS;
-  const Place p = place_of(c, true);
+  const Place p = place_of(c, blockIdx.x, true);
   const int row0 = p.tile * (BLOCKS * 32), wave_row = row0 + wave % BLOCKS * 32, h4 = (lane >> 5) * 4;
   // the queries come by the second slot, a wavefront's to its own part
   const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
@@ -735,7 +735,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   lds_char *own = lds + wave * OWN;
   const uint32_t own0 = (uint32_t)(uintptr_t)own;
-  const Place p = place_of(c, false);
+  const Place p = place_of(c, blockIdx.x, false);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, 0, lane);
   row.operands(c, p.b, lane);
@@ -892,6 +892,37 @@ __device__ __forceinline__ void deltas_of(const AttnCall &c, const Place &p, int
   }
 }
 
+// The order of a sequence's tiles of keys for dk and dv: by how many tiles of queries see them.  A workgroup of its own, which is done long before the others.
+enum { ORDER_COSTS = ATTN_ORDER_QUERIES * 16, ORDER_BYTES = ORDER_COSTS + ATTN_ORDER_TILES * 4 };
+__device__ __forceinline__ void order_keys(const AttnCall &c, int b, lds_char *lds) {
+  __attribute__((address_space(3))) i4 *queries = (__attribute__((address_space(3))) i4 *)lds;
+  __attribute__((address_space(3))) int *cost = (__attribute__((address_space(3))) int *)(lds + ORDER_COSTS);
+  const int n = c.order_tiles, each = c.order_keys / ATTN_TILE;
+  for (int i = threadIdx.x; i < c.q_tile_count; i += 256) queries[i] = *(const i4 *)&c.q_tiles[(int64_t)b * c.q_tile_count + i];
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int k0 = i * c.order_keys, k1 = k0 + c.order_keys - 1 < c.keys ? k0 + c.order_keys - 1 : c.keys - 1;
+    Range k{INT32_MAX, -1, 0};
+    for (int j = i * each; j < (i + 1) * each && j < c.tiles; ++j) {
+      const AttnTile x = c.k_tiles[(int64_t)b * c.tiles + j];
+      k = join(k, x);
+      k.flags |= x.flags & ATTN_SOME_PREFIX;
+    }
+    int seen = 0;
+    for (int j = 0; j < c.q_tile_count; ++j) {
+      const i4 x = queries[j];
+      seen += sees(c, j * ATTN_TILE + c.offset, j * ATTN_TILE + ATTN_TILE - 1 + c.offset, Range{x[0], x[1], x[2]}, k0, k1, k).some;
+    }
+    cost[i] = seen;
+  }
+  __syncthreads();
+  for (int i = threadIdx.x; i < n; i += 256) {
+    int before = 0;
+    for (int j = 0; j < n; ++j) before += cost[j] > cost[i] || (cost[j] == cost[i] && j < i);
+    c.order[(int64_t)b * n + before] = i;
+  }
+}
+
 // PARTS as in k_forward
 template <class T, int D, int CAP, int SLOPE, int PARTS>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_dq(const AttnCall c) {
@@ -899,12 +930,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   constexpr int WAVES = 4, BLOCKS = WAVES / PARTS, N = D / 32 / PARTS;
   typedef TileFeed<D, WAVES> Feed;
   constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 4096 : 0;
+  static_assert((int)ORDER_BYTES <= (int)Feed::BYTES, "shared memory holds what an order is worked out from");
   __shared__ float deltas[BLOCKS][32];
   __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > TURN + MEET ? Feed::BYTES : TURN + MEET];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
-  const Place p = place_of(c, true);
+  if ((int)blockIdx.x < c.order_groups) return order_keys(c, blockIdx.x, lds);
+  const Place p = place_of(c, blockIdx.x - c.order_groups, true);
   const int row0 = p.tile * (BLOCKS * 32), wave_row = row0 + block * 32, h4 = (lane >> 5) * 4;
   // dy comes by the second slot, a wavefront's rows to its own part
   const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
@@ -1101,7 +1134,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   lds_char *lds = (lds_char *)shared, *values = lds + VALUES;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
-  const Place p = place_of(c, false);
+  Place p = place_of(c, blockIdx.x, false);
+  if (c.order) p.tile = c.order[p.b * c.tiles_here + p.tile];
   const int key0 = p.tile * KEYS, wave_key = key0 + block * 32;
   const int h4 = (lane >> 5) * 4;
   s8 k[D / 16];

@@ -237,18 +237,19 @@ PAIRINGS = {"halves": 0, "neighbours": 1}
 
 
 def _strided(name, t, shape, dtype, device):
-    """checks a tensor of that many dimensions (sizes of None: any) whose last one has unit stride"""
+    """checks a tensor of that shape (a number: of so many dimensions), whose last dimension has unit stride, and returns its shape"""
     if not isinstance(t, torch.Tensor):
         raise B.ChmError(B.ERR_ARG, name + " must be a tensor")
-    if t.dim() != len(shape) or any([want is not None and n != want for n, want in zip(t.shape, shape)]):
-        raise B.ChmError(B.ERR_ARG, "%s must be %s, is %s" % (name, " x ".join(["any" if n is None else str(n) for n in shape]), list(t.shape)))
+    got = t.shape
+    if (len(got) if type(shape) is int else got) != shape:
+        raise B.ChmError(B.ERR_ARG, "%s must be %s, is %s" % (name, "of %d dimensions" % shape if type(shape) is int else list(shape), list(got)))
     if not t.is_cuda or (device is not None and t.get_device() != device):
         raise B.ChmError(B.ERR_ARG, name + " must be on the GPU, the same as the others")
     if dtype is not None and t.dtype != dtype:
         raise B.ChmError(B.ERR_ARG, "%s must be %s" % (name, dtype))
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
+    if got[-1] > 1 and t.stride(-1) != 1:
         raise B.ChmError(B.ERR_ARG, name + " must have unit stride along its last dimension")
-    return t
+    return got
 
 
 class Rotary:
@@ -284,15 +285,16 @@ class Rotary:
         self._pairing = PAIRINGS[pairing]
 
     def _turn(self, name, x, positions, backwards, out, stream):
-        _strided(name, x, (None, None, self.head_dim), None, None)
+        n, heads, dim = _strided(name, x, 3, None, None)
         dtype, dev = x.dtype, x.get_device()
+        _need(dim == self.head_dim, name + "'s heads must have the elements that were described")
         _need(dtype in DTYPES, name + " must be float32, bfloat16 or float16")
-        n, heads = x.shape[0], x.shape[1]
         _need(isinstance(positions, torch.Tensor) and positions.is_cuda and positions.get_device() == dev, "positions must be on the same GPU as the others")
         _need(positions.dtype in INDEX_BITS, "positions must be int32 or int64")
         if positions.dim() == 1 and self.axes == 1:
             positions = positions[None]
-        _need(tuple(positions.shape) == (self.axes, n), "positions must be %d x %d (axes x tokens)" % (self.axes, n))
+        if positions.shape != (self.axes, n):
+            raise B.ChmError(B.ERR_ARG, "positions must be %d x %d (axes x tokens)" % (self.axes, n))
         if out is not None:
             _strided("out", out, (n, heads, self.head_dim), dtype, dev)
         _unrecorded(x)
@@ -321,13 +323,13 @@ def _strides(t):
 
 def _attention(q, k, v, scale, cap, slopes, causal, documents, prefix):
     """the call's description, its GPU, and the tensors it points to"""
-    _strided("q", q, (None, None, None, None), None, None)
+    batch, tokens, heads, dim = _strided("q", q, 4, None, None)
     dtype, dev = q.dtype, q.get_device()
-    _need(dtype in (torch.bfloat16, torch.float16), "q must be bfloat16 or float16")
-    batch, tokens, heads, dim = q.shape
-    _strided("k", k, (batch, None, None, dim), dtype, dev)
-    keys, kv_heads = k.shape[1], k.shape[2]
-    _strided("v", v, (batch, keys, kv_heads, dim), dtype, dev)
+    _need(dtype is torch.bfloat16 or dtype is torch.float16, "q must be bfloat16 or float16")
+    shape = _strided("k", k, 4, dtype, dev)
+    keys, kv_heads = shape[1], shape[2]
+    _need(shape[0] == batch and shape[3] == dim, "q and k must have the same batch and elements of a head")
+    _strided("v", v, shape, dtype, dev)
     _need(kv_heads > 0 and heads > 0 and heads % kv_heads == 0, "the heads of q must be a multiple of those of k and v")
     _need(1 <= dim <= 128, "heads must have 1 to 128 elements")
     scale = dim ** -0.5 if scale is None else float(scale)
@@ -374,7 +376,7 @@ def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, do
     (bool [batch, keys]) names.  One that sees nothing gets zeros.  With save=True returns (y, saved), `saved` being what attention_backward wants."""
     d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
     if out is not None:
-        _strided("out", out, tuple(q.shape), q.dtype, dev)
+        _strided("out", out, q.shape, q.dtype, dev)
     if not save:
         _unrecorded(q, k, v)
     lib = B.lib()
@@ -387,8 +389,8 @@ def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, do
             d.saved = saved.data_ptr()
         if out is None:
             out = q.new_empty(q.shape)
-        ws = _bytes(scratch.value, q)
-        B._check(lib.chm_attention_forward(d, out.data_ptr(), B.Strides(*_strides(out)), ws.data_ptr(), ws.numel(), st))
+        ws = _bytes(scratch.value, q) if scratch.value else None
+        B._check(lib.chm_attention_forward(d, out.data_ptr(), B.Strides(*_strides(out)), ws.data_ptr() if ws is not None else None, scratch, st))
     return (out, saved) if save else out
 
 
@@ -396,15 +398,15 @@ def attention_backward(dy, q, k, v, y, saved, scale=None, cap=0.0, slopes=None, 
     """chm_attention_backward: (dq, dk, dv) for dy, the gradient with respect to y, from attention_forward's y and saved; the other arguments as there.
     `out`: the three tensors to write (of any strides: the parts of one projection's gradient)."""
     d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
-    _strided("dy", dy, tuple(q.shape), q.dtype, dev)
-    _strided("y", y, tuple(q.shape), q.dtype, dev)
+    _strided("dy", dy, q.shape, q.dtype, dev)
+    _strided("y", y, q.shape, q.dtype, dev)
     _need(isinstance(saved, torch.Tensor) and saved.get_device() == dev and saved.dtype == torch.uint8 and saved.is_contiguous(),
           "saved must be what attention_forward returned")
     if out is not None:
         out = tuple(out)
         _need(len(out) == 3, "out must be three tensors")
         for name, t, like in zip(("out[0]", "out[1]", "out[2]"), out, (q, k, v)):
-            _strided(name, t, tuple(like.shape), q.dtype, dev)
+            _strided(name, t, like.shape, q.dtype, dev)
     lib = B.lib()
     with _scope(stream, dev, dy, y, saved, *held, *(out or ())) as st:
         if out is None:

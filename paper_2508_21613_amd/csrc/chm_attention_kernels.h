@@ -331,39 +331,46 @@ struct KeyWalk {
   int at, end;                              // those of the present ballot: at .. at + 63; end: behind the last tile
   uint64_t visit, mine, documents, order, none;
 
-  // word: of the lane's row
-  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int wave_row, uint32_t word, int first_, int step_, int end_) {
+  // word: of the lane's row.  The first 64 tiles are asked for along with all else that is needed to choose among them.
+  __device__ __forceinline__ void start(const AttnCall &c, int b, int group_row, int wave_row, uint32_t word, int first_, int step_, int end_, int lane) {
     tiles = c.k_words ? c.k_tiles + (int64_t)b * c.tiles : nullptr;
     const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
     const int gf = token(group_row), gt = token(group_row + ROWS - 1), wf = token(wave_row), wt = token(wave_row + 31);
     group_from = gf + c.offset; group_to = gt + c.offset;
     wave_from = wf + c.offset; wave_to = wt + c.offset;
+    first = first_;
+    step = step_;
+    at = 0;
+    end = end_;
+    const AttnTile x = documents_of(lane);
     if (tiles) {
       group_docs = range_of<ROWS / 64 + 1>(c.q_tiles + (int64_t)b * c.q_tile_count, gf, gt);
       wave_docs = range_of(word);
     }
-    first = first_;
-    step = step_;
-    at = -64;
-    end = end_;
-    visit = 0;
+    choose(c, x, lane);
+  }
+  // of the lane's tile of the present 64
+  __device__ __forceinline__ AttnTile documents_of(int lane) const {
+    const int64_t t = (int64_t)(at + lane) * step + first;
+    return tiles && t < end ? tiles[t] : AttnTile{0, 0, 0, 0};
+  }
+  __device__ __forceinline__ void choose(const AttnCall &c, const AttnTile &x, int lane) {
+    const int64_t tt = (int64_t)(at + lane) * step + first;
+    const bool there = tt < end;
+    const int t = there ? (int)tt : 0, k0 = t * ATTN_TILE, k1 = k0 + ATTN_TILE - 1;
+    const Range k{x.first, x.last, x.flags};
+    const Sight group = sees(c, group_from, group_to, group_docs, k0, k1, k), wave = sees(c, wave_from, wave_to, wave_docs, k0, k1, k);
+    visit = __ballot(there && group.some);
+    mine = __ballot(there && wave.some);
+    documents = __ballot(there && tiles && !(wave.documents && k1 < c.keys));           // places behind the last key are of no document
+    order = __ballot(there && !(wave.order && (tiles || k1 < c.keys)));
+    none = __ballot(there && tiles && (k.flags & ATTN_SOME_NONE));
   }
   __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
+      if ((int64_t)(at + 64) * step + first >= end) return Visit{-1, false, false, false, false};
       at += 64;
-      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false, false};
-      const int64_t tt = (int64_t)(at + lane) * step + first;
-      const bool there = tt < end;
-      const int t = there ? (int)tt : 0;
-      Range k{0, 0, 0};
-      if (tiles && there) { const AttnTile x = tiles[t]; k = Range{x.first, x.last, x.flags}; }
-      const int k0 = t * ATTN_TILE, k1 = k0 + ATTN_TILE - 1;
-      const Sight group = sees(c, group_from, group_to, group_docs, k0, k1, k), wave = sees(c, wave_from, wave_to, wave_docs, k0, k1, k);
-      visit = __ballot(there && group.some);
-      mine = __ballot(there && wave.some);
-      documents = __ballot(there && tiles && !(wave.documents && k1 < c.keys));         // places behind the last key are of no document
-      order = __ballot(there && !(wave.order && (tiles || k1 < c.keys)));
-      none = __ballot(there && tiles && (k.flags & ATTN_SOME_NONE));
+      choose(c, documents_of(lane), lane);
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
@@ -628,7 +635,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
   KeyWalk<BLOCKS * 32> walk;
-  walk.start(c, p.b, row0, wave_row, row.raw, p.split, c.splits, c.tiles);
+  walk.start(c, p.b, row0, wave_row, row.raw, p.split, c.splits, c.tiles, lane);
   Visit next = walk.next(c, lane);
   if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
   Soft soft;
@@ -744,7 +751,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
   vf.start(c.v, p.b, p.h, c.keys, c.dim, 0, lane);
   const uint32_t *words = c.k_words ? c.k_words + (int64_t)p.b * c.tiles * ATTN_TILE : nullptr;
   KeyWalk<32> walk;
-  walk.start(c, p.b, 0, 0, row.raw, p.split * WAVES + wave, c.splits * WAVES, c.tiles);
+  walk.start(c, p.b, 0, 0, row.raw, p.split * WAVES + wave, c.splits * WAVES, c.tiles, lane);
   typedef Softmax<T, D, CAP, SLOPE> Soft;
   Soft soft;
   soft.start();
@@ -854,43 +861,50 @@ __device__ __forceinline__ void gradient(const AttnCall &c, float product, float
 // delta are near each other, and 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3
 // without, 2.4e-3 with).  A row by as many lanes as it has chunks.
 template <class T, int D, int ROWS>
-__device__ __forceinline__ void deltas_of(const AttnCall &c, const Place &p, int first, const lds_char *dys, int first_there, float *out, int lane) {
+struct Deltas {
   typedef Shape<D> S;
   typedef s8 s8_anywhere __attribute__((aligned(2)));
-  constexpr int EACH = S::CHUNKS, AT_ONCE = 64 / EACH, N = ROWS / AT_ONCE;
-  const int chunk = lane % EACH, d = chunk * 8;
-  s8 y[N], low[N];                          // all are asked for before the first is used
+  enum { EACH = S::CHUNKS, AT_ONCE = 64 / EACH, N = ROWS / AT_ONCE };
+  s8 y[N], low[N];
+  // asks for ROWS rows from `first` on
+  __device__ __forceinline__ void start(const AttnCall &c, const Place &p, int first, int lane) {
+    const int d = lane % EACH * 8;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int row = first + i * AT_ONCE + lane / EACH, r = row < c.rows ? row : c.rows - 1, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
-    const uint16_t *a = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
-    const uint16_t *b = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
-    if (c.width % 8 == 0) {                 // chunks behind the last: left out of the sum
-      const int at = d < c.width ? d : 0;
-      y[i] = *(const s8_anywhere *)(a + at);
-      low[i] = *(const s8_anywhere *)(b + at);
-    } else {
+    for (int i = 0; i < N; ++i) {
+      const int row = first + i * AT_ONCE + lane / EACH, r = row < c.rows ? row : c.rows - 1, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
+      const uint16_t *a = c.y_in.p + p.b * c.y_in.batch + token * c.y_in.token + head * c.y_in.head;
+      const uint16_t *b = c.low + (((int64_t)p.b * c.tokens + token) * (c.kv_heads * c.group) + head) * c.width;
+      if (c.width % 8 == 0) {               // chunks behind the last: left out of the sum
+        const int at = d < c.width ? d : 0;
+        y[i] = *(const s8_anywhere *)(a + at);
+        low[i] = *(const s8_anywhere *)(b + at);
+      } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const bool in = d + e < c.width;
-        y[i][e] = in ? (short)a[d + e] : (short)0;
-        low[i][e] = in ? (short)b[d + e] : (short)0;
+        for (int e = 0; e < 8; ++e) {
+          const bool in = d + e < c.width;
+          y[i][e] = in ? (short)a[d + e] : (short)0;
+          low[i][e] = in ? (short)b[d + e] : (short)0;
+        }
       }
     }
   }
+  // their dy are the rows from `first` on of `dys`
+  __device__ __forceinline__ void finish(const AttnCall &c, const lds_char *dys, int first, float *out, int lane) const {
+    const int chunk = lane % EACH;
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const int row = first_there + i * AT_ONCE + lane / EACH;
-    const s8 dy = *(const __attribute__((address_space(3))) s8 *)(dys + S::row_at(row) + ((uint32_t)chunk ^ S::swizzle(row)) * 16);
-    float sum = 0.f;
+    for (int i = 0; i < N; ++i) {
+      const int row = first + i * AT_ONCE + lane / EACH;
+      const s8 dy = *(const __attribute__((address_space(3))) s8 *)(dys + S::row_at(row) + ((uint32_t)chunk ^ S::swizzle(row)) * 16);
+      float sum = 0.f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[e]), T::up((uint16_t)y[i][e]) + T::up((uint16_t)low[i][e]), sum);
-    if (d >= c.width) sum = 0.f;
+      for (int e = 0; e < 8; ++e) sum = fmaf(T::up((uint16_t)dy[e]), T::up((uint16_t)y[i][e]) + T::up((uint16_t)low[i][e]), sum);
+      if (chunk * 8 >= c.width) sum = 0.f;
 #pragma unroll
-    for (int x = EACH / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
-    if (chunk == 0) out[i * AT_ONCE + lane / EACH] = sum;
+      for (int x = EACH / 2; x >= 1; x >>= 1) sum += __shfl_xor(sum, x);
+      if (chunk == 0) out[i * AT_ONCE + lane / EACH] = sum;
+    }
   }
-}
+};
 
 // The order of a sequence's tiles of keys for dk and dv: by how many tiles of queries see them.  A workgroup of its own, which is done long before the others.
 enum { ORDER_COSTS = ATTN_ORDER_QUERIES * 16, ORDER_BYTES = ORDER_COSTS + ATTN_ORDER_TILES * 4 };
@@ -947,19 +961,21 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   feed.start(c, p, wave, lane);
   QueryRow<T, D> row;
   row.start(c, p.b, p.h, wave_row, lane);
-  KeyWalk<BLOCKS * 32> walk;
-  walk.start(c, p.b, row0, wave_row, row.raw, 0, 1, c.tiles);
   row.operands(c, p.b, lane);
+  constexpr int SHARE = 32 / PARTS;         // rows whose delta a wavefront works out
+  Deltas<T, D, SHARE> known;
+  known.start(c, p, wave_row + part * SHARE, lane);
   const bool there = row.row < c.rows;
   const float lse = c.lse[(int64_t)p.hb * c.rows_pad + (there ? row.row : c.rows - 1)];
+  KeyWalk<BLOCKS * 32> walk;
+  walk.start(c, p.b, row0, wave_row, row.raw, 0, 1, c.tiles, lane);
   Visit next = walk.next(c, lane);
   if (next.tile >= 0) feed.load(next.tile, lds0, wave, lane);
   waited<0>();
   s8 dy[D / 16];
 #pragma unroll
   for (int k = 0; k < D / 16; ++k) dy[k] = row_fragment<D>(lds + mine, 0, k, lane);
-  constexpr int SHARE = 32 / PARTS;         // rows whose delta a wavefront works out
-  deltas_of<T, D, SHARE>(c, p, wave_row + part * SHARE, lds + mine, part * SHARE, &deltas[block][part * SHARE], lane);
+  known.finish(c, lds + mine, part * SHARE, &deltas[block][part * SHARE], lane);
   if (PARTS == 2) {
     __syncthreads();
   } else {
@@ -1045,23 +1061,32 @@ struct RowWalk {
   int own, first, step, at, end;
   uint64_t visit, mine, documents, order, none;
   // word: of the lane's key
-  __device__ __forceinline__ void start(const AttnCall &c, const Place &p, int group_key, int wave_key, uint32_t word, int own_, int first_, int step_, int end_) {
+  __device__ __forceinline__ void start(const AttnCall &c, const Place &p, int group_key, int wave_key, uint32_t word, int own_, int first_, int step_, int end_, int lane) {
     own = own_;
     group_from = group_key;
     group_to = group_key + KEYS - 1 < c.keys ? group_key + KEYS - 1 : c.keys - 1;
     wave_from = wave_key < c.keys ? wave_key : c.keys - 1;
     wave_to = wave_key + 31 < c.keys ? wave_key + 31 : c.keys - 1;
-    rows = nullptr;
-    if (c.k_words) {
-      rows = c.row_data + (int64_t)p.hb * (c.rows_pad / 32);
+    first = first_;
+    step = step_;
+    at = 0;
+    end = end_;
+    rows = c.k_words ? c.row_data + (int64_t)p.hb * (c.rows_pad / 32) : nullptr;
+    const Known x = documents_of(lane);
+    if (rows) {
       group_docs = keys_of<KEYS / 64>(c.k_tiles + (int64_t)p.b * c.tiles, group_from, group_to);
       wave_docs = range_of(word);
     }
-    first = first_;
-    step = step_;
-    at = -64;
-    end = end_;
-    visit = 0;
+    choose(c, x, lane);
+  }
+  struct Known { AttnTile x[ROWS / 32]; };
+  __device__ __forceinline__ Known documents_of(int lane) const {
+    Known known{};
+    const int64_t t = (int64_t)(at + lane) * step + first;
+    if (rows && t < end)
+#pragma unroll
+      for (int j = 0; j < ROWS / 32; ++j) known.x[j] = rows[t * (ROWS / 32) + j].documents;
+    return known;
   }
   template <int N>
   static __device__ __forceinline__ Range keys_of(const AttnTile *tiles, int from, int to) {
@@ -1077,36 +1102,27 @@ struct RowWalk {
     }
     return r;
   }
+  __device__ __forceinline__ void choose(const AttnCall &c, const Known &known, int lane) {
+    const int64_t tt = (int64_t)(at + lane) * step + first;
+    const bool there = tt < end;
+    const int r0 = there ? (int)tt * ROWS : 0;
+    const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
+    const int t0 = token(r0), t1 = token(r0 + ROWS - 1);
+    const Range one = join(Range{INT32_MAX, -1, 0}, known.x[0]);
+    const Range q = ROWS == 32 ? one : join(one, known.x[ROWS / 32 - 1]), mine_q = own == 0 ? one : join(Range{INT32_MAX, -1, 0}, known.x[ROWS / 32 - 1]);
+    const Sight group = sees(c, t0 + c.offset, t1 + c.offset, q, group_from, group_to, group_docs);
+    const Sight wave = sees(c, (ROWS == 32 ? t0 : token(r0 + own)) + c.offset, (ROWS == 32 ? t1 : token(r0 + own + 31)) + c.offset, mine_q, wave_from, wave_to, wave_docs);
+    visit = __ballot(there && group.some);
+    mine = __ballot(there && wave.some && r0 + own < c.rows);
+    documents = __ballot(there && rows && !wave.documents);
+    order = __ballot(there && !(wave.order && r0 + own + 32 <= c.rows));
+    none = __ballot(there && rows && (q.flags & ATTN_SOME_NONE));
+  }
   __device__ __forceinline__ Visit next(const AttnCall &c, int lane) {
     while (!visit) {
+      if ((int64_t)(at + 64) * step + first >= end) return Visit{-1, false, false, false, false};
       at += 64;
-      if ((int64_t)at * step + first >= end) return Visit{-1, false, false, false, false};
-      const int64_t tt = (int64_t)(at + lane) * step + first;
-      const bool there = tt < end;
-      const int r0 = there ? (int)tt * ROWS : 0;
-      const auto token = [&](int r) { return divide(c.by_group, r < c.rows ? r : c.rows - 1); };
-      const int t0 = token(r0), t1 = token(r0 + ROWS - 1);
-      Range q{0, 0, 0}, mine_q{0, 0, 0};
-      if (rows) {
-        const int at_rows = r0 / 32;
-        AttnTile x[ROWS / 32];
-#pragma unroll
-        for (int j = 0; j < ROWS / 32; ++j) x[j] = rows[at_rows + j].documents;
-        q = join(Range{INT32_MAX, -1, 0}, x[0]);
-        if (ROWS == 64) {
-          mine_q = join(Range{INT32_MAX, -1, 0}, own ? x[ROWS / 32 - 1] : x[0]);
-          q = join(q, x[ROWS / 32 - 1]);
-        } else {
-          mine_q = q;
-        }
-      }
-      const Sight group = sees(c, t0 + c.offset, t1 + c.offset, q, group_from, group_to, group_docs);
-      const Sight wave = sees(c, (ROWS == 32 ? t0 : token(r0 + own)) + c.offset, (ROWS == 32 ? t1 : token(r0 + own + 31)) + c.offset, mine_q, wave_from, wave_to, wave_docs);
-      visit = __ballot(there && group.some);
-      mine = __ballot(there && wave.some && r0 + own < c.rows);
-      documents = __ballot(there && rows && !wave.documents);
-      order = __ballot(there && !(wave.order && r0 + own + 32 <= c.rows));
-      none = __ballot(there && rows && (q.flags & ATTN_SOME_NONE));
+      choose(c, documents_of(lane), lane);
     }
     const int i = __builtin_ctzll(visit);
     visit &= visit - 1;
@@ -1169,7 +1185,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     first = f < blocks ? (int)f : blocks;
   }
   RowWalk<KEYS, STEP> walk;
-  walk.start(c, p, key0, wave_key, word, part * 32, first + p.split, c.splits, blocks);
+  walk.start(c, p, key0, wave_key, word, part * 32, first + p.split, c.splits, blocks, lane);
   if (lane < 32) words[wave][lane] = word;  // for this wavefront alone
   f16 dk[D / 32], dv[D / 32];
 #pragma unroll

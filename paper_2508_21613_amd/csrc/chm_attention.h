@@ -35,6 +35,10 @@ struct AttnRows {
 };
 constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // with or without the lowest bit it equals no key's word, ATTN_NONE neither
 
+// A workgroup of dk and dv: its tile of keys (-1: none), the parts that the rows are dealt to and which of them it is, and where its sums go if there are several
+struct AttnShare { int32_t tile, part, parts, slot; };
+struct AttnSlots { int32_t first, count; };
+
 struct AttnCall {
   AttnInput q, k, v, dy;
   AttnInput y_in;                          // the forward pass's result, at any alignment
@@ -58,17 +62,20 @@ struct AttnCall {
   AttnRows *row_data;                      // [batch * kv_heads][rows_pad / 32]
   // sums split over workgroups: float32 parts, joined in order
   int32_t splits;
-  float *part, *part2;                     // forward: [splits][batch * kv_heads][rows][width4] and (maximum, sum); backward: dk and dv [splits][batch * kv_heads][keys][width4]
+  float *part, *part2;                     // forward: [splits][batch * kv_heads][rows][width4] and (maximum, sum); backward: dk and dv [batch * kv_heads][share_slots][keys of a tile][width4]
   int32_t width4;                          // width rounded up to 4
   // layout of the launch: the workgroups' tiles of rows or keys
   int32_t tiles_here, heads_abreast;
   AttnDivide by_abreast, by_splits, by_tiles, by_kv_heads;
-  // tiles of `order_keys` keys of each sequence, those that most queries see first, or null; worked out by the first workgroups of dq's launch
-  int32_t *order;
-  int32_t order_groups, order_tiles, order_keys;
+  // dk and dv: `share_slots` parts of the sums of a sequence's tiles of keys (share_keys each).  Shared out by the first workgroups of dq's launch, or (null) evenly:
+  // `splits` for each tile
+  AttnShare *shares;                       // [batch][share_slots]
+  AttnSlots *tile_slots;                   // [batch][share_tiles]
+  int32_t share_groups, share_tiles, share_keys, share_slots;
+  int32_t share_unit, share_least, share_short;            // blocks of rows of 64 tokens; fewest blocks of a part; most of one that is short
 };
 
-enum { ATTN_ORDER_TILES = 1024, ATTN_ORDER_QUERIES = 1024 };      // tiles of keys and of queries that an order is worked out for
+enum { ATTN_SHARE_TILES = 1024, ATTN_SHARE_QUERIES = 1024 };        // most tiles of keys and of queries that are shared out on the GPU
 // Kernels of a pass; dim: 64 or 128; parts: wavefronts that share a sum, 1 or 2.  false: HIP failed.
 struct AttnLaunch { int32_t dim, parts; uint32_t groups; void *stream; };
 bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);

@@ -134,15 +134,17 @@ __global__ void __launch_bounds__(256) k_join_backward(const AttnCall c, int64_t
   const int words = c.width4 / 4;
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= all) return;
-  const int64_t at = i / words, step = (int64_t)c.batch * c.kv_heads * c.keys * c.width4;
-  const int d = (int)(i - at * words) * 4;
+  const int64_t at = i / words, hb = at / c.keys, b = hb / c.kv_heads, j = at - hb * c.keys;
+  const int d = (int)(i - at * words) * 4, h = (int)(hb - b * c.kv_heads), tile = (int)(j / c.share_keys);
+  AttnSlots slots{tile * c.splits, c.splits};
+  if (c.shares) slots = c.tile_slots[b * c.share_tiles + tile];
+  if (slots.count == 1) return;             // written as it was summed
+  const int64_t step = (int64_t)c.share_keys * c.width4, from = (hb * c.share_slots + slots.first) * step + (j - (int64_t)tile * c.share_keys) * c.width4 + d;
   f4 k{0.f, 0.f, 0.f, 0.f}, v = k;
-  for (int s = 0; s < c.splits; ++s) {
-    k += *(const f4 *)(c.part + s * step + at * c.width4 + d);
-    v += *(const f4 *)(c.part2 + s * step + at * c.width4 + d);
+  for (int s = 0; s < slots.count; ++s) {
+    k += *(const f4 *)(c.part + from + s * step);
+    v += *(const f4 *)(c.part2 + from + s * step);
   }
-  const int64_t hb = at / c.keys, b = hb / c.kv_heads, j = at - hb * c.keys;
-  const int h = (int)(hb - b * c.kv_heads);
   put4<DT>(c.dk.p + b * c.dk.batch + j * c.dk.token + h * c.dk.head, d, c.width, k);
   put4<DT>(c.dv.p + b * c.dv.batch + j * c.dv.token + h * c.dv.head, d, c.width, v);
 }
@@ -192,7 +194,7 @@ struct Pass {
   bool run, ok = true;
   bool fits = true;                        // every launch's threads can be counted in 32 bits
   AttnCall c{};
-  chm_attention_kernels chosen{0, 0, 0, 0, 0, 0, 1, 1};
+  chm_attention_kernels chosen{0, 0, 0, 0, 0, 0, 1, 1, 0};
 
   Pass(const chm_attention *a_, char *base, hipStream_t st_, bool run_) : a(a_), arena{base}, st(st_), run(run_) {
     const int64_t G = group_of(a), d8 = up(a->dim, 8) * 8;
@@ -319,17 +321,30 @@ struct Pass {
     if (s > steps / least) s = steps / least;
     return (int)(s < 1 ? 1 : s < 16 ? s : 16);
   }
-  // Of dk and dv: as many as run at once, two a compute unit; with a causal mask, where the first keys see the most rows, twice as many if each keeps work
-  // enough to be worth its sums' way through memory in float32.  us with the join, 32 heads, 8 of keys, 128, causal, by parts: 512 tokens 38 (4), 33 (8);
-  // 1,024 tokens 74 (4), 55 (8), 60 (12); 2,048 tokens 146 (4), 127 (8), 155 (12), without a mask 169 (4), 198 (8); 4,096 tokens 530 (2), 353 (4), 440 (8); 8,192
-  // tokens 2,087 (1), 1,297 (2), 1,308 (4).  Rows of 64 have twice the workgroups and half the steps: 16 heads, 512 tokens 15 (1), 18 (2).
+  // Of dk and dv, equal ones: as many as run at once, two a compute unit; with a causal mask, where the first keys see the most rows, twice as many if each
+  // keeps work enough to be worth its sums' way through memory in float32 (32 heads, 8 of keys, 128; us with the join, by parts: 2,048 tokens without a mask 455
+  // (1), 169 (4), 198 (8); 8,192 tokens causal 2,087 (1), 1,297 (2), 1,308 (4)).  Rows of 64 have twice the workgroups and half the steps: 16 heads, 512 tokens 15
+  // (1), 18 (2).
   static int dkdv_splits(int64_t groups, int64_t steps, bool causal, int dim) {
     const int a = tile_splits(groups, steps, 512, dim == 64 ? 8 : 4), b = causal ? tile_splits(groups, steps, 1024, 16) : 1;
     return a > b ? a : b;
   }
+  // Where a mask makes the tiles of keys differ, their parts are shared out on the GPU by what they cost, and the longest run first: as many as 1,024 workgroups, and
+  // with documents the order alone where there are more.  us against equal parts, both with the join, 32 heads, 8 of keys, 128: 4,096 packed tokens 129 and
+  // 150; causal 1,024 tokens 51 and 55, 2,048 tokens 109 and 126, 4 x 1,024 tokens 130 and 151, 4,096 tokens 360 and 353; 8,192 tokens (512 tiles) 1,390 and 1,350.
+  int dealt_parts() const { return tile_splits(heads() * key_tiles(), up(rows(), ATTN_TILE), 1024, chosen.dim == 64 ? 16 : 2); }
+  bool dealt() const {
+    const int64_t groups = heads() * key_tiles();
+    if (a->tokens == 0 || a->keys == 0 || key_tiles() > ATTN_SHARE_TILES || c.q_tile_count > ATTN_SHARE_QUERIES) return false;
+    return a->k_documents ? dealt_parts() > 1 || groups > 512 : a->causal && groups < 512 && dealt_parts() > 1;
+  }
+  int64_t key_tiles() const { return up(a->keys, chosen.dkdv_keys); }
 
-  // Rows of a workgroup.  64 of them take half as long as 128 and cost more: taken where the whole launch is no more than the workgroups that run at
-  // once, with a causal mask, where they differ, twice that.
+  // Rows of a workgroup.  64 of them take half as long as 128 but read the keys twice as often: taken where the whole launch is no more than the workgroups
+  // that run at once, with a causal mask, where they differ, twice that.  Rows of 64 elements leave room for a third workgroup with 64 rows, and only dq in large
+  // calls is the better for 128.  us with 64 and 128 rows, 32 heads, 8 of keys, 128, causal, forward and dq: 512 tokens 18 + 21 and 23 + 29, 2,048 tokens 65 + 77 and 71 + 90,
+  // without a mask 106 + 125 and 87 + 114, 4,096 tokens 212 + 258 and 175 + 230; 256 tokens over 2,048 keys 31 and 33 with the join, over 8,192 58 and 55.  64: 4 x 2,048
+  // tokens of 16 heads 72 + 92 and 85 + 102, 8,000 of 32 heads 413 + 532 and 418 + 488.
   bool few_groups() const { return heads() * up(rows(), 128) <= (a->causal ? 512 : 256); }
   int forward_tile() const { return chosen.dim == 64 || (few_groups() && c.tiles < 64) ? 64 : 128; }
   int dq_tile() const { return chosen.dim == 64 ? (heads() * up(rows(), 128) <= 1024 ? 64 : 128) : few_groups() ? 64 : 128; }
@@ -364,8 +379,6 @@ struct Pass {
     }
   }
 
-  int dkdv_parts() const { return dkdv_splits(heads() * up(a->keys, chosen.dkdv_keys), up(rows(), ATTN_TILE), a->causal != 0, chosen.dim); }
-
   void backward(const chm_attention_gradients *g) {
     if (a->batch == 0) return;
     const int64_t B = a->batch, T = a->tokens, K = a->keys;
@@ -377,33 +390,40 @@ struct Pass {
     inputs(g);
     c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
     chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
+    const int64_t tiles = key_tiles();
+    const bool shared = dealt();
+    const int splits = shared ? dealt_parts() : dkdv_splits(heads() * tiles, up(rows(), ATTN_TILE), a->causal != 0, chosen.dim);
+    c.share_tiles = (int32_t)tiles;
+    c.share_keys = chosen.dkdv_keys;
+    c.share_slots = (int32_t)(tiles * splits);
+    c.share_unit = (int32_t)(chosen.dim == 64 ? group_of(a) : 2 * group_of(a));
+    c.share_least = 4;
+    c.share_short = chosen.dim == 64 ? 8 : 64;
     if (T > 0) {
       chosen.dq_rows = dq_tile();
       AttnLaunch l = layout(up(rows(), chosen.dq_rows), 1, 128 / chosen.dq_rows);
-      // Where documents make key tiles differ and not all of them run at once, the longest go first.  Their order is worked out beside dq.
-      const int64_t tiles = up(K, chosen.dkdv_keys);
-      if (a->k_documents && heads() * tiles * dkdv_parts() > 512 && tiles <= ATTN_ORDER_TILES && c.q_tile_count <= ATTN_ORDER_QUERIES) {
-        c.order = (int32_t *)arena.take((uint64_t)(a->batch * tiles) * 4);
-        c.order_groups = a->batch;
-        c.order_tiles = (int32_t)tiles;
-        c.order_keys = chosen.dkdv_keys;
+      if (shared) {                        // worked out beside dq
+        c.shares = (AttnShare *)arena.take((uint64_t)(a->batch * c.share_slots) * sizeof(AttnShare));
+        c.tile_slots = (AttnSlots *)arena.take((uint64_t)(a->batch * c.share_tiles) * sizeof(AttnSlots));
+        c.share_groups = (int32_t)a->batch;
         l.groups = threads((int64_t)l.groups + a->batch, 256);
       }
       if (run && fits) ok = ok && (bf16() ? attn_dq_bf16 : attn_dq_f16)(c, l);
     }
     if (K > 0) {
-      const int64_t tiles = up(K, chosen.dkdv_keys);
-      const AttnLaunch l = layout(tiles, dkdv_parts(), 128 / chosen.dkdv_keys);
-      chosen.dkdv_splits = c.splits;
+      const AttnLaunch l = shared ? layout(c.share_slots, 1, 128 / chosen.dkdv_keys) : layout(tiles, splits, 128 / chosen.dkdv_keys);
+      chosen.dkdv_splits = splits;
+      chosen.dkdv_shared = shared;
       const int64_t words = heads() * K * (c.width4 / 4);
-      if (c.splits > 1) {
-        c.part = (float *)arena.take((uint64_t)(c.splits * words) * 16);
-        c.part2 = (float *)arena.take((uint64_t)(c.splits * words) * 16);
+      if (splits > 1) {
+        const uint64_t bytes = (uint64_t)(heads() * c.share_slots) * (uint64_t)(chosen.dkdv_keys * c.width4) * 4;
+        c.part = (float *)arena.take(bytes);
+        c.part2 = (float *)arena.take(bytes);
       }
       const uint32_t joins = threads(up(words, 256), 256);
       if (!run || !fits) return;
       ok = ok && (bf16() ? attn_dkdv_bf16 : attn_dkdv_f16)(c, l);
-      if (c.splits > 1) {
+      if (splits > 1) {
         if (bf16()) hipLaunchKernelGGL(k_join_backward<CHM_BF16>, dim3(joins), dim3(256), 0, st, c, words);
         else hipLaunchKernelGGL(k_join_backward<CHM_F16>, dim3(joins), dim3(256), 0, st, c, words);
         ok = ok && hipGetLastError() == hipSuccess;
@@ -530,6 +550,7 @@ extern "C" int chm_attention_selection(const chm_attention *a, const chm_attenti
     out->dq_rows = b.chosen.dq_rows;
     out->dkdv_keys = b.chosen.dkdv_keys;
     out->dkdv_splits = b.chosen.dkdv_splits;
+    out->dkdv_shared = b.chosen.dkdv_shared;
   }
   return CHM_OK;
 }

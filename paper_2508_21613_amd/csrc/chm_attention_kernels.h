@@ -82,6 +82,15 @@ template <class T> __device__ __forceinline__ s8 pack8(const f16 &v, int from) {
 // row of a 32 x 32 result in register r, less 4 h
 __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r >> 2); }
 
+// The call's description as the kernel's argument holds it, read anew: what only the end of a kernel asks for is otherwise kept in scalar registers from
+// its beginning, which then lack in its loop (dk and dv: 45 reads of saved ones a step).
+typedef __attribute__((address_space(4))) const AttnCall Argument;
+__device__ __forceinline__ Argument *argument() {
+  Argument *c = (Argument *)__builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(c));
+  return c;
+}
+
 // which rows, of which sequence and key head, a workgroup works on: heads_abreast heads side by side (one a die where there are 8), the last rows first,
 // which see the most
 struct Place { int b, h, hb, tile, split; };
@@ -906,35 +915,70 @@ struct Deltas {
   }
 };
 
-// The order of a sequence's tiles of keys for dk and dv: by how many tiles of queries see them.  A workgroup of its own, which is done long before the others.
-enum { ORDER_COSTS = ATTN_ORDER_QUERIES * 16, ORDER_BYTES = ORDER_COSTS + ATTN_ORDER_TILES * 4 };
-__device__ __forceinline__ void order_keys(const AttnCall &c, int b, lds_char *lds) {
+// How the sums of a sequence's tiles of keys are shared out for dk and dv: each tile by how many blocks of rows see it, in parts as equal as their number
+// allows, the longest first.  Half of the slots are used where that leaves short parts: what is saved is their sums' way through memory (4,096 packed
+// tokens, 32 heads of 128, 8 of keys: 512 parts 124 + 12 us, 1,024 parts 122 + 25), while longer ones fill the GPU better in twice as many (4,096 tokens in one
+// document 400 + 14, 347 + 24).  A workgroup of its own, which is done long before the others.
+enum { SHARE_COSTS = ATTN_SHARE_QUERIES * 16, SHARE_BYTES = SHARE_COSTS + ATTN_SHARE_TILES * 4 + 16 };
+__device__ __forceinline__ void share_keys(const AttnCall &c, int b, lds_char *lds) {
   __attribute__((address_space(3))) i4 *queries = (__attribute__((address_space(3))) i4 *)lds;
-  __attribute__((address_space(3))) int *cost = (__attribute__((address_space(3))) int *)(lds + ORDER_COSTS);
-  const int n = c.order_tiles, each = c.order_keys / ATTN_TILE;
-  for (int i = threadIdx.x; i < c.q_tile_count; i += 256) queries[i] = *(const i4 *)&c.q_tiles[(int64_t)b * c.q_tile_count + i];
+  __attribute__((address_space(3))) int *cost = (__attribute__((address_space(3))) int *)(lds + SHARE_COSTS), *total = cost + ATTN_SHARE_TILES;
+  const int n = c.share_tiles, each = c.share_keys / ATTN_TILE;
+  if (c.k_words)
+    for (int i = threadIdx.x; i < c.q_tile_count; i += 256) queries[i] = *(const i4 *)&c.q_tiles[(int64_t)b * c.q_tile_count + i];
   __syncthreads();
   for (int i = threadIdx.x; i < n; i += 256) {
-    const int k0 = i * c.order_keys, k1 = k0 + c.order_keys - 1 < c.keys ? k0 + c.order_keys - 1 : c.keys - 1;
+    const int k0 = i * c.share_keys, k1 = k0 + c.share_keys - 1 < c.keys ? k0 + c.share_keys - 1 : c.keys - 1;
     Range k{INT32_MAX, -1, 0};
-    for (int j = i * each; j < (i + 1) * each && j < c.tiles; ++j) {
-      const AttnTile x = c.k_tiles[(int64_t)b * c.tiles + j];
-      k = join(k, x);
-      k.flags |= x.flags & ATTN_SOME_PREFIX;
-    }
+    if (c.k_words)
+      for (int j = i * each; j < (i + 1) * each && j < c.tiles; ++j) {
+        const AttnTile x = c.k_tiles[(int64_t)b * c.tiles + j];
+        k = join(k, x);
+        k.flags |= x.flags & ATTN_SOME_PREFIX;
+      }
     int seen = 0;
     for (int j = 0; j < c.q_tile_count; ++j) {
-      const i4 x = queries[j];
+      const i4 x = c.k_words ? queries[j] : i4{};
       seen += sees(c, j * ATTN_TILE + c.offset, j * ATTN_TILE + ATTN_TILE - 1 + c.offset, Range{x[0], x[1], x[2]}, k0, k1, k).some;
     }
-    cost[i] = seen;
+    cost[i] = seen < 1 ? 1 : seen * c.share_unit;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < n; i += 256) {
-    int before = 0;
-    for (int j = 0; j < n; ++j) before += cost[j] > cost[i] || (cost[j] == cost[i] && j < i);
-    c.order[(int64_t)b * n + before] = i;
+  int64_t all = 0;
+  for (int j = 0; j < n; ++j) all += cost[j];
+  const int half = c.share_slots / 2 > n ? c.share_slots / 2 : n, limit = all <= half * c.share_short ? half : c.share_slots;
+  // the least length of a part with which there are enough of them
+  int low = c.share_least, high = c.q_tile_count * c.share_unit > c.share_least ? c.q_tile_count * c.share_unit : c.share_least;
+  while (low < high) {
+    const int length = (low + high) / 2;
+    __syncthreads();
+    if (threadIdx.x == 0) *total = 0;
+    __syncthreads();
+    int parts = 0;
+    for (int i = threadIdx.x; i < n; i += 256) parts += (cost[i] + length - 1) / length;
+    __hip_atomic_fetch_add(total, parts, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WORKGROUP);
+    __syncthreads();
+    if (*total <= limit) high = length;
+    else low = length + 1;
   }
+  __syncthreads();
+  const auto parts_of = [&](int cost) { return (cost + low - 1) / low; };
+  const auto length_of = [&](int cost) { return (cost + parts_of(cost) - 1) / parts_of(cost); };
+  AttnShare *shares = c.shares + (int64_t)b * c.share_slots;
+  int used = 0;
+  for (int j = 0; j < n; ++j) used += parts_of(cost[j]);
+  for (int i = threadIdx.x; i < n; i += 256) {
+    const int mine = cost[i], parts = parts_of(mine), length = length_of(mine);
+    int before = 0, slot = 0;
+    for (int j = 0; j < n; ++j) {
+      const int far = length_of(cost[j]), p = parts_of(cost[j]);
+      before += far > length || (far == length && j < i) ? p : 0;
+      slot += j < i ? p : 0;
+    }
+    for (int k = 0; k < parts; ++k) shares[before + k] = AttnShare{i, k, parts, slot + k};
+    c.tile_slots[(int64_t)b * n + i] = AttnSlots{slot, parts};
+  }
+  for (int i = used + threadIdx.x; i < c.share_slots; i += 256) shares[i] = AttnShare{-1, 0, 1, 0};
 }
 
 // PARTS as in k_forward
@@ -944,14 +988,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   constexpr int WAVES = 4, BLOCKS = WAVES / PARTS, N = D / 32 / PARTS;
   typedef TileFeed<D, WAVES> Feed;
   constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 4096 : 0;
-  static_assert((int)ORDER_BYTES <= (int)Feed::BYTES, "shared memory holds what an order is worked out from");
+  static_assert((int)SHARE_BYTES <= (int)Feed::BYTES, "shared memory holds what the shares are worked out from");
   __shared__ float deltas[BLOCKS][32];
   __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > TURN + MEET ? Feed::BYTES : TURN + MEET];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
-  if ((int)blockIdx.x < c.order_groups) return order_keys(c, blockIdx.x, lds);
-  const Place p = place_of(c, blockIdx.x - c.order_groups, true);
+  if ((int)blockIdx.x < c.share_groups) return share_keys(c, blockIdx.x, lds);
+  const Place p = place_of(c, blockIdx.x - c.share_groups, true);
   const int row0 = p.tile * (BLOCKS * 32), wave_row = row0 + block * 32, h4 = (lane >> 5) * 4;
   // dy comes by the second slot, a wavefront's rows to its own part
   const int mine = Feed::SLOT + wave * Shape<D>::bytes(32);
@@ -1150,9 +1194,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   lds_char *lds = (lds_char *)shared, *values = lds + VALUES;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), part = wave / BLOCKS, block = wave % BLOCKS;
-  Place p = place_of(c, blockIdx.x, false);
-  if (c.order) p.tile = c.order[p.b * c.tiles_here + p.tile];
-  const int key0 = p.tile * KEYS, wave_key = key0 + block * 32;
+  const Place p = place_of(c, blockIdx.x, false);
+  AttnShare share{p.tile, p.split, c.splits, p.tile * c.splits + p.split};
+  if (c.shares) share = c.shares[(int64_t)p.b * c.share_slots + p.tile];
+  if (share.tile < 0) return;
+  const int key0 = share.tile * KEYS, wave_key = key0 + block * 32;
   const int h4 = (lane >> 5) * 4;
   s8 k[D / 16];
   uint32_t word = 0;
@@ -1185,7 +1231,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     first = f < blocks ? (int)f : blocks;
   }
   RowWalk<KEYS, STEP> walk;
-  walk.start(c, p, key0, wave_key, word, part * 32, first + p.split, c.splits, blocks, lane);
+  walk.start(c, p, key0, wave_key, word, part * 32, first + share.part, share.parts, blocks, lane);
   if (lane < 32) words[wave][lane] = word;  // for this wavefront alone
   f16 dk[D / 32], dv[D / 32];
 #pragma unroll
@@ -1286,25 +1332,32 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   arrived();                                // the values, where no block was visited; and nobody reads shared memory any more
   lds_char *own = lds + wave * turn_bytes(N);
   const int d0 = part * (N * 32);
+  Argument *end = argument();
+  const int width = end->width, keys = end->keys;
+  const float scale = end->scale;
   const auto store = [&](const f16 (&k)[N], const f16 (&v)[N]) {
-    if (c.splits > 1) {
-      const int64_t at = ((int64_t)p.split * c.batch * c.kv_heads + p.hb) * c.keys + wave_key;
+    if (share.parts > 1) {
+      const int width4 = end->width4;
+      const int64_t at = ((int64_t)p.hb * end->share_slots + share.slot) * KEYS + block * 32;
       const auto put = [&](float *out, int row, int d, f4 a, f4 b) {
-        if (wave_key + row >= c.keys) return;
-        out += (at + row) * c.width4 + d;
-        if (d < c.width4) *(f4 *)out = a;
-        if (d + 4 < c.width4) *(f4 *)(out + 4) = b;
+        if (wave_key + row >= keys) return;
+        out += (at + row) * width4 + d;
+        if (d < width4) *(f4 *)out = a;
+        if (d + 4 < width4) *(f4 *)(out + 4) = b;
       };
-      by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.part, row, d, a, b); });
-      by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.part2, row, d, a, b); });
+      float *part = end->part, *part2 = end->part2;
+      by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(part, row, d, a, b); });
+      by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(part2, row, d, a, b); });
       return;
     }
-    const auto put = [&](const AttnOutput &o, int row, int d, f4 a, f4 b) {
+    const auto put = [&](uint16_t *out, int64_t token, int row, int d, f4 a, f4 b) {
       const int j = wave_key + row;
-      if (j < c.keys) store8<T>(o.p + p.b * o.batch + j * o.token + p.h * o.head, d, c.width, a, b);
+      if (j < keys) store8<T>(out + j * token, d, width, a, b);
     };
-    by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.dk, row, d, a, b); });
-    by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(c.dv, row, d, a, b); });
+    uint16_t *dk = end->dk.p + p.b * end->dk.batch + p.h * end->dk.head, *dv = end->dv.p + p.b * end->dv.batch + p.h * end->dv.head;
+    const int64_t dk_token = end->dk.token, dv_token = end->dv.token;
+    by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(dk, dk_token, row, d, a, b); });
+    by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(dv, dv_token, row, d, a, b); });
   };
   if constexpr (PARTS == 2) {
     f16 sk[N], sv[N];
@@ -1312,12 +1365,12 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     give<N>(meet + wave * (N * 8192), dk, sk, part == 1, lane);
     give<N>(meet + wave * (N * 8192) + N * 4096, dv, sv, part == 1, lane);
     __syncthreads();
-    take<N>(meet + (wave ^ BLOCKS) * (N * 8192), sk, c.scale, c.scale, lane);
+    take<N>(meet + (wave ^ BLOCKS) * (N * 8192), sk, scale, scale, lane);
     take<N>(meet + (wave ^ BLOCKS) * (N * 8192) + N * 4096, sv, 1.f, 1.f, lane);
     store(sk, sv);
   } else {
 #pragma unroll
-    for (int d = 0; d < N; ++d) dk[d] *= c.scale;
+    for (int d = 0; d < N; ++d) dk[d] *= scale;
     store(dk, dv);
   }
 #endif

@@ -244,6 +244,24 @@ def test_documents(ops, B, T, count, padding, which, dtype):
     assert all(torch.equal(got[n], got32[n]) for n in got)
 
 
+@pytest.mark.parametrize("B,T,K,H,Hk,d,causal,count", [
+    (1, 300, 1500, 2, 1, 64, True, 0), (1, 300, 1500, 2, 1, 128, True, 0), (9, 130, 130, 32, 32, 128, True, 0), (9, 130, 130, 32, 32, 128, True, 3),
+    (17, 130, 130, 32, 32, 64, True, 0), (17, 130, 130, 32, 32, 64, False, 3), (1, 700, 700, 6, 2, 128, True, 0), (1, 700, 700, 6, 2, 128, False, 0),
+    (1, 700, 700, 6, 2, 128, True, 5), (1, 1200, 1200, 8, 1, 64, True, 0), (1, 1200, 1200, 8, 1, 64, True, 4), (8, 1024, 1024, 16, 8, 128, True, 0),
+    (2, 900, 900, 4, 2, 128, False, 12)])
+def test_however_the_work_is_shared(ops, B, T, K, H, Hk, d, causal, count):
+    """calls of every rule by which rows and keys are given to workgroups, in parts or not, dealt by the mask or not"""
+    x = inputs(T + d, B, T, K, H, Hk, d, torch.bfloat16)
+    kw = dict(causal=causal, cap=8.0)
+    if count:
+        kw["documents"] = documents_of(B + d, B, T, count, T // 9)
+        if causal and B == 1:
+            kw["prefix"] = torch.rand((B, T), generator=gen(3), device="cuda") < 0.2
+    got, _ = compare(ops, x, **kw)
+    again = both(ops, *x, **kw)
+    assert all(torch.equal(got[n], again[n]) for n in got)
+
+
 def test_documents_in_any_order(ops):
     """numbers that alternate, repeat far apart, are as large as they may be, or mean none"""
     T = 300

@@ -69,7 +69,7 @@ def test_sizes():
 
 def test_which_kernels():
     assert _kernels(_attention(tokens=1, keys=32768, heads=32, kv_heads=8, dim=128, batch=8))[1] == dict(
-        few=1, dim=128, packed=0, forward_rows=32, dq_rows=0, dkdv_keys=0, forward_splits=4, dkdv_splits=1)
+        few=1, dim=128, packed=0, forward_rows=32, dq_rows=0, dkdv_keys=0, forward_splits=4, dkdv_splits=1, dkdv_shared=0)
     a = _attention(tokens=8192, keys=8192, heads=32, kv_heads=8, dim=128, batch=1)
     k = _kernels(a, _gradients(a))[1]
     assert (k["few"], k["packed"], k["forward_rows"], k["dq_rows"], k["dkdv_keys"], k["forward_splits"], k["dkdv_splits"]) == (0, 0, 128, 128, 128, 1, 2)
@@ -80,6 +80,28 @@ def test_which_kernels():
     # tokens so far apart that 64 of them are beyond offsets of 31 bits
     assert _kernels(_attention(batch=1, v_stride=(0, 1 << 25, 64)))[1]["packed"] == 4
     assert _kernels(_attention(batch=1, v_stride=(0, 1 << 24, 64)))[1]["packed"] == 0
+
+
+@pytest.mark.parametrize("kw,want", [
+    # (rows of the forward pass and of dq, keys, parts of the forward pass and of dk and dv, dealt)
+    (dict(batch=1, tokens=300, keys=1500, heads=2, kv_heads=1, dim=64), (64, 64, 64, 3, 1, 0)),
+    (dict(batch=1, tokens=300, keys=1500, heads=2, kv_heads=1, dim=128), (64, 64, 128, 3, 5, 1)),
+    (dict(batch=9, tokens=130, keys=130, heads=32, kv_heads=32, dim=128), (128, 128, 128, 1, 1, 0)),
+    (dict(batch=9, tokens=130, keys=130, heads=32, kv_heads=32, dim=128, documents=True), (128, 128, 128, 1, 1, 1)),
+    (dict(batch=17, tokens=130, keys=130, heads=32, kv_heads=32, dim=64), (64, 128, 64, 1, 1, 0)),
+    (dict(batch=17, tokens=130, keys=130, heads=32, kv_heads=32, dim=64, documents=True), (64, 128, 64, 1, 1, 1)),
+    (dict(batch=1, tokens=700, keys=700, heads=6, kv_heads=2, dim=128), (64, 64, 128, 1, 16, 1)),
+    (dict(batch=1, tokens=700, keys=700, heads=6, kv_heads=2, dim=128, causal=0), (64, 64, 128, 1, 8, 0)),
+    (dict(batch=1, tokens=1200, keys=1200, heads=8, kv_heads=1, dim=64), (64, 64, 64, 2, 9, 1)),
+    (dict(batch=8, tokens=1024, keys=1024, heads=16, kv_heads=8, dim=128), (128, 128, 128, 1, 2, 0)),
+    (dict(batch=1, tokens=100, keys=131073, heads=1, kv_heads=1, dim=128), (128, 64, 128, 16, 1, 0))])
+def test_how_work_is_shared(kw, want):
+    documents = kw.pop("documents", False)
+    a = _attention(**kw)
+    if documents:
+        a.index_bits, a.q_documents, a.k_documents, a.ld_q_documents, a.ld_k_documents = 32, BASE >> 1, BASE >> 1, a.tokens, a.keys
+    k = _kernels(a, _gradients(a))[1]
+    assert tuple(k[n] for n in ("forward_rows", "dq_rows", "dkdv_keys", "forward_splits", "dkdv_splits", "dkdv_shared")) == want
 
 
 @pytest.mark.parametrize("kw", [

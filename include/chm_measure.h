@@ -71,6 +71,7 @@ typedef struct {
   int32_t forward_rows, dq_rows, dkdv_keys;       /* of a workgroup; 0: not run */
   int32_t forward_splits, dkdv_splits;            /* parts of the sums */
   int32_t dkdv_shared;           /* 1: those of dk and dv are dealt to the tiles of keys by what they cost; splits: as many on average at most */
+  int32_t fine;                  /* 1: the gradients' products take p and ds with what their rounding took */
 } chm_attention_kernels;
 int chm_attention_selection(const chm_attention *a, const chm_attention_gradients *g, chm_attention_kernels *out);
 

@@ -144,7 +144,7 @@ class AttentionGradients(C.Structure):
 
 
 class AttentionKernels(C.Structure):
-    _fields_ = [(n, C.c_int32) for n in ("few", "dim", "packed", "forward_rows", "dq_rows", "dkdv_keys", "forward_splits", "dkdv_splits", "dkdv_shared")]
+    _fields_ = [(n, C.c_int32) for n in ("few", "dim", "packed", "forward_rows", "dq_rows", "dkdv_keys", "forward_splits", "dkdv_splits", "dkdv_shared", "fine")]
 
 
 class ChmError(RuntimeError):

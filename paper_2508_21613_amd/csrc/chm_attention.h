@@ -76,8 +76,8 @@ struct AttnCall {
 };
 
 enum { ATTN_SHARE_TILES = 1024, ATTN_SHARE_QUERIES = 1024 };        // most tiles of keys and of queries that are shared out on the GPU
-// Kernels of a pass; dim: 64 or 128; parts: wavefronts that share a sum, 1 or 2.  false: HIP failed.
-struct AttnLaunch { int32_t dim, parts; uint32_t groups; void *stream; };
+// Kernels of a pass; dim: 64 or 128; parts: wavefronts that share a sum, 1 or 2; fine: gradients by twice the products.  false: HIP failed.
+struct AttnLaunch { int32_t dim, parts, fine; uint32_t groups; void *stream; };
 bool attn_forward_bf16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_forward_f16(const AttnCall &c, const AttnLaunch &l, bool few);
 bool attn_dq_bf16(const AttnCall &c, const AttnLaunch &l);

@@ -194,7 +194,7 @@ struct Pass {
   bool run, ok = true;
   bool fits = true;                        // every launch's threads can be counted in 32 bits
   AttnCall c{};
-  chm_attention_kernels chosen{0, 0, 0, 0, 0, 0, 1, 1, 0};
+  chm_attention_kernels chosen{0, 0, 0, 0, 0, 0, 1, 1, 0, 0};
 
   Pass(const chm_attention *a_, char *base, hipStream_t st_, bool run_) : a(a_), arena{base}, st(st_), run(run_) {
     const int64_t G = group_of(a), d8 = up(a->dim, 8) * 8;
@@ -248,7 +248,7 @@ struct Pass {
     c.splits = splits;
     c.by_tiles = divide_by(tiles);
     c.by_splits = divide_by(splits);
-    return AttnLaunch{chosen.dim, parts, threads(heads() * tiles * splits, 256), st};
+    return AttnLaunch{chosen.dim, parts, chosen.fine, threads(heads() * tiles * splits, 256), st};
   }
 
   // Inputs as the tiles take them: 16-byte rows, and 64 of them within offsets of 31 bits
@@ -388,6 +388,7 @@ struct Pass {
     c.dk = output(g->dk, g->dk_stride, B, K, a->kv_heads);
     c.dv = output(g->dv, g->dv_stride, B, K, a->kv_heads);
     inputs(g);
+    chosen.fine = heads() * up(rows(), 64) <= 128;      // then dq's workgroups have 64 rows, one for every other compute unit at most
     c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
     chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
     const int64_t tiles = key_tiles();
@@ -551,6 +552,7 @@ extern "C" int chm_attention_selection(const chm_attention *a, const chm_attenti
     out->dkdv_keys = b.chosen.dkdv_keys;
     out->dkdv_splits = b.chosen.dkdv_splits;
     out->dkdv_shared = b.chosen.dkdv_shared;
+    out->fine = b.chosen.fine;
   }
   return CHM_OK;
 }

@@ -79,6 +79,13 @@ template <class T> __device__ __forceinline__ s8 pack8(const f16 &v, int from) {
   for (int i = 0; i < 8; ++i) r[i] = (short)T::down(v[from + i]);
   return r;
 }
+// what pack8 takes from them
+template <class T> __device__ __forceinline__ s8 pack8_low(const f16 &v, const s8 &high, int from) {
+  s8 r;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) r[i] = (short)T::down(v[from + i] - T::up((uint16_t)high[i]));
+  return r;
+}
 // row of a 32 x 32 result in register r, less 4 h
 __device__ __forceinline__ constexpr int row_of(int r) { return (r & 3) + 8 * (r >> 2); }
 
@@ -981,8 +988,11 @@ __device__ __forceinline__ void share_keys(const AttnCall &c, int b, lds_char *l
   for (int i = used + threadIdx.x; i < c.share_slots; i += 256) shares[i] = AttnShare{-1, 0, 1, 0};
 }
 
-// PARTS as in k_forward
-template <class T, int D, int CAP, int SLOPE, int PARTS>
+// PARTS as in k_forward.  FINE: ds enters its product with what its rounding took, a second product; so in dk and dv, and p as well.  Otherwise gradients are off by 1.4 times
+// what their own rounding makes, with it by hardly more than that.  Taken where a call leaves most compute units idle and sums are too few for
+// errors to be alike: 17 tokens, 4 heads of 64, dq + dk and dv 8.5 + 7.6 us without, 8.8 + 8.2 with; 2 x 515 tokens, 6 heads of 72 19.0 + 21.2, 19.1 + 23.1; 512 tokens, 32
+// heads of 128, 8 of keys (256 workgroups: not taken) 20.0 + 22.8, 21.8 + 29.0.
+template <class T, int D, int CAP, int SLOPE, int PARTS, int FINE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 3 : 2))) k_dq(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WAVES = 4, BLOCKS = WAVES / PARTS, N = D / 32 / PARTS;
@@ -1074,9 +1084,15 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       if (now.masked()) seen_keys(c, now, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
-      for (int k = 0; k < 2; ++k)
+      for (int k = 0; k < 2; ++k) {
+        const s8 low = FINE ? pack8_low<T>(dp, ds[k], k * 8) : s8{};
 #pragma unroll
-        for (int d = 0; d < D / 32; ++d) dq[d] = T::mfma(column_fragment<D>(keys, b * 32 + k * 16, d, lane), ds[k], dq[d]);
+        for (int d = 0; d < D / 32; ++d) {
+          const s8 key = column_fragment<D>(keys, b * 32 + k * 16, d, lane);
+          dq[d] = T::mfma(key, ds[k], dq[d]);
+          if (FINE) dq[d] = T::mfma(key, low, dq[d]);
+        }
+      }
     }
   }
   arrived();
@@ -1178,7 +1194,7 @@ struct RowWalk {
 // values stay in shared memory: they are read from there a block of 32 rows, as the queries and dy are.
 //
 // PARTS = 2: a workgroup has 64 keys and goes through 64 rows at a time, each wavefront through half of them.  Rows of 128 elements have no room for that.
-template <class T, int D, int CAP, int SLOPE, int PARTS>
+template <class T, int D, int CAP, int SLOPE, int PARTS, int FINE>
 __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 && PARTS == 2 ? 3 : 2))) k_dkdv(const AttnCall c) {
 #ifdef __HIP_DEVICE_COMPILE__
   constexpr int WAVES = 4, NT = 64 * WAVES, BLOCKS = WAVES / PARTS, KEYS = BLOCKS * 32, STEP = PARTS * 32, N = D / 32 / PARTS;
@@ -1322,10 +1338,16 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
       const s8 pp = pack8<T>(s, i * 8), ds = pack8<T>(dp, i * 8);
+      const s8 p_low = FINE ? pack8_low<T>(s, pp, i * 8) : s8{}, ds_low = FINE ? pack8_low<T>(dp, ds, i * 8) : s8{};
 #pragma unroll
       for (int d = 0; d < D / 32; ++d) {
-        dv[d] = T::mfma(column_fragment<D>(dys, part * 32 + i * 16, d, lane), pp, dv[d]);
-        dk[d] = T::mfma(column_fragment<D>(queries, part * 32 + i * 16, d, lane), ds, dk[d]);
+        const s8 dy = column_fragment<D>(dys, part * 32 + i * 16, d, lane), query = column_fragment<D>(queries, part * 32 + i * 16, d, lane);
+        dv[d] = T::mfma(dy, pp, dv[d]);
+        dk[d] = T::mfma(query, ds, dk[d]);
+        if (FINE) {
+          dv[d] = T::mfma(dy, p_low, dv[d]);
+          dk[d] = T::mfma(query, ds_low, dk[d]);
+        }
       }
     }
   }
@@ -1378,22 +1400,30 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 
 // ---------------------------------------------------------------------------------------------- launches
 enum { FORWARD, FEW, DQ, DKDV };
-template <class T, int WHAT, int D, int CAP, int SLOPE, int PARTS>
+template <class T, int WHAT, int D, int CAP, int SLOPE, int PARTS, int FINE>
 bool launch(const AttnCall &c, const AttnLaunch &l) {
   hipStream_t st = (hipStream_t)l.stream;
   const dim3 grid(l.groups), block(256);
   if constexpr (WHAT == FORWARD) hipLaunchKernelGGL((k_forward<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
   else if constexpr (WHAT == FEW) hipLaunchKernelGGL((k_forward_few<T, D, CAP, SLOPE>), grid, block, 0, st, c);
-  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
-  else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE, PARTS>), grid, block, 0, st, c);
+  else if constexpr (WHAT == DQ) hipLaunchKernelGGL((k_dq<T, D, CAP, SLOPE, PARTS, FINE>), grid, block, 0, st, c);
+  else hipLaunchKernelGGL((k_dkdv<T, D, CAP, SLOPE, PARTS, FINE>), grid, block, 0, st, c);
   return hipGetLastError() == hipSuccess;
 }
 template <class T, int WHAT, int D, int CAP, int SLOPE>
 bool launch_parts(const AttnCall &c, const AttnLaunch &l) {
   constexpr bool two = D == 64 ? WHAT != FEW : WHAT == FORWARD || WHAT == DQ, one = D == 128 || WHAT == DQ || WHAT == FEW;      // those that are chosen anywhere
-  if constexpr (two)
-    if (!one || l.parts == 2) return launch<T, WHAT, D, CAP, SLOPE, 2>(c, l);
-  if constexpr (one) return launch<T, WHAT, D, CAP, SLOPE, 1>(c, l);
+  constexpr bool fine = WHAT == DQ || WHAT == DKDV;
+  if constexpr (two) {
+    if constexpr (fine)
+      if (l.fine) return launch<T, WHAT, D, CAP, SLOPE, 2, 1>(c, l);
+    if (!one || l.parts == 2) return launch<T, WHAT, D, CAP, SLOPE, 2, 0>(c, l);
+  }
+  if constexpr (one) {
+    if constexpr (fine && !two)
+      if (l.fine) return launch<T, WHAT, D, CAP, SLOPE, 1, 1>(c, l);
+    return launch<T, WHAT, D, CAP, SLOPE, 1, 0>(c, l);
+  }
   return false;
 }
 template <class T, int WHAT, int D>

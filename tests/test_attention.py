@@ -71,8 +71,9 @@ def clean(t, documents, which):
     return torch.where(((ids >= 0) & (ids < 2 ** 31 - 1))[:, :, None, None], t, 0.0)
 
 
-def formula(q, k, v, dy=None, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None):
-    """{name: (value, variance of the error)} in 64 bits, one key head after the other"""
+def formula(q, k, v, dy=None, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None, kept=1.0):
+    """{name: (value, variance of the error)} in 64 bits, one key head after the other.  kept: share of their roundings that p and ds have in the gradients'
+    products"""
     dtype, (B, T, H, d), (K, Hk) = q.dtype, q.shape, k.shape[1:3]
     u, tiny, G = U[dtype], TINY[dtype], H // Hk
     scale = d ** -0.5 if scale is None else scale
@@ -119,8 +120,9 @@ def formula(q, k, v, dy=None, scale=None, cap=0.0, slopes=None, causal=True, doc
             vdelta = ((gy * gy) * (vy + (u * y).clamp(min=tiny) ** 2 / 3)).sum(1, keepdim=True) + ACC ** 2 * d * ((gy * y) ** 2).sum(1, keepdim=True)
             ds = p * (dp - delta) * dz
             vds = (p * dz) ** 2 * vdp + (ds * e) ** 2 + (p * (dp - delta) * more) ** 2 + (8 * ACC * p * dp * dz) ** 2 + (
-                (u * ds) ** 2 + torch.where(see[b], tiny, 0.0) ** 2) / 3
+                (kept * u * ds) ** 2 + torch.where(see[b], tiny, 0.0) ** 2) / 3
             pz = p * dz
+            vp = ((kept * u * p) ** 2 + torch.where(see[b], tiny, 0.0) ** 2) / 3
             dq, dk, dv = scale * ds @ kk, scale * ds.T @ qq, p.T @ gy
             put("dq", b, h, dq, scale ** 2 * (vds @ (kk * kk) + vdelta * (pz @ kk) ** 2 + ACC ** 2 * K * ((ds * ds) @ (kk * kk))) + (8 * ACC * dq) ** 2)
             put("dk", b, h // G, dk, scale ** 2 * ((vds + pz * pz * vdelta).T @ (qq * qq) + ACC ** 2 * T * G * ((ds * ds).T @ (qq * qq))) + (8 * ACC * dk) ** 2)
@@ -542,3 +544,14 @@ def test_offsets_beyond_32_bits(ops):
     wide = k.view(-1)[:(K // 8) * Hk * d * 8].view(1, 8, -1)[:, :, :Hk * d].unflatten(2, (Hk, d))          # 8 tokens 300 million elements apart
     y = ops.attention_forward(wide, wide, wide)
     check("y", y[:, :, :4], formula(wide[:, :, :4], wide[:, :, :4], wide[:, :, :4])["y"])
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("T,H,Hk,d", [(2, 1, 1, 64), (17, 4, 4, 64), (40, 6, 2, 128), (130, 4, 1, 80)])
+def test_gradients_of_small_calls(ops, T, H, Hk, d, dtype):
+    """there ds and p enter their products with what their rounding took: of the tensors' type's roundings are left the gradients' own and that of the forward pass's
+    weights, which y brings into delta"""
+    x = inputs(T, 1, T, T, H, Hk, d, dtype)
+    got, want = both(ops, *x, cap=20.0), formula(*x, cap=20.0, kept=U[dtype])
+    for name in NAMES:
+        check(name, got[name], want[name])

@@ -69,7 +69,7 @@ def test_sizes():
 
 def test_which_kernels():
     assert _kernels(_attention(tokens=1, keys=32768, heads=32, kv_heads=8, dim=128, batch=8))[1] == dict(
-        few=1, dim=128, packed=0, forward_rows=32, dq_rows=0, dkdv_keys=0, forward_splits=4, dkdv_splits=1, dkdv_shared=0)
+        few=1, dim=128, packed=0, forward_rows=32, dq_rows=0, dkdv_keys=0, forward_splits=4, dkdv_splits=1, dkdv_shared=0, fine=0)
     a = _attention(tokens=8192, keys=8192, heads=32, kv_heads=8, dim=128, batch=1)
     k = _kernels(a, _gradients(a))[1]
     assert (k["few"], k["packed"], k["forward_rows"], k["dq_rows"], k["dkdv_keys"], k["forward_splits"], k["dkdv_splits"]) == (0, 0, 128, 128, 128, 1, 2)
@@ -80,6 +80,14 @@ def test_which_kernels():
     # tokens so far apart that 64 of them are beyond offsets of 31 bits
     assert _kernels(_attention(batch=1, v_stride=(0, 1 << 25, 64)))[1]["packed"] == 4
     assert _kernels(_attention(batch=1, v_stride=(0, 1 << 24, 64)))[1]["packed"] == 0
+
+
+def test_gradients_by_twice_the_products():
+    for kw, want in ((dict(batch=1, tokens=17, keys=17, heads=4, kv_heads=4, dim=64), 1), (dict(batch=1, tokens=256, keys=256, heads=32, kv_heads=8, dim=128), 1),
+                     (dict(batch=1, tokens=257, keys=257, heads=32, kv_heads=8, dim=128), 0), (dict(batch=1, tokens=1, keys=100000, heads=32, kv_heads=8, dim=64, causal=0), 1)):
+        a = _attention(**kw)
+        k = _kernels(a, _gradients(a))[1]
+        assert k["fine"] == want and (k["dq_rows"] == 64 or not want)
 
 
 @pytest.mark.parametrize("kw,want", [

@@ -304,7 +304,9 @@ struct Pass {
     }
   }
 
-  // Parts of the keys of the kernel for few rows: as many workgroups as run at once (1 a compute unit, 2 with rows of 64), in whole rounds
+  // Parts of the keys of the kernel for few rows: as many workgroups as run at once (1 a compute unit, 2 with rows of 64), in whole rounds.  us by parts, 32
+  // heads of 128, 8 of keys: 8 answers of 32,768 keys 426 (1), 237 (2), 181 (4), 179 (8); one of 65,536 629 (1), 177 (4), 92 (8), 47 (32); 4 of 4,096 46 (1), 18 (4), 16
+  // (8); 64 answers of 2,048 keys, 16 heads of 64 104 (1), 106 (2), 128 (8).
   static int few_splits(int64_t heads, int64_t tiles, int dim) {
     const int64_t slots = dim == 64 ? 512 : 256;
     int best = 1;
@@ -316,6 +318,7 @@ struct Pass {
     return best;
   }
   // Parts of the sums of a tile kernel with `groups` workgroups, each of which goes through `steps` of 64: as many as fill `slots`, of `least` steps and more
+  // (forward, 512 workgroups run at once, three a compute unit with rows of 64: 768)
   static int tile_splits(int64_t groups, int64_t steps, int64_t slots, int64_t least) {
     int64_t s = slots / (groups < 1 ? 1 : groups);
     if (s > steps / least) s = steps / least;

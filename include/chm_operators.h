@@ -129,7 +129,7 @@ typedef struct {
   int64_t dim;                                /* 1 to 128 */
   const void *q, *k, *v;
   int64_t q_stride[3], k_stride[3], v_stride[3];  /* elements from one sequence, token, head to the next; >= 0 */
-  float scale, cap;                           /* scale finite and > 0; cap finite and >= 0, 0: none */
+  float scale, cap;                           /* scale > 0, cap finite and >= 0, 0: none; scale and scale / cap up to 1e30 */
   const float *slopes;                        /* [heads], nullable */
   int32_t index_bits;                         /* of the documents: 32 or 64 (signed) */
   const void *q_documents, *k_documents;      /* [batch, tokens], [batch, keys], rows of ld; both or neither */

@@ -25,7 +25,7 @@ constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles ar
 
 // What the kernel of dq leaves to that of dk and dv about 32 rows, one value after the other (rows behind the last see nothing)
 struct AttnRows {
-  float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap; +inf: the row sees nothing
+  float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap up to 256; +inf: the row sees nothing
   float delta[32];                         // dy . y; with a cap four times that
   int32_t last[32];                        // last key that a causal mask leaves (no mask: all)
   uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
@@ -51,7 +51,7 @@ struct AttnCall {
   int32_t even_group;                      // 32 is a multiple of the group
   float scale;                             // of the gradients dq and dk
   float to2;                               // score in powers of two: scale * log2(e)
-  float tanh2, cap2;                       // 2 scale / cap * log2(e); cap * log2(e)
+  float tanh2, cap2, to_cap;               // 2 scale / cap * log2(e); cap * log2(e); scale / cap
   const float *slopes;                     // [kv_heads * group], or null
   const uint32_t *q_words, *k_words;       // [batch][whole tiles], or null: no documents and no prefix
   const AttnTile *q_tiles, *k_tiles;       // [batch][tiles]

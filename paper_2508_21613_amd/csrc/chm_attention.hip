@@ -220,6 +220,7 @@ struct Pass {
     if (a->cap > 0) {
       c.tanh2 = (float)(2 * log2e * a->scale / a->cap);
       c.cap2 = (float)(a->cap * log2e);
+      c.to_cap = (float)((double)a->scale / a->cap);
     }
     c.slopes = a->slopes;
     c.lse = (float *)a->saved;
@@ -451,7 +452,8 @@ int check(const chm_attention *a) {
   if (a->kv_heads < 1 || a->kv_heads > (1 << 20) || a->heads < a->kv_heads || a->heads > (1 << 20) || a->heads % a->kv_heads || a->dim < 1 || a->dim > 128) return CHM_ERR_ARG;
   if (a->tokens * group_of(a) > ROWS_MAX || a->batch * a->kv_heads > INT32_MAX) return CHM_ERR_ARG;
   if (a->batch * a->kv_heads > 0 && rows_pad(a) > (1ll << 50) / (a->batch * a->kv_heads)) return CHM_ERR_ARG;
-  if (!(a->scale > 0) || !isfinite(a->scale) || !(a->cap >= 0) || !isfinite(a->cap)) return CHM_ERR_ARG;
+  if (!(a->scale > 0) || !(a->cap >= 0) || !isfinite(a->cap)) return CHM_ERR_ARG;
+  if (a->scale > 1e30f || (a->cap > 0 && a->scale / a->cap > 1e30f)) return CHM_ERR_ARG;       // what products are multiplied by has to be finite
   if (!fine(a->q_stride, a->batch, a->tokens, a->heads) || !fine(a->k_stride, a->batch, a->keys, a->kv_heads) ||
       !fine(a->v_stride, a->batch, a->keys, a->kv_heads)) return CHM_ERR_ARG;
   if (!aligned(a->q, 2) || !aligned(a->k, 2) || !aligned(a->v, 2) || !aligned(a->saved, 16) || !aligned(a->slopes, 4)) return CHM_ERR_ARG;

@@ -427,13 +427,19 @@ __device__ __forceinline__ void seen_keys(const AttnCall &c, const Visit &now, W
 __device__ __forceinline__ uint32_t query_word(uint32_t word) { return word == ATTN_NONE ? ATTN_NOBODY : word; }
 
 // ---------------------------------------------------------------------------------------------- scores
-// The score in powers of two from the product q.k.  CAP: the tanh is 1 - 2 / (1 + exp(2 x)), off by 2^-23 of the cap, not of itself, which is what
-// a weight heeds.  `share` is 1 / (1 + exp(2 x)): the tanh's derivative is 4 share (1 - share).
+// The score in powers of two from the product q.k, and `share` = 1 / (1 + exp(2 x)), x = score / cap: the tanh is 1 - 2 share, off by 2^-23 of the cap, not of
+// itself, and its derivative 4 share (1 - share).  That is what weights heed as long as the cap is not large.  CAP = 2, for large ones: scores up to 1 / 4 of
+// the cap are score (1 - x^2 / 3 + 2 x^4 / 15 - 17 x^6 / 315), where the next term is 2^-21 and less.
 template <int CAP>
 __device__ __forceinline__ float capped(const AttnCall &c, float product, float &share) {
   if (!CAP) return product * c.to2;
   share = __builtin_amdgcn_rcpf(1.f + exp2_(product * c.tanh2));
-  return fmaf(share, -2.f * c.cap2, c.cap2);
+  const float far = fmaf(share, -2.f * c.cap2, c.cap2);
+  if (CAP == 1) return far;
+  const float x = product * c.to_cap, x2 = x * x;
+  float near = product * c.to2 * fmaf(x2, fmaf(x2, fmaf(x2, -17.f / 315.f, 2.f / 15.f), -1.f / 3.f), 1.f);
+  asm volatile("" : "+v"(near));            // chosen, not branched to: branches around 16 of them would cost dk and dv their registers
+  return fabsf(x) < 0.25f ? near : far;
 }
 __device__ __forceinline__ float biased(float s, float slope2, float rel, int r) { return fmaf(-slope2, fabsf(rel - (float)row_of(r)), s); }
 
@@ -866,11 +872,15 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
 }
 
 // ---------------------------------------------------------------------------------------------- backward
-// p and ds of a score from the products q.k and dy.v.  less: lse (with a bias, and it) in powers of two, less cap2 with a cap; delta: dy.y, four times it with a
+// p and ds of a score from the products q.k and dy.v.  less: lse (with a bias, and it) in powers of two, less cap2 with a cap (CAP = 1); delta: dy.y, four times it with a
 // cap, where ds = p share (1 - share) (4 dy.v - 4 delta)
 template <int CAP>
 __device__ __forceinline__ void gradient(const AttnCall &c, float product, float dp, float less, float delta, float &p, float &ds) {
-  if (CAP) {
+  if (CAP == 2) {
+    float share;
+    p = exp2_(capped<CAP>(c, product, share) - less);
+    ds = p * fmaf(-share, share, share) * fmaf(dp, 4.f, -delta);
+  } else if (CAP) {
     const float share = __builtin_amdgcn_rcpf(1.f + exp2_(product * c.tanh2));
     p = exp2_(fmaf(share, -2.f * c.cap2, -less));
     ds = p * fmaf(-share, share, share) * fmaf(dp, 4.f, -delta);
@@ -1043,7 +1053,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  const float less = CAP ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[block][lane & 31] : deltas[block][lane & 31];
+  const float less = CAP == 1 ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[block][lane & 31] : deltas[block][lane & 31];
   if (part == 0 && lane < 32 && row.row < c.rows_pad) {
     AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
     block.less[lane] = there ? less : INFINITY;
@@ -1436,6 +1446,7 @@ bool launch_parts(const AttnCall &c, const AttnLaunch &l) {
 template <class T, int WHAT, int D>
 bool launch_terms(const AttnCall &c, const AttnLaunch &l) {
   const bool cap = c.cap2 != 0.f, slope = c.slopes != nullptr;
+  if (c.cap2 > 256 * 1.4427f) return launch_parts<T, WHAT, D, 2, 1>(c, l);      // 2^-23 of the cap is 2^-15; biased by nothing where there are no slopes
   if (cap) return slope ? launch_parts<T, WHAT, D, 1, 1>(c, l) : launch_parts<T, WHAT, D, 1, 0>(c, l);
   return slope ? launch_parts<T, WHAT, D, 0, 1>(c, l) : launch_parts<T, WHAT, D, 0, 0>(c, l);
 }

@@ -334,8 +334,8 @@ def _attention(q, k, v, scale, cap, slopes, causal, documents, prefix):
     _need(1 <= dim <= 128, "heads must have 1 to 128 elements")
     scale = dim ** -0.5 if scale is None else float(scale)
     cap = float(cap)
-    _need(scale > 0 and math.isfinite(scale), "scale must be positive")
-    _need(cap >= 0 and math.isfinite(cap), "cap must not be negative")
+    _need(0 < scale <= 1e30, "scale must be positive, up to 1e30")
+    _need(cap >= 0 and math.isfinite(cap) and scale <= 1e30 * (cap or 1.0), "cap must be positive (0: none), scale / cap up to 1e30")
     d = B.Attention(DTYPES[dtype], 1 if causal else 0, batch, tokens, keys, heads, kv_heads, dim, q.data_ptr(), k.data_ptr(), v.data_ptr(),
                     _strides(q), _strides(k), _strides(v), scale, cap)
     held = [q, k, v]

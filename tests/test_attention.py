@@ -99,7 +99,7 @@ def formula(q, k, v, dy=None, scale=None, cap=0.0, slopes=None, causal=True, doc
                 t = torch.tanh(x / cap)
                 z, dz = cap * t, 1 - t * t
                 more = 8 * ACC + 2 * e / cap                     # of dz
-                e = e * dz + 4 * ACC * cap
+                e = e * dz + (4 * ACC * cap if cap <= 256 else 16 * ACC * z.abs())       # of a series or the tanh from 1 / 4 on
             s = z - (float(slopes[h]) * far if slopes is not None else 0.0)
             s = s.masked_fill(~see[b], -math.inf)
             some = see[b].any(1, keepdim=True)
@@ -429,6 +429,18 @@ def test_lengths_of_zero(ops):
         got = both(ops, *x, causal=False)
         for name, like in zip(("y",) + NAMES, (x[0], x[0], x[1], x[2])):
             assert got[name].shape == like.shape and not bool(got[name].any())
+
+
+@pytest.mark.parametrize("dtype", BOTH)
+@pytest.mark.parametrize("cap", [255.0, 257.0, 3000.0, 1e6, 1e30, 3e38])
+@pytest.mark.parametrize("T,d", [(9, 64), (100, 128)])
+def test_large_caps(ops, T, d, cap, dtype):
+    """scores far below a cap keep their digits; a score of a tenth of the cap and more is there as well"""
+    q, k, v, dy = inputs(T, 1, T, T, 4, 2, d, dtype)
+    q[:, -1] *= 60.0
+    compare(ops, (q, k, v, dy), cap=cap)
+    one = ops.attention_forward(q[:, -1:], k, v, cap=cap)
+    check("y", one, tuple(t[:, -1:] for t in formula(q, k, v, cap=cap)["y"]))
 
 
 def test_scores_far_apart(ops):

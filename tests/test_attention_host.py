@@ -114,7 +114,7 @@ def test_how_work_is_shared(kw, want):
 
 @pytest.mark.parametrize("kw", [
     dict(dtype=0), dict(dtype=3), dict(batch=-1), dict(tokens=-1), dict(keys=-1), dict(tokens=(1 << 30) + 1), dict(keys=(1 << 30) + 1), dict(heads=0),
-    dict(kv_heads=0), dict(kv_heads=3), dict(kv_heads=16), dict(dim=0), dict(dim=129), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf),
+    dict(kv_heads=0), dict(kv_heads=3), dict(kv_heads=16), dict(dim=0), dict(dim=129), dict(scale=0.0), dict(scale=-1.0), dict(scale=math.inf), dict(scale=2e30), dict(cap=1e-32),
     dict(scale=math.nan), dict(cap=-1.0), dict(cap=math.nan), dict(cap=math.inf), dict(q=BASE + 1), dict(k=BASE + 1), dict(v=BASE + 1),
     dict(saved=BASE + 8), dict(slopes=BASE + 2), dict(q_stride=(-1, 512, 64)), dict(k_stride=(0, -5, 64)), dict(v_stride=(0, 0, 1 << 61)),
     dict(q_documents=BASE, index_bits=32), dict(k_documents=BASE, index_bits=32), dict(q_documents=BASE, k_documents=BASE, index_bits=16),

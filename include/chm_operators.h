@@ -136,8 +136,9 @@ typedef struct {
   int64_t ld_q_documents, ld_k_documents;
   const uint8_t *prefix;                      /* [batch, keys], rows of ld_prefix, 0 or not; nullable; causal only */
   int64_t ld_prefix;
-  void *saved;                                /* what the backward pass wants (opaque, 16-byte aligned): written by the forward call, read by the
-                                                 backward call; NULL in a forward call: not kept */
+  void *saved;                                /* what the backward pass wants (opaque, 16-byte aligned), what the tokens' documents are among it: written by the
+                                                 forward call, read by the backward call, all else of whose description is the same; NULL in a forward
+                                                 call: not kept */
 } chm_attention;
 
 typedef struct {

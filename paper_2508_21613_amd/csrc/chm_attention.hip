@@ -1,7 +1,7 @@
 // Attention: what its passes consist of, the small kernels around the tiles (documents, packing, joined sums), the entry points.
 //
 //   forward    [documents, packing] tiles [join]
-//   backward   [documents, packing] dq (and delta = dy.y), dk and dv [join]
+//   backward   [packing] dq (and delta = dy.y), dk and dv [join]
 // dq and dk with dv are kernels of their own, each of which works out the scores again: seven products in place of five, but no sums that several
 // workgroups add to, so that the same inputs give the same bits.
 #include <hip/hip_runtime.h>
@@ -175,9 +175,16 @@ constexpr int64_t LENGTH_MAX = 1ll << 30, ROWS_MAX = INT32_MAX - (1 << 13);
 
 int64_t group_of(const chm_attention *a) { return a->heads / a->kv_heads; }
 int64_t rows_pad(const chm_attention *a) { return up(a->tokens * group_of(a), ATTN_TILE) * ATTN_TILE; }
-// lse of every row; what rounding took from y
+// Kept for the backward pass: lse of every row; what rounding took from y; what the documents of keys and queries are (laid out by sizes alone: the backward
+// pass may name the same documents by other tensors)
 uint64_t lse_bytes(const chm_attention *a) { return (uint64_t)(a->batch * a->kv_heads * rows_pad(a)) * 4; }
-uint64_t saved_bytes(const chm_attention *a) { return lse_bytes(a) + (((uint64_t)(a->batch * a->tokens * a->heads) * a->dim * 2 + 15) & ~15ull); }
+uint64_t low_bytes(const chm_attention *a) { return ((uint64_t)(a->batch * a->tokens * a->heads) * a->dim * 2 + 255) & ~255ull; }
+uint64_t documents_bytes(const chm_attention *a) {
+  if (!a->k_documents && !a->prefix) return 0;
+  const int64_t tiles = a->batch * (up(a->keys, ATTN_TILE) + up(a->tokens, ATTN_TILE));
+  return (uint64_t)tiles * (ATTN_TILE * 4 + sizeof(AttnTile)) + 4 * 256;
+}
+uint64_t saved_bytes(const chm_attention *a) { return lse_bytes(a) + low_bytes(a) + documents_bytes(a); }
 
 // the strides of dimensions of one element say nothing
 AttnInput input(const void *p, const int64_t s[3], int64_t b, int64_t t, int64_t h) {
@@ -282,20 +289,23 @@ struct Pass {
     DocumentsCall kd{(const char *)a->k_documents, a->prefix, a->ld_k_documents, a->ld_prefix, nullptr, nullptr, c.keys, a->index_bits, c.tiles};
     DocumentsCall qd{(const char *)a->q_documents, nullptr, a->ld_q_documents, 0, nullptr, nullptr, c.tokens, a->index_bits, c.q_tile_count};
     if (a->k_documents || a->prefix) {
+      Arena kept{a->saved ? (char *)a->saved + lse_bytes(a) + low_bytes(a) : nullptr};      // written by the forward pass, if there is one to come back to
+      const bool keep = g || a->saved;
+      Arena &from = keep ? kept : arena;
       const auto room = [&](DocumentsCall &d) {
-        d.words = (uint32_t *)arena.take((uint64_t)a->batch * d.tiles_each * ATTN_TILE * 4);
-        d.tiles = (AttnTile *)arena.take((uint64_t)a->batch * d.tiles_each * sizeof(AttnTile));
+        d.words = (uint32_t *)from.take((uint64_t)a->batch * d.tiles_each * ATTN_TILE * 4);
+        d.tiles = (AttnTile *)from.take((uint64_t)a->batch * d.tiles_each * sizeof(AttnTile));
       };
       room(kd);
       // the queries' tokens are the keys': their words are (the prefix is asked of keys alone)
-      const bool same = a->tokens == a->keys && a->q_documents == a->k_documents && (a->batch == 1 || a->ld_q_documents == a->ld_k_documents);
+      const bool same = !keep && a->tokens == a->keys && a->q_documents == a->k_documents && (a->batch == 1 || a->ld_q_documents == a->ld_k_documents);
       if (same) qd.words = kd.words, qd.tiles = kd.tiles;
       else room(qd);
       c.k_words = kd.words; c.k_tiles = kd.tiles;
       c.q_words = qd.words; c.q_tiles = qd.tiles;
       if (!run) c.k_words = c.q_words = (const uint32_t *)1;      // only whether there are any is asked
       first = a->batch * kd.tiles_each;
-      all = first + (same ? 0 : a->batch * qd.tiles_each);
+      all = g ? 0 : first + (same ? 0 : a->batch * qd.tiles_each);
     }
     const int64_t documents = up(all, 4);
     const uint32_t n = threads(documents + packs, 256);

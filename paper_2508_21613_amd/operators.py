@@ -395,7 +395,8 @@ def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, do
 
 
 def attention_backward(dy, q, k, v, y, saved, scale=None, cap=0.0, slopes=None, causal=True, documents=None, prefix=None, out=None, stream=None):
-    """chm_attention_backward: (dq, dk, dv) for dy, the gradient with respect to y, from attention_forward's y and saved; the other arguments as there.
+    """chm_attention_backward: (dq, dk, dv) for dy, the gradient with respect to y, from attention_forward's y and saved; the other arguments as there
+    (documents and prefix by any tensors that hold the same: what they are lies in saved).
     `out`: the three tensors to write (of any strides: the parts of one projection's gradient)."""
     d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
     _strided("dy", dy, q.shape, q.dtype, dev)

@@ -274,6 +274,25 @@ def test_documents_in_any_order(ops):
     compare(ops, x, documents=ids, causal=False, cap=3.0)
 
 
+def test_documents_named_by_other_tensors(ops):
+    """the backward pass is told of the forward pass's documents by copies, pairs, other types and strides: the same gradients"""
+    B, T = 2, 200
+    x = inputs(5, B, T, T, 4, 2, 64, torch.bfloat16)
+    ids = documents_of(1, B, T, 4, 15)
+    prefix = torch.rand((B, T), generator=gen(2), device="cuda") < 0.3
+    want = both(ops, *x, documents=ids, prefix=prefix)
+    wide = torch.full((B, 2 * T), 9, dtype=torch.int32, device="cuda")
+    wide[:, T:] = ids
+    ways = (ids, ids.clone(), (ids, ids.clone()), wide[:, T:], (wide[:, T:], wide[:, T:].contiguous()))
+    for one in ways:
+        y, saved = ops.attention_forward(*x[:3], documents=one, prefix=prefix, save=True)
+        for other in ways:
+            got = ops.attention_backward(x[3], *x[:3], y, saved, documents=other, prefix=prefix.clone())
+            assert all(torch.equal(g, want[n]) for n, g in zip(NAMES, got))
+    with pytest.raises(Exception):
+        ops.attention_backward(x[3], *x[:3], y, ops.attention_forward(*x[:3], save=True)[1], documents=ids)
+
+
 @pytest.mark.parametrize("T,K,H,Hk", [(1, 700, 8, 2), (5, 300, 4, 2), (200, 700, 2, 1), (130, 64, 2, 2)])
 def test_documents_of_queries_and_keys(ops, T, K, H, Hk):
     B = 4

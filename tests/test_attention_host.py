@@ -62,7 +62,9 @@ def test_sizes():
     one = _attention(pad=3, batch=1)
     assert _sizes(one)[1][1] >= 100 * (8 + 2 + 2) * 64 * 2
     docs = _attention(index_bits=32, q_documents=BASE >> 1, k_documents=BASE >> 1, ld_q_documents=100, ld_k_documents=100)
-    assert _sizes(docs)[1][1] >= 2 * 128 * 4
+    assert _sizes(docs)[1][1] >= 2 * 128 * 4 and _sizes(docs)[1][0] >= saved + 2 * 128 * 4
+    docs.saved = BASE >> 2
+    assert _sizes(docs)[1][1] == 0                                         # what the tokens' documents are lies there
     for empty in (_attention(batch=0), _attention(tokens=0), _attention(keys=0), _attention(tokens=0, keys=0)):
         assert _sizes(empty, _gradients(empty))[0] == B.OK
 

@@ -27,7 +27,6 @@ constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles ar
 struct AttnRows {
   float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap up to 256; +inf: the row sees nothing
   float delta[32];                         // dy . y; with a cap four times that
-  int32_t last[32];                        // last key that a causal mask leaves (no mask: all)
   uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
   float slope2[32];
   int32_t pos[32];

@@ -14,8 +14,8 @@
 //
 // Long calls are bound by the matrix cores and exponentials at the clock that the power limit leaves (1.6 to 1.9 GHz): two wavefronts a SIMD, each of whose
 // steps is 1,024 cycles of matrix instructions, as many of other ones and 32 KB (forward) from shared memory.  8,192 tokens, 32 heads of 128, 8 of
-// keys, bfloat16, causal, capped: forward 760 us (0.72 PFLOP/s of the 4 d operations a pair), dq 1,020 (0.81 of 6 d), dk and dv 1,410 (0.78 of 8 d); without
-// the cap 660, 920, 1,330.
+// keys, bfloat16, causal, capped: forward 740 us (0.74 PFLOP/s of the 4 d operations a pair), dq 990 (0.83 of 6 d), dk and dv 1,380 (0.80 of 8 d); without
+// the cap 615, 835, 1,225 (0.89, 0.99, 0.90).
 //
 // Tiles that nobody sees are not visited: each lane looks at one tile of 64 keys (of documents: least and largest number, prefix or not), and the
 // ballot is the list of those to visit, and of those whose every pair is seen, where nothing is masked.
@@ -335,7 +335,7 @@ __device__ __forceinline__ Sight sees(const AttnCall &c, int from, int to, const
 }
 
 // A tile that the workgroup visits (-1: no more), whether this wavefront does, what it has to mask, whether there are places of no document.  Most
-// tiles of packed documents lie within one, so that only their order is asked for, or the documents where one ends: half of a mask's cost.
+// tiles of packed documents lie within one, so that only their order is asked for, or the documents where one ends.
 struct Visit {
   int tile;
   bool run, documents, order, some_none;
@@ -399,28 +399,37 @@ struct KeyWalk {
   }
 };
 
-// Of the keys k0 + row_of(r), whose words are at `words`: tells set(r, .) whether the query at `pos` of the document `word` sees it:
-// as far as documents go and as far as their order goes, what `now` asks for (the wavefront's other tiles need neither)
-template <class Words, class F>
-__device__ __forceinline__ void seen_keys(const AttnCall &c, const Visit &now, Words words, int k0, int pos, uint32_t word, F set) {
-  const int rel = (c.causal && (c.k_words || pos < c.keys - 1) ? pos : c.keys - 1) - k0;
-  if (now.documents) {
-#pragma unroll
-    for (int g = 0; g < 4; ++g)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) set(g * 4 + e, (words[g * 8 + e] & ~1u) == word);
-  }
+// Masks are 32 bits a lane, one for each key (row) of a block: worked out once, and each score costs two operations that wait for no comparison (4,096 packed
+// tokens, 32 heads of 128, 8 of keys: forward 74 -> 71 us, dq 99 -> 94).  A bit of `there` (the
+// lane's place in the block) whose word is the lane's own: a ballot for each document of the wavefront, of which there is mostly one.
+__device__ __forceinline__ uint32_t same_words(uint32_t own, uint32_t there) {
+  uint32_t bits = 0;
+  uint64_t left = ~0ull;
+  do {
+    const uint32_t one = __builtin_amdgcn_readlane(own, __builtin_ctzll(left));
+    const uint64_t lanes = __ballot(own == one);
+    const uint32_t equal = (uint32_t)__ballot(there == one);
+    bits = own == one ? equal : bits;
+    left &= ~lanes;
+  } while (left);
+  return bits;
+}
+// Of the 32 keys from k0 on those that the query at `pos` of the document `word` sees, as far as `now` asks (the wavefront's other tiles need no mask); there:
+// word of the key k0 + lane % 32.  Bit row_of(r): that of a score's register r
+__device__ __forceinline__ uint32_t seen_keys(const AttnCall &c, const Visit &now, uint32_t there, int k0, int pos, uint32_t word, int lane) {
+  uint32_t seen = now.documents ? same_words(word, there & ~1u) : ~0u;
   if (now.order) {
-    if (c.prefix) {
-#pragma unroll
-      for (int g = 0; g < 4; ++g)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) set(g * 4 + e, (g * 8 + e <= rel) | (words[g * 8 + e] & 1u));
-    } else {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) set(r, row_of(r) <= rel);
-    }
+    const int rel = (c.causal && (c.k_words || pos < c.keys - 1) ? pos : c.keys - 1) - k0;
+    uint32_t before = rel < 0 ? 0u : rel > 30 ? ~0u : (2u << rel) - 1;
+    if (c.prefix) before |= (uint32_t)__ballot(there & 1);
+    seen &= before;
   }
+  return seen >> (lane >> 5) * 4;
+}
+// v where the bit of register r is set, `hidden` elsewhere
+__device__ __forceinline__ float where_seen(uint32_t seen, int r, float v, uint32_t hidden) {
+  const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)seen, row_of(r), 1);
+  return __uint_as_float((__float_as_uint(v) & keep) | (hidden & ~keep));
 }
 
 // a query's document as the comparisons want it: one that equals no key's where it has none
@@ -519,9 +528,10 @@ struct Softmax {
     }
   }
   // those of hidden keys become the value of no weight
-  template <class Words>
-  static __device__ __forceinline__ void hide(const AttnCall &c, const QueryRow<T, D> &row, const Visit &now, Words words, int k0, f16 &s) {
-    seen_keys(c, now, words, k0, row.pos, row.word, [&](int r, bool see) { s[r] = see ? s[r] : LEAST ? INFINITY : -INFINITY; });
+  static __device__ __forceinline__ void hide(const AttnCall &c, const QueryRow<T, D> &row, const Visit &now, uint32_t there, int k0, int lane, f16 &s) {
+    const uint32_t seen = seen_keys(c, now, there, k0, row.pos, row.word, lane);
+#pragma unroll
+    for (int r = 0; r < 16; ++r) s[r] = where_seen(seen, r, s[r], LEAST ? 0x7f800000u : 0xff800000u);
   }
   static __device__ __forceinline__ float most_of(const f16 &s) {
     float m = s[0];
@@ -686,11 +696,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     if (next.tile >= 0) feed.load(next.tile, lds0 + slot * Feed::SLOT, wave, lane);
     if (!now.run) continue;
     const int first = PARTS == 2 ? part * 32 : 0, k0 = now.tile * ATTN_TILE + first + h4;
-    lds_word *words = (lds_word *)(here + Feed::WORDS) + first + h4;
+    lds_word *words = (lds_word *)(here + Feed::WORDS) + first + (lane & 31);
     f16 s = Soft::products(row, here, first, lane);
     if (PARTS == 2) {
       Soft::values_of(c, row, k0, s);
-      if (now.masked()) Soft::hide(c, row, now, words, k0, s);
+      if (now.masked()) Soft::hide(c, row, now, words[0], k0 - h4, lane, s);
       soft.follow(c, Soft::most_of(s));
       soft.add(c, s, values, first, lane);
     } else {
@@ -698,8 +708,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       Soft::values_of(c, row, k0, s);
       Soft::values_of(c, row, k0 + 32, t);
       if (now.masked()) {
-        Soft::hide(c, row, now, words, k0, s);
-        Soft::hide(c, row, now, words + 32, k0 + 32, t);
+        Soft::hide(c, row, now, words[0], k0 - h4, lane, s);
+        Soft::hide(c, row, now, words[32], k0 - h4 + 32, lane, t);
       }
       soft.follow(c, Soft::more(Soft::most_of(s), Soft::most_of(t)));
       soft.add(c, s, values, 0, lane);
@@ -815,7 +825,7 @@ __global__ void __launch_bounds__(256) k_forward_few(const AttnCall c) {
     }
     f16 s = Soft::products(row, here, 0, lane);
     Soft::values_of(c, row, k0 + (lane >> 5) * 4, s);
-    if (now.masked()) Soft::hide(c, row, now, words + (words ? k0 + (lane >> 5) * 4 : 0), k0 + (lane >> 5) * 4, s);
+    if (now.masked()) Soft::hide(c, row, now, words ? words[k0 + (lane & 31)] : 0, k0, lane, s);
     soft.follow(c, Soft::most_of(s));
     soft.add(c, s, here + Feed::BYTES, 0, lane);
     asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");      // the slot has been read: the next loads go there
@@ -1058,7 +1068,6 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
     block.less[lane] = there ? less : INFINITY;
     block.delta[lane] = delta;
-    block.last[lane] = !there ? INT32_MIN : c.causal ? row.pos : INT32_MAX;
     block.word[lane] = there ? row.word : ATTN_NOBODY;
     block.slope2[lane] = row.slope2;
     block.pos[lane] = row.pos;
@@ -1074,7 +1083,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     next = walk.next(c, lane);
     arrived();
     lds_char *keys = lds + slot * Feed::SLOT, *values = keys + Feed::VALUES;
-    lds_word *words = (lds_word *)(keys + Feed::WORDS) + h4;
+    lds_word *words = (lds_word *)(keys + Feed::WORDS) + (lane & 31);
     if (now.some_none) {
       Feed::clear(keys, keys, tid);
       arrived();
@@ -1084,6 +1093,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     if (!now.run) continue;
 #pragma unroll
     for (int half = 0; half < 2 / PARTS; ++half) {
+      if (CAP) __builtin_amdgcn_sched_barrier(0);      // 8,192 tokens, 32 heads of 128, 8 of keys: 990 us, without 1,035; without a cap 875 and 835
       const int b = PARTS == 2 ? part : half, k0 = now.tile * ATTN_TILE + b * 32 + h4;
       f16 s = {}, dp = {};
 #pragma unroll
@@ -1098,7 +1108,11 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
         gradient<CAP>(c, s[r], dp[r], SLOPE ? fmaf(row.slope2, fabsf(rel - (float)row_of(r)), less) : less, delta, weight, ds);
         dp[r] = ds;
       }
-      if (now.masked()) seen_keys(c, now, words + b * 32, k0, row.pos, row.word, [&](int r, bool see) { dp[r] = see ? dp[r] : 0.f; });
+      if (now.masked()) {
+        const uint32_t seen = seen_keys(c, now, words[b * 32], k0 - h4, row.pos, row.word, lane);
+#pragma unroll
+        for (int r = 0; r < 16; ++r) dp[r] = where_seen(seen, r, dp[r], 0);
+      }
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -1328,28 +1342,22 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
       }
     }
     if (now.masked()) {
-      const int i = own_lane() % 32;
-      const uint32_t mine = words[wave][i], word = mine & ~1u;
-      const int key = mine & 1 ? INT32_MIN + 1 : wave_key + i;      // in the prefix: before every row
-      const auto hide = [&](int r, bool see) {
-        s[r] = see ? s[r] : 0.f;
-        dp[r] = see ? dp[r] : 0.f;
-      };
-      if (now.documents) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const u4 row = *(__attribute__((address_space(3))) const u4 *)&known->word[g * 8 + h4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) hide(g * 4 + e, word == row[e]);
-        }
-      }
+      const int at = own_lane(), i = at & 31, row0 = now.tile * STEP + part * 32;
+      const uint32_t mine = words[wave][i];
+      uint32_t seen = now.documents ? same_words(mine & ~1u, known->word[i]) : ~0u;
       if (now.order) {
-#pragma unroll
-        for (int g = 0; g < 4; ++g) {
-          const i4 last = *(__attribute__((address_space(3))) const i4 *)&known->last[g * 8 + h4];
-#pragma unroll
-          for (int e = 0; e < 4; ++e) hide(g * 4 + e, key <= last[e]);
+        // the rows from the key's own position on, as far as there are rows
+        if (c.causal && !(mine & 1)) {
+          const int position = wave_key + i - c.offset, first = (position > 0 ? position : 0) * c.group - row0;
+          seen &= first > 31 ? 0u : ~0u << (first > 0 ? first : 0);
         }
+        if (c.rows - row0 < 32) seen &= (1u << (c.rows - row0)) - 1;
+      }
+      seen >>= (at >> 5) * 4;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        s[r] = where_seen(seen, r, s[r], 0);
+        dp[r] = where_seen(seen, r, dp[r], 0);
       }
     }
 #pragma unroll

@@ -32,7 +32,7 @@ struct AttnRows {
   int32_t pos[32];
   AttnTile documents;                      // of all of them
 };
-constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // with or without the lowest bit it equals no key's word, ATTN_NONE neither
+constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // odd: equal to no key's word without its lowest bit, ATTN_NONE among them
 
 // A workgroup of dk and dv: its tile of keys (-1: none), the parts that the rows are dealt to and which of them it is, and where its sums go if there are several
 struct AttnShare { int32_t tile, part, parts, slot; };

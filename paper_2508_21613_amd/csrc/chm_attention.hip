@@ -259,11 +259,12 @@ struct Pass {
     return AttnLaunch{chosen.dim, parts, chosen.fine, threads(heads() * tiles * splits, 256), st};
   }
 
-  // Inputs as the tiles take them: 16-byte rows, and 64 of them within offsets of 31 bits
+  // Inputs as the tiles take them: 16-byte rows, and those of one load (`rows`) within offsets of 31 bits: what a load leaves out asks for an offset
+  // just below 2^31 and arrives as zeros because no load's memory reaches that far
   PackCall pack{};
-  void packed(AttnInput &in, int64_t tokens, int64_t heads, int64_t group, int bit) {
-    const int64_t across = group == 1 ? 63 : 63 / group + 1;
-    const bool reach = 2 * (across * in.token + (group - 1) * in.head + 128) < (1ll << 31) - 256;
+  void packed(AttnInput &in, int64_t tokens, int64_t heads, int64_t group, int rows, int bit) {
+    const int64_t across = group == 1 ? rows - 1 : (rows - 1) / group + 1, most = ((1ll << 31) - 256) / 2 - 128;      // tokens, elements
+    const bool reach = in.token <= most / across && (group == 1 || in.head <= (most - across * in.token) / (group - 1));
     if ((uintptr_t)in.p % 16 == 0 && a->dim % 8 == 0 && in.batch % 8 == 0 && in.token % 8 == 0 && in.head % 8 == 0 && reach) return;
     chosen.packed |= bit;
     const int64_t d8 = c.dim, words = a->batch * tokens * heads * (d8 / 8);
@@ -278,10 +279,10 @@ struct Pass {
     in = AttnInput{m.out, tokens * heads * d8, heads * d8, d8};
   }
   void inputs(const chm_attention_gradients *g) {
-    packed(c.q, a->tokens, a->heads, group_of(a), 1);
-    packed(c.k, a->keys, a->kv_heads, 1, 2);
-    packed(c.v, a->keys, a->kv_heads, 1, 4);
-    if (g) packed(c.dy, a->tokens, a->heads, group_of(a), 8);
+    packed(c.q, a->tokens, a->heads, group_of(a), 64, 1);
+    packed(c.k, a->keys, a->kv_heads, 1, 64, 2);
+    packed(c.v, a->keys, a->kv_heads, 1, g && dkdv_tile() == 128 ? 128 : 64, 4);      // dk and dv keep the values of all their keys
+    if (g) packed(c.dy, a->tokens, a->heads, group_of(a), 64, 8);
     pack.dim = (int32_t)a->dim;
     pack.dim8 = c.dim;
     int64_t packs = 0, first = 0, all = 0;
@@ -352,7 +353,8 @@ struct Pass {
     if (a->tokens == 0 || a->keys == 0 || key_tiles() > ATTN_SHARE_TILES || c.q_tile_count > ATTN_SHARE_QUERIES) return false;
     return a->k_documents ? dealt_parts() > 1 || groups > 512 : a->causal && groups < 512 && dealt_parts() > 1;
   }
-  int64_t key_tiles() const { return up(a->keys, chosen.dkdv_keys); }
+  int dkdv_tile() const { return chosen.dim == 64 ? 64 : 128; }
+  int64_t key_tiles() const { return up(a->keys, dkdv_tile()); }
 
   // Rows of a workgroup.  64 of them take half as long as 128 but read the keys twice as often: taken where the whole launch is no more than the workgroups
   // that run at once, with a causal mask, where they differ, twice that.  Rows of 64 elements leave room for a third workgroup with 64 rows, and only dq in large
@@ -404,7 +406,7 @@ struct Pass {
     inputs(g);
     chosen.fine = heads() * up(rows(), 64) <= 128;      // then dq's workgroups have 64 rows, one for every other compute unit at most
     c.row_data = (AttnRows *)arena.take((uint64_t)(heads() * c.rows_pad / 32) * sizeof(AttnRows));
-    chosen.dkdv_keys = chosen.dim == 64 ? 64 : 128;
+    chosen.dkdv_keys = dkdv_tile();
     const int64_t tiles = key_tiles();
     const bool shared = dealt();
     const int splits = shared ? dealt_parts() : dkdv_splits(heads() * tiles, up(rows(), ATTN_TILE), a->causal != 0, chosen.dim);

@@ -586,3 +586,17 @@ def test_gradients_of_small_calls(ops, T, H, Hk, d, dtype):
     got, want = both(ops, *x, cap=20.0), formula(*x, cap=20.0, kept=U[dtype])
     for name in NAMES:
         check(name, got[name], want[name])
+
+
+@pytest.mark.parametrize("d,far", [(128, 17000000), (128, 8500000), (72, 8500000), (72, 8454650), (64, 17000000)])
+def test_values_far_apart(ops, d, far):
+    """values whose tokens lie millions of elements apart, others between them: the same bits as of values side by side"""
+    T, H = 140, 2
+    q, k, v, dy = inputs(d, 1, T, T, H, 1, d, torch.bfloat16)
+    far = far // 8 * 8
+    buf = torch.full((T * far,), float("nan"), dtype=torch.bfloat16, device="cuda")
+    wide = buf.view(1, T, far)[:, :, :d].unflatten(2, (1, d))
+    wide.copy_(v)
+    for kw in (dict(), dict(causal=False)):
+        want, got = both(ops, q, k, v, dy, **kw), both(ops, q, k, wide, dy, **kw)
+        assert all(torch.equal(got[n], want[n]) for n in want)

@@ -257,3 +257,26 @@ def test_tensors_that_are_not_on_the_gpu_are_refused():
     for bad in (x[0], x.float(), None, "x"):
         with pytest.raises(B.ChmError):
             ops.attention_forward(bad, x, x)
+
+
+def test_every_row_of_a_load_is_within_reach():
+    """offsets within a load of whole rows count 31 bits: 64 rows of every input, 128 of the values where the gradients' kernels take 128 keys at a time"""
+    at = ((1 << 31) - 256) // 2 - 128                                      # elements
+    for dim, rows in ((64, 64), (65, 128), (72, 128), (128, 128)):
+        kw = dict(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=dim)
+        token = at // (rows - 1) // 8 * 8
+        odd = 7 if dim % 8 else 0                                          # every input is packed: its rows are no whole words
+        for far, forward, backward in ((token, 0, 0), (token + 8, 4 if rows == 64 else 0, 4), (17000000 // 8 * 8, 4 if rows == 64 and token < 17000000 else 0, 4 if token < 17000000 else 0)):
+            a = _attention(**dict(kw, v_stride=(0, far, dim)))
+            assert _kernels(a)[1]["packed"] == (odd or forward)
+            assert _kernels(a, _gradients(a))[1]["packed"] == ((odd and 15) or backward)
+    # keys are taken 64 at a time, or row by row
+    a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, k_stride=(0, 17000000, 128))
+    assert _kernels(a, _gradients(a))[1]["packed"] == 0
+    # strides of which no 64 can be counted
+    for stride in (1 << 30, 1 << 31, 1 << 40, (1 << 60) // 200):
+        for name in ("q_stride", "k_stride", "v_stride"):
+            a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, **{name: (0, stride, 128)})
+            assert _kernels(a)[1]["packed"] == {"q_stride": 1, "k_stride": 2, "v_stride": 4}[name]
+    a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, q_stride=(0, 256, (1 << 60) // 2))
+    assert _kernels(a)[1]["packed"] == 1

@@ -121,7 +121,8 @@ int chm_rotary_turn(const chm_rotary *r, int32_t backwards, void *hip_stream);
  * Gradients, of a scalar of which dy is the gradient with respect to y:
  *   ds = p (dy.v - dy.y);  dq = scale sum_j ds z' k;  dk = scale sum_i ds z' q;  dv = sum_i p dy    (sums over the group's heads)
  * p and ds are worked out in float32 and rounded to the tensors' type once, where they enter a product (in small calls the gradients' products also
- * take what that took): against the formulas in 64 bits gradients are off by 1.4 times (1.1 times) what one rounding to that type makes. */
+ * take what that took): against the formulas in 64 bits gradients are off by up to 1.5 times (1.1 times) what one rounding to that type makes.  In float16 that
+ * holds for small and large dy, too: p and ds are rounded 2^12 times as large, a row's ds by a smaller power of two where they would pass what float16 holds. */
 typedef struct {
   int32_t dtype;                              /* CHM_BF16 or CHM_F16: type of all tensors */
   int32_t causal;

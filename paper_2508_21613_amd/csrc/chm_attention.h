@@ -25,12 +25,13 @@ constexpr int ATTN_TILE = 64;              // keys of a tile; words and tiles ar
 
 // What the kernel of dq leaves to that of dk and dv about 32 rows, one value after the other (rows behind the last see nothing)
 struct AttnRows {
-  float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap up to 256; +inf: the row sees nothing
+  float less[32];                          // log2 of the sum of powers of two, less cap2 where there is a cap up to 256, less the lift of p; +inf: the row sees nothing
   float delta[32];                         // dy . y; with a cap four times that
   uint32_t word[32];                       // document * 2; ATTN_NOBODY: none
   float slope2[32];
   int32_t pos[32];
   AttnTile documents;                      // of all of them
+  int32_t lowered, unused[3];              // float16: ds is within its range if lifted by so much less
 };
 constexpr uint32_t ATTN_NOBODY = 0xffffffffu;      // odd: equal to no key's word without its lowest bit, ATTN_NONE among them
 

@@ -41,7 +41,11 @@ typedef _Float16 h8 __attribute__((ext_vector_type(8)));
 typedef __attribute__((address_space(3))) char lds_char;
 typedef __attribute__((address_space(3))) const uint32_t lds_word;
 
+// LIFT: the gradients' p and ds are worked out 2^LIFT times as large, and their sums taken down again at the end.  Bf16 reaches as far down as float32; float16's
+// least step, 2^-24, is much of a ds of 1 / keys and a small dy long before the results come near it (4,096 keys, 128 elements, no mask: dk off by 8.1e-4 with a dy
+// of 1e-3 and by 3.4e-3 with one of 2e-4, with the lift by 3.0e-4 and 3.5e-4, where rounding it alone takes 2.1e-4 and 2.8e-4).  2^16 / 2^12 leaves p room for what rounding does to scores of up to 2^26; ds has lower().
 struct Bf16 {
+  enum { LIFT = 0 };
   static __device__ __forceinline__ f16 mfma(s8 a, s8 b, f16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf8, a), __builtin_bit_cast(bf8, b), c, 0, 0, 0);
   }
@@ -49,6 +53,7 @@ struct Bf16 {
   static __device__ __forceinline__ float up(uint16_t u) { return __builtin_bit_cast(float, (uint32_t)u << 16); }
 };
 struct F16 {
+  enum { LIFT = 12 };
   static __device__ __forceinline__ f16 mfma(s8 a, s8 b, f16 c) {
     return __builtin_amdgcn_mfma_f32_32x32x16_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
   }
@@ -900,6 +905,42 @@ __device__ __forceinline__ void gradient(const AttnCall &c, float product, float
   }
 }
 
+// A block of 32 keys whose lifted ds pass 2^15: from here on the lane's row has less of the lift, in its weights, this block and the sums, so that the largest lies between 2^13 and
+// 2^14.  How much less is kept for dk (rows of 32 together, AttnRows::lowered).  A bound that is known beforehand, |dy| times the largest |v|, would cost a launch of its own and half of the lift in
+// calls that need none taken away.  Time, 8,192 tokens, 32 heads of 128, 8 of keys: dq 870 us for 805 without, capped 973 for 925, dk and dv 1,207 for 1,195, capped
+// 1,272 for 1,262; 4 x 1,024 tokens of 64: 36 for 33.5 and 43.6 for 43.
+template <int D>
+__device__ __forceinline__ void lower(f16 &ds, f16 (&sums)[D / 32], float &less, int &lowered) {
+  const auto largest = [](float a, float b, float c) {        // written out: the compiler makes values that passed a mask canonical first, one more operation each
+    float m;
+    asm("v_max3_f32 %0, |%1|, |%2|, |%3|" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+  };
+  float m = ds[0];
+#pragma unroll
+  for (int r = 1; r < 15; r += 2) m = largest(m, ds[r], ds[r + 1]);
+  m = both_max(largest(m, ds[15], ds[15]));
+  if (__any(m >= 32768.f)) {
+    const int e = m >= 32768.f ? __builtin_amdgcn_frexp_expf(m) : 0, n = e > 14 ? e - 14 : 0;       // infinities: 0, they stay
+    less += (float)n;
+    lowered += n;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) ds[r] = ldexpf(ds[r], -n);
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) sums[d][r] = ldexpf(sums[d][r], -n);
+  }
+}
+// sums without their lift
+template <int N>
+__device__ __forceinline__ void take_down(f16 (&sums)[N], int by) {
+#pragma unroll
+  for (int d = 0; d < N; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) sums[d][r] = ldexpf(sums[d][r], by);
+}
+
 // delta = dy.y of a wavefront's 32 rows, whose dy lie at `dys`, to `out`.  y is taken with what its rounding took from it: where few keys share a row, dy.v and
 // delta are near each other, and 2^-9 of y would be 1.5 times the error that the gradients have otherwise (17 tokens in bfloat16, dk: 3.7e-3
 // without, 2.4e-3 with).  A row by as many lanes as it has chunks.
@@ -1027,6 +1068,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   constexpr int TURN = WAVES * turn_bytes(N), MEET = PARTS == 2 ? WAVES * N * 4096 : 0;
   static_assert((int)SHARE_BYTES <= (int)Feed::BYTES, "shared memory holds what the shares are worked out from");
   __shared__ float deltas[BLOCKS][32];
+  __shared__ int most[WAVES];
   __shared__ __attribute__((aligned(1024))) char shared[Feed::BYTES > TURN + MEET ? Feed::BYTES : TURN + MEET];
   lds_char *lds = (lds_char *)shared;
   const uint32_t lds0 = (uint32_t)(uintptr_t)lds;
@@ -1063,7 +1105,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
-  const float less = CAP == 1 ? lse - c.cap2 : lse, delta = CAP ? 4.f * deltas[block][lane & 31] : deltas[block][lane & 31];
+  float less = (CAP == 1 ? lse - c.cap2 : lse) - T::LIFT;
+  const float delta = CAP ? 4.f * deltas[block][lane & 31] : deltas[block][lane & 31];
   if (part == 0 && lane < 32 && row.row < c.rows_pad) {
     AttnRows &block = c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (row.row >> 5)];
     block.less[lane] = there ? less : INFINITY;
@@ -1074,6 +1117,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     if (c.k_words && lane == 0) block.documents = AttnTile{walk.wave_docs.first, walk.wave_docs.last, walk.wave_docs.flags, 0};
   }
   f16 dq[D / 32];
+  int lowered = 0;
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dq[d] = f16{};
 
@@ -1093,7 +1137,8 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     if (!now.run) continue;
 #pragma unroll
     for (int half = 0; half < 2 / PARTS; ++half) {
-      if (CAP) __builtin_amdgcn_sched_barrier(0);      // 8,192 tokens, 32 heads of 128, 8 of keys: 990 us, without 1,035; without a cap 875 and 835
+      // 8,192 tokens, 32 heads of 128, 8 of keys, capped: 990 us, without it 1,035; without a cap 875 and 835, but in float16, where lower() parts the halves, 860 and 944
+      if (CAP || T::LIFT != 0) __builtin_amdgcn_sched_barrier(0);
       const int b = PARTS == 2 ? part : half, k0 = now.tile * ATTN_TILE + b * 32 + h4;
       f16 s = {}, dp = {};
 #pragma unroll
@@ -1113,6 +1158,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
 #pragma unroll
         for (int r = 0; r < 16; ++r) dp[r] = where_seen(seen, r, dp[r], 0);
       }
+      if constexpr (T::LIFT != 0) lower<D>(dp, dq, less, lowered);
       const s8 ds[2] = {pack8<T>(dp, 0), pack8<T>(dp, 8)};
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
@@ -1127,15 +1173,26 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     }
   }
   arrived();
+  if constexpr (T::LIFT != 0) {
+    take_down<D / 32>(dq, lowered - T::LIFT);
+#pragma unroll
+    for (int x = 16; x >= 1; x >>= 1) {
+      const int other = __shfl_xor(lowered, x);
+      lowered = other > lowered ? other : lowered;
+    }
+    if (lane == 0) most[wave] = lowered;
+  }
   f16 sum[N];
   if constexpr (PARTS == 2) {
     give<N>(lds + TURN + wave * (N * 4096), dq, sum, part == 1, lane);
     __syncthreads();
+    if (T::LIFT != 0 && most[wave ^ BLOCKS] > lowered) lowered = most[wave ^ BLOCKS];
     take<N>(lds + TURN + (wave ^ BLOCKS) * (N * 4096), sum, c.scale, c.scale, lane);
   } else {
 #pragma unroll
     for (int d = 0; d < N; ++d) sum[d] = dq[d] * c.scale;
   }
+  if (T::LIFT != 0 && part == 0 && lane == 0 && wave_row < c.rows_pad) c.row_data[(int64_t)p.hb * (c.rows_pad / 32) + (wave_row >> 5)].lowered = lowered;
   by_rows(lds + wave * turn_bytes(N), sum, part * (N * 32), lane, [&](int i, int d, f4 a, f4 b) {
     const int r = wave_row + i, token = divide(c.by_group, r), head = p.h * c.group + r - token * c.group;
     if (r < c.rows) store8<T>(c.dq.p + p.b * c.dq.batch + token * c.dq.token + head * c.dq.head, d, c.width, a, b);
@@ -1280,6 +1337,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
   RowWalk<KEYS, STEP> walk;
   walk.start(c, p, key0, wave_key, word, part * 32, first + share.part, share.parts, blocks, lane);
   if (lane < 32) words[wave][lane] = word;  // for this wavefront alone
+  int lowered = 0;                          // of dk's sums and of ds
   f16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int d = 0; d < D / 32; ++d) dk[d] = dv[d] = f16{};
@@ -1322,6 +1380,7 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     for (int i = 0; i < D / 16; ++i) dp = T::mfma(row_fragment<D>(dys, part * 32, i, lane), row_fragment<D>(values, block * 32, i, lane), dp);
     __builtin_amdgcn_sched_barrier(0);      // reads of shared memory that are moved up from below would take the registers of k
     if (next.tile >= 0) load(next.tile, slot);
+    const int rows_lowered = T::LIFT != 0 ? __builtin_amdgcn_readfirstlane(known->lowered) : 0;
 #pragma unroll
     for (int g = 0; g < 4; ++g) {
       f4 less = *(lds_f4 *)&known->less[g * 8 + h4];
@@ -1359,6 +1418,14 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
         s[r] = where_seen(seen, r, s[r], 0);
         dp[r] = where_seen(seen, r, dp[r], 0);
       }
+    }
+    if (T::LIFT != 0 && (rows_lowered | lowered)) {      // some rows' ds are beyond float16
+      if (rows_lowered > lowered) {
+        take_down<D / 32>(dk, lowered - rows_lowered);
+        lowered = rows_lowered;
+      }
+#pragma unroll
+      for (int r = 0; r < 16; ++r) dp[r] = ldexpf(dp[r], -lowered);
     }
 #pragma unroll
     for (int i = 0; i < 2; ++i) {
@@ -1406,6 +1473,10 @@ __global__ void __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 6
     by_rows(own, k, d0, lane, [&](int row, int d, f4 a, f4 b) { put(dk, dk_token, row, d, a, b); });
     by_rows(own, v, d0, lane, [&](int row, int d, f4 a, f4 b) { put(dv, dv_token, row, d, a, b); });
   };
+  if constexpr (T::LIFT != 0) {
+    take_down<D / 32>(dk, lowered - T::LIFT);
+    take_down<D / 32>(dv, -T::LIFT);
+  }
   if constexpr (PARTS == 2) {
     f16 sk[N], sv[N];
     lds_char *meet = lds + TURN;

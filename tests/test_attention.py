@@ -600,3 +600,59 @@ def test_values_far_apart(ops, d, far):
     for kw in (dict(), dict(causal=False)):
         want, got = both(ops, q, k, v, dy, **kw), both(ops, q, k, wide, dy, **kw)
         assert all(torch.equal(got[n], want[n]) for n in want)
+
+
+def quantum(monkeypatch, least):
+    """what float16's rounding of p and ds takes at least, for formula()"""
+    monkeypatch.setitem(TINY, torch.float16, least)
+
+
+@pytest.mark.parametrize("std", [0.05, 1e-3, 2e-4, 5e-5])
+@pytest.mark.parametrize("T,K,H,Hk,d,causal,cap", [(2048, 2048, 2, 2, 64, True, 0.0), (4096, 4096, 2, 1, 128, False, 0.0), (1500, 1500, 3, 1, 128, True, 20.0),
+                                                   (300, 9000, 1, 1, 64, False, 500.0), (17, 17, 4, 4, 64, True, 0.0), (130, 3000, 2, 1, 72, True, 0.0)])
+def test_gradients_of_small_dy_in_float16(ops, monkeypatch, T, K, H, Hk, d, causal, cap, std):
+    """p and ds are taken 2^12 times as large: what rounding takes of them at least is 2^-37.  That of the forward pass's weights (2^-25, of weights whose sum is 1 and more)
+    comes into delta, for which formula() grants y's rounding as well, which is kept: 2^-11 / sqrt(3) of an element of y of some 1 / sqrt(keys) is more
+    than sqrt(keys) 2^-25 / sqrt(3) up to 2^14 keys.  As a whole, too, the error is within 1.1 standard deviations: of a hundred thousand elements and more that
+    is 30 of its own standard deviations, and the few rows of the small calls, whose errors are alike, have 1.5."""
+    x = inputs(T + d, 1, T, K, H, Hk, d, torch.float16)
+    x[3].mul_(std / 0.3)
+    quantum(monkeypatch, 2.0 ** -37)
+    want = formula(*x, causal=causal, cap=cap)
+    quantum(monkeypatch, 2.0 ** -25)
+    got = both(ops, *x, causal=causal, cap=cap)
+    for name in NAMES:
+        check(name, got[name], want[name])
+        value, var = want[name]
+        own = torch.clamp(value.abs() * U[torch.float16], min=TINY[torch.float16]) ** 2 / 3
+        assert float((got[name].double() - value).norm()) <= (1.1 if T > 1000 else 1.5) * float((var + own).sum().sqrt()), name
+
+
+@pytest.mark.parametrize("std,scale", [(30.0, None), (1000.0, 0.002), (10000.0, 1e-4)])
+@pytest.mark.parametrize("T,H,Hk,d,cap,which", [(50, 2, 1, 64, 0.0, 0), (700, 4, 2, 64, 0.0, 0), (700, 2, 2, 128, 0.0, 1), (1300, 2, 1, 128, 30.0, 0), (900, 2, 1, 80, 300.0, 1)])
+def test_gradients_of_large_dy_in_float16(ops, monkeypatch, T, H, Hk, d, cap, which, std, scale):
+    """ds of 8 and more are lifted by less than 2^12, those beyond 65,504 taken down: by what brings the largest that a row (for dk: a wavefront) has met to between 2^13
+    and 2^15, so that rounding takes at least 2^-38 of that.  |ds| is at most |dy.v| + |dy.y|.  dy is a thousand times larger in a few rows than in the others, as
+    loss scaling or single tokens make it.  Elements near the end of float16's range are left out."""
+    x = inputs(T + d, 1, T, T, H, Hk, d, torch.float16)
+    q, k, v, dy = x
+    v.mul_(4.0)
+    dy.mul_(std / 0.3 / 1000)
+    dy[:, 1::37] *= 1000
+    assert bool(torch.isfinite(dy).all())
+    kw = dict(cap=cap, **({} if which == 0 else dict(slopes=slopes_of(H))), **({} if scale is None else dict(scale=scale)))
+    quantum(monkeypatch, 2.0 ** -37)
+    want = formula(*x, **kw)
+    quantum(monkeypatch, 2.0 ** -25)
+    largest = 2 * dy.double().norm(dim=3) * v.double().norm(dim=3).max()            # [1, T, H]
+    assert float(largest.max()) > 65504 or std < 1000
+    see, G = visible(1, T, T)[0].double(), H // Hk
+    step = (kw.get("scale", d ** -0.5) * 2.0 ** -38) ** 2 / 3
+    for h in range(H):
+        want["dq"][1][0, :, h] += step * largest[0, :, h, None] ** 2 * (see @ k[0, :, h // G].double() ** 2)
+        want["dk"][1][0, :, h // G] += step * largest.max() ** 2 * (see.T @ q[0, :, h].double() ** 2)
+    got = both(ops, *x, **kw)
+    for name in NAMES:
+        inside = want[name][0].abs() < 60000
+        assert float(inside.double().mean()) > 0.9
+        check(name, got[name][inside], tuple(t[inside] for t in want[name]))

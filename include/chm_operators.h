@@ -153,7 +153,8 @@ typedef struct {
 int chm_attention_sizes(const chm_attention *a, const chm_attention_gradients *g, uint64_t *saved, uint64_t *forward_scratch, uint64_t *backward_scratch);
 
 /* With up to 32 tokens times heads of a group it is bound by reading the keys and values, and runs on a kernel for that; few rows over many keys are
- * split over the keys and joined.  Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
+ * split over the keys and joined.  A launch has fewer than 2^24 workgroups: calls of more tiles (32 rows of a small call, 64 or 128 of others; 64 or 128 keys of dk and dv)
+ * times sequences and key heads are refused, by chm_attention_sizes as well, and so are inputs of 2^35 elements and more that have to be packed.  Errors: CHM_ERR_ARG, CHM_ERR_LIMIT (scratch too short), CHM_ERR_HIP. */
 int chm_attention_forward(const chm_attention *a, void *y, const int64_t y_stride[3], void *scratch, uint64_t scratch_bytes, void *hip_stream);
 int chm_attention_backward(const chm_attention *a, const chm_attention_gradients *g, void *scratch, uint64_t scratch_bytes, void *hip_stream);
 

@@ -171,6 +171,7 @@ struct Arena {
 };
 
 constexpr int FEW_ROWS = 32;
+constexpr int64_t GROUPS_MAX = UINT32_MAX / 256;          // workgroups of a launch: threads are counted in 32 bits
 constexpr int64_t LENGTH_MAX = 1ll << 30, ROWS_MAX = INT32_MAX - (1 << 13);
 
 int64_t group_of(const chm_attention *a) { return a->heads / a->kv_heads; }
@@ -246,7 +247,7 @@ struct Pass {
   bool bf16() const { return a->dtype == CHM_BF16; }
 
   uint32_t threads(int64_t groups, int64_t each) {
-    fits = fits && groups * each <= UINT32_MAX;
+    fits = fits && groups <= UINT32_MAX / each;
     return (uint32_t)groups;
   }
 
@@ -323,7 +324,7 @@ struct Pass {
     const int64_t slots = dim == 64 ? 512 : 256;
     int best = 1;
     double least = 1e30;
-    for (int64_t s = 1; s <= 64 && (s == 1 || s * 4 <= tiles); ++s) {
+    for (int64_t s = 1; s <= 64 && (s == 1 || (s * 4 <= tiles && heads * s <= GROUPS_MAX)); ++s) {
       const double cost = (double)up(heads * s, slots) / s + 0.002 * s;
       if (cost < least) least = cost, best = (int)s;
     }
@@ -370,27 +371,27 @@ struct Pass {
     if (a->batch == 0 || a->tokens == 0) return;
     inputs(nullptr);
     chosen.few = rows() <= FEW_ROWS;
+    const int64_t all = heads() * rows(), joins = up(all * (c.width4 / 4), 256);
     AttnLaunch l;
     if (chosen.few) {
       chosen.forward_rows = FEW_ROWS;
-      l = layout(1, few_splits(heads(), c.tiles, chosen.dim), 1);
+      l = layout(1, joins <= GROUPS_MAX ? few_splits(heads(), c.tiles, chosen.dim) : 1, 1);
     } else {
       chosen.forward_rows = forward_tile();
       const int64_t tiles = up(rows(), chosen.forward_rows);
       l = layout(tiles, tile_splits(heads() * tiles, c.tiles, chosen.dim == 64 ? 768 : 512, 8), 128 / chosen.forward_rows);
     }
     chosen.forward_splits = c.splits;
-    const int64_t all = heads() * rows();
     if (c.splits > 1) {
       c.part = (float *)arena.take((uint64_t)(c.splits * all * c.width4) * 4);
       c.part2 = (float *)arena.take((uint64_t)(c.splits * all * 2) * 4);
+      threads(joins, 256);
     }
-    const uint32_t joins = threads(up(all * (c.width4 / 4), 256), 256);
     if (!run || !fits) return;
     ok = ok && (bf16() ? attn_forward_bf16 : attn_forward_f16)(c, l, chosen.few);
     if (c.splits > 1) {
-      if (bf16()) hipLaunchKernelGGL(k_join_forward<CHM_BF16>, dim3(joins), dim3(256), 0, st, c, all * (c.width4 / 4));
-      else hipLaunchKernelGGL(k_join_forward<CHM_F16>, dim3(joins), dim3(256), 0, st, c, all * (c.width4 / 4));
+      if (bf16()) hipLaunchKernelGGL(k_join_forward<CHM_BF16>, dim3((uint32_t)joins), dim3(256), 0, st, c, all * (c.width4 / 4));
+      else hipLaunchKernelGGL(k_join_forward<CHM_F16>, dim3((uint32_t)joins), dim3(256), 0, st, c, all * (c.width4 / 4));
       ok = ok && hipGetLastError() == hipSuccess;
     }
   }
@@ -431,18 +432,18 @@ struct Pass {
       const AttnLaunch l = shared ? layout(c.share_slots, 1, 128 / chosen.dkdv_keys) : layout(tiles, splits, 128 / chosen.dkdv_keys);
       chosen.dkdv_splits = splits;
       chosen.dkdv_shared = shared;
-      const int64_t words = heads() * K * (c.width4 / 4);
+      const int64_t words = heads() * K * (c.width4 / 4), joins = up(words, 256);
       if (splits > 1) {
         const uint64_t bytes = (uint64_t)(heads() * c.share_slots) * (uint64_t)(chosen.dkdv_keys * c.width4) * 4;
         c.part = (float *)arena.take(bytes);
         c.part2 = (float *)arena.take(bytes);
+        threads(joins, 256);
       }
-      const uint32_t joins = threads(up(words, 256), 256);
       if (!run || !fits) return;
       ok = ok && (bf16() ? attn_dkdv_bf16 : attn_dkdv_f16)(c, l);
       if (splits > 1) {
-        if (bf16()) hipLaunchKernelGGL(k_join_backward<CHM_BF16>, dim3(joins), dim3(256), 0, st, c, words);
-        else hipLaunchKernelGGL(k_join_backward<CHM_F16>, dim3(joins), dim3(256), 0, st, c, words);
+        if (bf16()) hipLaunchKernelGGL(k_join_backward<CHM_BF16>, dim3((uint32_t)joins), dim3(256), 0, st, c, words);
+        else hipLaunchKernelGGL(k_join_backward<CHM_F16>, dim3((uint32_t)joins), dim3(256), 0, st, c, words);
         ok = ok && hipGetLastError() == hipSuccess;
       }
     }

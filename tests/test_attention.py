@@ -656,3 +656,22 @@ def test_gradients_of_large_dy_in_float16(ops, monkeypatch, T, H, Hk, d, cap, wh
         inside = want[name][0].abs() < 60000
         assert float(inside.double().mean()) > 0.9
         check(name, got[name][inside], tuple(t[inside] for t in want[name]))
+
+
+def test_results_of_more_words_than_a_join_counts(ops):
+    """2^20 tokens of 128 heads of 128 over 64 keys: nothing is split, so nothing is joined.  All queries and all dy of a head are the same memory, so all rows of the results are
+    the same bits; the first are those of a single token, up to the order of sums, of which the formula's errors hold."""
+    T, K, H, d = 1 << 20, 64, 128, 128
+    q, k, v, dy = inputs(7, 1, 1, K, H, H, d, torch.bfloat16)
+    want = formula(q, k, v, dy, causal=False)
+    many = [t.expand(1, T, H, d) for t in (q, dy)]
+    y, saved = ops.attention_forward(many[0], k, v, causal=False, save=True)
+    dq, dk, dv = ops.attention_backward(many[1], many[0], k, v, y, saved, causal=False)
+    for name, t in (("y", y), ("dq", dq)):
+        check(name, t[:, :1], want[name])
+        check(name, t[:, -1:], want[name])
+        for part in t[0].split(1 << 17):
+            assert torch.equal(part, t[0, :1].expand(len(part), -1, -1)), name
+    assert bool(torch.isfinite(dk).all()) and bool(torch.isfinite(dv).all())
+    del y, saved, dq, part, t
+    torch.cuda.empty_cache()

@@ -280,3 +280,27 @@ def test_every_row_of_a_load_is_within_reach():
             assert _kernels(a)[1]["packed"] == {"q_stride": 1, "k_stride": 2, "v_stride": 4}[name]
     a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, q_stride=(0, 256, (1 << 60) // 2))
     assert _kernels(a)[1]["packed"] == 1
+
+
+@pytest.mark.parametrize("kw", [dict(batch=1, tokens=1 << 20, keys=64, heads=128, kv_heads=128, dim=128), dict(batch=64, tokens=65536, keys=65536, heads=64, kv_heads=64, dim=128),
+                                dict(batch=1, tokens=64, keys=1 << 22, heads=64, kv_heads=64, dim=64)])
+def test_unsplit_calls_need_no_join(kw):
+    """results of more words than the join's threads can count are refused only where there is a join"""
+    a = _attention(**kw)
+    g = _gradients(a, at=BASE + (1 << 46))
+    rc, (saved, forward, backward) = _sizes(a, g)
+    assert rc == B.OK and saved > 0 and backward > 0
+    k = _kernels(a, g)[1]
+    words = [a.batch * n * h * (a.dim // 4) for n, h in ((a.tokens, a.heads), (a.keys, a.kv_heads))]
+    assert max(words) >= 1 << 32
+    for splits, n in ((k["forward_splits"], words[0]), (k["dkdv_splits"], words[1])):
+        assert splits == 1 or n < 1 << 32
+
+
+@pytest.mark.parametrize("batch,tokens", [(1 << 18, 1), (1 << 17, 1), (1 << 16, 32), (65535, 32)])
+def test_few_rows_of_very_many_heads_are_not_split(batch, tokens):
+    """where two parts of every head, or their join, would be more than a grid counts"""
+    a = _attention(batch=batch, tokens=tokens, keys=2048, heads=63, kv_heads=63, dim=128, causal=0)
+    rc, k = _kernels(a)
+    assert rc == B.OK and k["few"] == 1 and batch * 63 * k["forward_splits"] * 256 < 1 << 32
+    assert k["forward_splits"] == 1 or batch * 63 * tokens * 32 < 1 << 32

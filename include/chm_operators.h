@@ -133,7 +133,7 @@ typedef struct {
   float scale, cap;                           /* scale > 0, cap finite and >= 0, 0: none; scale and scale / cap up to 1e30 */
   const float *slopes;                        /* [heads], nullable */
   int32_t index_bits;                         /* of the documents: 32 or 64 (signed) */
-  const void *q_documents, *k_documents;      /* [batch, tokens], [batch, keys], rows of ld; both or neither */
+  const void *q_documents, *k_documents;      /* [batch, tokens], [batch, keys], rows of ld; both or neither (where there are queries and keys) */
   int64_t ld_q_documents, ld_k_documents;
   const uint8_t *prefix;                      /* [batch, keys], rows of ld_prefix, 0 or not; nullable; causal only */
   int64_t ld_prefix;

@@ -180,8 +180,11 @@ int64_t rows_pad(const chm_attention *a) { return up(a->tokens * group_of(a), AT
 // pass may name the same documents by other tensors)
 uint64_t lse_bytes(const chm_attention *a) { return (uint64_t)(a->batch * a->kv_heads * rows_pad(a)) * 4; }
 uint64_t low_bytes(const chm_attention *a) { return ((uint64_t)(a->batch * a->tokens * a->heads) * a->dim * 2 + 255) & ~255ull; }
+// Without queries or without keys there is nothing to mask, and a tensor of no elements has no address
+bool some_pairs(const chm_attention *a) { return a->batch > 0 && a->tokens > 0 && a->keys > 0; }
+bool has_words(const chm_attention *a) { return some_pairs(a) && (a->k_documents || a->prefix); }
 uint64_t documents_bytes(const chm_attention *a) {
-  if (!a->k_documents && !a->prefix) return 0;
+  if (!has_words(a)) return 0;
   const int64_t tiles = a->batch * (up(a->keys, ATTN_TILE) + up(a->tokens, ATTN_TILE));
   return (uint64_t)tiles * (ATTN_TILE * 4 + sizeof(AttnTile)) + 4 * 256;
 }
@@ -290,7 +293,7 @@ struct Pass {
     for (int i = 0; i < pack.count; ++i) packs += pack.m[i].groups;
     DocumentsCall kd{(const char *)a->k_documents, a->prefix, a->ld_k_documents, a->ld_prefix, nullptr, nullptr, c.keys, a->index_bits, c.tiles};
     DocumentsCall qd{(const char *)a->q_documents, nullptr, a->ld_q_documents, 0, nullptr, nullptr, c.tokens, a->index_bits, c.q_tile_count};
-    if (a->k_documents || a->prefix) {
+    if (has_words(a)) {
       Arena kept{a->saved ? (char *)a->saved + lse_bytes(a) + low_bytes(a) : nullptr};      // written by the forward pass, if there is one to come back to
       const bool keep = g || a->saved;
       Arena &from = keep ? kept : arena;
@@ -470,8 +473,8 @@ int check(const chm_attention *a) {
   if (!fine(a->q_stride, a->batch, a->tokens, a->heads) || !fine(a->k_stride, a->batch, a->keys, a->kv_heads) ||
       !fine(a->v_stride, a->batch, a->keys, a->kv_heads)) return CHM_ERR_ARG;
   if (!aligned(a->q, 2) || !aligned(a->k, 2) || !aligned(a->v, 2) || !aligned(a->saved, 16) || !aligned(a->slopes, 4)) return CHM_ERR_ARG;
-  if (!a->q_documents != !a->k_documents || (a->prefix && !a->causal)) return CHM_ERR_ARG;
-  if (a->k_documents) {
+  if ((some_pairs(a) && !a->q_documents != !a->k_documents) || (a->prefix && !a->causal)) return CHM_ERR_ARG;
+  if (a->q_documents || a->k_documents) {
     if (a->index_bits != 32 && a->index_bits != 64) return CHM_ERR_ARG;
     if (!aligned(a->q_documents, a->index_bits / 8) || !aligned(a->k_documents, a->index_bits / 8)) return CHM_ERR_ARG;
     if (a->batch > 1 && (a->ld_q_documents < 0 || a->ld_k_documents < 0)) return CHM_ERR_ARG;

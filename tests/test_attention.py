@@ -675,3 +675,14 @@ def test_results_of_more_words_than_a_join_counts(ops):
     assert bool(torch.isfinite(dk).all()) and bool(torch.isfinite(dv).all())
     del y, saved, dq, part, t
     torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("B,T,K", [(0, 5, 5), (2, 0, 0), (2, 0, 70), (2, 70, 0), (2, 3, 0), (0, 0, 9)])
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_documents_and_prefixes_of_lengths_of_zero(ops, B, T, K, index):
+    q, k, v, dy = inputs(1, B, T, K, 4, 2, 64, torch.bfloat16)
+    qid, kid = (torch.zeros((B, n), dtype=index, device="cuda") for n in (T, K))
+    for kw in (dict(documents=(qid, kid)), dict(documents=(qid, kid), causal=False), dict(prefix=kid.bool()), dict(documents=(qid, kid), prefix=kid.bool())):
+        got = both(ops, q, k, v, dy, **kw)
+        for name, like in zip(("y",) + NAMES, (q, q, k, v)):
+            assert got[name].shape == like.shape and not bool(got[name].any())

@@ -304,3 +304,21 @@ def test_few_rows_of_very_many_heads_are_not_split(batch, tokens):
     rc, k = _kernels(a)
     assert rc == B.OK and k["few"] == 1 and batch * 63 * k["forward_splits"] * 256 < 1 << 32
     assert k["forward_splits"] == 1 or batch * 63 * tokens * 32 < 1 << 32
+
+
+@pytest.mark.parametrize("bits", [32, 64])
+def test_documents_of_nothing(bits):
+    """a tensor of no elements has no address: documents are asked for where there are queries and keys"""
+    for kw in (dict(tokens=0), dict(keys=0), dict(tokens=0, keys=0), dict(batch=0)):
+        for q, k in ((0, BASE >> 1), (BASE >> 1, 0), (0, 0), (BASE >> 1, BASE >> 2)):
+            a = _attention(**kw, index_bits=bits, q_documents=q, k_documents=k, ld_q_documents=100, ld_k_documents=100, prefix=BASE >> 3, ld_prefix=100)
+            g = _gradients(a)
+            rc, (saved, forward, backward) = _sizes(a, g)
+            assert rc == B.OK and _kernels(a, g)[0] == B.OK
+            assert (saved, forward, backward) == tuple(_sizes(_attention(**kw), _gradients(_attention(**kw)))[1])       # nothing is kept of them
+            if a.batch == 0 or a.tokens == 0:
+                assert _forward(a, scratch=0, have=0) == B.OK
+            if a.batch == 0 or (a.tokens == 0 and a.keys == 0):
+                assert _backward(a, g, scratch=0, have=0) == B.OK
+    for q, k in ((0, BASE >> 1), (BASE >> 1, 0)):
+        assert _sizes(_attention(index_bits=bits, q_documents=q, k_documents=k, ld_q_documents=100, ld_k_documents=100))[0] == B.ERR_ARG

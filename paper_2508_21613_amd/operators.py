@@ -9,11 +9,14 @@ other (ffn_forward's may lie over x).  Wrong arguments raise binding.ChmError wi
 
 Results are no part of autograd's graph; the gradients are calls of their own.  While torch records gradients, inputs that require one are
 taken only where the caller asks for what the gradient's call wants (ffn_forward and attention_forward with save=True): anything else would lose it without a word.
+So would the backward calls' gradients with respect to their dy: those of attention and the rotary positions refuse one that requires a gradient.  Inputs
+with tangents of torch.autograd.forward_ad are refused.
 """
 import ctypes as C
 import math
 
 import torch
+from torch.autograd import forward_ad
 
 from . import binding as B
 
@@ -95,10 +98,13 @@ def _scope(stream, device, *tensors):
     return _Other(stream, device, tensors)
 
 
-def _unrecorded(*tensors):
-    if any([t.requires_grad for t in tensors]) and torch.is_grad_enabled():
+def _unrecorded(*tensors, kept=False):
+    """refuses inputs whose derivatives would be lost; kept: the caller has what the gradient's call wants"""
+    if not kept and any([t.requires_grad for t in tensors]) and torch.is_grad_enabled():
         raise B.ChmError(B.ERR_ARG, "the result would carry no gradient to inputs that require one: call under torch.no_grad() and take the "
                                     "gradients from ffn_backward, embedding_gradient, Rotary.gradient and attention_backward")
+    if forward_ad._current_level >= 0 and any([forward_ad.unpack_dual(t).tangent is not None for t in tensors]):
+        raise B.ChmError(B.ERR_ARG, "the result would carry no tangent: there are no derivatives in forward mode")
 
 
 def _bytes(n, like):
@@ -127,8 +133,7 @@ def ffn_forward(x, w_gate, w_up, w_down, activation="silu", save=False, out=None
     save=True returns (y, saved), `saved` being what ffn_backward wants (opaque; 6 bytes per token and feature)."""
     d, T, D, F, dtype, dev = _ffn(x, w_gate, w_up, w_down, activation)
     ld_y = D if out is None else _matrix("out", out, T, D, dtype, dev)
-    if not save:
-        _unrecorded(x, w_gate, w_up, w_down)
+    _unrecorded(x, w_gate, w_up, w_down, kept=save)
     lib = B.lib()
     with _scope(stream, dev, x, w_gate, w_up, w_down, out) as st:
         need, scratch = C.c_uint64(), C.c_uint64()
@@ -161,6 +166,7 @@ def ffn_backward(dy, x, w_gate, w_up, w_down, saved, activation="silu", grads=No
         _need(dtype in (x_dtype, torch.float32), "grads must be of the weights' type or float32")
         lds = (_matrix("grads[0]", grads[0], F, D, dtype, dev), _matrix("grads[1]", grads[1], F, D, dtype, dev),
                _matrix("grads[2]", grads[2], D, F, dtype, dev))
+    _unrecorded(dy, x, w_gate, w_up, w_down, kept=True)
     lib = B.lib()
     with _scope(stream, dev, dy, x, w_gate, w_up, w_down, saved, out, *(grads or ())) as st:
         if out is None:
@@ -221,6 +227,7 @@ def embedding_gradient(dy, tokens, rows=None, scale=1.0, out=None, accumulate=Fa
         ld_out = _matrix("out", out, rows, width, None, dev)
         rows, grad_dtype = out.shape[0], out.dtype
         _need(grad_dtype in (dtype, torch.float32), "out must be of dy's type or float32")
+    _unrecorded(dy, kept=True)
     lib = B.lib()
     with _scope(stream, dev, dy, tokens, out) as st:
         if out is None:
@@ -375,8 +382,7 @@ def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, do
     d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
     if out is not None:
         _strided("out", out, q.shape, q.dtype, dev)
-    if not save:
-        _unrecorded(q, k, v)
+    _unrecorded(q, k, v, kept=save)
     lib = B.lib()
     with _scope(stream, dev, out, *held) as st:
         need, scratch = C.c_uint64(), C.c_uint64()
@@ -406,6 +412,8 @@ def attention_backward(dy, q, k, v, y, saved, scale=None, cap=0.0, slopes=None, 
         _need(len(out) == 3, "out must be three tensors")
         for name, t, like in zip(("out[0]", "out[1]", "out[2]"), out, (q, k, v)):
             _strided(name, t, like.shape, q.dtype, dev)
+    _unrecorded(dy)
+    _unrecorded(q, k, v, y, kept=True)
     lib = B.lib()
     with _scope(stream, dev, dy, y, saved, *held, *(out or ())) as st:
         if out is None:
@@ -444,6 +452,7 @@ class Gradients:
         out = None if out is None else list(out)
         _need(out is None or len(out) == len(grads), "out must have a tensor for each gradient")
         _need(all(isinstance(t, torch.Tensor) for t in grads), "gradients must be tensors")
+        _unrecorded(*grads, kept=True)
         self.device = grads[0].device if grads else torch.device("cuda", torch.cuda.current_device())
         items = (B.Gradient * max(len(grads), 1))()
         for i, t in enumerate(grads):

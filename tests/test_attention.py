@@ -686,3 +686,53 @@ def test_documents_and_prefixes_of_lengths_of_zero(ops, B, T, K, index):
         got = both(ops, q, k, v, dy, **kw)
         for name, like in zip(("y",) + NAMES, (q, q, k, v)):
             assert got[name].shape == like.shape and not bool(got[name].any())
+
+
+def test_gradients_that_would_be_lost(ops):
+    """the backward pass is no part of autograd's graph either: a dy that carries one is refused; inputs and results that are leaves of the caller's are not"""
+    from paper_2508_21613_amd.binding import ChmError
+    q, k, v, dy = inputs(1, 1, 20, 20, 2, 2, 64, torch.bfloat16)
+    want = both(ops, q, k, v, dy)
+    y, saved = ops.attention_forward(q, k, v, save=True)
+    for t in (q, k, v, y):
+        t.requires_grad_(True)
+    w = torch.ones((), device="cuda", requires_grad=True)
+    with pytest.raises(ChmError):
+        ops.attention_backward(dy * w.bfloat16(), q, k, v, y, saved)
+    (y.float() * dy.float()).sum().backward()                   # y as the leaf of what follows
+    got = ops.attention_backward(y.grad, q, k, v, y, saved)
+    assert all(torch.equal(g, want[n]) for n, g in zip(NAMES, got))
+    with torch.no_grad():
+        got = ops.attention_backward(dy * w.bfloat16(), q, k, v, y, saved)
+    assert all(torch.equal(g, want[n]) for n, g in zip(NAMES, got))
+
+
+def test_tangents_are_refused(ops):
+    """derivatives in forward mode have no call: they would come out as none, also where nothing is recorded"""
+    import torch.autograd.forward_ad as forward_ad
+    from paper_2508_21613_amd.binding import ChmError
+    q, k, v, dy = inputs(1, 1, 20, 20, 2, 2, 64, torch.bfloat16)
+    y, saved = ops.attention_forward(q, k, v, save=True)
+    rope, pos = ops.Rotary(64), torch.arange(20, device="cuda")
+    w = torch.randn((3, 96, 40), device="cuda").bfloat16()
+    x, table = torch.randn((7, 40), device="cuda").bfloat16(), torch.randn((9, 40), device="cuda")
+    kept = ops.ffn_forward(x, w[0], w[1], w[2].T.contiguous(), save=True)[1]
+    calls = {"attention_forward": (lambda *t: ops.attention_forward(*t), (q, k, v)),
+             "attention_forward, save": (lambda *t: ops.attention_forward(*t, save=True), (q, k, v)),
+             "attention_backward": (lambda *t: ops.attention_backward(t[0], *t[1:5], saved), (dy, q, k, v, y)),
+             "rotate": (lambda t: rope.rotate(t, pos), (q[0],)), "gradient": (lambda t: rope.gradient(t, pos), (dy[0],)),
+             "ffn_forward": (lambda *t: ops.ffn_forward(*t), (x, w[0], w[1], w[2].T.contiguous())),
+             "ffn_forward, save": (lambda *t: ops.ffn_forward(*t, save=True), (x, w[0], w[1], w[2].T.contiguous())),
+             "embedding_lookup": (lambda t: ops.embedding_lookup(pos[:5], t), (table,)),
+             "embedding_gradient": (lambda t: ops.embedding_gradient(t, pos[:9], rows=20), (table,)),
+             "ffn_backward": (lambda *t: ops.ffn_backward(*t, kept), (x, x, w[0], w[1], w[2].T.contiguous())),
+             "Gradients": (lambda *t: ops.Gradients(t).close(), (table, x))}
+    for name, (call, args) in calls.items():
+        call(*args)
+        with forward_ad.dual_level():
+            call(*args)
+            for i in range(len(args)):
+                for recorded in (True, False):
+                    with torch.set_grad_enabled(recorded), pytest.raises(ChmError):
+                        call(*[forward_ad.make_dual(t, torch.ones_like(t)) if i == j else t for j, t in enumerate(args)])
+        call(*args)

@@ -322,3 +322,27 @@ def test_documents_of_nothing(bits):
                 assert _backward(a, g, scratch=0, have=0) == B.OK
     for q, k in ((0, BASE >> 1), (BASE >> 1, 0)):
         assert _sizes(_attention(index_bits=bits, q_documents=q, k_documents=k, ld_q_documents=100, ld_k_documents=100))[0] == B.ERR_ARG
+
+
+def test_what_carries_a_derivative_is_told():
+    import torch
+    import torch.autograd.forward_ad as forward_ad
+    from paper_2508_21613_amd import operators as ops
+    a, w = torch.ones(3), torch.ones(3, requires_grad=True)
+    ops._unrecorded(a, a)
+    for t in (w, w * 2):
+        with pytest.raises(B.ChmError):
+            ops._unrecorded(a, t)
+        ops._unrecorded(a, t, kept=True)
+        with torch.no_grad():
+            ops._unrecorded(a, t)
+    with forward_ad.dual_level():
+        ops._unrecorded(a)
+        dual = forward_ad.make_dual(a, torch.ones(3))
+        for t in (dual, dual.view(1, 3), dual * 2):
+            for kept in (False, True):
+                with pytest.raises(B.ChmError):
+                    ops._unrecorded(a, t, kept=kept)
+                with torch.no_grad(), pytest.raises(B.ChmError):
+                    ops._unrecorded(a, t, kept=kept)
+    ops._unrecorded(a)

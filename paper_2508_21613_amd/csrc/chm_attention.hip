@@ -454,13 +454,8 @@ struct Pass {
 };
 
 bool aligned(const void *p, int64_t to) { return (uintptr_t)p % to == 0; }
-// strides that are no negative ones and whose ends can be counted in bytes
-bool fine(const int64_t s[3], int64_t b, int64_t t, int64_t h) {
-  const int64_t n[3] = {b, t, h};
-  for (int i = 0; i < 3; ++i)
-    if (s[i] < 0 || (n[i] > 1 && s[i] > (1ll << 60) / n[i])) return false;
-  return true;
-}
+using chm_strided::countable;
+bool fine(const int64_t s[3], int64_t b, int64_t t, int64_t h) { return countable(s[0], b) && countable(s[1], t) && countable(s[2], h); }
 
 int check(const chm_attention *a) {
   if (!a || (a->dtype != CHM_BF16 && a->dtype != CHM_F16)) return CHM_ERR_ARG;
@@ -477,9 +472,9 @@ int check(const chm_attention *a) {
   if (a->q_documents || a->k_documents) {
     if (a->index_bits != 32 && a->index_bits != 64) return CHM_ERR_ARG;
     if (!aligned(a->q_documents, a->index_bits / 8) || !aligned(a->k_documents, a->index_bits / 8)) return CHM_ERR_ARG;
-    if (a->batch > 1 && (a->ld_q_documents < 0 || a->ld_k_documents < 0)) return CHM_ERR_ARG;
+    if (a->batch > 1 && (!countable(a->ld_q_documents, a->batch) || !countable(a->ld_k_documents, a->batch))) return CHM_ERR_ARG;
   }
-  if (a->prefix && a->batch > 1 && a->ld_prefix < 0) return CHM_ERR_ARG;
+  if (a->prefix && a->batch > 1 && !countable(a->ld_prefix, a->batch)) return CHM_ERR_ARG;
   return CHM_OK;
 }
 

@@ -145,7 +145,9 @@ extern "C" int chm_rotary_turn(const chm_rotary *r, int32_t backwards, void *hip
   if (r->pairs < 1 || r->pairs > PAIRS || r->head_dim < 2 * r->pairs || r->head_dim > (1 << 20) || !r->frequencies) return CHM_ERR_ARG;
   const int size = r->dtype == CHM_F32 ? 4 : 2;
   if (((uintptr_t)r->x | (uintptr_t)r->out) % size || (uintptr_t)r->positions % (r->index_bits / 8)) return CHM_ERR_ARG;
-  if (r->x_token < 0 || r->x_head < 0 || r->out_token < 0 || r->out_head < 0 || r->positions_axis < 0 || r->positions_token < 0) return CHM_ERR_ARG;
+  using chm_strided::countable;
+  if (!countable(r->x_token, r->tokens) || !countable(r->x_head, r->heads) || !countable(r->out_token, r->tokens) || !countable(r->out_head, r->heads) ||
+      !countable(r->positions_axis, r->axes) || !countable(r->positions_token, r->tokens)) return CHM_ERR_ARG;
   RotaryCall c{};
   for (int i = 0; i < r->pairs; ++i) {
     const int32_t a = r->axis ? r->axis[i] : 0;
@@ -168,9 +170,10 @@ extern "C" int chm_rotary_turn(const chm_rotary *r, int32_t backwards, void *hip
   c.x = (const char *)r->x;
   c.out = (char *)r->out;
   c.positions = (const char *)r->positions;
-  c.x_token = r->x_token * size; c.x_head = r->x_head * size;
-  c.out_token = r->out_token * size; c.out_head = r->out_head * size;
-  c.p_axis = r->positions_axis; c.p_token = r->positions_token;
+  const auto step = [](int64_t stride, int64_t n) { return n < 2 ? 0 : stride; };
+  c.x_token = step(r->x_token, r->tokens) * size; c.x_head = step(r->x_head, r->heads) * size;
+  c.out_token = step(r->out_token, r->tokens) * size; c.out_head = step(r->out_head, r->heads) * size;
+  c.p_axis = step(r->positions_axis, r->axes); c.p_token = step(r->positions_token, r->tokens);
   c.tokens = r->tokens;
   c.heads = (int32_t)r->heads; c.head_dim = r->head_dim; c.pairs = r->pairs; c.index_bits = r->index_bits;
   c.turned = (int32_t)(r->pairing == CHM_PAIRS_NEIGHBOURS ? up(2 * r->pairs, n) : up(r->pairs, n));

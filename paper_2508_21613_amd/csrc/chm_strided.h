@@ -9,6 +9,9 @@ namespace chm_strided {
 
 struct Dim { int64_t n, stride; };
 
+// whether n elements `stride` elements apart (up to 8 bytes each) end within what 64 bits count of bytes
+inline bool countable(int64_t stride, int64_t n) { return stride >= 0 && (n < 2 || stride <= (1ll << 58) / n); }
+
 // `outer` times (a multiple of `step` bytes apart) some rows
 struct Block { const void *p; int64_t outer, step; chm_overlap::Rows rows; };
 
@@ -23,7 +26,7 @@ struct Tensor {
   Tensor(const void *p_, int64_t width, int size, const Dim (&d)[3]) : p(p_), run(width * size), dims(0), empty(width < 1), repeats(false) {
     for (const Dim &x : d) {
       if (x.n < 1) empty = true;
-      if (x.n < 2) continue;
+      if (x.n < 2) continue;               // its stride says nothing
       if (x.stride == 0) { repeats = true; continue; }
       int at = dims++;
       for (; at > 0 && dim[at - 1].stride > x.stride * size; --at) dim[at] = dim[at - 1];

@@ -274,11 +274,11 @@ def test_every_row_of_a_load_is_within_reach():
     a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, k_stride=(0, 17000000, 128))
     assert _kernels(a, _gradients(a))[1]["packed"] == 0
     # strides of which no 64 can be counted
-    for stride in (1 << 30, 1 << 31, 1 << 40, (1 << 60) // 200):
+    for stride in (1 << 30, 1 << 31, 1 << 40, (1 << 58) // 200):
         for name in ("q_stride", "k_stride", "v_stride"):
             a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, **{name: (0, stride, 128)})
             assert _kernels(a)[1]["packed"] == {"q_stride": 1, "k_stride": 2, "v_stride": 4}[name]
-    a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, q_stride=(0, 256, (1 << 60) // 2))
+    a = _attention(batch=1, tokens=200, keys=200, heads=2, kv_heads=1, dim=128, q_stride=(0, 256, (1 << 58) // 2))
     assert _kernels(a)[1]["packed"] == 1
 
 
@@ -346,3 +346,21 @@ def test_what_carries_a_derivative_is_told():
                 with torch.no_grad(), pytest.raises(B.ChmError):
                     ops._unrecorded(a, t, kept=kept)
     ops._unrecorded(a)
+
+
+@pytest.mark.parametrize("far", [1 << 62, (1 << 63) - 8, 1 << 60])
+def test_strides_beyond_what_bytes_can_count(far):
+    """their ends wrap in 64 bits: refused, not compared with other tensors' places"""
+    for name in ("x_token", "x_head", "out_token", "out_head", "positions_axis", "positions_token"):
+        r, keep = _rotary(dtype=0, axes=2, **{name: far})
+        assert B.lib().chm_rotary_turn(r, 0, None) == B.ERR_ARG, name
+    docs = dict(index_bits=64, q_documents=BASE >> 1, k_documents=BASE >> 2, ld_q_documents=100, ld_k_documents=100, prefix=BASE >> 3, ld_prefix=100)
+    assert _sizes(_attention(**docs))[0] == B.OK
+    for name in ("ld_q_documents", "ld_k_documents", "ld_prefix"):
+        assert _sizes(_attention(**dict(docs, **{name: far})))[0] == B.ERR_ARG, name
+        one = _attention(batch=1, **dict(docs, **{name: far}))               # says nothing there
+        assert _sizes(one)[0] == B.OK
+        assert _forward(one, scratch=0) == B.ERR_ARG
+    for nothing in (dict(tokens=1, x_token=far, out_token=far, positions_token=far), dict(heads=1, x_head=far, out_head=far)):
+        r, keep = _rotary(**nothing, x=0)                                   # nor of a single token or head: refused for x
+        assert B.lib().chm_rotary_turn(r, 0, None) == B.ERR_ARG

@@ -63,7 +63,7 @@ typedef struct {
 int chm_ffn_selection(const chm_ffn *f, const chm_ffn_gradients *g, chm_ffn_kernels *out);
 
 /* Which kernels attention's passes over these tensors run on.  Host only; the decision the calls take; results do not depend on it but for the
- * order of float32 sums.  Errors: CHM_ERR_ARG. */
+ * order of float32 sums and, where `fine` is set, the roundings that the gradients' products then keep.  Errors: CHM_ERR_ARG. */
 typedef struct {
   int32_t few;                   /* 1: forward on the kernel for few rows */
   int32_t dim;                   /* elements of a row that the kernels are made for: 64 or 128 */

@@ -116,8 +116,9 @@ int chm_rotary_turn(const chm_rotary *r, int32_t backwards, void *hip_stream);
  * Query i stands at position i + keys - tokens (new tokens behind those whose keys are there).  Visible are the keys j
  *   - of its own document (documents: a number a token; outside [0, 2^31 - 1) it stands for none, such a token sees nothing and is seen by nobody),
  *   - causal: up to its own position, and wherever prefix[j] is set (a prompt that all of its document sees).
- * A query that sees nothing has a result of zeros and no gradient.  Queries, keys and values of tokens of no document may hold anything; a
- * value that is not finite at a key which some queries see may reach the results of others of the same sequence.
+ * A query that sees nothing has a result of zeros and no gradient.  Queries, keys, values and dy of tokens of no document may hold anything; a
+ * value that is not finite at a key which some queries see may reach the results of others of the same sequence, and so may a query or dy that is not
+ * finite, of a token that has a document, the gradients of keys that it does not see.
  * Gradients, of a scalar of which dy is the gradient with respect to y:
  *   ds = p (dy.v - dy.y);  dq = scale sum_j ds z' k;  dk = scale sum_i ds z' q;  dv = sum_i p dy    (sums over the group's heads)
  * p and ds are worked out in float32 and rounded to the tensors' type once, where they enter a product (in small calls the gradients' products also

@@ -40,7 +40,6 @@ struct RotaryCall {
   int32_t tokens_each, heads_each, head_groups;        // of a workgroup; groups of heads
   int32_t turned, chunks;                              // pieces of a head that are turned, and all
   Divide by_pairs, by_chunks, by_heads;
-  int32_t copies;                                      // elements behind the pairs have to be copied
   float sign;
   double turns[PAIRS];                                 // frequency / 2 pi
   uint8_t axis[PAIRS];

@@ -12,10 +12,11 @@
 // Keys and values (queries and dy for dk and dv) go to shared memory by direct loads, 64 (32) rows at a time, two such steps deep; 16-byte chunks
 // of a row are stored at chunk ^ swizzle(row), which spreads both the reads of rows and the transposing reads over the banks.
 //
-// Long calls are bound by the matrix cores and exponentials at the clock that the power limit leaves (1.6 to 1.9 GHz): two wavefronts a SIMD, each of whose
-// steps is 1,024 cycles of matrix instructions, as many of other ones and 32 KB (forward) from shared memory.  8,192 tokens, 32 heads of 128, 8 of
-// keys, bfloat16, causal, capped: forward 740 us (0.74 PFLOP/s of the 4 d operations a pair), dq 990 (0.83 of 6 d), dk and dv 1,380 (0.80 of 8 d); without
-// the cap 615, 835, 1,225 (0.89, 0.99, 0.90).
+// Two wavefronts a SIMD, each of whose steps is 1,024 cycles of matrix instructions, as many of other ones and 32 KB (forward) from shared memory.  In long calls little
+// of one's work runs beside the other's: matrix core and vector unit are busy for 39 and 66% of the time in the forward pass, 44 and 60% in dq, 42 and 46% in dk and dv (shared memory 20 to 32%), without
+// a cap for 50 and 47, 59 and 41, 49 and 29%, at 1.8 to 2.1 GHz of 2.4.  8,192 tokens, 32 heads of 128, 8 of keys, bfloat16, causal, capped, call after call: forward
+// 650 us (0.85 PFLOP/s of the 4 d operations a pair), dq 885 (0.93 of 6 d), dk and dv 1,225 (0.90 of 8 d); without the cap 547, 735, 1,058 (1.00, 1.12, 1.04).  The first calls
+// after a pause take up to a fifth longer.
 //
 // Tiles that nobody sees are not visited: each lane looks at one tile of 64 keys (of documents: least and largest number, prefix or not), and the
 // ballot is the list of those to visit, and of those whose every pair is seen, where nothing is masked.
@@ -124,10 +125,10 @@ __device__ __forceinline__ Place place_of(const AttnCall &c, int i, bool last_fi
 }
 
 // ---------------------------------------------------------------------------------------------- shared memory
-// Rows of D elements (64, or up to 128 in rows of 128), as direct loads leave them: 1 KiB of whole rows by each.  The banks give 256 bytes a cycle: 16 lanes of
-// a read of rows, one chunk of 16 rows each, or 32 lanes of a transposing read, 4 chunks of 4 rows.  The chunks of a row are exchanged in fours by
+// Rows of D elements (64, or up to 128 in rows of 128), as direct loads leave them: 1 KiB of whole rows by each.  Laid out for 64 banks of 4 bytes: 16 lanes of
+// a read of rows, one chunk of 16 rows each, or 32 lanes of a transposing read, 4 chunks of 4 rows, go to all of them once.  The chunks of a row are exchanged in fours by
 // the row's last two bits, and 16 bytes between the loads do the rest: so most of a read's address is a constant.  With 8 chunks a row, where two rows
-// fill the banks, they are exchanged by three bits of the row.
+// fill the banks, they are exchanged by three bits of the row.  Measured in long calls: conflicts are 0.3 to 0.7% of shared memory's busy cycles.
 template <int D> struct Shape {
   enum { PITCH = D == 64 ? 128 : 256, CHUNKS = PITCH / 16, GROUP = 1024 / PITCH, GROUP_BYTES = 1024 + (D == 64 ? 0 : 16) };
   static __device__ __forceinline__ uint32_t swizzle(uint32_t row) {

@@ -378,7 +378,8 @@ def attention_forward(q, k, v, scale=None, cap=0.0, slopes=None, causal=True, do
 
     Query i stands at position i + keys - tokens.  It sees the keys of its document (documents: whole numbers [batch, tokens], or a pair of them for
     queries and keys; outside [0, 2^31 - 1) they stand for none) and, if causal, those up to its own position and those that prefix
-    (bool [batch, keys]) names.  One that sees nothing gets zeros.  With save=True returns (y, saved), `saved` being what attention_backward wants."""
+    (bool [batch, keys]) names.  One that sees nothing gets zeros.  With save=True returns (y, saved), `saved` being what attention_backward wants
+    (opaque; 2 bytes per element of y, 4 per row, with documents or a prefix some 5 per token and key)."""
     d, dev, held = _attention(q, k, v, scale, cap, slopes, causal, documents, prefix)
     if out is not None:
         _strided("out", out, q.shape, q.dtype, dev)

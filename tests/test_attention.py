@@ -736,3 +736,46 @@ def test_tangents_are_refused(ops):
                     with torch.set_grad_enabled(recorded), pytest.raises(ChmError):
                         call(*[forward_ad.make_dual(t, torch.ones_like(t)) if i == j else t for j, t in enumerate(args)])
         call(*args)
+
+
+@pytest.mark.parametrize("T,d", [(20, 128), (300, 64), (900, 128)])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_places_of_no_document_say_nothing_of_float16s_range(ops, monkeypatch, T, d, value):
+    """what is taken from ds's lift goes by the pairs that are seen: the same gradients, bit by bit, as with zeros in the places of no document, for a dy that passes the range as for
+    one that does not"""
+    ids = documents_of(T, 2, T, 2, T // 3)
+    ids[1, 3:9] = -1
+    for std in (0.01, 3000.0):
+        x = inputs(T, 2, T, T, 4, 2, d, torch.float16)
+        x[3].mul_(std / 0.3)
+        got = []
+        for fill in (0.0, value):
+            for t in x:
+                t[ids < 0] = fill
+            for causal in (True, False):
+                got.append(both(ops, *x, documents=ids, causal=causal, scale=0.001))
+        for want, other in zip(got[:2], got[2:]):
+            for name in want:
+                assert bool(torch.isfinite(other[name]).all()) or (std > 1000 and name == "dv")
+                assert torch.equal(want[name].nan_to_num(7.0), other[name].nan_to_num(7.0)), name
+
+
+def test_float16_captured_with_other_ranges(ops):
+    """a captured backward pass takes as much of the lift as the dy at hand wants, at every replay"""
+    x = inputs(11, 1, 400, 400, 4, 2, 128, torch.float16)
+    dy = x[3].clone()
+    y, saved = ops.attention_forward(*x[:3], save=True, scale=0.001)
+    stream = torch.cuda.Stream()
+    stream.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(stream):
+        ops.attention_backward(dy, *x[:3], y, saved, scale=0.001)
+    torch.cuda.current_stream().wait_stream(stream)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = ops.attention_backward(dy, *x[:3], y, saved, scale=0.001)
+    for factor in (1.0, 1e4, 1e-3, 3e3, 1.0):
+        dy.copy_(x[3] * factor)
+        graph.replay()
+        want = ops.attention_backward(dy, *x[:3], y, saved, scale=0.001)
+        torch.cuda.synchronize()
+        assert all(torch.equal(g, w) for g, w in zip(got, want)) and bool(torch.isfinite(got[0]).all())
